@@ -440,6 +440,113 @@ int ps_verify_batch(ps_ctx* ctx, const ps_verify_shape* shape /* host */, const 
                     uint64_t n, const double* d_data, uint64_t data_len, ps_verify_result* d_out,
                     double* d_theta_out);
 
+/* ------------------------------------------------------------------ operators of a training step */
+/* The operators behind three of the terms that the space prices -- the V*H elements
+ * of the embedding, the dropout masks of 34*S*b*H and the attention matrices of
+ * 5*a*S^2*b -- in the form that the paper's reasoning asks for.  State that mode M
+ * (Definition 1) reconstructs is never stored: a dropout mask comes out of a counter,
+ * attention's probabilities out of a log-sum-exp.  And a shard computes the bits that
+ * a single device computes (Definition 4): a mask depends on an element's index in the whole
+ * tensor, a row's gradient is summed in the order of its tokens, and nothing depends
+ * on the order in which blocks run.  So ps_verify_batch's protocol can be followed
+ * on them.
+ *
+ * All data pointers are device pointers; strides count elements.  Outputs must not
+ * overlap inputs or one another except where said.  Elements are float (PS_F32),
+ * bfloat16 (PS_BF16) or IEEE half (PS_F16); arithmetic is in 32 bits and a result is
+ * rounded once, to nearest even, except for the two matrices that attention multiplies
+ * in its operands' type (see there). */
+enum { PS_F32 = 0, PS_BF16 = 1, PS_F16 = 2 };
+
+/* Dropout, with an optional residual:
+ *   y[r][c] = (word(first + r * pitch + c) >= threshold ? x[r][c] / (1 - p) : 0) + residual[r][c]
+ * with threshold = round(p * 2^32) and word(g) the word g mod 4 of Philox4x32-10 at the
+ * counter (g / 4, stream) under the key `seed`.  The gradient of x is the same call on
+ * the gradient of y, without a residual.  A dropped element's value is not looked at
+ * (it may be NaN).  p = 1 drops everything.  A shard that starts at element `first` of
+ * a tensor whose rows are `pitch` elements long draws the whole tensor's mask: rows of
+ * a data axis shift `first` by rows, columns of a tensor axis by columns.  y may be x
+ * or residual itself (same pointer and stride). */
+typedef struct {
+  uint64_t rows, cols;             /* either may be 0; rows * cols <= 2^48                */
+  uint64_t x_stride, residual_stride, y_stride; /* between rows; y_stride >= cols         */
+  uint64_t seed, stream;           /* say, of the run, and of the step and layer          */
+  uint64_t first, pitch;           /* first + rows * pitch + cols <= 2^63                 */
+  double p;                        /* 0 .. 1                                              */
+  uint32_t dtype, pad;             /* of x, residual and y                                */
+} ps_dropout_desc;
+int ps_dropout(ps_ctx* ctx, const ps_dropout_desc* desc, const void* d_x, const void* d_residual /* may be null */,
+               void* d_y);
+
+/* Embedding lookup:  out[t] = scale * table[token[t] - first_row], zeros where the table
+ * does not hold that row (first_row <= token < first_row + rows is held): padding, or
+ * the rows of another shard.
+ * Its gradient:  d_table[v] = scale * sum of d_out[t] over the t that look up row v, t
+ * ascending and in 32 bits (long lists in a fixed tree of parts); every row is
+ * written.  With accumulate, the sum is added to d_table (rounded once) and rows
+ * without tokens are left alone.  The gradient has the same bits on every run.
+ * d_work of ps_embed_backward: ps_embed_backward_bytes bytes, 256-byte aligned, in use
+ * until the call's work is done; it needs no initial value and may be used again for the
+ * next call on the same stream. */
+typedef struct {
+  uint64_t tokens;                 /* 0 .. 2^30                                           */
+  uint64_t first_row, rows;        /* rows 1 .. 2^30                                      */
+  uint64_t dim;                    /* 1 .. 2^20                                           */
+  uint64_t table_stride, out_stride; /* between rows, >= dim                              */
+  double scale;
+  uint32_t dtype;                  /* of table and out; backward: of d_out                */
+  uint32_t grad_dtype;             /* backward: of d_table                                */
+  uint32_t token_bytes;            /* tokens are int32_t (4) or int64_t (8)               */
+  uint32_t accumulate;             /* backward: 0 or 1                                    */
+} ps_embed_desc;
+int ps_embed_forward(ps_ctx* ctx, const ps_embed_desc* desc, const void* d_table, const void* d_tokens, void* d_out);
+uint64_t ps_embed_backward_bytes(const ps_embed_desc* desc);
+int ps_embed_backward(ps_ctx* ctx, const ps_embed_desc* desc, const void* d_out_grad, const void* d_tokens,
+                      void* d_table_grad, void* d_work, uint64_t work_bytes);
+
+/* Attention over whole sequences, heads of queries sharing heads of keys and values:
+ *   S = scale * Q K^T;  lse_i = log sum_j exp(S_ij);  out = exp(S - lse) V
+ * and its gradients, which recompute exp(S - lse) block by block instead of keeping it:
+ *   delta_i = sum_d d_out_id out_id;  dS = exp(S - lse) o (d_out V^T - delta)
+ *   d_q = scale * dS K;  d_k = scale * dS^T Q;  d_v = exp(S - lse)^T d_out
+ * with d_k and d_v summed over the query heads of a key head.
+ *
+ * Sequence b has n = q_lens[b] queries and m = k_lens[b] keys (null: q_len and k_len;
+ * values are clamped to 0 .. q_len and 0 .. k_len).  Query i sees the keys j < m, under the causal mask
+ * those with j <= i + m - n (the last query sees all keys).  A query that sees no key
+ * has out = 0, lse = -infinity and no gradient.  Queries behind n and keys behind m are
+ * padding: whatever they hold (NaN as well) is not used, and zeros are written for them (lse: -infinity).
+ * A key that the causal mask alone hides from a query is multiplied by a probability of
+ * 0 where it shares a block with keys that are seen: its values have to be finite.
+ *
+ * exp(S - lse) and dS are rounded to the operands' type before they are multiplied;
+ * everything else is in 32 bits.  Results have the same bits on every run, and a
+ * sequence's and a key head's do not depend on the others in the call.
+ * d_lse is [batch][heads][q_len].  d_work: ps_attention_backward_bytes bytes, 256-byte
+ * aligned, used like ps_embed_backward's. */
+typedef struct {
+  void* data;                      /* 16-byte aligned                                     */
+  uint64_t batch_stride, token_stride, head_stride; /* multiples of 8, not 0 where that extent is above 1; dim is contiguous */
+} ps_heads;
+typedef struct {
+  uint32_t batch;                  /* 0 .. 2^16 - 1                                       */
+  uint32_t q_len, k_len;           /* 0 .. 2^24                                           */
+  uint32_t heads, kv_heads;        /* 1 .. 2^15, heads a multiple of kv_heads             */
+  uint32_t dim;                    /* 8 .. 128, a multiple of 8                           */
+  uint32_t dtype;                  /* PS_BF16 or PS_F16, of all of them                   */
+  uint32_t causal;                 /* 0 or 1                                              */
+  float scale;                     /* finite                                              */
+  uint32_t pad;
+} ps_attention_shape;
+int ps_attention_forward(ps_ctx* ctx, const ps_attention_shape* shape, const ps_heads* q, const ps_heads* k,
+                         const ps_heads* v, const ps_heads* out, float* d_lse, const int32_t* d_q_lens,
+                         const int32_t* d_k_lens);
+uint64_t ps_attention_backward_bytes(const ps_attention_shape* shape);
+int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps_heads* q, const ps_heads* k,
+                          const ps_heads* v, const ps_heads* out, const float* d_lse, const ps_heads* d_out,
+                          const ps_heads* d_q, const ps_heads* d_k, const ps_heads* d_v, const int32_t* d_q_lens,
+                          const int32_t* d_k_lens, void* d_work, uint64_t work_bytes);
+
 /* ------------------------------------------------------------------ measurement */
 /* Integer-pipe microbenchmark: `blocks` x 256 threads each run `iters` rounds
  * of 8 independent 32-bit add/logic chains of 16 operations.  Returns through

@@ -2,11 +2,13 @@
 // factorisations, scratch management and kernel launches.  No arithmetic of the
 // method happens on the host; every evaluation runs in the kernels.
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdlib.h>
 #include <string.h>
 #include <algorithm>
 #include <atomic>
 #include <chrono>
+#include <cmath>
 #include <new>
 #include <vector>
 
@@ -103,6 +105,18 @@ u32 reported(const ps_ctx* ctx) {
 // a problem that a kernel has reported by now
 int pending_device_error(ps_ctx* ctx) {
   return reported(ctx) & ~(u32)ST_TRUNCATED ? PS_E_DEVICE : PS_OK;     // a truncated frontier blocks nothing
+}
+
+// Whether writing rows of `cols` elements at y (y_stride apart) may change what is still to be read of the
+// rows at x: they share memory, and not as the very same elements, nor as column ranges of the same rows.
+bool overwrites(const void* y, u64 y_stride, const void* x, u64 x_stride, u64 rows, u64 cols, u64 width) {
+  if (y == x && (rows == 1 || y_stride == x_stride)) return false;
+  const u64 ya = (u64)(uintptr_t)y, xa = (u64)(uintptr_t)x;
+  const u64 y_end = ya + ((rows - 1) * y_stride + cols) * width, x_end = xa + ((rows - 1) * x_stride + cols) * width;
+  if (y_end <= xa || x_end <= ya) return false;
+  if (y_stride != x_stride) return true;
+  const u64 pitch = y_stride * width, off = (ya > xa ? ya - xa : xa - ya) % pitch;
+  return off < cols * width || pitch - off < cols * width;
 }
 
 // flag bits a filter may require
@@ -594,6 +608,188 @@ int ps_verify_batch(ps_ctx* ctx, const ps_verify_shape* shape, const ps_verify_c
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return PS_E_CUDA;
   CUDA_OK(launch_verify(s, d_cases, n, d_data, data_len, d_theta_out, d_out, ctx->h->status, ctx->stream));
+  return PS_OK;
+}
+
+// ------------------------------------------------------------ operators of a training step
+int ps_dropout(ps_ctx* ctx, const ps_dropout_desc* desc, const void* d_x, const void* d_residual, void* d_y) {
+  if (!ctx || !desc) return PS_E_NULLPTR;
+  const ps_dropout_desc& d = *desc;
+  if (d.dtype > PS_F16 || !(d.p >= 0 && d.p <= 1)) return PS_E_RANGE;
+  if (d.rows == 0 || d.cols == 0) return PS_OK;
+  if (!d_x || !d_y) return PS_E_NULLPTR;
+  const u64 width = d.dtype == PS_F32 ? 4 : 2;
+  if (!aligned(d_x, width) || !aligned(d_residual, width) || !aligned(d_y, width)) return PS_E_ALIGN;
+  typedef unsigned __int128 u128;
+  const u64 stride_most = (u64)1 << 40;
+  if ((u128)d.rows * d.cols > (u128)1 << 48 || d.x_stride > stride_most || d.residual_stride > stride_most ||
+      d.y_stride > stride_most || (d.rows > 1 && d.y_stride < d.cols) ||
+      (u128)d.first + (u128)d.rows * d.pitch + d.cols > (u128)1 << 63)
+    return PS_E_RANGE;
+  if (overwrites(d_y, d.y_stride, d_x, d.x_stride, d.rows, d.cols, width) ||
+      (d_residual && overwrites(d_y, d.y_stride, d_residual, d.residual_stride, d.rows, d.cols, width)))
+    return PS_E_RANGE;
+  int rc = pending_device_error(ctx);
+  if (rc != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  DropoutArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = d_x; a.residual = d_residual; a.y = d_y;
+  a.rows = d.rows; a.cols = d.cols;
+  a.x_stride = d.x_stride; a.residual_stride = d.residual_stride; a.y_stride = d.y_stride;
+  a.first = d.first; a.pitch = d.pitch; a.seed = d.seed; a.stream = d.stream;
+  a.threshold = (u64)rint(d.p * 4294967296.0);
+  a.scale = d.p < 1 ? (float)(1.0 / (1.0 - d.p)) : 0.f;
+  CUDA_OK(launch_dropout(d.dtype, a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
+static int embed_args(const ps_embed_desc& d, EmbedArgs& a) {
+  if (d.tokens > ((u64)1 << 30) || d.rows < 1 || d.rows > ((u64)1 << 30) || d.dim < 1 || d.dim > ((u64)1 << 20) ||
+      d.table_stride < d.dim || d.out_stride < d.dim || d.table_stride > ((u64)1 << 32) || d.out_stride > ((u64)1 << 32) ||
+      d.dtype > PS_F16 || d.grad_dtype > PS_F16 || (d.token_bytes != 4 && d.token_bytes != 8) || d.accumulate > 1 ||
+      !std::isfinite(d.scale))
+    return PS_E_RANGE;
+  memset(&a, 0, sizeof(a));
+  a.n_tokens = d.tokens; a.first_row = d.first_row; a.rows = d.rows; a.dim = d.dim;
+  a.table_stride = d.table_stride; a.out_stride = d.out_stride;
+  a.scale = (float)d.scale;
+  a.token_bytes = d.token_bytes; a.accumulate = d.accumulate;
+  return PS_OK;
+}
+
+int ps_embed_forward(ps_ctx* ctx, const ps_embed_desc* desc, const void* d_table, const void* d_tokens, void* d_out) {
+  if (!ctx || !desc) return PS_E_NULLPTR;
+  EmbedArgs a;
+  int rc = embed_args(*desc, a);
+  if (rc != PS_OK) return rc;
+  if (a.n_tokens == 0) return PS_OK;
+  if (!d_table || !d_tokens || !d_out) return PS_E_NULLPTR;
+  const size_t width = desc->dtype == PS_F32 ? 4 : 2;
+  if (!aligned(d_table, width) || !aligned(d_out, width) || !aligned(d_tokens, a.token_bytes)) return PS_E_ALIGN;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  a.table = const_cast<void*>(d_table); a.tokens = d_tokens; a.out = d_out;
+  CUDA_OK(launch_embed_forward(desc->dtype, a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
+uint64_t ps_embed_backward_bytes(const ps_embed_desc* desc) {
+  EmbedArgs a;
+  return desc && embed_args(*desc, a) == PS_OK ? embed_backward_bytes(a) : 0;
+}
+
+int ps_embed_backward(ps_ctx* ctx, const ps_embed_desc* desc, const void* d_out_grad, const void* d_tokens,
+                      void* d_table_grad, void* d_work, uint64_t work_bytes) {
+  if (!ctx || !desc || !d_table_grad) return PS_E_NULLPTR;
+  EmbedArgs a;
+  int rc = embed_args(*desc, a);
+  if (rc != PS_OK) return rc;
+  const u64 need = embed_backward_bytes(a);
+  if ((a.n_tokens && (!d_out_grad || !d_tokens)) || (need && !d_work)) return PS_E_NULLPTR;
+  if (!aligned(d_out_grad, desc->dtype == PS_F32 ? 4 : 2) || !aligned(d_table_grad, desc->grad_dtype == PS_F32 ? 4 : 2) ||
+      !aligned(d_tokens, a.token_bytes) || !aligned(d_work, 256))
+    return PS_E_ALIGN;
+  if (work_bytes < need) return PS_E_RANGE;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  a.table = d_table_grad; a.tokens = d_tokens; a.out = const_cast<void*>(d_out_grad); a.work = d_work;
+  CUDA_OK(launch_embed_backward(desc->dtype, desc->grad_dtype, a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
+static int attention_args(const ps_attention_shape& s, AttentionArgs& a) {
+  if (s.batch > 65535 || s.q_len > (1u << 24) || s.k_len > (1u << 24) || s.heads < 1 || s.heads > 32768 || s.kv_heads < 1 ||
+      s.heads % s.kv_heads || s.dim < 8 || s.dim > 128 || s.dim % 8 || (s.dtype != PS_BF16 && s.dtype != PS_F16) ||
+      s.causal > 1 || !std::isfinite(s.scale))
+    return PS_E_RANGE;
+  // what a grid can hold, a block for 128 queries or keys of a head
+  if ((u64)s.batch * s.heads * ((std::max(s.q_len, s.k_len) + 127) / 128) > 0x7fffffffu) return PS_E_RANGE;
+  memset(&a, 0, sizeof(a));
+  a.batch = (int)s.batch; a.q_len = (int)s.q_len; a.k_len = (int)s.k_len;
+  a.heads = (int)s.heads; a.kv_heads = (int)s.kv_heads; a.dim = (int)s.dim; a.causal = (int)s.causal;
+  a.scale = s.scale;
+  return PS_OK;
+}
+
+// a tensor [batch][len][heads][dim] of attention, and what has to hold of it
+static int take_heads(const ps_heads* h, u32 batch, u32 len, u32 heads, ps_heads& into) {
+  if (!h) return PS_E_NULLPTR;
+  into = *h;
+  if (batch == 0 || len == 0) return PS_OK;                     // no element is touched
+  if (!h->data) return PS_E_NULLPTR;
+  if (!aligned(h->data, 16)) return PS_E_ALIGN;
+  u64* strides[3] = {&into.batch_stride, &into.token_stride, &into.head_stride};
+  const u32 extents[3] = {batch, len, heads};
+  for (int i = 0; i < 3; ++i) {
+    if (extents[i] == 1) *strides[i] = 8;                       // never multiplied by more than 0
+    if (*strides[i] % 8) return PS_E_ALIGN;
+    if (*strides[i] == 0 || *strides[i] >= ((u64)1 << 38)) return PS_E_RANGE;
+  }
+  return PS_OK;
+}
+
+int ps_attention_forward(ps_ctx* ctx, const ps_attention_shape* shape, const ps_heads* q, const ps_heads* k,
+                         const ps_heads* v, const ps_heads* out, float* d_lse, const int32_t* d_q_lens,
+                         const int32_t* d_k_lens) {
+  if (!ctx || !shape) return PS_E_NULLPTR;
+  AttentionArgs a;
+  int rc = attention_args(*shape, a);
+  if (rc != PS_OK) return rc;
+  const ps_attention_shape& s = *shape;
+  if ((rc = take_heads(q, s.batch, s.q_len, s.heads, a.q)) != PS_OK ||
+      (rc = take_heads(k, s.batch, s.k_len, s.kv_heads, a.k)) != PS_OK ||
+      (rc = take_heads(v, s.batch, s.k_len, s.kv_heads, a.v)) != PS_OK ||
+      (rc = take_heads(out, s.batch, s.q_len, s.heads, a.out)) != PS_OK)
+    return rc;
+  if (s.batch == 0 || s.q_len == 0) return PS_OK;
+  if (!d_lse) return PS_E_NULLPTR;
+  if (!aligned(d_lse, 4) || !aligned(d_q_lens, 4) || !aligned(d_k_lens, 4)) return PS_E_ALIGN;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  a.lse = d_lse; a.q_lens = d_q_lens; a.k_lens = d_k_lens; a.status = ctx->h->status;
+  CUDA_OK(launch_attention_forward(s.dtype, a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
+uint64_t ps_attention_backward_bytes(const ps_attention_shape* shape) {
+  AttentionArgs a;
+  return shape && attention_args(*shape, a) == PS_OK ? attention_backward_bytes(a) : 0;
+}
+
+int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps_heads* q, const ps_heads* k,
+                          const ps_heads* v, const ps_heads* out, const float* d_lse, const ps_heads* d_out,
+                          const ps_heads* d_q, const ps_heads* d_k, const ps_heads* d_v, const int32_t* d_q_lens,
+                          const int32_t* d_k_lens, void* d_work, uint64_t work_bytes) {
+  if (!ctx || !shape) return PS_E_NULLPTR;
+  AttentionArgs a;
+  int rc = attention_args(*shape, a);
+  if (rc != PS_OK) return rc;
+  const ps_attention_shape& s = *shape;
+  if ((rc = take_heads(q, s.batch, s.q_len, s.heads, a.q)) != PS_OK ||
+      (rc = take_heads(k, s.batch, s.k_len, s.kv_heads, a.k)) != PS_OK ||
+      (rc = take_heads(v, s.batch, s.k_len, s.kv_heads, a.v)) != PS_OK ||
+      (rc = take_heads(out, s.batch, s.q_len, s.heads, a.out)) != PS_OK ||
+      (rc = take_heads(d_out, s.batch, s.q_len, s.heads, a.d_out)) != PS_OK ||
+      (rc = take_heads(d_q, s.batch, s.q_len, s.heads, a.d_q)) != PS_OK ||
+      (rc = take_heads(d_k, s.batch, s.k_len, s.kv_heads, a.d_k)) != PS_OK ||
+      (rc = take_heads(d_v, s.batch, s.k_len, s.kv_heads, a.d_v)) != PS_OK)
+    return rc;
+  if (s.batch == 0 || (s.q_len == 0 && s.k_len == 0)) return PS_OK;
+  const u64 need = attention_backward_bytes(a);
+  if ((s.q_len && !d_lse) || (need && !d_work)) return PS_E_NULLPTR;
+  if (!aligned(d_lse, 4) || !aligned(d_q_lens, 4) || !aligned(d_k_lens, 4) || !aligned(d_work, 256)) return PS_E_ALIGN;
+  if (work_bytes < need) return PS_E_RANGE;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  a.lse = const_cast<float*>(d_lse); a.q_lens = d_q_lens; a.k_lens = d_k_lens; a.status = ctx->h->status;
+  a.delta = (float*)d_work;
+  CUDA_OK(launch_attention_backward(s.dtype, a, ctx->sm_count, ctx->stream));
   return PS_OK;
 }
 

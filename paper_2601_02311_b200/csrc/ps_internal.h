@@ -125,3 +125,39 @@ cudaError_t launch_select_compare(const SpaceDev& sp, u32 unit_begin, u32 unit_e
                                   u64 host_cap, u32 require_flags, u32 comm_kind, const ps_front_entry* d_frontier,
                                   const u32* d_counts, u32 n_caps, u32 cap_index, u32 max_entries,
                                   ps_select_compare_result* d_out, cudaStream_t stream);
+
+// ---- operators of a training step
+struct DropoutArgs {
+  const void *x, *residual;   // residual may be null
+  void* y;
+  u64 rows, cols, x_stride, residual_stride, y_stride;   // strides between rows, in elements
+  u64 first, pitch, seed, stream;
+  u64 threshold;              // words below it drop their element; 2^32 drops all
+  float scale;
+};
+cudaError_t launch_dropout(u32 dtype, const DropoutArgs& a, int sm_count, cudaStream_t stream);
+
+struct EmbedArgs {
+  const void* tokens;
+  void *table, *out;          // backward: the table's gradient, and the gradient of the output
+  u64 n_tokens, first_row, rows, dim, table_stride, out_stride;
+  float scale;
+  u32 token_bytes, accumulate;
+  void* work;
+};
+cudaError_t launch_embed_forward(u32 dtype, const EmbedArgs& a, int sm_count, cudaStream_t stream);
+size_t embed_backward_bytes(const EmbedArgs& a);
+cudaError_t launch_embed_backward(u32 dtype, u32 grad_dtype, const EmbedArgs& a, int sm_count, cudaStream_t stream);
+
+struct AttentionArgs {
+  ps_heads q, k, v, out, d_out, d_q, d_k, d_v;
+  float* lse;                 // [batch][heads][q_len]
+  const int *q_lens, *k_lens; // per sequence, or null
+  int batch, q_len, k_len, heads, kv_heads, dim, causal;
+  float scale;
+  float* delta;               // backward's work space: [batch][heads][q_len]
+  volatile u32* status;
+};
+cudaError_t launch_attention_forward(u32 dtype, const AttentionArgs& a, int sm_count, cudaStream_t stream);
+size_t attention_backward_bytes(const AttentionArgs& a);
+cudaError_t launch_attention_backward(u32 dtype, const AttentionArgs& a, int sm_count, cudaStream_t stream);
