@@ -529,7 +529,7 @@ typedef struct {
   uint64_t batch_stride, token_stride, head_stride; /* multiples of 8, not 0 where that extent is above 1; dim is contiguous */
 } ps_heads;
 typedef struct {
-  uint32_t batch;                  /* 0 .. 2^16 - 1                                       */
+  uint32_t batch;                  /* 0 .. 2^16 - 1; batch * heads * tokens up to 2^33    */
   uint32_t q_len, k_len;           /* 0 .. 2^24                                           */
   uint32_t heads, kv_heads;        /* 1 .. 2^15, heads a multiple of kv_heads             */
   uint32_t dim;                    /* 8 .. 128, a multiple of 8                           */

@@ -706,8 +706,8 @@ static int attention_args(const ps_attention_shape& s, AttentionArgs& a) {
       s.heads % s.kv_heads || s.dim < 8 || s.dim > 128 || s.dim % 8 || (s.dtype != PS_BF16 && s.dtype != PS_F16) ||
       s.causal > 1 || !std::isfinite(s.scale))
     return PS_E_RANGE;
-  // what a grid can hold, a block for 128 queries or keys of a head
-  if ((u64)s.batch * s.heads * ((std::max(s.q_len, s.k_len) + 127) / 128) > 0x7fffffffu) return PS_E_RANGE;
+  // what the grids can hold (a block for 128 queries or keys of a head, or for 16 rows)
+  if ((u64)s.batch * s.heads * ((std::max(s.q_len, s.k_len) + 127) / 128) > (1u << 26)) return PS_E_RANGE;
   memset(&a, 0, sizeof(a));
   a.batch = (int)s.batch; a.q_len = (int)s.q_len; a.k_len = (int)s.k_len;
   a.heads = (int)s.heads; a.kv_heads = (int)s.kv_heads; a.dim = (int)s.dim; a.causal = (int)s.causal;
@@ -788,7 +788,7 @@ int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return PS_E_CUDA;
   a.lse = const_cast<float*>(d_lse); a.q_lens = d_q_lens; a.k_lens = d_k_lens; a.status = ctx->h->status;
-  a.delta = (float*)d_work;
+  a.work = d_work;
   CUDA_OK(launch_attention_backward(s.dtype, a, ctx->sm_count, ctx->stream));
   return PS_OK;
 }

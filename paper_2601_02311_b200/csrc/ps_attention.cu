@@ -7,141 +7,863 @@
 // Query i of a sequence of n queries and m keys sees key j < m, under the causal mask those with j <= i + m - n.
 // A query that sees nothing has O = 0 and lse = -infinity, and no gradient.  Queries behind n and keys behind m are
 // padding: nothing of theirs is used, and zeros are written for them.
-#include "ps_train.cuh"
+//
+// All products run on the tensor cores (ps_tensor.cuh) on tiles of 128 queries and 128 keys; the matrices between two
+// products (P, dS) stay in tensor memory.  A block has a warp that copies tiles, a warp that starts products, and two
+// groups of four warps that take the exponentials.
+//
+// Exponents are taken to base 2: exp(S - lse) = 2^(c S' - lse log2 e) with S' = Q K^T and c = |scale| log2 e (a negative
+// scale negates an operand of the product; c is at least 1e-30, so that what a mask sets to -infinity stays there).
+//
+// The backward pass is two kernels, one that owns keys (dK, dV) and one that owns queries (dQ).  That is seven products a
+// tile pair instead of the five of a single pass, which would have to add dQ from many blocks in memory: in an order
+// that changes from run to run, or with waits between blocks.  So every result has one order of its sums.
+#include "ps_tensor.cuh"
 
 namespace {
 using namespace train;
+using namespace tensor;
 
 constexpr float MINUS_INF = -INFINITY;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int THREADS = 320;            // two groups of four warps, the copying warp, the products' warp
+constexpr int COPY_WARP = 8, MMA_WARP = 9;
 
-template <class T>
-__device__ __forceinline__ const T* token_of(const ps_heads& h, u64 b, u64 t, u64 head) {
-  return (const T*)h.data + b * h.batch_stride + t * h.token_stride + head * h.head_stride;
-}
-__device__ __forceinline__ int length_of(const int* lens, int b, int most) { return lens ? max(0, min(lens[b], most)) : most; }
-__device__ __forceinline__ float warp_sum(float v) {
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// a token's elements of a head, 4 to a lane (dim <= 128)
-struct Row {
-  float v[4];
+// what a kernel needs beside the maps of its operands
+struct Args {
+  ps_heads out, d_q, d_k, d_v;
+  float* lse;
+  const int *q_lens, *k_lens;
+  int batch, q_len, k_len, heads, kv_heads, dim, causal;
+  float scale, c;
+  // the backward pass's rows: lse log2 e (+infinity for a query without keys) and delta, of every query head with q_len
+  // rounded up to whole tiles; and for types with a small range the norms, see gradient_factor
+  float *lse2, *delta;
+  u32* norms;
+  int padded;
+  volatile u32* status;
 };
+struct Lengths {
+  int n, m;
+};
+__device__ __forceinline__ Lengths lengths_of(const Args& a, int b) {
+  return {a.q_lens ? max(0, min(a.q_lens[b], a.q_len)) : a.q_len, a.k_lens ? max(0, min(a.k_lens[b], a.k_len)) : a.k_len};
+}
+// the keys that query i sees are those before this one
+__device__ __forceinline__ int end_of(const Args& a, Lengths l, int i) {
+  return i >= l.n ? 0 : a.causal ? max(0, min(l.m, i + l.m - l.n + 1)) : l.m;
+}
+// the tiles of keys that the 128 queries from i on see
+__device__ __forceinline__ int key_tiles(const Args& a, Lengths l, int i) {
+  return i >= l.n ? 0 : (end_of(a, l, min(i + ROWS, l.n) - 1) + ROWS - 1) / ROWS;
+}
+
+// 32 columns of a row of results, times `by`, to memory; columns behind dim are not there
 template <class T>
-__device__ __forceinline__ Row load_row(const T* p, int dim) {
-  Row r;
-  for (int e = 0; e < 4; ++e) {
-    const int c = threadIdx.x % 32 + 32 * e;
-    r.v[e] = c < dim ? widen(p[c]) : 0.f;
+__device__ __forceinline__ void store32(T* row, const u32 (&v)[32], int column, int dim, float by) {
+#pragma unroll
+  for (int c = 0; c < 32; c += 8)
+    if (column + c < dim) {
+      uint4 w;
+      w.x = pack<T>(__uint_as_float(v[c]) * by, __uint_as_float(v[c + 1]) * by);
+      w.y = pack<T>(__uint_as_float(v[c + 2]) * by, __uint_as_float(v[c + 3]) * by);
+      w.z = pack<T>(__uint_as_float(v[c + 4]) * by, __uint_as_float(v[c + 5]) * by);
+      w.w = pack<T>(__uint_as_float(v[c + 6]) * by, __uint_as_float(v[c + 7]) * by);
+      *reinterpret_cast<uint4*>(row + column + c) = w;
+    }
+}
+template <class T>
+__device__ __forceinline__ T* row_of(const ps_heads& h, int b, int t, int head) {
+  return (T*)h.data + b * h.batch_stride + t * h.token_stride + head * h.head_stride;
+}
+// a row of results from tensor memory (all lanes of a warp take part), or zeros
+template <class T, int D>
+__device__ __forceinline__ void store_row(T* row, u32 from, bool any, bool there, int dim, float by) {
+#pragma unroll
+  for (int c = 0; c < D; c += 32) {
+    u32 v[32];
+    if (any) {
+      tmem_load32(v, from + c);
+      wait_loads();
+    }
+    if (!any || by == 0.f)
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] = 0;
+    if (there) store32(row, v, c, dim, by);
   }
+}
+
+// the smallest address in the block's shared memory that a tile may have
+__device__ __forceinline__ u32 tiles_begin() {
+  extern __shared__ unsigned char shared[];
+  return (smem_address(shared) + 1023u) & ~1023u;
+}
+// leaving after a wait that did not end: copies and products that are still under way have time to end
+__device__ __forceinline__ void linger(bool dead) {
+  if (dead)
+    for (int i = 0; i < 20; ++i) __nanosleep(1000000);
+}
+
+// ------------------------------------------------------------------ forward
+// A block owns two tiles of 128 queries of a head, a group of warps each, a thread a query.  While one group takes the
+// exponentials of its scores the tensor cores work for the other.  A group's turn: the scores S = Q K^T (128 columns of
+// tensor memory), their row maximum, P = 2^(c S - c maximum) written over S in 16 bits, O += P V.  O is rescaled only when a
+// row's maximum has grown by more than a factor of 2^8: until then P is larger than 1 by up to that, which the 32-bit
+// sums and the types' exponents hold, and lse comes from the same maximum.
+template <class T, int D>
+__global__ void __launch_bounds__(THREADS, 1)
+k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+          const __grid_constant__ CUtensorMap map_v, const Args a) {
+  constexpr u32 TILE = PANEL * (D / 64);
+  constexpr int RING = 4;
+  __shared__ u64 bars[2 + 2 * RING + 6];
+  __shared__ u32 tmem_at;
+  const u32 tiles = tiles_begin(), ring = tiles + 2 * TILE;
+  const u32 q_full = smem_address(bars), full = q_full + 16, empty = full + 8 * RING, s_full = empty + 8 * RING,
+            p_ready = s_full + 16, o_done = p_ready + 16;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+  // the tiles with the most keys first
+  const int per = a.heads * a.batch, n_tiles = (a.q_len + 2 * ROWS - 1) / (2 * ROWS), at = blockIdx.x / per;
+  const int q0 = (a.causal ? n_tiles - 1 - at : at) * 2 * ROWS, b = blockIdx.x % per / a.heads, h = blockIdx.x % a.heads;
+  const int kh = h / (a.heads / a.kv_heads);
+  const Lengths l = lengths_of(a, b);
+  const int count[2] = {key_tiles(a, l, q0), key_tiles(a, l, q0 + ROWS)}, most = max(count[0], count[1]);
+
+  if (warp == MMA_WARP) tmem_alloc(smem_address(&tmem_at), 512);
+  if (threadIdx.x == 0) {
+    for (int t = 0; t < 2; ++t) {
+      barrier_init(q_full + 8 * t, 1);
+      barrier_init(s_full + 8 * t, 1);
+      barrier_init(p_ready + 8 * t, 4);
+      barrier_init(o_done + 8 * t, 1);
+    }
+    for (int i = 0; i < RING; ++i) {
+      barrier_init(full + 8 * i, 1);
+      barrier_init(empty + 8 * i, 1);
+    }
+    fence_barrier_init();
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const u32 tmem = tmem_at;
+  Waiter w(a.status);
+
+  if (warp == COPY_WARP) {
+    if (lane == 0) {
+      for (int t = 0; t < 2; ++t)
+        if (count[t]) {
+          barrier_expect(q_full + 8 * t, TILE);
+          load_tile<D>(tiles + t * TILE, &map_q, h, q0 + t * ROWS, b, q_full + 8 * t);
+        }
+      for (int x = 0; x < 2 * most && !w.dead; ++x) {        // K of tile 0, V of tile 0, K of tile 1, ...
+        const int slot = x % RING;
+        w.wait(empty + 8 * slot, (x / RING & 1) ^ 1);
+        if (w.dead) break;
+        barrier_expect(full + 8 * slot, TILE);
+        load_tile<D>(ring + slot * TILE, x & 1 ? &map_v : &map_k, kh, x / 2 * ROWS, b, full + 8 * slot);
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_o = instruction<T>(D, true, false);
+    auto scores = [&](int t, int j) {
+      const u32 k = ring + (2 * j % RING) * TILE;
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) mma_smem(tmem + t * ROWS, desc_along(tiles + t * TILE, s), desc_along(k, s), ins_s, s > 0);
+      commit(s_full + 8 * t);
+    };
+    if (most > 0) {
+      w.wait_together(full, 0);
+      for (int t = 0; t < 2; ++t)
+        if (count[t]) {
+          w.wait_together(q_full + 8 * t, 0);
+          if (lane == 0 && !w.dead) scores(t, 0);
+        }
+      if (lane == 0 && !w.dead) commit(empty);
+    }
+    for (int j = 0; j < most; ++j) {
+      const int x = 2 * j + 1, slot = x % RING, next = (x + 1) % RING;
+      const u32 v = ring + slot * TILE;
+      w.wait_together(full + 8 * slot, x / RING & 1);
+      if (l.m < a.k_len && (j + 1) * ROWS > l.m && !w.dead) clear_rows<D>(v, l.m - j * ROWS);
+      if (j + 1 < most) w.wait_together(full + 8 * next, (x + 1) / RING & 1);
+      for (int t = 0; t < 2; ++t) {
+        if (j >= count[t]) continue;
+        w.wait_together(p_ready + 8 * t, j & 1);
+        fence_after();
+        if (lane == 0 && !w.dead) {
+#pragma unroll
+          for (int s = 0; s < ROWS / 16; ++s)
+            mma_tmem(tmem + 2 * ROWS + t * D, tmem + t * ROWS + 8 * s, desc_across(v, s), ins_o, j > 0 || s > 0);
+          if (j + 1 < count[t]) scores(t, j + 1);
+          else commit(o_done + 8 * t);
+        }
+      }
+      if (lane == 0 && !w.dead) {
+        commit(empty + 8 * slot);
+        if (j + 1 < most) commit(empty + 8 * next);
+      }
+      __syncwarp();
+    }
+  } else {
+    const int t = warp / 4, row = threadIdx.x % ROWS, i = q0 + t * ROWS + row, end = end_of(a, l, i);
+    const u32 lanes = (u32)(warp % 4 * 32) << 16, s_at = tmem + lanes + t * ROWS, o_at = tmem + lanes + 2 * ROWS + t * D;
+    // the first tile of keys of which some query of this tile does not see all
+    const int masked = (q0 + (t + 1) * ROWS > l.n ? 0 : end_of(a, l, q0 + t * ROWS)) / ROWS;
+    const float slack = 8.f / a.c;
+    float most_s = MINUS_INF, total = 0.f;
+    for (int j = 0; j < count[t]; ++j) {
+      w.wait(s_full + 8 * t, j & 1);
+      fence_after();
+      u32 s[4][32];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tmem_load32(s[q], s_at + 32 * q);
+      wait_loads();
+      if (j >= masked) {
+        const int left = end - j * ROWS;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (32 * q + e >= left) s[q][e] = __float_as_uint(MINUS_INF);
+      }
+      float top[4] = {MINUS_INF, MINUS_INF, MINUS_INF, MINUS_INF};
+#pragma unroll
+      for (int e = 0; e < 32; ++e)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) top[q] = fmaxf(top[q], __uint_as_float(s[q][e]));
+      const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      const bool grown = now > most_s + slack;
+      if (__any_sync(0xffffffffu, grown)) {
+        const float by = grown ? exp2_fast((most_s - now) * a.c) : 1.f;
+        if (grown) most_s = now;
+        total *= by;
+        if (j > 0) {           // (the product that wrote O last is done: S, which was started behind it, is there)
+#pragma unroll
+          for (int c = 0; c < D; c += 32) {
+            u32 o[32];
+            tmem_load32(o, o_at + c);
+            wait_loads();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+            tmem_store32(o_at + c, o);
+          }
+        }
+      }
+      const float off = most_s == MINUS_INF ? 0.f : most_s * a.c;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        u32 p[16];
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const float x = exp2_fast(fmaf(__uint_as_float(s[q][e]), a.c, -off));
+          const float y = exp2_fast(fmaf(__uint_as_float(s[q][e + 1]), a.c, -off));
+          sum[e / 2 % 4] += x + y;
+          p[e / 2] = pack<T>(x, y);
+        }
+        tmem_store16(s_at + 16 * q, p);
+      }
+      total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      wait_stores();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) barrier_arrive(p_ready + 8 * t);
+    }
+    if (count[t]) {
+      w.wait(o_done + 8 * t, 0);
+      fence_after();
+    }
+    const bool there = i < a.q_len;
+    const int safe = min(i, a.q_len - 1);
+    store_row<T, D>(row_of<T>(a.out, b, safe, h), o_at, count[t] > 0, there, a.dim, most_s == MINUS_INF && total == 0.f ? 0.f : 1.f / total);
+    if (there)
+      a.lse[((u64)b * a.heads + h) * a.q_len + i] = most_s == MINUS_INF && total == 0.f ? MINUS_INF : (most_s * a.c + log2f(total)) * LN2;
+  }
+  linger(w.dead);
+  fence_before();
+  __syncthreads();
+  if (warp == MMA_WARP) {
+    fence_after();
+    tmem_free(tmem, 512);
+  }
+}
+
+// ------------------------------------------------------------------ backward
+// Half precision has 2^-24 as its smallest number, and probabilities and gradients go below it.  P is held
+// 2^12 times as large (at most 4096), dS times a power of two that follows from the largest norms: |dP - delta| is at
+// most 2 |dO_i| |V_j|, and that bound is brought to 2^14 or just below for each key head (its queries are summed over).
+// bfloat16 has float's exponents and needs neither.
+template <class T> struct Range { static constexpr bool small = false; };
+template <> struct Range<__half> { static constexpr bool small = true; };
+constexpr int P_SHIFT = 12;
+// dS is held times 2^P_SHIFT times this
+__device__ __forceinline__ float gradient_factor(const Args& a, int b, int kh) {
+  const u32* at = a.norms + 2 * (b * a.kv_heads + kh);
+  const float bound = 2.f * sqrtf(__uint_as_float(at[0])) * sqrtf(__uint_as_float(at[1]));
+  if (!(bound > 0.f && bound < INFINITY)) return exp2_fast(-P_SHIFT);
+  const int e = 14 - ilogbf(bound) - 1;
+  return exp2_fast((float)(max(-60, min(60, e)) - P_SHIFT));
+}
+
+__device__ __forceinline__ void widen8(const uint4& w, float (&v)[8], __nv_bfloat16) {
+  const u32 x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[2 * e] = __uint_as_float(x[e] << 16);
+    v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void widen8(const uint4& w, float (&v)[8], __half) {
+  const u32 x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[e]));
+    v[2 * e] = f.x;
+    v[2 * e + 1] = f.y;
+  }
+}
+
+// The rows that both kernels read: 16 lanes a query, delta and the exponent's offset; in half precision the largest
+// norms of each key head's dO and V rows as well (as bits: norms are not negative, so they compare as integers).
+template <class T>
+__global__ void __launch_bounds__(256) k_rows(const ps_heads d_out, const ps_heads out, const ps_heads v, const Args a) {
+  const int part = threadIdx.x % 16;
+  const u64 queries = (u64)a.batch * a.heads * a.padded, r = ((u64)blockIdx.x * blockDim.x + threadIdx.x) / 16;
+  const bool query = r < queries;
+  const u64 k = r - queries;
+  if (!query && (!Range<T>::small || k >= (u64)a.batch * a.kv_heads * a.k_len)) return;
+  const int per = query ? a.padded : a.k_len, heads = query ? a.heads : a.kv_heads;
+  const u64 rest = (query ? r : k) / per;
+  const int i = (int)((query ? r : k) % per), h = (int)(rest % heads), b = (int)(rest / heads);
+  const Lengths l = lengths_of(a, b);
+  const bool there = i < (query ? l.n : l.m) && part * 8 < a.dim;
+  float x[8] = {}, dot = 0.f, norm = 0.f;
+  if (there) {
+    widen8(*reinterpret_cast<const uint4*>(row_of<const T>(query ? d_out : v, b, i, h) + part * 8), x, T());
+    if (query) {
+      float y[8];
+      widen8(*reinterpret_cast<const uint4*>(row_of<const T>(out, b, i, h) + part * 8), y, T());
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dot = fmaf(x[e], y[e], dot);
+    }
+    if (Range<T>::small)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) norm = fmaf(x[e], x[e], norm);
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    dot += __shfl_xor_sync(0xffffu << (threadIdx.x & 16), dot, o);
+    if (Range<T>::small) norm += __shfl_xor_sync(0xffffu << (threadIdx.x & 16), norm, o);
+  }
+  if (part != 0) return;
+  if (query) {
+    const float lse = i < l.n ? a.lse[((u64)b * a.heads + h) * a.q_len + i] : MINUS_INF;
+    a.lse2[r] = lse == MINUS_INF || end_of(a, l, i) == 0 ? INFINITY : lse * LOG2E - (Range<T>::small ? P_SHIFT : 0);
+    a.delta[r] = dot;
+  }
+  if (Range<T>::small && i < (query ? l.n : l.m))
+    atomicMax(a.norms + 2 * (b * a.kv_heads + (query ? h / (a.heads / a.kv_heads) : h)) + (query ? 0 : 1), __float_as_uint(norm));
+}
+
+// A block owns 128 keys of a key head and walks the queries that see them, through all query heads that share it.  Scores are
+// transposed: S^T = K Q^T has a key a lane, so P^T and dS^T are left operands in tensor memory, and Q and dO serve as right
+// operands of both kinds from one copy.  Tensor memory (D = 128): S^T, dP^T, dV and dK, 128 columns each.  Order of the products:
+//   dV += P^T dO (i), S^T (i + 1)   while the groups take dS of i
+//   dK += dS^T Q (i), dP^T (i + 1)  while the groups take P of i + 1
+// The two groups of warps share each tile pair: a thread has a key and 64 of the 128 queries.
+template <class T, int D>
+__global__ void __launch_bounds__(THREADS, 1)
+k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
+  constexpr u32 TILE = PANEL * (D / 64), VECTORS = 2 * ROWS * 4;
+  __shared__ u64 bars[16];
+  __shared__ u32 tmem_at;
+  const u32 k_tile = tiles_begin(), v_tile = k_tile + TILE, q_ring = v_tile + TILE, do_ring = q_ring + 2 * TILE,
+            vectors = do_ring + 2 * TILE;
+  const u32 kv_full = smem_address(bars), q_full = kv_full + 8, q_empty = q_full + 16, do_full = q_empty + 16, do_empty = do_full + 16,
+            s_full = do_empty + 16, p_ready = s_full + 8, dp_full = p_ready + 8, ds_ready = dp_full + 8, done = ds_ready + 8;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+  // (under the causal mask the first keys have the most queries)
+  const int per = a.kv_heads * a.batch, j0 = blockIdx.x / per * ROWS, b = blockIdx.x % per / a.kv_heads, kh = blockIdx.x % a.kv_heads;
+  const int group = a.heads / a.kv_heads;
+  const Lengths l = lengths_of(a, b);
+  const int first = a.causal ? max(0, j0 - l.m + l.n) / ROWS : 0, last = (l.n + ROWS - 1) / ROWS;     // tiles of queries
+  const int walk = j0 < l.m ? max(0, last - first) : 0, total = walk * group;
+
+  if (warp == MMA_WARP) tmem_alloc(smem_address(&tmem_at), 512);
+  if (threadIdx.x == 0) {
+    barrier_init(kv_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(q_full + 8 * i, 1);
+      barrier_init(q_empty + 8 * i, 1);
+      barrier_init(do_full + 8 * i, 1);
+      barrier_init(do_empty + 8 * i, 1);
+    }
+    barrier_init(s_full, 1);
+    barrier_init(p_ready, 8);
+    barrier_init(dp_full, 1);
+    barrier_init(ds_ready, 8);
+    barrier_init(done, 1);
+    fence_barrier_init();
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const u32 tmem = tmem_at, tmem_s = tmem, tmem_dp = tmem + ROWS, tmem_dv = tmem + 2 * ROWS, tmem_dk = tmem_dv + D;
+  Waiter w(a.status);
+
+  if (warp == COPY_WARP) {
+    if (lane == 0 && total > 0) {
+      barrier_expect(kv_full, 2 * TILE);
+      load_tile<D>(k_tile, &map_k, kh, j0, b, kv_full);
+      load_tile<D>(v_tile, &map_v, kh, j0, b, kv_full);
+      for (int x = 0; x < total; ++x) {
+        const int slot = x & 1, parity = (x >> 1 & 1) ^ 1, h = kh * group + x / walk, i0 = (first + x % walk) * ROWS;
+        const u64 at = ((u64)b * a.heads + h) * a.padded + i0;
+        w.wait(q_empty + 8 * slot, parity);
+        if (w.dead) break;
+        barrier_expect(q_full + 8 * slot, TILE + VECTORS);
+        load_tile<D>(q_ring + slot * TILE, &map_q, h, i0, b, q_full + 8 * slot);
+        load_bytes(vectors + slot * VECTORS, a.lse2 + at, ROWS * 4, q_full + 8 * slot);
+        load_bytes(vectors + slot * VECTORS + ROWS * 4, a.delta + at, ROWS * 4, q_full + 8 * slot);
+        w.wait(do_empty + 8 * slot, parity);
+        if (w.dead) break;
+        barrier_expect(do_full + 8 * slot, TILE);
+        load_tile<D>(do_ring + slot * TILE, &map_do, h, i0, b, do_full + 8 * slot);
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false), ins_acc = instruction<T>(D, true, false);
+    // queries behind the sequence's end, in its last tile
+    auto pad_from = [&](int x) {
+      const int i0 = (first + x % walk) * ROWS;
+      return l.n < a.q_len && i0 + ROWS > l.n ? l.n - i0 : ROWS;
+    };
+    auto scores = [&](int x) {
+      const u32 q = q_ring + (x & 1) * TILE;
+      w.wait_together(q_full + 8 * (x & 1), x >> 1 & 1);
+      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) mma_smem(tmem_s, desc_along(k_tile, s), desc_along(q, s), ins_s, s > 0);
+        commit(s_full);
+      }
+    };
+    auto d_probabilities = [&](int x) {
+      const u32 d = do_ring + (x & 1) * TILE;
+      w.wait_together(do_full + 8 * (x & 1), x >> 1 & 1);
+      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) mma_smem(tmem_dp, desc_along(v_tile, s), desc_along(d, s), ins_dp, s > 0);
+        commit(dp_full);
+      }
+    };
+    if (total > 0) {
+      w.wait_together(kv_full, 0);
+      scores(0);
+      d_probabilities(0);
+    }
+    for (int x = 0; x < total; ++x) {
+      const int slot = x & 1;
+      w.wait_together(p_ready, x & 1);
+      fence_after();
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < ROWS / 16; ++s)
+          mma_tmem(tmem_dv, tmem_s + (s / 4) * 64 + (s % 4) * 8, desc_across(do_ring + slot * TILE, s), ins_acc, x > 0 || s > 0);
+        commit(do_empty + 8 * slot);
+      }
+      __syncwarp();
+      if (x + 1 < total) scores(x + 1);
+      w.wait_together(ds_ready, x & 1);
+      fence_after();
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < ROWS / 16; ++s)
+          mma_tmem(tmem_dk, tmem_dp + (s / 4) * 64 + (s % 4) * 8, desc_across(q_ring + slot * TILE, s), ins_acc, x > 0 || s > 0);
+        commit(q_empty + 8 * slot);
+        if (x + 1 == total) commit(done);
+      }
+      __syncwarp();
+      if (x + 1 < total) d_probabilities(x + 1);
+    }
+  } else {
+    const int half = warp / 4, j = j0 + threadIdx.x % ROWS;
+    const u32 lanes = (u32)(warp % 4 * 32) << 16, s_at = tmem_s + lanes + 64 * half, dp_at = tmem_dp + lanes + 64 * half;
+    // this key's first query; the first query that all of the tile's keys have
+    const int begin = j >= l.m ? 0x7fffffff : a.causal ? j - l.m + l.n : 0;
+    const int whole = j0 + ROWS > l.m ? 0x7fffffff : a.causal ? j0 + ROWS - 1 - l.m + l.n : 0;
+    const float factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
+    for (int x = 0; x < total; ++x) {
+      const int slot = x & 1, i0 = (first + x % walk) * ROWS;
+      const u32 lse_at = vectors + slot * VECTORS + 64 * half * 4, delta_at = lse_at + ROWS * 4;
+      w.wait(q_full + 8 * slot, x >> 1 & 1);
+      w.wait(s_full, x & 1);
+      fence_after();
+      float p[2][32];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32 s[32], out[16];
+        tmem_load32(s, s_at + 32 * q);
+        wait_loads();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          float o[4];
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o[0]), "=f"(o[1]), "=f"(o[2]), "=f"(o[3]) : "r"(lse_at + (32 * q + e) * 4));
+#pragma unroll
+          for (int f = 0; f < 4; ++f) p[q][e + f] = exp2_fast(fmaf(__uint_as_float(s[e + f]), a.c, -o[f]));
+        }
+        if (i0 < whole) {
+          const int skip = begin - i0 - 64 * half - 32 * q;
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (e < skip) p[q][e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) out[e] = pack<T>(p[q][2 * e], p[q][2 * e + 1]);
+        tmem_store16(s_at + 16 * q, out);
+      }
+      wait_stores();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) barrier_arrive(p_ready);
+      w.wait(dp_full, x & 1);
+      fence_after();
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32 s[32], out[16];
+        tmem_load32(s, dp_at + 32 * q);
+        wait_loads();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          float o[4];
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o[0]), "=f"(o[1]), "=f"(o[2]), "=f"(o[3]) : "r"(delta_at + (32 * q + e) * 4));
+#pragma unroll
+          for (int f = 0; f < 4; f += 2) {
+            float u = __uint_as_float(s[e + f]) - o[f], v = __uint_as_float(s[e + f + 1]) - o[f + 1];
+            if (Range<T>::small) u *= factor, v *= factor;
+            out[(e + f) / 2] = pack<T>(p[q][e + f] * u, p[q][e + f + 1] * v);
+          }
+        }
+        tmem_store16(dp_at + 16 * q, out);
+      }
+      wait_stores();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) barrier_arrive(ds_ready);
+    }
+    if (total > 0) {
+      w.wait(done, 0);
+      fence_after();
+    }
+    // one group stores dV, the other dK
+    const bool there = j < a.k_len, used = total > 0 && j < l.m;
+    const int safe = min(j, a.k_len - 1);
+    const float undo = Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f;
+    if (half == 0) store_row<T, D>(row_of<T>(a.d_v, b, safe, kh), tmem_dv + lanes, total > 0, there, a.dim, used ? undo : 0.f);
+    else store_row<T, D>(row_of<T>(a.d_k, b, safe, kh), tmem_dk + lanes, total > 0, there, a.dim, used ? a.scale / factor * undo : 0.f);
+  }
+  linger(w.dead);
+  fence_before();
+  __syncthreads();
+  if (warp == MMA_WARP) {
+    fence_after();
+    tmem_free(tmem, 512);
+  }
+}
+
+// A block owns 128 queries of a head and walks the keys they see.  Tensor memory (D = 128): two buffers of S (the next
+// scores are there when the groups come to them; dS is written over its own S), dP and dQ.  The two groups share each tile
+// pair: a thread has a query and 64 of the 128 keys.
+template <class T, int D>
+__global__ void __launch_bounds__(THREADS, 1)
+k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+          const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
+  constexpr u32 TILE = PANEL * (D / 64);
+  __shared__ u64 bars[16];
+  __shared__ u32 tmem_at;
+  const u32 q_tile = tiles_begin(), do_tile = q_tile + TILE, k_ring = do_tile + TILE, v_ring = k_ring + 2 * TILE;
+  const u32 q_full = smem_address(bars), k_full = q_full + 8, k_empty = k_full + 16, v_full = k_empty + 16, v_empty = v_full + 16,
+            s_full = v_empty + 16, dp_full = s_full + 16, ds_ready = dp_full + 8, done = ds_ready + 8;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+  const int per = a.heads * a.batch, n_tiles = (a.q_len + ROWS - 1) / ROWS, at = blockIdx.x / per;
+  const int q0 = (a.causal ? n_tiles - 1 - at : at) * ROWS, b = blockIdx.x % per / a.heads, h = blockIdx.x % a.heads;
+  const int kh = h / (a.heads / a.kv_heads);
+  const Lengths l = lengths_of(a, b);
+  const int total = key_tiles(a, l, q0);
+
+  if (warp == MMA_WARP) tmem_alloc(smem_address(&tmem_at), 512);
+  if (threadIdx.x == 0) {
+    barrier_init(q_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(k_full + 8 * i, 1);
+      barrier_init(k_empty + 8 * i, 1);
+      barrier_init(v_full + 8 * i, 1);
+      barrier_init(v_empty + 8 * i, 1);
+      barrier_init(s_full + 8 * i, 1);
+    }
+    barrier_init(dp_full, 1);
+    barrier_init(ds_ready, 8);
+    barrier_init(done, 1);
+    fence_barrier_init();
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const u32 tmem = tmem_at, tmem_dp = tmem + 2 * ROWS, tmem_dq = tmem + 3 * ROWS;
+  Waiter w(a.status);
+
+  if (warp == COPY_WARP) {
+    if (lane == 0 && total > 0) {
+      barrier_expect(q_full, 2 * TILE);
+      load_tile<D>(q_tile, &map_q, h, q0, b, q_full);
+      load_tile<D>(do_tile, &map_do, h, q0, b, q_full);
+      for (int x = 0; x < total; ++x) {
+        const int slot = x & 1, parity = (x >> 1 & 1) ^ 1;
+        w.wait(k_empty + 8 * slot, parity);
+        if (w.dead) break;
+        barrier_expect(k_full + 8 * slot, TILE);
+        load_tile<D>(k_ring + slot * TILE, &map_k, kh, x * ROWS, b, k_full + 8 * slot);
+        w.wait(v_empty + 8 * slot, parity);
+        if (w.dead) break;
+        barrier_expect(v_full + 8 * slot, TILE);
+        load_tile<D>(v_ring + slot * TILE, &map_v, kh, x * ROWS, b, v_full + 8 * slot);
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false), ins_acc = instruction<T>(D, true, false);
+    // keys behind the sequence's end, in its last tile
+    auto pad_from = [&](int x) { return l.m < a.k_len && (x + 1) * ROWS > l.m ? l.m - x * ROWS : ROWS; };
+    auto scores = [&](int x) {
+      const u32 k = k_ring + (x & 1) * TILE;
+      w.wait_together(k_full + 8 * (x & 1), x >> 1 & 1);
+      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) mma_smem(tmem + (x & 1) * ROWS, desc_along(q_tile, s), desc_along(k, s), ins_s, s > 0);
+        commit(s_full + 8 * (x & 1));
+      }
+    };
+    auto d_probabilities = [&](int x) {
+      const u32 v = v_ring + (x & 1) * TILE;
+      w.wait_together(v_full + 8 * (x & 1), x >> 1 & 1);
+      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) mma_smem(tmem_dp, desc_along(do_tile, s), desc_along(v, s), ins_dp, s > 0);
+        commit(dp_full);
+        commit(v_empty + 8 * (x & 1));
+      }
+    };
+    if (total > 0) {
+      w.wait_together(q_full, 0);
+      scores(0);
+      d_probabilities(0);
+    }
+    for (int x = 0; x < total; ++x) {
+      const int slot = x & 1;
+      if (x + 1 < total) scores(x + 1);
+      w.wait_together(ds_ready, x & 1);
+      fence_after();
+      if (x + 1 < total) d_probabilities(x + 1);
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < ROWS / 16; ++s)
+          mma_tmem(tmem_dq, tmem + slot * ROWS + (s / 4) * 64 + (s % 4) * 8, desc_across(k_ring + slot * TILE, s), ins_acc, x > 0 || s > 0);
+        commit(k_empty + 8 * slot);
+        if (x + 1 == total) commit(done);
+      }
+      __syncwarp();
+    }
+  } else {
+    const int half = warp / 4, i = q0 + threadIdx.x % ROWS, end = end_of(a, l, i);
+    const u32 lanes = (u32)(warp % 4 * 32) << 16, dp_at = tmem_dp + lanes + 64 * half;
+    const int masked = (q0 + ROWS > l.n ? 0 : end_of(a, l, q0)) / ROWS;
+    const u64 at = ((u64)b * a.heads + h) * a.padded + i;
+    const float off = a.lse2[at], delta = a.delta[at], factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
+    for (int x = 0; x < total; ++x) {
+      const u32 s_at = tmem + lanes + (x & 1) * ROWS + 64 * half;
+      w.wait(s_full + 8 * (x & 1), x >> 1 & 1);
+      fence_after();
+      float p[2][32];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32 s[32];
+        tmem_load32(s, s_at + 32 * q);
+        wait_loads();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) p[q][e] = exp2_fast(fmaf(__uint_as_float(s[e]), a.c, -off));
+        if (x >= masked) {
+          const int left = end - x * ROWS - 64 * half - 32 * q;
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (e >= left) p[q][e] = 0.f;
+        }
+      }
+      w.wait(dp_full, x & 1);
+      fence_after();
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32 s[32], out[16];
+        tmem_load32(s, dp_at + 32 * q);
+        wait_loads();
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          float u = __uint_as_float(s[e]) - delta, v = __uint_as_float(s[e + 1]) - delta;
+          if (Range<T>::small) u *= factor, v *= factor;
+          out[e / 2] = pack<T>(p[q][e] * u, p[q][e + 1] * v);
+        }
+        tmem_store16(s_at + 16 * q, out);
+      }
+      wait_stores();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) barrier_arrive(ds_ready);
+    }
+    if (total > 0) {
+      w.wait(done, 0);
+      fence_after();
+    }
+    // each group stores half of the columns
+    const bool there = i < a.q_len;
+    const int safe = min(i, a.q_len - 1);
+    const float by = off == INFINITY ? 0.f : a.scale / factor * (Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f);
+    store_row<T, D / 2>(row_of<T>(a.d_q, b, safe, h) + half * (D / 2), tmem_dq + lanes + half * (D / 2), total > 0, there,
+                        a.dim - half * (D / 2), by);
+  }
+  linger(w.dead);
+  fence_before();
+  __syncthreads();
+  if (warp == MMA_WARP) {
+    fence_after();
+    tmem_free(tmem, 512);
+  }
+}
+
+// ------------------------------------------------------------------ host
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encoder() {
+  static const EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return (EncodeTiled)p;
+  }();
+  return f;
+}
+
+// a tensor [batch][len][heads][dim] as tiles of 128 tokens and 64 elements
+bool encode(CUtensorMap& map, u32 dtype, const ps_heads& h, int batch, int len, int heads, int dim) {
+  const cuuint64_t extents[4] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)len, (cuuint64_t)batch};
+  const cuuint64_t strides[3] = {h.head_stride * 2, h.token_stride * 2, h.batch_stride * 2};
+  const cuuint32_t box[4] = {64, 1, (cuuint32_t)ROWS, 1}, steps[4] = {1, 1, 1, 1};
+  return encoder()(&map, dtype == PS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, h.data, extents,
+                   strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+Args args_of(const AttentionArgs& a) {
+  Args r;
+  r.out = a.out; r.d_q = a.d_q; r.d_k = a.d_k; r.d_v = a.d_v;
+  r.lse = a.lse; r.q_lens = a.q_lens; r.k_lens = a.k_lens;
+  r.batch = a.batch; r.q_len = a.q_len; r.k_len = a.k_len; r.heads = a.heads; r.kv_heads = a.kv_heads; r.dim = a.dim;
+  r.causal = a.causal;
+  r.scale = a.scale;
+  r.c = fmaxf(fabsf(a.scale) * LOG2E, 1e-30f);
+  r.padded = (a.q_len + ROWS - 1) / ROWS * ROWS;
+  const size_t rows = (size_t)a.batch * a.heads * r.padded;
+  r.lse2 = (float*)a.work;
+  r.delta = r.lse2 + rows;
+  r.norms = (u32*)(r.delta + rows);
+  r.status = a.status;
   return r;
 }
-template <class T>
-__device__ __forceinline__ void store_row(const T* at, const Row& r, int dim, float by) {
-  T* p = const_cast<T*>(at);
-  for (int e = 0; e < 4; ++e) {
-    const int c = threadIdx.x % 32 + 32 * e;
-    if (c < dim) p[c] = narrow<T>(r.v[e] * by);
-  }
+
+// Tensor memory is shared by the blocks of an SM, and each takes all of it: shared memory keeps a second block away.
+u32 smem_for(int tiles, int d, u32 more) {
+  const u32 want = 1024 + tiles * PANEL * (d / 64) + more;
+  return want < 120 * 1024 ? 120 * 1024 : want;
 }
-__device__ __forceinline__ float dot(const Row& a, const Row& b) {
-  float s = 0.f;
-  for (int e = 0; e < 4; ++e) s += a.v[e] * b.v[e];
-  return warp_sum(s);
-}
-__device__ __forceinline__ void add(Row& a, const Row& b, float by) {
-  for (int e = 0; e < 4; ++e) a.v[e] += b.v[e] * by;
+template <class K>
+cudaError_t allow(K kernel, u32 smem) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
 }
 
-// one warp, one query
-template <class T>
-__global__ void k_attend(AttentionArgs a) {
-  const u64 w = ((u64)blockIdx.x * blockDim.x + threadIdx.x) / 32;
-  if (w >= (u64)a.batch * a.heads * a.q_len) return;
-  const int i = (int)(w % a.q_len), h = (int)(w / a.q_len % a.heads), b = (int)(w / a.q_len / a.heads), kh = h / (a.heads / a.kv_heads);
-  const int n = length_of(a.q_lens, b, a.q_len), m = length_of(a.k_lens, b, a.k_len);
-  const int end = i >= n ? 0 : a.causal ? min(m, i + m - n + 1) : m;
-  const Row q = load_row(token_of<T>(a.q, b, i, h), a.dim);
-  Row sum = {};
-  float most = MINUS_INF, total = 0.f;
-  for (int j = 0; j < end; ++j) {
-    const float s = dot(q, load_row(token_of<T>(a.k, b, j, kh), a.dim)) * a.scale;
-    const float next = fmaxf(most, s), by = most == MINUS_INF ? 0.f : __expf(most - next);
-    const float p = __expf(s - next);
-    for (int e = 0; e < 4; ++e) sum.v[e] *= by;
-    total = total * by + p;
-    most = next;
-    add(sum, load_row(token_of<T>(a.v, b, j, kh), a.dim), p);
+template <class T, int D>
+cudaError_t forward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
+  CUtensorMap q, k, v;
+  if (!encode(q, dtype, a.q, a.batch, a.q_len, a.heads, a.dim)) return cudaErrorInvalidValue;
+  if (a.k_len == 0) {
+    k = v = q;                    // there are no keys: never read
+  } else if (!encode(k, dtype, a.k, a.batch, a.k_len, a.kv_heads, a.dim) || !encode(v, dtype, a.v, a.batch, a.k_len, a.kv_heads, a.dim)) {
+    return cudaErrorInvalidValue;
   }
-  store_row(token_of<T>(a.out, b, i, h), sum, a.dim, total > 0.f ? 1.f / total : 0.f);
-  if (threadIdx.x % 32 == 0) a.lse[w] = total > 0.f ? most + __logf(total) : MINUS_INF;
+  const u32 smem = smem_for(6, D, 0), grid = (u32)((a.q_len + 2 * ROWS - 1) / (2 * ROWS)) * a.heads * a.batch;
+  cudaError_t e = allow(k_forward<T, D>, smem);
+  if (e != cudaSuccess) return e;
+  k_forward<T, D><<<grid, THREADS, smem, stream>>>(q, k, v, args_of(a));
+  return cudaGetLastError();
 }
 
-// one warp, one query: delta and dQ
-template <class T>
-__global__ void k_query_gradient(AttentionArgs a) {
-  const u64 w = ((u64)blockIdx.x * blockDim.x + threadIdx.x) / 32;
-  if (w >= (u64)a.batch * a.heads * a.q_len) return;
-  const int i = (int)(w % a.q_len), h = (int)(w / a.q_len % a.heads), b = (int)(w / a.q_len / a.heads), kh = h / (a.heads / a.kv_heads);
-  const int n = length_of(a.q_lens, b, a.q_len), m = length_of(a.k_lens, b, a.k_len);
-  const int end = i >= n ? 0 : a.causal ? min(m, i + m - n + 1) : m;
-  const Row q = load_row(token_of<T>(a.q, b, i, h), a.dim), d_out = load_row(token_of<T>(a.d_out, b, i, h), a.dim);
-  const float delta = dot(d_out, load_row(token_of<T>(a.out, b, i, h), a.dim)), lse = a.lse[w];
-  if (threadIdx.x % 32 == 0) a.delta[w] = delta;
-  Row sum = {};
-  for (int j = 0; j < end; ++j) {
-    const Row k = load_row(token_of<T>(a.k, b, j, kh), a.dim);
-    const float p = __expf(dot(q, k) * a.scale - lse);
-    add(sum, k, p * (dot(d_out, load_row(token_of<T>(a.v, b, j, kh), a.dim)) - delta));
+template <class T, int D>
+cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
+  const Args r = args_of(a);
+  CUtensorMap q, k, v, d;
+  if (a.q_len && (!encode(q, dtype, a.q, a.batch, a.q_len, a.heads, a.dim) || !encode(d, dtype, a.d_out, a.batch, a.q_len, a.heads, a.dim)))
+    return cudaErrorInvalidValue;
+  if (a.k_len && (!encode(k, dtype, a.k, a.batch, a.k_len, a.kv_heads, a.dim) || !encode(v, dtype, a.v, a.batch, a.k_len, a.kv_heads, a.dim)))
+    return cudaErrorInvalidValue;
+  if (!a.q_len) q = d = k;        // on one side there is nothing: never read
+  if (!a.k_len) k = v = q;
+  u64 rows = (u64)a.batch * a.heads * r.padded;
+  cudaError_t e;
+  if (Range<T>::small) {
+    e = cudaMemsetAsync(r.norms, 0, sizeof(u32) * 2 * a.batch * a.kv_heads, stream);
+    if (e != cudaSuccess) return e;
+    rows += (u64)a.batch * a.kv_heads * a.k_len;
   }
-  store_row(token_of<T>(a.d_q, b, i, h), sum, a.dim, a.scale);
-}
-
-// one warp, one key: dK and dV
-template <class T>
-__global__ void k_key_gradient(AttentionArgs a) {
-  const u64 w = ((u64)blockIdx.x * blockDim.x + threadIdx.x) / 32;
-  if (w >= (u64)a.batch * a.kv_heads * a.k_len) return;
-  const int j = (int)(w % a.k_len), kh = (int)(w / a.k_len % a.kv_heads), b = (int)(w / a.k_len / a.kv_heads), group = a.heads / a.kv_heads;
-  const int n = length_of(a.q_lens, b, a.q_len), m = length_of(a.k_lens, b, a.k_len);
-  const int begin = j >= m ? n : a.causal ? max(0, j - m + n) : 0;
-  const Row k = load_row(token_of<T>(a.k, b, j, kh), a.dim), v = load_row(token_of<T>(a.v, b, j, kh), a.dim);
-  Row sum_k = {}, sum_v = {};
-  for (int h = kh * group; h < (kh + 1) * group; ++h)
-    for (int i = begin; i < n; ++i) {
-      const u64 at = ((u64)b * a.heads + h) * a.q_len + i;
-      const Row q = load_row(token_of<T>(a.q, b, i, h), a.dim), d_out = load_row(token_of<T>(a.d_out, b, i, h), a.dim);
-      const float p = __expf(dot(q, k) * a.scale - a.lse[at]);
-      add(sum_v, d_out, p);
-      add(sum_k, q, p * (dot(d_out, v) - a.delta[at]));
-    }
-  store_row(token_of<T>(a.d_k, b, j, kh), sum_k, a.dim, a.scale);
-  store_row(token_of<T>(a.d_v, b, j, kh), sum_v, a.dim, 1.f);
+  if (a.q_len) {
+    k_rows<T><<<(u32)((rows + 15) / 16), 256, 0, stream>>>(a.d_out, a.out, a.v, r);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  if (a.k_len) {
+    const u32 smem = smem_for(6, D, 2 * 2 * ROWS * 4);
+    if ((e = allow(k_keys<T, D>, smem)) != cudaSuccess) return e;
+    k_keys<T, D><<<(u32)((a.k_len + ROWS - 1) / ROWS) * a.kv_heads * a.batch, THREADS, smem, stream>>>(q, k, v, d, r);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  if (a.q_len) {
+    const u32 smem = smem_for(6, D, 0);
+    if ((e = allow(k_queries<T, D>, smem)) != cudaSuccess) return e;
+    k_queries<T, D><<<(u32)(r.padded / ROWS) * a.heads * a.batch, THREADS, smem, stream>>>(q, k, v, d, r);
+  }
+  return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_attention_forward(u32 dtype, const AttentionArgs& a, int, cudaStream_t stream) {
-  const u64 rows = (u64)a.batch * a.heads * a.q_len;
-  const u32 grid = (u32)((rows + 7) / 8);
-  if (rows == 0) return cudaSuccess;
-  if (dtype == PS_BF16) k_attend<__nv_bfloat16><<<grid, 256, 0, stream>>>(a);
-  else k_attend<__half><<<grid, 256, 0, stream>>>(a);
-  return cudaGetLastError();
+  if (!encoder()) return cudaErrorNotSupported;
+  if (dtype == PS_BF16) return a.dim <= 64 ? forward<__nv_bfloat16, 64>(dtype, a, stream) : forward<__nv_bfloat16, 128>(dtype, a, stream);
+  return a.dim <= 64 ? forward<__half, 64>(dtype, a, stream) : forward<__half, 128>(dtype, a, stream);
 }
 
-size_t attention_backward_bytes(const AttentionArgs& a) { return (size_t)a.batch * a.heads * a.q_len * sizeof(float); }
+size_t attention_backward_bytes(const AttentionArgs& a) {
+  const size_t padded = ((size_t)a.q_len + ROWS - 1) / ROWS * ROWS;
+  return sizeof(float) * 2 * a.batch * a.heads * padded + sizeof(u32) * 2 * a.batch * a.kv_heads;
+}
 
 cudaError_t launch_attention_backward(u32 dtype, const AttentionArgs& a, int, cudaStream_t stream) {
-  const u64 rows = (u64)a.batch * a.heads * a.q_len, keys = (u64)a.batch * a.kv_heads * a.k_len;
-  const u32 grid = (u32)((rows + 7) / 8), grid_k = (u32)((keys + 7) / 8);
-  if (dtype == PS_BF16) {
-    if (rows) k_query_gradient<__nv_bfloat16><<<grid, 256, 0, stream>>>(a);
-    if (keys) k_key_gradient<__nv_bfloat16><<<grid_k, 256, 0, stream>>>(a);
-  } else {
-    if (rows) k_query_gradient<__half><<<grid, 256, 0, stream>>>(a);
-    if (keys) k_key_gradient<__half><<<grid_k, 256, 0, stream>>>(a);
-  }
-  return cudaGetLastError();
+  if (!encoder()) return cudaErrorNotSupported;
+  if (dtype == PS_BF16) return a.dim <= 64 ? backward<__nv_bfloat16, 64>(dtype, a, stream) : backward<__nv_bfloat16, 128>(dtype, a, stream);
+  return a.dim <= 64 ? backward<__half, 64>(dtype, a, stream) : backward<__half, 128>(dtype, a, stream);
 }

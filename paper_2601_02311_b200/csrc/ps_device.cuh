@@ -436,6 +436,7 @@ enum : u32 {
   ST_BAD_SHAPE = 1u << 0,      // a model shape outside the supported ranges
   ST_SELF_CHECK = 1u << 2,     // an emitted entry did not re-evaluate to itself
   ST_TRUNCATED = 1u << 3,      // a frontier was longer than the caller's max_entries (a notice, not a fault)
-  ST_BAD_CASE = 1u << 4        // a verifier case outside the supported ranges or the given data
+  ST_BAD_CASE = 1u << 4,       // a verifier case outside the supported ranges or the given data
+  ST_TIMEOUT = 1u << 5         // a wait inside a block did not end
 };
 __device__ __forceinline__ void report(volatile u32* status, u32 bit) { status[__ffs(bit) - 1] = 1u; }

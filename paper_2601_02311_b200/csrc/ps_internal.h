@@ -155,7 +155,7 @@ struct AttentionArgs {
   const int *q_lens, *k_lens; // per sequence, or null
   int batch, q_len, k_len, heads, kv_heads, dim, causal;
   float scale;
-  float* delta;               // backward's work space: [batch][heads][q_len]
+  void* work;                 // backward: attention_backward_bytes
   volatile u32* status;
 };
 cudaError_t launch_attention_forward(u32 dtype, const AttentionArgs& a, int sm_count, cudaStream_t stream);
