@@ -468,7 +468,7 @@ enum { PS_F32 = 0, PS_BF16 = 1, PS_F16 = 2 };
  * a data axis shift `first` by rows, columns of a tensor axis by columns.  y may be x
  * or residual itself (same pointer and stride). */
 typedef struct {
-  uint64_t rows, cols;             /* either may be 0; rows * cols <= 2^48                */
+  uint64_t rows, cols;             /* either may be 0; rows * cols <= 2^48, cols <= 2^32 of several rows */
   uint64_t x_stride, residual_stride, y_stride; /* between rows; y_stride >= cols         */
   uint64_t seed, stream;           /* say, of the run, and of the step and layer          */
   uint64_t first, pitch;           /* first + rows * pitch + cols <= 2^63                 */

@@ -622,7 +622,7 @@ int ps_dropout(ps_ctx* ctx, const ps_dropout_desc* desc, const void* d_x, const 
   if (!aligned(d_x, width) || !aligned(d_residual, width) || !aligned(d_y, width)) return PS_E_ALIGN;
   typedef unsigned __int128 u128;
   const u64 stride_most = (u64)1 << 40;
-  if ((u128)d.rows * d.cols > (u128)1 << 48 || d.x_stride > stride_most || d.residual_stride > stride_most ||
+  if ((u128)d.rows * d.cols > (u128)1 << 48 || (d.rows > 1 && d.cols > ((u64)1 << 32)) || d.x_stride > stride_most || d.residual_stride > stride_most ||
       d.y_stride > stride_most || (d.rows > 1 && d.y_stride < d.cols) ||
       (u128)d.first + (u128)d.rows * d.pitch + d.cols > (u128)1 << 63)
     return PS_E_RANGE;

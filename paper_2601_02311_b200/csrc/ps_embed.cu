@@ -3,8 +3,14 @@
 //   out[t]     = scale * table[token[t] - first_row]           (zeros where that row is not held)
 //   d_table[v] = scale * sum over t with token[t] - first_row = v, t ascending, of d_out[t]
 //
-// Sums are held in 32 bits and rounded once.  Which token adds to which row in which order follows from the tokens
-// alone, so the gradient has the same bits on every run.
+// Sums are held in 32 bits and rounded once.
+//
+// The gradient sorts (row, t) by row with t ascending (a stable radix sort of row numbers alone, so nothing is left to the
+// order in which blocks run), marks where each row's list begins and ends, and gives each row of the table to warps that
+// sum its list: every row of d_table is written once, every row of d_out read once.  A list of c tokens is cut
+// from its own beginning into pieces of 32 and pieces of 1024, which other blocks sum first; the warp adds the sums of
+// the pieces of 1024, then of the pieces of 32 behind them, then the rest: at most c / 1024 + 62 terms.  The cut
+// follows from c alone, so a row's bits are the same whatever else the table holds.
 #include "ps_train.cuh"
 
 namespace {
@@ -17,54 +23,503 @@ __device__ __forceinline__ u32 row_of(const EmbedArgs& a, u64 t) {
   return id >= 0 && (u64)id >= a.first_row && row < a.rows ? (u32)row : (u32)a.rows;
 }
 
-template <class T>
-__global__ void k_lookup(EmbedArgs a) {
-  for (u64 t = blockIdx.x; t < a.n_tokens; t += gridDim.x) {
-    const u32 row = row_of(a, t);
-    for (u64 c = threadIdx.x; c < a.dim; c += blockDim.x)
-      ((T*)a.out)[t * a.out_stride + c] =
-          row < a.rows ? narrow<T>(widen(((const T*)a.table)[row * a.table_stride + c]) * a.scale) : narrow<T>(0.f);
+// ------------------------------------------------------------------ lookup
+// a warp takes LOADS packs a lane of a token's row at a time
+constexpr int LOADS = 4;
+template <class T, int N>
+__global__ void __launch_bounds__(256) k_lookup(EmbedArgs a, u32 chunks, Divider by_chunk, u32 items) {
+  const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
+  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
+    const u32 t = by_chunk.of(item), row = row_of(a, t);
+    const u64 column = (u64)(item - t * chunks) * (32 * N * LOADS) + lane * N;
+    Pack<T, N> v[LOADS];
+    if (row < a.rows) {
+      const T* from = (const T*)a.table + row * a.table_stride + column;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        if (column + i * 32 * N < a.dim) v[i] = load_pack<T, N>(from + i * 32 * N);
+    }
+    T* to = (T*)a.out + t * a.out_stride + column;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      if (column + i * 32 * N < a.dim) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[i].v[e] = row < a.rows ? narrow<T>(widen(v[i].v[e]) * a.scale) : narrow<T>(0.f);
+        store_pack<T, N>(to + i * 32 * N, v[i]);
+      }
   }
 }
 
-// one block, one row of the table
-template <class T, class G>
-__global__ void k_gradient(EmbedArgs a) {
-  for (u64 v = blockIdx.x; v < a.rows; v += gridDim.x)
-    for (u64 c = threadIdx.x; c < a.dim; c += blockDim.x) {
-      float sum = 0.f;
-      for (u64 t = 0; t < a.n_tokens; ++t)
-        if (row_of(a, t) == v) sum += widen(((const T*)a.out)[t * a.out_stride + c]);
-      G* at = (G*)a.table + v * a.table_stride + c;
-      *at = narrow<G>(sum * a.scale + (a.accumulate ? widen(*at) : 0.f));
+// ------------------------------------------------------------------ sort
+constexpr int SORT_THREADS = 512, SORT_ITEMS = 8, SORT_TILE = SORT_THREADS * SORT_ITEMS, SORT_WARPS = SORT_THREADS / 32;
+constexpr int MAX_BITS = 9, MAX_DIGITS = 1 << MAX_BITS;
+constexpr u32 SORT_ALONE = 2 * SORT_TILE;      // so many tokens are sorted by one block
+
+struct SortArgs {
+  u32 n, chunk, blocks;        // tokens, and how many of them in a row a block takes
+  u32 shift, bits, passes;
+  const u32 *keys_in, *values_in;   // null: the tokens themselves, and their places
+  u32 *keys_out, *values_out;
+  u32* counts;                 // [blocks][1 << bits]
+};
+
+__device__ __forceinline__ u32 key_at(const EmbedArgs& a, const u32* keys, u32 i) { return keys ? keys[i] : row_of(a, i); }
+
+// exclusive sums of v over the block's threads (512)
+__device__ __forceinline__ u32 scan_block(u32 v, u32* warp_sums) {
+  const u32 lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  u32 sum = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const u32 other = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= (u32)o) sum += other;
+  }
+  if (lane == 31) warp_sums[warp] = sum;
+  __syncthreads();
+  if (warp == 0) {
+    u32 w = lane < SORT_WARPS ? warp_sums[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < SORT_WARPS; o <<= 1) {
+      const u32 other = __shfl_up_sync(0xffffffffu, w, o);
+      if (lane >= (u32)o) w += other;
     }
+    if (lane < SORT_WARPS) warp_sums[lane] = w;
+  }
+  __syncthreads();
+  return sum - v + (warp ? warp_sums[warp - 1] : 0);
 }
 
+static_assert(MAX_DIGITS == SORT_THREADS, "a thread a digit");
+struct SortShared {
+  u32 base[MAX_DIGITS];                   // where the block's next item of a digit goes
+  u32 count[SORT_WARPS][MAX_DIGITS];
+  u32 warp_sums[SORT_WARPS];
+};
+
+// Puts items [begin, end) in their places, base[digit] on.  A warp takes 32 * SORT_ITEMS items in a row; an item's rank among those of its
+// digit is the number before it in the lanes, in the warp's earlier rounds and in the earlier warps.
+__device__ void place_items(const EmbedArgs& a, const SortArgs& s, u32 begin, u32 end, SortShared& sh) {
+  const u32 lane = threadIdx.x % 32, warp = threadIdx.x / 32, digits = 1u << s.bits;
+  for (u32 tile = begin; tile < end; tile += SORT_TILE) {
+#pragma unroll
+    for (int w = 0; w < SORT_WARPS; ++w) sh.count[w][threadIdx.x] = 0;
+    __syncthreads();
+    u32 key[SORT_ITEMS], rank[SORT_ITEMS];
+#pragma unroll
+    for (int r = 0; r < SORT_ITEMS; ++r) {
+      const u32 i = tile + warp * 32 * SORT_ITEMS + r * 32 + lane;
+      key[r] = i < end ? key_at(a, s.keys_in, i) : 0;
+    }
+#pragma unroll
+    for (int r = 0; r < SORT_ITEMS; ++r) {
+      const bool there = tile + warp * 32 * SORT_ITEMS + r * 32 + lane < end;
+      const u32 digit = there ? (key[r] >> s.shift) & (digits - 1) : digits;     // the absent ones are each other's
+      const u32 same = __match_any_sync(0xffffffffu, digit), before = __popc(same & ((1u << lane) - 1));
+      u32 had = 0;
+      if (there) had = sh.count[warp][digit];
+      __syncwarp();
+      if (there && before == 0) sh.count[warp][digit] = had + __popc(same);
+      __syncwarp();
+      rank[r] = had + before;
+    }
+    __syncthreads();
+    if (threadIdx.x < digits) {
+      u32 sum = sh.base[threadIdx.x];
+#pragma unroll
+      for (int w = 0; w < SORT_WARPS; ++w) {
+        const u32 c = sh.count[w][threadIdx.x];
+        sh.count[w][threadIdx.x] = sum;
+        sum += c;
+      }
+      sh.base[threadIdx.x] = sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < SORT_ITEMS; ++r) {
+      const u32 i = tile + warp * 32 * SORT_ITEMS + r * 32 + lane;
+      if (i < end) {
+        const u32 to = sh.count[warp][(key[r] >> s.shift) & (digits - 1)] + rank[r];
+        s.keys_out[to] = key[r];
+        s.values_out[to] = s.keys_in ? s.values_in[i] : i;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(SORT_THREADS) k_sort_count(EmbedArgs a, SortArgs s) {
+  __shared__ u32 count[MAX_DIGITS];
+  count[threadIdx.x] = 0;
+  __syncthreads();
+  const u32 digits = 1u << s.bits, end = min(s.n, (blockIdx.x + 1) * s.chunk);
+  for (u32 i = blockIdx.x * s.chunk + threadIdx.x; i < end; i += SORT_THREADS)
+    atomicAdd(&count[(key_at(a, s.keys_in, i) >> s.shift) & (digits - 1)], 1u);
+  __syncthreads();
+  if (threadIdx.x < digits) s.counts[blockIdx.x * digits + threadIdx.x] = count[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(SORT_THREADS) k_sort_place(EmbedArgs a, SortArgs s) {
+  __shared__ SortShared sh;
+  const u32 digits = 1u << s.bits;
+  u32 before = 0, all = 0;
+  if (threadIdx.x < digits) {
+#pragma unroll 8
+    for (u32 b = 0; b < s.blocks; ++b) {
+      const u32 c = s.counts[b * digits + threadIdx.x];
+      all += c;
+      before += b < blockIdx.x ? c : 0;
+    }
+  }
+  sh.base[threadIdx.x] = scan_block(all, sh.warp_sums) + before;
+  place_items(a, s, blockIdx.x * s.chunk, min(s.n, (blockIdx.x + 1) * s.chunk), sh);
+}
+
+// Where a row's list begins and ends in the sorted order.  (The array is zeros before: a row without tokens has none.)
+__device__ __forceinline__ void mark(const u32* keys, u32 n, uint2* ranges, u64 rows, u32 i) {
+  const u32 key = keys[i];
+  if (key >= rows) return;
+  if (i == 0 || keys[i - 1] != key) ranges[key].x = i;
+  if (i + 1 == n || keys[i + 1] != key) ranges[key].y = i + 1;
+}
+__global__ void __launch_bounds__(256) k_mark(const u32* keys, u32 n, uint2* ranges, u64 rows) {
+  const u32 i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) mark(keys, n, ranges, rows, i);
+}
+
+// all passes of a short sort, and the marks
+__global__ void __launch_bounds__(SORT_THREADS) k_sort_alone(EmbedArgs a, SortArgs s, u32* keys2, u32* values2, uint2* ranges) {
+  __shared__ SortShared sh;
+  u32 *keys[2] = {s.keys_out, keys2}, *values[2] = {s.values_out, values2};
+  const u32 digits = 1u << s.bits;
+  s.keys_in = nullptr;
+  for (u32 pass = 0; pass < s.passes; ++pass) {
+    const int to = (s.passes - 1 - pass) & 1;         // the last pass ends in keys_out
+    s.shift = pass * s.bits;
+    s.keys_out = keys[to];
+    s.values_out = values[to];
+    sh.base[threadIdx.x] = 0;
+    __syncthreads();
+    for (u32 i = threadIdx.x; i < s.n; i += SORT_THREADS) atomicAdd(&sh.base[(key_at(a, s.keys_in, i) >> s.shift) & (digits - 1)], 1u);
+    __syncthreads();
+    const u32 at = scan_block(sh.base[threadIdx.x], sh.warp_sums);
+    sh.base[threadIdx.x] = at;
+    place_items(a, s, 0, s.n, sh);
+    s.keys_in = s.keys_out;
+    s.values_in = s.values_out;
+    __syncthreads();
+  }
+  for (u32 i = threadIdx.x; i < s.n; i += SORT_THREADS) mark(s.keys_in, s.n, ranges, a.rows, i);
+}
+
+// ------------------------------------------------------------------ gradient
+constexpr u32 PIECE = 32, PIECE2 = PIECE * PIECE;
+
+struct GradientArgs {
+  const u32 *keys, *places;    // sorted
+  const uint2* ranges;
+  float *sums, *sums2;         // of the pieces of 32 and of 1024, by the place of their first item / their size
+  u32 n;
+  u64 width;                   // of a row of sums: dim rounded up to whole packs
+  u32 chunks;
+  Divider by_chunk;
+};
+
+template <int N>
+struct Sum {
+  float v[LOADS][N];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[i][e] = 0.f;
+  }
+  // adds `count` rows in order: row r is at base + place(r) * stride; `columns` of them are left from this lane's first on
+  template <class T, class Place>
+  __device__ __forceinline__ void add_rows(const T* base, u64 stride, u32 count, s64 columns, Place place) {
+    constexpr int AHEAD = 4;
+    for (u32 r = 0; r < count; r += AHEAD) {
+      Pack<T, N> p[AHEAD][LOADS];
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q) {
+        const T* at = base + (u64)place(min(r + q, count - 1)) * stride;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          if (r + q < count && i * 32 * N < columns) p[q][i] = load_pack<T, N>(at + i * 32 * N);
+      }
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          if (r + q < count && i * 32 * N < columns)
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[i][e] += widen(p[q][i].v[e]);
+    }
+  }
+  __device__ __forceinline__ void store(float* to, s64 columns) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      if (i * 32 * N < columns) {
+        Pack<float, N> p;
+#pragma unroll
+        for (int e = 0; e < N; ++e) p.v[e] = v[i][e];
+        store_pack<float, N>(to + i * 32 * N, p);
+      }
+  }
+};
+
+// A piece of a list that begins among the items [size * w, size * w + size): its first item's place, or n.  Such a piece has the
+// last of these items in it, so that there is one at most.
+__device__ __forceinline__ u32 piece_in(const EmbedArgs& a, const GradientArgs& g, u32 w, u32 size) {
+  const u32 last = w * size + size - 1;
+  if (last >= g.n) return g.n;
+  const u32 key = g.keys[last];
+  if (key >= a.rows) return g.n;
+  const uint2 range = g.ranges[key];
+  const u32 first = last - (last - range.x) % size;
+  return first + size <= range.y ? first : g.n;
+}
+
+template <class T, int N>
+__global__ void __launch_bounds__(256) k_pieces(EmbedArgs a, GradientArgs g, u32 items) {
+  const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
+  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
+    const u32 w = g.by_chunk.of(item), first = piece_in(a, g, w, PIECE);
+    if (first >= g.n) continue;
+    const u64 column = (u64)(item - w * g.chunks) * (32 * N * LOADS) + lane * N;
+    const s64 columns = (s64)a.dim - (s64)column;
+    const u32 place = g.places[first + lane];
+    Sum<N> sum;
+    sum.clear();
+    sum.template add_rows<T>((const T*)a.out + column, a.out_stride, PIECE, columns,
+                             [&](u32 r) { return __shfl_sync(0xffffffffu, place, r); });
+    sum.store(g.sums + w * g.width + column, columns);
+  }
+}
+
+template <int N>
+__global__ void __launch_bounds__(256) k_pieces2(EmbedArgs a, GradientArgs g, u32 items) {
+  const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
+  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
+    const u32 w = g.by_chunk.of(item), first = piece_in(a, g, w, PIECE2);
+    if (first >= g.n) continue;
+    const u64 column = (u64)(item - w * g.chunks) * (32 * N * LOADS) + lane * N;
+    const s64 columns = (s64)a.dim - (s64)column;
+    Sum<N> sum;
+    sum.clear();
+    sum.template add_rows<float>(g.sums + column, g.width, PIECE, columns, [&](u32 r) { return first / PIECE + r; });
+    sum.store(g.sums2 + w * g.width + column, columns);
+  }
+}
+
+template <class T, class G, int N, bool LONG>
+__global__ void __launch_bounds__(256) k_gradient(EmbedArgs a, GradientArgs g, u32 items) {
+  const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
+  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
+    const u32 row = g.by_chunk.of(item);
+    const uint2 range = a.n_tokens ? g.ranges[row] : make_uint2(0, 0);
+    const u64 column = (u64)(item - row * g.chunks) * (32 * N * LOADS) + lane * N;
+    const s64 columns = (s64)a.dim - (s64)column;
+    const u32 count = range.y - range.x;
+    if (count == 0 && a.accumulate) continue;
+    Sum<N> sum;
+    sum.clear();
+    u32 at = range.x;
+    if (count >= PIECE) {
+      if (LONG && count >= PIECE2) {
+        const u32 pieces = count / PIECE2;
+        sum.template add_rows<float>(g.sums2 + column, g.width, pieces, columns, [&](u32 r) { return at / PIECE2 + r; });
+        at += pieces * PIECE2;
+      }
+      const u32 pieces = (range.y - at) / PIECE;
+      sum.template add_rows<float>(g.sums + column, g.width, pieces, columns, [&](u32 r) { return at / PIECE + r; });
+      at += pieces * PIECE;
+    }
+    if (at < range.y) {
+      const u32 place = at + lane < range.y ? g.places[at + lane] : 0;
+      sum.template add_rows<T>((const T*)a.out + column, a.out_stride, range.y - at, columns,
+                               [&](u32 r) { return __shfl_sync(0xffffffffu, place, r); });
+    }
+    G* to = (G*)a.table + row * a.table_stride + column;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      if (i * 32 * N < columns) {
+        Pack<G, N> p;
+        if (a.accumulate) p = load_pack<G, N>(to + i * 32 * N);
+#pragma unroll
+        for (int e = 0; e < N; ++e) p.v[e] = narrow<G>(a.accumulate ? fmaf(sum.v[i][e], a.scale, widen(p.v[e])) : sum.v[i][e] * a.scale);
+        store_pack<G, N>(to + i * 32 * N, p);
+      }
+  }
+}
+
+// ------------------------------------------------------------------ host
+u32 chunks_of(u64 dim, int n) { return (u32)((dim + 32 * n * LOADS - 1) / (32 * n * LOADS)); }
+// columns of a row of sums, for every size of packs
+u64 width_of(u64 dim) { return (dim + 7) / 8 * 8; }
+
+// How the radix sort goes: rows + 1 keys (the last one for tokens without a row), digits of up to 9 bits, a block for a
+// tile of 4096 tokens and no more blocks than the GPU has room for at once (each of them reads all blocks' counts).
+constexpr u32 SORT_BLOCKS = 148;
+SortArgs sort_plan(const EmbedArgs& a) {
+  SortArgs s;
+  memset(&s, 0, sizeof(s));
+  s.n = (u32)a.n_tokens;
+  u32 bits = 1;
+  while (((u64)1 << bits) < a.rows + 1) ++bits;
+  s.passes = (bits + MAX_BITS - 1) / MAX_BITS;
+  s.bits = (bits + s.passes - 1) / s.passes;
+  const u32 tiles = (s.n + SORT_TILE - 1) / SORT_TILE, a_block = tiles ? (tiles + SORT_BLOCKS - 1) / SORT_BLOCKS : 1;
+  s.chunk = a_block * SORT_TILE;
+  s.blocks = (s.n + s.chunk - 1) / s.chunk;
+  return s;
+}
+
+struct Work {
+  u32 *keys[2], *values[2], *counts;
+  uint2* ranges;
+  float *sums, *sums2;
+  size_t bytes;
+};
+Work work_of(const EmbedArgs& a) {
+  const SortArgs s = sort_plan(a);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    char* p = (char*)a.work + at;
+    at += (bytes + 255) / 256 * 256;
+    return p;
+  };
+  Work w;
+  for (int i = 0; i < 2; ++i) {
+    w.keys[i] = (u32*)take(4 * (size_t)s.n);
+    w.values[i] = (u32*)take(4 * (size_t)s.n);
+  }
+  w.counts = (u32*)take(s.n > SORT_ALONE ? (size_t)s.blocks * 4 << s.bits : 0);
+  w.ranges = (uint2*)take(8 * a.rows);
+  w.sums = (float*)take(s.n / PIECE * width_of(a.dim) * 4);
+  w.sums2 = (float*)take(s.n / PIECE2 * width_of(a.dim) * 4);
+  w.bytes = a.n_tokens ? at : 0;
+  return w;
+}
+
+// items of a grid: as many as a 31-bit index holds in one launch (each launch takes whole first coordinates)
+template <class Launch>
+cudaError_t in_parts(u64 count, u32 chunks, Launch launch) {
+  const u64 most = 0x7fffffffu / chunks;
+  for (u64 at = 0; at < count; at += most) {
+    launch(at, (u32)(count - at < most ? count - at : most));
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+u32 grid_for(u32 items, int sm_count) {
+  const u32 blocks = (items + 7) / 8, most = (u32)sm_count * 8;
+  return blocks < most ? blocks : most;
+}
+
+template <class T, int N>
+cudaError_t lookup(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
+  const u32 chunks = chunks_of(a.dim, N);
+  return in_parts(a.n_tokens, chunks, [&](u64 at, u32 count) {
+    EmbedArgs part = a;
+    part.tokens = (const char*)a.tokens + at * a.token_bytes;
+    part.out = (T*)a.out + at * a.out_stride;
+    k_lookup<T, N><<<grid_for(count * chunks, sm_count), 256, 0, stream>>>(part, chunks, Divider(chunks), count * chunks);
+  });
+}
+
+template <class T, class G, int N>
+cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
+  cudaError_t e;
+  GradientArgs g;
+  memset((void*)&g, 0, sizeof(g));
+  g.n = (u32)a.n_tokens;
+  g.width = width_of(a.dim);
+  g.chunks = chunks_of(a.dim, N);
+  g.by_chunk = Divider(g.chunks);
+  const Work w = work_of(a);
+  if (g.n) {
+    SortArgs s = sort_plan(a);
+    if ((e = cudaMemsetAsync(w.ranges, 0, 8 * a.rows, stream)) != cudaSuccess) return e;
+    s.counts = w.counts;
+    if (g.n <= SORT_ALONE) {
+      s.keys_out = w.keys[0];
+      s.values_out = w.values[0];
+      k_sort_alone<<<1, SORT_THREADS, 0, stream>>>(a, s, w.keys[1], w.values[1], w.ranges);
+      if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    } else {
+      for (u32 pass = 0; pass < s.passes; ++pass) {
+        const int to = (s.passes - 1 - pass) & 1;
+        s.shift = pass * s.bits;
+        s.keys_in = pass ? w.keys[to ^ 1] : nullptr;
+        s.values_in = pass ? w.values[to ^ 1] : nullptr;
+        s.keys_out = w.keys[to];
+        s.values_out = w.values[to];
+        k_sort_count<<<s.blocks, SORT_THREADS, 0, stream>>>(a, s);
+        k_sort_place<<<s.blocks, SORT_THREADS, 0, stream>>>(a, s);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+      }
+      k_mark<<<(g.n + 255) / 256, 256, 0, stream>>>(w.keys[0], g.n, w.ranges, a.rows);
+      if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    }
+    g.keys = w.keys[0];
+    g.places = w.values[0];
+    g.ranges = w.ranges;
+    g.sums = w.sums;
+    g.sums2 = w.sums2;
+  }
+  // (pieces number n / 32 at most, and a row of the sums is as long as d_out's: fewer items than 2^31 for any d_out that fits)
+  if (g.n >= PIECE) {
+    const u32 items = g.n / PIECE * g.chunks;
+    k_pieces<T, N><<<grid_for(items, sm_count), 256, 0, stream>>>(a, g, items);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  if (g.n >= PIECE2) {
+    const u32 items = g.n / PIECE2 * g.chunks;
+    k_pieces2<N><<<grid_for(items, sm_count), 256, 0, stream>>>(a, g, items);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  return in_parts(a.rows, g.chunks, [&](u64 at, u32 count) {
+    EmbedArgs part = a;
+    GradientArgs gp = g;
+    part.table = (G*)a.table + at * a.table_stride;
+    gp.ranges = g.ranges + (g.n ? at : 0);
+    if (g.n >= PIECE2) k_gradient<T, G, N, true><<<grid_for(count * g.chunks, sm_count), 256, 0, stream>>>(part, gp, count * g.chunks);
+    else k_gradient<T, G, N, false><<<grid_for(count * g.chunks, sm_count), 256, 0, stream>>>(part, gp, count * g.chunks);
+  });
+}
+
+// packs of 16 bytes of the values that are read, where both tensors allow it
+template <class T, class G>
+cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
+  constexpr int N = 16 / sizeof(T);
+  if (a.dim % N == 0 && packs_at(a.out, a.out_stride, N, sizeof(T)) && packs_at(a.table, a.table_stride, N, sizeof(G)))
+    return gradient<T, G, N>(a, sm_count, stream);
+  return gradient<T, G, 1>(a, sm_count, stream);
+}
 template <class T>
-void gradient(u32 grad_dtype, const EmbedArgs& a, u32 grid, cudaStream_t stream) {
-  if (grad_dtype == PS_F32) k_gradient<T, float><<<grid, 256, 0, stream>>>(a);
-  else if (grad_dtype == PS_BF16) k_gradient<T, __nv_bfloat16><<<grid, 256, 0, stream>>>(a);
-  else k_gradient<T, __half><<<grid, 256, 0, stream>>>(a);
+cudaError_t gradient(u32 grad_dtype, const EmbedArgs& a, int sm_count, cudaStream_t stream) {
+  if (grad_dtype == PS_F32) return gradient<T, float>(a, sm_count, stream);
+  return grad_dtype == PS_BF16 ? gradient<T, __nv_bfloat16>(a, sm_count, stream) : gradient<T, __half>(a, sm_count, stream);
+}
+template <class T>
+cudaError_t lookup(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
+  constexpr int N = 16 / sizeof(T);
+  if (a.dim % N == 0 && packs_at(a.out, a.out_stride, N, sizeof(T)) && packs_at(a.table, a.table_stride, N, sizeof(T)))
+    return lookup<T, N>(a, sm_count, stream);
+  return lookup<T, 1>(a, sm_count, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_embed_forward(u32 dtype, const EmbedArgs& a, int sm_count, cudaStream_t stream) {
-  const u64 most = (u64)sm_count * 8;
-  const u32 grid = (u32)(a.n_tokens < most ? a.n_tokens : most);
-  if (dtype == PS_F32) k_lookup<float><<<grid, 256, 0, stream>>>(a);
-  else if (dtype == PS_BF16) k_lookup<__nv_bfloat16><<<grid, 256, 0, stream>>>(a);
-  else k_lookup<__half><<<grid, 256, 0, stream>>>(a);
-  return cudaGetLastError();
+  if (dtype == PS_F32) return lookup<float>(a, sm_count, stream);
+  return dtype == PS_BF16 ? lookup<__nv_bfloat16>(a, sm_count, stream) : lookup<__half>(a, sm_count, stream);
 }
 
-size_t embed_backward_bytes(const EmbedArgs&) { return 0; }
+size_t embed_backward_bytes(const EmbedArgs& a) { return work_of(a).bytes; }
 
 cudaError_t launch_embed_backward(u32 dtype, u32 grad_dtype, const EmbedArgs& a, int sm_count, cudaStream_t stream) {
-  const u64 most = (u64)sm_count * 8;
-  const u32 grid = (u32)(a.rows < most ? a.rows : most);
-  if (dtype == PS_F32) gradient<float>(grad_dtype, a, grid, stream);
-  else if (dtype == PS_BF16) gradient<__nv_bfloat16>(grad_dtype, a, grid, stream);
-  else gradient<__half>(grad_dtype, a, grid, stream);
-  return cudaGetLastError();
+  if (dtype == PS_F32) return gradient<float>(grad_dtype, a, sm_count, stream);
+  return dtype == PS_BF16 ? gradient<__nv_bfloat16>(grad_dtype, a, sm_count, stream) : gradient<__half>(grad_dtype, a, sm_count, stream);
 }
