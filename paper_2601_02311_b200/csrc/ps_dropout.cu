@@ -49,20 +49,23 @@ __global__ void __launch_bounds__(256) k_packs(DropoutArgs a, u32 per_row, Divid
   for (u32 i = blockIdx.x * 256 + threadIdx.x; i < packs; i += gridDim.x * 256) {
     const u32 r = by_row.of(i);
     const u64 c = (u64)(i - r * per_row) * N;
-    const Pack<T, N> x = load_pack<T, N>((const T*)a.x + r * a.x_stride + c);
-    Pack<T, N> y;
-    if (RESIDUAL) y = load_pack<T, N>((const T*)a.residual + r * a.residual_stride + c);
+    Pack<T, N> x, y;
+    float v[N], add[N];
+    x.load((const T*)a.x + r * a.x_stride + c);
+    if (RESIDUAL) y.load((const T*)a.residual + r * a.residual_stride + c);
     const u64 counter = (a.first + r * a.pitch + c) >> 2;
+    Words words[N / 4];
 #pragma unroll
-    for (int q = 0; q < N / 4; ++q) {
-      const Words w = philox(counter + q, a.stream, a.seed);
+    for (int q = 0; q < N / 4; ++q) words[q] = philox(counter + q, a.stream, a.seed);
+    x.widen(v);
+    if (RESIDUAL) y.widen(add);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float v = keep.of(w.w[e], widen(x.v[4 * q + e]));
-        y.v[4 * q + e] = narrow<T>(RESIDUAL ? v + widen(y.v[4 * q + e]) : v);
-      }
+    for (int e = 0; e < N; ++e) {
+      v[e] = keep.of(words[e / 4].w[e % 4], v[e]);
+      if (RESIDUAL) v[e] += add[e];
     }
-    store_pack<T, N>((T*)a.y + r * a.y_stride + c, y);
+    y.narrow(v);
+    y.store((T*)a.y + r * a.y_stride + c);
   }
 }
 

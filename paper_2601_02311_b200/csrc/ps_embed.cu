@@ -25,35 +25,38 @@ __device__ __forceinline__ u32 row_of(const EmbedArgs& a, u64 t) {
 
 // ------------------------------------------------------------------ lookup
 // a warp takes LOADS packs a lane of a token's row at a time
-constexpr int LOADS = 4;
+constexpr int LOOKUP_LOADS = 4;
 template <class T, int N>
 __global__ void __launch_bounds__(256) k_lookup(EmbedArgs a, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
     const u32 t = by_chunk.of(item), row = row_of(a, t);
-    const u64 column = (u64)(item - t * chunks) * (32 * N * LOADS) + lane * N;
-    Pack<T, N> v[LOADS];
-    if (row < a.rows) {
-      const T* from = (const T*)a.table + row * a.table_stride + column;
+    const u64 column = (u64)(item - t * chunks) * (32 * N * LOOKUP_LOADS) + lane * N;
+    Pack<T, N> v[LOOKUP_LOADS];
+    const T* from = (const T*)a.table + row * a.table_stride + column;
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        if (column + i * 32 * N < a.dim) v[i] = load_pack<T, N>(from + i * 32 * N);
+    for (int i = 0; i < LOOKUP_LOADS; ++i) {
+      v[i].clear();
+      if (row < a.rows && column + i * 32 * N < a.dim) v[i].load(from + i * 32 * N);
     }
     T* to = (T*)a.out + t * a.out_stride + column;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i)
+    for (int i = 0; i < LOOKUP_LOADS; ++i)
       if (column + i * 32 * N < a.dim) {
+        float x[N];
+        v[i].widen(x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[i].v[e] = row < a.rows ? narrow<T>(widen(v[i].v[e]) * a.scale) : narrow<T>(0.f);
-        store_pack<T, N>(to + i * 32 * N, v[i]);
+        for (int e = 0; e < N; ++e) x[e] = row < a.rows ? x[e] * a.scale : 0.f;
+        v[i].narrow(x);
+        v[i].store(to + i * 32 * N);
       }
   }
 }
 
 // ------------------------------------------------------------------ sort
-constexpr int SORT_THREADS = 512, SORT_ITEMS = 8, SORT_TILE = SORT_THREADS * SORT_ITEMS, SORT_WARPS = SORT_THREADS / 32;
+constexpr int SORT_THREADS = 512, SORT_ITEMS = 4, SORT_TILE = SORT_THREADS * SORT_ITEMS, SORT_WARPS = SORT_THREADS / 32;
 constexpr int MAX_BITS = 9, MAX_DIGITS = 1 << MAX_BITS;
-constexpr u32 SORT_ALONE = 2 * SORT_TILE;      // so many tokens are sorted by one block
+constexpr u32 SORT_ALONE = 4 * SORT_TILE;      // so many tokens are sorted by one block
 
 struct SortArgs {
   u32 n, chunk, blocks;        // tokens, and how many of them in a row a block takes
@@ -186,84 +189,80 @@ __global__ void __launch_bounds__(256) k_mark(const u32* keys, u32 n, uint2* ran
   if (i < n) mark(keys, n, ranges, rows, i);
 }
 
-// all passes of a short sort, and the marks
-__global__ void __launch_bounds__(SORT_THREADS) k_sort_alone(EmbedArgs a, SortArgs s, u32* keys2, u32* values2, uint2* ranges) {
+// All passes of a short sort, in shared memory, and the marks.
+__global__ void __launch_bounds__(SORT_THREADS) k_sort_alone(EmbedArgs a, SortArgs s, uint2* ranges) {
+  extern __shared__ u32 items[];
   __shared__ SortShared sh;
-  u32 *keys[2] = {s.keys_out, keys2}, *values[2] = {s.values_out, values2};
-  const u32 digits = 1u << s.bits;
-  s.keys_in = nullptr;
+  u32 *const keys = s.keys_out, *const values = s.values_out, n = s.n, digits = 1u << s.bits;
+  s.keys_in = s.values_in = nullptr;
   for (u32 pass = 0; pass < s.passes; ++pass) {
-    const int to = (s.passes - 1 - pass) & 1;         // the last pass ends in keys_out
     s.shift = pass * s.bits;
-    s.keys_out = keys[to];
-    s.values_out = values[to];
+    s.keys_out = items + (pass & 1) * 2 * n;
+    s.values_out = s.keys_out + n;
     sh.base[threadIdx.x] = 0;
     __syncthreads();
-    for (u32 i = threadIdx.x; i < s.n; i += SORT_THREADS) atomicAdd(&sh.base[(key_at(a, s.keys_in, i) >> s.shift) & (digits - 1)], 1u);
+    for (u32 i = threadIdx.x; i < n; i += SORT_THREADS) atomicAdd(&sh.base[(key_at(a, s.keys_in, i) >> s.shift) & (digits - 1)], 1u);
     __syncthreads();
-    const u32 at = scan_block(sh.base[threadIdx.x], sh.warp_sums);
-    sh.base[threadIdx.x] = at;
-    place_items(a, s, 0, s.n, sh);
+    sh.base[threadIdx.x] = scan_block(sh.base[threadIdx.x], sh.warp_sums);
+    place_items(a, s, 0, n, sh);
     s.keys_in = s.keys_out;
     s.values_in = s.values_out;
-    __syncthreads();
   }
-  for (u32 i = threadIdx.x; i < s.n; i += SORT_THREADS) mark(s.keys_in, s.n, ranges, a.rows, i);
+  for (u32 i = threadIdx.x; i < n; i += SORT_THREADS) {
+    keys[i] = s.keys_in[i];
+    values[i] = s.values_in[i];
+    mark(s.keys_in, n, ranges, a.rows, i);
+  }
 }
 
 // ------------------------------------------------------------------ gradient
 constexpr u32 PIECE = 32, PIECE2 = PIECE * PIECE;
+constexpr u32 LONG = 4096;     // from so many tokens on, pieces of 1024 are summed first (a launch; below, a list has up to 128 of 32)
 
 struct GradientArgs {
   const u32 *keys, *places;    // sorted
   const uint2* ranges;
-  float *sums, *sums2;         // of the pieces of 32 and of 1024, by the place of their first item / their size
+  float *sums, *sums2;         // of the pieces of 32 and of 1024 (or null), by the place of their first item / their size
   u32 n;
   u64 width;                   // of a row of sums: dim rounded up to whole packs
-  u32 chunks;
-  Divider by_chunk;
 };
 
-template <int N>
+// N * LOADS sums of a lane, its columns 32 * N apart
+template <int N, int LOADS>
 struct Sum {
   float v[LOADS][N];
-  __device__ __forceinline__ void clear() {
+  __device__ __forceinline__ Sum() {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
 #pragma unroll
       for (int e = 0; e < N; ++e) v[i][e] = 0.f;
   }
-  // adds `count` rows in order: row r is at base + place(r) * stride; `columns` of them are left from this lane's first on
-  template <class T, class Place>
+  // Adds `count` rows in order, AHEAD of them under way at once: row r is at base + place(r) * stride; `columns` of them
+  // are left from this lane's first on.
+  template <int AHEAD, class T, class Place>
   __device__ __forceinline__ void add_rows(const T* base, u64 stride, u32 count, s64 columns, Place place) {
-    constexpr int AHEAD = 4;
+#pragma unroll 1
     for (u32 r = 0; r < count; r += AHEAD) {
       Pack<T, N> p[AHEAD][LOADS];
 #pragma unroll
       for (int q = 0; q < AHEAD; ++q) {
         const T* at = base + (u64)place(min(r + q, count - 1)) * stride;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          if (r + q < count && i * 32 * N < columns) p[q][i] = load_pack<T, N>(at + i * 32 * N);
+        for (int i = 0; i < LOADS; ++i) {
+          p[q][i].clear();
+          if (r + q < count && i * 32 * N < columns) p[q][i].load(at + i * 32 * N);
+        }
       }
 #pragma unroll
       for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          if (r + q < count && i * 32 * N < columns)
+        for (int i = 0; i < LOADS; ++i) {
+          float x[N];
+          p[q][i].widen(x);
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[i][e] += widen(p[q][i].v[e]);
+          for (int e = 0; e < N; ++e) v[i][e] += x[e];
+        }
     }
-  }
-  __device__ __forceinline__ void store(float* to, s64 columns) const {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-      if (i * 32 * N < columns) {
-        Pack<float, N> p;
-#pragma unroll
-        for (int e = 0; e < N; ++e) p.v[e] = v[i][e];
-        store_pack<float, N>(to + i * 32 * N, p);
-      }
   }
 };
 
@@ -279,81 +278,100 @@ __device__ __forceinline__ u32 piece_in(const EmbedArgs& a, const GradientArgs& 
   return first + size <= range.y ? first : g.n;
 }
 
+// (A warp has few columns here, so that the pieces make many warps: a short list is a chain of loads.)
 template <class T, int N>
-__global__ void __launch_bounds__(256) k_pieces(EmbedArgs a, GradientArgs g, u32 items) {
+__global__ void __launch_bounds__(256) k_pieces(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
-    const u32 w = g.by_chunk.of(item), first = piece_in(a, g, w, PIECE);
+    const u32 w = by_chunk.of(item), first = piece_in(a, g, w, PIECE);
     if (first >= g.n) continue;
-    const u64 column = (u64)(item - w * g.chunks) * (32 * N * LOADS) + lane * N;
+    const u64 column = (u64)(item - w * chunks) * (32 * N) + lane * N;
     const s64 columns = (s64)a.dim - (s64)column;
     const u32 place = g.places[first + lane];
-    Sum<N> sum;
-    sum.clear();
-    sum.template add_rows<T>((const T*)a.out + column, a.out_stride, PIECE, columns,
+    Sum<N, 1> sum;
+    sum.template add_rows<8>((const T*)a.out + column, a.out_stride, PIECE, columns,
                              [&](u32 r) { return __shfl_sync(0xffffffffu, place, r); });
-    sum.store(g.sums + w * g.width + column, columns);
+    if (columns > 0) {
+      Pack<float, N> p;
+      p.narrow(sum.v[0]);
+      p.store(g.sums + w * g.width + column);
+    }
   }
 }
 
-template <int N>
-__global__ void __launch_bounds__(256) k_pieces2(EmbedArgs a, GradientArgs g, u32 items) {
+__global__ void __launch_bounds__(256) k_pieces2(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
-    const u32 w = g.by_chunk.of(item), first = piece_in(a, g, w, PIECE2);
+    const u32 w = by_chunk.of(item), first = piece_in(a, g, w, PIECE2);
     if (first >= g.n) continue;
-    const u64 column = (u64)(item - w * g.chunks) * (32 * N * LOADS) + lane * N;
-    const s64 columns = (s64)a.dim - (s64)column;
-    Sum<N> sum;
-    sum.clear();
-    sum.template add_rows<float>(g.sums + column, g.width, PIECE, columns, [&](u32 r) { return first / PIECE + r; });
-    sum.store(g.sums2 + w * g.width + column, columns);
+    const u64 column = (u64)(item - w * chunks) * 128 + lane * 4;
+    const s64 columns = (s64)g.width - (s64)column;       // (sums behind dim are there, and not used)
+    Sum<4, 1> sum;
+    sum.add_rows<8>(g.sums + column, g.width, PIECE, columns, [&](u32 r) { return first / PIECE + r; });
+    if (columns > 0) {
+      Pack<float, 4> p;
+      p.narrow(sum.v[0]);
+      p.store(g.sums2 + w * g.width + column);
+    }
   }
 }
 
-template <class T, class G, int N, bool LONG>
-__global__ void __launch_bounds__(256) k_gradient(EmbedArgs a, GradientArgs g, u32 items) {
+// a warp, LOADS packs a lane of a row
+constexpr int LOADS = 2;
+template <class T, class G, int N>
+__global__ void __launch_bounds__(256, 3) k_gradient(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
-  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
-    const u32 row = g.by_chunk.of(item);
-    const uint2 range = a.n_tokens ? g.ranges[row] : make_uint2(0, 0);
-    const u64 column = (u64)(item - row * g.chunks) * (32 * N * LOADS) + lane * N;
+  const uint2 none = make_uint2(0, 0);
+  u32 item = blockIdx.x * 8 + threadIdx.x / 32, row = by_chunk.of(item);
+  uint2 range = g.n && item < items ? g.ranges[row] : none;
+  for (; item < items;) {
+    const u64 column = (u64)(item - row * chunks) * (32 * N * LOADS) + lane * N;
     const s64 columns = (s64)a.dim - (s64)column;
     const u32 count = range.y - range.x;
-    if (count == 0 && a.accumulate) continue;
-    Sum<N> sum;
-    sum.clear();
     u32 at = range.x;
+    const u32 end = range.y, this_row = row;
+    item += step;
+    row = by_chunk.of(item);
+    range = g.n && item < items ? g.ranges[row] : none;          // (the next one's, ahead)
+    if (count == 0 && a.accumulate) continue;
+    Sum<N, LOADS> sum;
     if (count >= PIECE) {
-      if (LONG && count >= PIECE2) {
+      if (g.sums2 && count >= PIECE2) {
         const u32 pieces = count / PIECE2;
-        sum.template add_rows<float>(g.sums2 + column, g.width, pieces, columns, [&](u32 r) { return at / PIECE2 + r; });
+        sum.template add_rows<2>(g.sums2 + column, g.width, pieces, columns, [&](u32 r) { return at / PIECE2 + r; });
         at += pieces * PIECE2;
       }
-      const u32 pieces = (range.y - at) / PIECE;
-      sum.template add_rows<float>(g.sums + column, g.width, pieces, columns, [&](u32 r) { return at / PIECE + r; });
+      const u32 pieces = (end - at) / PIECE;
+      sum.template add_rows<2>(g.sums + column, g.width, pieces, columns, [&](u32 r) { return at / PIECE + r; });
       at += pieces * PIECE;
     }
-    if (at < range.y) {
-      const u32 place = at + lane < range.y ? g.places[at + lane] : 0;
-      sum.template add_rows<T>((const T*)a.out + column, a.out_stride, range.y - at, columns,
+    if (at < end) {
+      const u32 place = at + lane < end ? g.places[at + lane] : 0;
+      sum.template add_rows<4>((const T*)a.out + column, a.out_stride, end - at, columns,
                                [&](u32 r) { return __shfl_sync(0xffffffffu, place, r); });
     }
-    G* to = (G*)a.table + row * a.table_stride + column;
+    G* to = (G*)a.table + this_row * a.table_stride + column;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
       if (i * 32 * N < columns) {
         Pack<G, N> p;
-        if (a.accumulate) p = load_pack<G, N>(to + i * 32 * N);
+        float x[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) p.v[e] = narrow<G>(a.accumulate ? fmaf(sum.v[i][e], a.scale, widen(p.v[e])) : sum.v[i][e] * a.scale);
-        store_pack<G, N>(to + i * 32 * N, p);
+        for (int e = 0; e < N; ++e) x[e] = 0.f;
+        if (a.accumulate) {
+          p.load(to + i * 32 * N);
+          p.widen(x);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = a.accumulate ? fmaf(sum.v[i][e], a.scale, x[e]) : sum.v[i][e] * a.scale;
+        p.narrow(x);
+        p.store(to + i * 32 * N);
       }
   }
 }
 
 // ------------------------------------------------------------------ host
-u32 chunks_of(u64 dim, int n) { return (u32)((dim + 32 * n * LOADS - 1) / (32 * n * LOADS)); }
+u32 chunks_of(u64 dim, int columns) { return (u32)((dim + columns - 1) / columns); }
 // columns of a row of sums, for every size of packs
 u64 width_of(u64 dim) { return (dim + 7) / 8 * 8; }
 
@@ -419,7 +437,7 @@ u32 grid_for(u32 items, int sm_count) {
 
 template <class T, int N>
 cudaError_t lookup(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
-  const u32 chunks = chunks_of(a.dim, N);
+  const u32 chunks = chunks_of(a.dim, 32 * N * LOOKUP_LOADS);
   return in_parts(a.n_tokens, chunks, [&](u64 at, u32 count) {
     EmbedArgs part = a;
     part.tokens = (const char*)a.tokens + at * a.token_bytes;
@@ -435,8 +453,6 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   memset((void*)&g, 0, sizeof(g));
   g.n = (u32)a.n_tokens;
   g.width = width_of(a.dim);
-  g.chunks = chunks_of(a.dim, N);
-  g.by_chunk = Divider(g.chunks);
   const Work w = work_of(a);
   if (g.n) {
     SortArgs s = sort_plan(a);
@@ -445,7 +461,9 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
     if (g.n <= SORT_ALONE) {
       s.keys_out = w.keys[0];
       s.values_out = w.values[0];
-      k_sort_alone<<<1, SORT_THREADS, 0, stream>>>(a, s, w.keys[1], w.values[1], w.ranges);
+      const u32 smem = 16 * g.n;
+      if ((e = cudaFuncSetAttribute(k_sort_alone, cudaFuncAttributeMaxDynamicSharedMemorySize, 16 * SORT_ALONE)) != cudaSuccess) return e;
+      k_sort_alone<<<1, SORT_THREADS, smem, stream>>>(a, s, w.ranges);
       if ((e = cudaGetLastError()) != cudaSuccess) return e;
     } else {
       for (u32 pass = 0; pass < s.passes; ++pass) {
@@ -466,26 +484,26 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
     g.places = w.values[0];
     g.ranges = w.ranges;
     g.sums = w.sums;
-    g.sums2 = w.sums2;
+    g.sums2 = g.n >= LONG ? w.sums2 : nullptr;
   }
   // (pieces number n / 32 at most, and a row of the sums is as long as d_out's: fewer items than 2^31 for any d_out that fits)
   if (g.n >= PIECE) {
-    const u32 items = g.n / PIECE * g.chunks;
-    k_pieces<T, N><<<grid_for(items, sm_count), 256, 0, stream>>>(a, g, items);
+    const u32 chunks = chunks_of(a.dim, 32 * N), items = g.n / PIECE * chunks;
+    k_pieces<T, N><<<grid_for(items, sm_count), 256, 0, stream>>>(a, g, chunks, Divider(chunks), items);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
-  if (g.n >= PIECE2) {
-    const u32 items = g.n / PIECE2 * g.chunks;
-    k_pieces2<N><<<grid_for(items, sm_count), 256, 0, stream>>>(a, g, items);
+  if (g.n >= LONG) {
+    const u32 chunks = chunks_of(g.width, 128), items = g.n / PIECE2 * chunks;
+    k_pieces2<<<grid_for(items, sm_count), 256, 0, stream>>>(a, g, chunks, Divider(chunks), items);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
-  return in_parts(a.rows, g.chunks, [&](u64 at, u32 count) {
+  const u32 chunks = chunks_of(a.dim, 32 * N * LOADS);
+  return in_parts(a.rows, chunks, [&](u64 at, u32 count) {
     EmbedArgs part = a;
     GradientArgs gp = g;
     part.table = (G*)a.table + at * a.table_stride;
     gp.ranges = g.ranges + (g.n ? at : 0);
-    if (g.n >= PIECE2) k_gradient<T, G, N, true><<<grid_for(count * g.chunks, sm_count), 256, 0, stream>>>(part, gp, count * g.chunks);
-    else k_gradient<T, G, N, false><<<grid_for(count * g.chunks, sm_count), 256, 0, stream>>>(part, gp, count * g.chunks);
+    k_gradient<T, G, N><<<grid_for(count * chunks, sm_count), 256, 0, stream>>>(part, gp, chunks, Divider(chunks), count * chunks);
   });
 }
 

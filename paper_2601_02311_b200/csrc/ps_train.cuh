@@ -17,15 +17,83 @@ template <> __device__ __forceinline__ float narrow<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half narrow<__half>(float v) { return __float2half_rn(v); }
 
-// N consecutive elements, moved in accesses of up to 16 bytes
+// N consecutive elements in the 32-bit words that they were loaded as, by accesses of up to 16 bytes
 template <class T, int N>
-struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack {
-  T v[N];
+struct Pack {
+  static constexpr int WORDS = (N * (int)sizeof(T) + 3) / 4;
+  u32 w[WORDS];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ void load(const T* p) {
+    if (sizeof(T) * N == 2) {
+      w[0] = *reinterpret_cast<const unsigned short*>(p);
+    } else if (WORDS % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 4) {
+        const uint4 v = reinterpret_cast<const uint4*>(p)[i / 4];
+        w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+      }
+    } else if (WORDS % 2 == 0) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 2) {
+        const uint2 v = reinterpret_cast<const uint2*>(p)[i / 2];
+        w[i] = v.x, w[i + 1] = v.y;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) w[i] = reinterpret_cast<const u32*>(p)[i];
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if (sizeof(T) * N == 2) {
+      *reinterpret_cast<unsigned short*>(p) = (unsigned short)w[0];
+    } else if (WORDS % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 4) reinterpret_cast<uint4*>(p)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+    } else if (WORDS % 2 == 0) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 2) reinterpret_cast<uint2*>(p)[i / 2] = make_uint2(w[i], w[i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) reinterpret_cast<u32*>(p)[i] = w[i];
+    }
+  }
+  __device__ __forceinline__ void widen(float (&v)[N]) const {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = one(w, e, (const T*)nullptr);
+  }
+  __device__ __forceinline__ void narrow(const float (&v)[N]) {
+    if (sizeof(T) == 4) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) w[e] = __float_as_uint(v[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; e += 2) w[e / 2] = two(v[e], e + 1 < N ? v[e + 1 < N ? e + 1 : e] : 0.f, (const T*)nullptr);
+    }
+  }
+
+ private:
+  __device__ static __forceinline__ float one(const u32* w, int e, const float*) { return __uint_as_float(w[e]); }
+  __device__ static __forceinline__ float one(const u32* w, int e, const __nv_bfloat16*) {
+    return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
+  __device__ static __forceinline__ float one(const u32* w, int e, const __half*) {
+    return __half2float(__ushort_as_half((unsigned short)(e & 1 ? w[e / 2] >> 16 : w[e / 2])));
+  }
+  __device__ static __forceinline__ u32 two(float, float, const float*) { return 0; }
+  __device__ static __forceinline__ u32 two(float lo, float hi, const __nv_bfloat16*) {
+    u32 r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+  __device__ static __forceinline__ u32 two(float lo, float hi, const __half*) {
+    u32 r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
 };
-template <class T, int N>
-__device__ __forceinline__ Pack<T, N> load_pack(const T* p) { return *reinterpret_cast<const Pack<T, N>*>(p); }
-template <class T, int N>
-__device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) { *reinterpret_cast<Pack<T, N>*>(p) = v; }
 
 // whether packs of n elements may be used at `p` and at rows `stride` elements apart
 inline bool packs_at(const void* p, u64 stride, int n, size_t width) {
