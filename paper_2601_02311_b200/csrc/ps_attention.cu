@@ -26,8 +26,11 @@ using namespace tensor;
 
 constexpr float MINUS_INF = -INFINITY;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int THREADS = 320;            // two groups of four warps, the copying warp, the products' warp
+constexpr int THREADS = 384;            // two groups of four warps, and one of the copying warp, the products' warp and two idle ones
 constexpr int COPY_WARP = 8, MMA_WARP = 9;
+// registers of a thread: as launched, and as the third group gives to the others (3 * 168 = 2 * 208 + 88)
+constexpr int LAUNCHED = 168, TAKEN = 208, LEFT = 88;
+static_assert(3 * LAUNCHED == 2 * TAKEN + LEFT && THREADS * LAUNCHED <= 65536, "registers that the block has");
 
 // what a kernel needs beside the maps of its operands
 struct Args {
@@ -150,63 +153,8 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   const u32 tmem = tmem_at;
   Waiter w(a.status);
 
-  if (warp == COPY_WARP) {
-    if (lane == 0) {
-      for (int t = 0; t < 2; ++t)
-        if (count[t]) {
-          barrier_expect(q_full + 8 * t, TILE);
-          load_tile<D>(tiles + t * TILE, &map_q, h, q0 + t * ROWS, b, q_full + 8 * t);
-        }
-      for (int x = 0; x < 2 * most && !w.dead; ++x) {        // K of tile 0, V of tile 0, K of tile 1, ...
-        const int slot = x % RING;
-        w.wait(empty + 8 * slot, (x / RING & 1) ^ 1);
-        if (w.dead) break;
-        barrier_expect(full + 8 * slot, TILE);
-        load_tile<D>(ring + slot * TILE, x & 1 ? &map_v : &map_k, kh, x / 2 * ROWS, b, full + 8 * slot);
-      }
-    }
-  } else if (warp == MMA_WARP) {
-    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_o = instruction<T>(D, true, false);
-    auto scores = [&](int t, int j) {
-      const u32 k = ring + (2 * j % RING) * TILE;
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) mma_smem(tmem + t * ROWS, desc_along(tiles + t * TILE, s), desc_along(k, s), ins_s, s > 0);
-      commit(s_full + 8 * t);
-    };
-    if (most > 0) {
-      w.wait_together(full, 0);
-      for (int t = 0; t < 2; ++t)
-        if (count[t]) {
-          w.wait_together(q_full + 8 * t, 0);
-          if (lane == 0 && !w.dead) scores(t, 0);
-        }
-      if (lane == 0 && !w.dead) commit(empty);
-    }
-    for (int j = 0; j < most; ++j) {
-      const int x = 2 * j + 1, slot = x % RING, next = (x + 1) % RING;
-      const u32 v = ring + slot * TILE;
-      w.wait_together(full + 8 * slot, x / RING & 1);
-      if (l.m < a.k_len && (j + 1) * ROWS > l.m && !w.dead) clear_rows<D>(v, l.m - j * ROWS);
-      if (j + 1 < most) w.wait_together(full + 8 * next, (x + 1) / RING & 1);
-      for (int t = 0; t < 2; ++t) {
-        if (j >= count[t]) continue;
-        w.wait_together(p_ready + 8 * t, j & 1);
-        fence_after();
-        if (lane == 0 && !w.dead) {
-#pragma unroll
-          for (int s = 0; s < ROWS / 16; ++s)
-            mma_tmem(tmem + 2 * ROWS + t * D, tmem + t * ROWS + 8 * s, desc_across(v, s), ins_o, j > 0 || s > 0);
-          if (j + 1 < count[t]) scores(t, j + 1);
-          else commit(o_done + 8 * t);
-        }
-      }
-      if (lane == 0 && !w.dead) {
-        commit(empty + 8 * slot);
-        if (j + 1 < most) commit(empty + 8 * next);
-      }
-      __syncwarp();
-    }
-  } else {
+  if (warp < COPY_WARP) {
+    take_registers<TAKEN>();
     const int t = warp / 4, row = threadIdx.x % ROWS, i = q0 + t * ROWS + row, end = end_of(a, l, i);
     const u32 lanes = (u32)(warp % 4 * 32) << 16, s_at = tmem + lanes + t * ROWS, o_at = tmem + lanes + 2 * ROWS + t * D;
     // the first tile of keys of which some query of this tile does not see all
@@ -280,6 +228,66 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     store_row<T, D>(row_of<T>(a.out, b, safe, h), o_at, count[t] > 0, there, a.dim, most_s == MINUS_INF && total == 0.f ? 0.f : 1.f / total);
     if (there)
       a.lse[((u64)b * a.heads + h) * a.q_len + i] = most_s == MINUS_INF && total == 0.f ? MINUS_INF : (most_s * a.c + log2f(total)) * LN2;
+  } else if (warp == COPY_WARP) {
+    give_registers<LEFT>();
+    if (lane == 0) {
+      for (int t = 0; t < 2; ++t)
+        if (count[t]) {
+          barrier_expect(q_full + 8 * t, TILE);
+          load_tile<D>(tiles + t * TILE, &map_q, h, q0 + t * ROWS, b, q_full + 8 * t);
+        }
+      for (int x = 0; x < 2 * most && !w.dead; ++x) {        // K of tile 0, V of tile 0, K of tile 1, ...
+        const int slot = x % RING;
+        w.wait(empty + 8 * slot, (x / RING & 1) ^ 1);
+        if (w.dead) break;
+        barrier_expect(full + 8 * slot, TILE);
+        load_tile<D>(ring + slot * TILE, x & 1 ? &map_v : &map_k, kh, x / 2 * ROWS, b, full + 8 * slot);
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    give_registers<LEFT>();
+    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_o = instruction<T>(D, true, false);
+    auto scores = [&](int t, int j) {
+      const u32 k = ring + (2 * j % RING) * TILE;
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) mma_smem(tmem + t * ROWS, desc_along(tiles + t * TILE, s), desc_along(k, s), ins_s, s > 0);
+      commit(s_full + 8 * t);
+    };
+    if (most > 0) {
+      w.wait_together(full, 0);
+      for (int t = 0; t < 2; ++t)
+        if (count[t]) {
+          w.wait_together(q_full + 8 * t, 0);
+          if (lane == 0 && !w.dead) scores(t, 0);
+        }
+      if (lane == 0 && !w.dead) commit(empty);
+    }
+    for (int j = 0; j < most; ++j) {
+      const int x = 2 * j + 1, slot = x % RING, next = (x + 1) % RING;
+      const u32 v = ring + slot * TILE;
+      w.wait_together(full + 8 * slot, x / RING & 1);
+      if (l.m < a.k_len && (j + 1) * ROWS > l.m && !w.dead) clear_rows<D>(v, l.m - j * ROWS);
+      if (j + 1 < most) w.wait_together(full + 8 * next, (x + 1) / RING & 1);
+      for (int t = 0; t < 2; ++t) {
+        if (j >= count[t]) continue;
+        w.wait_together(p_ready + 8 * t, j & 1);
+        fence_after();
+        if (lane == 0 && !w.dead) {
+#pragma unroll
+          for (int s = 0; s < ROWS / 16; ++s)
+            mma_tmem(tmem + 2 * ROWS + t * D, tmem + t * ROWS + 8 * s, desc_across(v, s), ins_o, j > 0 || s > 0);
+          if (j + 1 < count[t]) scores(t, j + 1);
+          else commit(o_done + 8 * t);
+        }
+      }
+      if (lane == 0 && !w.dead) {
+        commit(empty + 8 * slot);
+        if (j + 1 < most) commit(empty + 8 * next);
+      }
+      __syncwarp();
+    }
+  } else {
+    give_registers<LEFT>();
   }
   linger(w.dead);
   fence_before();
@@ -491,7 +499,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       __syncwarp();
       if (x + 1 < total) d_probabilities(x + 1);
     }
-  } else {
+  } else if (warp < COPY_WARP) {
     const int half = warp / 4, j = j0 + threadIdx.x % ROWS;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, s_at = tmem_s + lanes + 64 * half, dp_at = tmem_dp + lanes + 64 * half;
     // this key's first query; the first query that all of the tile's keys have
@@ -680,7 +688,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       }
       __syncwarp();
     }
-  } else {
+  } else if (warp < COPY_WARP) {
     const int half = warp / 4, i = q0 + threadIdx.x % ROWS, end = end_of(a, l, i);
     const u32 lanes = (u32)(warp % 4 * 32) << 16, dp_at = tmem_dp + lanes + 64 * half;
     const int masked = (q0 + ROWS > l.n ? 0 : end_of(a, l, q0)) / ROWS;

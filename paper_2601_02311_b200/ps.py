@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import struct
 
 import numpy as np
 import torch
@@ -94,29 +95,12 @@ VERIFY_RESULT_DTYPE = np.dtype([("mem", "<u8"), ("comm", "<u8"), ("host", "<u8")
                                 ("pad", "<u4"), ("max_rel_err", "<f8")])
 
 
-class _DropoutDesc(C.Structure):
-    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("x_stride", C.c_uint64), ("residual_stride", C.c_uint64),
-                ("y_stride", C.c_uint64), ("seed", C.c_uint64), ("stream", C.c_uint64), ("first", C.c_uint64),
-                ("pitch", C.c_uint64), ("p", C.c_double), ("dtype", C.c_uint32), ("pad", C.c_uint32)]
-
-
-class _EmbedDesc(C.Structure):
-    _fields_ = [("tokens", C.c_uint64), ("first_row", C.c_uint64), ("rows", C.c_uint64), ("dim", C.c_uint64),
-                ("table_stride", C.c_uint64), ("out_stride", C.c_uint64), ("scale", C.c_double), ("dtype", C.c_uint32),
-                ("grad_dtype", C.c_uint32), ("token_bytes", C.c_uint32), ("accumulate", C.c_uint32)]
-
-
-class _Heads(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_uint64), ("token_stride", C.c_uint64),
-                ("head_stride", C.c_uint64)]
-
-
-class _AttentionShape(C.Structure):
-    _fields_ = [("batch", C.c_uint32), ("q_len", C.c_uint32), ("k_len", C.c_uint32), ("heads", C.c_uint32),
-                ("kv_heads", C.c_uint32), ("dim", C.c_uint32), ("dtype", C.c_uint32), ("causal", C.c_uint32),
-                ("scale", C.c_float), ("pad", C.c_uint32)]
-
-
+# The training step's descriptors (ps_dropout_desc, ps_embed_desc, ps_heads, ps_attention_shape) as bytes: a ctypes
+# Structure of as many fields takes a call several microseconds longer.
+_DROPOUT_DESC = struct.Struct("9QdII").pack
+_EMBED_DESC = struct.Struct("6Qd4I").pack
+_HEADS = struct.Struct("4Q").pack
+_ATTENTION_SHAPE = struct.Struct("8IfI").pack
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # PS_F32, PS_BF16, PS_F16
 
 
@@ -158,17 +142,15 @@ _lib.ps_select_compare.argtypes = [C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint6
                                    C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_void_p]
 _lib.ps_verify_batch.argtypes = [C.c_void_p, C.POINTER(_VerifyShape), C.c_void_p, C.c_uint64, C.c_void_p,
                                  C.c_uint64, C.c_void_p, C.c_void_p]
-_lib.ps_dropout.argtypes = [C.c_void_p, C.POINTER(_DropoutDesc), C.c_void_p, C.c_void_p, C.c_void_p]
-_lib.ps_embed_forward.argtypes = [C.c_void_p, C.POINTER(_EmbedDesc), C.c_void_p, C.c_void_p, C.c_void_p]
-_lib.ps_embed_backward_bytes.argtypes = [C.POINTER(_EmbedDesc)]
+_lib.ps_dropout.argtypes = [C.c_void_p] * 5
+_lib.ps_embed_forward.argtypes = [C.c_void_p] * 5
+_lib.ps_embed_backward_bytes.argtypes = [C.c_void_p]
 _lib.ps_embed_backward_bytes.restype = C.c_uint64
-_lib.ps_embed_backward.argtypes = [C.c_void_p, C.POINTER(_EmbedDesc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
-                                   C.c_uint64]
-_lib.ps_attention_forward.argtypes = [C.c_void_p, C.POINTER(_AttentionShape)] + [C.POINTER(_Heads)] * 4 + [C.c_void_p] * 3
-_lib.ps_attention_backward_bytes.argtypes = [C.POINTER(_AttentionShape)]
+_lib.ps_embed_backward.argtypes = [C.c_void_p] * 6 + [C.c_uint64]
+_lib.ps_attention_forward.argtypes = [C.c_void_p] * 9
+_lib.ps_attention_backward_bytes.argtypes = [C.c_void_p]
 _lib.ps_attention_backward_bytes.restype = C.c_uint64
-_lib.ps_attention_backward.argtypes = [C.c_void_p, C.POINTER(_AttentionShape)] + [C.POINTER(_Heads)] * 4 + [C.c_void_p] + \
-    [C.POINTER(_Heads)] * 4 + [C.c_void_p] * 3 + [C.c_uint64]
+_lib.ps_attention_backward.argtypes = [C.c_void_p] * 14 + [C.c_uint64]
 _lib.ps_int_peak.argtypes = [C.c_void_p, C.c_uint32, C.c_uint32, C.c_void_p,
                              C.POINTER(C.c_uint64)]
 
@@ -342,66 +324,79 @@ class Context:
     def _refuse(self, code: int, where: str, what: str):
         raise PsError(code, f"{where}: {what}")
 
-    def _matrix(self, t: torch.Tensor, where: str, name: str, shape=None, dtype=None):
-        """(pointer, stride between rows) of [rows, cols] whose columns are contiguous."""
-        if t.device != self.torch_device:
-            self._refuse(E_RANGE, where, f"{name} is on {t.device}, the context on {self.torch_device}")
-        if t.dim() != 2 or (shape is not None and t.shape != shape):
-            self._refuse(E_RANGE, where, f"{name} has shape {tuple(t.shape)}, wanted {'two dimensions' if shape is None else tuple(shape)}")
-        if t.dtype not in _DTYPE or (dtype is not None and t.dtype != dtype):
-            self._refuse(E_RANGE, where, f"{name} has type {t.dtype}")
-        rows, cols = t.shape
-        if cols > 1 and t.stride(1) != 1:
+    def _row_stride(self, t: torch.Tensor, where: str, name: str, shape, dtype) -> int:
+        """Elements between the rows of [rows, cols] whose columns are contiguous."""
+        if t.shape != shape or t.dtype != dtype or dtype not in _DTYPE or len(shape) != 2 or t.get_device() != self.device:
+            self._refuse(E_RANGE, where, f"{name} is {t.dtype} of {tuple(t.shape)} on {t.device}, wanted {dtype} of two "
+                         f"dimensions {tuple(shape)} on device {self.device}")
+        rows, cols = shape
+        stride = t.stride()
+        if cols > 1 and stride[1] != 1:
             self._refuse(E_ALIGN, where, f"{name}'s columns are not contiguous")
-        return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1)
+        return stride[0] if rows > 1 else max(cols, 1)
 
-    def _tokens(self, t: torch.Tensor, where: str, n: int):
-        if t.device != self.torch_device or t.dtype not in (torch.int32, torch.int64) or t.shape != (n,):
-            self._refuse(E_RANGE, where, f"tokens have to be {n} int32 or int64 on {self.torch_device}")
-        if n > 1 and t.stride(0) != 1:
+    def _tokens(self, t: torch.Tensor, where: str) -> int:
+        """Bytes of a token."""
+        if t.dim() != 1 or t.dtype not in (torch.int64, torch.int32) or t.get_device() != self.device:
+            self._refuse(E_RANGE, where, f"tokens have to be a row of int32 or int64 on device {self.device}")
+        if not t.is_contiguous():
             self._refuse(E_ALIGN, where, "tokens are not contiguous")
-        return t.data_ptr(), t.element_size()
+        return t.element_size()
+
+    def _work(self, work: torch.Tensor | None, need: int, where: str) -> torch.Tensor:
+        if work is None:                # (freed when the call returns: torch gives it out again on this stream only)
+            return self._allocate_work(need)
+        if work.get_device() != self.device or work.dtype != torch.uint8 or not work.is_contiguous():
+            self._refuse(E_RANGE, where, f"work has to be a contiguous uint8 tensor on device {self.device}")
+        return work
+
+    @_on_own_stream
+    def _allocate_work(self, need: int) -> torch.Tensor:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=self.torch_device)
 
     def dropout_into(self, x: torch.Tensor, y: torch.Tensor, p: float, seed: int, stream: int = 0,
                      residual: torch.Tensor | None = None, first: int = 0, pitch: int | None = None):
         """ps_dropout on [rows, cols]; `pitch` is the rows' length in the whole tensor (default cols)."""
-        where = "ps_dropout"
-        x_at, x_stride = self._matrix(x, where, "x")
-        y_at, y_stride = self._matrix(y, where, "y", x.shape, x.dtype)
-        r_at, r_stride = (None, 0) if residual is None else self._matrix(residual, where, "residual", x.shape, x.dtype)
-        rows, cols = x.shape
-        if not (0 <= seed < 1 << 64 and 0 <= stream < 1 << 64 and 0 <= first < 1 << 63 and (pitch is None or 0 <= pitch < 1 << 63)):
+        where, shape, dtype = "ps_dropout", x.shape, x.dtype
+        x_stride = self._row_stride(x, where, "x", shape, dtype)
+        y_stride = self._row_stride(y, where, "y", shape, dtype)
+        r_stride = 0 if residual is None else self._row_stride(residual, where, "residual", shape, dtype)
+        rows, cols = shape
+        if pitch is None:
+            pitch = cols
+        if not (0 <= seed < 1 << 64 and 0 <= stream < 1 << 64 and 0 <= first < 1 << 63 and 0 <= pitch < 1 << 63):
             self._refuse(E_RANGE, where, "seed, stream, first or pitch")
-        desc = _DropoutDesc(rows, cols, x_stride, r_stride, y_stride, seed, stream, first, cols if pitch is None else pitch,
-                            p, _DTYPE[x.dtype], 0)
-        _check(_lib.ps_dropout(self._h, desc, x_at, r_at, y_at), where)
+        _check(_lib.ps_dropout(
+            self._h, _DROPOUT_DESC(rows, cols, x_stride, r_stride, y_stride, seed, stream, first, pitch, p, _DTYPE[dtype], 0),
+            x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr()), where)
 
     @_on_own_stream
     def dropout(self, x: torch.Tensor, p: float, seed: int, stream: int = 0, residual: torch.Tensor | None = None,
                 first: int = 0, pitch: int | None = None) -> torch.Tensor:
         """x with a share p of its elements dropped and the others divided by 1 - p, plus `residual`.
         The gradient of x is the same call on the result's gradient, without a residual."""
-        y = torch.empty(x.shape, dtype=x.dtype, device=self.torch_device)
+        y = x.new_empty(x.shape)
         self.dropout_into(x, y, p, seed, stream, residual, first, pitch)
         return y
 
     def embed_forward_into(self, table: torch.Tensor, tokens: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
                            first_row: int = 0):
         """ps_embed_forward: out[t] = scale * table[tokens[t] - first_row], zeros where that row is not held."""
-        where = "ps_embed_forward"
-        t_at, t_stride = self._matrix(table, where, "table")
-        o_at, o_stride = self._matrix(out, where, "out", (tokens.numel(), table.shape[1]), table.dtype)
-        at, width = self._tokens(tokens, where, tokens.numel())
+        where, shape, dtype = "ps_embed_forward", table.shape, table.dtype
+        width, n = self._tokens(tokens, where), tokens.shape[0]
+        t_stride = self._row_stride(table, where, "table", shape, dtype)
+        o_stride = self._row_stride(out, where, "out", (n, shape[1]), dtype)
         if not 0 <= first_row < 1 << 62:
             self._refuse(E_RANGE, where, "first_row")
-        desc = _EmbedDesc(tokens.numel(), first_row, table.shape[0], table.shape[1], t_stride, o_stride, scale,
-                          _DTYPE[table.dtype], _DTYPE[table.dtype], width, 0)
-        _check(_lib.ps_embed_forward(self._h, desc, t_at, at, o_at), where)
+        code = _DTYPE[dtype]
+        _check(_lib.ps_embed_forward(
+            self._h, _EMBED_DESC(n, first_row, shape[0], shape[1], t_stride, o_stride, scale, code, code, width, 0),
+            table.data_ptr(), tokens.data_ptr(), out.data_ptr()), where)
 
     @_on_own_stream
     def embed_forward(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, first_row: int = 0) -> torch.Tensor:
         """The scaled rows [tokens, dim] of the table that the tokens name."""
-        out = torch.empty((tokens.numel(), table.shape[1]), dtype=table.dtype, device=self.torch_device)
+        out = table.new_empty((tokens.numel(), table.shape[-1]))
         self.embed_forward_into(table, tokens, out, scale, first_row)
         return out
 
@@ -409,83 +404,77 @@ class Context:
                             first_row: int = 0, accumulate: bool = False, work: torch.Tensor | None = None):
         """ps_embed_backward: the gradient of the table, written to or (accumulate) added to d_table.
         `work`: a uint8 buffer of embed_backward_bytes; without it one is allocated for the call."""
-        where = "ps_embed_backward"
-        g_at, g_stride = self._matrix(d_table, where, "d_table")
-        o_at, o_stride = self._matrix(d_out, where, "d_out", (tokens.numel(), d_table.shape[1]))
-        at, width = self._tokens(tokens, where, tokens.numel())
+        where, shape = "ps_embed_backward", d_table.shape
+        width, n = self._tokens(tokens, where), tokens.shape[0]
+        g_stride = self._row_stride(d_table, where, "d_table", shape, d_table.dtype)
+        o_stride = self._row_stride(d_out, where, "d_out", (n, shape[1]), d_out.dtype)
         if not 0 <= first_row < 1 << 62:
             self._refuse(E_RANGE, where, "first_row")
-        desc = _EmbedDesc(tokens.numel(), first_row, d_table.shape[0], d_table.shape[1], g_stride, o_stride, scale,
-                          _DTYPE[d_out.dtype], _DTYPE[d_table.dtype], width, 1 if accumulate else 0)
+        desc = _EMBED_DESC(n, first_row, shape[0], shape[1], g_stride, o_stride, scale, _DTYPE[d_out.dtype],
+                           _DTYPE[d_table.dtype], width, 1 if accumulate else 0)
         work = self._work(work, _lib.ps_embed_backward_bytes(desc), where)
-        _check(_lib.ps_embed_backward(self._h, desc, o_at, at, g_at, work.data_ptr(), work.numel()), where)
+        _check(_lib.ps_embed_backward(self._h, desc, d_out.data_ptr(), tokens.data_ptr(), d_table.data_ptr(), work.data_ptr(),
+                                      work.numel()), where)
 
     @_on_own_stream
     def embed_backward(self, d_out: torch.Tensor, tokens: torch.Tensor, rows: int, scale: float = 1.0, first_row: int = 0,
                        dtype: torch.dtype | None = None) -> torch.Tensor:
         """The gradient [rows, dim] of the table, in d_out's type or `dtype`."""
-        d_table = torch.empty((rows, d_out.shape[1]), dtype=dtype or d_out.dtype, device=self.torch_device)
+        d_table = d_out.new_empty((rows, d_out.shape[-1]), dtype=dtype)
         self.embed_backward_into(d_out, tokens, d_table, scale, first_row)
         return d_table
 
     @staticmethod
     def embed_backward_bytes(tokens: int, rows: int, dim: int) -> int:
         """Bytes of the work buffer that embed_backward_into takes."""
-        return _lib.ps_embed_backward_bytes(_EmbedDesc(tokens, 0, rows, dim, dim, dim, 1.0, 0, 0, 8, 0))
+        return _lib.ps_embed_backward_bytes(_EMBED_DESC(tokens, 0, rows, dim, dim, dim, 1.0, 0, 0, 8, 0))
 
-    @_on_own_stream
-    def _work(self, work: torch.Tensor | None, need: int, where: str) -> torch.Tensor:
-        if work is None:                # (freed when the call returns: torch gives it out again on this stream only)
-            return torch.empty(max(need, 1), dtype=torch.uint8, device=self.torch_device)
-        if work.device != self.torch_device or work.dtype != torch.uint8 or not work.is_contiguous():
-            self._refuse(E_RANGE, where, f"work has to be a contiguous uint8 tensor on {self.torch_device}")
-        return work
-
-    def _heads(self, t: torch.Tensor, where: str, name: str, shape, dtype) -> _Heads:
-        if t.device != self.torch_device:
-            self._refuse(E_RANGE, where, f"{name} is on {t.device}, the context on {self.torch_device}")
-        if t.shape != shape or t.dtype != dtype:
-            self._refuse(E_RANGE, where, f"{name} is {t.dtype} of {tuple(t.shape)}, wanted {dtype} of {tuple(shape)}")
+    def _heads(self, t: torch.Tensor, where: str, name: str, shape, dtype) -> bytes:
+        if t.shape != shape or t.dtype != dtype or t.get_device() != self.device:
+            self._refuse(E_RANGE, where, f"{name} is {t.dtype} of {tuple(t.shape)} on {t.device}, wanted {dtype} of "
+                         f"{tuple(shape)} on device {self.device}")
         b, n, h, d = t.stride()
-        if d != 1:
+        if d != 1 and shape[3] > 1:
             self._refuse(E_ALIGN, where, f"{name}'s last dimension is not contiguous")
-        return _Heads(t.data_ptr(), b, n, h)
+        return _HEADS(t.data_ptr(), b, n, h)
 
     def _attention(self, q, k, where, scale, causal, q_lens, k_lens, lse):
-        """The shape, the tensors' expected shapes, and the small arrays' pointers."""
+        """The shape's bytes, the shape of q and of k, and the lengths' pointers."""
         if q.dim() != 4 or k.dim() != 4 or q.dtype not in _DTYPE:
             self._refuse(E_RANGE, where, "q and k are [batch, len, heads, dim] of a 16-bit type")
-        batch, q_len, heads, dim = q.shape
-        k_len, kv_heads = k.shape[1], k.shape[2]
-        shape = _AttentionShape(batch, q_len, k_len, heads, kv_heads, dim, _DTYPE[q.dtype], 1 if causal else 0,
-                                dim ** -0.5 if scale is None else scale, 0)
+        queries, (_, k_len, kv_heads, _) = q.shape, k.shape
+        batch, q_len, heads, dim = queries
         for name, lens in (("q_lens", q_lens), ("k_lens", k_lens)):
-            if lens is not None and (lens.device != self.torch_device or lens.dtype != torch.int32 or lens.shape != (batch,)
+            if lens is not None and (lens.dtype != torch.int32 or lens.shape != (batch,) or lens.get_device() != self.device
                                      or not lens.is_contiguous()):
-                self._refuse(E_RANGE, where, f"{name} has to be {batch} contiguous int32 on {self.torch_device}")
-        if lse.device != self.torch_device or lse.dtype != torch.float32 or lse.shape != (batch, heads, q_len) \
+                self._refuse(E_RANGE, where, f"{name} has to be {batch} contiguous int32 on device {self.device}")
+        if lse.dtype != torch.float32 or lse.shape != (batch, heads, q_len) or lse.get_device() != self.device \
                 or not lse.is_contiguous():
-            self._refuse(E_RANGE, where, f"lse has to be contiguous float32 [batch, heads, q_len] on {self.torch_device}")
-        return (shape, (batch, k_len, kv_heads, dim), None if q_lens is None else q_lens.data_ptr(),
+            self._refuse(E_RANGE, where, f"lse has to be contiguous float32 [batch, heads, q_len] on device {self.device}")
+        shape = _ATTENTION_SHAPE(batch, q_len, k_len, heads, kv_heads, dim, _DTYPE[q.dtype], 1 if causal else 0,
+                                 (dim or 1) ** -0.5 if scale is None else scale, 0)
+        return (shape, queries, (batch, k_len, kv_heads, dim), None if q_lens is None else q_lens.data_ptr(),
                 None if k_lens is None else k_lens.data_ptr())
 
     def attention_forward_into(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
                                scale: float | None = None, causal: bool = True, q_lens: torch.Tensor | None = None,
                                k_lens: torch.Tensor | None = None):
         """ps_attention_forward on [batch, len, heads, dim] of any strides; scale defaults to dim ** -0.5."""
-        where = "ps_attention_forward"
-        shape, keys, ql, kl = self._attention(q, k, where, scale, causal, q_lens, k_lens, lse)
+        where, dtype = "ps_attention_forward", q.dtype
+        shape, qs, ks, ql, kl = self._attention(q, k, where, scale, causal, q_lens, k_lens, lse)
         _check(_lib.ps_attention_forward(
-            self._h, shape, self._heads(q, where, "q", q.shape, q.dtype), self._heads(k, where, "k", keys, q.dtype),
-            self._heads(v, where, "v", keys, q.dtype), self._heads(out, where, "out", q.shape, q.dtype), lse.data_ptr(), ql, kl),
-            where)
+            self._h, shape, self._heads(q, where, "q", qs, dtype), self._heads(k, where, "k", ks, dtype),
+            self._heads(v, where, "v", ks, dtype), self._heads(out, where, "out", qs, dtype), lse.data_ptr(), ql, kl), where)
 
     @_on_own_stream
     def attention_forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float | None = None,
                           causal: bool = True, q_lens: torch.Tensor | None = None, k_lens: torch.Tensor | None = None):
         """(out [batch, q_len, heads, dim], lse [batch, heads, q_len])."""
-        out = torch.empty(q.shape, dtype=q.dtype, device=self.torch_device)
-        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=self.torch_device)
+        if q.dim() != 4:
+            self._refuse(E_RANGE, "ps_attention_forward", "q has to be [batch, len, heads, dim]")
+        shape = q.shape
+        out = q.new_empty(shape)
+        lse = q.new_empty((shape[0], shape[2], shape[1]), dtype=torch.float32)
         self.attention_forward_into(q, k, v, out, lse, scale, causal, q_lens, k_lens)
         return out, lse
 
@@ -494,30 +483,30 @@ class Context:
                                 scale: float | None = None, causal: bool = True, q_lens: torch.Tensor | None = None,
                                 k_lens: torch.Tensor | None = None, work: torch.Tensor | None = None):
         """ps_attention_backward: gradients of q, k and v from what the forward pass took and gave.
-        `work`: a uint8 buffer of ps_attention_backward_bytes; without it one is allocated for the call."""
-        where = "ps_attention_backward"
-        shape, keys, ql, kl = self._attention(q, k, where, scale, causal, q_lens, k_lens, lse)
+        `work`: a uint8 buffer of attention_backward_bytes; without it one is allocated for the call."""
+        where, dtype = "ps_attention_backward", q.dtype
+        shape, qs, ks, ql, kl = self._attention(q, k, where, scale, causal, q_lens, k_lens, lse)
         work = self._work(work, _lib.ps_attention_backward_bytes(shape), where)
         _check(_lib.ps_attention_backward(
-            self._h, shape, self._heads(q, where, "q", q.shape, q.dtype), self._heads(k, where, "k", keys, q.dtype),
-            self._heads(v, where, "v", keys, q.dtype), self._heads(out, where, "out", q.shape, q.dtype), lse.data_ptr(),
-            self._heads(d_out, where, "d_out", q.shape, q.dtype), self._heads(d_q, where, "d_q", q.shape, q.dtype),
-            self._heads(d_k, where, "d_k", keys, q.dtype), self._heads(d_v, where, "d_v", keys, q.dtype), ql, kl,
-            work.data_ptr(), work.numel()), where)
+            self._h, shape, self._heads(q, where, "q", qs, dtype), self._heads(k, where, "k", ks, dtype),
+            self._heads(v, where, "v", ks, dtype), self._heads(out, where, "out", qs, dtype), lse.data_ptr(),
+            self._heads(d_out, where, "d_out", qs, dtype), self._heads(d_q, where, "d_q", qs, dtype),
+            self._heads(d_k, where, "d_k", ks, dtype), self._heads(d_v, where, "d_v", ks, dtype), ql, kl, work.data_ptr(),
+            work.numel()), where)
 
     @_on_own_stream
     def attention_backward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
                            d_out: torch.Tensor, scale: float | None = None, causal: bool = True,
                            q_lens: torch.Tensor | None = None, k_lens: torch.Tensor | None = None):
         """(d_q, d_k, d_v), contiguous."""
-        d_q, d_k, d_v = (torch.empty(t.shape, dtype=q.dtype, device=self.torch_device) for t in (q, k, v))
+        d_q, d_k, d_v = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
         self.attention_backward_into(q, k, v, out, lse, d_out, d_q, d_k, d_v, scale, causal, q_lens, k_lens)
         return d_q, d_k, d_v
 
     @staticmethod
     def attention_backward_bytes(batch: int, q_len: int, k_len: int, heads: int, kv_heads: int, dim: int) -> int:
         """Bytes of the work buffer that attention_backward_into takes."""
-        return _lib.ps_attention_backward_bytes(_AttentionShape(batch, q_len, k_len, heads, kv_heads, dim, 1, 0, 1.0, 0))
+        return _lib.ps_attention_backward_bytes(_ATTENTION_SHAPE(batch, q_len, k_len, heads, kv_heads, dim, 1, 0, 1.0, 0))
 
     def int_peak(self, blocks: int, iters: int, sink: torch.Tensor) -> int:
         ops = C.c_uint64()

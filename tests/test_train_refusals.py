@@ -8,6 +8,26 @@ import torch
 
 import paper_2601_02311_b200.ps as ps
 
+
+class DropoutDesc(C.Structure):
+    _fields_ = [(n, C.c_uint64) for n in ("rows", "cols", "x_stride", "residual_stride", "y_stride", "seed", "stream", "first", "pitch")] + \
+        [("p", C.c_double), ("dtype", C.c_uint32), ("pad", C.c_uint32)]
+
+
+class EmbedDesc(C.Structure):
+    _fields_ = [(n, C.c_uint64) for n in ("tokens", "first_row", "rows", "dim", "table_stride", "out_stride")] + \
+        [("scale", C.c_double)] + [(n, C.c_uint32) for n in ("dtype", "grad_dtype", "token_bytes", "accumulate")]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_uint64), ("token_stride", C.c_uint64), ("head_stride", C.c_uint64)]
+
+
+class AttentionShape(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("batch", "q_len", "k_len", "heads", "kv_heads", "dim", "dtype", "causal")] + \
+        [("scale", C.c_float), ("pad", C.c_uint32)]
+
+
 FAKE = C.create_string_buffer(4096)
 CTX = C.cast(FAKE, C.c_void_p)
 BUF = C.create_string_buffer(1 << 16)
@@ -19,7 +39,7 @@ def dropout(**kw):
     ptr = dict(ctx=CTX, x=AT, residual=None, y=AT + 4096)
     for k, v in kw.items():
         (ptr if k in ptr else args)[k] = v
-    return ps._lib.ps_dropout(ptr["ctx"], ps._DropoutDesc(**args), ptr["x"], ptr["residual"], ptr["y"])
+    return ps._lib.ps_dropout(ptr["ctx"], C.byref(DropoutDesc(**args)), ptr["x"], ptr["residual"], ptr["y"])
 
 
 @pytest.mark.parametrize("change, code", [
@@ -49,8 +69,8 @@ def embed(backward=False, **kw):
     for k, v in kw.items():
         (ptr if k in ptr else args)[k] = v
     if not backward:
-        return ps._lib.ps_embed_forward(ptr["ctx"], ps._EmbedDesc(**args), ptr["table"], ptr["tokens_at"], ptr["out"])
-    return ps._lib.ps_embed_backward(ptr["ctx"], ps._EmbedDesc(**args), ptr["out"], ptr["tokens_at"], ptr["table"], ptr["work"],
+        return ps._lib.ps_embed_forward(ptr["ctx"], C.byref(EmbedDesc(**args)), ptr["table"], ptr["tokens_at"], ptr["out"])
+    return ps._lib.ps_embed_backward(ptr["ctx"], C.byref(EmbedDesc(**args)), ptr["out"], ptr["tokens_at"], ptr["table"], ptr["work"],
                                      ptr["work_bytes"])
 
 
@@ -93,8 +113,8 @@ def attention(backward=False, **kw):
             heads[k] = None
         else:
             (ptr if k in ptr else args)[k] = v
-    h = {n: None if v is None else C.byref(ps._Heads(*[x or None if i == 0 else x for i, x in enumerate(v)])) for n, v in heads.items()}
-    shape = ps._AttentionShape(**args)
+    h = {n: None if v is None else C.byref(Heads(*[x or None if i == 0 else x for i, x in enumerate(v)])) for n, v in heads.items()}
+    shape = C.byref(AttentionShape(**args))
     if not backward:
         return ps._lib.ps_attention_forward(ptr["ctx"], shape, h["q"], h["k"], h["v"], h["out"], ptr["lse"], ptr["q_lens"], ptr["k_lens"])
     return ps._lib.ps_attention_backward(ptr["ctx"], shape, h["q"], h["k"], h["v"], h["out"], ptr["lse"], h["d_out"], h["d_q"],
@@ -137,7 +157,7 @@ def test_attention_of_nothing_is_done():
 @pytest.fixture
 def ctx():
     c = ps.Context.__new__(ps.Context)
-    c.torch_device, c.device, c.stream, c._h = torch.device("cpu"), 0, None, None
+    c.torch_device, c.device, c.stream, c._h = torch.device("cpu"), -1, None, None     # a host tensor's device is -1
     return c
 
 
@@ -156,7 +176,9 @@ def test_binding_refuses_shapes_types_and_strides(ctx):
     refused(ps.E_ALIGN, ctx.dropout_into, x.t(), x.t(), 0.1, 1)
     refused(ps.E_RANGE, ctx.dropout_into, x, x, 0.1, -1)
     refused(ps.E_RANGE, ctx.dropout_into, x, x, 0.1, 1, first=-4)
-    refused(ps.E_RANGE, ctx.dropout_into, x.to("meta"), x, 0.1, 1)
+    ctx.device = 0                                                  # and another device's tensor is refused
+    refused(ps.E_RANGE, ctx.dropout_into, x, x.clone(), 0.1, 1)
+    ctx.device = -1
     tokens = torch.zeros(3, dtype=torch.int64)
     refused(ps.E_RANGE, ctx.embed_forward_into, x, tokens.short(), torch.zeros(3, 8))
     refused(ps.E_RANGE, ctx.embed_forward_into, x, tokens, torch.zeros(4, 8))
