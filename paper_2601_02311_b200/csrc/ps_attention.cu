@@ -375,23 +375,34 @@ __global__ void __launch_bounds__(256) k_rows(const ps_heads d_out, const ps_hea
     atomicMax(a.norms + 2 * (b * a.kv_heads + (query ? h / (a.heads / a.kv_heads) : h)) + (query ? 0 : 1), __float_as_uint(norm));
 }
 
+// Both kernels of the backward pass let their two groups of warps take turns: tile pairs are numbered, a group has the even
+// ones and the other the odd ones, each with a buffer of 128 columns of tensor memory of its own, a thread a row.  A
+// pair's buffer holds S, then what its products leave of P, then dP, then dS.  While one group works the tensor cores
+// multiply for the other; the products are started in an order fixed by the numbers.
+//
+// Shared memory is full (224 KB of tiles for D = 128), so barriers and vectors share what is behind the tiles.
+struct Shared {
+  u64 bars[24];
+  u32 tmem_at;
+};
+
 // A block owns 128 keys of a key head and walks the queries that see them, through all query heads that share it.  Scores are
 // transposed: S^T = K Q^T has a key a lane, so P^T and dS^T are left operands in tensor memory, and Q and dO serve as right
-// operands of both kinds from one copy.  Tensor memory (D = 128): S^T, dP^T, dV and dK, 128 columns each.  Order of the products:
-//   dV += P^T dO (i), S^T (i + 1)   while the groups take dS of i
-//   dK += dS^T Q (i), dP^T (i + 1)  while the groups take P of i + 1
-// The two groups of warps share each tile pair: a thread has a key and 64 of the 128 queries.
+// operands of both kinds from one copy.  Tensor memory (D = 128): the two buffers, dV and dK, 128 columns each.
+// Products: S S | dV dP, dV dP | dK S, dK S | ..., so that a buffer's P is used up before dP is written over it.
+// Q has three slots, since S of pair x + 2 follows on dK of pair x; dO, with two, is free after dP.
 template <class T, int D>
 __global__ void __launch_bounds__(THREADS, 1)
 k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
-  constexpr u32 TILE = PANEL * (D / 64), VECTORS = 2 * ROWS * 4;
-  __shared__ u64 bars[16];
-  __shared__ u32 tmem_at;
-  const u32 k_tile = tiles_begin(), v_tile = k_tile + TILE, q_ring = v_tile + TILE, do_ring = q_ring + 2 * TILE,
-            vectors = do_ring + 2 * TILE;
-  const u32 kv_full = smem_address(bars), q_full = kv_full + 8, q_empty = q_full + 16, do_full = q_empty + 16, do_empty = do_full + 16,
-            s_full = do_empty + 16, p_ready = s_full + 8, dp_full = p_ready + 8, ds_ready = dp_full + 8, done = ds_ready + 8;
+  constexpr u32 TILE = PANEL * (D / 64), VECTOR = ROWS * 4;
+  extern __shared__ __align__(1024) unsigned char shared[];
+  const u32 k_tile = smem_address(shared), v_tile = k_tile + TILE, q_ring = v_tile + TILE, do_ring = q_ring + 3 * TILE,
+            lse_ring = do_ring + 2 * TILE, delta_ring = lse_ring + 3 * VECTOR;
+  Shared& sh = *reinterpret_cast<Shared*>(shared + 7 * TILE + 5 * VECTOR);
+  const u32 kv_full = smem_address(sh.bars), q_full = kv_full + 8, q_empty = q_full + 24, do_full = q_empty + 24, do_empty = do_full + 16,
+            delta_full = do_empty + 16, s_full = delta_full + 16, p_ready = s_full + 16, dp_full = p_ready + 16,
+            ds_ready = dp_full + 16, done = ds_ready + 16;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
   // (under the causal mask the first keys have the most queries)
@@ -401,168 +412,102 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   const int first = a.causal ? max(0, j0 - l.m + l.n) / ROWS : 0, last = (l.n + ROWS - 1) / ROWS;     // tiles of queries
   const int walk = j0 < l.m ? max(0, last - first) : 0, total = walk * group;
 
-  if (warp == MMA_WARP) tmem_alloc(smem_address(&tmem_at), 512);
+  if (warp == MMA_WARP) tmem_alloc(smem_address(&sh.tmem_at), 512);
   if (threadIdx.x == 0) {
     barrier_init(kv_full, 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 3; ++i) {
       barrier_init(q_full + 8 * i, 1);
       barrier_init(q_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
       barrier_init(do_full + 8 * i, 1);
       barrier_init(do_empty + 8 * i, 1);
+      barrier_init(delta_full + 8 * i, 1);
+      barrier_init(s_full + 8 * i, 1);
+      barrier_init(p_ready + 8 * i, 4);
+      barrier_init(dp_full + 8 * i, 1);
+      barrier_init(ds_ready + 8 * i, 4);
     }
-    barrier_init(s_full, 1);
-    barrier_init(p_ready, 8);
-    barrier_init(dp_full, 1);
-    barrier_init(ds_ready, 8);
     barrier_init(done, 1);
     fence_barrier_init();
   }
   fence_before();
   __syncthreads();
   fence_after();
-  const u32 tmem = tmem_at, tmem_s = tmem, tmem_dp = tmem + ROWS, tmem_dv = tmem + 2 * ROWS, tmem_dk = tmem_dv + D;
+  const u32 tmem = sh.tmem_at, tmem_dv = tmem + 2 * ROWS, tmem_dk = tmem_dv + D;
   Waiter w(a.status);
 
-  if (warp == COPY_WARP) {
-    if (lane == 0 && total > 0) {
-      barrier_expect(kv_full, 2 * TILE);
-      load_tile<D>(k_tile, &map_k, kh, j0, b, kv_full);
-      load_tile<D>(v_tile, &map_v, kh, j0, b, kv_full);
-      for (int x = 0; x < total; ++x) {
-        const int slot = x & 1, parity = (x >> 1 & 1) ^ 1, h = kh * group + x / walk, i0 = (first + x % walk) * ROWS;
-        const u64 at = ((u64)b * a.heads + h) * a.padded + i0;
-        w.wait(q_empty + 8 * slot, parity);
-        if (w.dead) break;
-        barrier_expect(q_full + 8 * slot, TILE + VECTORS);
-        load_tile<D>(q_ring + slot * TILE, &map_q, h, i0, b, q_full + 8 * slot);
-        load_bytes(vectors + slot * VECTORS, a.lse2 + at, ROWS * 4, q_full + 8 * slot);
-        load_bytes(vectors + slot * VECTORS + ROWS * 4, a.delta + at, ROWS * 4, q_full + 8 * slot);
-        w.wait(do_empty + 8 * slot, parity);
-        if (w.dead) break;
-        barrier_expect(do_full + 8 * slot, TILE);
-        load_tile<D>(do_ring + slot * TILE, &map_do, h, i0, b, do_full + 8 * slot);
-      }
-    }
-  } else if (warp == MMA_WARP) {
-    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false), ins_acc = instruction<T>(D, true, false);
-    // queries behind the sequence's end, in its last tile
-    auto pad_from = [&](int x) {
-      const int i0 = (first + x % walk) * ROWS;
-      return l.n < a.q_len && i0 + ROWS > l.n ? l.n - i0 : ROWS;
-    };
-    auto scores = [&](int x) {
-      const u32 q = q_ring + (x & 1) * TILE;
-      w.wait_together(q_full + 8 * (x & 1), x >> 1 & 1);
-      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) mma_smem(tmem_s, desc_along(k_tile, s), desc_along(q, s), ins_s, s > 0);
-        commit(s_full);
-      }
-    };
-    auto d_probabilities = [&](int x) {
-      const u32 d = do_ring + (x & 1) * TILE;
-      w.wait_together(do_full + 8 * (x & 1), x >> 1 & 1);
-      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) mma_smem(tmem_dp, desc_along(v_tile, s), desc_along(d, s), ins_dp, s > 0);
-        commit(dp_full);
-      }
-    };
-    if (total > 0) {
-      w.wait_together(kv_full, 0);
-      scores(0);
-      d_probabilities(0);
-    }
-    for (int x = 0; x < total; ++x) {
-      const int slot = x & 1;
-      w.wait_together(p_ready, x & 1);
-      fence_after();
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < ROWS / 16; ++s)
-          mma_tmem(tmem_dv, tmem_s + (s / 4) * 64 + (s % 4) * 8, desc_across(do_ring + slot * TILE, s), ins_acc, x > 0 || s > 0);
-        commit(do_empty + 8 * slot);
-      }
-      __syncwarp();
-      if (x + 1 < total) scores(x + 1);
-      w.wait_together(ds_ready, x & 1);
-      fence_after();
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < ROWS / 16; ++s)
-          mma_tmem(tmem_dk, tmem_dp + (s / 4) * 64 + (s % 4) * 8, desc_across(q_ring + slot * TILE, s), ins_acc, x > 0 || s > 0);
-        commit(q_empty + 8 * slot);
-        if (x + 1 == total) commit(done);
-      }
-      __syncwarp();
-      if (x + 1 < total) d_probabilities(x + 1);
-    }
-  } else if (warp < COPY_WARP) {
-    const int half = warp / 4, j = j0 + threadIdx.x % ROWS;
-    const u32 lanes = (u32)(warp % 4 * 32) << 16, s_at = tmem_s + lanes + 64 * half, dp_at = tmem_dp + lanes + 64 * half;
+  if (warp < COPY_WARP) {
+    take_registers<TAKEN>();
+    const int mine = warp / 4, j = j0 + threadIdx.x % ROWS;
+    const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
     // this key's first query; the first query that all of the tile's keys have
     const int begin = j >= l.m ? 0x7fffffff : a.causal ? j - l.m + l.n : 0;
     const int whole = j0 + ROWS > l.m ? 0x7fffffff : a.causal ? j0 + ROWS - 1 - l.m + l.n : 0;
     const float factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
-    for (int x = 0; x < total; ++x) {
-      const int slot = x & 1, i0 = (first + x % walk) * ROWS;
-      const u32 lse_at = vectors + slot * VECTORS + 64 * half * 4, delta_at = lse_at + ROWS * 4;
-      w.wait(q_full + 8 * slot, x >> 1 & 1);
-      w.wait(s_full, x & 1);
+    for (int x = mine; x < total; x += 2) {
+      const int i0 = (first + x % walk) * ROWS, turn = x >> 1 & 1;
+      const u32 lse_at = lse_ring + x % 3 * VECTOR, delta_at = delta_ring + mine * VECTOR;
+      w.wait(q_full + 8 * (x % 3), x / 3 & 1);
+      w.wait(s_full + 8 * mine, turn);
       fence_after();
-      float p[2][32];
+      u32 p[4][32];
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32 s[32], out[16];
-        tmem_load32(s, s_at + 32 * q);
-        wait_loads();
+      for (int q = 0; q < 4; ++q) tmem_load32(p[q], at + 32 * q);
+      wait_loads();
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
 #pragma unroll
         for (int e = 0; e < 32; e += 4) {
-          float o[4];
-          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o[0]), "=f"(o[1]), "=f"(o[2]), "=f"(o[3]) : "r"(lse_at + (32 * q + e) * 4));
+          float off[4];
+          load_shared4(off, lse_at + (32 * q + e) * 4);
 #pragma unroll
-          for (int f = 0; f < 4; ++f) p[q][e + f] = exp2_fast(fmaf(__uint_as_float(s[e + f]), a.c, -o[f]));
+          for (int f = 0; f < 4; ++f) p[q][e + f] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(p[q][e + f]), a.c, -off[f])));
         }
         if (i0 < whole) {
-          const int skip = begin - i0 - 64 * half - 32 * q;
+          const int skip = begin - i0 - 32 * q;
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (e < skip) p[q][e] = 0.f;
+            if (e < skip) p[q][e] = 0;
         }
+        u32 out[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) out[e] = pack<T>(p[q][2 * e], p[q][2 * e + 1]);
-        tmem_store16(s_at + 16 * q, out);
+        for (int e = 0; e < 16; ++e) out[e] = pack<T>(__uint_as_float(p[q][2 * e]), __uint_as_float(p[q][2 * e + 1]));
+        tmem_store16(at + 16 * q, out);
       }
       wait_stores();
       fence_before();
       __syncwarp();
-      if (lane == 0) barrier_arrive(p_ready);
-      w.wait(dp_full, x & 1);
+      if (lane == 0) barrier_arrive(p_ready + 8 * mine);
+      w.wait(delta_full + 8 * mine, turn);
+      w.wait(dp_full + 8 * mine, turn);
       fence_after();
+      u32 d[2][16];
+      tmem_load16(d[0], at);
+      wait_loads();
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32 s[32], out[16];
-        tmem_load32(s, dp_at + 32 * q);
-        wait_loads();
+      for (int q = 0; q < 8; ++q) {
+        if (q < 7) tmem_load16(d[(q + 1) & 1], at + 16 * (q + 1));
+        u32 out[8];
 #pragma unroll
-        for (int e = 0; e < 32; e += 4) {
-          float o[4];
-          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o[0]), "=f"(o[1]), "=f"(o[2]), "=f"(o[3]) : "r"(delta_at + (32 * q + e) * 4));
+        for (int e = 0; e < 16; e += 4) {
+          float off[4];
+          load_shared4(off, delta_at + (16 * q + e) * 4);
 #pragma unroll
           for (int f = 0; f < 4; f += 2) {
-            float u = __uint_as_float(s[e + f]) - o[f], v = __uint_as_float(s[e + f + 1]) - o[f + 1];
+            const int c = 16 * (q & 1) + e + f;
+            float u = __uint_as_float(d[q & 1][e + f]) - off[f], v = __uint_as_float(d[q & 1][e + f + 1]) - off[f + 1];
             if (Range<T>::small) u *= factor, v *= factor;
-            out[(e + f) / 2] = pack<T>(p[q][e + f] * u, p[q][e + f + 1] * v);
+            out[(e + f) / 2] = pack<T>(__uint_as_float(p[q / 2][c]) * u, __uint_as_float(p[q / 2][c + 1]) * v);
           }
         }
-        tmem_store16(dp_at + 16 * q, out);
+        wait_loads();                // (dS goes over columns that have been read)
+        tmem_store8(at + 8 * q, out);
       }
       wait_stores();
       fence_before();
       __syncwarp();
-      if (lane == 0) barrier_arrive(ds_ready);
+      if (lane == 0) barrier_arrive(ds_ready + 8 * mine);
     }
     if (total > 0) {
       w.wait(done, 0);
@@ -572,8 +517,95 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
     const bool there = j < a.k_len, used = total > 0 && j < l.m;
     const int safe = min(j, a.k_len - 1);
     const float undo = Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f;
-    if (half == 0) store_row<T, D>(row_of<T>(a.d_v, b, safe, kh), tmem_dv + lanes, total > 0, there, a.dim, used ? undo : 0.f);
+    if (mine == 0) store_row<T, D>(row_of<T>(a.d_v, b, safe, kh), tmem_dv + lanes, total > 0, there, a.dim, used ? undo : 0.f);
     else store_row<T, D>(row_of<T>(a.d_k, b, safe, kh), tmem_dk + lanes, total > 0, there, a.dim, used ? a.scale / factor * undo : 0.f);
+  } else if (warp == COPY_WARP) {
+    give_registers<LEFT>();
+    if (lane == 0 && total > 0) {
+      barrier_expect(kv_full, 2 * TILE);
+      load_tile<D>(k_tile, &map_k, kh, j0, b, kv_full);
+      load_tile<D>(v_tile, &map_v, kh, j0, b, kv_full);
+      for (int x = 0; x < total; ++x) {
+        const int slot = x % 3, two = x & 1, h = kh * group + x / walk, i0 = (first + x % walk) * ROWS;
+        const u64 row = ((u64)b * a.heads + h) * a.padded + i0;
+        w.wait(q_empty + 8 * slot, (x / 3 & 1) ^ 1);
+        if (w.dead) break;
+        barrier_expect(q_full + 8 * slot, TILE + VECTOR);
+        load_tile<D>(q_ring + slot * TILE, &map_q, h, i0, b, q_full + 8 * slot);
+        load_bytes(lse_ring + slot * VECTOR, a.lse2 + row, VECTOR, q_full + 8 * slot);
+        w.wait(do_empty + 8 * two, (x >> 1 & 1) ^ 1);
+        if (w.dead) break;
+        barrier_expect(do_full + 8 * two, TILE);
+        load_tile<D>(do_ring + two * TILE, &map_do, h, i0, b, do_full + 8 * two);
+        // the delta before last has been read once its pair's dK is done
+        if (x >= 2) w.wait(q_empty + 8 * ((x - 2) % 3), (x - 2) / 3 & 1);
+        if (w.dead) break;
+        barrier_expect(delta_full + 8 * two, VECTOR);
+        load_bytes(delta_ring + two * VECTOR, a.delta + row, VECTOR, delta_full + 8 * two);
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    give_registers<LEFT>();
+    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false), ins_acc = instruction<T>(D, true, false);
+    // queries behind the sequence's end, in its last tile
+    auto pad_from = [&](int x) {
+      const int i0 = (first + x % walk) * ROWS;
+      return l.n < a.q_len && i0 + ROWS > l.n ? l.n - i0 : ROWS;
+    };
+    auto scores = [&](int x) {
+      const u32 q = q_ring + x % 3 * TILE;
+      w.wait_together(q_full + 8 * (x % 3), x / 3 & 1);
+      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) mma_smem(tmem + (x & 1) * ROWS, desc_along(k_tile, s), desc_along(q, s), ins_s, s > 0);
+        commit(s_full + 8 * (x & 1));
+      }
+      __syncwarp();
+    };
+    if (total > 0) {
+      w.wait_together(kv_full, 0);
+      scores(0);
+      if (total > 1) scores(1);
+    }
+    for (int x0 = 0; x0 < total; x0 += 2) {
+      const int turn = x0 >> 1 & 1, end = min(x0 + 2, total);
+      for (int x = x0; x < end; ++x) {
+        const int two = x & 1;
+        const u32 d = do_ring + two * TILE;
+        w.wait_together(do_full + 8 * two, turn);
+        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+        w.wait_together(p_ready + 8 * two, turn);
+        fence_after();
+        if (lane == 0 && !w.dead) {
+#pragma unroll
+          for (int s = 0; s < ROWS / 16; ++s)
+            mma_tmem(tmem_dv, tmem + two * ROWS + 8 * s, desc_across(d, s), ins_acc, x > 0 || s > 0);
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s) mma_smem(tmem + two * ROWS, desc_along(v_tile, s), desc_along(d, s), ins_dp, s > 0);
+          commit(dp_full + 8 * two);
+          commit(do_empty + 8 * two);
+        }
+        __syncwarp();
+      }
+      for (int x = x0; x < end; ++x) {
+        const int two = x & 1;
+        const u32 q = q_ring + x % 3 * TILE;
+        w.wait_together(ds_ready + 8 * two, turn);
+        fence_after();
+        if (lane == 0 && !w.dead) {
+#pragma unroll
+          for (int s = 0; s < ROWS / 16; ++s)
+            mma_tmem(tmem_dk, tmem + two * ROWS + 8 * s, desc_across(q, s), ins_acc, x > 0 || s > 0);
+          commit(q_empty + 8 * (x % 3));
+          if (x + 1 == total) commit(done);
+        }
+        __syncwarp();
+        if (x + 2 < total) scores(x + 2);
+      }
+    }
+  } else {
+    give_registers<LEFT>();
   }
   linger(w.dead);
   fence_before();
@@ -584,154 +616,103 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   }
 }
 
-// A block owns 128 queries of a head and walks the keys they see.  Tensor memory (D = 128): two buffers of S (the next
-// scores are there when the groups come to them; dS is written over its own S), dP and dQ.  The two groups share each tile
-// pair: a thread has a query and 64 of the 128 keys.
+// A block owns 128 queries of a head and walks the keys they see.  Tensor memory (D = 128): the two buffers and dQ, 128 columns
+// each.  P stays in registers, so dP may be written over S as soon as S has been read.
+// Products: S S | dP dP | dQ S, dQ S | dP dP | ...  K has three slots, V two, as Q and dO above.
 template <class T, int D>
 __global__ void __launch_bounds__(THREADS, 1)
 k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
   constexpr u32 TILE = PANEL * (D / 64);
-  __shared__ u64 bars[16];
-  __shared__ u32 tmem_at;
-  const u32 q_tile = tiles_begin(), do_tile = q_tile + TILE, k_ring = do_tile + TILE, v_ring = k_ring + 2 * TILE;
-  const u32 q_full = smem_address(bars), k_full = q_full + 8, k_empty = k_full + 16, v_full = k_empty + 16, v_empty = v_full + 16,
-            s_full = v_empty + 16, dp_full = s_full + 16, ds_ready = dp_full + 8, done = ds_ready + 8;
+  extern __shared__ __align__(1024) unsigned char shared[];
+  const u32 q_tile = smem_address(shared), do_tile = q_tile + TILE, k_ring = do_tile + TILE, v_ring = k_ring + 3 * TILE;
+  Shared& sh = *reinterpret_cast<Shared*>(shared + 7 * TILE);
+  const u32 q_full = smem_address(sh.bars), k_full = q_full + 8, k_empty = k_full + 24, v_full = k_empty + 24, v_empty = v_full + 16,
+            s_full = v_empty + 16, s_read = s_full + 16, dp_full = s_read + 16, ds_ready = dp_full + 16, done = ds_ready + 16;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
-  const int per = a.heads * a.batch, n_tiles = (a.q_len + ROWS - 1) / ROWS, at = blockIdx.x / per;
-  const int q0 = (a.causal ? n_tiles - 1 - at : at) * ROWS, b = blockIdx.x % per / a.heads, h = blockIdx.x % a.heads;
+  const int per = a.heads * a.batch, n_tiles = (a.q_len + ROWS - 1) / ROWS, order = blockIdx.x / per;
+  const int q0 = (a.causal ? n_tiles - 1 - order : order) * ROWS, b = blockIdx.x % per / a.heads, h = blockIdx.x % a.heads;
   const int kh = h / (a.heads / a.kv_heads);
   const Lengths l = lengths_of(a, b);
   const int total = key_tiles(a, l, q0);
 
-  if (warp == MMA_WARP) tmem_alloc(smem_address(&tmem_at), 512);
+  if (warp == MMA_WARP) tmem_alloc(smem_address(&sh.tmem_at), 512);
   if (threadIdx.x == 0) {
     barrier_init(q_full, 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 3; ++i) {
       barrier_init(k_full + 8 * i, 1);
       barrier_init(k_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
       barrier_init(v_full + 8 * i, 1);
       barrier_init(v_empty + 8 * i, 1);
       barrier_init(s_full + 8 * i, 1);
+      barrier_init(s_read + 8 * i, 4);
+      barrier_init(dp_full + 8 * i, 1);
+      barrier_init(ds_ready + 8 * i, 4);
     }
-    barrier_init(dp_full, 1);
-    barrier_init(ds_ready, 8);
     barrier_init(done, 1);
     fence_barrier_init();
   }
   fence_before();
   __syncthreads();
   fence_after();
-  const u32 tmem = tmem_at, tmem_dp = tmem + 2 * ROWS, tmem_dq = tmem + 3 * ROWS;
+  const u32 tmem = sh.tmem_at, tmem_dq = tmem + 2 * ROWS;
   Waiter w(a.status);
 
-  if (warp == COPY_WARP) {
-    if (lane == 0 && total > 0) {
-      barrier_expect(q_full, 2 * TILE);
-      load_tile<D>(q_tile, &map_q, h, q0, b, q_full);
-      load_tile<D>(do_tile, &map_do, h, q0, b, q_full);
-      for (int x = 0; x < total; ++x) {
-        const int slot = x & 1, parity = (x >> 1 & 1) ^ 1;
-        w.wait(k_empty + 8 * slot, parity);
-        if (w.dead) break;
-        barrier_expect(k_full + 8 * slot, TILE);
-        load_tile<D>(k_ring + slot * TILE, &map_k, kh, x * ROWS, b, k_full + 8 * slot);
-        w.wait(v_empty + 8 * slot, parity);
-        if (w.dead) break;
-        barrier_expect(v_full + 8 * slot, TILE);
-        load_tile<D>(v_ring + slot * TILE, &map_v, kh, x * ROWS, b, v_full + 8 * slot);
-      }
-    }
-  } else if (warp == MMA_WARP) {
-    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false), ins_acc = instruction<T>(D, true, false);
-    // keys behind the sequence's end, in its last tile
-    auto pad_from = [&](int x) { return l.m < a.k_len && (x + 1) * ROWS > l.m ? l.m - x * ROWS : ROWS; };
-    auto scores = [&](int x) {
-      const u32 k = k_ring + (x & 1) * TILE;
-      w.wait_together(k_full + 8 * (x & 1), x >> 1 & 1);
-      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) mma_smem(tmem + (x & 1) * ROWS, desc_along(q_tile, s), desc_along(k, s), ins_s, s > 0);
-        commit(s_full + 8 * (x & 1));
-      }
-    };
-    auto d_probabilities = [&](int x) {
-      const u32 v = v_ring + (x & 1) * TILE;
-      w.wait_together(v_full + 8 * (x & 1), x >> 1 & 1);
-      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) mma_smem(tmem_dp, desc_along(do_tile, s), desc_along(v, s), ins_dp, s > 0);
-        commit(dp_full);
-        commit(v_empty + 8 * (x & 1));
-      }
-    };
-    if (total > 0) {
-      w.wait_together(q_full, 0);
-      scores(0);
-      d_probabilities(0);
-    }
-    for (int x = 0; x < total; ++x) {
-      const int slot = x & 1;
-      if (x + 1 < total) scores(x + 1);
-      w.wait_together(ds_ready, x & 1);
-      fence_after();
-      if (x + 1 < total) d_probabilities(x + 1);
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < ROWS / 16; ++s)
-          mma_tmem(tmem_dq, tmem + slot * ROWS + (s / 4) * 64 + (s % 4) * 8, desc_across(k_ring + slot * TILE, s), ins_acc, x > 0 || s > 0);
-        commit(k_empty + 8 * slot);
-        if (x + 1 == total) commit(done);
-      }
-      __syncwarp();
-    }
-  } else if (warp < COPY_WARP) {
-    const int half = warp / 4, i = q0 + threadIdx.x % ROWS, end = end_of(a, l, i);
-    const u32 lanes = (u32)(warp % 4 * 32) << 16, dp_at = tmem_dp + lanes + 64 * half;
+  if (warp < COPY_WARP) {
+    take_registers<TAKEN>();
+    const int mine = warp / 4, i = q0 + threadIdx.x % ROWS, end = end_of(a, l, i);
+    const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
     const int masked = (q0 + ROWS > l.n ? 0 : end_of(a, l, q0)) / ROWS;
-    const u64 at = ((u64)b * a.heads + h) * a.padded + i;
-    const float off = a.lse2[at], delta = a.delta[at], factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
-    for (int x = 0; x < total; ++x) {
-      const u32 s_at = tmem + lanes + (x & 1) * ROWS + 64 * half;
-      w.wait(s_full + 8 * (x & 1), x >> 1 & 1);
+    const u64 row = ((u64)b * a.heads + h) * a.padded + i;
+    const float off = a.lse2[row], delta = a.delta[row], factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
+    for (int x = mine; x < total; x += 2) {
+      const int turn = x >> 1 & 1;
+      w.wait(s_full + 8 * mine, turn);
       fence_after();
-      float p[2][32];
+      u32 p[4][32];
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32 s[32];
-        tmem_load32(s, s_at + 32 * q);
-        wait_loads();
+      for (int q = 0; q < 4; ++q) tmem_load32(p[q], at + 32 * q);
+      wait_loads();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) barrier_arrive(s_read + 8 * mine);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) p[q][e] = exp2_fast(fmaf(__uint_as_float(s[e]), a.c, -off));
+      for (int q = 0; q < 4; ++q) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) p[q][e] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(p[q][e]), a.c, -off)));
         if (x >= masked) {
-          const int left = end - x * ROWS - 64 * half - 32 * q;
+          const int left = end - x * ROWS - 32 * q;
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (e >= left) p[q][e] = 0.f;
+            if (e >= left) p[q][e] = 0;
         }
       }
-      w.wait(dp_full, x & 1);
+      w.wait(dp_full + 8 * mine, turn);
       fence_after();
+      u32 d[2][16];
+      tmem_load16(d[0], at);
+      wait_loads();
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32 s[32], out[16];
-        tmem_load32(s, dp_at + 32 * q);
-        wait_loads();
+      for (int q = 0; q < 8; ++q) {
+        if (q < 7) tmem_load16(d[(q + 1) & 1], at + 16 * (q + 1));
+        u32 out[8];
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          float u = __uint_as_float(s[e]) - delta, v = __uint_as_float(s[e + 1]) - delta;
+        for (int e = 0; e < 16; e += 2) {
+          const int c = 16 * (q & 1) + e;
+          float u = __uint_as_float(d[q & 1][e]) - delta, v = __uint_as_float(d[q & 1][e + 1]) - delta;
           if (Range<T>::small) u *= factor, v *= factor;
-          out[e / 2] = pack<T>(p[q][e] * u, p[q][e + 1] * v);
+          out[e / 2] = pack<T>(__uint_as_float(p[q / 2][c]) * u, __uint_as_float(p[q / 2][c + 1]) * v);
         }
-        tmem_store16(s_at + 16 * q, out);
+        wait_loads();                // (dS goes over columns that have been read)
+        tmem_store8(at + 8 * q, out);
       }
       wait_stores();
       fence_before();
       __syncwarp();
-      if (lane == 0) barrier_arrive(ds_ready);
+      if (lane == 0) barrier_arrive(ds_ready + 8 * mine);
     }
     if (total > 0) {
       w.wait(done, 0);
@@ -741,8 +722,82 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const bool there = i < a.q_len;
     const int safe = min(i, a.q_len - 1);
     const float by = off == INFINITY ? 0.f : a.scale / factor * (Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f);
-    store_row<T, D / 2>(row_of<T>(a.d_q, b, safe, h) + half * (D / 2), tmem_dq + lanes + half * (D / 2), total > 0, there,
-                        a.dim - half * (D / 2), by);
+    store_row<T, D / 2>(row_of<T>(a.d_q, b, safe, h) + mine * (D / 2), tmem_dq + lanes + mine * (D / 2), total > 0, there,
+                        a.dim - mine * (D / 2), by);
+  } else if (warp == COPY_WARP) {
+    give_registers<LEFT>();
+    if (lane == 0 && total > 0) {
+      barrier_expect(q_full, 2 * TILE);
+      load_tile<D>(q_tile, &map_q, h, q0, b, q_full);
+      load_tile<D>(do_tile, &map_do, h, q0, b, q_full);
+      for (int x = 0; x < total; ++x) {
+        const int slot = x % 3, two = x & 1;
+        w.wait(k_empty + 8 * slot, (x / 3 & 1) ^ 1);
+        if (w.dead) break;
+        barrier_expect(k_full + 8 * slot, TILE);
+        load_tile<D>(k_ring + slot * TILE, &map_k, kh, x * ROWS, b, k_full + 8 * slot);
+        w.wait(v_empty + 8 * two, (x >> 1 & 1) ^ 1);
+        if (w.dead) break;
+        barrier_expect(v_full + 8 * two, TILE);
+        load_tile<D>(v_ring + two * TILE, &map_v, kh, x * ROWS, b, v_full + 8 * two);
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    give_registers<LEFT>();
+    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false), ins_acc = instruction<T>(D, true, false);
+    // keys behind the sequence's end, in its last tile
+    auto pad_from = [&](int x) { return l.m < a.k_len && (x + 1) * ROWS > l.m ? l.m - x * ROWS : ROWS; };
+    auto scores = [&](int x) {
+      const u32 k = k_ring + x % 3 * TILE;
+      w.wait_together(k_full + 8 * (x % 3), x / 3 & 1);
+      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
+      if (lane == 0 && !w.dead) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) mma_smem(tmem + (x & 1) * ROWS, desc_along(q_tile, s), desc_along(k, s), ins_s, s > 0);
+        commit(s_full + 8 * (x & 1));
+      }
+      __syncwarp();
+    };
+    if (total > 0) {
+      w.wait_together(q_full, 0);
+      scores(0);
+      if (total > 1) scores(1);
+    }
+    for (int x0 = 0; x0 < total; x0 += 2) {
+      const int turn = x0 >> 1 & 1, end = min(x0 + 2, total);
+      for (int x = x0; x < end; ++x) {
+        const int two = x & 1;
+        const u32 v = v_ring + two * TILE;
+        w.wait_together(v_full + 8 * two, turn);
+        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
+        w.wait_together(s_read + 8 * two, turn);
+        fence_after();
+        if (lane == 0 && !w.dead) {
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s) mma_smem(tmem + two * ROWS, desc_along(do_tile, s), desc_along(v, s), ins_dp, s > 0);
+          commit(dp_full + 8 * two);
+          commit(v_empty + 8 * two);
+        }
+        __syncwarp();
+      }
+      for (int x = x0; x < end; ++x) {
+        const int two = x & 1;
+        const u32 k = k_ring + x % 3 * TILE;
+        w.wait_together(ds_ready + 8 * two, turn);
+        fence_after();
+        if (lane == 0 && !w.dead) {
+#pragma unroll
+          for (int s = 0; s < ROWS / 16; ++s)
+            mma_tmem(tmem_dq, tmem + two * ROWS + 8 * s, desc_across(k, s), ins_acc, x > 0 || s > 0);
+          commit(k_empty + 8 * (x % 3));
+          if (x + 1 == total) commit(done);
+        }
+        __syncwarp();
+        if (x + 2 < total) scores(x + 2);
+      }
+    }
+  } else {
+    give_registers<LEFT>();
   }
   linger(w.dead);
   fence_before();
@@ -798,7 +853,7 @@ Args args_of(const AttentionArgs& a) {
 
 // Tensor memory is shared by the blocks of an SM, and each takes all of it: shared memory keeps a second block away.
 u32 smem_for(int tiles, int d, u32 more) {
-  const u32 want = 1024 + tiles * PANEL * (d / 64) + more;
+  const u32 want = tiles * PANEL * (d / 64) + more;
   return want < 120 * 1024 ? 120 * 1024 : want;
 }
 template <class K>
@@ -815,7 +870,7 @@ cudaError_t forward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
   } else if (!encode(k, dtype, a.k, a.batch, a.k_len, a.kv_heads, a.dim) || !encode(v, dtype, a.v, a.batch, a.k_len, a.kv_heads, a.dim)) {
     return cudaErrorInvalidValue;
   }
-  const u32 smem = smem_for(6, D, 0), grid = (u32)((a.q_len + 2 * ROWS - 1) / (2 * ROWS)) * a.heads * a.batch;
+  const u32 smem = smem_for(6, D, 1024), grid = (u32)((a.q_len + 2 * ROWS - 1) / (2 * ROWS)) * a.heads * a.batch;
   cudaError_t e = allow(k_forward<T, D>, smem);
   if (e != cudaSuccess) return e;
   k_forward<T, D><<<grid, THREADS, smem, stream>>>(q, k, v, args_of(a));
@@ -844,13 +899,13 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   if (a.k_len) {
-    const u32 smem = smem_for(6, D, 2 * 2 * ROWS * 4);
+    const u32 smem = smem_for(7, D, 5 * ROWS * 4 + sizeof(Shared));
     if ((e = allow(k_keys<T, D>, smem)) != cudaSuccess) return e;
     k_keys<T, D><<<(u32)((a.k_len + ROWS - 1) / ROWS) * a.kv_heads * a.batch, THREADS, smem, stream>>>(q, k, v, d, r);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   if (a.q_len) {
-    const u32 smem = smem_for(6, D, 0);
+    const u32 smem = smem_for(7, D, sizeof(Shared));
     if ((e = allow(k_queries<T, D>, smem)) != cudaSuccess) return e;
     k_queries<T, D><<<(u32)(r.padded / ROWS) * a.heads * a.batch, THREADS, smem, stream>>>(q, k, v, d, r);
   }

@@ -80,6 +80,9 @@ __device__ __forceinline__ void load_bytes(u32 to, const void* from, u32 bytes, 
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void load_shared4(float (&v)[4], u32 at) {
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at));
+}
 // a warp: zeros in the rows of a tile from `first` on
 template <int D>
 __device__ __forceinline__ void clear_rows(u32 tile, int first) {
@@ -112,6 +115,14 @@ __device__ __forceinline__ void tmem_load32(u32 (&v)[32], u32 at) {
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
       "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
       : PS_R8(v, 0), PS_R8(v, 8), PS_R8(v, 16), PS_R8(v, 24) : "r"(at));
+}
+__device__ __forceinline__ void tmem_load16(u32 (&v)[16], u32 at) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : PS_R8(v, 0), PS_R8(v, 8) : "r"(at));
+}
+__device__ __forceinline__ void tmem_store8(u32 at, const u32 (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::PS_I8(v, 0), "r"(at) : "memory");
 }
 __device__ __forceinline__ void tmem_store32(u32 at, const u32 (&v)[32]) {
   asm volatile(
