@@ -248,39 +248,35 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     give_registers<LEFT>();
     const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_o = instruction<T>(D, true, false);
     auto scores = [&](int t, int j) {
-      const u32 k = ring + (2 * j % RING) * TILE;
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) mma_smem(tmem + t * ROWS, desc_along(tiles + t * TILE, s), desc_along(k, s), ins_s, s > 0);
+      multiply_along<D>(tmem + t * ROWS, tiles + t * TILE, ring + (2 * j % RING) * TILE, ins_s);
       commit(s_full + 8 * t);
     };
     if (most > 0) {
-      w.wait_together(full, 0);
+      w.wait(full, 0);
       for (int t = 0; t < 2; ++t)
         if (count[t]) {
-          w.wait_together(q_full + 8 * t, 0);
-          if (lane == 0 && !w.dead) scores(t, 0);
+          w.wait(q_full + 8 * t, 0);
+          if (elected() && !w.dead) scores(t, 0);
         }
-      if (lane == 0 && !w.dead) commit(empty);
+      if (elected() && !w.dead) commit(empty);
     }
     for (int j = 0; j < most; ++j) {
       const int x = 2 * j + 1, slot = x % RING, next = (x + 1) % RING;
       const u32 v = ring + slot * TILE;
-      w.wait_together(full + 8 * slot, x / RING & 1);
+      w.wait(full + 8 * slot, x / RING & 1);
       if (l.m < a.k_len && (j + 1) * ROWS > l.m && !w.dead) clear_rows<D>(v, l.m - j * ROWS);
-      if (j + 1 < most) w.wait_together(full + 8 * next, (x + 1) / RING & 1);
+      if (j + 1 < most) w.wait(full + 8 * next, (x + 1) / RING & 1);
       for (int t = 0; t < 2; ++t) {
         if (j >= count[t]) continue;
-        w.wait_together(p_ready + 8 * t, j & 1);
+        w.wait(p_ready + 8 * t, j & 1);
         fence_after();
-        if (lane == 0 && !w.dead) {
-#pragma unroll
-          for (int s = 0; s < ROWS / 16; ++s)
-            mma_tmem(tmem + 2 * ROWS + t * D, tmem + t * ROWS + 8 * s, desc_across(v, s), ins_o, j > 0 || s > 0);
+        if (elected() && !w.dead) {
+          multiply_across(tmem + 2 * ROWS + t * D, tmem + t * ROWS, v, ins_o, j > 0);
           if (j + 1 < count[t]) scores(t, j + 1);
           else commit(o_done + 8 * t);
         }
       }
-      if (lane == 0 && !w.dead) {
+      if (elected() && !w.dead) {
         commit(empty + 8 * slot);
         if (j + 1 < most) commit(empty + 8 * next);
       }
@@ -554,17 +550,16 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
     };
     auto scores = [&](int x) {
       const u32 q = q_ring + x % 3 * TILE;
-      w.wait_together(q_full + 8 * (x % 3), x / 3 & 1);
+      w.wait(q_full + 8 * (x % 3), x / 3 & 1);
       if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) mma_smem(tmem + (x & 1) * ROWS, desc_along(k_tile, s), desc_along(q, s), ins_s, s > 0);
+      if (elected() && !w.dead) {
+        multiply_along<D>(tmem + (x & 1) * ROWS, k_tile, q, ins_s);
         commit(s_full + 8 * (x & 1));
       }
       __syncwarp();
     };
     if (total > 0) {
-      w.wait_together(kv_full, 0);
+      w.wait(kv_full, 0);
       scores(0);
       if (total > 1) scores(1);
     }
@@ -573,16 +568,13 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       for (int x = x0; x < end; ++x) {
         const int two = x & 1;
         const u32 d = do_ring + two * TILE;
-        w.wait_together(do_full + 8 * two, turn);
+        w.wait(do_full + 8 * two, turn);
         if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
-        w.wait_together(p_ready + 8 * two, turn);
+        w.wait(p_ready + 8 * two, turn);
         fence_after();
-        if (lane == 0 && !w.dead) {
-#pragma unroll
-          for (int s = 0; s < ROWS / 16; ++s)
-            mma_tmem(tmem_dv, tmem + two * ROWS + 8 * s, desc_across(d, s), ins_acc, x > 0 || s > 0);
-#pragma unroll
-          for (int s = 0; s < D / 16; ++s) mma_smem(tmem + two * ROWS, desc_along(v_tile, s), desc_along(d, s), ins_dp, s > 0);
+        if (elected() && !w.dead) {
+          multiply_across(tmem_dv, tmem + two * ROWS, d, ins_acc, x > 0);
+          multiply_along<D>(tmem + two * ROWS, v_tile, d, ins_dp);
           commit(dp_full + 8 * two);
           commit(do_empty + 8 * two);
         }
@@ -591,12 +583,10 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       for (int x = x0; x < end; ++x) {
         const int two = x & 1;
         const u32 q = q_ring + x % 3 * TILE;
-        w.wait_together(ds_ready + 8 * two, turn);
+        w.wait(ds_ready + 8 * two, turn);
         fence_after();
-        if (lane == 0 && !w.dead) {
-#pragma unroll
-          for (int s = 0; s < ROWS / 16; ++s)
-            mma_tmem(tmem_dk, tmem + two * ROWS + 8 * s, desc_across(q, s), ins_acc, x > 0 || s > 0);
+        if (elected() && !w.dead) {
+          multiply_across(tmem_dk, tmem + two * ROWS, q, ins_acc, x > 0);
           commit(q_empty + 8 * (x % 3));
           if (x + 1 == total) commit(done);
         }
@@ -749,17 +739,16 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     auto pad_from = [&](int x) { return l.m < a.k_len && (x + 1) * ROWS > l.m ? l.m - x * ROWS : ROWS; };
     auto scores = [&](int x) {
       const u32 k = k_ring + x % 3 * TILE;
-      w.wait_together(k_full + 8 * (x % 3), x / 3 & 1);
+      w.wait(k_full + 8 * (x % 3), x / 3 & 1);
       if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
-      if (lane == 0 && !w.dead) {
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) mma_smem(tmem + (x & 1) * ROWS, desc_along(q_tile, s), desc_along(k, s), ins_s, s > 0);
+      if (elected() && !w.dead) {
+        multiply_along<D>(tmem + (x & 1) * ROWS, q_tile, k, ins_s);
         commit(s_full + 8 * (x & 1));
       }
       __syncwarp();
     };
     if (total > 0) {
-      w.wait_together(q_full, 0);
+      w.wait(q_full, 0);
       scores(0);
       if (total > 1) scores(1);
     }
@@ -768,13 +757,12 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       for (int x = x0; x < end; ++x) {
         const int two = x & 1;
         const u32 v = v_ring + two * TILE;
-        w.wait_together(v_full + 8 * two, turn);
+        w.wait(v_full + 8 * two, turn);
         if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
-        w.wait_together(s_read + 8 * two, turn);
+        w.wait(s_read + 8 * two, turn);
         fence_after();
-        if (lane == 0 && !w.dead) {
-#pragma unroll
-          for (int s = 0; s < D / 16; ++s) mma_smem(tmem + two * ROWS, desc_along(do_tile, s), desc_along(v, s), ins_dp, s > 0);
+        if (elected() && !w.dead) {
+          multiply_along<D>(tmem + two * ROWS, do_tile, v, ins_dp);
           commit(dp_full + 8 * two);
           commit(v_empty + 8 * two);
         }
@@ -783,12 +771,10 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       for (int x = x0; x < end; ++x) {
         const int two = x & 1;
         const u32 k = k_ring + x % 3 * TILE;
-        w.wait_together(ds_ready + 8 * two, turn);
+        w.wait(ds_ready + 8 * two, turn);
         fence_after();
-        if (lane == 0 && !w.dead) {
-#pragma unroll
-          for (int s = 0; s < ROWS / 16; ++s)
-            mma_tmem(tmem_dq, tmem + two * ROWS + 8 * s, desc_across(k, s), ins_acc, x > 0 || s > 0);
+        if (elected() && !w.dead) {
+          multiply_across(tmem_dq, tmem + two * ROWS, k, ins_acc, x > 0);
           commit(k_empty + 8 * (x % 3));
           if (x + 1 == total) commit(done);
         }

@@ -54,11 +54,6 @@ struct Waiter {
         return;
       }
   }
-  // all lanes of a warp, which go on alike
-  __device__ __forceinline__ void wait_together(u32 bar, u32 parity) {
-    wait(bar, parity);
-    dead = __any_sync(0xffffffffu, dead);
-  }
 };
 
 // ---- copies
@@ -137,16 +132,14 @@ __device__ __forceinline__ void tmem_store16(u32 at, const u32 (&v)[16]) {
 }
 
 // ---- products
-// Operand descriptors: start, leading and stride offsets in 16-byte units, 128-byte swizzle.  A step of 16 along the
-// contraction moves the start.
-__device__ __forceinline__ u64 desc_along(u32 tile, int step) {       // contraction along the tile's columns
-  const u32 at = tile + (step / 4) * PANEL + (step % 4) * 32;
-  return (u64)((at & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
-}
-__device__ __forceinline__ u64 desc_across(u32 tile, int step) {      // contraction along the tile's rows
-  const u32 at = tile + step * 2048;
-  return (u64)((at & 0x3FFFFu) >> 4) | ((u64)(PANEL >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
-}
+// Operand descriptors: start, leading and stride offsets in 16-byte units, 128-byte swizzle.  Of a tile's descriptors only the
+// start differs, in the low word; a step of 16 along the contraction adds a constant to it.
+constexpr u32 DESC_HIGH = 64u | (1u << 14) | (2u << 29);
+__device__ __forceinline__ u32 desc_along(u32 tile) { return ((tile & 0x3FFFFu) >> 4) | (1u << 16); }         // contraction along the tile's columns
+__device__ __forceinline__ u32 desc_across(u32 tile) { return ((tile & 0x3FFFFu) >> 4) | ((PANEL >> 4) << 16); }   // along its rows
+__device__ __forceinline__ constexpr u32 step_along(int s) { return (s / 4) * (PANEL >> 4) + (s % 4) * 2; }
+__device__ __forceinline__ constexpr u32 step_across(int s) { return s * 128; }
+
 template <class T> struct Format;
 template <> struct Format<__half> { static constexpr u32 code = 0; };
 template <> struct Format<__nv_bfloat16> { static constexpr u32 code = 1; };
@@ -156,13 +149,37 @@ __device__ __forceinline__ constexpr u32 instruction(int n, bool across, bool mi
   return (1u << 4) | (Format<T>::code << 7) | (Format<T>::code << 10) | ((minus ? 1u : 0u) << 13) | ((across ? 1u : 0u) << 16) |
          ((u32)(n >> 3) << 17) | ((u32)(128 >> 4) << 24);
 }
-__device__ __forceinline__ void mma_smem(u32 d, u64 a, u64 b, u32 ins, bool add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               ::"r"(d), "l"(a), "l"(b), "r"(ins), "r"(add ? 1u : 0u) : "memory");
+// One lane of the warp, always the same one.  (The compiler knows of elect.sync that one thread is left, and keeps the operands of
+// products in uniform registers; behind a comparison of the lane's number it moved each of them there for every product.)
+__device__ __forceinline__ bool elected() {
+  u32 one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
 }
-__device__ __forceinline__ void mma_tmem(u32 d, u32 a, u64 b, u32 ins, bool add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "l"(b), "r"(ins), "r"(add ? 1u : 0u) : "memory");
+__device__ __forceinline__ void mma_smem(u32 d, u32 a, u32 b, u32 ins, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(ins), "r"(DESC_HIGH), "r"(add ? 1u : 0u) : "memory");
+}
+__device__ __forceinline__ void mma_tmem(u32 d, u32 a, u32 b, u32 ins, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 b, {%2, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(ins), "r"(DESC_HIGH), "r"(add ? 1u : 0u) : "memory");
+}
+// d = a b^T: both tiles' contraction along their columns, D of them
+template <int D>
+__device__ __forceinline__ void multiply_along(u32 d, u32 a, u32 b, u32 ins) {
+  const u32 x = desc_along(a), y = desc_along(b);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) mma_smem(d, x + step_along(s), y + step_along(s), ins, s > 0);
+}
+// d (+)= a b: a in tensor memory, its 128 columns of 16 bits against the rows of tile b
+__device__ __forceinline__ void multiply_across(u32 d, u32 a, u32 b, u32 ins, bool add) {
+  const u32 y = desc_across(b);
+#pragma unroll
+  for (int s = 0; s < ROWS / 16; ++s) mma_tmem(d, a + 8 * s, y + step_across(s), ins, add || s > 0);
 }
 // the barrier is arrived at once all products that this thread has issued are done
 __device__ __forceinline__ void commit(u32 bar) {
