@@ -443,7 +443,8 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
     const float factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
     for (int x = mine; x < total; x += 2) {
       const int i0 = (first + x % walk) * ROWS, turn = x >> 1 & 1;
-      const u32 lse_at = lse_ring + x % 3 * VECTOR, delta_at = delta_ring + mine * VECTOR;
+      const float4* const lse_at = reinterpret_cast<const float4*>(shared + 7 * TILE + x % 3 * VECTOR);
+      const float4* const delta_at = reinterpret_cast<const float4*>(shared + 7 * TILE + (3 + mine) * VECTOR);
       w.wait(q_full + 8 * (x % 3), x / 3 & 1);
       w.wait(s_full + 8 * mine, turn);
       fence_after();
@@ -455,8 +456,8 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       for (int q = 0; q < 4; ++q) {
 #pragma unroll
         for (int e = 0; e < 32; e += 4) {
-          float off[4];
-          load_shared4(off, lse_at + (32 * q + e) * 4);
+          const float4 o = lse_at[(32 * q + e) / 4];
+          const float off[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
           for (int f = 0; f < 4; ++f) p[q][e + f] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(p[q][e + f]), a.c, -off[f])));
         }
@@ -487,8 +488,8 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
         u32 out[8];
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-          float off[4];
-          load_shared4(off, delta_at + (16 * q + e) * 4);
+          const float4 o = delta_at[(16 * q + e) / 4];
+          const float off[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
           for (int f = 0; f < 4; f += 2) {
             const int c = 16 * (q & 1) + e + f;

@@ -75,9 +75,6 @@ __device__ __forceinline__ void load_bytes(u32 to, const void* from, u32 bytes, 
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void load_shared4(float (&v)[4], u32 at) {
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at));
-}
 // a warp: zeros in the rows of a tile from `first` on
 template <int D>
 __device__ __forceinline__ void clear_rows(u32 tile, int first) {
