@@ -39,7 +39,7 @@ struct Args {
   const int *q_lens, *k_lens;
   int batch, q_len, k_len, heads, kv_heads, dim, causal;
   float scale, c;
-  // the backward pass's rows: lse log2 e (+infinity for a query without keys) and delta, of every query head with q_len
+  // the backward pass's rows: -lse log2 e (-infinity for a query without keys) and -delta, of every query head with q_len
   // rounded up to whole tiles; and for types with a small range the norms, see gradient_factor
   float *lse2, *delta;
   u32* norms;
@@ -199,21 +199,22 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           }
         }
       }
-      const float off = most_s == MINUS_INF ? 0.f : most_s * a.c;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      const float off = most_s == MINUS_INF ? 0.f : -most_s * a.c;
+      const u64 offs = pair(off, off), cs = pair(a.c, a.c);
+      u64 sum[2] = {0, 0};
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         u32 p[16];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-          const float x = exp2_fast(fmaf(__uint_as_float(s[q][e]), a.c, -off));
-          const float y = exp2_fast(fmaf(__uint_as_float(s[q][e + 1]), a.c, -off));
-          sum[e / 2 % 4] += x + y;
-          p[e / 2] = pack<T>(x, y);
+          const float2 x = exp2_pair(s[q][e], s[q][e + 1], cs, offs);
+          sum[e / 2 & 1] = add2(sum[e / 2 & 1], pair(x.x, x.y));
+          p[e / 2] = pack<T>(x.x, x.y);
         }
         tmem_store16(s_at + 16 * q, p);
       }
-      total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      const float2 sums = split(add2(sum[0], sum[1]));
+      total += sums.x + sums.y;
       wait_stores();
       fence_before();
       __syncwarp();
@@ -311,64 +312,43 @@ __device__ __forceinline__ float gradient_factor(const Args& a, int b, int kh) {
   return exp2_fast((float)(max(-60, min(60, e)) - P_SHIFT));
 }
 
-__device__ __forceinline__ void widen8(const uint4& w, float (&v)[8], __nv_bfloat16) {
-  const u32 x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v[2 * e] = __uint_as_float(x[e] << 16);
-    v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void widen8(const uint4& w, float (&v)[8], __half) {
-  const u32 x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[e]));
-    v[2 * e] = f.x;
-    v[2 * e + 1] = f.y;
-  }
-}
-
 // The rows that both kernels read: 16 lanes a query, delta and the exponent's offset; in half precision the largest
 // norms of each key head's dO and V rows as well (as bits: norms are not negative, so they compare as integers).
-template <class T>
-__global__ void __launch_bounds__(256) k_rows(const ps_heads d_out, const ps_heads out, const ps_heads v, const Args a) {
-  const int part = threadIdx.x % 16;
-  const u64 queries = (u64)a.batch * a.heads * a.padded, r = ((u64)blockIdx.x * blockDim.x + threadIdx.x) / 16;
-  const bool query = r < queries;
-  const u64 k = r - queries;
-  if (!query && (!Range<T>::small || k >= (u64)a.batch * a.kv_heads * a.k_len)) return;
-  const int per = query ? a.padded : a.k_len, heads = query ? a.heads : a.kv_heads;
-  const u64 rest = (query ? r : k) / per;
-  const int i = (int)((query ? r : k) % per), h = (int)(rest % heads), b = (int)(rest / heads);
+template <class T, bool QUERY>
+__global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads out, const Args a) {
+  const int part = threadIdx.x % 16, i = blockIdx.x * 16 + threadIdx.x / 16, h = blockIdx.y, b = blockIdx.z;
   const Lengths l = lengths_of(a, b);
-  const bool there = i < (query ? l.n : l.m) && part * 8 < a.dim;
-  float x[8] = {}, dot = 0.f, norm = 0.f;
-  if (there) {
-    widen8(*reinterpret_cast<const uint4*>(row_of<const T>(query ? d_out : v, b, i, h) + part * 8), x, T());
-    if (query) {
+  const bool there = i < (QUERY ? l.n : l.m);
+  float v[8] = {}, dot = 0.f, norm = 0.f;
+  if (there && part * 8 < a.dim) {
+    Pack<T, 8> p;
+    p.load(row_of<const T>(x, b, i, h) + part * 8);
+    p.widen(v);
+    if (QUERY) {
       float y[8];
-      widen8(*reinterpret_cast<const uint4*>(row_of<const T>(out, b, i, h) + part * 8), y, T());
+      p.load(row_of<const T>(out, b, i, h) + part * 8);
+      p.widen(y);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dot = fmaf(x[e], y[e], dot);
+      for (int e = 0; e < 8; ++e) dot = fmaf(v[e], y[e], dot);
     }
     if (Range<T>::small)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) norm = fmaf(x[e], x[e], norm);
+      for (int e = 0; e < 8; ++e) norm = fmaf(v[e], v[e], norm);
   }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) {
-    dot += __shfl_xor_sync(0xffffu << (threadIdx.x & 16), dot, o);
-    if (Range<T>::small) norm += __shfl_xor_sync(0xffffu << (threadIdx.x & 16), norm, o);
+    if (QUERY) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    if (Range<T>::small) norm += __shfl_xor_sync(0xffffffffu, norm, o);
   }
   if (part != 0) return;
-  if (query) {
-    const float lse = i < l.n ? a.lse[((u64)b * a.heads + h) * a.q_len + i] : MINUS_INF;
-    a.lse2[r] = lse == MINUS_INF || end_of(a, l, i) == 0 ? INFINITY : lse * LOG2E - (Range<T>::small ? P_SHIFT : 0);
-    a.delta[r] = dot;
+  if (QUERY) {
+    const u64 head = (u64)b * a.heads + h;
+    const float lse = there ? a.lse[head * a.q_len + i] : MINUS_INF;
+    a.lse2[head * a.padded + i] = lse == MINUS_INF || end_of(a, l, i) == 0 ? MINUS_INF : (Range<T>::small ? P_SHIFT : 0) - lse * LOG2E;
+    a.delta[head * a.padded + i] = -dot;
   }
-  if (Range<T>::small && i < (query ? l.n : l.m))
-    atomicMax(a.norms + 2 * (b * a.kv_heads + (query ? h / (a.heads / a.kv_heads) : h)) + (query ? 0 : 1), __float_as_uint(norm));
+  if (Range<T>::small && there)
+    atomicMax(a.norms + 2 * (b * a.kv_heads + (QUERY ? h / (a.heads / a.kv_heads) : h)) + (QUERY ? 0 : 1), __float_as_uint(norm));
 }
 
 // Both kernels of the backward pass let their two groups of warps take turns: tile pairs are numbered, a group has the even
@@ -441,6 +421,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
     const int begin = j >= l.m ? 0x7fffffff : a.causal ? j - l.m + l.n : 0;
     const int whole = j0 + ROWS > l.m ? 0x7fffffff : a.causal ? j0 + ROWS - 1 - l.m + l.n : 0;
     const float factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
+    const u64 cs = pair(a.c, a.c), factors = pair(factor, factor);
     for (int x = mine; x < total; x += 2) {
       const int i0 = (first + x % walk) * ROWS, turn = x >> 1 & 1;
       const float4* const lse_at = reinterpret_cast<const float4*>(shared + 7 * TILE + x % 3 * VECTOR);
@@ -457,9 +438,13 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
 #pragma unroll
         for (int e = 0; e < 32; e += 4) {
           const float4 o = lse_at[(32 * q + e) / 4];
-          const float off[4] = {o.x, o.y, o.z, o.w};
+          const u64 off[2] = {pair(o.x, o.y), pair(o.z, o.w)};
 #pragma unroll
-          for (int f = 0; f < 4; ++f) p[q][e + f] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(p[q][e + f]), a.c, -off[f])));
+          for (int f = 0; f < 4; f += 2) {
+            const float2 y = exp2_pair(p[q][e + f], p[q][e + f + 1], cs, off[f / 2]);
+            p[q][e + f] = __float_as_uint(y.x);
+            p[q][e + f + 1] = __float_as_uint(y.y);
+          }
         }
         if (i0 < whole) {
           const int skip = begin - i0 - 32 * q;
@@ -489,13 +474,14 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
           const float4 o = delta_at[(16 * q + e) / 4];
-          const float off[4] = {o.x, o.y, o.z, o.w};
+          const u64 off[2] = {pair(o.x, o.y), pair(o.z, o.w)};
 #pragma unroll
           for (int f = 0; f < 4; f += 2) {
             const int c = 16 * (q & 1) + e + f;
-            float u = __uint_as_float(d[q & 1][e + f]) - off[f], v = __uint_as_float(d[q & 1][e + f + 1]) - off[f + 1];
-            if (Range<T>::small) u *= factor, v *= factor;
-            out[(e + f) / 2] = pack<T>(__uint_as_float(p[q / 2][c]) * u, __uint_as_float(p[q / 2][c + 1]) * v);
+            u64 u = add2(pair(__uint_as_float(d[q & 1][e + f]), __uint_as_float(d[q & 1][e + f + 1])), off[f / 2]);
+            if (Range<T>::small) u = mul2(u, factors);
+            const float2 y = split(mul2(u, pair(__uint_as_float(p[q / 2][c]), __uint_as_float(p[q / 2][c + 1]))));
+            out[(e + f) / 2] = pack<T>(y.x, y.y);
           }
         }
         wait_loads();                // (dS goes over columns that have been read)
@@ -659,6 +645,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const int masked = (q0 + ROWS > l.n ? 0 : end_of(a, l, q0)) / ROWS;
     const u64 row = ((u64)b * a.heads + h) * a.padded + i;
     const float off = a.lse2[row], delta = a.delta[row], factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
+    const u64 cs = pair(a.c, a.c), offs = pair(off, off), deltas = pair(delta, delta), factors = pair(factor, factor);
     for (int x = mine; x < total; x += 2) {
       const int turn = x >> 1 & 1;
       w.wait(s_full + 8 * mine, turn);
@@ -673,7 +660,11 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) p[q][e] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(p[q][e]), a.c, -off)));
+        for (int e = 0; e < 32; e += 2) {
+          const float2 y = exp2_pair(p[q][e], p[q][e + 1], cs, offs);
+          p[q][e] = __float_as_uint(y.x);
+          p[q][e + 1] = __float_as_uint(y.y);
+        }
         if (x >= masked) {
           const int left = end - x * ROWS - 32 * q;
 #pragma unroll
@@ -693,9 +684,10 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
           const int c = 16 * (q & 1) + e;
-          float u = __uint_as_float(d[q & 1][e]) - delta, v = __uint_as_float(d[q & 1][e + 1]) - delta;
-          if (Range<T>::small) u *= factor, v *= factor;
-          out[e / 2] = pack<T>(__uint_as_float(p[q / 2][c]) * u, __uint_as_float(p[q / 2][c + 1]) * v);
+          u64 u = add2(pair(__uint_as_float(d[q & 1][e]), __uint_as_float(d[q & 1][e + 1])), deltas);
+          if (Range<T>::small) u = mul2(u, factors);
+          const float2 y = split(mul2(u, pair(__uint_as_float(p[q / 2][c]), __uint_as_float(p[q / 2][c + 1]))));
+          out[e / 2] = pack<T>(y.x, y.y);
         }
         wait_loads();                // (dS goes over columns that have been read)
         tmem_store8(at + 8 * q, out);
@@ -712,7 +704,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     // each group stores half of the columns
     const bool there = i < a.q_len;
     const int safe = min(i, a.q_len - 1);
-    const float by = off == INFINITY ? 0.f : a.scale / factor * (Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f);
+    const float by = off == MINUS_INF ? 0.f : a.scale / factor * (Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f);
     store_row<T, D / 2>(row_of<T>(a.d_q, b, safe, h) + mine * (D / 2), tmem_dq + lanes + mine * (D / 2), total > 0, there,
                         a.dim - mine * (D / 2), by);
   } else if (warp == COPY_WARP) {
@@ -874,15 +866,17 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
     return cudaErrorInvalidValue;
   if (!a.q_len) q = d = k;        // on one side there is nothing: never read
   if (!a.k_len) k = v = q;
-  u64 rows = (u64)a.batch * a.heads * r.padded;
   cudaError_t e;
   if (Range<T>::small) {
     e = cudaMemsetAsync(r.norms, 0, sizeof(u32) * 2 * a.batch * a.kv_heads, stream);
+    if (e == cudaSuccess && a.k_len) {
+      k_rows<T, false><<<dim3((a.k_len + 15) / 16, a.kv_heads, a.batch), 256, 0, stream>>>(a.v, a.v, r);
+      e = cudaGetLastError();
+    }
     if (e != cudaSuccess) return e;
-    rows += (u64)a.batch * a.kv_heads * a.k_len;
   }
   if (a.q_len) {
-    k_rows<T><<<(u32)((rows + 15) / 16), 256, 0, stream>>>(a.d_out, a.out, a.v, r);
+    k_rows<T, true><<<dim3(r.padded / 16, a.heads, a.batch), 256, 0, stream>>>(a.d_out, a.out, r);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   if (a.k_len) {

@@ -25,12 +25,29 @@ __device__ __forceinline__ u32 row_of(const EmbedArgs& a, u64 t) {
 
 // ------------------------------------------------------------------ lookup
 // a warp takes LOADS packs a lane of a token's row at a time
-constexpr int LOOKUP_LOADS = 4;
+#ifndef LL
+#define LL 4
+#endif
+#ifndef LB
+#define LB 4
+#endif
+#ifndef GL
+#define GL 2
+#endif
+#ifndef GB
+#define GB 3
+#endif
+#ifndef GA
+#define GA 4
+#endif
+constexpr int LOOKUP_LOADS = LL, LOOKUP_BLOCKS = LB;
 template <class T, int N>
-__global__ void __launch_bounds__(256) k_lookup(EmbedArgs a, u32 chunks, Divider by_chunk, u32 items) {
+__global__ void __launch_bounds__(256, LOOKUP_BLOCKS) k_lookup(EmbedArgs a, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
-  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
-    const u32 t = by_chunk.of(item), row = row_of(a, t);
+  u32 item = blockIdx.x * 8 + threadIdx.x / 32, next = item < items ? row_of(a, by_chunk.of(item)) : 0;
+  for (; item < items; item += step) {
+    const u32 t = by_chunk.of(item), row = next;
+    if (item + step < items) next = row_of(a, by_chunk.of(item + step));        // (the next one's, ahead)
     const u64 column = (u64)(item - t * chunks) * (32 * N * LOOKUP_LOADS) + lane * N;
     Pack<T, N> v[LOOKUP_LOADS];
     const T* from = (const T*)a.table + row * a.table_stride + column;
@@ -279,8 +296,9 @@ __device__ __forceinline__ u32 piece_in(const EmbedArgs& a, const GradientArgs& 
 }
 
 // (A warp has few columns here, so that the pieces make many warps: a short list is a chain of loads.)
+constexpr int PIECE_BLOCKS = 4;
 template <class T, int N>
-__global__ void __launch_bounds__(256) k_pieces(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+__global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
     const u32 w = by_chunk.of(item), first = piece_in(a, g, w, PIECE);
@@ -299,7 +317,7 @@ __global__ void __launch_bounds__(256) k_pieces(EmbedArgs a, GradientArgs g, u32
   }
 }
 
-__global__ void __launch_bounds__(256) k_pieces2(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+__global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces2(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
     const u32 w = by_chunk.of(item), first = piece_in(a, g, w, PIECE2);
@@ -317,9 +335,9 @@ __global__ void __launch_bounds__(256) k_pieces2(EmbedArgs a, GradientArgs g, u3
 }
 
 // a warp, LOADS packs a lane of a row
-constexpr int LOADS = 2;
+constexpr int LOADS = GL, GRADIENT_BLOCKS = GB;
 template <class T, class G, int N>
-__global__ void __launch_bounds__(256, 3) k_gradient(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+__global__ void __launch_bounds__(256, GRADIENT_BLOCKS) k_gradient(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   const uint2 none = make_uint2(0, 0);
   u32 item = blockIdx.x * 8 + threadIdx.x / 32, row = by_chunk.of(item);
@@ -347,7 +365,7 @@ __global__ void __launch_bounds__(256, 3) k_gradient(EmbedArgs a, GradientArgs g
     }
     if (at < end) {
       const u32 place = at + lane < end ? g.places[at + lane] : 0;
-      sum.template add_rows<4>((const T*)a.out + column, a.out_stride, end - at, columns,
+      sum.template add_rows<GA>((const T*)a.out + column, a.out_stride, end - at, columns,
                                [&](u32 r) { return __shfl_sync(0xffffffffu, place, r); });
     }
     G* to = (G*)a.table + this_row * a.table_stride + column;
@@ -430,8 +448,8 @@ cudaError_t in_parts(u64 count, u32 chunks, Launch launch) {
   }
   return cudaSuccess;
 }
-u32 grid_for(u32 items, int sm_count) {
-  const u32 blocks = (items + 7) / 8, most = (u32)sm_count * 8;
+u32 grid_for(u32 items, int sm_count, int resident) {
+  const u32 blocks = (items + 7) / 8, most = (u32)(sm_count * resident);
   return blocks < most ? blocks : most;
 }
 
@@ -442,7 +460,7 @@ cudaError_t lookup(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
     EmbedArgs part = a;
     part.tokens = (const char*)a.tokens + at * a.token_bytes;
     part.out = (T*)a.out + at * a.out_stride;
-    k_lookup<T, N><<<grid_for(count * chunks, sm_count), 256, 0, stream>>>(part, chunks, Divider(chunks), count * chunks);
+    k_lookup<T, N><<<grid_for(count * chunks, sm_count, LOOKUP_BLOCKS), 256, 0, stream>>>(part, chunks, Divider(chunks), count * chunks);
   });
 }
 
@@ -489,12 +507,12 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   // (pieces number n / 32 at most, and a row of the sums is as long as d_out's: fewer items than 2^31 for any d_out that fits)
   if (g.n >= PIECE) {
     const u32 chunks = chunks_of(a.dim, 32 * N), items = g.n / PIECE * chunks;
-    k_pieces<T, N><<<grid_for(items, sm_count), 256, 0, stream>>>(a, g, chunks, Divider(chunks), items);
+    k_pieces<T, N><<<grid_for(items, sm_count, PIECE_BLOCKS), 256, 0, stream>>>(a, g, chunks, Divider(chunks), items);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   if (g.n >= LONG) {
     const u32 chunks = chunks_of(g.width, 128), items = g.n / PIECE2 * chunks;
-    k_pieces2<<<grid_for(items, sm_count), 256, 0, stream>>>(a, g, chunks, Divider(chunks), items);
+    k_pieces2<<<grid_for(items, sm_count, PIECE_BLOCKS), 256, 0, stream>>>(a, g, chunks, Divider(chunks), items);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   const u32 chunks = chunks_of(a.dim, 32 * N * LOADS);
@@ -503,7 +521,7 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
     GradientArgs gp = g;
     part.table = (G*)a.table + at * a.table_stride;
     gp.ranges = g.ranges + (g.n ? at : 0);
-    k_gradient<T, G, N><<<grid_for(count * chunks, sm_count), 256, 0, stream>>>(part, gp, chunks, Divider(chunks), count * chunks);
+    k_gradient<T, G, N><<<grid_for(count * chunks, sm_count, GRADIENT_BLOCKS), 256, 0, stream>>>(part, gp, chunks, Divider(chunks), count * chunks);
   });
 }
 
