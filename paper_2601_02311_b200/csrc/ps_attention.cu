@@ -316,6 +316,7 @@ __device__ __forceinline__ float gradient_factor(const Args& a, int b, int kh) {
 // norms of each key head's dO and V rows as well (as bits: norms are not negative, so they compare as integers).
 template <class T, bool QUERY>
 __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads out, const Args a) {
+  let_next_begin();
   const int part = threadIdx.x % 16, i = blockIdx.x * 16 + threadIdx.x / 16, h = blockIdx.y, b = blockIdx.z;
   const Lengths l = lengths_of(a, b);
   const bool there = i < (QUERY ? l.n : l.m);
@@ -410,6 +411,8 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   fence_before();
   __syncthreads();
   fence_after();
+  wait_for_earlier();          // the rows
+  let_next_begin();            // behind the wait: k_queries needs the rows too, and nothing of this kernel
   const u32 tmem = sh.tmem_at, tmem_dv = tmem + 2 * ROWS, tmem_dk = tmem_dv + D;
   Waiter w(a.status);
 
@@ -779,6 +782,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     give_registers<LEFT>();
   }
   linger(w.dead);
+  wait_for_earlier();          // k_keys: this kernel ends behind it, as whatever follows in the stream expects
   fence_before();
   __syncthreads();
   if (warp == MMA_WARP) {
@@ -882,13 +886,15 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
   if (a.k_len) {
     const u32 smem = smem_for(7, D, 5 * ROWS * 4 + sizeof(Shared));
     if ((e = allow(k_keys<T, D>, smem)) != cudaSuccess) return e;
-    k_keys<T, D><<<(u32)((a.k_len + ROWS - 1) / ROWS) * a.kv_heads * a.batch, THREADS, smem, stream>>>(q, k, v, d, r);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    const u32 grid = (u32)((a.k_len + ROWS - 1) / ROWS) * a.kv_heads * a.batch;
+    if ((e = launch_next(k_keys<T, D>, grid, THREADS, smem, stream, q, k, v, d, r)) != cudaSuccess) return e;
   }
   if (a.q_len) {
     const u32 smem = smem_for(7, D, sizeof(Shared));
     if ((e = allow(k_queries<T, D>, smem)) != cudaSuccess) return e;
-    k_queries<T, D><<<(u32)(r.padded / ROWS) * a.heads * a.batch, THREADS, smem, stream>>>(q, k, v, d, r);
+    const u32 grid = (u32)(r.padded / ROWS) * a.heads * a.batch;
+    if (a.k_len) return launch_next(k_queries<T, D>, grid, THREADS, smem, stream, q, k, v, d, r);
+    k_queries<T, D><<<grid, THREADS, smem, stream>>>(q, k, v, d, r);      // (no kernel is between it and the rows)
   }
   return cudaGetLastError();
 }

@@ -16,18 +16,26 @@ struct Words {
   u32 w[4];
 };
 
-__device__ __forceinline__ Words philox(u64 counter, u64 stream, u64 seed) {
+// the keys of the generator's rounds, which depend on the seed alone
+struct Keys {
+  u32 k[10][2];
+  explicit Keys(u64 seed) {
+    for (u32 r = 0; r < 10; ++r) {
+      k[r][0] = (u32)seed + r * 0x9E3779B9u;
+      k[r][1] = (u32)(seed >> 32) + r * 0xBB67AE85u;
+    }
+  }
+};
+
+__device__ __forceinline__ Words philox(u64 counter, u64 stream, const Keys& keys) {
   u32 a = (u32)counter, b = (u32)(counter >> 32), c = (u32)stream, d = (u32)(stream >> 32);
-  u32 k0 = (u32)seed, k1 = (u32)(seed >> 32);
 #pragma unroll
-  for (int round = 0; round < 10; ++round) {
+  for (int r = 0; r < 10; ++r) {
     const u64 p = (u64)a * 0xD2511F53u, q = (u64)c * 0xCD9E8D57u;
-    a = (u32)(q >> 32) ^ b ^ k0;
+    a = (u32)(q >> 32) ^ b ^ keys.k[r][0];
     b = (u32)q;
-    c = (u32)(p >> 32) ^ d ^ k1;
+    c = (u32)(p >> 32) ^ d ^ keys.k[r][1];
     d = (u32)p;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
   }
   return {{a, b, c, d}};
 }
@@ -38,56 +46,93 @@ struct Keep {
   float scale;
   __device__ __forceinline__ explicit Keep(const DropoutArgs& a)
       : least((u32)a.threshold), none(a.threshold >> 32), scale(a.scale) {}
-  __device__ __forceinline__ float of(u32 word, float x) const { return word >= least && !none ? x * scale : 0.f; }
+  __device__ __forceinline__ float of(u32 word, float x, float add) const {
+    return fmaf(word >= least && !none ? x : 0.f, scale, add);
+  }
 };
 
-// A thread takes N consecutive elements (16 bytes, or 8 elements with half a load each) at a time; rows, strides and the
+#ifndef DU
+#define DU 1
+#endif
+#ifndef DB
+#define DB 8
+#endif
+constexpr int UNROLL = DU, RESIDENT = DB;
+// A thread takes UNROLL packs of N consecutive elements (16 bytes) at a time, a grid apart; rows, strides and the
 // first element's index are such that packs are aligned in memory and begin with a word 0.
 template <class T, int N, bool RESIDUAL>
-__global__ void __launch_bounds__(256) k_packs(DropoutArgs a, u32 per_row, Divider by_row, u32 packs) {
+__global__ void __launch_bounds__(256, RESIDENT) k_packs(const DropoutArgs a, const __grid_constant__ Keys keys, u32 per_row, Divider by_row, u32 packs) {
   const Keep keep(a);
-  for (u32 i = blockIdx.x * 256 + threadIdx.x; i < packs; i += gridDim.x * 256) {
-    const u32 r = by_row.of(i);
-    const u64 c = (u64)(i - r * per_row) * N;
-    Pack<T, N> x, y;
-    float v[N], add[N];
-    x.load((const T*)a.x + r * a.x_stride + c);
-    if (RESIDUAL) y.load((const T*)a.residual + r * a.residual_stride + c);
-    const u64 counter = (a.first + r * a.pitch + c) >> 2;
-    Words words[N / 4];
+  const u32 step = gridDim.x * 256;
+  for (u32 i = blockIdx.x * 256 + threadIdx.x; i < packs; i += step * UNROLL) {
+    Pack<T, N> x[UNROLL], y[UNROLL];
+    u32 row[UNROLL];
+    u64 column[UNROLL];
 #pragma unroll
-    for (int q = 0; q < N / 4; ++q) words[q] = philox(counter + q, a.stream, a.seed);
-    x.widen(v);
-    if (RESIDUAL) y.widen(add);
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      v[e] = keep.of(words[e / 4].w[e % 4], v[e]);
-      if (RESIDUAL) v[e] += add[e];
+    for (int u = 0; u < UNROLL; ++u) {
+      const u32 at = i + u * step;
+      row[u] = by_row.of(at);
+      column[u] = (u64)(at - row[u] * per_row) * N;
+      if (at < packs) {
+        x[u].load((const T*)a.x + row[u] * a.x_stride + column[u]);
+        if (RESIDUAL) y[u].load((const T*)a.residual + row[u] * a.residual_stride + column[u]);
+      }
     }
-    y.narrow(v);
-    y.store((T*)a.y + r * a.y_stride + c);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const u64 counter = (a.first + row[u] * a.pitch + column[u]) >> 2;
+      Words words[N / 4];
+      float v[N], add[N];
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) words[q] = philox(counter + q, a.stream, keys);
+      if (i + u * step < packs) {
+        x[u].widen(v);
+        if (RESIDUAL) y[u].widen(add);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = keep.of(words[e / 4].w[e % 4], v[e], RESIDUAL ? add[e] : 0.f);
+        y[u].narrow(v);
+        y[u].store((T*)a.y + row[u] * a.y_stride + column[u]);
+      }
+    }
   }
 }
 
 // Any alignment: a thread takes the elements of a row that share a counter, element by element.
 template <class T, bool RESIDUAL>
-__global__ void __launch_bounds__(256) k_groups(DropoutArgs a, u32 per_row, Divider by_row, u32 groups) {
+__global__ void __launch_bounds__(256, RESIDENT) k_groups(const DropoutArgs a, const __grid_constant__ Keys keys, u32 per_row, Divider by_row, u32 groups) {
   const Keep keep(a);
-  for (u32 i = blockIdx.x * 256 + threadIdx.x; i < groups; i += gridDim.x * 256) {
-    const u32 r = by_row.of(i);
-    const u64 begin = a.first + r * a.pitch, counter = (begin >> 2) + (i - r * per_row);
-    const s64 c = (s64)(counter * 4 - begin);             // of word 0: the first group may begin before the row
-    float x[4], y[4] = {0.f, 0.f, 0.f, 0.f};
+  const u32 step = gridDim.x * 256;
+  for (u32 i = blockIdx.x * 256 + threadIdx.x; i < groups; i += step * UNROLL) {
+    float x[UNROLL][4], y[UNROLL][4];
+    u32 row[UNROLL];
+    u64 counter[UNROLL];
+    s64 column[UNROLL];                                         // of word 0: a row's first group may begin before it
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e >= 0 && c + e < (s64)a.cols) {
-        x[e] = widen(((const T*)a.x)[(s64)(r * a.x_stride) + c + e]);
-        if (RESIDUAL) y[e] = widen(((const T*)a.residual)[(s64)(r * a.residual_stride) + c + e]);
+    for (int u = 0; u < UNROLL; ++u) {
+      const u32 at = i + u * step, r = by_row.of(at);
+      const u64 begin = a.first + r * a.pitch;
+      row[u] = r;
+      counter[u] = (begin >> 2) + (at - r * per_row);
+      column[u] = at < groups ? (s64)(counter[u] * 4 - begin) : (s64)a.cols;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const s64 c = column[u] + e;
+        x[u][e] = y[u][e] = 0.f;
+        if (c >= 0 && c < (s64)a.cols) {
+          x[u][e] = widen(((const T*)a.x)[(s64)(r * a.x_stride) + c]);
+          if (RESIDUAL) y[u][e] = widen(((const T*)a.residual)[(s64)(r * a.residual_stride) + c]);
+        }
       }
-    const Words w = philox(counter, a.stream, a.seed);
+    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e >= 0 && c + e < (s64)a.cols) ((T*)a.y)[(s64)(r * a.y_stride) + c + e] = narrow<T>(keep.of(w.w[e], x[e]) + y[e]);
+    for (int u = 0; u < UNROLL; ++u) {
+      const Words w = philox(counter[u], a.stream, keys);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const s64 c = column[u] + e;
+        if (c >= 0 && c < (s64)a.cols) ((T*)a.y)[(s64)(row[u] * a.y_stride) + c] = narrow<T>(keep.of(w.w[e], x[u][e], y[u][e]));
+      }
+    }
   }
 }
 
@@ -109,6 +154,7 @@ cudaError_t dropout(DropoutArgs a, int sm_count, cudaStream_t stream) {
   const u64 per_row = packs ? cols / N : cols / 4 + 2;
   if (per_row > 0x7fffffffu) return cudaErrorInvalidValue;        // (cols above 2^32 in rows of a larger tensor are refused before)
   const u64 rows = 0x7fffffffu / per_row;
+  const Keys keys(a.seed);
   for (u64 r = 0; r < a.rows; r += rows)
     for (u64 c = 0; c < a.cols; c += cols) {
       DropoutArgs p = a;
@@ -119,10 +165,10 @@ cudaError_t dropout(DropoutArgs a, int sm_count, cudaStream_t stream) {
       if (RESIDUAL) p.residual = (const T*)a.residual + r * a.residual_stride + c;
       p.y = (T*)a.y + r * a.y_stride + c;
       const u32 n = packs ? (u32)(p.cols / N) : (u32)(p.cols / 4 + 2), items = (u32)p.rows * n;
-      const u64 blocks = ((u64)items + 255) / 256, most = (u64)sm_count * 8;
+      const u64 blocks = ((u64)items + 255) / 256, most = (u64)sm_count * RESIDENT;
       const u32 grid = (u32)(blocks < most ? blocks : most);
-      if (packs) k_packs<T, N, RESIDUAL><<<grid, 256, 0, stream>>>(p, n, Divider(n), items);
-      else k_groups<T, RESIDUAL><<<grid, 256, 0, stream>>>(p, n, Divider(n), items);
+      if (packs) k_packs<T, N, RESIDUAL><<<grid, 256, 0, stream>>>(p, keys, n, Divider(n), items);
+      else k_groups<T, RESIDUAL><<<grid, 256, 0, stream>>>(p, keys, n, Divider(n), items);
       const cudaError_t e = cudaGetLastError();
       if (e != cudaSuccess) return e;
     }

@@ -25,22 +25,7 @@ __device__ __forceinline__ u32 row_of(const EmbedArgs& a, u64 t) {
 
 // ------------------------------------------------------------------ lookup
 // a warp takes LOADS packs a lane of a token's row at a time
-#ifndef LL
-#define LL 4
-#endif
-#ifndef LB
-#define LB 4
-#endif
-#ifndef GL
-#define GL 2
-#endif
-#ifndef GB
-#define GB 3
-#endif
-#ifndef GA
-#define GA 4
-#endif
-constexpr int LOOKUP_LOADS = LL, LOOKUP_BLOCKS = LB;
+constexpr int LOOKUP_LOADS = 4, LOOKUP_BLOCKS = 4;
 template <class T, int N>
 __global__ void __launch_bounds__(256, LOOKUP_BLOCKS) k_lookup(EmbedArgs a, u32 chunks, Divider by_chunk, u32 items) {
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
@@ -73,7 +58,6 @@ __global__ void __launch_bounds__(256, LOOKUP_BLOCKS) k_lookup(EmbedArgs a, u32 
 // ------------------------------------------------------------------ sort
 constexpr int SORT_THREADS = 512, SORT_ITEMS = 4, SORT_TILE = SORT_THREADS * SORT_ITEMS, SORT_WARPS = SORT_THREADS / 32;
 constexpr int MAX_BITS = 9, MAX_DIGITS = 1 << MAX_BITS;
-constexpr u32 SORT_ALONE = 4 * SORT_TILE;      // so many tokens are sorted by one block
 
 struct SortArgs {
   u32 n, chunk, blocks;        // tokens, and how many of them in a row a block takes
@@ -169,7 +153,9 @@ __device__ void place_items(const EmbedArgs& a, const SortArgs& s, u32 begin, u3
 
 __global__ void __launch_bounds__(SORT_THREADS) k_sort_count(EmbedArgs a, SortArgs s) {
   __shared__ u32 count[MAX_DIGITS];
+  let_next_begin();
   count[threadIdx.x] = 0;
+  if (s.keys_in) wait_for_earlier();        // (the first pass reads tokens alone)
   __syncthreads();
   const u32 digits = 1u << s.bits, end = min(s.n, (blockIdx.x + 1) * s.chunk);
   for (u32 i = blockIdx.x * s.chunk + threadIdx.x; i < end; i += SORT_THREADS)
@@ -180,6 +166,8 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_count(EmbedArgs a, SortAr
 
 __global__ void __launch_bounds__(SORT_THREADS) k_sort_place(EmbedArgs a, SortArgs s) {
   __shared__ SortShared sh;
+  let_next_begin();
+  wait_for_earlier();
   const u32 digits = 1u << s.bits;
   u32 before = 0, all = 0;
   if (threadIdx.x < digits) {
@@ -195,40 +183,52 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_place(EmbedArgs a, SortAr
 }
 
 // Where a row's list begins and ends in the sorted order.  (The array is zeros before: a row without tokens has none.)
-__device__ __forceinline__ void mark(const u32* keys, u32 n, uint2* ranges, u64 rows, u32 i) {
+__global__ void __launch_bounds__(256) k_mark(const u32* keys, u32 n, uint2* ranges, u64 rows) {
+  let_next_begin();
+  wait_for_earlier();
+  const u32 i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
   const u32 key = keys[i];
   if (key >= rows) return;
   if (i == 0 || keys[i - 1] != key) ranges[key].x = i;
   if (i + 1 == n || keys[i + 1] != key) ranges[key].y = i + 1;
 }
-__global__ void __launch_bounds__(256) k_mark(const u32* keys, u32 n, uint2* ranges, u64 rows) {
-  const u32 i = blockIdx.x * 256 + threadIdx.x;
-  if (i < n) mark(keys, n, ranges, rows, i);
-}
 
-// All passes of a short sort, in shared memory, and the marks.
-__global__ void __launch_bounds__(SORT_THREADS) k_sort_alone(EmbedArgs a, SortArgs s, uint2* ranges) {
-  extern __shared__ u32 items[];
-  __shared__ SortShared sh;
-  u32 *const keys = s.keys_out, *const values = s.values_out, n = s.n, digits = 1u << s.bits;
-  s.keys_in = s.values_in = nullptr;
-  for (u32 pass = 0; pass < s.passes; ++pass) {
-    s.shift = pass * s.bits;
-    s.keys_out = items + (pass & 1) * 2 * n;
-    s.values_out = s.keys_out + n;
-    sh.base[threadIdx.x] = 0;
-    __syncthreads();
-    for (u32 i = threadIdx.x; i < n; i += SORT_THREADS) atomicAdd(&sh.base[(key_at(a, s.keys_in, i) >> s.shift) & (digits - 1)], 1u);
-    __syncthreads();
-    sh.base[threadIdx.x] = scan_block(sh.base[threadIdx.x], sh.warp_sums);
-    place_items(a, s, 0, n, sh);
-    s.keys_in = s.keys_out;
-    s.values_in = s.values_out;
-  }
-  for (u32 i = threadIdx.x; i < n; i += SORT_THREADS) {
-    keys[i] = s.keys_in[i];
-    values[i] = s.values_in[i];
-    mark(s.keys_in, n, ranges, a.rows, i);
+// Few tokens need no passes: a token's place is the number of smaller rows before or behind it plus the number of equal ones before it, and
+// its row's list begins behind the smaller ones.  A warp counts for a token, over all rows in shared memory: n^2 comparisons on all
+// SMs, 1.5 us of work for 2048 tokens, where one block's radix passes took 8.
+constexpr u32 RANK_MOST = 8192;
+__global__ void __launch_bounds__(256) k_rank(EmbedArgs a, u32 n, u32* keys, u32* places, uint2* ranges) {
+  extern __shared__ uint4 rows4[];
+  u32* const rows = reinterpret_cast<u32*>(rows4);
+  let_next_begin();
+  const u32 lane = threadIdx.x % 32, fours = (n + 3) / 4;
+  for (u32 i = threadIdx.x; i < fours * 4; i += 256) rows[i] = i < n ? row_of(a, i) : 0xffffffffu;
+  __syncthreads();
+  for (u32 t = blockIdx.x * 8 + threadIdx.x / 32; t < n; t += gridDim.x * 8) {
+    const u32 key = rows[t];
+    u32 less = 0, same = 0, before = 0;
+    for (u32 i = lane; i < fours; i += 32) {
+      const uint4 v = rows4[i];
+      const u32 k[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (u32 e = 0; e < 4; ++e) {
+        less += k[e] < key;
+        same += k[e] == key;
+        before += k[e] == key && 4 * i + e < t;
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      less += __shfl_xor_sync(0xffffffffu, less, o);
+      same += __shfl_xor_sync(0xffffffffu, same, o);
+      before += __shfl_xor_sync(0xffffffffu, before, o);
+    }
+    if (lane == 0) {
+      keys[less + before] = key;
+      places[less + before] = t;
+      if (before == 0 && key < a.rows) ranges[key] = make_uint2(less, less + same);
+    }
   }
 }
 
@@ -296,9 +296,11 @@ __device__ __forceinline__ u32 piece_in(const EmbedArgs& a, const GradientArgs& 
 }
 
 // (A warp has few columns here, so that the pieces make many warps: a short list is a chain of loads.)
-constexpr int PIECE_BLOCKS = 4;
-template <class T, int N>
-__global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+constexpr int PIECE_BLOCKS = 4, PIECE_BLOCKS_FEW = 1;
+template <class T, int N, int AHEAD, int BLOCKS>
+__global__ void __launch_bounds__(256, BLOCKS) k_pieces(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+  let_next_begin();
+  wait_for_earlier();
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
     const u32 w = by_chunk.of(item), first = piece_in(a, g, w, PIECE);
@@ -307,7 +309,7 @@ __global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces(EmbedArgs a, Gradi
     const s64 columns = (s64)a.dim - (s64)column;
     const u32 place = g.places[first + lane];
     Sum<N, 1> sum;
-    sum.template add_rows<8>((const T*)a.out + column, a.out_stride, PIECE, columns,
+    sum.template add_rows<AHEAD>((const T*)a.out + column, a.out_stride, PIECE, columns,
                              [&](u32 r) { return __shfl_sync(0xffffffffu, place, r); });
     if (columns > 0) {
       Pack<float, N> p;
@@ -318,6 +320,8 @@ __global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces(EmbedArgs a, Gradi
 }
 
 __global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces2(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+  let_next_begin();
+  wait_for_earlier();
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
     const u32 w = by_chunk.of(item), first = piece_in(a, g, w, PIECE2);
@@ -334,61 +338,73 @@ __global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces2(EmbedArgs a, Grad
   }
 }
 
-// a warp, LOADS packs a lane of a row
-constexpr int LOADS = GL, GRADIENT_BLOCKS = GB;
-template <class T, class G, int N>
+// A warp takes GROUP rows, LOADS packs a lane of each: their lists' bounds come in one load, so that rows without tokens, often
+// most of them, are a store each and nothing is waited for.
+constexpr int GRADIENT_BLOCKS = 3;
+template <class T, class G, int N, int GROUP, int LOADS, int AHEAD>
 __global__ void __launch_bounds__(256, GRADIENT_BLOCKS) k_gradient(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+  wait_for_earlier();
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
-  const uint2 none = make_uint2(0, 0);
-  u32 item = blockIdx.x * 8 + threadIdx.x / 32, row = by_chunk.of(item);
-  uint2 range = g.n && item < items ? g.ranges[row] : none;
-  for (; item < items;) {
-    const u64 column = (u64)(item - row * chunks) * (32 * N * LOADS) + lane * N;
+  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
+    const u32 first = by_chunk.of(item) * GROUP, rows = min((u32)GROUP, (u32)a.rows - first);
+    const u64 column = (u64)(item - first / GROUP * chunks) * (32 * N * LOADS) + lane * N;
     const s64 columns = (s64)a.dim - (s64)column;
-    const u32 count = range.y - range.x;
-    u32 at = range.x;
-    const u32 end = range.y, this_row = row;
-    item += step;
-    row = by_chunk.of(item);
-    range = g.n && item < items ? g.ranges[row] : none;          // (the next one's, ahead)
-    if (count == 0 && a.accumulate) continue;
-    Sum<N, LOADS> sum;
-    if (count >= PIECE) {
-      if (g.sums2 && count >= PIECE2) {
-        const u32 pieces = count / PIECE2;
-        sum.template add_rows<2>(g.sums2 + column, g.width, pieces, columns, [&](u32 r) { return at / PIECE2 + r; });
-        at += pieces * PIECE2;
-      }
-      const u32 pieces = (end - at) / PIECE;
-      sum.template add_rows<2>(g.sums + column, g.width, pieces, columns, [&](u32 r) { return at / PIECE + r; });
-      at += pieces * PIECE;
-    }
-    if (at < end) {
-      const u32 place = at + lane < end ? g.places[at + lane] : 0;
-      sum.template add_rows<GA>((const T*)a.out + column, a.out_stride, end - at, columns,
-                               [&](u32 r) { return __shfl_sync(0xffffffffu, place, r); });
-    }
-    G* to = (G*)a.table + this_row * a.table_stride + column;
+    const uint2 ranges = g.n && lane < rows ? g.ranges[first + lane] : make_uint2(0, 0);
+    G* to = (G*)a.table + first * a.table_stride + column;
+#pragma unroll 1
+    for (u32 r = 0; r < rows; ++r, to += a.table_stride) {
+      u32 at = __shfl_sync(0xffffffffu, ranges.x, r);
+      const u32 end = __shfl_sync(0xffffffffu, ranges.y, r), count = end - at;
+      if (count == 0) {
+        if (!a.accumulate) {
+          Pack<G, N> zero;
+          zero.clear();
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-      if (i * 32 * N < columns) {
-        Pack<G, N> p;
-        float x[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = 0.f;
-        if (a.accumulate) {
-          p.load(to + i * 32 * N);
-          p.widen(x);
+          for (int i = 0; i < LOADS; ++i)
+            if (i * 32 * N < columns) zero.store(to + i * 32 * N);
         }
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = a.accumulate ? fmaf(sum.v[i][e], a.scale, x[e]) : sum.v[i][e] * a.scale;
-        p.narrow(x);
-        p.store(to + i * 32 * N);
+        continue;
       }
+      Sum<N, LOADS> sum;
+      if (count >= PIECE) {
+        if (g.sums2 && count >= PIECE2) {
+          const u32 pieces = count / PIECE2;
+          sum.template add_rows<2>(g.sums2 + column, g.width, pieces, columns, [&](u32 q) { return at / PIECE2 + q; });
+          at += pieces * PIECE2;
+        }
+        const u32 pieces = (end - at) / PIECE;
+        sum.template add_rows<2>(g.sums + column, g.width, pieces, columns, [&](u32 q) { return at / PIECE + q; });
+        at += pieces * PIECE;
+      }
+      if (at < end) {
+        const u32 place = at + lane < end ? g.places[at + lane] : 0;
+        sum.template add_rows<AHEAD>((const T*)a.out + column, a.out_stride, end - at, columns,
+                                  [&](u32 q) { return __shfl_sync(0xffffffffu, place, q); });
+      }
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        if (i * 32 * N < columns) {
+          Pack<G, N> p;
+          float x[N];
+#pragma unroll
+          for (int e = 0; e < N; ++e) x[e] = 0.f;
+          if (a.accumulate) {
+            p.load(to + i * 32 * N);
+            p.widen(x);
+          }
+#pragma unroll
+          for (int e = 0; e < N; ++e) x[e] = a.accumulate ? fmaf(sum.v[i][e], a.scale, x[e]) : sum.v[i][e] * a.scale;
+          p.narrow(x);
+          p.store(to + i * 32 * N);
+        }
+    }
   }
 }
 
 // ------------------------------------------------------------------ host
+#ifndef SMALL_TABLE
+#define SMALL_TABLE ((u64)1 << 27)
+#endif
 u32 chunks_of(u64 dim, int columns) { return (u32)((dim + columns - 1) / columns); }
 // columns of a row of sums, for every size of packs
 u64 width_of(u64 dim) { return (dim + 7) / 8 * 8; }
@@ -429,7 +445,7 @@ Work work_of(const EmbedArgs& a) {
     w.keys[i] = (u32*)take(4 * (size_t)s.n);
     w.values[i] = (u32*)take(4 * (size_t)s.n);
   }
-  w.counts = (u32*)take(s.n > SORT_ALONE ? (size_t)s.blocks * 4 << s.bits : 0);
+  w.counts = (u32*)take(s.n > RANK_MOST ? (size_t)s.blocks * 4 << s.bits : 0);
   w.ranges = (uint2*)take(8 * a.rows);
   w.sums = (float*)take(s.n / PIECE * width_of(a.dim) * 4);
   w.sums2 = (float*)take(s.n / PIECE2 * width_of(a.dim) * 4);
@@ -464,6 +480,23 @@ cudaError_t lookup(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   });
 }
 
+template <class T, class G, int N, int GROUP, int LOADS, int AHEAD>
+cudaError_t write_rows(const EmbedArgs& a, const GradientArgs& g, int sm_count, cudaStream_t stream) {
+  const u32 chunks = chunks_of(a.dim, 32 * N * LOADS);
+  cudaError_t e = cudaSuccess;
+  const cudaError_t e2 = in_parts((a.rows + GROUP - 1) / GROUP, chunks, [&](u64 at, u32 count) {
+    EmbedArgs part = a;
+    GradientArgs gp = g;
+    part.table = (G*)a.table + at * GROUP * a.table_stride;
+    part.rows = a.rows - at * GROUP;
+    gp.ranges = g.ranges + (g.n ? at * GROUP : 0);
+    const cudaError_t e1 = launch_next(k_gradient<T, G, N, GROUP, LOADS, AHEAD>, grid_for(count * chunks, sm_count, GRADIENT_BLOCKS), 256, 0,
+                                       stream, part, gp, chunks, Divider(chunks), count * chunks);
+    if (e1 != cudaSuccess) e = e1;
+  });
+  return e != cudaSuccess ? e : e2;
+}
+
 template <class T, class G, int N>
 cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   cudaError_t e;
@@ -476,12 +509,8 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
     SortArgs s = sort_plan(a);
     if ((e = cudaMemsetAsync(w.ranges, 0, 8 * a.rows, stream)) != cudaSuccess) return e;
     s.counts = w.counts;
-    if (g.n <= SORT_ALONE) {
-      s.keys_out = w.keys[0];
-      s.values_out = w.values[0];
-      const u32 smem = 16 * g.n;
-      if ((e = cudaFuncSetAttribute(k_sort_alone, cudaFuncAttributeMaxDynamicSharedMemorySize, 16 * SORT_ALONE)) != cudaSuccess) return e;
-      k_sort_alone<<<1, SORT_THREADS, smem, stream>>>(a, s, w.ranges);
+    if (g.n <= RANK_MOST) {
+      k_rank<<<grid_for(g.n, sm_count, 4), 256, (g.n + 3) / 4 * 16, stream>>>(a, g.n, w.keys[0], w.values[0], w.ranges);
       if ((e = cudaGetLastError()) != cudaSuccess) return e;
     } else {
       for (u32 pass = 0; pass < s.passes; ++pass) {
@@ -491,12 +520,12 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
         s.values_in = pass ? w.values[to ^ 1] : nullptr;
         s.keys_out = w.keys[to];
         s.values_out = w.values[to];
-        k_sort_count<<<s.blocks, SORT_THREADS, 0, stream>>>(a, s);
-        k_sort_place<<<s.blocks, SORT_THREADS, 0, stream>>>(a, s);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if (pass) e = launch_next(k_sort_count, s.blocks, SORT_THREADS, 0, stream, a, s);
+        else k_sort_count<<<s.blocks, SORT_THREADS, 0, stream>>>(a, s), e = cudaGetLastError();
+        if (e == cudaSuccess) e = launch_next(k_sort_place, s.blocks, SORT_THREADS, 0, stream, a, s);
+        if (e != cudaSuccess) return e;
       }
-      k_mark<<<(g.n + 255) / 256, 256, 0, stream>>>(w.keys[0], g.n, w.ranges, a.rows);
-      if ((e = cudaGetLastError()) != cudaSuccess) return e;
+      if ((e = launch_next(k_mark, (g.n + 255) / 256, 256, 0, stream, w.keys[0], g.n, w.ranges, a.rows)) != cudaSuccess) return e;
     }
     g.keys = w.keys[0];
     g.places = w.values[0];
@@ -507,22 +536,21 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   // (pieces number n / 32 at most, and a row of the sums is as long as d_out's: fewer items than 2^31 for any d_out that fits)
   if (g.n >= PIECE) {
     const u32 chunks = chunks_of(a.dim, 32 * N), items = g.n / PIECE * chunks;
-    k_pieces<T, N><<<grid_for(items, sm_count, PIECE_BLOCKS), 256, 0, stream>>>(a, g, chunks, Divider(chunks), items);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    // pieces that all run at once are a chain of loads each: all of a piece's rows are loaded ahead
+    if (items <= (u32)sm_count * 8 * PIECE_BLOCKS_FEW)
+      e = launch_next(k_pieces<T, N, (int)PIECE, PIECE_BLOCKS_FEW>, (items + 7) / 8, 256, 0, stream, a, g, chunks, Divider(chunks), items);
+    else
+      e = launch_next(k_pieces<T, N, 8, PIECE_BLOCKS>, grid_for(items, sm_count, PIECE_BLOCKS), 256, 0, stream, a, g, chunks, Divider(chunks), items);
+    if (e != cudaSuccess) return e;
   }
   if (g.n >= LONG) {
     const u32 chunks = chunks_of(g.width, 128), items = g.n / PIECE2 * chunks;
-    k_pieces2<<<grid_for(items, sm_count, PIECE_BLOCKS), 256, 0, stream>>>(a, g, chunks, Divider(chunks), items);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_next(k_pieces2, grid_for(items, sm_count, PIECE_BLOCKS), 256, 0, stream, a, g, chunks, Divider(chunks), items)) != cudaSuccess)
+      return e;
   }
-  const u32 chunks = chunks_of(a.dim, 32 * N * LOADS);
-  return in_parts(a.rows, chunks, [&](u64 at, u32 count) {
-    EmbedArgs part = a;
-    GradientArgs gp = g;
-    part.table = (G*)a.table + at * a.table_stride;
-    gp.ranges = g.ranges + (g.n ? at : 0);
-    k_gradient<T, G, N><<<grid_for(count * chunks, sm_count, GRADIENT_BLOCKS), 256, 0, stream>>>(part, gp, chunks, Divider(chunks), count * chunks);
-  });
+  // a warp's share of a small table is small, of a large one the better one for bandwidth
+  if (a.rows * a.dim <= SMALL_TABLE) return write_rows<T, G, N, 4, 1, 8>(a, g, sm_count, stream);
+  return write_rows<T, G, N, 8, 2, 4>(a, g, sm_count, stream);
 }
 
 // packs of 16 bytes of the values that are read, where both tensors allow it

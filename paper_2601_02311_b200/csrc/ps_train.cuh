@@ -95,6 +95,26 @@ struct Pack {
   }
 };
 
+// ---- A chain of kernels of one call.  A kernel that is started by launch_next may begin while the kernel before it in the
+// stream still runs: as soon as each block of that one has called let_next_begin (or ended).  What it reads of earlier kernels it reads
+// behind wait_for_earlier, which returns once they are done and their results visible.
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <class... Parameters, class... Arguments>
+cudaError_t launch_next(void (*kernel)(Parameters...), dim3 grid, u32 threads, u32 smem, cudaStream_t stream, const Arguments&... arguments) {
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = grid;
+  config.blockDim = dim3(threads);
+  config.dynamicSmemBytes = smem;
+  config.stream = stream;
+  config.attrs = &early;
+  config.numAttrs = 1;
+  return cudaLaunchKernelEx(&config, kernel, Parameters(arguments)...);
+}
+
 // whether packs of n elements may be used at `p` and at rows `stride` elements apart
 inline bool packs_at(const void* p, u64 stride, int n, size_t width) {
   const size_t bytes = n * width < 16 ? n * width : 16;
