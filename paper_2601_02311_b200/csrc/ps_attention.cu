@@ -18,6 +18,7 @@
 // The backward pass is two kernels, one that owns keys (dK, dV) and one that owns queries (dQ).  That is seven products a
 // tile pair instead of the five of a single pass, which would have to add dQ from many blocks in memory: in an order
 // that changes from run to run, or with waits between blocks.  So every result has one order of its sums.
+#include <atomic>
 #include "ps_tensor.cuh"
 
 namespace {
@@ -839,9 +840,15 @@ u32 smem_for(int tiles, int d, u32 more) {
   const u32 want = tiles * PANEL * (d / 64) + more;
   return want < 120 * 1024 ? 120 * 1024 : want;
 }
+// (once a kernel and device: the call takes half a microsecond)
 template <class K>
-cudaError_t allow(K kernel, u32 smem) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+cudaError_t allow(K kernel, u32 smem, std::atomic<u64>& done) {
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess || (device < 64 && (done.load(std::memory_order_relaxed) >> device & 1))) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess && device < 64) done.fetch_or((u64)1 << device, std::memory_order_relaxed);
+  return e;
 }
 
 template <class T, int D>
@@ -854,7 +861,8 @@ cudaError_t forward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
     return cudaErrorInvalidValue;
   }
   const u32 smem = smem_for(6, D, 1024), grid = (u32)((a.q_len + 2 * ROWS - 1) / (2 * ROWS)) * a.heads * a.batch;
-  cudaError_t e = allow(k_forward<T, D>, smem);
+  static std::atomic<u64> allowed{0};
+  cudaError_t e = allow(k_forward<T, D>, smem, allowed);
   if (e != cudaSuccess) return e;
   k_forward<T, D><<<grid, THREADS, smem, stream>>>(q, k, v, args_of(a));
   return cudaGetLastError();
@@ -885,13 +893,15 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
   }
   if (a.k_len) {
     const u32 smem = smem_for(7, D, 5 * ROWS * 4 + sizeof(Shared));
-    if ((e = allow(k_keys<T, D>, smem)) != cudaSuccess) return e;
+    static std::atomic<u64> allowed{0};
+    if ((e = allow(k_keys<T, D>, smem, allowed)) != cudaSuccess) return e;
     const u32 grid = (u32)((a.k_len + ROWS - 1) / ROWS) * a.kv_heads * a.batch;
     if ((e = launch_next(k_keys<T, D>, grid, THREADS, smem, stream, q, k, v, d, r)) != cudaSuccess) return e;
   }
   if (a.q_len) {
     const u32 smem = smem_for(7, D, sizeof(Shared));
-    if ((e = allow(k_queries<T, D>, smem)) != cudaSuccess) return e;
+    static std::atomic<u64> allowed{0};
+    if ((e = allow(k_queries<T, D>, smem, allowed)) != cudaSuccess) return e;
     const u32 grid = (u32)(r.padded / ROWS) * a.heads * a.batch;
     if (a.k_len) return launch_next(k_queries<T, D>, grid, THREADS, smem, stream, q, k, v, d, r);
     k_queries<T, D><<<grid, THREADS, smem, stream>>>(q, k, v, d, r);      // (no kernel is between it and the rows)

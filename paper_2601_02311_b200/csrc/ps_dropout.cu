@@ -46,92 +46,72 @@ struct Keep {
   float scale;
   __device__ __forceinline__ explicit Keep(const DropoutArgs& a)
       : least((u32)a.threshold), none(a.threshold >> 32), scale(a.scale) {}
-  __device__ __forceinline__ float of(u32 word, float x, float add) const {
-    return fmaf(word >= least && !none ? x : 0.f, scale, add);
-  }
+  __device__ __forceinline__ bool kept(u32 word) const { return word >= least && !none; }
+  __device__ __forceinline__ float of(bool kept, float x, float add) const { return fmaf(kept ? x : 0.f, scale, add); }
 };
 
-#ifndef DU
-#define DU 1
-#endif
-#ifndef DB
-#define DB 8
-#endif
-constexpr int UNROLL = DU, RESIDENT = DB;
-// A thread takes UNROLL packs of N consecutive elements (16 bytes) at a time, a grid apart; rows, strides and the
-// first element's index are such that packs are aligned in memory and begin with a word 0.
+constexpr int RESIDENT = 8;         // blocks of 256 threads on an SM
+// A thread takes N consecutive elements (16 bytes) at a time; rows, strides and the first element's index are such that packs
+// are aligned in memory and begin with a word 0.
 template <class T, int N, bool RESIDUAL>
 __global__ void __launch_bounds__(256, RESIDENT) k_packs(const DropoutArgs a, const __grid_constant__ Keys keys, u32 per_row, Divider by_row, u32 packs) {
   const Keep keep(a);
-  const u32 step = gridDim.x * 256;
-  for (u32 i = blockIdx.x * 256 + threadIdx.x; i < packs; i += step * UNROLL) {
-    Pack<T, N> x[UNROLL], y[UNROLL];
-    u32 row[UNROLL];
-    u64 column[UNROLL];
+  for (u32 i = blockIdx.x * 256 + threadIdx.x; i < packs; i += gridDim.x * 256) {
+    const u32 r = by_row.of(i);
+    const u64 c = (u64)(i - r * per_row) * N, counter = (a.first + r * a.pitch + c) >> 2;
+    Pack<T, N> x, y;
+    x.load((const T*)a.x + r * a.x_stride + c);
+    if (RESIDUAL) y.load((const T*)a.residual + r * a.residual_stride + c);
+    Words words[N / 4];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const u32 at = i + u * step;
-      row[u] = by_row.of(at);
-      column[u] = (u64)(at - row[u] * per_row) * N;
-      if (at < packs) {
-        x[u].load((const T*)a.x + row[u] * a.x_stride + column[u]);
-        if (RESIDUAL) y[u].load((const T*)a.residual + row[u] * a.residual_stride + column[u]);
-      }
-    }
+    for (int q = 0; q < N / 4; ++q) words[q] = philox(counter + q, a.stream, keys);
+    float v[N], add[N];
+    x.widen(v);
+    if (RESIDUAL) y.widen(add);
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const u64 counter = (a.first + row[u] * a.pitch + column[u]) >> 2;
-      Words words[N / 4];
-      float v[N], add[N];
-#pragma unroll
-      for (int q = 0; q < N / 4; ++q) words[q] = philox(counter + q, a.stream, keys);
-      if (i + u * step < packs) {
-        x[u].widen(v);
-        if (RESIDUAL) y[u].widen(add);
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = keep.of(words[e / 4].w[e % 4], v[e], RESIDUAL ? add[e] : 0.f);
-        y[u].narrow(v);
-        y[u].store((T*)a.y + row[u] * a.y_stride + column[u]);
-      }
-    }
+    for (int e = 0; e < N; ++e) v[e] = keep.of(keep.kept(words[e / 4].w[e % 4]), v[e], RESIDUAL ? add[e] : 0.f);
+    y.narrow(v);
+    y.store((T*)a.y + r * a.y_stride + c);
   }
 }
 
-// Any alignment: a thread takes the elements of a row that share a counter, element by element.
+// Any alignment: a warp takes SPAN elements of a row at a time, 32 counters for each 128 of them.  A lane draws the four words of a
+// counter but moves elements 32 apart, so that a warp's accesses are consecutive; four ballots carry the words' verdicts
+// over: bit i of the j-th says whether element 4 i + j is kept.
+constexpr int SPAN = 512, RESIDENT_GROUPS = 4;
 template <class T, bool RESIDUAL>
-__global__ void __launch_bounds__(256, RESIDENT) k_groups(const DropoutArgs a, const __grid_constant__ Keys keys, u32 per_row, Divider by_row, u32 groups) {
+__global__ void __launch_bounds__(256, RESIDENT_GROUPS) k_groups(const DropoutArgs a, const __grid_constant__ Keys keys, u32 per_row, Divider by_row, u32 items) {
   const Keep keep(a);
-  const u32 step = gridDim.x * 256;
-  for (u32 i = blockIdx.x * 256 + threadIdx.x; i < groups; i += step * UNROLL) {
-    float x[UNROLL][4], y[UNROLL][4];
-    u32 row[UNROLL];
-    u64 counter[UNROLL];
-    s64 column[UNROLL];                                         // of word 0: a row's first group may begin before it
+  const int lane = threadIdx.x % 32;
+  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += gridDim.x * 8) {
+    const u32 r = by_row.of(item), span = item - r * per_row;
+    const u64 begin = a.first + r * a.pitch;
+    // elements [low, high) of the SPAN from `column` on are the row's: its first counter may begin before it
+    const s64 column = (s64)span * SPAN - (s64)(begin & 3);
+    const int low = column < 0 ? (int)-column : 0, high = (int)min((s64)a.cols - column, (s64)SPAN);
+    const T* const from = (const T*)a.x + (s64)(r * a.x_stride) + column + lane;
+    const T* const more = (const T*)a.residual + (s64)(r * a.residual_stride) + column + lane;
+    T* const to = (T*)a.y + (s64)(r * a.y_stride) + column + lane;
+    float x[SPAN / 32], add[SPAN / 32];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const u32 at = i + u * step, r = by_row.of(at);
-      const u64 begin = a.first + r * a.pitch;
-      row[u] = r;
-      counter[u] = (begin >> 2) + (at - r * per_row);
-      column[u] = at < groups ? (s64)(counter[u] * 4 - begin) : (s64)a.cols;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const s64 c = column[u] + e;
-        x[u][e] = y[u][e] = 0.f;
-        if (c >= 0 && c < (s64)a.cols) {
-          x[u][e] = widen(((const T*)a.x)[(s64)(r * a.x_stride) + c]);
-          if (RESIDUAL) y[u][e] = widen(((const T*)a.residual)[(s64)(r * a.residual_stride) + c]);
-        }
+    for (int k = 0; k < SPAN / 32; ++k) {
+      x[k] = add[k] = 0.f;
+      if (lane + 32 * k >= low && lane + 32 * k < high) {
+        x[k] = widen(from[32 * k]);
+        if (RESIDUAL) add[k] = widen(more[32 * k]);
       }
     }
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const Words w = philox(counter[u], a.stream, keys);
+    for (int q = 0; q < SPAN / 128; ++q) {
+      if (128 * q >= high) break;
+      const Words w = philox((begin >> 2) + span * (SPAN / 4) + 32 * q + lane, a.stream, keys);
+      u32 kept[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const s64 c = column[u] + e;
-        if (c >= 0 && c < (s64)a.cols) ((T*)a.y)[(s64)(row[u] * a.y_stride) + c] = narrow<T>(keep.of(w.w[e], x[u][e], y[u][e]));
-      }
+      for (int j = 0; j < 4; ++j) kept[j] = __ballot_sync(0xffffffffu, keep.kept(w.w[j]));
+      const u32 mine = (lane & 2 ? (lane & 1 ? kept[3] : kept[2]) : (lane & 1 ? kept[1] : kept[0])) >> (lane / 4);
+#pragma unroll
+      for (int k = 4 * q; k < 4 * q + 4; ++k)
+        if (lane + 32 * k >= low && lane + 32 * k < high) to[32 * k] = narrow<T>(keep.of(mine >> (8 * (k % 4)) & 1, x[k], add[k]));
     }
   }
 }
@@ -151,7 +131,7 @@ cudaError_t dropout(DropoutArgs a, int sm_count, cudaStream_t stream) {
   // a launch for up to 2^31 items: whole rows, or of a single row a part (2^32 elements, a multiple of N and of 4)
   const u64 part = (u64)1 << 32;
   const u64 cols = a.rows == 1 && a.cols > part ? part : a.cols;
-  const u64 per_row = packs ? cols / N : cols / 4 + 2;
+  const u64 per_row = packs ? cols / N : (cols + 3 + SPAN - 1) / SPAN;
   if (per_row > 0x7fffffffu) return cudaErrorInvalidValue;        // (cols above 2^32 in rows of a larger tensor are refused before)
   const u64 rows = 0x7fffffffu / per_row;
   const Keys keys(a.seed);
@@ -164,8 +144,8 @@ cudaError_t dropout(DropoutArgs a, int sm_count, cudaStream_t stream) {
       p.x = (const T*)a.x + r * a.x_stride + c;
       if (RESIDUAL) p.residual = (const T*)a.residual + r * a.residual_stride + c;
       p.y = (T*)a.y + r * a.y_stride + c;
-      const u32 n = packs ? (u32)(p.cols / N) : (u32)(p.cols / 4 + 2), items = (u32)p.rows * n;
-      const u64 blocks = ((u64)items + 255) / 256, most = (u64)sm_count * RESIDENT;
+      const u32 n = packs ? (u32)(p.cols / N) : (u32)((p.cols + 3 + SPAN - 1) / SPAN), items = (u32)p.rows * n;
+      const u64 a_block = packs ? 256 : 8, blocks = (items + a_block - 1) / a_block, most = (u64)sm_count * (packs ? RESIDENT : RESIDENT_GROUPS);
       const u32 grid = (u32)(blocks < most ? blocks : most);
       if (packs) k_packs<T, N, RESIDUAL><<<grid, 256, 0, stream>>>(p, keys, n, Divider(n), items);
       else k_groups<T, RESIDUAL><<<grid, 256, 0, stream>>>(p, keys, n, Divider(n), items);

@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(256, LOOKUP_BLOCKS) k_lookup(EmbedArgs a, u32 
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = row < a.rows ? x[e] * a.scale : 0.f;
         v[i].narrow(x);
-        v[i].store(to + i * 32 * N);
+        v[i].store_passing(to + i * 32 * N);
       }
   }
 }
@@ -340,16 +340,22 @@ __global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces2(EmbedArgs a, Grad
 
 // A warp takes GROUP rows, LOADS packs a lane of each: their lists' bounds come in one load, so that rows without tokens, often
 // most of them, are a store each and nothing is waited for.
-constexpr int GRADIENT_BLOCKS = 3;
-template <class T, class G, int N, int GROUP, int LOADS, int AHEAD>
-__global__ void __launch_bounds__(256, GRADIENT_BLOCKS) k_gradient(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+template <class T, class G, int N, int GROUP, int LOADS, int AHEAD, int BLOCKS>
+__global__ void __launch_bounds__(256, BLOCKS) k_gradient(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
   wait_for_earlier();
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
-  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
+  auto ranges_of = [&](u32 item) {
+    const u32 row = by_chunk.of(item) * GROUP + lane;
+    return g.n && item < items && lane < GROUP && row < (u32)a.rows ? g.ranges[row] : make_uint2(0, 0);
+  };
+  u32 item = blockIdx.x * 8 + threadIdx.x / 32;
+  uint2 next = ranges_of(item);
+  for (; item < items; item += step) {
     const u32 first = by_chunk.of(item) * GROUP, rows = min((u32)GROUP, (u32)a.rows - first);
     const u64 column = (u64)(item - first / GROUP * chunks) * (32 * N * LOADS) + lane * N;
     const s64 columns = (s64)a.dim - (s64)column;
-    const uint2 ranges = g.n && lane < rows ? g.ranges[first + lane] : make_uint2(0, 0);
+    const uint2 ranges = next;
+    next = ranges_of(item + step);
     G* to = (G*)a.table + first * a.table_stride + column;
 #pragma unroll 1
     for (u32 r = 0; r < rows; ++r, to += a.table_stride) {
@@ -402,9 +408,7 @@ __global__ void __launch_bounds__(256, GRADIENT_BLOCKS) k_gradient(EmbedArgs a, 
 }
 
 // ------------------------------------------------------------------ host
-#ifndef SMALL_TABLE
-#define SMALL_TABLE ((u64)1 << 27)
-#endif
+constexpr u64 SMALL_TABLE = (u64)1 << 25;
 u32 chunks_of(u64 dim, int columns) { return (u32)((dim + columns - 1) / columns); }
 // columns of a row of sums, for every size of packs
 u64 width_of(u64 dim) { return (dim + 7) / 8 * 8; }
@@ -480,7 +484,7 @@ cudaError_t lookup(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   });
 }
 
-template <class T, class G, int N, int GROUP, int LOADS, int AHEAD>
+template <class T, class G, int N, int GROUP, int LOADS, int AHEAD, int BLOCKS>
 cudaError_t write_rows(const EmbedArgs& a, const GradientArgs& g, int sm_count, cudaStream_t stream) {
   const u32 chunks = chunks_of(a.dim, 32 * N * LOADS);
   cudaError_t e = cudaSuccess;
@@ -490,7 +494,7 @@ cudaError_t write_rows(const EmbedArgs& a, const GradientArgs& g, int sm_count, 
     part.table = (G*)a.table + at * GROUP * a.table_stride;
     part.rows = a.rows - at * GROUP;
     gp.ranges = g.ranges + (g.n ? at * GROUP : 0);
-    const cudaError_t e1 = launch_next(k_gradient<T, G, N, GROUP, LOADS, AHEAD>, grid_for(count * chunks, sm_count, GRADIENT_BLOCKS), 256, 0,
+    const cudaError_t e1 = launch_next(k_gradient<T, G, N, GROUP, LOADS, AHEAD, BLOCKS>, grid_for(count * chunks, sm_count, BLOCKS), 256, 0,
                                        stream, part, gp, chunks, Divider(chunks), count * chunks);
     if (e1 != cudaSuccess) e = e1;
   });
@@ -548,9 +552,10 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
     if ((e = launch_next(k_pieces2, grid_for(items, sm_count, PIECE_BLOCKS), 256, 0, stream, a, g, chunks, Divider(chunks), items)) != cudaSuccess)
       return e;
   }
-  // a warp's share of a small table is small, of a large one the better one for bandwidth
-  if (a.rows * a.dim <= SMALL_TABLE) return write_rows<T, G, N, 4, 1, 8>(a, g, sm_count, stream);
-  return write_rows<T, G, N, 8, 2, 4>(a, g, sm_count, stream);
+  // (32000 rows of 768: 33.8 us with 256 columns a warp, 37.9 with 512; 256000 rows of 8192: 1225 and 1194; alike between 2^26 and
+  // 2^30 elements)
+  if (a.rows * a.dim <= SMALL_TABLE) return write_rows<T, G, N, 8, 1, 4, 5>(a, g, sm_count, stream);
+  return write_rows<T, G, N, 8, 2, 4, 3>(a, g, sm_count, stream);
 }
 
 // packs of 16 bytes of the values that are read, where both tensors allow it

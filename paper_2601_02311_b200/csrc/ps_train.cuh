@@ -60,6 +60,15 @@ struct Pack {
       for (int i = 0; i < WORDS; ++i) reinterpret_cast<u32*>(p)[i] = w[i];
     }
   }
+  // for results that this kernel does not read again: they are the first to leave the L2
+  __device__ __forceinline__ void store_passing(T* p) const {
+    if (WORDS % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 4) __stcs(reinterpret_cast<uint4*>(p) + i / 4, make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]));
+    } else {
+      store(p);
+    }
+  }
   __device__ __forceinline__ void widen(float (&v)[N]) const {
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = one(w, e, (const T*)nullptr);

@@ -375,7 +375,7 @@ class Context:
                 first: int = 0, pitch: int | None = None) -> torch.Tensor:
         """x with a share p of its elements dropped and the others divided by 1 - p, plus `residual`.
         The gradient of x is the same call on the result's gradient, without a residual."""
-        y = x.new_empty(x.shape)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
         self.dropout_into(x, y, p, seed, stream, residual, first, pitch)
         return y
 
@@ -473,7 +473,7 @@ class Context:
         if q.dim() != 4:
             self._refuse(E_RANGE, "ps_attention_forward", "q has to be [batch, len, heads, dim]")
         shape = q.shape
-        out = q.new_empty(shape)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
         lse = q.new_empty((shape[0], shape[2], shape[1]), dtype=torch.float32)
         self.attention_forward_into(q, k, v, out, lse, scale, causal, q_lens, k_lens)
         return out, lse
@@ -499,7 +499,7 @@ class Context:
                            d_out: torch.Tensor, scale: float | None = None, causal: bool = True,
                            q_lens: torch.Tensor | None = None, k_lens: torch.Tensor | None = None):
         """(d_q, d_k, d_v), contiguous."""
-        d_q, d_k, d_v = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+        d_q, d_k, d_v = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
         self.attention_backward_into(q, k, v, out, lse, d_out, d_q, d_k, d_v, scale, causal, q_lens, k_lens)
         return d_q, d_k, d_v
 
