@@ -120,11 +120,12 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           const __grid_constant__ CUtensorMap map_v, const Args a) {
   constexpr u32 TILE = PANEL * (D / 64);
   constexpr int RING = 4;
-  __shared__ u64 bars[2 + 2 * RING + 6];
+  constexpr bool TMEM = D == 64;          // Q is the left operand from tensor memory where there is room for it
+  __shared__ u64 bars[2 + 2 * RING + 8];
   __shared__ u32 tmem_at;
   const u32 tiles = tiles_begin(), ring = tiles + 2 * TILE;
   const u32 q_full = smem_address(bars), full = q_full + 16, empty = full + 8 * RING, s_full = empty + 8 * RING,
-            p_ready = s_full + 16, o_done = p_ready + 16;
+            p_ready = s_full + 16, o_done = p_ready + 16, in_tmem = o_done + 16;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
   // the tiles with the most keys first
@@ -141,6 +142,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       barrier_init(s_full + 8 * t, 1);
       barrier_init(p_ready + 8 * t, 4);
       barrier_init(o_done + 8 * t, 1);
+      barrier_init(in_tmem + 8 * t, 4);
     }
     for (int i = 0; i < RING; ++i) {
       barrier_init(full + 8 * i, 1);
@@ -151,7 +153,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   fence_before();
   __syncthreads();
   fence_after();
-  const u32 tmem = tmem_at;
+  const u32 tmem = tmem_at, tmem_q = tmem + 2 * ROWS + 2 * D;      // (D = 64)
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
@@ -162,6 +164,11 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const int masked = (q0 + (t + 1) * ROWS > l.n ? 0 : end_of(a, l, q0 + t * ROWS)) / ROWS;
     const float slack = 8.f / a.c;
     float most_s = MINUS_INF, total = 0.f;
+    if (TMEM && count[t]) {
+      w.wait(q_full + 8 * t, 0);
+      tile_to_tmem<D>(tmem_q + lanes + t * (D / 2), tiles + t * TILE);
+      if (lane == 0) barrier_arrive(in_tmem + 8 * t);
+    }
     for (int j = 0; j < count[t]; ++j) {
       w.wait(s_full + 8 * t, j & 1);
       fence_after();
@@ -250,14 +257,17 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     give_registers<LEFT>();
     const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_o = instruction<T>(D, true, false);
     auto scores = [&](int t, int j) {
-      multiply_along<D>(tmem + t * ROWS, tiles + t * TILE, ring + (2 * j % RING) * TILE, ins_s);
+      const u32 k = ring + (2 * j % RING) * TILE;
+      if (TMEM) multiply_along_tmem<D>(tmem + t * ROWS, tmem_q + t * (D / 2), k, ins_s);
+      else multiply_along<D>(tmem + t * ROWS, tiles + t * TILE, k, ins_s);
       commit(s_full + 8 * t);
     };
     if (most > 0) {
       w.wait(full, 0);
       for (int t = 0; t < 2; ++t)
         if (count[t]) {
-          w.wait(q_full + 8 * t, 0);
+          w.wait((TMEM ? in_tmem : q_full) + 8 * t, 0);
+          fence_after();
           if (elected() && !w.dead) scores(t, 0);
         }
       if (elected() && !w.dead) commit(empty);
@@ -374,13 +384,14 @@ __global__ void __launch_bounds__(THREADS, 1)
 k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
   constexpr u32 TILE = PANEL * (D / 64), VECTOR = ROWS * 4;
+  constexpr bool TMEM = D == 64;          // K and V are left operands from tensor memory where there is room for them
   extern __shared__ __align__(1024) unsigned char shared[];
   const u32 k_tile = smem_address(shared), v_tile = k_tile + TILE, q_ring = v_tile + TILE, do_ring = q_ring + 3 * TILE,
             lse_ring = do_ring + 2 * TILE, delta_ring = lse_ring + 3 * VECTOR;
   Shared& sh = *reinterpret_cast<Shared*>(shared + 7 * TILE + 5 * VECTOR);
   const u32 kv_full = smem_address(sh.bars), q_full = kv_full + 8, q_empty = q_full + 24, do_full = q_empty + 24, do_empty = do_full + 16,
             delta_full = do_empty + 16, s_full = delta_full + 16, p_ready = s_full + 16, dp_full = p_ready + 16,
-            ds_ready = dp_full + 16, done = ds_ready + 16;
+            ds_ready = dp_full + 16, done = ds_ready + 16, in_tmem = done + 8;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
   // (under the causal mask the first keys have the most queries)
@@ -407,6 +418,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       barrier_init(ds_ready + 8 * i, 4);
     }
     barrier_init(done, 1);
+    barrier_init(in_tmem, 8);
     fence_barrier_init();
   }
   fence_before();
@@ -414,7 +426,8 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   fence_after();
   wait_for_earlier();          // the rows
   let_next_begin();            // behind the wait: k_queries needs the rows too, and nothing of this kernel
-  const u32 tmem = sh.tmem_at, tmem_dv = tmem + 2 * ROWS, tmem_dk = tmem_dv + D;
+  const u32 tmem = sh.tmem_at, tmem_dv = tmem + 2 * ROWS, tmem_dk = tmem_dv + D,
+            tmem_k = tmem_dk + D, tmem_v = tmem_k + D / 2;      // (D = 64)
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
@@ -426,6 +439,12 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
     const int whole = j0 + ROWS > l.m ? 0x7fffffff : a.causal ? j0 + ROWS - 1 - l.m + l.n : 0;
     const float factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
     const u64 cs = pair(a.c, a.c), factors = pair(factor, factor);
+    if (TMEM && total > 0) {
+      w.wait(kv_full, 0);
+      if (mine == 0) tile_to_tmem<D>(tmem_k + lanes, k_tile);
+      else tile_to_tmem<D>(tmem_v + lanes, v_tile);
+      if (lane == 0) barrier_arrive(in_tmem);
+    }
     for (int x = mine; x < total; x += 2) {
       const int i0 = (first + x % walk) * ROWS, turn = x >> 1 & 1;
       const float4* const lse_at = reinterpret_cast<const float4*>(shared + 7 * TILE + x % 3 * VECTOR);
@@ -544,13 +563,15 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       w.wait(q_full + 8 * (x % 3), x / 3 & 1);
       if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
       if (elected() && !w.dead) {
-        multiply_along<D>(tmem + (x & 1) * ROWS, k_tile, q, ins_s);
+        if (TMEM) multiply_along_tmem<D>(tmem + (x & 1) * ROWS, tmem_k, q, ins_s);
+        else multiply_along<D>(tmem + (x & 1) * ROWS, k_tile, q, ins_s);
         commit(s_full + 8 * (x & 1));
       }
       __syncwarp();
     };
     if (total > 0) {
-      w.wait(kv_full, 0);
+      w.wait(TMEM ? in_tmem : kv_full, 0);
+      fence_after();
       scores(0);
       if (total > 1) scores(1);
     }
@@ -565,7 +586,8 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
         fence_after();
         if (elected() && !w.dead) {
           multiply_across(tmem_dv, tmem + two * ROWS, d, ins_acc, x > 0);
-          multiply_along<D>(tmem + two * ROWS, v_tile, d, ins_dp);
+          if (TMEM) multiply_along_tmem<D>(tmem + two * ROWS, tmem_v, d, ins_dp);
+          else multiply_along<D>(tmem + two * ROWS, v_tile, d, ins_dp);
           commit(dp_full + 8 * two);
           commit(do_empty + 8 * two);
         }
@@ -609,7 +631,8 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   const u32 q_tile = smem_address(shared), do_tile = q_tile + TILE, k_ring = do_tile + TILE, v_ring = k_ring + 3 * TILE;
   Shared& sh = *reinterpret_cast<Shared*>(shared + 7 * TILE);
   const u32 q_full = smem_address(sh.bars), k_full = q_full + 8, k_empty = k_full + 24, v_full = k_empty + 24, v_empty = v_full + 16,
-            s_full = v_empty + 16, s_read = s_full + 16, dp_full = s_read + 16, ds_ready = dp_full + 16, done = ds_ready + 16;
+            s_full = v_empty + 16, s_read = s_full + 16, dp_full = s_read + 16, ds_ready = dp_full + 16, done = ds_ready + 16,
+            in_tmem = done + 8;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
   const int per = a.heads * a.batch, n_tiles = (a.q_len + ROWS - 1) / ROWS, order = blockIdx.x / per;
@@ -634,12 +657,13 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       barrier_init(ds_ready + 8 * i, 4);
     }
     barrier_init(done, 1);
+    barrier_init(in_tmem, 8);
     fence_barrier_init();
   }
   fence_before();
   __syncthreads();
   fence_after();
-  const u32 tmem = sh.tmem_at, tmem_dq = tmem + 2 * ROWS;
+  const u32 tmem = sh.tmem_at, tmem_dq = tmem + 2 * ROWS, tmem_q = tmem_dq + D, tmem_do = tmem_q + D / 2;
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
@@ -650,6 +674,12 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const u64 row = ((u64)b * a.heads + h) * a.padded + i;
     const float off = a.lse2[row], delta = a.delta[row], factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
     const u64 cs = pair(a.c, a.c), offs = pair(off, off), deltas = pair(delta, delta), factors = pair(factor, factor);
+    if (total > 0) {            // Q and dO are left operands of every pair
+      w.wait(q_full, 0);
+      if (mine == 0) tile_to_tmem<D>(tmem_q + lanes, q_tile);
+      else tile_to_tmem<D>(tmem_do + lanes, do_tile);
+      if (lane == 0) barrier_arrive(in_tmem);
+    }
     for (int x = mine; x < total; x += 2) {
       const int turn = x >> 1 & 1;
       w.wait(s_full + 8 * mine, turn);
@@ -739,13 +769,14 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       w.wait(k_full + 8 * (x % 3), x / 3 & 1);
       if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
       if (elected() && !w.dead) {
-        multiply_along<D>(tmem + (x & 1) * ROWS, q_tile, k, ins_s);
+        multiply_along_tmem<D>(tmem + (x & 1) * ROWS, tmem_q, k, ins_s);
         commit(s_full + 8 * (x & 1));
       }
       __syncwarp();
     };
     if (total > 0) {
-      w.wait(q_full, 0);
+      w.wait(in_tmem, 0);
+      fence_after();
       scores(0);
       if (total > 1) scores(1);
     }
@@ -759,7 +790,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         w.wait(s_read + 8 * two, turn);
         fence_after();
         if (elected() && !w.dead) {
-          multiply_along<D>(tmem + two * ROWS, do_tile, v, ins_dp);
+          multiply_along_tmem<D>(tmem + two * ROWS, tmem_do, v, ins_dp);
           commit(dp_full + 8 * two);
           commit(v_empty + 8 * two);
         }

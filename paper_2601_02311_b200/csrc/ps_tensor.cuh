@@ -128,6 +128,25 @@ __device__ __forceinline__ void tmem_store16(u32 at, const u32 (&v)[16]) {
       ::PS_I8(v, 0), PS_I8(v, 8), "r"(at) : "memory");
 }
 
+// a tile's rows from shared memory to the lanes of tensor memory, by four warps: a thread has a row
+template <int D>
+__device__ __forceinline__ void tile_to_tmem(u32 at, u32 tile) {
+  const u32 row = threadIdx.x % ROWS;
+#pragma unroll
+  for (int p = 0; p < D / 64; ++p) {
+    u32 v[32];
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(v[4 * c]), "=r"(v[4 * c + 1]), "=r"(v[4 * c + 2]), "=r"(v[4 * c + 3])
+                   : "r"(tile + p * PANEL + row * 128 + ((c ^ (row & 7)) << 4)));
+    tmem_store32(at + 32 * p, v);
+  }
+  wait_stores();
+  fence_before();
+  __syncwarp();
+}
+
 // ---- products
 // Operand descriptors: start, leading and stride offsets in 16-byte units, 128-byte swizzle.  Of a tile's descriptors only the
 // start differs, in the low word; a step of 16 along the contraction adds a constant to it.
@@ -171,6 +190,14 @@ __device__ __forceinline__ void multiply_along(u32 d, u32 a, u32 b, u32 ins) {
   const u32 x = desc_along(a), y = desc_along(b);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) mma_smem(d, x + step_along(s), y + step_along(s), ins, s > 0);
+}
+// the same with a in tensor memory, D columns of 16 bits: only b's tile is read from shared memory, whose 128 bytes a cycle both
+// tiles of 128 rows just use up
+template <int D>
+__device__ __forceinline__ void multiply_along_tmem(u32 d, u32 a, u32 b, u32 ins) {
+  const u32 y = desc_along(b);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) mma_tmem(d, a + 8 * s, y + step_along(s), ins, s > 0);
 }
 // d (+)= a b: a in tensor memory, its 128 columns of 16 bits against the rows of tile b
 __device__ __forceinline__ void multiply_across(u32 d, u32 a, u32 b, u32 ins, bool add) {
