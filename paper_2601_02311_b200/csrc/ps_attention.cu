@@ -324,44 +324,61 @@ __device__ __forceinline__ float gradient_factor(const Args& a, int b, int kh) {
 }
 
 // The rows that both kernels read: 16 lanes a query, delta and the exponent's offset; in half precision the largest
-// norms of each key head's dO and V rows as well (as bits: norms are not negative, so they compare as integers).
+// norms of each key head's dO and V rows as well (as bits: norms are not negative, so they compare as integers), one atomic
+// a block.
+constexpr int ROWS_A_THREAD = 4, ROWS_A_BLOCK = 16 * ROWS_A_THREAD;
 template <class T, bool QUERY>
 __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads out, const Args a) {
   let_next_begin();
-  const int part = threadIdx.x % 16, i = blockIdx.x * 16 + threadIdx.x / 16, h = blockIdx.y, b = blockIdx.z;
+  __shared__ u32 largest;
+  if (Range<T>::small) {
+    if (threadIdx.x == 0) largest = 0;
+    __syncthreads();
+  }
+  const int part = threadIdx.x % 16, first = blockIdx.x * ROWS_A_BLOCK + threadIdx.x / 16, h = blockIdx.y, b = blockIdx.z;
   const Lengths l = lengths_of(a, b);
-  const bool there = i < (QUERY ? l.n : l.m);
-  float v[8] = {}, dot = 0.f, norm = 0.f;
-  if (there && part * 8 < a.dim) {
-    Pack<T, 8> p;
-    p.load(row_of<const T>(x, b, i, h) + part * 8);
-    p.widen(v);
-    if (QUERY) {
-      float y[8];
-      p.load(row_of<const T>(out, b, i, h) + part * 8);
-      p.widen(y);
+  Pack<T, 8> p[ROWS_A_THREAD], q[ROWS_A_THREAD];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dot = fmaf(v[e], y[e], dot);
+  for (int r = 0; r < ROWS_A_THREAD; ++r) {
+    const int i = first + 16 * r;
+    p[r].clear();
+    q[r].clear();
+    if (i < (QUERY ? l.n : l.m) && part * 8 < a.dim) {
+      p[r].load(row_of<const T>(x, b, i, h) + part * 8);
+      if (QUERY) q[r].load(row_of<const T>(out, b, i, h) + part * 8);
     }
-    if (Range<T>::small)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) norm = fmaf(v[e], v[e], norm);
   }
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) {
-    if (QUERY) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-    if (Range<T>::small) norm += __shfl_xor_sync(0xffffffffu, norm, o);
+  for (int r = 0; r < ROWS_A_THREAD; ++r) {
+    const int i = first + 16 * r;
+    float v[8], y[8], dot = 0.f, norm = 0.f;
+    p[r].widen(v);
+    q[r].widen(y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (QUERY) dot = fmaf(v[e], y[e], dot);
+      if (Range<T>::small) norm = fmaf(v[e], v[e], norm);
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
+      if (QUERY) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      if (Range<T>::small) norm += __shfl_xor_sync(0xffffffffu, norm, o);
+    }
+    if (part != 0) continue;
+    if (QUERY) {
+      const u64 head = (u64)b * a.heads + h;
+      const float lse = i < l.n ? a.lse[head * a.q_len + i] : MINUS_INF;
+      a.lse2[head * a.padded + i] = lse == MINUS_INF || end_of(a, l, i) == 0 ? MINUS_INF : (Range<T>::small ? P_SHIFT : 0) - lse * LOG2E;
+      a.delta[head * a.padded + i] = -dot;
+    }
+    if (Range<T>::small) atomicMax(&largest, __float_as_uint(norm));
   }
-  if (part != 0) return;
-  if (QUERY) {
-    const u64 head = (u64)b * a.heads + h;
-    const float lse = there ? a.lse[head * a.q_len + i] : MINUS_INF;
-    a.lse2[head * a.padded + i] = lse == MINUS_INF || end_of(a, l, i) == 0 ? MINUS_INF : (Range<T>::small ? P_SHIFT : 0) - lse * LOG2E;
-    a.delta[head * a.padded + i] = -dot;
+  if (Range<T>::small) {
+    __syncthreads();
+    if (threadIdx.x == 0) atomicMax(a.norms + 2 * (b * a.kv_heads + (QUERY ? h / (a.heads / a.kv_heads) : h)) + (QUERY ? 0 : 1), largest);
   }
-  if (Range<T>::small && there)
-    atomicMax(a.norms + 2 * (b * a.kv_heads + (QUERY ? h / (a.heads / a.kv_heads) : h)) + (QUERY ? 0 : 1), __float_as_uint(norm));
 }
+static_assert(ROWS % ROWS_A_BLOCK == 0, "whole blocks of rows in whole tiles");
 
 // Both kernels of the backward pass let their two groups of warps take turns: tile pairs are numbered, a group has the even
 // ones and the other the odd ones, each with a buffer of 128 columns of tensor memory of its own, a thread a row.  A
@@ -913,13 +930,13 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
   if (Range<T>::small) {
     e = cudaMemsetAsync(r.norms, 0, sizeof(u32) * 2 * a.batch * a.kv_heads, stream);
     if (e == cudaSuccess && a.k_len) {
-      k_rows<T, false><<<dim3((a.k_len + 15) / 16, a.kv_heads, a.batch), 256, 0, stream>>>(a.v, a.v, r);
+      k_rows<T, false><<<dim3((a.k_len + ROWS_A_BLOCK - 1) / ROWS_A_BLOCK, a.kv_heads, a.batch), 256, 0, stream>>>(a.v, a.v, r);
       e = cudaGetLastError();
     }
     if (e != cudaSuccess) return e;
   }
   if (a.q_len) {
-    k_rows<T, true><<<dim3(r.padded / 16, a.heads, a.batch), 256, 0, stream>>>(a.d_out, a.out, r);
+    k_rows<T, true><<<dim3(r.padded / ROWS_A_BLOCK, a.heads, a.batch), 256, 0, stream>>>(a.d_out, a.out, r);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   if (a.k_len) {
