@@ -927,7 +927,7 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
   if (!a.q_len) q = d = k;        // on one side there is nothing: never read
   if (!a.k_len) k = v = q;
   cudaError_t e;
-  if (Range<T>::small) {
+  if constexpr (Range<T>::small) {
     e = cudaMemsetAsync(r.norms, 0, sizeof(u32) * 2 * a.batch * a.kv_heads, stream);
     if (e == cudaSuccess && a.k_len) {
       k_rows<T, false><<<dim3((a.k_len + ROWS_A_BLOCK - 1) / ROWS_A_BLOCK, a.kv_heads, a.batch), 256, 0, stream>>>(a.v, a.v, r);
