@@ -229,7 +229,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       if (lane == 0) barrier_arrive(p_ready + 8 * t);
     }
     if (count[t]) {
-      w.wait(o_done + 8 * t, 0);
+      w.wait(o_done + 8 * t, (count[t] - 1) & 1);
       fence_after();
     }
     const bool there = i < a.q_len;
@@ -284,8 +284,14 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         fence_after();
         if (elected() && !w.dead) {
           multiply_across(tmem + 2 * ROWS + t * D, tmem + t * ROWS, v, ins_o, j > 0);
-          if (j + 1 < count[t]) scores(t, j + 1);
-          else commit(o_done + 8 * t);
+          commit(o_done + 8 * t);
+        }
+        __syncwarp();
+        if (j + 1 < count[t]) {           // S goes over P, which that product reads: nothing but its end orders the two
+          w.wait(o_done + 8 * t, j & 1);
+          fence_after();
+          if (elected() && !w.dead) scores(t, j + 1);
+          __syncwarp();
         }
       }
       if (elected() && !w.dead) {
@@ -408,7 +414,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   Shared& sh = *reinterpret_cast<Shared*>(shared + 7 * TILE + 5 * VECTOR);
   const u32 kv_full = smem_address(sh.bars), q_full = kv_full + 8, q_empty = q_full + 24, do_full = q_empty + 24, do_empty = do_full + 16,
             delta_full = do_empty + 16, s_full = delta_full + 16, p_ready = s_full + 16, dp_full = p_ready + 16,
-            ds_ready = dp_full + 16, done = ds_ready + 16, in_tmem = done + 8;
+            ds_ready = dp_full + 16, done = ds_ready + 16, in_tmem = done + 8, dv_done = in_tmem + 8;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
   // (under the causal mask the first keys have the most queries)
@@ -433,6 +439,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       barrier_init(p_ready + 8 * i, 4);
       barrier_init(dp_full + 8 * i, 1);
       barrier_init(ds_ready + 8 * i, 4);
+      barrier_init(dv_done + 8 * i, 1);
     }
     barrier_init(done, 1);
     barrier_init(in_tmem, 8);
@@ -592,36 +599,62 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       scores(0);
       if (total > 1) scores(1);
     }
-    for (int x0 = 0; x0 < total; x0 += 2) {
-      const int turn = x0 >> 1 & 1, end = min(x0 + 2, total);
-      for (int x = x0; x < end; ++x) {
-        const int two = x & 1;
-        const u32 d = do_ring + two * TILE;
-        w.wait(do_full + 8 * two, turn);
-        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
-        w.wait(p_ready + 8 * two, turn);
-        fence_after();
-        if (elected() && !w.dead) {
-          multiply_across(tmem_dv, tmem + two * ROWS, d, ins_acc, x > 0);
-          if (TMEM) multiply_along_tmem<D>(tmem + two * ROWS, tmem_v, d, ins_dp);
-          else multiply_along<D>(tmem + two * ROWS, v_tile, d, ins_dp);
-          commit(dp_full + 8 * two);
-          commit(do_empty + 8 * two);
-        }
-        __syncwarp();
+    // A product that writes a buffer waits for the end of the one that reads it: nothing else orders the two.  So the products
+    // of the two pairs are interleaved.
+    auto values = [&](int x) {                 // dV += P^T dO
+      const int two = x & 1;
+      const u32 d = do_ring + two * TILE;
+      w.wait(do_full + 8 * two, x >> 1 & 1);
+      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+      w.wait(p_ready + 8 * two, x >> 1 & 1);
+      fence_after();
+      if (elected() && !w.dead) {
+        multiply_across(tmem_dv, tmem + two * ROWS, d, ins_acc, x > 0);
+        commit(dv_done + 8 * two);
       }
-      for (int x = x0; x < end; ++x) {
-        const int two = x & 1;
-        const u32 q = q_ring + x % 3 * TILE;
-        w.wait(ds_ready + 8 * two, turn);
-        fence_after();
-        if (elected() && !w.dead) {
-          multiply_across(tmem_dk, tmem + two * ROWS, q, ins_acc, x > 0);
-          commit(q_empty + 8 * (x % 3));
-          if (x + 1 == total) commit(done);
-        }
-        __syncwarp();
-        if (x + 2 < total) scores(x + 2);
+      __syncwarp();
+    };
+    auto d_probabilities = [&](int x) {        // dP^T = V dO^T, over P^T
+      const int two = x & 1;
+      const u32 d = do_ring + two * TILE;
+      w.wait(dv_done + 8 * two, x >> 1 & 1);
+      fence_after();
+      if (elected() && !w.dead) {
+        if (TMEM) multiply_along_tmem<D>(tmem + two * ROWS, tmem_v, d, ins_dp);
+        else multiply_along<D>(tmem + two * ROWS, v_tile, d, ins_dp);
+        commit(dp_full + 8 * two);
+        commit(do_empty + 8 * two);
+      }
+      __syncwarp();
+    };
+    auto keys = [&](int x) {                   // dK += dS^T Q
+      const int two = x & 1;
+      w.wait(ds_ready + 8 * two, x >> 1 & 1);
+      fence_after();
+      if (elected() && !w.dead) {
+        multiply_across(tmem_dk, tmem + two * ROWS, q_ring + x % 3 * TILE, ins_acc, x > 0);
+        commit(q_empty + 8 * (x % 3));
+        if (x + 1 == total) commit(done);
+      }
+      __syncwarp();
+    };
+    auto next_scores = [&](int x) {            // S^T of pair x + 2, over dS^T of pair x
+      if (x + 2 >= total) return;
+      w.wait(q_empty + 8 * (x % 3), x / 3 & 1);
+      fence_after();
+      scores(x + 2);
+    };
+    for (int x = 0; x < total; x += 2) {
+      const bool both = x + 1 < total;
+      values(x);
+      d_probabilities(x);
+      if (both) values(x + 1);
+      keys(x);
+      if (both) d_probabilities(x + 1);
+      next_scores(x);
+      if (both) {
+        keys(x + 1);
+        next_scores(x + 1);
       }
     }
   } else {
@@ -797,34 +830,46 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       scores(0);
       if (total > 1) scores(1);
     }
-    for (int x0 = 0; x0 < total; x0 += 2) {
-      const int turn = x0 >> 1 & 1, end = min(x0 + 2, total);
-      for (int x = x0; x < end; ++x) {
-        const int two = x & 1;
-        const u32 v = v_ring + two * TILE;
-        w.wait(v_full + 8 * two, turn);
-        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
-        w.wait(s_read + 8 * two, turn);
-        fence_after();
-        if (elected() && !w.dead) {
-          multiply_along_tmem<D>(tmem + two * ROWS, tmem_do, v, ins_dp);
-          commit(dp_full + 8 * two);
-          commit(v_empty + 8 * two);
-        }
-        __syncwarp();
+    auto d_probabilities = [&](int x) {        // dP = dO V^T, over S, which has been read
+      const int two = x & 1;
+      const u32 v = v_ring + two * TILE;
+      w.wait(v_full + 8 * two, x >> 1 & 1);
+      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
+      w.wait(s_read + 8 * two, x >> 1 & 1);
+      fence_after();
+      if (elected() && !w.dead) {
+        multiply_along_tmem<D>(tmem + two * ROWS, tmem_do, v, ins_dp);
+        commit(dp_full + 8 * two);
+        commit(v_empty + 8 * two);
       }
-      for (int x = x0; x < end; ++x) {
-        const int two = x & 1;
-        const u32 k = k_ring + x % 3 * TILE;
-        w.wait(ds_ready + 8 * two, turn);
-        fence_after();
-        if (elected() && !w.dead) {
-          multiply_across(tmem_dq, tmem + two * ROWS, k, ins_acc, x > 0);
-          commit(k_empty + 8 * (x % 3));
-          if (x + 1 == total) commit(done);
-        }
-        __syncwarp();
-        if (x + 2 < total) scores(x + 2);
+      __syncwarp();
+    };
+    auto queries = [&](int x) {                // dQ += dS K
+      const int two = x & 1;
+      w.wait(ds_ready + 8 * two, x >> 1 & 1);
+      fence_after();
+      if (elected() && !w.dead) {
+        multiply_across(tmem_dq, tmem + two * ROWS, k_ring + x % 3 * TILE, ins_acc, x > 0);
+        commit(k_empty + 8 * (x % 3));
+        if (x + 1 == total) commit(done);
+      }
+      __syncwarp();
+    };
+    auto next_scores = [&](int x) {            // S of pair x + 2, over dS of pair x: that product has to be done
+      if (x + 2 >= total) return;
+      w.wait(k_empty + 8 * (x % 3), x / 3 & 1);
+      fence_after();
+      scores(x + 2);
+    };
+    for (int x = 0; x < total; x += 2) {
+      const bool both = x + 1 < total;
+      d_probabilities(x);
+      if (both) d_probabilities(x + 1);
+      queries(x);
+      next_scores(x);
+      if (both) {
+        queries(x + 1);
+        next_scores(x + 1);
       }
     }
   } else {
