@@ -27,8 +27,8 @@ using namespace tensor;
 
 constexpr float MINUS_INF = -INFINITY;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int THREADS = 384;            // two groups of four warps, and one of the copying warp, the products' warp and two idle ones
-constexpr int COPY_WARP = 8, MMA_WARP = 9;
+constexpr int THREADS = 384;            // two groups of four warps, and one of the copying warp, the two that start products and an idle one
+constexpr int COPY_WARP = 8, MMA_WARP = 9, MMA_WARP2 = 10;
 // registers of a thread: as launched, and as the third group gives to the others (3 * 168 = 2 * 208 + 88)
 constexpr int LAUNCHED = 168, TAKEN = 208, LEFT = 88;
 static_assert(3 * LAUNCHED == 2 * TAKEN + LEFT && THREADS * LAUNCHED <= 65536, "registers that the block has");
@@ -574,87 +574,84 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
         load_bytes(delta_ring + two * VECTOR, a.delta + row, VECTOR, delta_full + 8 * two);
       }
     }
-  } else if (warp == MMA_WARP) {
+  } else if (warp == MMA_WARP || warp == MMA_WARP2) {
+    // One warp starts the sums dV and dK, in the pairs' order, the other the products that fill the buffers.  A product that
+    // writes a buffer waits for the end of the one that reads it: nothing else orders the two.
     give_registers<LEFT>();
-    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false), ins_acc = instruction<T>(D, true, false);
     // queries behind the sequence's end, in its last tile
     auto pad_from = [&](int x) {
       const int i0 = (first + x % walk) * ROWS;
       return l.n < a.q_len && i0 + ROWS > l.n ? l.n - i0 : ROWS;
     };
-    auto scores = [&](int x) {
-      const u32 q = q_ring + x % 3 * TILE;
-      w.wait(q_full + 8 * (x % 3), x / 3 & 1);
-      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
-      if (elected() && !w.dead) {
-        if (TMEM) multiply_along_tmem<D>(tmem + (x & 1) * ROWS, tmem_k, q, ins_s);
-        else multiply_along<D>(tmem + (x & 1) * ROWS, k_tile, q, ins_s);
-        commit(s_full + 8 * (x & 1));
+    if (warp == MMA_WARP) {
+      const u32 ins = instruction<T>(D, true, false);
+      auto values = [&](int x) {                 // dV += P^T dO
+        const int two = x & 1;
+        const u32 d = do_ring + two * TILE;
+        w.wait(do_full + 8 * two, x >> 1 & 1);
+        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+        w.wait(p_ready + 8 * two, x >> 1 & 1);
+        fence_after();
+        if (elected() && !w.dead) {
+          multiply_across(tmem_dv, tmem + two * ROWS, d, ins, x > 0);
+          commit(dv_done + 8 * two);
+        }
+        __syncwarp();
+      };
+      auto keys = [&](int x) {                   // dK += dS^T Q
+        const int two = x & 1;
+        w.wait(ds_ready + 8 * two, x >> 1 & 1);
+        fence_after();
+        if (elected() && !w.dead) {
+          multiply_across(tmem_dk, tmem + two * ROWS, q_ring + x % 3 * TILE, ins, x > 0);
+          commit(q_empty + 8 * (x % 3));
+          if (x + 1 == total) commit(done);
+        }
+        __syncwarp();
+      };
+      for (int x = 0; x < total; x += 2) {
+        values(x);
+        if (x + 1 < total) values(x + 1);
+        keys(x);
+        if (x + 1 < total) keys(x + 1);
       }
-      __syncwarp();
-    };
-    if (total > 0) {
+    } else if (total > 0) {
+      const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false);
+      auto scores = [&](int x) {                 // S^T = K Q^T, over dS^T of pair x - 2
+        const u32 q = q_ring + x % 3 * TILE;
+        w.wait(q_full + 8 * (x % 3), x / 3 & 1);
+        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
+        if (x >= 2) w.wait(q_empty + 8 * ((x - 2) % 3), (x - 2) / 3 & 1);
+        fence_after();
+        if (elected() && !w.dead) {
+          if (TMEM) multiply_along_tmem<D>(tmem + (x & 1) * ROWS, tmem_k, q, ins_s);
+          else multiply_along<D>(tmem + (x & 1) * ROWS, k_tile, q, ins_s);
+          commit(s_full + 8 * (x & 1));
+        }
+        __syncwarp();
+      };
+      auto d_probabilities = [&](int x) {        // dP^T = V dO^T, over P^T
+        const int two = x & 1;
+        const u32 d = do_ring + two * TILE;
+        w.wait(dv_done + 8 * two, x >> 1 & 1);
+        fence_after();
+        if (elected() && !w.dead) {
+          if (TMEM) multiply_along_tmem<D>(tmem + two * ROWS, tmem_v, d, ins_dp);
+          else multiply_along<D>(tmem + two * ROWS, v_tile, d, ins_dp);
+          commit(dp_full + 8 * two);
+          commit(do_empty + 8 * two);
+        }
+        __syncwarp();
+      };
       w.wait(TMEM ? in_tmem : kv_full, 0);
       fence_after();
       scores(0);
       if (total > 1) scores(1);
-    }
-    // A product that writes a buffer waits for the end of the one that reads it: nothing else orders the two.  So the products
-    // of the two pairs are interleaved.
-    auto values = [&](int x) {                 // dV += P^T dO
-      const int two = x & 1;
-      const u32 d = do_ring + two * TILE;
-      w.wait(do_full + 8 * two, x >> 1 & 1);
-      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
-      w.wait(p_ready + 8 * two, x >> 1 & 1);
-      fence_after();
-      if (elected() && !w.dead) {
-        multiply_across(tmem_dv, tmem + two * ROWS, d, ins_acc, x > 0);
-        commit(dv_done + 8 * two);
-      }
-      __syncwarp();
-    };
-    auto d_probabilities = [&](int x) {        // dP^T = V dO^T, over P^T
-      const int two = x & 1;
-      const u32 d = do_ring + two * TILE;
-      w.wait(dv_done + 8 * two, x >> 1 & 1);
-      fence_after();
-      if (elected() && !w.dead) {
-        if (TMEM) multiply_along_tmem<D>(tmem + two * ROWS, tmem_v, d, ins_dp);
-        else multiply_along<D>(tmem + two * ROWS, v_tile, d, ins_dp);
-        commit(dp_full + 8 * two);
-        commit(do_empty + 8 * two);
-      }
-      __syncwarp();
-    };
-    auto keys = [&](int x) {                   // dK += dS^T Q
-      const int two = x & 1;
-      w.wait(ds_ready + 8 * two, x >> 1 & 1);
-      fence_after();
-      if (elected() && !w.dead) {
-        multiply_across(tmem_dk, tmem + two * ROWS, q_ring + x % 3 * TILE, ins_acc, x > 0);
-        commit(q_empty + 8 * (x % 3));
-        if (x + 1 == total) commit(done);
-      }
-      __syncwarp();
-    };
-    auto next_scores = [&](int x) {            // S^T of pair x + 2, over dS^T of pair x
-      if (x + 2 >= total) return;
-      w.wait(q_empty + 8 * (x % 3), x / 3 & 1);
-      fence_after();
-      scores(x + 2);
-    };
-    for (int x = 0; x < total; x += 2) {
-      const bool both = x + 1 < total;
-      values(x);
-      d_probabilities(x);
-      if (both) values(x + 1);
-      keys(x);
-      if (both) d_probabilities(x + 1);
-      next_scores(x);
-      if (both) {
-        keys(x + 1);
-        next_scores(x + 1);
+      for (int x = 0; x < total; x += 2) {
+        d_probabilities(x);
+        if (x + 1 < total) d_probabilities(x + 1);
+        if (x + 2 < total) scores(x + 2);
+        if (x + 3 < total) scores(x + 3);
       }
     }
   } else {
@@ -809,67 +806,61 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         load_tile<D>(v_ring + two * TILE, &map_v, kh, x * ROWS, b, v_full + 8 * two);
       }
     }
-  } else if (warp == MMA_WARP) {
+  } else if (warp == MMA_WARP || warp == MMA_WARP2) {
+    // (as in k_keys: one warp for the sum, the other for the products that fill the buffers)
     give_registers<LEFT>();
-    const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false), ins_acc = instruction<T>(D, true, false);
-    // keys behind the sequence's end, in its last tile
-    auto pad_from = [&](int x) { return l.m < a.k_len && (x + 1) * ROWS > l.m ? l.m - x * ROWS : ROWS; };
-    auto scores = [&](int x) {
-      const u32 k = k_ring + x % 3 * TILE;
-      w.wait(k_full + 8 * (x % 3), x / 3 & 1);
-      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
-      if (elected() && !w.dead) {
-        multiply_along_tmem<D>(tmem + (x & 1) * ROWS, tmem_q, k, ins_s);
-        commit(s_full + 8 * (x & 1));
+    if (warp == MMA_WARP) {
+      const u32 ins = instruction<T>(D, true, false);
+      for (int x = 0; x < total; ++x) {          // dQ += dS K
+        const int two = x & 1;
+        w.wait(ds_ready + 8 * two, x >> 1 & 1);
+        fence_after();
+        if (elected() && !w.dead) {
+          multiply_across(tmem_dq, tmem + two * ROWS, k_ring + x % 3 * TILE, ins, x > 0);
+          commit(k_empty + 8 * (x % 3));
+          if (x + 1 == total) commit(done);
+        }
+        __syncwarp();
       }
-      __syncwarp();
-    };
-    if (total > 0) {
+    } else if (total > 0) {
+      const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false);
+      // keys behind the sequence's end, in its last tile
+      auto pad_from = [&](int x) { return l.m < a.k_len && (x + 1) * ROWS > l.m ? l.m - x * ROWS : ROWS; };
+      auto scores = [&](int x) {                 // S = Q K^T, over dS of pair x - 2
+        const u32 k = k_ring + x % 3 * TILE;
+        w.wait(k_full + 8 * (x % 3), x / 3 & 1);
+        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
+        if (x >= 2) w.wait(k_empty + 8 * ((x - 2) % 3), (x - 2) / 3 & 1);
+        fence_after();
+        if (elected() && !w.dead) {
+          multiply_along_tmem<D>(tmem + (x & 1) * ROWS, tmem_q, k, ins_s);
+          commit(s_full + 8 * (x & 1));
+        }
+        __syncwarp();
+      };
+      auto d_probabilities = [&](int x) {        // dP = dO V^T, over S, which has been read
+        const int two = x & 1;
+        const u32 v = v_ring + two * TILE;
+        w.wait(v_full + 8 * two, x >> 1 & 1);
+        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
+        w.wait(s_read + 8 * two, x >> 1 & 1);
+        fence_after();
+        if (elected() && !w.dead) {
+          multiply_along_tmem<D>(tmem + two * ROWS, tmem_do, v, ins_dp);
+          commit(dp_full + 8 * two);
+          commit(v_empty + 8 * two);
+        }
+        __syncwarp();
+      };
       w.wait(in_tmem, 0);
       fence_after();
       scores(0);
       if (total > 1) scores(1);
-    }
-    auto d_probabilities = [&](int x) {        // dP = dO V^T, over S, which has been read
-      const int two = x & 1;
-      const u32 v = v_ring + two * TILE;
-      w.wait(v_full + 8 * two, x >> 1 & 1);
-      if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
-      w.wait(s_read + 8 * two, x >> 1 & 1);
-      fence_after();
-      if (elected() && !w.dead) {
-        multiply_along_tmem<D>(tmem + two * ROWS, tmem_do, v, ins_dp);
-        commit(dp_full + 8 * two);
-        commit(v_empty + 8 * two);
-      }
-      __syncwarp();
-    };
-    auto queries = [&](int x) {                // dQ += dS K
-      const int two = x & 1;
-      w.wait(ds_ready + 8 * two, x >> 1 & 1);
-      fence_after();
-      if (elected() && !w.dead) {
-        multiply_across(tmem_dq, tmem + two * ROWS, k_ring + x % 3 * TILE, ins_acc, x > 0);
-        commit(k_empty + 8 * (x % 3));
-        if (x + 1 == total) commit(done);
-      }
-      __syncwarp();
-    };
-    auto next_scores = [&](int x) {            // S of pair x + 2, over dS of pair x: that product has to be done
-      if (x + 2 >= total) return;
-      w.wait(k_empty + 8 * (x % 3), x / 3 & 1);
-      fence_after();
-      scores(x + 2);
-    };
-    for (int x = 0; x < total; x += 2) {
-      const bool both = x + 1 < total;
-      d_probabilities(x);
-      if (both) d_probabilities(x + 1);
-      queries(x);
-      next_scores(x);
-      if (both) {
-        queries(x + 1);
-        next_scores(x + 1);
+      for (int x = 0; x < total; x += 2) {
+        d_probabilities(x);
+        if (x + 1 < total) d_probabilities(x + 1);
+        if (x + 2 < total) scores(x + 2);
+        if (x + 3 < total) scores(x + 3);
       }
     }
   } else {
