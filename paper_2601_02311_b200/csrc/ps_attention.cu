@@ -121,11 +121,14 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   constexpr u32 TILE = PANEL * (D / 64);
   constexpr int RING = 4;
   constexpr bool TMEM = D == 64;          // Q is the left operand from tensor memory where there is room for it
-  __shared__ u64 bars[2 + 2 * RING + 8];
+  // P is handed over in parts where the product is short beside the exponentials (8192 queries, 32 heads of 64: 437 us in one part, 375
+  // in two; heads of 128: 454 and 552, since the products' warp then waits with the other tile's work behind it)
+  constexpr int PARTS = D == 64 ? 2 : 1;
+  __shared__ u64 bars[2 + 2 * RING + 10];
   __shared__ u32 tmem_at;
   const u32 tiles = tiles_begin(), ring = tiles + 2 * TILE;
   const u32 q_full = smem_address(bars), full = q_full + 16, empty = full + 8 * RING, s_full = empty + 8 * RING,
-            p_ready = s_full + 16, o_done = p_ready + 16, in_tmem = o_done + 16;
+            p_ready = s_full + 16, o_done = p_ready + 32, in_tmem = o_done + 16;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
   // the tiles with the most keys first
@@ -140,7 +143,8 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     for (int t = 0; t < 2; ++t) {
       barrier_init(q_full + 8 * t, 1);
       barrier_init(s_full + 8 * t, 1);
-      barrier_init(p_ready + 8 * t, 4);
+      barrier_init(p_ready + 16 * t, 4);
+      barrier_init(p_ready + 16 * t + 8, 4);
       barrier_init(o_done + 8 * t, 1);
       barrier_init(in_tmem + 8 * t, 4);
     }
@@ -220,13 +224,15 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           p[e / 2] = pack<T>(x.x, x.y);
         }
         tmem_store16(s_at + 16 * q, p);
+        if (q == 3 || (PARTS == 2 && q == 1)) {
+          wait_stores();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) barrier_arrive(p_ready + 16 * t + (PARTS == 2 ? 8 * (q / 2) : 0));
+        }
       }
       const float2 sums = split(add2(sum[0], sum[1]));
       total += sums.x + sums.y;
-      wait_stores();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) barrier_arrive(p_ready + 8 * t);
     }
     if (count[t]) {
       w.wait(o_done + 8 * t, (count[t] - 1) & 1);
@@ -280,11 +286,16 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       if (j + 1 < most) w.wait(full + 8 * next, (x + 1) / RING & 1);
       for (int t = 0; t < 2; ++t) {
         if (j >= count[t]) continue;
-        w.wait(p_ready + 8 * t, j & 1);
-        fence_after();
-        if (elected() && !w.dead) {
-          multiply_across(tmem + 2 * ROWS + t * D, tmem + t * ROWS, v, ins_o, j > 0);
-          commit(o_done + 8 * t);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+          w.wait(p_ready + 16 * t + 8 * part, j & 1);
+          fence_after();
+          if (elected() && !w.dead) {
+            multiply_across<ROWS / PARTS>(tmem + 2 * ROWS + t * D, tmem + t * ROWS + part * (ROWS / 2 / PARTS), v + part * (ROWS / PARTS) * 128,
+                                          ins_o, j > 0 || part > 0);
+            if (part + 1 == PARTS) commit(o_done + 8 * t);
+          }
+          __syncwarp();
         }
         __syncwarp();
         if (j + 1 < count[t]) {           // S goes over P, which that product reads: nothing but its end orders the two

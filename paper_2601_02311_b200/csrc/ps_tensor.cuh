@@ -199,11 +199,12 @@ __device__ __forceinline__ void multiply_along_tmem(u32 d, u32 a, u32 b, u32 ins
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) mma_tmem(d, a + 8 * s, y + step_along(s), ins, s > 0);
 }
-// d (+)= a b: a in tensor memory, its 128 columns of 16 bits against the rows of tile b
+// d (+)= a b: a in tensor memory, its K columns of 16 bits against K rows of tile b
+template <int K = ROWS>
 __device__ __forceinline__ void multiply_across(u32 d, u32 a, u32 b, u32 ins, bool add) {
   const u32 y = desc_across(b);
 #pragma unroll
-  for (int s = 0; s < ROWS / 16; ++s) mma_tmem(d, a + 8 * s, y + step_across(s), ins, add || s > 0);
+  for (int s = 0; s < K / 16; ++s) mma_tmem(d, a + 8 * s, y + step_across(s), ins, add || s > 0);
 }
 // the barrier is arrived at once all products that this thread has issued are done
 __device__ __forceinline__ void commit(u32 bar) {
