@@ -522,8 +522,9 @@ int ps_embed_backward(ps_ctx* ctx, const ps_embed_desc* desc, const void* d_out_
  * exp(S - lse) and dS are rounded to the operands' type before they are multiplied;
  * everything else is in 32 bits.  Results have the same bits on every run, and a
  * sequence's and a key head's do not depend on the others in the call.
- * d_lse is [batch][heads][q_len].  d_work: ps_attention_backward_bytes bytes, 256-byte
- * aligned, used like ps_embed_backward's. */
+ * d_lse is [batch][heads][q_len].  d_work: ps_attention_forward_bytes bytes (0 for most shapes:
+ * then it may be null) or ps_attention_backward_bytes, 256-byte aligned, used like
+ * ps_embed_backward's. */
 typedef struct {
   void* data;                      /* 16-byte aligned                                     */
   uint64_t batch_stride, token_stride, head_stride; /* multiples of 8, not 0 where that extent is above 1; dim is contiguous */
@@ -540,7 +541,8 @@ typedef struct {
 } ps_attention_shape;
 int ps_attention_forward(ps_ctx* ctx, const ps_attention_shape* shape, const ps_heads* q, const ps_heads* k,
                          const ps_heads* v, const ps_heads* out, float* d_lse, const int32_t* d_q_lens,
-                         const int32_t* d_k_lens);
+                         const int32_t* d_k_lens, void* d_work, uint64_t work_bytes);
+uint64_t ps_attention_forward_bytes(const ps_attention_shape* shape);
 uint64_t ps_attention_backward_bytes(const ps_attention_shape* shape);
 int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps_heads* q, const ps_heads* k,
                           const ps_heads* v, const ps_heads* out, const float* d_lse, const ps_heads* d_out,

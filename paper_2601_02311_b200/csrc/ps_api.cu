@@ -734,7 +734,7 @@ static int take_heads(const ps_heads* h, u32 batch, u32 len, u32 heads, ps_heads
 
 int ps_attention_forward(ps_ctx* ctx, const ps_attention_shape* shape, const ps_heads* q, const ps_heads* k,
                          const ps_heads* v, const ps_heads* out, float* d_lse, const int32_t* d_q_lens,
-                         const int32_t* d_k_lens) {
+                         const int32_t* d_k_lens, void* d_work, uint64_t work_bytes) {
   if (!ctx || !shape) return PS_E_NULLPTR;
   AttentionArgs a;
   int rc = attention_args(*shape, a);
@@ -746,14 +746,22 @@ int ps_attention_forward(ps_ctx* ctx, const ps_attention_shape* shape, const ps_
       (rc = take_heads(out, s.batch, s.q_len, s.heads, a.out)) != PS_OK)
     return rc;
   if (s.batch == 0 || s.q_len == 0) return PS_OK;
-  if (!d_lse) return PS_E_NULLPTR;
-  if (!aligned(d_lse, 4) || !aligned(d_q_lens, 4) || !aligned(d_k_lens, 4)) return PS_E_ALIGN;
+  const u64 need = attention_forward_bytes(a);
+  if (!d_lse || (need && !d_work)) return PS_E_NULLPTR;
+  if (!aligned(d_lse, 4) || !aligned(d_q_lens, 4) || !aligned(d_k_lens, 4) || !aligned(d_work, 256)) return PS_E_ALIGN;
+  if (work_bytes < need) return PS_E_RANGE;
   if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return PS_E_CUDA;
   a.lse = d_lse; a.q_lens = d_q_lens; a.k_lens = d_k_lens; a.status = ctx->h->status;
+  a.work = d_work;
   CUDA_OK(launch_attention_forward(s.dtype, a, ctx->sm_count, ctx->stream));
   return PS_OK;
+}
+
+uint64_t ps_attention_forward_bytes(const ps_attention_shape* shape) {
+  AttentionArgs a;
+  return shape && attention_args(*shape, a) == PS_OK ? attention_forward_bytes(a) : 0;
 }
 
 uint64_t ps_attention_backward_bytes(const ps_attention_shape* shape) {

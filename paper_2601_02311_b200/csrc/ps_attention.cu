@@ -45,6 +45,9 @@ struct Args {
   float *lse2, *delta;
   u32* norms;
   int padded;
+  // few queries before many keys, or the other way: the long side is cut into chunks, a block each, whose results in 32 bits are
+  // joined by another kernel
+  float *parts, *part_lse;
   volatile u32* status;
 };
 struct Lengths {
@@ -61,6 +64,16 @@ __device__ __forceinline__ int end_of(const Args& a, Lengths l, int i) {
 __device__ __forceinline__ int key_tiles(const Args& a, Lengths l, int i) {
   return i >= l.n ? 0 : (end_of(a, l, min(i + ROWS, l.n) - 1) + ROWS - 1) / ROWS;
 }
+
+// the first tile of queries that sees keys from j on
+__device__ __forceinline__ int first_query_tile(const Args& a, Lengths l, int j) { return a.causal ? max(0, j - l.m + l.n) / ROWS : 0; }
+
+// A block of few rows would walk a long axis alone: at up to FEW rows of one side and more than two chunks of the other, blocks take
+// a chunk of CHUNK tiles each.  The rule looks at the two lengths alone, so that a sequence's bits do not depend on how many
+// others there are.
+constexpr int FEW = 2 * ROWS, CHUNK = 16;
+__host__ __device__ constexpr bool chunked(int rows, int along) { return rows <= FEW && along > 2 * CHUNK * ROWS; }
+__host__ __device__ constexpr int chunks_of(int along) { return (along + CHUNK * ROWS - 1) / (CHUNK * ROWS); }
 
 // 32 columns of a row of results, times `by`, to memory; columns behind dim are not there
 template <class T>
@@ -97,6 +110,22 @@ __device__ __forceinline__ void store_row(T* row, u32 from, bool any, bool there
   }
 }
 
+// the same in 32 bits, all D columns
+template <int D>
+__device__ __forceinline__ void store_part(float* row, u32 from, bool there, float by) {
+#pragma unroll
+  for (int c = 0; c < D; c += 32) {
+    u32 v[32];
+    tmem_load32(v, from + c);
+    wait_loads();
+    if (there)
+#pragma unroll
+      for (int e = 0; e < 32; e += 4)
+        *reinterpret_cast<float4*>(row + c + e) = make_float4(__uint_as_float(v[e]) * by, __uint_as_float(v[e + 1]) * by,
+                                                              __uint_as_float(v[e + 2]) * by, __uint_as_float(v[e + 3]) * by);
+  }
+}
+
 // the smallest address in the block's shared memory that a tile may have
 __device__ __forceinline__ u32 tiles_begin() {
   extern __shared__ unsigned char shared[];
@@ -114,7 +143,7 @@ __device__ __forceinline__ void linger(bool dead) {
 // tensor memory), their row maximum, P = 2^(c S - c maximum) written over S in 16 bits, O += P V.  O is rescaled only when a
 // row's maximum has grown by more than a factor of 2^8: until then P is larger than 1 by up to that, which the 32-bit
 // sums and the types' exponents hold, and lse comes from the same maximum.
-template <class T, int D>
+template <class T, int D, bool CHUNKED>
 __global__ void __launch_bounds__(THREADS, 1)
 k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
           const __grid_constant__ CUtensorMap map_v, const Args a) {
@@ -136,7 +165,9 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   const int q0 = (a.causal ? n_tiles - 1 - at : at) * 2 * ROWS, b = blockIdx.x % per / a.heads, h = blockIdx.x % a.heads;
   const int kh = h / (a.heads / a.kv_heads);
   const Lengths l = lengths_of(a, b);
-  const int count[2] = {key_tiles(a, l, q0), key_tiles(a, l, q0 + ROWS)}, most = max(count[0], count[1]);
+  const int skip = CHUNKED ? blockIdx.y * CHUNK : 0, key0 = skip * ROWS;        // tiles of keys before this block's, and its first key
+  const auto tiles_of = [&](int i) { return CHUNKED ? max(0, min(key_tiles(a, l, i) - skip, CHUNK)) : key_tiles(a, l, i); };
+  const int count[2] = {tiles_of(q0), tiles_of(q0 + ROWS)}, most = max(count[0], count[1]);
 
   if (warp == MMA_WARP) tmem_alloc(smem_address(&tmem_at), 512);
   if (threadIdx.x == 0) {
@@ -162,10 +193,10 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
 
   if (warp < COPY_WARP) {
     take_registers<TAKEN>();
-    const int t = warp / 4, row = threadIdx.x % ROWS, i = q0 + t * ROWS + row, end = end_of(a, l, i);
+    const int t = warp / 4, row = threadIdx.x % ROWS, i = q0 + t * ROWS + row, end = end_of(a, l, i) - key0;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, s_at = tmem + lanes + t * ROWS, o_at = tmem + lanes + 2 * ROWS + t * D;
     // the first tile of keys of which some query of this tile does not see all
-    const int masked = (q0 + (t + 1) * ROWS > l.n ? 0 : end_of(a, l, q0 + t * ROWS)) / ROWS;
+    const int masked = q0 + (t + 1) * ROWS > l.n ? 0 : (end_of(a, l, q0 + t * ROWS) - key0) / ROWS;
     const float slack = 8.f / a.c;
     float most_s = MINUS_INF, total = 0.f;
     if (TMEM && count[t]) {
@@ -238,11 +269,17 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       w.wait(o_done + 8 * t, (count[t] - 1) & 1);
       fence_after();
     }
-    const bool there = i < a.q_len;
+    const bool there = i < a.q_len, none = most_s == MINUS_INF && total == 0.f;
     const int safe = min(i, a.q_len - 1);
-    store_row<T, D>(row_of<T>(a.out, b, safe, h), o_at, count[t] > 0, there, a.dim, most_s == MINUS_INF && total == 0.f ? 0.f : 1.f / total);
-    if (there)
-      a.lse[((u64)b * a.heads + h) * a.q_len + i] = most_s == MINUS_INF && total == 0.f ? MINUS_INF : (most_s * a.c + log2f(total)) * LN2;
+    const float lse = none ? MINUS_INF : (most_s * a.c + log2f(total)) * LN2, by = none ? 0.f : 1.f / total;
+    if constexpr (CHUNKED) {
+      const u64 at = (((u64)blockIdx.y * a.batch + b) * a.heads + h) * a.q_len + safe;
+      if (count[t]) store_part<D>(a.parts + at * D, o_at, there, by);
+      if (there) a.part_lse[at] = lse;
+    } else {
+      store_row<T, D>(row_of<T>(a.out, b, safe, h), o_at, count[t] > 0, there, a.dim, by);
+      if (there) a.lse[((u64)b * a.heads + h) * a.q_len + i] = lse;
+    }
   } else if (warp == COPY_WARP) {
     give_registers<LEFT>();
     if (lane == 0) {
@@ -256,7 +293,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         w.wait(empty + 8 * slot, (x / RING & 1) ^ 1);
         if (w.dead) break;
         barrier_expect(full + 8 * slot, TILE);
-        load_tile<D>(ring + slot * TILE, x & 1 ? &map_v : &map_k, kh, x / 2 * ROWS, b, full + 8 * slot);
+        load_tile<D>(ring + slot * TILE, x & 1 ? &map_v : &map_k, kh, key0 + x / 2 * ROWS, b, full + 8 * slot);
       }
     }
   } else if (warp == MMA_WARP) {
@@ -282,7 +319,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       const int x = 2 * j + 1, slot = x % RING, next = (x + 1) % RING;
       const u32 v = ring + slot * TILE;
       w.wait(full + 8 * slot, x / RING & 1);
-      if (l.m < a.k_len && (j + 1) * ROWS > l.m && !w.dead) clear_rows<D>(v, l.m - j * ROWS);
+      if (l.m < a.k_len && key0 + (j + 1) * ROWS > l.m && !w.dead) clear_rows<D>(v, l.m - key0 - j * ROWS);
       if (j + 1 < most) w.wait(full + 8 * next, (x + 1) / RING & 1);
       for (int t = 0; t < 2; ++t) {
         if (j >= count[t]) continue;
@@ -321,6 +358,31 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     fence_after();
     tmem_free(tmem, 512);
   }
+}
+
+// The chunks' outputs, each normalised by itself, weighted by exp(their lse - the row's): a warp a query.
+template <class T, int D>
+__global__ void __launch_bounds__(256) k_join_outputs(const Args a, int chunks) {
+  wait_for_earlier();
+  const int lane = threadIdx.x % 32, i = blockIdx.x * 8 + threadIdx.x / 32, h = blockIdx.y, b = blockIdx.z;
+  if (i >= a.q_len) return;
+  const u64 row = ((u64)b * a.heads + h) * a.q_len + i, stride = (u64)a.batch * a.heads * a.q_len;
+  float most = MINUS_INF, total = 0.f, sum[D / 32] = {};
+  for (int s = 0; s < chunks; ++s) most = fmaxf(most, a.part_lse[s * stride + row]);
+  for (int s = 0; s < chunks; ++s) {
+    const float lse = a.part_lse[s * stride + row];
+    if (lse == MINUS_INF) continue;                  // (its output was not written)
+    const float weight = exp2_fast((lse - most) * LOG2E);
+    total += weight;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) sum[e] = fmaf(weight, a.parts[(s * stride + row) * D + lane + 32 * e], sum[e]);
+  }
+  const float by = total > 0.f || total != total ? 1.f / total : 0.f;
+  T* const to = row_of<T>(a.out, b, i, h);
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+    if (lane + 32 * e < a.dim) to[lane + 32 * e] = narrow<T>(sum[e] * by);
+  if (lane == 0) a.lse[row] = by == 0.f ? MINUS_INF : most + log2f(total) * LN2;
 }
 
 // ------------------------------------------------------------------ backward
@@ -413,7 +475,7 @@ struct Shared {
 // operands of both kinds from one copy.  Tensor memory (D = 128): the two buffers, dV and dK, 128 columns each.
 // Products: S S | dV dP, dV dP | dK S, dK S | ..., so that a buffer's P is used up before dP is written over it.
 // Q has three slots, since S of pair x + 2 follows on dK of pair x; dO, with two, is free after dP.
-template <class T, int D>
+template <class T, int D, bool CHUNKED>
 __global__ void __launch_bounds__(THREADS, 1)
 k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
@@ -432,8 +494,8 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   const int per = a.kv_heads * a.batch, j0 = blockIdx.x / per * ROWS, b = blockIdx.x % per / a.kv_heads, kh = blockIdx.x % a.kv_heads;
   const int group = a.heads / a.kv_heads;
   const Lengths l = lengths_of(a, b);
-  const int first = a.causal ? max(0, j0 - l.m + l.n) / ROWS : 0, last = (l.n + ROWS - 1) / ROWS;     // tiles of queries
-  const int walk = j0 < l.m ? max(0, last - first) : 0, total = walk * group;
+  const int first = first_query_tile(a, l, j0) + (CHUNKED ? blockIdx.y * CHUNK : 0), rest = (l.n + ROWS - 1) / ROWS - first;
+  const int walk = j0 < l.m ? max(0, CHUNKED ? min(rest, CHUNK) : rest) : 0, total = walk * group;     // tiles of queries
 
   if (warp == MMA_WARP) tmem_alloc(smem_address(&sh.tmem_at), 512);
   if (threadIdx.x == 0) {
@@ -558,8 +620,13 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
     const bool there = j < a.k_len, used = total > 0 && j < l.m;
     const int safe = min(j, a.k_len - 1);
     const float undo = Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f;
-    if (mine == 0) store_row<T, D>(row_of<T>(a.d_v, b, safe, kh), tmem_dv + lanes, total > 0, there, a.dim, used ? undo : 0.f);
-    else store_row<T, D>(row_of<T>(a.d_k, b, safe, kh), tmem_dk + lanes, total > 0, there, a.dim, used ? a.scale / factor * undo : 0.f);
+    const float by = mine ? a.scale / factor * undo : undo;
+    const u32 from = (mine ? tmem_dk : tmem_dv) + lanes;
+    if constexpr (CHUNKED) {
+      if (total > 0) store_part<D>(a.parts + ((((u64)(2 * blockIdx.y + mine) * a.batch + b) * a.kv_heads + kh) * a.k_len + safe) * D, from, there, by);
+    } else {
+      store_row<T, D>(row_of<T>(mine ? a.d_k : a.d_v, b, safe, kh), from, total > 0, there, a.dim, used ? by : 0.f);
+    }
   } else if (warp == COPY_WARP) {
     give_registers<LEFT>();
     if (lane == 0 && total > 0) {
@@ -680,7 +747,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
 // A block owns 128 queries of a head and walks the keys they see.  Tensor memory (D = 128): the two buffers and dQ, 128 columns
 // each.  P stays in registers, so dP may be written over S as soon as S has been read.
 // Products: S S | dP dP | dQ S, dQ S | dP dP | ...  K has three slots, V two, as Q and dO above.
-template <class T, int D>
+template <class T, int D, bool CHUNKED>
 __global__ void __launch_bounds__(THREADS, 1)
 k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
@@ -697,7 +764,8 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   const int q0 = (a.causal ? n_tiles - 1 - order : order) * ROWS, b = blockIdx.x % per / a.heads, h = blockIdx.x % a.heads;
   const int kh = h / (a.heads / a.kv_heads);
   const Lengths l = lengths_of(a, b);
-  const int total = key_tiles(a, l, q0);
+  const int skip = CHUNKED ? blockIdx.y * CHUNK : 0, key0 = skip * ROWS;        // tiles of keys before this block's, and its first key
+  const int total = CHUNKED ? max(0, min(key_tiles(a, l, q0) - skip, CHUNK)) : key_tiles(a, l, q0);
 
   if (warp == MMA_WARP) tmem_alloc(smem_address(&sh.tmem_at), 512);
   if (threadIdx.x == 0) {
@@ -726,9 +794,9 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
 
   if (warp < COPY_WARP) {
     take_registers<TAKEN>();
-    const int mine = warp / 4, i = q0 + threadIdx.x % ROWS, end = end_of(a, l, i);
+    const int mine = warp / 4, i = q0 + threadIdx.x % ROWS, end = end_of(a, l, i) - key0;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
-    const int masked = (q0 + ROWS > l.n ? 0 : end_of(a, l, q0)) / ROWS;
+    const int masked = q0 + ROWS > l.n ? 0 : (end_of(a, l, q0) - key0) / ROWS;
     const u64 row = ((u64)b * a.heads + h) * a.padded + i;
     const float off = a.lse2[row], delta = a.delta[row], factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
     const u64 cs = pair(a.c, a.c), offs = pair(off, off), deltas = pair(delta, delta), factors = pair(factor, factor);
@@ -797,8 +865,12 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const bool there = i < a.q_len;
     const int safe = min(i, a.q_len - 1);
     const float by = off == MINUS_INF ? 0.f : a.scale / factor * (Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f);
-    store_row<T, D / 2>(row_of<T>(a.d_q, b, safe, h) + mine * (D / 2), tmem_dq + lanes + mine * (D / 2), total > 0, there,
-                        a.dim - mine * (D / 2), by);
+    const u32 from = tmem_dq + lanes + mine * (D / 2);
+    if constexpr (CHUNKED) {
+      if (total > 0) store_part<D / 2>(a.parts + ((((u64)blockIdx.y * a.batch + b) * a.heads + h) * a.q_len + safe) * D + mine * (D / 2), from, there, by);
+    } else {
+      store_row<T, D / 2>(row_of<T>(a.d_q, b, safe, h) + mine * (D / 2), from, total > 0, there, a.dim - mine * (D / 2), by);
+    }
   } else if (warp == COPY_WARP) {
     give_registers<LEFT>();
     if (lane == 0 && total > 0) {
@@ -810,11 +882,11 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         w.wait(k_empty + 8 * slot, (x / 3 & 1) ^ 1);
         if (w.dead) break;
         barrier_expect(k_full + 8 * slot, TILE);
-        load_tile<D>(k_ring + slot * TILE, &map_k, kh, x * ROWS, b, k_full + 8 * slot);
+        load_tile<D>(k_ring + slot * TILE, &map_k, kh, key0 + x * ROWS, b, k_full + 8 * slot);
         w.wait(v_empty + 8 * two, (x >> 1 & 1) ^ 1);
         if (w.dead) break;
         barrier_expect(v_full + 8 * two, TILE);
-        load_tile<D>(v_ring + two * TILE, &map_v, kh, x * ROWS, b, v_full + 8 * two);
+        load_tile<D>(v_ring + two * TILE, &map_v, kh, key0 + x * ROWS, b, v_full + 8 * two);
       }
     }
   } else if (warp == MMA_WARP || warp == MMA_WARP2) {
@@ -836,7 +908,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     } else if (total > 0) {
       const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false);
       // keys behind the sequence's end, in its last tile
-      auto pad_from = [&](int x) { return l.m < a.k_len && (x + 1) * ROWS > l.m ? l.m - x * ROWS : ROWS; };
+      auto pad_from = [&](int x) { return l.m < a.k_len && key0 + (x + 1) * ROWS > l.m ? l.m - key0 - x * ROWS : ROWS; };
       auto scores = [&](int x) {                 // S = Q K^T, over dS of pair x - 2
         const u32 k = k_ring + x % 3 * TILE;
         w.wait(k_full + 8 * (x % 3), x / 3 & 1);
@@ -887,6 +959,31 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   }
 }
 
+// The chunks' shares of dQ, or of dV and dK, added in their order: a warp a row.
+template <class T, int D, bool KEYS>
+__global__ void __launch_bounds__(256) k_join_gradients(const Args a) {
+  wait_for_earlier();
+  const int lane = threadIdx.x % 32, r = blockIdx.x * 8 + threadIdx.x / 32, b = blockIdx.z;
+  const int len = KEYS ? a.k_len : a.q_len, h = KEYS ? blockIdx.y / 2 : blockIdx.y, which = KEYS ? blockIdx.y % 2 : 0;
+  if (r >= len) return;
+  const Lengths l = lengths_of(a, b);
+  const int tile = r / ROWS * ROWS;
+  int chunks;
+  if (KEYS) chunks = r < l.m ? chunks_of(max(0, (l.n + ROWS - 1) / ROWS - first_query_tile(a, l, tile)) * ROWS) : 0;
+  else chunks = end_of(a, l, r) > 0 ? chunks_of(key_tiles(a, l, tile) * ROWS) : 0;
+  float sum[D / 32] = {};
+  for (int s = 0; s < chunks; ++s) {
+    const u64 slice = KEYS ? (u64)(2 * s + which) * a.batch + b : (u64)s * a.batch + b;
+    const float* const from = a.parts + ((slice * (KEYS ? a.kv_heads : a.heads) + h) * len + r) * D;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) sum[e] += from[lane + 32 * e];
+  }
+  T* const to = row_of<T>(KEYS ? (which ? a.d_k : a.d_v) : a.d_q, b, r, h);
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+    if (lane + 32 * e < a.dim) to[lane + 32 * e] = narrow<T>(sum[e]);
+}
+
 // ------------------------------------------------------------------ host
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -926,6 +1023,7 @@ Args args_of(const AttentionArgs& a) {
   r.lse2 = (float*)a.work;
   r.delta = r.lse2 + rows;
   r.norms = (u32*)(r.delta + rows);
+  r.parts = r.part_lse = nullptr;
   r.status = a.status;
   return r;
 }
@@ -956,16 +1054,34 @@ cudaError_t forward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
     return cudaErrorInvalidValue;
   }
   const u32 smem = smem_for(6, D, 1024), grid = (u32)((a.q_len + 2 * ROWS - 1) / (2 * ROWS)) * a.heads * a.batch;
+  Args r = args_of(a);
+  cudaError_t e;
+  if (chunked(a.q_len, a.k_len)) {
+    const int chunks = chunks_of(a.k_len);
+    r.parts = (float*)a.work;
+    r.part_lse = r.parts + (u64)chunks * a.batch * a.heads * a.q_len * D;
+    static std::atomic<u64> allowed{0};
+    if ((e = allow(k_forward<T, D, true>, smem, allowed)) != cudaSuccess) return e;
+    k_forward<T, D, true><<<dim3(grid, chunks), THREADS, smem, stream>>>(q, k, v, r);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    return launch_next(k_join_outputs<T, D>, dim3((a.q_len + 7) / 8, a.heads, a.batch), 256, 0, stream, r, chunks);
+  }
   static std::atomic<u64> allowed{0};
-  cudaError_t e = allow(k_forward<T, D>, smem, allowed);
-  if (e != cudaSuccess) return e;
-  k_forward<T, D><<<grid, THREADS, smem, stream>>>(q, k, v, args_of(a));
+  if ((e = allow(k_forward<T, D, false>, smem, allowed)) != cudaSuccess) return e;
+  k_forward<T, D, false><<<grid, THREADS, smem, stream>>>(q, k, v, r);
   return cudaGetLastError();
+}
+
+// the backward pass's work buffer: both vectors of the padded rows and the norms, then the chunks' shares
+size_t rows_bytes(const AttentionArgs& a) {
+  const size_t padded = ((size_t)a.q_len + ROWS - 1) / ROWS * ROWS;
+  return (sizeof(float) * 2 * a.batch * a.heads * padded + sizeof(u32) * 2 * a.batch * a.kv_heads + 255) / 256 * 256;
 }
 
 template <class T, int D>
 cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
-  const Args r = args_of(a);
+  Args r = args_of(a);
+  r.parts = (float*)((char*)a.work + rows_bytes(a));
   CUtensorMap q, k, v, d;
   if (a.q_len && (!encode(q, dtype, a.q, a.batch, a.q_len, a.heads, a.dim) || !encode(d, dtype, a.d_out, a.batch, a.q_len, a.heads, a.dim)))
     return cudaErrorInvalidValue;
@@ -986,22 +1102,33 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
     k_rows<T, true><<<dim3(r.padded / ROWS_A_BLOCK, a.heads, a.batch), 256, 0, stream>>>(a.d_out, a.out, r);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
+  // (one side at most is cut: few rows of it and many of the other)
+  const bool cut_queries = chunked(a.k_len, a.q_len), cut_keys = chunked(a.q_len, a.k_len);
   if (a.k_len) {
-    const u32 smem = smem_for(7, D, 5 * ROWS * 4 + sizeof(Shared));
-    static std::atomic<u64> allowed{0};
-    if ((e = allow(k_keys<T, D>, smem, allowed)) != cudaSuccess) return e;
-    const u32 grid = (u32)((a.k_len + ROWS - 1) / ROWS) * a.kv_heads * a.batch;
-    if ((e = launch_next(k_keys<T, D>, grid, THREADS, smem, stream, q, k, v, d, r)) != cudaSuccess) return e;
+    const u32 smem = smem_for(7, D, 5 * ROWS * 4 + sizeof(Shared)), grid = (u32)((a.k_len + ROWS - 1) / ROWS) * a.kv_heads * a.batch;
+    static std::atomic<u64> allowed{0}, allowed_cut{0};
+    if ((e = cut_queries ? allow(k_keys<T, D, true>, smem, allowed_cut) : allow(k_keys<T, D, false>, smem, allowed)) != cudaSuccess) return e;
+    e = cut_queries ? launch_next(k_keys<T, D, true>, dim3(grid, chunks_of(a.q_len)), THREADS, smem, stream, q, k, v, d, r)
+                    : launch_next(k_keys<T, D, false>, grid, THREADS, smem, stream, q, k, v, d, r);
+    if (e != cudaSuccess) return e;
   }
   if (a.q_len) {
-    const u32 smem = smem_for(7, D, sizeof(Shared));
-    static std::atomic<u64> allowed{0};
-    if ((e = allow(k_queries<T, D>, smem, allowed)) != cudaSuccess) return e;
-    const u32 grid = (u32)(r.padded / ROWS) * a.heads * a.batch;
-    if (a.k_len) return launch_next(k_queries<T, D>, grid, THREADS, smem, stream, q, k, v, d, r);
-    k_queries<T, D><<<grid, THREADS, smem, stream>>>(q, k, v, d, r);      // (no kernel is between it and the rows)
+    const u32 smem = smem_for(7, D, sizeof(Shared)), grid = (u32)(r.padded / ROWS) * a.heads * a.batch;
+    static std::atomic<u64> allowed{0}, allowed_cut{0};
+    if ((e = cut_keys ? allow(k_queries<T, D, true>, smem, allowed_cut) : allow(k_queries<T, D, false>, smem, allowed)) != cudaSuccess) return e;
+    if (cut_keys) {
+      e = launch_next(k_queries<T, D, true>, dim3(grid, chunks_of(a.k_len)), THREADS, smem, stream, q, k, v, d, r);
+    } else if (a.k_len) {
+      e = launch_next(k_queries<T, D, false>, grid, THREADS, smem, stream, q, k, v, d, r);
+    } else {
+      k_queries<T, D, false><<<grid, THREADS, smem, stream>>>(q, k, v, d, r);      // (no kernel is between it and the rows)
+      e = cudaGetLastError();
+    }
+    if (e != cudaSuccess) return e;
   }
-  return cudaGetLastError();
+  if (cut_keys) return launch_next(k_join_gradients<T, D, false>, dim3((a.q_len + 7) / 8, a.heads, a.batch), 256, 0, stream, r);
+  if (cut_queries) return launch_next(k_join_gradients<T, D, true>, dim3((a.k_len + 7) / 8, 2 * a.kv_heads, a.batch), 256, 0, stream, r);
+  return cudaSuccess;
 }
 
 }  // namespace
@@ -1012,9 +1139,16 @@ cudaError_t launch_attention_forward(u32 dtype, const AttentionArgs& a, int, cud
   return a.dim <= 64 ? forward<__half, 64>(dtype, a, stream) : forward<__half, 128>(dtype, a, stream);
 }
 
+size_t attention_forward_bytes(const AttentionArgs& a) {
+  if (!chunked(a.q_len, a.k_len)) return 0;
+  return sizeof(float) * chunks_of(a.k_len) * a.batch * a.heads * a.q_len * ((a.dim <= 64 ? 64 : 128) + 1);
+}
+
 size_t attention_backward_bytes(const AttentionArgs& a) {
-  const size_t padded = ((size_t)a.q_len + ROWS - 1) / ROWS * ROWS;
-  return sizeof(float) * 2 * a.batch * a.heads * padded + sizeof(u32) * 2 * a.batch * a.kv_heads;
+  size_t parts = 0;
+  if (chunked(a.q_len, a.k_len)) parts = (size_t)chunks_of(a.k_len) * a.batch * a.heads * a.q_len;
+  if (chunked(a.k_len, a.q_len)) parts = (size_t)chunks_of(a.q_len) * 2 * a.batch * a.kv_heads * a.k_len;
+  return rows_bytes(a) + sizeof(float) * parts * (a.dim <= 64 ? 64 : 128);
 }
 
 cudaError_t launch_attention_backward(u32 dtype, const AttentionArgs& a, int, cudaStream_t stream) {

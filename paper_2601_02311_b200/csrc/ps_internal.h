@@ -155,9 +155,10 @@ struct AttentionArgs {
   const int *q_lens, *k_lens; // per sequence, or null
   int batch, q_len, k_len, heads, kv_heads, dim, causal;
   float scale;
-  void* work;                 // backward: attention_backward_bytes
+  void* work;                 // attention_forward_bytes, attention_backward_bytes
   volatile u32* status;
 };
 cudaError_t launch_attention_forward(u32 dtype, const AttentionArgs& a, int sm_count, cudaStream_t stream);
+size_t attention_forward_bytes(const AttentionArgs& a);
 size_t attention_backward_bytes(const AttentionArgs& a);
 cudaError_t launch_attention_backward(u32 dtype, const AttentionArgs& a, int sm_count, cudaStream_t stream);

@@ -53,7 +53,7 @@ EXPORTS = ("ps_create", "ps_destroy", "ps_status", "ps_strerror", "ps_space_crea
            "ps_space_points_per_model", "ps_space_decode", "ps_eval_batch", "ps_sweep_pareto",
            "ps_check_composition", "ps_int_peak", "ps_eval_compact_noalloc", "ps_select",
            "ps_verify_batch", "ps_select_compare", "ps_dropout", "ps_embed_forward", "ps_embed_backward_bytes",
-           "ps_embed_backward", "ps_attention_forward", "ps_attention_backward_bytes", "ps_attention_backward")
+           "ps_embed_backward", "ps_attention_forward", "ps_attention_forward_bytes", "ps_attention_backward_bytes", "ps_attention_backward")
 
 
 class _SpaceDesc(C.Structure):
@@ -147,7 +147,9 @@ _lib.ps_embed_forward.argtypes = [C.c_void_p] * 5
 _lib.ps_embed_backward_bytes.argtypes = [C.c_void_p]
 _lib.ps_embed_backward_bytes.restype = C.c_uint64
 _lib.ps_embed_backward.argtypes = [C.c_void_p] * 6 + [C.c_uint64]
-_lib.ps_attention_forward.argtypes = [C.c_void_p] * 9
+_lib.ps_attention_forward.argtypes = [C.c_void_p] * 10 + [C.c_uint64]
+_lib.ps_attention_forward_bytes.argtypes = [C.c_void_p]
+_lib.ps_attention_forward_bytes.restype = C.c_uint64
 _lib.ps_attention_backward_bytes.argtypes = [C.c_void_p]
 _lib.ps_attention_backward_bytes.restype = C.c_uint64
 _lib.ps_attention_backward.argtypes = [C.c_void_p] * 14 + [C.c_uint64]
@@ -458,13 +460,20 @@ class Context:
 
     def attention_forward_into(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
                                scale: float | None = None, causal: bool = True, q_lens: torch.Tensor | None = None,
-                               k_lens: torch.Tensor | None = None):
-        """ps_attention_forward on [batch, len, heads, dim] of any strides; scale defaults to dim ** -0.5."""
+                               k_lens: torch.Tensor | None = None, work: torch.Tensor | None = None):
+        """ps_attention_forward on [batch, len, heads, dim] of any strides; scale defaults to dim ** -0.5.
+        `work`: a uint8 buffer of attention_forward_bytes; without it one is allocated for a call that needs it."""
         where, dtype = "ps_attention_forward", q.dtype
         shape, qs, ks, ql, kl = self._attention(q, k, where, scale, causal, q_lens, k_lens, lse)
+        at, size = None, 0
+        need = _lib.ps_attention_forward_bytes(shape)
+        if need or work is not None:
+            work = self._work(work, need, where)
+            at, size = work.data_ptr(), work.numel()
         _check(_lib.ps_attention_forward(
             self._h, shape, self._heads(q, where, "q", qs, dtype), self._heads(k, where, "k", ks, dtype),
-            self._heads(v, where, "v", ks, dtype), self._heads(out, where, "out", qs, dtype), lse.data_ptr(), ql, kl), where)
+            self._heads(v, where, "v", ks, dtype), self._heads(out, where, "out", qs, dtype), lse.data_ptr(), ql, kl, at, size),
+            where)
 
     @_on_own_stream
     def attention_forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float | None = None,
@@ -502,6 +511,11 @@ class Context:
         d_q, d_k, d_v = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
         self.attention_backward_into(q, k, v, out, lse, d_out, d_q, d_k, d_v, scale, causal, q_lens, k_lens)
         return d_q, d_k, d_v
+
+    @staticmethod
+    def attention_forward_bytes(batch: int, q_len: int, k_len: int, heads: int, kv_heads: int, dim: int) -> int:
+        """Bytes of the work buffer that attention_forward_into takes: 0 unless few queries go over many keys."""
+        return _lib.ps_attention_forward_bytes(_ATTENTION_SHAPE(batch, q_len, k_len, heads, kv_heads, dim, 1, 0, 1.0, 0))
 
     @staticmethod
     def attention_backward_bytes(batch: int, q_len: int, k_len: int, heads: int, kv_heads: int, dim: int) -> int:

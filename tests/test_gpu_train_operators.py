@@ -409,6 +409,24 @@ def test_attention_of_padded_sequences(ctx, dtype, causal, q_lens, k_lens):
     check_backward(ctx, q, k, v, d_out, None, causal, *lens)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(1, 1, 4097, 2, 1, 128), (2, 250, 6000, 4, 2, 64), (1, 256, 4300, 3, 3, 96), (3, 5, 9000, 2, 2, 40),
+                                   (1, 4500, 256, 2, 1, 128), (2, 6001, 3, 4, 2, 64)])
+def test_attention_of_few_rows_and_a_long_axis(ctx, dtype, causal, shape):
+    """Chunks of the long axis, joined: with lengths that leave chunks, and whole sequences, without keys or queries."""
+    q, k, v, d_out = tensors(16, *shape, dtype)
+    check_forward(ctx, q, k, v, None, causal)
+    check_backward(ctx, q, k, v, d_out, None, causal)
+    batch, q_len, k_len = shape[:3]
+    lens = [torch.tensor([n, n // 3, 0][:batch], device="cuda", dtype=torch.int32) for n in (q_len, k_len)]
+    for x, n, length in ((q, lens[0], q_len), (d_out, lens[0], q_len), (k, lens[1], k_len), (v, lens[1], k_len)):
+        for b in range(batch):
+            x[b, int(n[b]):] = math.nan
+    check_forward(ctx, q, k, v, None, causal, *lens)
+    check_backward(ctx, q, k, v, d_out, None, causal, *lens)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 4.0])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_attention_scales(ctx, dtype, scale):

@@ -116,7 +116,8 @@ def attention(backward=False, **kw):
     h = {n: None if v is None else C.byref(Heads(*[x or None if i == 0 else x for i, x in enumerate(v)])) for n, v in heads.items()}
     shape = C.byref(AttentionShape(**args))
     if not backward:
-        return ps._lib.ps_attention_forward(ptr["ctx"], shape, h["q"], h["k"], h["v"], h["out"], ptr["lse"], ptr["q_lens"], ptr["k_lens"])
+        return ps._lib.ps_attention_forward(ptr["ctx"], shape, h["q"], h["k"], h["v"], h["out"], ptr["lse"], ptr["q_lens"], ptr["k_lens"],
+                                            ptr["work"], ptr["work_bytes"])
     return ps._lib.ps_attention_backward(ptr["ctx"], shape, h["q"], h["k"], h["v"], h["out"], ptr["lse"], h["d_out"], h["d_q"],
                                          h["d_k"], h["d_v"], ptr["q_lens"], ptr["k_lens"], ptr["work"], ptr["work_bytes"])
 
@@ -145,6 +146,15 @@ def test_attention_refuses(backward, change, code):
     (dict(work_bytes=8), ps.E_RANGE)])
 def test_attention_backward_refuses(change, code):
     assert attention(True, **change) == code
+
+
+def test_attention_forward_refuses_a_short_work_buffer():
+    """Few queries over many keys are cut into chunks, whose results need room; other shapes need none."""
+    need = ps.Context.attention_forward_bytes(2, 4, 5000, 4, 2, 8)
+    assert need > 0 and ps.Context.attention_forward_bytes(2, 4, 4, 4, 2, 8) == 0
+    assert attention(k_len=5000, work=None) == ps.E_NULLPTR
+    assert attention(k_len=5000, work_bytes=need - 1) == ps.E_RANGE
+    assert attention(k_len=5000, work=AT + 16384 + 64, work_bytes=need) == ps.E_ALIGN
 
 
 def test_attention_of_nothing_is_done():
