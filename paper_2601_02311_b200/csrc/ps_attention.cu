@@ -29,9 +29,16 @@ constexpr float MINUS_INF = -INFINITY;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int THREADS = 384;            // two groups of four warps, and one of the copying warp, the two that start products and an idle one
 constexpr int COPY_WARP = 8, MMA_WARP = 9, MMA_WARP2 = 10;
-// registers of a thread: as launched, and as the third group gives to the others (3 * 168 = 2 * 208 + 88)
-constexpr int LAUNCHED = 168, TAKEN = 208, LEFT = 88;
-static_assert(3 * LAUNCHED == 2 * TAKEN + LEFT && THREADS * LAUNCHED <= 65536, "registers that the block has");
+// Registers of a thread: as launched, and as the third group gives to the others.  (Forward, 8192 queries, 32 heads of 64: 437 us with 208
+// and 88, where the groups spill, 366 with 216 and 72; of 128: 453 with either, 588 with 224 and 56, where the products' warp
+// does.  Backward, heads of 128: 1508 with 208, 1543 with 216.)
+constexpr int LAUNCHED = 168;
+template <int TAKEN> struct Registers {
+  static constexpr int taken = TAKEN, left = 3 * LAUNCHED - 2 * TAKEN;
+};
+typedef Registers<216> ForwardRegisters;
+typedef Registers<208> BackwardRegisters;
+static_assert(THREADS * LAUNCHED <= 65536, "registers that the block has");
 
 // what a kernel needs beside the maps of its operands
 struct Args {
@@ -167,7 +174,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   const Lengths l = lengths_of(a, b);
   const int skip = CHUNKED ? blockIdx.y * CHUNK : 0, key0 = skip * ROWS;        // tiles of keys before this block's, and its first key
   const auto tiles_of = [&](int i) { return CHUNKED ? max(0, min(key_tiles(a, l, i) - skip, CHUNK)) : key_tiles(a, l, i); };
-  const int count[2] = {tiles_of(q0), tiles_of(q0 + ROWS)}, most = max(count[0], count[1]);
+  const int count0 = tiles_of(q0), count1 = tiles_of(q0 + ROWS), most = max(count0, count1);
 
   if (warp == MMA_WARP) tmem_alloc(smem_address(&tmem_at), 512);
   if (threadIdx.x == 0) {
@@ -192,19 +199,20 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
-    take_registers<TAKEN>();
+    take_registers<ForwardRegisters::taken>();
     const int t = warp / 4, row = threadIdx.x % ROWS, i = q0 + t * ROWS + row, end = end_of(a, l, i) - key0;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, s_at = tmem + lanes + t * ROWS, o_at = tmem + lanes + 2 * ROWS + t * D;
     // the first tile of keys of which some query of this tile does not see all
     const int masked = q0 + (t + 1) * ROWS > l.n ? 0 : (end_of(a, l, q0 + t * ROWS) - key0) / ROWS;
     const float slack = 8.f / a.c;
+    const int count = t ? count1 : count0;
     float most_s = MINUS_INF, total = 0.f;
-    if (TMEM && count[t]) {
+    if (TMEM && count) {
       w.wait(q_full + 8 * t, 0);
       tile_to_tmem<D>(tmem_q + lanes + t * (D / 2), tiles + t * TILE);
       if (lane == 0) barrier_arrive(in_tmem + 8 * t);
     }
-    for (int j = 0; j < count[t]; ++j) {
+    for (int j = 0; j < count; ++j) {
       w.wait(s_full + 8 * t, j & 1);
       fence_after();
       u32 s[4][32];
@@ -265,8 +273,8 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       const float2 sums = split(add2(sum[0], sum[1]));
       total += sums.x + sums.y;
     }
-    if (count[t]) {
-      w.wait(o_done + 8 * t, (count[t] - 1) & 1);
+    if (count) {
+      w.wait(o_done + 8 * t, (count - 1) & 1);
       fence_after();
     }
     const bool there = i < a.q_len, none = most_s == MINUS_INF && total == 0.f;
@@ -274,17 +282,18 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const float lse = none ? MINUS_INF : (most_s * a.c + log2f(total)) * LN2, by = none ? 0.f : 1.f / total;
     if constexpr (CHUNKED) {
       const u64 at = (((u64)blockIdx.y * a.batch + b) * a.heads + h) * a.q_len + safe;
-      if (count[t]) store_part<D>(a.parts + at * D, o_at, there, by);
+      if (count) store_part<D>(a.parts + at * D, o_at, there, by);
       if (there) a.part_lse[at] = lse;
     } else {
-      store_row<T, D>(row_of<T>(a.out, b, safe, h), o_at, count[t] > 0, there, a.dim, by);
+      store_row<T, D>(row_of<T>(a.out, b, safe, h), o_at, count > 0, there, a.dim, by);
       if (there) a.lse[((u64)b * a.heads + h) * a.q_len + i] = lse;
     }
   } else if (warp == COPY_WARP) {
-    give_registers<LEFT>();
+    give_registers<ForwardRegisters::left>();
     if (lane == 0) {
+#pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (count[t]) {
+        if (t ? count1 : count0) {
           barrier_expect(q_full + 8 * t, TILE);
           load_tile<D>(tiles + t * TILE, &map_q, h, q0 + t * ROWS, b, q_full + 8 * t);
         }
@@ -297,7 +306,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       }
     }
   } else if (warp == MMA_WARP) {
-    give_registers<LEFT>();
+    give_registers<ForwardRegisters::left>();
     const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_o = instruction<T>(D, true, false);
     auto scores = [&](int t, int j) {
       const u32 k = ring + (2 * j % RING) * TILE;
@@ -307,8 +316,9 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     };
     if (most > 0) {
       w.wait(full, 0);
+#pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (count[t]) {
+        if (t ? count1 : count0) {
           w.wait((TMEM ? in_tmem : q_full) + 8 * t, 0);
           fence_after();
           if (elected() && !w.dead) scores(t, 0);
@@ -321,8 +331,10 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       w.wait(full + 8 * slot, x / RING & 1);
       if (l.m < a.k_len && key0 + (j + 1) * ROWS > l.m && !w.dead) clear_rows<D>(v, l.m - key0 - j * ROWS);
       if (j + 1 < most) w.wait(full + 8 * next, (x + 1) / RING & 1);
+#pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (j >= count[t]) continue;
+        const int count = t ? count1 : count0;
+        if (j >= count) continue;
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) {
           w.wait(p_ready + 16 * t + 8 * part, j & 1);
@@ -335,7 +347,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           __syncwarp();
         }
         __syncwarp();
-        if (j + 1 < count[t]) {           // S goes over P, which that product reads: nothing but its end orders the two
+        if (j + 1 < count) {           // S goes over P, which that product reads: nothing but its end orders the two
           w.wait(o_done + 8 * t, j & 1);
           fence_after();
           if (elected() && !w.dead) scores(t, j + 1);
@@ -349,7 +361,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       __syncwarp();
     }
   } else {
-    give_registers<LEFT>();
+    give_registers<ForwardRegisters::left>();
   }
   linger(w.dead);
   fence_before();
@@ -528,7 +540,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
-    take_registers<TAKEN>();
+    take_registers<BackwardRegisters::taken>();
     const int mine = warp / 4, j = j0 + threadIdx.x % ROWS;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
     // this key's first query; the first query that all of the tile's keys have
@@ -628,7 +640,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       store_row<T, D>(row_of<T>(mine ? a.d_k : a.d_v, b, safe, kh), from, total > 0, there, a.dim, used ? by : 0.f);
     }
   } else if (warp == COPY_WARP) {
-    give_registers<LEFT>();
+    give_registers<BackwardRegisters::left>();
     if (lane == 0 && total > 0) {
       barrier_expect(kv_full, 2 * TILE);
       load_tile<D>(k_tile, &map_k, kh, j0, b, kv_full);
@@ -655,7 +667,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   } else if (warp == MMA_WARP || warp == MMA_WARP2) {
     // One warp starts the sums dV and dK, in the pairs' order, the other the products that fill the buffers.  A product that
     // writes a buffer waits for the end of the one that reads it: nothing else orders the two.
-    give_registers<LEFT>();
+    give_registers<BackwardRegisters::left>();
     // queries behind the sequence's end, in its last tile
     auto pad_from = [&](int x) {
       const int i0 = (first + x % walk) * ROWS;
@@ -733,7 +745,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       }
     }
   } else {
-    give_registers<LEFT>();
+    give_registers<BackwardRegisters::left>();
   }
   linger(w.dead);
   fence_before();
@@ -793,7 +805,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
-    take_registers<TAKEN>();
+    take_registers<BackwardRegisters::taken>();
     const int mine = warp / 4, i = q0 + threadIdx.x % ROWS, end = end_of(a, l, i) - key0;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
     const int masked = q0 + ROWS > l.n ? 0 : (end_of(a, l, q0) - key0) / ROWS;
@@ -872,7 +884,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       store_row<T, D / 2>(row_of<T>(a.d_q, b, safe, h) + mine * (D / 2), from, total > 0, there, a.dim - mine * (D / 2), by);
     }
   } else if (warp == COPY_WARP) {
-    give_registers<LEFT>();
+    give_registers<BackwardRegisters::left>();
     if (lane == 0 && total > 0) {
       barrier_expect(q_full, 2 * TILE);
       load_tile<D>(q_tile, &map_q, h, q0, b, q_full);
@@ -891,7 +903,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     }
   } else if (warp == MMA_WARP || warp == MMA_WARP2) {
     // (as in k_keys: one warp for the sum, the other for the products that fill the buffers)
-    give_registers<LEFT>();
+    give_registers<BackwardRegisters::left>();
     if (warp == MMA_WARP) {
       const u32 ins = instruction<T>(D, true, false);
       for (int x = 0; x < total; ++x) {          // dQ += dS K
@@ -947,7 +959,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       }
     }
   } else {
-    give_registers<LEFT>();
+    give_registers<BackwardRegisters::left>();
   }
   linger(w.dead);
   wait_for_earlier();          // k_keys: this kernel ends behind it, as whatever follows in the stream expects
