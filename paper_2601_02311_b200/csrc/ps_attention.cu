@@ -157,9 +157,6 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   constexpr u32 TILE = PANEL * (D / 64);
   constexpr int RING = 4;
   constexpr bool TMEM = D == 64;          // Q is the left operand from tensor memory where there is room for it
-  // P is handed over in parts where the product is short beside the exponentials (8192 queries, 32 heads of 64: 437 us in one part, 375
-  // in two; heads of 128: 454 and 552, since the products' warp then waits with the other tile's work behind it)
-  constexpr int PARTS = D == 64 ? 2 : 1;
   __shared__ u64 bars[2 + 2 * RING + 10];
   __shared__ u32 tmem_at;
   const u32 tiles = tiles_begin(), ring = tiles + 2 * TILE;
@@ -263,11 +260,11 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           p[e / 2] = pack<T>(x.x, x.y);
         }
         tmem_store16(s_at + 16 * q, p);
-        if (q == 3 || (PARTS == 2 && q == 1)) {
+        if (q & 1) {             // half of P: the product's first steps may begin
           wait_stores();
           fence_before();
           __syncwarp();
-          if (lane == 0) barrier_arrive(p_ready + 16 * t + (PARTS == 2 ? 8 * (q / 2) : 0));
+          if (lane == 0) barrier_arrive(p_ready + 16 * t + 8 * (q / 2));
         }
       }
       const float2 sums = split(add2(sum[0], sum[1]));
@@ -336,13 +333,13 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         const int count = t ? count1 : count0;
         if (j >= count) continue;
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
+        for (int part = 0; part < 2; ++part) {
           w.wait(p_ready + 16 * t + 8 * part, j & 1);
           fence_after();
           if (elected() && !w.dead) {
-            multiply_across<ROWS / PARTS>(tmem + 2 * ROWS + t * D, tmem + t * ROWS + part * (ROWS / 2 / PARTS), v + part * (ROWS / PARTS) * 128,
-                                          ins_o, j > 0 || part > 0);
-            if (part + 1 == PARTS) commit(o_done + 8 * t);
+            multiply_across<ROWS / 2>(tmem + 2 * ROWS + t * D, tmem + t * ROWS + part * (ROWS / 4), v + part * (ROWS / 2) * 128, ins_o,
+                                      j > 0 || part > 0);
+            if (part) commit(o_done + 8 * t);
           }
           __syncwarp();
         }
