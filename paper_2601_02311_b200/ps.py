@@ -189,8 +189,8 @@ def _on_own_stream(method):
     before it still uses."""
     @functools.wraps(method)
     def run(self, *args, **kwargs):
-        ctx = getattr(self, "ctx", self)
-        if ctx.on_current_stream():
+        ctx = self if isinstance(self, Context) else self.ctx
+        if torch._C._cuda_getCurrentRawStream(ctx.device) == ctx._raw_stream:      # (ctx.on_current_stream)
             return method(self, *args, **kwargs)
         with torch.cuda.stream(ctx.stream if ctx.stream is not None else torch.cuda.default_stream(ctx.device)):
             return method(self, *args, **kwargs)
@@ -206,6 +206,7 @@ class Context:
         self.device = device
         self.torch_device = torch.device("cuda", device)
         self.stream = stream
+        self._raw_stream = stream.cuda_stream if stream is not None else 0
         handle = C.c_void_p()
         sptr = C.c_void_p(stream.cuda_stream) if stream is not None else None
         _check(_lib.ps_create(C.byref(handle), device, sptr), "ps_create")
@@ -222,9 +223,8 @@ class Context:
 
     def on_current_stream(self) -> bool:
         """Whether torch's current stream on the device is the one the library enqueues on."""
-        mine = self.stream.cuda_stream if self.stream is not None else 0
         # (asked before every call that allocates: a Stream object made for it costs a sweep of 60 us 2 us)
-        return torch._C._cuda_getCurrentRawStream(self.device) == mine
+        return torch._C._cuda_getCurrentRawStream(self.device) == self._raw_stream
 
     def status(self) -> int:
         return _lib.ps_status(self._h)

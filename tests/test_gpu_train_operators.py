@@ -201,7 +201,8 @@ def gradient_want(d_out, ids, rows, scale, first_row, dtype):
 @pytest.mark.parametrize("dtype, grad", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32"), ("f32", "bf16")])
 @pytest.mark.parametrize("tokens, rows, dim, spread", [
     (0, 4, 8, 1), (1, 1, 1, 1), (1, 300, 8, 1), (40, 7, 3, 1), (513, 2000, 130, 1), (4096, 40, 264, 3), (5000, 1, 72, 1),
-    (3000, 70001, 16, 2), (20000, 257, 8, 6), (2500, 5, 1030, 1)])
+    (3000, 70001, 16, 2), (20000, 257, 8, 6), (2500, 5, 1030, 1),
+    (8192, 300, 24, 2), (8193, 300, 24, 2), (20000, 300001, 8, 5), (33000, 2, 40, 1)])
 def test_table_gradient(ctx, dtype, grad, tokens, rows, dim, spread):
     gen = torch.Generator("cuda").manual_seed(tokens + dim)
     d_out = normal(gen, tokens, dim, dtype=TYPES[dtype])
@@ -252,6 +253,21 @@ def test_table_gradient_of_shards_is_the_whole_tables(ctx):
     for begin, end in ((0, 1), (1, 400), (400, 1000)):
         assert torch.equal(ctx.embed_backward(d_out, ids, end - begin, first_row=begin), whole[begin:end])
     ctx.check_status()
+
+
+def test_embedding_rows_behind_two_to_the_32_bytes(ctx):
+    """Offsets that pass 32 bits, in elements and bytes, on both sides."""
+    rows, dim = 70000, 1 << 16                          # 4.6e9 elements
+    table = torch.zeros(rows, dim, device="cuda", dtype=torch.bfloat16)
+    table[-3:] = 2.0
+    ids = torch.tensor([rows - 1, 0, rows - 3, -1], device="cuda")
+    out = ctx.embed_forward(table, ids)
+    assert out.amin(1).tolist() == [2.0, 0.0, 2.0, 0.0] and out.amax(1).tolist() == [2.0, 0.0, 2.0, 0.0]
+    ids = torch.tensor([rows - 1, rows - 1, rows - 2], device="cuda")
+    ctx.embed_backward_into(torch.ones(3, dim, device="cuda", dtype=torch.bfloat16), ids, table)
+    ctx.check_status()
+    assert table[-3:].amin(1).tolist() == [0.0, 1.0, 2.0] and table[-3:].amax(1).tolist() == [0.0, 1.0, 2.0]
+    assert not table[:-3].any()
 
 
 def test_table_gradient_agrees_with_differences(ctx):
@@ -477,6 +493,22 @@ def test_attention_of_any_strides(ctx, order):
     ctx.check_status()
 
 
+def test_attention_of_strides_behind_two_to_the_31(ctx):
+    """Tokens 2^29 elements apart and sequences 2^31: a view of a few rows of a very large tensor."""
+    q, k, v, d_out = tensors(17, 2, 4, 4, 1, 1, 64, "bf16")
+    hold = torch.zeros((1 << 32) + 256, device="cuda", dtype=torch.bfloat16)
+    far = [hold.as_strided((2, 4, 1, 64), (1 << 31, 1 << 29, 64, 1), 64 * i) for i in range(4)]
+    for f, x in zip(far, (q, k, v, d_out)):
+        f.copy_(x)
+    out, lse = ctx.attention_forward(*far[:3])
+    want = ctx.attention_forward(q, k, v)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    grads = ctx.attention_backward(*far[:3], out, lse, far[3])
+    for g, w in zip(grads, ctx.attention_backward(q, k, v, out, lse, d_out)):
+        assert torch.equal(g, w)
+    ctx.check_status()
+
+
 def test_attention_leaves_what_lies_around_its_results(ctx):
     q, k, v, d_out = tensors(8, 2, 130, 140, 2, 1, 40, "bf16")
     out, lse = ctx.attention_forward(q, k, v)
@@ -607,19 +639,51 @@ def test_a_step_on_shards_is_the_single_devices(ctx):
     ctx.check_status()
 
 
+def test_operators_on_two_streams_at_once(ps):
+    """Two contexts whose calls overlap on the device: no work space is shared."""
+    contexts = [ps.Context(0, torch.cuda.Stream()) for _ in range(2)]
+    gen = torch.Generator("cuda").manual_seed(18)
+    inputs = []
+    for i in range(2):
+        q, k, v, d_out = tensors(19 + i, 2, 700, 900, 8, 4, 128 if i else 64, "f16" if i else "bf16")
+        rows = normal(gen, 9000 + i, 256, dtype=torch.bfloat16)
+        inputs.append((q, k, v, d_out, rows, torch.randint(0, 50, (9000 + i,), device="cuda", generator=gen)))
+
+    def every(ctx, q, k, v, d_out, rows, ids):
+        out, lse = ctx.attention_forward(q, k, v)
+        return (out, lse) + ctx.attention_backward(q, k, v, out, lse, d_out) + (
+            ctx.embed_backward(rows, ids, 60), ctx.dropout(rows, 0.3, 5))
+    torch.cuda.synchronize()
+    want = []
+    for ctx, x in zip(contexts, inputs):
+        want.append(every(ctx, *x))
+        torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for _ in range(3):
+            got = [every(ctx, *x) for ctx, x in zip(contexts, inputs)]
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(g, w))
+    for ctx in contexts:
+        ctx.check_status()
+
+
 def test_operators_on_other_streams_and_in_graphs(ps):
     """A context of its own stream, and every operator captured once and replayed on new data, two graphs in turn."""
     side = torch.cuda.Stream()
     ctx = ps.Context(0, side)
     gen = torch.Generator("cuda").manual_seed(14)
     q, k, v, d_out = tensors(15, 2, 140, 140, 4, 2, 64, "bf16")
+    qh, kh, vh, gh = tensors(16, 1, 9, 5000, 2, 1, 128, "f16")       # (with norms and chunks)
     table = normal(gen, 90, 256, dtype=torch.bfloat16)
     tokens = torch.randint(0, 90, (280,), device="cuda", generator=gen)
     rows = normal(gen, 280, 256, dtype=torch.bfloat16)
 
     def every():
         out, lse = ctx.attention_forward(q, k, v)
-        return (out, lse) + ctx.attention_backward(q, k, v, out, lse, d_out) + (
+        half = ctx.attention_forward(qh, kh, vh)
+        return (out, lse) + half + ctx.attention_backward(qh, kh, vh, *half, gh) + ctx.attention_backward(q, k, v, out, lse, d_out) + (
             ctx.embed_forward(table, tokens), ctx.embed_backward(rows, tokens, 90), ctx.dropout(rows, 0.1, 3, residual=rows))
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
