@@ -530,14 +530,14 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   fence_before();
   __syncthreads();
   fence_after();
-  wait_for_earlier();          // the rows
-  let_next_begin();            // behind the wait: k_queries needs the rows too, and nothing of this kernel
   const u32 tmem = sh.tmem_at, tmem_dv = tmem + 2 * ROWS, tmem_dk = tmem_dv + D,
             tmem_k = tmem_dk + D, tmem_v = tmem_k + D / 2;      // (D = 64)
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
     take_registers<BackwardRegisters::taken>();
+    wait_for_earlier();          // the rows
+    let_next_begin();            // behind the wait: k_queries needs the rows too, and nothing of this kernel
     const int mine = warp / 4, j = j0 + threadIdx.x % ROWS;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
     // this key's first query; the first query that all of the tile's keys have
@@ -649,6 +649,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
         if (w.dead) break;
         barrier_expect(q_full + 8 * slot, TILE + VECTOR);
         load_tile<D>(q_ring + slot * TILE, &map_q, h, i0, b, q_full + 8 * slot);
+        if (x == 0) wait_for_earlier();          // (tiles come from the caller, vectors from the rows' kernel)
         load_bytes(lse_ring + slot * VECTOR, a.lse2 + row, VECTOR, q_full + 8 * slot);
         w.wait(do_empty + 8 * two, (x >> 1 & 1) ^ 1);
         if (w.dead) break;
