@@ -9,7 +9,7 @@
 // padding: nothing of theirs is used, and zeros are written for them.
 //
 // All products run on the tensor cores (ps_tensor.cuh) on tiles of 128 queries and 128 keys; the matrices between two
-// products (P, dS) stay in tensor memory.  A block has a warp that copies tiles, a warp that starts products, and two
+// products (P, dS) stay in tensor memory.  A block has a warp that copies tiles, one or two that start products, and two
 // groups of four warps that take the exponentials.
 //
 // Exponents are taken to base 2: exp(S - lse) = 2^(c S' - lse log2 e) with S' = Q K^T and c = |scale| log2 e (a negative
@@ -343,7 +343,6 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           }
           __syncwarp();
         }
-        __syncwarp();
         if (j + 1 < count) {           // S goes over P, which that product reads: nothing but its end orders the two
           w.wait(o_done + 8 * t, j & 1);
           fence_after();
@@ -411,11 +410,12 @@ __device__ __forceinline__ float gradient_factor(const Args& a, int b, int kh) {
   return exp2_fast((float)(max(-60, min(60, e)) - P_SHIFT));
 }
 
-// The rows that both kernels read: 16 lanes a query, delta and the exponent's offset; in half precision the largest
+// The rows that both kernels read: D / 8 lanes a query, delta and the exponent's offset; in half precision the largest
 // norms of each key head's dO and V rows as well (as bits: norms are not negative, so they compare as integers), one atomic
 // a block.
-constexpr int ROWS_A_THREAD = 4, ROWS_A_BLOCK = 16 * ROWS_A_THREAD;
-template <class T, bool QUERY>
+constexpr int ROWS_A_THREAD = 4;
+template <int D> constexpr int ROWS_A_BLOCK = 256 / (D / 8) * ROWS_A_THREAD;
+template <class T, int D, bool QUERY>
 __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads out, const Args a) {
   let_next_begin();
   __shared__ u32 largest;
@@ -423,12 +423,13 @@ __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads o
     if (threadIdx.x == 0) largest = 0;
     __syncthreads();
   }
-  const int part = threadIdx.x % 16, first = blockIdx.x * ROWS_A_BLOCK + threadIdx.x / 16, h = blockIdx.y, b = blockIdx.z;
+  constexpr int LANES = D / 8, STEP = 256 / LANES;
+  const int part = threadIdx.x % LANES, first = blockIdx.x * ROWS_A_BLOCK<D> + threadIdx.x / LANES, h = blockIdx.y, b = blockIdx.z;
   const Lengths l = lengths_of(a, b);
   Pack<T, 8> p[ROWS_A_THREAD], q[ROWS_A_THREAD];
 #pragma unroll
   for (int r = 0; r < ROWS_A_THREAD; ++r) {
-    const int i = first + 16 * r;
+    const int i = first + STEP * r;
     p[r].clear();
     q[r].clear();
     if (i < (QUERY ? l.n : l.m) && part * 8 < a.dim) {
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads o
   }
 #pragma unroll
   for (int r = 0; r < ROWS_A_THREAD; ++r) {
-    const int i = first + 16 * r;
+    const int i = first + STEP * r;
     float v[8], y[8], dot = 0.f, norm = 0.f;
     p[r].widen(v);
     q[r].widen(y);
@@ -448,11 +449,11 @@ __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads o
       if (Range<T>::small) norm = fmaf(v[e], v[e], norm);
     }
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) {
+    for (int o = LANES / 2; o > 0; o >>= 1) {
       if (QUERY) dot += __shfl_xor_sync(0xffffffffu, dot, o);
       if (Range<T>::small) norm += __shfl_xor_sync(0xffffffffu, norm, o);
     }
-    if (part != 0) continue;
+    if (part != 0 || i >= (QUERY ? a.padded : a.k_len)) continue;
     if (QUERY) {
       const u64 head = (u64)b * a.heads + h;
       const float lse = i < l.n ? a.lse[head * a.q_len + i] : MINUS_INF;
@@ -466,7 +467,6 @@ __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads o
     if (threadIdx.x == 0) atomicMax(a.norms + 2 * (b * a.kv_heads + (QUERY ? h / (a.heads / a.kv_heads) : h)) + (QUERY ? 0 : 1), largest);
   }
 }
-static_assert(ROWS % ROWS_A_BLOCK == 0, "whole blocks of rows in whole tiles");
 
 // Both kernels of the backward pass let their two groups of warps take turns: tile pairs are numbered, a group has the even
 // ones and the other the odd ones, each with a buffer of 128 columns of tensor memory of its own, a thread a row.  A
@@ -1103,13 +1103,13 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
   if constexpr (Range<T>::small) {
     e = cudaMemsetAsync(r.norms, 0, sizeof(u32) * 2 * a.batch * a.kv_heads, stream);
     if (e == cudaSuccess && a.k_len) {
-      k_rows<T, false><<<dim3((a.k_len + ROWS_A_BLOCK - 1) / ROWS_A_BLOCK, a.kv_heads, a.batch), 256, 0, stream>>>(a.v, a.v, r);
+      k_rows<T, D, false><<<dim3((a.k_len + ROWS_A_BLOCK<D> - 1) / ROWS_A_BLOCK<D>, a.kv_heads, a.batch), 256, 0, stream>>>(a.v, a.v, r);
       e = cudaGetLastError();
     }
     if (e != cudaSuccess) return e;
   }
   if (a.q_len) {
-    k_rows<T, true><<<dim3(r.padded / ROWS_A_BLOCK, a.heads, a.batch), 256, 0, stream>>>(a.d_out, a.out, r);
+    k_rows<T, D, true><<<dim3((r.padded + ROWS_A_BLOCK<D> - 1) / ROWS_A_BLOCK<D>, a.heads, a.batch), 256, 0, stream>>>(a.d_out, a.out, r);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   // (one side at most is cut: few rows of it and many of the other)
