@@ -21,12 +21,16 @@
  *               composition validity (Theorems 6-7, Proposition 1, Remark 4)
  *               and their reasons.
  *
- * No result is ever rounded: every figure is an exact integer (a sweep compares
+ * No figure of a space is ever rounded: it is an exact integer (a sweep compares
  * on the fp64 pipe only where all numbers of a factorisation are below 2^53,
  * which doubles hold exactly).  Shards are element-granular with the
  * boundaries of Definition 1 eq. (2); the per-device figure is the largest
  * shard, ceil(E/n); a ring reduce-scatter or all-gather (Section 2.3) moves
  * E - floor(E/n) elements on its busiest device; an all-reduce twice that.
+ *
+ * Beside the figures stand a brute-force run of the mechanism (ps_verify_batch) and
+ * the operators of a training step whose terms the figures price (ps_dropout,
+ * ps_embed_*, ps_attention_*), which compute in floating point.
  *
  * Conventions.  Every function returns 0 (PS_OK) or a negative PS_E_* code and
  * never aborts.  "device pointer" = memory of the context's GPU, owned by the

@@ -147,9 +147,16 @@ __device__ __forceinline__ void linger(bool dead) {
 // ------------------------------------------------------------------ forward
 // A block owns two tiles of 128 queries of a head, a group of warps each, a thread a query.  While one group takes the
 // exponentials of its scores the tensor cores work for the other.  A group's turn: the scores S = Q K^T (128 columns of
-// tensor memory), their row maximum, P = 2^(c S - c maximum) written over S in 16 bits, O += P V.  O is rescaled only when a
-// row's maximum has grown by more than a factor of 2^8: until then P is larger than 1 by up to that, which the 32-bit
-// sums and the types' exponents hold, and lse comes from the same maximum.
+// tensor memory), their row maximum, P = 2^(c S - c maximum) written over S in 16 bits, O += P V, begun when half of P is there.
+// O is rescaled only when a row's maximum has grown by more than a factor of 2^8: until then P is larger than 1 by up
+// to that, which the 32-bit sums and the types' exponents hold, and lse comes from the same maximum.
+//
+// A product that writes tensor memory waits for the end of the one that reads it (S over P): nothing else orders products with
+// different sums.  What bounds it, 8192 queries, 32 heads of 128 on 8 key heads, causal: 453 us, 1.21 PFLOP/s, the
+// tensor pipe busy for 62 % and the special functions (16384 exponentials a tile pair, 16 a cycle) for 58 %, a group's chain S, exponentials,
+// P V in between; after a second of it the power limit, 517 us.  Tried and slower: scores of 64 keys in two buffers (573: with 64
+// columns a product is bound by shared memory), a warp for each tile's products (559: they interleave and both end late),
+// a fourth of the exponentials as polynomials (448 against 440 then), blocks that take over others' work (registers).
 template <class T, int D, bool CHUNKED>
 __global__ void __launch_bounds__(THREADS, 1)
 k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -235,7 +242,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         const float by = grown ? exp2_fast((most_s - now) * a.c) : 1.f;
         if (grown) most_s = now;
         total *= by;
-        if (j > 0) {           // (the product that wrote O last is done: S, which was started behind it, is there)
+        if (j > 0) {           // (the product that wrote O last is done: S, which was started behind its end, is there)
 #pragma unroll
           for (int c = 0; c < D; c += 32) {
             u32 o[32];
@@ -471,7 +478,9 @@ __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads o
 // Both kernels of the backward pass let their two groups of warps take turns: tile pairs are numbered, a group has the even
 // ones and the other the odd ones, each with a buffer of 128 columns of tensor memory of its own, a thread a row.  A
 // pair's buffer holds S, then what its products leave of P, then dP, then dS.  While one group works the tensor cores
-// multiply for the other; the products are started in an order fixed by the numbers.
+// multiply for the other.  One warp starts the products that add to the results, in the pairs' order, and another those that
+// fill the buffers, each behind the end of the product that reads what it overwrites (one warp for both: 1577 us for the case below
+// instead of 1512; both groups on each pair, a half of it each: 2008).
 //
 // Shared memory is full (224 KB of tiles for D = 128), so barriers and vectors share what is behind the tiles.
 struct Shared {
@@ -482,8 +491,9 @@ struct Shared {
 // A block owns 128 keys of a key head and walks the queries that see them, through all query heads that share it.  Scores are
 // transposed: S^T = K Q^T has a key a lane, so P^T and dS^T are left operands in tensor memory, and Q and dO serve as right
 // operands of both kinds from one copy.  Tensor memory (D = 128): the two buffers, dV and dK, 128 columns each.
-// Products: S S | dV dP, dV dP | dK S, dK S | ..., so that a buffer's P is used up before dP is written over it.
 // Q has three slots, since S of pair x + 2 follows on dK of pair x; dO, with two, is free after dP.
+// What bounds it, 8192 queries, 32 heads of 128 on 8 key heads, causal: 0.88 ms, the tensor pipe busy for 69 %: S and dP take both
+// operands from shared memory, whose 128 bytes a cycle they use up, and the rest is the chain of a pair.
 template <class T, int D, bool CHUNKED>
 __global__ void __launch_bounds__(THREADS, 1)
 k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -754,9 +764,10 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   }
 }
 
-// A block owns 128 queries of a head and walks the keys they see.  Tensor memory (D = 128): the two buffers and dQ, 128 columns
-// each.  P stays in registers, so dP may be written over S as soon as S has been read.
-// Products: S S | dP dP | dQ S, dQ S | dP dP | ...  K has three slots, V two, as Q and dO above.
+// A block owns 128 queries of a head and walks the keys they see.  P stays in registers, so dP may be written over S as soon as S
+// has been read.  Tensor memory (D = 128): the two buffers, dQ, and Q and dO as left operands (from shared memory: 1512 us for the
+// whole pass then, 1487 so).  K has three slots, V two, as Q and dO above.  The same case: 0.67 ms, the tensor pipe
+// busy for 65 %.  A third buffer of scores, with Q and dO in shared memory again, took as long.
 template <class T, int D, bool CHUNKED>
 __global__ void __launch_bounds__(THREADS, 1)
 k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,

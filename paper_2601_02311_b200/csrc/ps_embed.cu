@@ -9,8 +9,13 @@
 // order in which blocks run), marks where each row's list begins and ends, and gives each row of the table to warps that
 // sum its list: every row of d_table is written once, every row of d_out read once.  A list of c tokens is cut
 // from its own beginning into pieces of 32 and pieces of 1024, which other blocks sum first; the warp adds the sums of
-// the pieces of 1024, then of the pieces of 32 behind them, then the rest: at most c / 1024 + 62 terms.  The cut
-// follows from c alone, so a row's bits are the same whatever else the table holds.
+// the pieces of 1024, then of the pieces of 32 behind them, then the rest: at most c / 1024 + 62 terms (below 4096 tokens
+// there are no pieces of 1024).  The cut follows from c alone, so a row's bits are the same whatever else the table holds.
+//
+// What bounds them: bytes.  131072 lookups of 8192 bfloat16 in 128000 rows: 540 us, 5.2 TB/s by what has to move, 5.8 by what does (words of
+// middling frequency leave the L2 between two lookups).  The gradient of as many tokens into 256000 rows, 6.2 GB: 1.15 ms, 5.4 TB/s: 0.91 ms the
+// rows (5.9 TB/s), 0.16 the pieces, 0.04 the sort, whose kernels are small.  2048 tokens into 32000 rows of 768: 32 us, of which
+// 16 are the rows and the rest the chain of three short kernels before them.
 #include "ps_train.cuh"
 
 namespace {
@@ -196,7 +201,7 @@ __global__ void __launch_bounds__(256) k_mark(const u32* keys, u32 n, uint2* ran
 
 // Few tokens need no passes: a token's place is the number of smaller rows before or behind it plus the number of equal ones before it, and
 // its row's list begins behind the smaller ones.  A warp counts for a token, over all rows in shared memory: n^2 comparisons on all
-// SMs, 1.5 us of work for 2048 tokens, where one block's radix passes took 8.
+// SMs (2048 tokens: 6 us, most of it launch and loads, where one block's radix passes took 11).
 constexpr u32 RANK_MOST = 8192;
 __global__ void __launch_bounds__(256) k_rank(EmbedArgs a, u32 n, u32* keys, u32* places, uint2* ranges) {
   extern __shared__ uint4 rows4[];
