@@ -9,9 +9,9 @@
 // key seed; threshold = round(p * 2^32) and scale = 1 / (1 - p).
 //
 // What bounds it: bytes, two or three arrays.  65536 x 8192 in bfloat16 with a residual, 3.2 GB: 567 us, 5.7 TB/s (0.88 of a
-// copy's rate), issue slots taken for 56 %: a group of four words is 20 wide products and 20 exclusive-ors, and five to six elements a
-// cycle and SM pass at that rate.  12301 x 5003 floats in rows that begin anywhere, 0.49 GB: 114 us, 4.3 TB/s (a thread for each
-// four elements, with accesses of their own: 152).
+// copy's rate), issue slots taken for 56 %: a group of four words is 20 wide products and 20 exclusive-ors, and three to four elements
+// a cycle and SM pass at that rate.  12301 x 5003 floats in rows that begin anywhere, 0.49 GB: 114 us, 4.3 TB/s, issue slots
+// taken for 53 %: accesses of 4 bytes (a thread for each four elements, with accesses of their own: 148 to 151).
 #include "ps_train.cuh"
 
 namespace {

@@ -12,10 +12,10 @@
 // the pieces of 1024, then of the pieces of 32 behind them, then the rest: at most c / 1024 + 62 terms (below 4096 tokens
 // there are no pieces of 1024).  The cut follows from c alone, so a row's bits are the same whatever else the table holds.
 //
-// What bounds them: bytes.  131072 lookups of 8192 bfloat16 in 128000 rows: 540 us, 5.2 TB/s by what has to move, 5.8 by what does (words of
+// What bounds them: bytes.  131072 lookups of 8192 bfloat16 in 128000 rows: 540 us, 5.2 TB/s by what has to move, 5.7 by what does (words of
 // middling frequency leave the L2 between two lookups).  The gradient of as many tokens into 256000 rows, 6.2 GB: 1.15 ms, 5.4 TB/s: 0.91 ms the
 // rows (5.9 TB/s), 0.16 the pieces, 0.04 the sort, whose kernels are small.  2048 tokens into 32000 rows of 768: 32 us, of which
-// 16 are the rows and the rest the chain of three short kernels before them.
+// 17 are the rows and 12 the two short kernels before them.
 #include "ps_train.cuh"
 
 namespace {
