@@ -114,7 +114,7 @@ bool overwrites(const void* y, u64 y_stride, const void* x, u64 x_stride, u64 ro
   const u64 ya = (u64)(uintptr_t)y, xa = (u64)(uintptr_t)x;
   const u64 y_end = ya + ((rows - 1) * y_stride + cols) * width, x_end = xa + ((rows - 1) * x_stride + cols) * width;
   if (y_end <= xa || x_end <= ya) return false;
-  if (y_stride != x_stride) return true;
+  if (rows == 1 || y_stride != x_stride) return true;           // (a single row's strides say nothing, and may be 0)
   const u64 pitch = y_stride * width, off = (ya > xa ? ya - xa : xa - ya) % pitch;
   return off < cols * width || pitch - off < cols * width;
 }

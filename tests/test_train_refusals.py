@@ -52,6 +52,10 @@ def dropout(**kw):
     (dict(y=AT, y_stride=16), ps.E_RANGE),                         # x itself with other strides
     (dict(residual=AT + 4096 + 32), ps.E_RANGE),                   # overlaps y
     (dict(x_stride=32, y_stride=32, y=AT + 64, cols=20), ps.E_RANGE),
+    (dict(rows=1, x_stride=0, y_stride=0, y=AT + 4), ps.E_RANGE),  # a single row, whose stride says nothing
+    (dict(rows=1, x_stride=1, y_stride=1, y=AT + 16), ps.E_RANGE),
+    (dict(rows=1, x_stride=99, y_stride=99, y=AT - 28), ps.E_RANGE),
+    (dict(rows=1, x_stride=0, y_stride=0, residual_stride=0, residual=AT + 4096 + 4), ps.E_RANGE),
 ])
 def test_dropout_refuses(change, code):
     assert dropout(**change) == code
