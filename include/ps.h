@@ -497,7 +497,7 @@ typedef struct {
   uint64_t first_row, rows;        /* rows 1 .. 2^30                                      */
   uint64_t dim;                    /* 1 .. 2^20                                           */
   uint64_t table_stride, out_stride; /* between rows, >= dim                              */
-  double scale;
+  double scale;                    /* finite as a float                                   */
   uint32_t dtype;                  /* of table and out; backward: of d_out                */
   uint32_t grad_dtype;             /* backward: of d_table                                */
   uint32_t token_bytes;            /* tokens are int32_t (4) or int64_t (8)               */

@@ -649,7 +649,7 @@ static int embed_args(const ps_embed_desc& d, EmbedArgs& a) {
   if (d.tokens > ((u64)1 << 30) || d.rows < 1 || d.rows > ((u64)1 << 30) || d.dim < 1 || d.dim > ((u64)1 << 20) ||
       d.table_stride < d.dim || d.out_stride < d.dim || d.table_stride > ((u64)1 << 32) || d.out_stride > ((u64)1 << 32) ||
       d.dtype > PS_F16 || d.grad_dtype > PS_F16 || (d.token_bytes != 4 && d.token_bytes != 8) || d.accumulate > 1 ||
-      !std::isfinite(d.scale))
+      !std::isfinite((float)d.scale))
     return PS_E_RANGE;
   memset(&a, 0, sizeof(a));
   a.n_tokens = d.tokens; a.first_row = d.first_row; a.rows = d.rows; a.dim = d.dim;

@@ -83,7 +83,7 @@ EMBED = [(dict(ctx=None), ps.E_NULLPTR), (dict(table=None), ps.E_NULLPTR), (dict
          (dict(table=AT + 1), ps.E_ALIGN), (dict(rows=0), ps.E_RANGE), (dict(rows=(1 << 30) + 1), ps.E_RANGE),
          (dict(tokens=(1 << 30) + 1), ps.E_RANGE), (dict(dim=0), ps.E_RANGE), (dict(table_stride=7), ps.E_RANGE),
          (dict(out_stride=7), ps.E_RANGE), (dict(dtype=3), ps.E_RANGE), (dict(token_bytes=2), ps.E_RANGE),
-         (dict(scale=math.inf), ps.E_RANGE), (dict(accumulate=2), ps.E_RANGE), (dict(grad_dtype=9), ps.E_RANGE)]
+         (dict(scale=math.inf), ps.E_RANGE), (dict(scale=-1e39), ps.E_RANGE), (dict(accumulate=2), ps.E_RANGE), (dict(grad_dtype=9), ps.E_RANGE)]
 
 
 @pytest.mark.parametrize("change, code", EMBED)
