@@ -984,8 +984,8 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
 template <class T, int D, bool KEYS>
 __global__ void __launch_bounds__(256) k_join_gradients(const Args a) {
   wait_for_earlier();
-  const int lane = threadIdx.x % 32, r = blockIdx.x * 8 + threadIdx.x / 32, b = blockIdx.z;
-  const int len = KEYS ? a.k_len : a.q_len, h = KEYS ? blockIdx.y / 2 : blockIdx.y, which = KEYS ? blockIdx.y % 2 : 0;
+  const int lane = threadIdx.x % 32, at = KEYS ? blockIdx.x / 2 : blockIdx.x, which = KEYS ? blockIdx.x % 2 : 0;
+  const int r = at * 8 + threadIdx.x / 32, h = blockIdx.y, b = blockIdx.z, len = KEYS ? a.k_len : a.q_len;
   if (r >= len) return;
   const Lengths l = lengths_of(a, b);
   const int tile = r / ROWS * ROWS;
@@ -1148,7 +1148,7 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
   }
   if (cut_keys) return launch_next(k_join_gradients<T, D, false>, dim3((a.q_len + 7) / 8, a.heads, a.batch), 256, 0, stream, r);
-  if (cut_queries) return launch_next(k_join_gradients<T, D, true>, dim3((a.k_len + 7) / 8, 2 * a.kv_heads, a.batch), 256, 0, stream, r);
+  if (cut_queries) return launch_next(k_join_gradients<T, D, true>, dim3((a.k_len + 7) / 8 * 2, a.kv_heads, a.batch), 256, 0, stream, r);
   return cudaSuccess;
 }
 

@@ -443,6 +443,24 @@ def test_attention_of_few_rows_and_a_long_axis(ctx, dtype, causal, shape):
     check_backward(ctx, q, k, v, d_out, None, causal, *lens)
 
 
+def test_attention_gradients_of_the_most_heads_before_a_long_axis(ctx):
+    """One key, so that every probability is 1: dV is the sum of dO, dK nothing but rounding, and so is dQ."""
+    q, k, v, d_out = tensors(17, 1, 4097, 1, 32768, 32768, 8, "bf16")
+    out, lse = ctx.attention_forward(q, k, v, None, False)
+    d_q, d_k, d_v = ctx.attention_backward(q, k, v, out, lse, d_out, None, False)
+    ctx.check_status()
+    assert torch.equal(out, v.expand_as(out))
+    # P in 32 bits is off by less than 2^-9, so that it is rounded to 1; 4097 terms in 32 bits, one rounding
+    want, sizes = d_out.double().sum(1, keepdim=True), d_out.double().abs().sum(1, keepdim=True)
+    u = u_of(torch.bfloat16)
+    within(d_v, want, 4097 * F * sizes + u * want.abs())
+    # dO V^T and delta are sums of the same 8 products, each off by at most 8 roundings; dS by twice that and its own
+    ds = 2 * 10 * F * (d_out.double().abs() * v.double().abs()).sum(-1, keepdim=True)
+    scale = 8 ** -0.5
+    within(d_q, torch.zeros_like(d_q).double(), ds * k.double().abs() * scale * (1 + 4 * u))
+    within(d_k, torch.zeros_like(d_k).double(), (ds * q.double().abs()).sum(1, keepdim=True) * scale * (1 + 4 * u))
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 4.0])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_attention_scales(ctx, dtype, scale):
