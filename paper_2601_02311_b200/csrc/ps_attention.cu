@@ -492,6 +492,9 @@ struct Shared {
 // transposed: S^T = K Q^T has a key a lane, so P^T and dS^T are left operands in tensor memory, and Q and dO serve as right
 // operands of both kinds from one copy.  Tensor memory (D = 128): the two buffers, dV and dK, 128 columns each.
 // Q has three slots, since S of pair x + 2 follows on dK of pair x; dO, with two, is free after dP.
+// With D = 64 there is room for dP apart from the buffers, where P then lies beside dS: dP is multiplied during the exponentials and not
+// behind dV, which takes a pair from 2544 to 2304 cycles (8192 queries, 32 heads on 8, causal; the whole pass 1214 us to 1112, or 1312 to 1209 on
+// a warmer GPU), although K and V are read from shared memory for it, which slows the other group's exponentials.
 // What bounds it, 8192 queries, 32 heads of 128 on 8 key heads, causal: 0.88 ms, the tensor pipe busy for 69 %: S and dP take both
 // operands from shared memory, whose 128 bytes a cycle they use up, and the rest is the chain of a pair.
 template <class T, int D, bool CHUNKED>
@@ -499,14 +502,14 @@ __global__ void __launch_bounds__(THREADS, 1)
 k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
   constexpr u32 TILE = PANEL * (D / 64), VECTOR = ROWS * 4;
-  constexpr bool TMEM = D == 64;          // K and V are left operands from tensor memory where there is room for them
+  constexpr bool APART = D == 64;         // dP has columns of its own
   extern __shared__ __align__(1024) unsigned char shared[];
   const u32 k_tile = smem_address(shared), v_tile = k_tile + TILE, q_ring = v_tile + TILE, do_ring = q_ring + 3 * TILE,
             lse_ring = do_ring + 2 * TILE, delta_ring = lse_ring + 3 * VECTOR;
   Shared& sh = *reinterpret_cast<Shared*>(shared + 7 * TILE + 5 * VECTOR);
   const u32 kv_full = smem_address(sh.bars), q_full = kv_full + 8, q_empty = q_full + 24, do_full = q_empty + 24, do_empty = do_full + 16,
             delta_full = do_empty + 16, s_full = delta_full + 16, p_ready = s_full + 16, dp_full = p_ready + 16,
-            ds_ready = dp_full + 16, done = ds_ready + 16, in_tmem = done + 8, dv_done = in_tmem + 8;
+            ds_ready = dp_full + 16, done = ds_ready + 16, dv_done = done + 8;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
   // (under the causal mask the first keys have the most queries)
@@ -534,14 +537,13 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       barrier_init(dv_done + 8 * i, 1);
     }
     barrier_init(done, 1);
-    barrier_init(in_tmem, 8);
     fence_barrier_init();
   }
   fence_before();
   __syncthreads();
   fence_after();
-  const u32 tmem = sh.tmem_at, tmem_dv = tmem + 2 * ROWS, tmem_dk = tmem_dv + D,
-            tmem_k = tmem_dk + D, tmem_v = tmem_k + D / 2;      // (D = 64)
+  // columns: the two buffers, dP where it is apart, dV, dK
+  const u32 tmem = sh.tmem_at, tmem_dp = tmem + 2 * ROWS, tmem_dv = tmem + (APART ? 3 : 2) * ROWS, tmem_dk = tmem_dv + D;
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
@@ -555,12 +557,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
     const int whole = j0 + ROWS > l.m ? 0x7fffffff : a.causal ? j0 + ROWS - 1 - l.m + l.n : 0;
     const float factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
     const u64 cs = pair(a.c, a.c), factors = pair(factor, factor);
-    if (TMEM && total > 0) {
-      w.wait(kv_full, 0);
-      if (mine == 0) tile_to_tmem<D>(tmem_k + lanes, k_tile);
-      else tile_to_tmem<D>(tmem_v + lanes, v_tile);
-      if (lane == 0) barrier_arrive(in_tmem);
-    }
+    const u32 dp_at = APART ? tmem_dp + lanes : at, ds_at = APART ? at + ROWS / 2 : at;      // (P takes half of a buffer)
     for (int x = mine; x < total; x += 2) {
       const int i0 = (first + x % walk) * ROWS, turn = x >> 1 & 1;
       const float4* const lse_at = reinterpret_cast<const float4*>(shared + 7 * TILE + x % 3 * VECTOR);
@@ -604,11 +601,11 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       w.wait(dp_full + 8 * mine, turn);
       fence_after();
       u32 d[2][16];
-      tmem_load16(d[0], at);
+      tmem_load16(d[0], dp_at);
       wait_loads();
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        if (q < 7) tmem_load16(d[(q + 1) & 1], at + 16 * (q + 1));
+        if (q < 7) tmem_load16(d[(q + 1) & 1], dp_at + 16 * (q + 1));
         u32 out[8];
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
@@ -624,7 +621,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
           }
         }
         wait_loads();                // (dS goes over columns that have been read)
-        tmem_store8(at + 8 * q, out);
+        tmem_store8(ds_at + 8 * q, out);
       }
       wait_stores();
       fence_before();
@@ -686,13 +683,17 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       auto values = [&](int x) {                 // dV += P^T dO
         const int two = x & 1;
         const u32 d = do_ring + two * TILE;
-        w.wait(do_full + 8 * two, x >> 1 & 1);
-        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+        if (APART) {
+          w.wait(dp_full + 8 * two, x >> 1 & 1);           // (dP has read dO before, and cleared what is behind the end)
+        } else {
+          w.wait(do_full + 8 * two, x >> 1 & 1);
+          if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+        }
         w.wait(p_ready + 8 * two, x >> 1 & 1);
         fence_after();
         if (elected() && !w.dead) {
           multiply_across(tmem_dv, tmem + two * ROWS, d, ins, x > 0);
-          commit(dv_done + 8 * two);
+          commit((APART ? do_empty : dv_done) + 8 * two);
         }
         __syncwarp();
       };
@@ -701,17 +702,24 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
         w.wait(ds_ready + 8 * two, x >> 1 & 1);
         fence_after();
         if (elected() && !w.dead) {
-          multiply_across(tmem_dk, tmem + two * ROWS, q_ring + x % 3 * TILE, ins, x > 0);
+          multiply_across(tmem_dk, tmem + two * ROWS + (APART ? ROWS / 2 : 0), q_ring + x % 3 * TILE, ins, x > 0);
           commit(q_empty + 8 * (x % 3));
           if (x + 1 == total) commit(done);
         }
         __syncwarp();
       };
-      for (int x = 0; x < total; x += 2) {
-        values(x);
-        if (x + 1 < total) values(x + 1);
-        keys(x);
-        if (x + 1 < total) keys(x + 1);
+      if (APART) {
+        for (int x = 0; x < total; ++x) {
+          values(x);
+          keys(x);
+        }
+      } else {
+        for (int x = 0; x < total; x += 2) {
+          values(x);
+          if (x + 1 < total) values(x + 1);
+          keys(x);
+          if (x + 1 < total) keys(x + 1);
+        }
       }
     } else if (total > 0) {
       const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false);
@@ -722,34 +730,46 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
         if (x >= 2) w.wait(q_empty + 8 * ((x - 2) % 3), (x - 2) / 3 & 1);
         fence_after();
         if (elected() && !w.dead) {
-          if (TMEM) multiply_along_tmem<D>(tmem + (x & 1) * ROWS, tmem_k, q, ins_s);
-          else multiply_along<D>(tmem + (x & 1) * ROWS, k_tile, q, ins_s);
+          multiply_along<D>(tmem + (x & 1) * ROWS, k_tile, q, ins_s);
           commit(s_full + 8 * (x & 1));
         }
         __syncwarp();
       };
-      auto d_probabilities = [&](int x) {        // dP^T = V dO^T, over P^T
+      auto d_probabilities = [&](int x) {        // dP^T = V dO^T, over P^T or over dP^T of pair x - 1
         const int two = x & 1;
         const u32 d = do_ring + two * TILE;
-        w.wait(dv_done + 8 * two, x >> 1 & 1);
+        if (APART) {
+          w.wait(do_full + 8 * two, x >> 1 & 1);
+          if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+          if (x > 0) w.wait(ds_ready + 8 * (two ^ 1), (x - 1) >> 1 & 1);
+        } else {
+          w.wait(dv_done + 8 * two, x >> 1 & 1);
+        }
         fence_after();
         if (elected() && !w.dead) {
-          if (TMEM) multiply_along_tmem<D>(tmem + two * ROWS, tmem_v, d, ins_dp);
-          else multiply_along<D>(tmem + two * ROWS, v_tile, d, ins_dp);
+          multiply_along<D>(APART ? tmem_dp : tmem + two * ROWS, v_tile, d, ins_dp);
           commit(dp_full + 8 * two);
-          commit(do_empty + 8 * two);
+          if (!APART) commit(do_empty + 8 * two);
         }
         __syncwarp();
       };
-      w.wait(TMEM ? in_tmem : kv_full, 0);
+      w.wait(kv_full, 0);
       fence_after();
       scores(0);
       if (total > 1) scores(1);
-      for (int x = 0; x < total; x += 2) {
-        d_probabilities(x);
-        if (x + 1 < total) d_probabilities(x + 1);
-        if (x + 2 < total) scores(x + 2);
-        if (x + 3 < total) scores(x + 3);
+      if (APART) {
+        d_probabilities(0);
+        for (int x = 0; x < total; ++x) {
+          if (x + 1 < total) d_probabilities(x + 1);
+          if (x + 2 < total) scores(x + 2);
+        }
+      } else {
+        for (int x = 0; x < total; x += 2) {
+          d_probabilities(x);
+          if (x + 1 < total) d_probabilities(x + 1);
+          if (x + 2 < total) scores(x + 2);
+          if (x + 3 < total) scores(x + 3);
+        }
       }
     }
   } else {
