@@ -123,7 +123,7 @@ __device__ __forceinline__ void store_row(T* row, u32 from, bool any, bool there
 template <class T>
 __device__ __forceinline__ void clear_results(const ps_heads& h, int b, int head, int first, int rows, int len, int dim) {
   const int packs = dim / 8, n = max(0, min(rows, len - first)) * packs;
-  for (int i = threadIdx.x; i < n; i += THREADS) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const int r = i / packs;
     *reinterpret_cast<uint4*>(row_of<T>(h, b, first + r, head) + (i - r * packs) * 8) = make_uint4(0, 0, 0, 0);
   }
@@ -805,15 +805,28 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   }
 }
 
+// With heads of up to 64 a block has one group, one buffer and half of the tensor memory, and an SM has two such blocks:
+// they take turns like the groups of one, and one begins or ends while the other works.  (A block has 5 tiles of keys on average in six sequences
+// of 528 to 1475, 16 heads: the whole pass 177 us with 192 and 64 registers, 188 with one block of two groups; 8192 queries with 32 heads 1104 and
+// 1120.  184 registers spill in the group, and 200 leave too few to the warps that start products.)
+template <int D> struct QueryBlock {
+  static constexpr int groups = D == 64 ? 1 : 2, threads = 128 * (groups + 1), resident = 3 - groups, columns = 256 * groups;
+  static constexpr int launched = groups == 1 ? 128 : LAUNCHED, taken = groups == 1 ? 192 : BackwardRegisters::taken,
+                       left = (groups + 1) * launched - groups * taken;
+  static_assert(resident * threads * launched <= 65536, "registers that the blocks have");
+};
+
 // A block owns 128 queries of a head and walks the keys they see.  P stays in registers, so dP may be written over S as soon as S
 // has been read.  Tensor memory (D = 128): the two buffers, dQ, and Q and dO as left operands (from shared memory: 1512 us for the
 // whole pass then, 1487 so).  K has three slots, V two, as Q and dO above.  The same case: 0.67 ms, the tensor pipe
 // busy for 65 %.  A third buffer of scores, with Q and dO in shared memory again, took as long.
 template <class T, int D, bool CHUNKED>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(QueryBlock<D>::threads, QueryBlock<D>::resident)
 k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const Args a) {
   constexpr u32 TILE = PANEL * (D / 64);
+  typedef QueryBlock<D> Block;
+  constexpr int GROUPS = Block::groups, COPY_WARP = 4 * GROUPS, MMA_WARP = COPY_WARP + 1, MMA_WARP2 = COPY_WARP + 2;
   extern __shared__ __align__(1024) unsigned char shared[];
   const u32 q_tile = smem_address(shared), do_tile = q_tile + TILE, k_ring = do_tile + TILE, v_ring = k_ring + 3 * TILE;
   Shared& sh = *reinterpret_cast<Shared*>(shared + 7 * TILE);
@@ -834,7 +847,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     return;
   }
 
-  if (warp == MMA_WARP) tmem_alloc(smem_address(&sh.tmem_at), 512);
+  if (warp == MMA_WARP) tmem_alloc(smem_address(&sh.tmem_at), Block::columns);
   if (threadIdx.x == 0) {
     barrier_init(q_full, 1);
     for (int i = 0; i < 3; ++i) {
@@ -850,17 +863,17 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       barrier_init(ds_ready + 8 * i, 4);
     }
     barrier_init(done, 1);
-    barrier_init(in_tmem, 8);
+    barrier_init(in_tmem, 4 * GROUPS);
     fence_barrier_init();
   }
   fence_before();
   __syncthreads();
   fence_after();
-  const u32 tmem = sh.tmem_at, tmem_dq = tmem + 2 * ROWS, tmem_q = tmem_dq + D, tmem_do = tmem_q + D / 2;
+  const u32 tmem = sh.tmem_at, tmem_dq = tmem + GROUPS * ROWS, tmem_q = tmem_dq + D, tmem_do = tmem_q + D / 2;
   Waiter w(a.status);
 
   if (warp < COPY_WARP) {
-    take_registers<BackwardRegisters::taken>();
+    take_registers<Block::taken>();
     const int mine = warp / 4, i = q0 + threadIdx.x % ROWS, end = end_of(a, l, i) - key0;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
     const int masked = q0 + ROWS > l.n ? 0 : (end_of(a, l, q0) - key0) / ROWS;
@@ -870,11 +883,11 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     if (total > 0) {            // Q and dO are left operands of every pair
       w.wait(q_full, 0);
       if (mine == 0) tile_to_tmem<D>(tmem_q + lanes, q_tile);
-      else tile_to_tmem<D>(tmem_do + lanes, do_tile);
+      if (mine == GROUPS - 1) tile_to_tmem<D>(tmem_do + lanes, do_tile);
       if (lane == 0) barrier_arrive(in_tmem);
     }
-    for (int x = mine; x < total; x += 2) {
-      const int turn = x >> 1 & 1;
+    for (int x = mine; x < total; x += GROUPS) {
+      const int turn = x / GROUPS & 1;
       w.wait(s_full + 8 * mine, turn);
       fence_after();
       u32 p[4][32];
@@ -928,18 +941,19 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       w.wait(done, 0);
       fence_after();
     }
-    // each group stores half of the columns
+    // each group stores its share of the columns
+    constexpr int SHARE = D / GROUPS;
     const bool there = i < a.q_len;
     const int safe = min(i, a.q_len - 1);
     const float by = off == MINUS_INF ? 0.f : a.scale / factor * (Range<T>::small ? exp2_fast(-P_SHIFT) : 1.f);
-    const u32 from = tmem_dq + lanes + mine * (D / 2);
+    const u32 from = tmem_dq + lanes + mine * SHARE;
     if constexpr (CHUNKED) {
-      if (total > 0) store_part<D / 2>(a.parts + ((((u64)blockIdx.y * a.batch + b) * a.heads + h) * a.q_len + safe) * D + mine * (D / 2), from, there, by);
+      if (total > 0) store_part<SHARE>(a.parts + ((((u64)blockIdx.y * a.batch + b) * a.heads + h) * a.q_len + safe) * D + mine * SHARE, from, there, by);
     } else {
-      store_row<T, D / 2>(row_of<T>(a.d_q, b, safe, h) + mine * (D / 2), from, total > 0, there, a.dim - mine * (D / 2), by);
+      store_row<T, SHARE>(row_of<T>(a.d_q, b, safe, h) + mine * SHARE, from, total > 0, there, a.dim - mine * SHARE, by);
     }
   } else if (warp == COPY_WARP) {
-    give_registers<BackwardRegisters::left>();
+    give_registers<Block::left>();
     if (lane == 0 && total > 0) {
       barrier_expect(q_full, 2 * TILE);
       load_tile<D>(q_tile, &map_q, h, q0, b, q_full);
@@ -958,15 +972,15 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     }
   } else if (warp == MMA_WARP || warp == MMA_WARP2) {
     // (as in k_keys: one warp for the sum, the other for the products that fill the buffers)
-    give_registers<BackwardRegisters::left>();
+    give_registers<Block::left>();
     if (warp == MMA_WARP) {
       const u32 ins = instruction<T>(D, true, false);
       for (int x = 0; x < total; ++x) {          // dQ += dS K
-        const int two = x & 1;
-        w.wait(ds_ready + 8 * two, x >> 1 & 1);
+        const int at = x % GROUPS;
+        w.wait(ds_ready + 8 * at, x / GROUPS & 1);
         fence_after();
         if (elected() && !w.dead) {
-          multiply_across(tmem_dq, tmem + two * ROWS, k_ring + x % 3 * TILE, ins, x > 0);
+          multiply_across(tmem_dq, tmem + at * ROWS, k_ring + x % 3 * TILE, ins, x > 0);
           commit(k_empty + 8 * (x % 3));
           if (x + 1 == total) commit(done);
         }
@@ -976,45 +990,46 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       const u32 ins_s = instruction<T>(ROWS, false, a.scale < 0), ins_dp = instruction<T>(ROWS, false, false);
       // keys behind the sequence's end, in its last tile
       auto pad_from = [&](int x) { return l.m < a.k_len && key0 + (x + 1) * ROWS > l.m ? l.m - key0 - x * ROWS : ROWS; };
-      auto scores = [&](int x) {                 // S = Q K^T, over dS of pair x - 2
+      auto scores = [&](int x) {                 // S = Q K^T, over dS of pair x - GROUPS
         const u32 k = k_ring + x % 3 * TILE;
         w.wait(k_full + 8 * (x % 3), x / 3 & 1);
         if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
-        if (x >= 2) w.wait(k_empty + 8 * ((x - 2) % 3), (x - 2) / 3 & 1);
+        if (x >= GROUPS) w.wait(k_empty + 8 * ((x - GROUPS) % 3), (x - GROUPS) / 3 & 1);
         fence_after();
         if (elected() && !w.dead) {
-          multiply_along_tmem<D>(tmem + (x & 1) * ROWS, tmem_q, k, ins_s);
-          commit(s_full + 8 * (x & 1));
+          multiply_along_tmem<D>(tmem + x % GROUPS * ROWS, tmem_q, k, ins_s);
+          commit(s_full + 8 * (x % GROUPS));
         }
         __syncwarp();
       };
       auto d_probabilities = [&](int x) {        // dP = dO V^T, over S, which has been read
-        const int two = x & 1;
+        const int two = x & 1, at = x % GROUPS;
         const u32 v = v_ring + two * TILE;
         w.wait(v_full + 8 * two, x >> 1 & 1);
         if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
-        w.wait(s_read + 8 * two, x >> 1 & 1);
+        w.wait(s_read + 8 * at, x / GROUPS & 1);
         fence_after();
         if (elected() && !w.dead) {
-          multiply_along_tmem<D>(tmem + two * ROWS, tmem_do, v, ins_dp);
-          commit(dp_full + 8 * two);
+          multiply_along_tmem<D>(tmem + at * ROWS, tmem_do, v, ins_dp);
+          commit(dp_full + 8 * at);
           commit(v_empty + 8 * two);
         }
         __syncwarp();
       };
       w.wait(in_tmem, 0);
       fence_after();
-      scores(0);
-      if (total > 1) scores(1);
-      for (int x = 0; x < total; x += 2) {
-        d_probabilities(x);
-        if (x + 1 < total) d_probabilities(x + 1);
-        if (x + 2 < total) scores(x + 2);
-        if (x + 3 < total) scores(x + 3);
+      for (int x = 0; x < min(total, GROUPS); ++x) scores(x);
+      for (int x = 0; x < total; x += GROUPS) {
+#pragma unroll
+        for (int y = x; y < x + GROUPS; ++y)
+          if (y < total) d_probabilities(y);
+#pragma unroll
+        for (int y = x + GROUPS; y < x + 2 * GROUPS; ++y)
+          if (y < total) scores(y);
       }
     }
   } else {
-    give_registers<BackwardRegisters::left>();
+    give_registers<Block::left>();
   }
   linger(w.dead);
   wait_for_earlier();          // k_keys: this kernel ends behind it, as whatever follows in the stream expects
@@ -1022,7 +1037,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
   __syncthreads();
   if (warp == MMA_WARP) {
     fence_after();
-    tmem_free(tmem, 512);
+    tmem_free(tmem, Block::columns);
   }
 }
 
@@ -1180,15 +1195,15 @@ cudaError_t backward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
   }
   if (a.q_len) {
-    const u32 smem = smem_for(7, D, sizeof(Shared)), grid = (u32)(r.padded / ROWS) * a.heads * a.batch;
+    const u32 smem = D == 64 ? 7 * PANEL + sizeof(Shared) : smem_for(7, D, sizeof(Shared)), threads = QueryBlock<D>::threads, grid = (u32)(r.padded / ROWS) * a.heads * a.batch;
     static std::atomic<u64> allowed{0}, allowed_cut{0};
     if ((e = cut_keys ? allow(k_queries<T, D, true>, smem, allowed_cut) : allow(k_queries<T, D, false>, smem, allowed)) != cudaSuccess) return e;
     if (cut_keys) {
-      e = launch_next(k_queries<T, D, true>, dim3(grid, chunks_of(a.k_len)), THREADS, smem, stream, q, k, v, d, r);
+      e = launch_next(k_queries<T, D, true>, dim3(grid, chunks_of(a.k_len)), threads, smem, stream, q, k, v, d, r);
     } else if (a.k_len) {
-      e = launch_next(k_queries<T, D, false>, grid, THREADS, smem, stream, q, k, v, d, r);
+      e = launch_next(k_queries<T, D, false>, grid, threads, smem, stream, q, k, v, d, r);
     } else {
-      k_queries<T, D, false><<<grid, THREADS, smem, stream>>>(q, k, v, d, r);      // (no kernel is between it and the rows)
+      k_queries<T, D, false><<<grid, threads, smem, stream>>>(q, k, v, d, r);      // (no kernel is between it and the rows)
       e = cudaGetLastError();
     }
     if (e != cudaSuccess) return e;
