@@ -8,10 +8,10 @@
 // "Parallel Random Numbers: As Easy as 1, 2, 3", 2011) at the counter (g / 4, stream) under the
 // key seed; threshold = round(p * 2^32) and scale = 1 / (1 - p).
 //
-// What bounds it: bytes, two or three arrays.  65536 x 8192 in bfloat16 with a residual, 3.2 GB: 567 us, 5.7 TB/s (0.88 of a
-// copy's rate), issue slots taken for 56 %: a group of four words is 20 wide products and 20 exclusive-ors, and three to four elements
-// a cycle and SM pass at that rate.  12301 x 5003 floats in rows that begin anywhere, 0.49 GB: 114 us, 4.3 TB/s, issue slots
-// taken for 53 %: accesses of 4 bytes (a thread for each four elements, with accesses of their own: 148 to 151).
+// What bounds it: with a residual bytes, 65536 x 8192 in bfloat16, 3.2 GB: 528 us, 6.1 TB/s (0.94 of a copy's rate).  Without one the generator:
+// a group of four words is 20 wide products, of which an SM does 25 to 32 a cycle, and 20 exclusive-ors, 64 a cycle; 490 us where a copy takes 334.
+// Accesses of 32 bytes are fewer instructions: with 16 the two took 567 and 542 us.  12301 x 5003 floats in rows that begin anywhere, 0.49 GB:
+// 114 us, 4.3 TB/s, issue slots taken for 53 %: accesses of 4 bytes (a thread for each four elements, with accesses of their own: 148 to 151).
 #include "ps_train.cuh"
 
 namespace {
@@ -55,18 +55,24 @@ struct Keep {
   __device__ __forceinline__ float of(bool kept, float x, float add) const { return fmaf(kept ? x : 0.f, scale, add); }
 };
 
-constexpr int RESIDENT = 8;         // blocks of 256 threads on an SM
-// A thread takes N consecutive elements (16 bytes) at a time; rows, strides and the first element's index are such that packs
+// A thread takes N consecutive elements (16 or 32 bytes) at a time; rows, strides and the first element's index are such that packs
 // are aligned in memory and begin with a word 0.
+template <class T, int N> constexpr int PACK_BLOCKS = sizeof(T) * N == 32 ? 5 : 8;         // of 256 threads on an SM
 template <class T, int N, bool RESIDUAL>
-__global__ void __launch_bounds__(256, RESIDENT) k_packs(const DropoutArgs a, const __grid_constant__ Keys keys, u32 per_row, Divider by_row, u32 packs) {
+__global__ void __launch_bounds__(256, PACK_BLOCKS<T, N>) k_packs(const DropoutArgs a, const __grid_constant__ Keys keys, u32 per_row, Divider by_row, u32 packs) {
+  constexpr bool WIDE = sizeof(T) * N == 32;
   const Keep keep(a);
   for (u32 i = blockIdx.x * 256 + threadIdx.x; i < packs; i += gridDim.x * 256) {
     const u32 r = by_row.of(i);
     const u64 c = (u64)(i - r * per_row) * N, counter = (a.first + r * a.pitch + c) >> 2;
     Pack<T, N> x, y;
-    x.load((const T*)a.x + r * a.x_stride + c);
-    if (RESIDUAL) y.load((const T*)a.residual + r * a.residual_stride + c);
+    if constexpr (WIDE) {
+      x.load32((const T*)a.x + r * a.x_stride + c);
+      if (RESIDUAL) y.load32((const T*)a.residual + r * a.residual_stride + c);
+    } else {
+      x.load((const T*)a.x + r * a.x_stride + c);
+      if (RESIDUAL) y.load((const T*)a.residual + r * a.residual_stride + c);
+    }
     Words words[N / 4];
 #pragma unroll
     for (int q = 0; q < N / 4; ++q) words[q] = philox(counter + q, a.stream, keys);
@@ -76,7 +82,8 @@ __global__ void __launch_bounds__(256, RESIDENT) k_packs(const DropoutArgs a, co
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = keep.of(keep.kept(words[e / 4].w[e % 4]), v[e], RESIDUAL ? add[e] : 0.f);
     y.narrow(v);
-    y.store((T*)a.y + r * a.y_stride + c);
+    if constexpr (WIDE) y.store32((T*)a.y + r * a.y_stride + c);
+    else y.store((T*)a.y + r * a.y_stride + c);
   }
 }
 
@@ -133,10 +140,12 @@ cudaError_t dropout(DropoutArgs a, int sm_count, cudaStream_t stream) {
   }
   const bool packs = a.cols % N == 0 && a.first % 4 == 0 && a.pitch % 4 == 0 && packs_at(a.x, a.x_stride, N, sizeof(T)) &&
                      packs_at(a.y, a.y_stride, N, sizeof(T)) && (!RESIDUAL || packs_at(a.residual, a.residual_stride, N, sizeof(T)));
-  // a launch for up to 2^31 items: whole rows, or of a single row a part (2^32 elements, a multiple of N and of 4)
+  const bool wide = packs && a.cols % (2 * N) == 0 && aligned_rows(a.x, a.x_stride, sizeof(T), 32) && aligned_rows(a.y, a.y_stride, sizeof(T), 32) &&
+                    (!RESIDUAL || aligned_rows(a.residual, a.residual_stride, sizeof(T), 32));
+  // a launch for up to 2^31 items: whole rows, or of a single row a part (2^32 elements, a multiple of 2 N and of 4)
   const u64 part = (u64)1 << 32;
   const u64 cols = a.rows == 1 && a.cols > part ? part : a.cols;
-  const u64 per_row = packs ? cols / N : (cols + 3 + SPAN - 1) / SPAN;
+  const u64 per_row = packs ? cols / (wide ? 2 * N : N) : (cols + 3 + SPAN - 1) / SPAN;
   if (per_row > 0x7fffffffu) return cudaErrorInvalidValue;        // (cols above 2^32 in rows of a larger tensor are refused before)
   const u64 rows = 0x7fffffffu / per_row;
   const Keys keys(a.seed);
@@ -149,10 +158,11 @@ cudaError_t dropout(DropoutArgs a, int sm_count, cudaStream_t stream) {
       p.x = (const T*)a.x + r * a.x_stride + c;
       if (RESIDUAL) p.residual = (const T*)a.residual + r * a.residual_stride + c;
       p.y = (T*)a.y + r * a.y_stride + c;
-      const u32 n = packs ? (u32)(p.cols / N) : (u32)((p.cols + 3 + SPAN - 1) / SPAN), items = (u32)p.rows * n;
-      const u64 a_block = packs ? 256 : 8, blocks = (items + a_block - 1) / a_block, most = (u64)sm_count * (packs ? RESIDENT : RESIDENT_GROUPS);
+      const u32 n = packs ? (u32)(p.cols / (wide ? 2 * N : N)) : (u32)((p.cols + 3 + SPAN - 1) / SPAN), items = (u32)p.rows * n;
+      const u64 a_block = packs ? 256 : 8, blocks = (items + a_block - 1) / a_block, most = (u64)sm_count * (wide ? PACK_BLOCKS<T, 2 * N> : packs ? PACK_BLOCKS<T, N> : RESIDENT_GROUPS);
       const u32 grid = (u32)(blocks < most ? blocks : most);
-      if (packs) k_packs<T, N, RESIDUAL><<<grid, 256, 0, stream>>>(p, keys, n, Divider(n), items);
+      if (wide) k_packs<T, 2 * N, RESIDUAL><<<grid, 256, 0, stream>>>(p, keys, n, Divider(n), items);
+      else if (packs) k_packs<T, N, RESIDUAL><<<grid, 256, 0, stream>>>(p, keys, n, Divider(n), items);
       else k_groups<T, RESIDUAL><<<grid, 256, 0, stream>>>(p, keys, n, Divider(n), items);
       const cudaError_t e = cudaGetLastError();
       if (e != cudaSuccess) return e;

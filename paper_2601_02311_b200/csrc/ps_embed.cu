@@ -10,10 +10,11 @@
 // sum its list: every row of d_table is written once, every row of d_out read once.  A list of c tokens is cut
 // from its own beginning into pieces of 32 and pieces of 1024, which other blocks sum first; the warp adds the sums of
 // the pieces of 1024, then of the pieces of 32 behind them, then the rest: at most c / 1024 + 62 terms (below 4096 tokens
-// there are no pieces of 1024).  The cut follows from c alone, so a row's bits are the same whatever else the table holds.
+// in all there are no pieces of 1024).  The cut follows from c and the number of tokens, so a row's bits are the same whatever other rows the
+// table holds.
 //
-// What bounds them: bytes.  131072 lookups of 8192 bfloat16 in 128000 rows: 540 us, 5.2 TB/s by what has to move, 5.7 by what does (words of
-// middling frequency leave the L2 between two lookups).  The gradient of as many tokens into 256000 rows, 6.2 GB: 1.15 ms, 5.4 TB/s: 0.91 ms the
+// What bounds them: bytes.  131072 lookups of 8192 bfloat16 in 128000 rows: 494 us, 5.7 TB/s by what has to move (words of middling frequency
+// leave the L2 between two lookups and are read again).  The gradient of as many tokens into 256000 rows, 6.2 GB: 1.15 ms, 5.4 TB/s: 0.91 ms the
 // rows (5.9 TB/s), 0.16 the pieces, 0.04 the sort, whose kernels are small.  2048 tokens into 32000 rows of 768: 32 us, of which
 // 17 are the rows and 12 the two short kernels before them.
 #include "ps_train.cuh"
@@ -29,33 +30,42 @@ __device__ __forceinline__ u32 row_of(const EmbedArgs& a, u64 t) {
 }
 
 // ------------------------------------------------------------------ lookup
-// a warp takes LOADS packs a lane of a token's row at a time
-constexpr int LOOKUP_LOADS = 4, LOOKUP_BLOCKS = 4;
+// A warp takes LOADS packs a lane of a token's row at a time, of 32 bytes where all rows begin at multiples of that.  (131072 lookups of 8192
+// bfloat16 in 128000 rows: 494 us; with results that stay in the L2 506, with two packs 559, with four of 16 bytes 551.  More or fewer
+// blocks an SM take longer: 560 with five, 548 with three.)
+constexpr int LOOKUP_BLOCKS = 4;
+template <class T, int N> constexpr int LOOKUP_LOADS = sizeof(T) * N == 32 ? 1 : 4;
 template <class T, int N>
 __global__ void __launch_bounds__(256, LOOKUP_BLOCKS) k_lookup(EmbedArgs a, u32 chunks, Divider by_chunk, u32 items) {
+  constexpr bool WIDE = sizeof(T) * N == 32;
+  constexpr int LOADS = LOOKUP_LOADS<T, N>;
   const u32 lane = threadIdx.x % 32, step = gridDim.x * 8;
   u32 item = blockIdx.x * 8 + threadIdx.x / 32, next = item < items ? row_of(a, by_chunk.of(item)) : 0;
   for (; item < items; item += step) {
     const u32 t = by_chunk.of(item), row = next;
     if (item + step < items) next = row_of(a, by_chunk.of(item + step));        // (the next one's, ahead)
-    const u64 column = (u64)(item - t * chunks) * (32 * N * LOOKUP_LOADS) + lane * N;
-    Pack<T, N> v[LOOKUP_LOADS];
+    const u64 column = (u64)(item - t * chunks) * (32 * N * LOADS) + lane * N;
+    Pack<T, N> v[LOADS];
     const T* from = (const T*)a.table + row * a.table_stride + column;
 #pragma unroll
-    for (int i = 0; i < LOOKUP_LOADS; ++i) {
+    for (int i = 0; i < LOADS; ++i) {
       v[i].clear();
-      if (row < a.rows && column + i * 32 * N < a.dim) v[i].load(from + i * 32 * N);
+      if (row < a.rows && column + i * 32 * N < a.dim) {
+        if constexpr (WIDE) v[i].load32(from + i * 32 * N);
+        else v[i].load(from + i * 32 * N);
+      }
     }
     T* to = (T*)a.out + t * a.out_stride + column;
 #pragma unroll
-    for (int i = 0; i < LOOKUP_LOADS; ++i)
+    for (int i = 0; i < LOADS; ++i)
       if (column + i * 32 * N < a.dim) {
         float x[N];
         v[i].widen(x);
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = row < a.rows ? x[e] * a.scale : 0.f;
         v[i].narrow(x);
-        v[i].store_passing(to + i * 32 * N);
+        if constexpr (WIDE) v[i].store32_passing(to + i * 32 * N);
+        else v[i].store_passing(to + i * 32 * N);
       }
   }
 }
@@ -480,7 +490,7 @@ u32 grid_for(u32 items, int sm_count, int resident) {
 
 template <class T, int N>
 cudaError_t lookup(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
-  const u32 chunks = chunks_of(a.dim, 32 * N * LOOKUP_LOADS);
+  const u32 chunks = chunks_of(a.dim, 32 * N * LOOKUP_LOADS<T, N>);
   return in_parts(a.n_tokens, chunks, [&](u64 at, u32 count) {
     EmbedArgs part = a;
     part.tokens = (const char*)a.tokens + at * a.token_bytes;
@@ -579,6 +589,8 @@ cudaError_t gradient(u32 grad_dtype, const EmbedArgs& a, int sm_count, cudaStrea
 template <class T>
 cudaError_t lookup(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   constexpr int N = 16 / sizeof(T);
+  if (a.dim % (2 * N) == 0 && aligned_rows(a.out, a.out_stride, sizeof(T), 32) && aligned_rows(a.table, a.table_stride, sizeof(T), 32))
+    return lookup<T, 2 * N>(a, sm_count, stream);
   if (a.dim % N == 0 && packs_at(a.out, a.out_stride, N, sizeof(T)) && packs_at(a.table, a.table_stride, N, sizeof(T)))
     return lookup<T, N>(a, sm_count, stream);
   return lookup<T, 1>(a, sm_count, stream);

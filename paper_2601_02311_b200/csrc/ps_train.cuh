@@ -17,7 +17,8 @@ template <> __device__ __forceinline__ float narrow<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half narrow<__half>(float v) { return __float2half_rn(v); }
 
-// N consecutive elements in the 32-bit words that they were loaded as, by accesses of up to 16 bytes
+// N consecutive elements in the 32-bit words that they were loaded as, by accesses of up to 16 bytes (load, store) or of
+// 32 (load32, store32: the address is a multiple of it)
 template <class T, int N>
 struct Pack {
   static constexpr int WORDS = (N * (int)sizeof(T) + 3) / 4;
@@ -60,7 +61,24 @@ struct Pack {
       for (int i = 0; i < WORDS; ++i) reinterpret_cast<u32*>(p)[i] = w[i];
     }
   }
+  __device__ __forceinline__ void load32(const T* p) {
+    static_assert(WORDS == 8, "32 bytes");
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p));
+  }
+  __device__ __forceinline__ void store32(T* p) const {
+    static_assert(WORDS == 8, "32 bytes");
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  }
   // for results that this kernel does not read again: they are the first to leave the L2
+  __device__ __forceinline__ void store32_passing(T* p) const {
+    static_assert(WORDS == 8, "32 bytes");
+    asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+  }
   __device__ __forceinline__ void store_passing(T* p) const {
     if (WORDS % 4 == 0) {
 #pragma unroll
@@ -124,10 +142,14 @@ cudaError_t launch_next(void (*kernel)(Parameters...), dim3 grid, u32 threads, u
   return cudaLaunchKernelEx(&config, kernel, Parameters(arguments)...);
 }
 
+// whether `p` and rows `stride` elements apart begin at multiples of `bytes`
+inline bool aligned_rows(const void* p, u64 stride, size_t width, size_t bytes) {
+  return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (stride * width) % bytes == 0;
+}
 // whether packs of n elements may be used at `p` and at rows `stride` elements apart
 inline bool packs_at(const void* p, u64 stride, int n, size_t width) {
   const size_t bytes = n * width < 16 ? n * width : 16;
-  return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (stride * width) % bytes == 0;
+  return aligned_rows(p, stride, width, bytes);
 }
 
 // n / d for n < 2^31 by a product and a shift: with 2^(s - 1) < d <= 2^s and m = ceil(2^(31 + s) / d), n m 2^-(31 + s)

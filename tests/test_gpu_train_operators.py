@@ -117,6 +117,27 @@ def test_dropout_of_rows_in_a_larger_tensor(ctx, dtype, offset, stride):
     assert torch.equal(y[:, :offset], before[:, :offset]) and torch.equal(y[:, offset + 130:], before[:, offset + 130:])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("nth", [0, 1, 2])
+@pytest.mark.parametrize("offset, stride, cols", [(32, 96, 64), (16, 80, 64), (48, 96, 48), (32, 96, 40), (4, 96, 64)])
+def test_dropout_at_every_alignment_of_one_tensor(ctx, dtype, nth, offset, stride, cols):
+    """Rows of one of the three tensors begin `offset` bytes behind a multiple of 64, `stride` elements apart: accesses of 32 bytes, of
+    16 or of an element."""
+    gen = torch.Generator("cuda").manual_seed(offset + cols)
+    whole = [normal(gen, 5, 128, dtype=TYPES[dtype]) for _ in range(3)]
+    at = offset // whole[0].element_size()
+    part = [t.view(-1).as_strided((5, cols), (stride if i == nth else 128, 1), at if i == nth else 0) for i, t in enumerate(whole)]
+    before = whole[2].clone()
+    want, _, bound = dropout_want(part[0], 0.2, 5, 1, part[1], 4, 96)
+    ctx.dropout_into(part[0], part[2], 0.2, 5, stream=1, residual=part[1], first=4, pitch=96)
+    ctx.check_status()
+    within(part[2], want, bound)
+    # what lies around y's rows is as it was
+    rest = torch.ones(5 * 128, dtype=torch.bool, device="cuda")
+    rest.as_strided((5, cols), part[2].stride(), part[2].storage_offset()).zero_()
+    assert torch.equal(whole[2].view(-1)[rest], before.view(-1)[rest])
+
+
 def test_dropout_in_place_and_of_broadcast_rows(ctx):
     gen = torch.Generator("cuda").manual_seed(1)
     x, res = normal(gen, 10, 72, dtype=torch.bfloat16), normal(gen, 10, 72, dtype=torch.bfloat16)
@@ -186,6 +207,28 @@ def test_lookup(ctx, dtype, token_type, tokens, rows, dim, first_row):
     ctx.check_status()
     # the scale and the product rounded to float32, the result to its type
     within(got, want, u_of(table.dtype) * want.abs() + tiny_of(table.dtype) + 3 * F * want.abs())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("of_table", [False, True])
+@pytest.mark.parametrize("offset, stride, dim", [(32, 160, 128), (16, 160, 128), (32, 136, 128), (32, 160, 72), (64, 1088, 1040), (4, 160, 128)])
+def test_lookup_at_every_alignment(ctx, dtype, of_table, offset, stride, dim):
+    """The table's or the result's rows begin `offset` bytes behind a multiple of 64: accesses of 32 bytes, of 16 or of an element."""
+    gen = torch.Generator("cuda").manual_seed(offset + dim)
+    table, out = normal(gen, 40, 1152, dtype=TYPES[dtype]), normal(gen, 60, 1152, dtype=TYPES[dtype])
+    at = offset // table.element_size()
+    t = table.view(-1).as_strided((40, dim), (stride if of_table else 1152, 1), at if of_table else 0)
+    o = out.view(-1).as_strided((60, dim), (1152 if of_table else stride, 1), 0 if of_table else at)
+    ids = torch.randint(-1, 42, (60,), device="cuda", generator=gen)
+    held = (ids >= 0) & (ids < 40)
+    want = t[ids.clamp(0, 39)].double() * 1.7 * held[:, None]
+    before = out.clone()
+    ctx.embed_forward_into(t, ids, o, 1.7)
+    ctx.check_status()
+    within(o, want, u_of(table.dtype) * want.abs() + tiny_of(table.dtype) + 3 * F * want.abs())
+    rest = torch.ones(60 * 1152, dtype=torch.bool, device="cuda")
+    rest.as_strided((60, dim), o.stride(), o.storage_offset()).zero_()
+    assert torch.equal(out.view(-1)[rest], before.view(-1)[rest])
 
 
 def gradient_want(d_out, ids, rows, scale, first_row, dtype):
