@@ -5,9 +5,9 @@
 //
 // Sums are held in 32 bits and rounded once.
 //
-// The gradient sorts (row, t) by row with t ascending (a stable radix sort of row numbers alone, so nothing is left to the
-// order in which blocks run), marks where each row's list begins and ends, and gives each row of the table to warps that
-// sum its list: every row of d_table is written once, every row of d_out read once.  A list of c tokens is cut
+// The gradient sorts (row, t) by row with t ascending (a stable radix sort of row numbers alone, or for few tokens a count, so nothing is left
+// to the order in which blocks run), marks where each row's list begins and ends, and gives each row of the table to warps that
+// sum its list: every row of d_table is written once (by few tokens twice where it has some), every row of d_out read once.  A list of c tokens is cut
 // from its own beginning into pieces of 32 and pieces of 1024, which other blocks sum first; the warp adds the sums of
 // the pieces of 1024, then of the pieces of 32 behind them, then the rest: at most c / 1024 + 62 terms (below 4096 tokens
 // in all there are no pieces of 1024).  The cut follows from c and the number of tokens, so a row's bits are the same whatever other rows the
@@ -15,8 +15,8 @@
 //
 // What bounds them: bytes.  131072 lookups of 8192 bfloat16 in 128000 rows: 494 us, 5.7 TB/s by what has to move (words of middling frequency
 // leave the L2 between two lookups and are read again).  The gradient of as many tokens into 256000 rows, 6.2 GB: 1.15 ms, 5.4 TB/s: 0.91 ms the
-// rows (5.9 TB/s), 0.16 the pieces, 0.04 the sort, whose kernels are small.  2048 tokens into 32000 rows of 768: 32 us, of which
-// 17 are the rows and 12 the two short kernels before them.
+// rows (5.9 TB/s), 0.16 the pieces, 0.04 the sort, whose kernels are small.  2048 tokens into 32000 rows of 768: 18.8 us, a
+// chain of three kernels of which the first writes the 49 MB of zeros.
 #include "ps_train.cuh"
 
 namespace {
@@ -212,15 +212,47 @@ __global__ void __launch_bounds__(256) k_mark(const u32* keys, u32 n, uint2* ran
 // Few tokens need no passes: a token's place is the number of smaller rows before or behind it plus the number of equal ones before it, and
 // its row's list begins behind the smaller ones.  A warp counts for a token, over all rows in shared memory: n^2 comparisons on all
 // SMs (2048 tokens: 6 us, most of it launch and loads, where one block's radix passes took 11).
+//
+// Few tokens leave most rows of the table without any.  Blocks behind those that count write zeros to all rows meanwhile, and
+// the rows that have tokens are written again by k_lists.  (2048 tokens into 32000 rows of 768: 18.8 us in a loop, 27.6 with the L2 flushed
+// before; 23.8 and 33.8 with k_gradient over all rows behind the places, and an array of lists to clear.  8192 into 128000 rows of 4096:
+// 250 and 253, into 300 of 1024: 71 and 93, into 8000: 70 and 68.)
 constexpr u32 RANK_MOST = 8192;
-__global__ void __launch_bounds__(256) k_rank(EmbedArgs a, u32 n, u32* keys, u32* places, uint2* ranges) {
+struct Fill {
+  char* table;                 // null: nothing is to be cleared
+  u64 units, stride;           // of a row: accesses of WIDTH bytes, and bytes from one to the next
+  u32 rows;
+};
+template <int WIDTH> struct Unit { typedef uint4 type; };
+template <> struct Unit<4> { typedef u32 type; };
+template <> struct Unit<2> { typedef unsigned short type; };
+template <int WIDTH>
+__device__ __forceinline__ void fill(const Fill& f, u32 block, u32 blocks) {
+  typedef typename Unit<WIDTH>::type U;
+  // a row of so many accesses, or a part of it, to a block at a time
+  constexpr u32 PART = 256 * 8;
+  const u64 parts = (f.units + PART - 1) / PART;
+  for (u64 i = block; i < f.rows * parts; i += blocks) {
+    const u64 r = parts == 1 ? i : i / parts, first = (i - r * parts) * PART;
+    U* const at = reinterpret_cast<U*>(f.table + r * f.stride) + first;
+#pragma unroll
+    for (u32 e = 0; e < 8; ++e)
+      if (first + e * 256 + threadIdx.x < f.units) at[e * 256 + threadIdx.x] = U{};
+  }
+}
+template <int WIDTH>
+__global__ void __launch_bounds__(256) k_rank(EmbedArgs a, u32 n, u32* keys, u32* places, uint2* ranges, u32 counting, Fill f) {
   extern __shared__ uint4 rows4[];
   u32* const rows = reinterpret_cast<u32*>(rows4);
   let_next_begin();
+  if (blockIdx.x >= counting) {
+    fill<WIDTH>(f, blockIdx.x - counting, gridDim.x - counting);
+    return;
+  }
   const u32 lane = threadIdx.x % 32, fours = (n + 3) / 4;
   for (u32 i = threadIdx.x; i < fours * 4; i += 256) rows[i] = i < n ? row_of(a, i) : 0xffffffffu;
   __syncthreads();
-  for (u32 t = blockIdx.x * 8 + threadIdx.x / 32; t < n; t += gridDim.x * 8) {
+  for (u32 t = blockIdx.x * 8 + threadIdx.x / 32; t < n; t += counting * 8) {
     const u32 key = rows[t];
     u32 less = 0, same = 0, before = 0;
     for (u32 i = lane; i < fours; i += 32) {
@@ -353,6 +385,44 @@ __global__ void __launch_bounds__(256, PIECE_BLOCKS) k_pieces2(EmbedArgs a, Grad
   }
 }
 
+// The gradient of one row, from `column` on (of which `columns` are left): its list is the places [at, end).
+template <class T, class G, int N, int LOADS, int AHEAD>
+__device__ __forceinline__ void write_row(const EmbedArgs& a, const GradientArgs& g, u32 at, u32 end, u64 column, s64 columns, G* to) {
+  const u32 lane = threadIdx.x % 32, count = end - at;
+  Sum<N, LOADS> sum;
+  if (count >= PIECE) {
+    if (g.sums2 && count >= PIECE2) {
+      const u32 pieces = count / PIECE2;
+      sum.template add_rows<2>(g.sums2 + column, g.width, pieces, columns, [&](u32 q) { return at / PIECE2 + q; });
+      at += pieces * PIECE2;
+    }
+    const u32 pieces = (end - at) / PIECE;
+    sum.template add_rows<2>(g.sums + column, g.width, pieces, columns, [&](u32 q) { return at / PIECE + q; });
+    at += pieces * PIECE;
+  }
+  if (at < end) {
+    const u32 place = at + lane < end ? g.places[at + lane] : 0;
+    sum.template add_rows<AHEAD>((const T*)a.out + column, a.out_stride, end - at, columns,
+                              [&](u32 q) { return __shfl_sync(0xffffffffu, place, q); });
+  }
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i)
+    if (i * 32 * N < columns) {
+      Pack<G, N> p;
+      float x[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = 0.f;
+      if (a.accumulate) {
+        p.load(to + i * 32 * N);
+        p.widen(x);
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = a.accumulate ? fmaf(sum.v[i][e], a.scale, x[e]) : sum.v[i][e] * a.scale;
+      p.narrow(x);
+      p.store(to + i * 32 * N);
+    }
+}
+
 // A warp takes GROUP rows, LOADS packs a lane of each: their lists' bounds come in one load, so that rows without tokens, often
 // most of them, are a store each and nothing is waited for.
 template <class T, class G, int N, int GROUP, int LOADS, int AHEAD, int BLOCKS>
@@ -374,9 +444,8 @@ __global__ void __launch_bounds__(256, BLOCKS) k_gradient(EmbedArgs a, GradientA
     G* to = (G*)a.table + first * a.table_stride + column;
 #pragma unroll 1
     for (u32 r = 0; r < rows; ++r, to += a.table_stride) {
-      u32 at = __shfl_sync(0xffffffffu, ranges.x, r);
-      const u32 end = __shfl_sync(0xffffffffu, ranges.y, r), count = end - at;
-      if (count == 0) {
+      const u32 at = __shfl_sync(0xffffffffu, ranges.x, r), end = __shfl_sync(0xffffffffu, ranges.y, r);
+      if (at == end) {
         if (!a.accumulate) {
           Pack<G, N> zero;
           zero.clear();
@@ -386,43 +455,27 @@ __global__ void __launch_bounds__(256, BLOCKS) k_gradient(EmbedArgs a, GradientA
         }
         continue;
       }
-      Sum<N, LOADS> sum;
-      if (count >= PIECE) {
-        if (g.sums2 && count >= PIECE2) {
-          const u32 pieces = count / PIECE2;
-          sum.template add_rows<2>(g.sums2 + column, g.width, pieces, columns, [&](u32 q) { return at / PIECE2 + q; });
-          at += pieces * PIECE2;
-        }
-        const u32 pieces = (end - at) / PIECE;
-        sum.template add_rows<2>(g.sums + column, g.width, pieces, columns, [&](u32 q) { return at / PIECE + q; });
-        at += pieces * PIECE;
-      }
-      if (at < end) {
-        const u32 place = at + lane < end ? g.places[at + lane] : 0;
-        sum.template add_rows<AHEAD>((const T*)a.out + column, a.out_stride, end - at, columns,
-                                  [&](u32 q) { return __shfl_sync(0xffffffffu, place, q); });
-      }
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        if (i * 32 * N < columns) {
-          Pack<G, N> p;
-          float x[N];
-#pragma unroll
-          for (int e = 0; e < N; ++e) x[e] = 0.f;
-          if (a.accumulate) {
-            p.load(to + i * 32 * N);
-            p.widen(x);
-          }
-#pragma unroll
-          for (int e = 0; e < N; ++e) x[e] = a.accumulate ? fmaf(sum.v[i][e], a.scale, x[e]) : sum.v[i][e] * a.scale;
-          p.narrow(x);
-          p.store(to + i * 32 * N);
-        }
+      write_row<T, G, N, LOADS, AHEAD>(a, g, at, end, column, columns, to);
     }
   }
 }
 
+// The rows that have tokens alone: a warp takes the place where a row's list begins, and leaves the others.
+constexpr int LIST_BLOCKS = 5;
+template <class T, class G, int N>
+__global__ void __launch_bounds__(256, LIST_BLOCKS) k_lists(EmbedArgs a, GradientArgs g, u32 chunks, Divider by_chunk, u32 items) {
+  wait_for_earlier();
+  const u32 step = gridDim.x * 8;
+  for (u32 item = blockIdx.x * 8 + threadIdx.x / 32; item < items; item += step) {
+    const u32 place = by_chunk.of(item), key = g.keys[place];
+    if (key >= a.rows || (place > 0 && g.keys[place - 1] == key)) continue;
+    const u64 column = (u64)(item - place * chunks) * (32 * N) + threadIdx.x % 32 * N;
+    write_row<T, G, N, 1, 4>(a, g, place, g.ranges[key].y, column, (s64)a.dim - (s64)column, (G*)a.table + key * a.table_stride + column);
+  }
+}
+
 // ------------------------------------------------------------------ host
+constexpr int FILL_BLOCKS = 8;
 constexpr u64 SMALL_TABLE = (u64)1 << 25;
 u32 chunks_of(u64 dim, int columns) { return (u32)((dim + columns - 1) / columns); }
 // columns of a row of sums, for every size of packs
@@ -516,6 +569,20 @@ cudaError_t write_rows(const EmbedArgs& a, const GradientArgs& g, int sm_count, 
   return e != cudaSuccess ? e : e2;
 }
 
+// The places and lists of few tokens, and zeros in the whole table
+template <class G>
+cudaError_t rank(const EmbedArgs& a, const Work& w, u32 n, int sm_count, cudaStream_t stream) {
+  const u32 counting = grid_for(n, sm_count, 4), shared = (n + 3) / 4 * 16;
+  const bool one = a.table_stride == a.dim, wide = aligned_rows(a.table, one ? a.rows * a.dim : a.table_stride, sizeof(G), 16) && (one || a.dim * sizeof(G) % 16 == 0);
+  const u64 width = wide ? 16 : sizeof(G), bytes = (one ? a.rows * a.dim : a.dim) * sizeof(G);
+  Fill f = {a.accumulate ? nullptr : (char*)a.table, bytes / width, a.table_stride * sizeof(G), one ? 1 : (u32)a.rows};
+  const u64 parts = f.rows * ((f.units + 2047) / 2048), most = (u64)sm_count * FILL_BLOCKS;
+  const u32 grid = counting + (f.table ? (u32)(parts < most ? parts : most) : 0);
+  if (wide) k_rank<16><<<grid, 256, shared, stream>>>(a, n, w.keys[0], w.values[0], w.ranges, counting, f);
+  else k_rank<sizeof(G)><<<grid, 256, shared, stream>>>(a, n, w.keys[0], w.values[0], w.ranges, counting, f);
+  return cudaGetLastError();
+}
+
 template <class T, class G, int N>
 cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   cudaError_t e;
@@ -526,12 +593,11 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
   const Work w = work_of(a);
   if (g.n) {
     SortArgs s = sort_plan(a);
-    if ((e = cudaMemsetAsync(w.ranges, 0, 8 * a.rows, stream)) != cudaSuccess) return e;
     s.counts = w.counts;
     if (g.n <= RANK_MOST) {
-      k_rank<<<grid_for(g.n, sm_count, 4), 256, (g.n + 3) / 4 * 16, stream>>>(a, g.n, w.keys[0], w.values[0], w.ranges);
-      if ((e = cudaGetLastError()) != cudaSuccess) return e;
+      if ((e = rank<G>(a, w, g.n, sm_count, stream)) != cudaSuccess) return e;
     } else {
+      if ((e = cudaMemsetAsync(w.ranges, 0, 8 * a.rows, stream)) != cudaSuccess) return e;
       for (u32 pass = 0; pass < s.passes; ++pass) {
         const int to = (s.passes - 1 - pass) & 1;
         s.shift = pass * s.bits;
@@ -566,6 +632,10 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
     const u32 chunks = chunks_of(g.width, 128), items = g.n / PIECE2 * chunks;
     if ((e = launch_next(k_pieces2, grid_for(items, sm_count, PIECE_BLOCKS), 256, 0, stream, a, g, chunks, Divider(chunks), items)) != cudaSuccess)
       return e;
+  }
+  if (g.n && g.n <= RANK_MOST) {
+    const u32 chunks = chunks_of(a.dim, 32 * N);       // (up to 2^15, for up to 2^13 places)
+    return launch_next(k_lists<T, G, N>, grid_for(g.n * chunks, sm_count, LIST_BLOCKS), 256, 0, stream, a, g, chunks, Divider(chunks), g.n * chunks);
   }
   // (32000 rows of 768: 33.8 us with 256 columns a warp, 37.9 with 512; 256000 rows of 8192: 1225 and 1194; alike between 2^26 and
   // 2^30 elements)
