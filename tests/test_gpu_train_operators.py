@@ -138,6 +138,28 @@ def test_dropout_at_every_alignment_of_one_tensor(ctx, dtype, nth, offset, strid
     assert torch.equal(whole[2].view(-1)[rest], before.view(-1)[rest])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("alike", [True, False])
+@pytest.mark.parametrize("cols, first, offset", [(1, 0, 1), (2, 3, 3), (15, 1, 7), (127, 2, 0), (505, 1, 3), (508, 0, 1), (509, 3, 0), (1013, 2, 5), (1531, 1, 6),
+                                                 (2040, 3, 2)])
+def test_dropout_of_rows_that_begin_anywhere(ctx, dtype, alike, cols, first, offset):
+    """Rows at every distance from a multiple of 16 bytes, the same in all tensors or another in the residual."""
+    gen = torch.Generator("cuda").manual_seed(cols)
+    stride = cols + 9 - cols % 2
+    whole = [normal(gen, 6 * stride + 32, dtype=TYPES[dtype]) for _ in range(3)]
+    part = [t.as_strided((6, cols), (stride, 1), offset + (0 if alike or i != 1 else 3)) for i, t in enumerate(whole)]
+    before = whole[2].clone()
+    want, _, bound = dropout_want(part[0], 0.3, 11, 2, part[1], first, 4 * cols + 1)
+    ctx.dropout_into(part[0], part[2], 0.3, 11, stream=2, residual=part[1], first=first, pitch=4 * cols + 1)
+    ctx.check_status()
+    within(part[2], want, bound)
+    rest = torch.ones_like(whole[2], dtype=torch.bool)
+    rest.as_strided((6, cols), (stride, 1), offset).zero_()
+    assert torch.equal(whole[2][rest], before[rest])
+    ctx.dropout_into(part[0], part[0], 0.3, 11, stream=2, residual=part[1], first=first, pitch=4 * cols + 1)
+    assert torch.equal(part[0], part[2])
+
+
 def test_dropout_in_place_and_of_broadcast_rows(ctx):
     gen = torch.Generator("cuda").manual_seed(1)
     x, res = normal(gen, 10, 72, dtype=torch.bfloat16), normal(gen, 10, 72, dtype=torch.bfloat16)
