@@ -101,6 +101,7 @@ _DROPOUT_DESC = struct.Struct("9QdII").pack
 _EMBED_DESC = struct.Struct("6Qd4I").pack
 _HEADS = struct.Struct("4Q").pack
 _ATTENTION_SHAPE = struct.Struct("8IfI").pack
+_FLOAT_MOST = torch.finfo(torch.float32).max
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # PS_F32, PS_BF16, PS_F16
 
 
@@ -453,6 +454,8 @@ class Context:
         if lse.dtype != torch.float32 or lse.shape != (batch, heads, q_len) or lse.get_device() != self.device \
                 or not lse.is_contiguous():
             self._refuse(E_RANGE, where, f"lse has to be contiguous float32 [batch, heads, q_len] on device {self.device}")
+        if scale is not None and not -_FLOAT_MOST <= scale <= _FLOAT_MOST:
+            self._refuse(E_RANGE, where, "scale")
         shape = _ATTENTION_SHAPE(batch, q_len, k_len, heads, kv_heads, dim, _DTYPE[q.dtype], 1 if causal else 0,
                                  (dim or 1) ** -0.5 if scale is None else scale, 0)
         return (shape, queries, (batch, k_len, kv_heads, dim), None if q_lens is None else q_lens.data_ptr(),

@@ -209,3 +209,10 @@ def test_binding_refuses_shapes_types_and_strides(ctx):
     refused(ps.E_RANGE, ctx.attention_forward_into, q, k, k, q, lse, q_lens=torch.zeros(2))
     refused(ps.E_RANGE, ctx.attention_forward_into, q, k, k, q, lse, k_lens=torch.zeros(3, dtype=torch.int32))
     refused(ps.E_ALIGN, ctx.attention_forward_into, q, k, k, torch.zeros(2, 5, 4, 32, dtype=torch.bfloat16)[..., ::2], lse)
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e39, math.inf, math.nan])
+def test_binding_refuses_a_scale_that_is_no_float(ctx, scale):
+    q, k = torch.zeros(2, 5, 4, 16, dtype=torch.bfloat16), torch.zeros(2, 6, 2, 16, dtype=torch.bfloat16)
+    refused(ps.E_RANGE, ctx.attention_forward_into, q, k, k, q, torch.zeros(2, 4, 5), scale=scale)
+    refused(ps.E_RANGE, ctx.attention_backward_into, q, k, k, q, torch.zeros(2, 4, 5), q, q, k, k, scale=scale)
