@@ -77,9 +77,9 @@ __device__ __forceinline__ int first_query_tile(const Args& a, Lengths l, int j)
 
 // A block of few rows would walk a long axis alone: at up to FEW rows of one side and more than two chunks of the other, blocks take
 // a chunk of CHUNK tiles each.  The rule looks at the two lengths alone, so that a sequence's bits do not depend on how many
-// others there are.
+// others there are.  (Without rows there is nothing to cut, and nothing to join.)
 constexpr int FEW = 2 * ROWS, CHUNK = 16;
-__host__ __device__ constexpr bool chunked(int rows, int along) { return rows <= FEW && along > 2 * CHUNK * ROWS; }
+__host__ __device__ constexpr bool chunked(int rows, int along) { return rows > 0 && rows <= FEW && along > 2 * CHUNK * ROWS; }
 __host__ __device__ constexpr int chunks_of(int along) { return (along + CHUNK * ROWS - 1) / (CHUNK * ROWS); }
 
 // 32 columns of a row of results, times `by`, to memory; columns behind dim are not there
