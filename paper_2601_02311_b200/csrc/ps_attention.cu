@@ -156,12 +156,24 @@ __device__ __forceinline__ void linger(bool dead) {
     for (int i = 0; i < 20; ++i) __nanosleep(1000000);
 }
 
+// Half precision has 2^-24 as its smallest number, and probabilities and gradients go below it.  P is held larger there, by
+// 2^FORWARD_SHIFT in the forward pass and 2^P_SHIFT in the backward pass.  bfloat16 has float's exponents and needs nothing of the kind.
+template <class T> struct Range { static constexpr bool small = false; };
+template <> struct Range<__half> { static constexpr bool small = true; };
+constexpr int FORWARD_SHIFT = 7, P_SHIFT = 12;
+
 // ------------------------------------------------------------------ forward
 // A block owns two tiles of 128 queries of a head, a group of warps each, a thread a query.  While one group takes the
 // exponentials of its scores the tensor cores work for the other.  A group's turn: the scores S = Q K^T (128 columns of
 // tensor memory), their row maximum, P = 2^(c S - c maximum) written over S in 16 bits, O += P V, begun when half of P is there.
 // O is rescaled only when a row's maximum has grown by more than a factor of 2^8: until then P is larger than 1 by up
 // to that, which the 32-bit sums and the types' exponents hold, and lse comes from the same maximum.
+//
+// In half precision P and its sum are both held 2^7 times as large, which with the 2^8 just fits: a probability keeps its 11 bits down to
+// 2^-21 of the row's largest and is lost below 2^-32 of it; as it is, 2^-14 and 2^-25.  (2000 keys 14 below a key whose value is zero: out
+// is off by 3.5e-3 as it is, and by its rounding with this; 16.5 below: 0.13 and 3e-3.  A factor of 2^9 leaves 2^6 until O is rescaled: 412 us instead
+// of 391 with 8192 queries, 32 heads of 64 and scores of deviation 3; of 2^12 leaves 2^3: 426.)  Not so for scores of 2^20 and more, to
+// base 2: the exponent of the largest is then off by as much as float32 rounds it, which would take P out of the type earlier.
 //
 // A product that writes tensor memory waits for the end of the one that reads it (S over P): nothing else orders products with
 // different sums.  What bounds it, 8192 queries, 32 heads of 128 on 8 key heads, causal: 453 us, 1.21 PFLOP/s, the
@@ -221,6 +233,8 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     // the first tile of keys of which some query of this tile does not see all
     const int masked = q0 + (t + 1) * ROWS > l.n ? 0 : (end_of(a, l, q0 + t * ROWS) - key0) / ROWS;
     const float slack = 8.f / a.c;
+    // the power of two that P is held larger by, for a reference score
+    const auto shift_of = [&](float most) { return Range<T>::small && fabsf(most * a.c) < 0x1p20f ? (float)FORWARD_SHIFT : 0.f; };
     const int count = t ? count1 : count0;
     float most_s = MINUS_INF, total = 0.f;
     if (TMEM && count) {
@@ -251,7 +265,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
       const bool grown = now > most_s + slack;
       if (__any_sync(0xffffffffu, grown)) {
-        const float by = grown ? exp2_fast((most_s - now) * a.c) : 1.f;
+        const float by = grown ? exp2_fast((most_s - now) * a.c + (shift_of(now) - shift_of(most_s))) : 1.f;
         if (grown) most_s = now;
         total *= by;
         if (j > 0) {           // (the product that wrote O last is done: S, which was started behind its end, is there)
@@ -266,7 +280,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
           }
         }
       }
-      const float off = most_s == MINUS_INF ? 0.f : -most_s * a.c;
+      const float off = most_s == MINUS_INF ? 0.f : fmaf(-most_s, a.c, shift_of(most_s));
       const u64 offs = pair(off, off), cs = pair(a.c, a.c);
       u64 sum[2] = {0, 0};
 #pragma unroll
@@ -295,7 +309,8 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     }
     const bool there = i < a.q_len, none = most_s == MINUS_INF && total == 0.f;
     const int safe = min(i, a.q_len - 1);
-    const float lse = none ? MINUS_INF : (most_s * a.c + log2f(total)) * LN2, by = none ? 0.f : 1.f / total;
+    const float lse = none ? MINUS_INF : (most_s * a.c + log2f(Range<T>::small ? total * exp2_fast(-shift_of(most_s)) : total)) * LN2,
+                by = none ? 0.f : 1.f / total;
     if constexpr (CHUNKED) {
       const u64 at = (((u64)blockIdx.y * a.batch + b) * a.heads + h) * a.q_len + safe;
       if (count) store_part<D>(a.parts + at * D, o_at, there, by);
@@ -413,13 +428,8 @@ __global__ void __launch_bounds__(256) k_join_outputs(const Args a, int chunks) 
 }
 
 // ------------------------------------------------------------------ backward
-// Half precision has 2^-24 as its smallest number, and probabilities and gradients go below it.  P is held
-// 2^12 times as large (at most 4096), dS times a power of two that follows from the largest norms: |dP - delta| is at
+// In half precision P is at most 2^P_SHIFT here, and dS is held times a power of two that follows from the largest norms: |dP - delta| is at
 // most 2 |dO_i| |V_j|, and that bound is brought to 2^14 or just below for each key head (its queries are summed over).
-// bfloat16 has float's exponents and needs neither.
-template <class T> struct Range { static constexpr bool small = false; };
-template <> struct Range<__half> { static constexpr bool small = true; };
-constexpr int P_SHIFT = 12;
 // dS is held times 2^P_SHIFT times this
 __device__ __forceinline__ float gradient_factor(const Args& a, int b, int kh) {
   const u32* at = a.norms + 2 * (b * a.kv_heads + kh);

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_train_operators import tensors
+from test_gpu_train_operators import F, TYPES, normal, tensors, tiny_of, u_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,77 @@ def test_attention_with_an_empty_side(ctx, dtype, dim, q_len, k_len):
     assert all(g.eq(0).all() for g in grads)
     # and no error is left behind for the next launch to find
     assert torch.ones(8, device="cuda").sum().item() == 8
+
+
+def far_keys(n, at, below, dim, heads, seed, spread):
+    """One query whose key `at` has a value of zero and whose other keys' scores lie `below` (and up to `spread` more) under
+    that one's, in numbers that half precision holds."""
+    gen = torch.Generator("cuda").manual_seed(seed)
+    q = torch.zeros(1, 1, heads, dim, device="cuda", dtype=torch.float16)
+    q[..., 0] = 1.0
+    k = torch.zeros(1, n, heads, dim, device="cuda", dtype=torch.float16)
+    k[..., 0] = -below - spread * torch.rand(1, n, heads, device="cuda", generator=gen)
+    k[:, at, :, 0] = 0.0
+    v = torch.rand(1, n, heads, dim, device="cuda", generator=gen).add_(0.5).half()
+    v[:, at] = 0.0
+    return q, k, v
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("below, spread", [(9.0, 0.0), (14.0, 0.0), (14.0, 1.0), (16.5, 0.0), (16.5, 1.0)])
+@pytest.mark.parametrize("n, at", [(2000, 0), (2000, 1990), (2000, 700), (8192, 5), (8192, 8191)])
+def test_half_precision_keeps_small_probabilities(ctx, dim, below, spread, n, at):
+    """All of the output comes from keys far below the row's largest."""
+    q, k, v = far_keys(n, at, below, dim, 2, n + at, spread)
+    out, lse = ctx.attention_forward(q, k, v, 1.0, False)
+    ctx.check_status()
+    s = k[0, :, :, 0].double().t()                              # [head, key]: q is a unit vector
+    want = (torch.softmax(s, -1)[:, None] @ v[0].double().transpose(0, 1))[:, 0]
+    # A probability: rounded to half, relative; where that is subnormal, by half of 2^-24, of a number that is held 2^7 as large (the
+    # row's largest number is at least 2^7, so is the sum that divides it); the exponent in float32, off by 4 roundings of
+    # numbers up to (below + spread) log2 e + 7; the exponential itself; n terms summed twice and divided.
+    u, exponent = u_of(torch.float16), 4 * F * ((below + spread) * 1.4427 + 7)
+    bound = (2 * u + exponent + (2 * n + 16) * F + 2.0 ** -21) * want + 2.0 ** -32 * v[0].double().sum(0)
+    within(out[0, 0], want, bound, "out")
+    within(lse[0, :, 0], torch.logsumexp(s, -1), torch.full_like(lse[0, :, 0], 1e-5 + (n + 16) * F).double(), "lse")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("step", [0.7, 1.0, 2.0, 3.0, 8.0, 20.0])
+def test_attention_whose_largest_score_moves_with_every_block(ctx, dtype, step):
+    """Blocks of 128 keys with equal scores, each `step` above the last one's and by that much heavier: whether the sums
+    are rescaled or not, no weight leaves the type's range."""
+    blocks, heads, dim = 12, 2, 64
+    gen = torch.Generator("cuda").manual_seed(int(step * 10))
+    q = torch.zeros(1, 300, heads, dim, device="cuda", dtype=TYPES[dtype])
+    q[..., 0] = 1.0
+    k = torch.zeros(1, 128 * blocks, heads, dim, device="cuda", dtype=TYPES[dtype])
+    k[..., 0] = (torch.arange(blocks, device="cuda") * step).repeat_interleave(128)[None, :, None]
+    v = normal(gen, 1, 128 * blocks, heads, dim, dtype=TYPES[dtype])
+    out, lse = ctx.attention_forward(q, k, v, 1.0, False)
+    ctx.check_status()
+    s = k[0, :, 0, 0].double()
+    p = torch.softmax(s, -1)
+    want, size = (torch.einsum("j,jhd->hd", p, x) for x in (v[0].double(), v[0].double().abs()))
+    u, n = u_of(TYPES[dtype]), 128 * blocks
+    most = float(s.abs().max()) * 1.4427 + 7
+    bound = u * want.abs() + tiny_of(TYPES[dtype]) + (u + 4 * F * most + (2 * n + 16) * F + 2.0 ** -21) * size + 2.0 ** -32 * v[0].double().abs().sum(0)
+    within(out[0], want.expand(300, heads, dim), bound, "out")
+    within(lse[0], torch.logsumexp(s, -1).expand(heads, 300), torch.full((heads, 300), (n + 16) * F + 8 * F * most, device="cuda").double(), "lse")
+
+
+@pytest.mark.parametrize("size", [100.0, 700.0, 1000.0, 1500.0, 2000.0])
+@pytest.mark.parametrize("at", [0, 130, 511])
+def test_half_precision_with_scores_of_millions(ctx, size, at):
+    """One key far above the others, at scores (up to 5e8) of which float32 holds whole numbers only: its value is the output."""
+    q = torch.full((1, 200, 1, 128), size, device="cuda", dtype=torch.float16)
+    k = torch.full((1, 512, 1, 128), 0.5 * size, device="cuda", dtype=torch.float16)
+    k[:, at] = size
+    v = normal(torch.Generator("cuda").manual_seed(at), 1, 512, 1, 128, dtype=torch.float16)
+    out, lse = ctx.attention_forward(q, k, v, None, False)
+    ctx.check_status()
+    # the one weight cancels but for its own rounding to half and the division's; the others are zero
+    want = v[0, at].double().expand(200, 1, 128)
+    within(out[0], want, 2 * u_of(torch.float16) * want.abs() + 4 * F * want.abs() + tiny_of(torch.float16))
+    score = size * size * 128 * 128 ** -0.5
+    within(lse[0, 0], torch.full((200,), score, device="cuda").double(), torch.full((200,), (128 + 8) * F * score, device="cuda").double())
