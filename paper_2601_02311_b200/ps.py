@@ -320,9 +320,25 @@ class Context:
         status = self.check_status(allow_truncated)
         return d_all.cpu().numpy(), status
 
-    # ---- operators of a training step.  Tensors live on the context's device; work is enqueued on the context's
-    # stream, on which the short forms allocate their results as well.  The library sees sizes and strides, so what it
-    # cannot see is refused here, with its codes: another device, another type, a shape that does not match.
+    # ---- operators of a training step.  Tensors live on the context's device, and a call takes its place in the order of
+    # torch's current stream, as one of torch's own would: its tensors may come from there and its results be used there at
+    # once, and they and its work buffer are allocated there.  The library sees sizes and strides, so what it cannot see is
+    # refused here, with its codes: another device, another type, a shape that does not match.
+
+    def _enqueue(self, where: str, call, *args):
+        """The library's call, on the context's stream.  Where that is not torch's current one, it waits for what the current one
+        has been given so far, and the current one for the call (8 us on the host; contexts whose calls are to
+        overlap are used with their own streams current).  So memory that torch gives out again there is not in use
+        any more, and a capture of the current stream takes the call in."""
+        if torch._C._cuda_getCurrentRawStream(self.device) == self._raw_stream:
+            return _check(call(self._h, *args), where)
+        current = torch.cuda.current_stream(self.device)
+        own = self.stream if self.stream is not None else torch.cuda.default_stream(self.device)
+        own.wait_stream(current)
+        try:
+            _check(call(self._h, *args), where)
+        finally:
+            current.wait_stream(own)
 
     def _refuse(self, code: int, where: str, what: str):
         raise PsError(code, f"{where}: {what}")
@@ -347,15 +363,11 @@ class Context:
         return t.element_size()
 
     def _work(self, work: torch.Tensor | None, need: int, where: str) -> torch.Tensor:
-        if work is None:                # (freed when the call returns: torch gives it out again on this stream only)
-            return self._allocate_work(need)
+        if work is None:                # (freed when the call returns: torch gives it out again on the current stream only)
+            return torch.empty(max(need, 1), dtype=torch.uint8, device=self.torch_device)
         if work.get_device() != self.device or work.dtype != torch.uint8 or not work.is_contiguous():
             self._refuse(E_RANGE, where, f"work has to be a contiguous uint8 tensor on device {self.device}")
         return work
-
-    @_on_own_stream
-    def _allocate_work(self, need: int) -> torch.Tensor:
-        return torch.empty(max(need, 1), dtype=torch.uint8, device=self.torch_device)
 
     def dropout_into(self, x: torch.Tensor, y: torch.Tensor, p: float, seed: int, stream: int = 0,
                      residual: torch.Tensor | None = None, first: int = 0, pitch: int | None = None):
@@ -369,11 +381,10 @@ class Context:
             pitch = cols
         if not (0 <= seed < 1 << 64 and 0 <= stream < 1 << 64 and 0 <= first < 1 << 63 and 0 <= pitch < 1 << 63):
             self._refuse(E_RANGE, where, "seed, stream, first or pitch")
-        _check(_lib.ps_dropout(
-            self._h, _DROPOUT_DESC(rows, cols, x_stride, r_stride, y_stride, seed, stream, first, pitch, p, _DTYPE[dtype], 0),
-            x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr()), where)
+        self._enqueue(where, _lib.ps_dropout,
+                      _DROPOUT_DESC(rows, cols, x_stride, r_stride, y_stride, seed, stream, first, pitch, p, _DTYPE[dtype], 0),
+                      x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr())
 
-    @_on_own_stream
     def dropout(self, x: torch.Tensor, p: float, seed: int, stream: int = 0, residual: torch.Tensor | None = None,
                 first: int = 0, pitch: int | None = None) -> torch.Tensor:
         """x with a share p of its elements dropped and the others divided by 1 - p, plus `residual`.
@@ -392,11 +403,10 @@ class Context:
         if not 0 <= first_row < 1 << 62:
             self._refuse(E_RANGE, where, "first_row")
         code = _DTYPE[dtype]
-        _check(_lib.ps_embed_forward(
-            self._h, _EMBED_DESC(n, first_row, shape[0], shape[1], t_stride, o_stride, scale, code, code, width, 0),
-            table.data_ptr(), tokens.data_ptr(), out.data_ptr()), where)
+        self._enqueue(where, _lib.ps_embed_forward,
+                      _EMBED_DESC(n, first_row, shape[0], shape[1], t_stride, o_stride, scale, code, code, width, 0),
+                      table.data_ptr(), tokens.data_ptr(), out.data_ptr())
 
-    @_on_own_stream
     def embed_forward(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, first_row: int = 0) -> torch.Tensor:
         """The scaled rows [tokens, dim] of the table that the tokens name."""
         out = table.new_empty((tokens.numel(), table.shape[-1]))
@@ -416,10 +426,9 @@ class Context:
         desc = _EMBED_DESC(n, first_row, shape[0], shape[1], g_stride, o_stride, scale, _DTYPE[d_out.dtype],
                            _DTYPE[d_table.dtype], width, 1 if accumulate else 0)
         work = self._work(work, _lib.ps_embed_backward_bytes(desc), where)
-        _check(_lib.ps_embed_backward(self._h, desc, d_out.data_ptr(), tokens.data_ptr(), d_table.data_ptr(), work.data_ptr(),
-                                      work.numel()), where)
+        self._enqueue(where, _lib.ps_embed_backward, desc, d_out.data_ptr(), tokens.data_ptr(), d_table.data_ptr(), work.data_ptr(),
+                      work.numel())
 
-    @_on_own_stream
     def embed_backward(self, d_out: torch.Tensor, tokens: torch.Tensor, rows: int, scale: float = 1.0, first_row: int = 0,
                        dtype: torch.dtype | None = None) -> torch.Tensor:
         """The gradient [rows, dim] of the table, in d_out's type or `dtype`."""
@@ -473,12 +482,10 @@ class Context:
         if need or work is not None:
             work = self._work(work, need, where)
             at, size = work.data_ptr(), work.numel()
-        _check(_lib.ps_attention_forward(
-            self._h, shape, self._heads(q, where, "q", qs, dtype), self._heads(k, where, "k", ks, dtype),
-            self._heads(v, where, "v", ks, dtype), self._heads(out, where, "out", qs, dtype), lse.data_ptr(), ql, kl, at, size),
-            where)
+        self._enqueue(
+            where, _lib.ps_attention_forward, shape, self._heads(q, where, "q", qs, dtype), self._heads(k, where, "k", ks, dtype),
+            self._heads(v, where, "v", ks, dtype), self._heads(out, where, "out", qs, dtype), lse.data_ptr(), ql, kl, at, size)
 
-    @_on_own_stream
     def attention_forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float | None = None,
                           causal: bool = True, q_lens: torch.Tensor | None = None, k_lens: torch.Tensor | None = None):
         """(out [batch, q_len, heads, dim], lse [batch, heads, q_len])."""
@@ -499,14 +506,13 @@ class Context:
         where, dtype = "ps_attention_backward", q.dtype
         shape, qs, ks, ql, kl = self._attention(q, k, where, scale, causal, q_lens, k_lens, lse)
         work = self._work(work, _lib.ps_attention_backward_bytes(shape), where)
-        _check(_lib.ps_attention_backward(
-            self._h, shape, self._heads(q, where, "q", qs, dtype), self._heads(k, where, "k", ks, dtype),
+        self._enqueue(
+            where, _lib.ps_attention_backward, shape, self._heads(q, where, "q", qs, dtype), self._heads(k, where, "k", ks, dtype),
             self._heads(v, where, "v", ks, dtype), self._heads(out, where, "out", qs, dtype), lse.data_ptr(),
             self._heads(d_out, where, "d_out", qs, dtype), self._heads(d_q, where, "d_q", qs, dtype),
             self._heads(d_k, where, "d_k", ks, dtype), self._heads(d_v, where, "d_v", ks, dtype), ql, kl, work.data_ptr(),
-            work.numel()), where)
+            work.numel())
 
-    @_on_own_stream
     def attention_backward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
                            d_out: torch.Tensor, scale: float | None = None, causal: bool = True,
                            q_lens: torch.Tensor | None = None, k_lens: torch.Tensor | None = None):

@@ -111,3 +111,99 @@ def test_half_precision_with_scores_of_millions(ctx, size, at):
     within(out[0], want, 2 * u_of(torch.float16) * want.abs() + 4 * F * want.abs() + tiny_of(torch.float16))
     score = size * size * 128 * 128 ** -0.5
     within(lse[0, 0], torch.full((200,), score, device="cuda").double(), torch.full((200,), (128 + 8) * F * score, device="cuda").double())
+
+
+# ------------------------------------------------------------------ streams
+
+def all_operators(ctx, x):
+    q, k, v, d_out, rows, ids = x
+    out, lse = ctx.attention_forward(q, k, v)
+    into = torch.empty_like(rows)
+    ctx.dropout_into(rows, into, 0.2, 9)
+    few = ctx.attention_forward(q[:, :1], k, v)                     # (in chunks, with a work buffer)
+    return (out, lse, into) + few + ctx.attention_backward(q, k, v, out, lse, d_out) + (
+        ctx.embed_forward(rows, ids), ctx.embed_backward(rows, ids, 50), ctx.dropout(rows, 0.3, 5, residual=rows))
+
+
+def operands(seed):
+    q, k, v, d_out = tensors(seed, 1, 300, 4200, 4, 2, 64, "f16")
+    gen = torch.Generator("cuda").manual_seed(seed)
+    return q, k, v, d_out, normal(gen, 400, 256, dtype=torch.bfloat16), torch.randint(0, 50, (400,), device="cuda", generator=gen)
+
+
+@pytest.mark.parametrize("own, current", [(True, False), (True, True), (False, True)])
+def test_operators_in_the_order_of_another_stream(ps, own, current):
+    """A context's stream is not the current one: operands still in the making, temporaries freed and their memory filled at once, results
+    used at once."""
+    torch.cuda.synchronize()
+    ctx = ps.Context(0, torch.cuda.Stream() if own else None)
+    with torch.cuda.stream(torch.cuda.Stream() if current else torch.cuda.default_stream()):
+        plain = ps.Context(0, torch.cuda.current_stream() if current else None)
+        sources = [operands(seed) for seed in (31, 32, 33)]
+        want = [all_operators(plain, x) for x in sources]
+        torch.cuda.synchronize()
+        held = [torch.zeros_like(t) for t in sources[0]]
+        for turn in range(6):
+            torch.cuda._sleep(10_000_000)                           # (a few milliseconds)
+            for h, t in zip(held, sources[turn % 3]):
+                h.copy_(t)
+            got = all_operators(ctx, [h.clone() for h in held])
+            seen = [g.clone() for g in got]
+            for h in held:
+                h.zero_()
+            del got
+            junk = [torch.full_like(s, 3.0) for s in seen + held]
+            for s, w in zip(seen, want[turn % 3]):
+                assert torch.equal(s, w)
+            del junk
+        torch.cuda.current_stream().synchronize()
+    ctx.check_status()
+
+
+def test_operators_of_another_stream_in_a_capture(ps):
+    """A capture of the current stream takes in the calls of a context with a stream of its own."""
+    ctx = ps.Context(0, torch.cuda.Stream())
+    side = torch.cuda.Stream()
+    first, second = operands(34), operands(35)
+    held = [t.clone() for t in first]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        want = [all_operators(ctx, x) for x in (first, second)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = all_operators(ctx, held)
+        for x, w in ((first, want[0]), (second, want[1]), (first, want[0])):
+            for h, t in zip(held, x):
+                h.copy_(t)
+            for g in got:
+                g.fill_(1.0)
+            graph.replay()
+            for g, t in zip(got, w):
+                assert torch.equal(g, t)
+        side.synchronize()
+    ctx.check_status()
+    del graph, got
+
+
+def test_operators_of_contexts_on_their_own_streams_overlap(ps):
+    """Each context's stream is current for its calls, so nothing orders the two: no work space is shared."""
+    contexts = [ps.Context(0, torch.cuda.Stream()) for _ in range(2)]
+    inputs = [operands(36), operands(37)]
+    torch.cuda.synchronize()
+    want = []
+    for ctx, x in zip(contexts, inputs):
+        with torch.cuda.stream(ctx.stream):
+            want.append(all_operators(ctx, x))
+        torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for _ in range(3):
+            got = []
+            for ctx, x in zip(contexts, inputs):
+                with torch.cuda.stream(ctx.stream):
+                    got.append(all_operators(ctx, x))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(g, w))
+    for ctx in contexts:
+        ctx.check_status()
