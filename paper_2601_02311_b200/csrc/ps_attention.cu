@@ -51,6 +51,7 @@ struct Args {
   // rounded up to whole tiles; and for types with a small range the norms, see gradient_factor
   float *lse2, *delta;
   u32* norms;
+  u32* rows_there;      // see publish_rows
   int padded;
   // few queries before many keys, or the other way: the long side is cut into chunks, a block each, whose results in 32 bits are
   // joined by another kernel
@@ -447,6 +448,7 @@ template <int D> constexpr int ROWS_A_BLOCK = 256 / (D / 8) * ROWS_A_THREAD;
 template <class T, int D, bool QUERY>
 __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads out, const Args a) {
   let_next_begin();
+  if (QUERY && (threadIdx.x | blockIdx.x | blockIdx.y | blockIdx.z) == 0) *a.rows_there = 0;
   __shared__ u32 largest;
   if (Range<T>::small) {
     if (threadIdx.x == 0) largest = 0;
@@ -497,6 +499,18 @@ __global__ void __launch_bounds__(256) k_rows(const ps_heads x, const ps_heads o
   }
 }
 
+// k_queries may begin while k_keys runs, and reads what k_rows wrote: the kernel before the one that its wait is for.  So a thread of each
+// block of k_keys, behind that block's wait for the rows, says so in memory before it lets k_queries begin, and whoever reads that there
+// sees the rows as well.  Else k_queries waits for all of k_keys.
+__device__ __forceinline__ void publish_rows(const Args& a) {
+  asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(a.rows_there), "r"(1u) : "memory");
+}
+__device__ __forceinline__ void wait_for_rows(const Args& a) {
+  u32 there;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(there) : "l"(a.rows_there) : "memory");
+  if (!there) wait_for_earlier();
+}
+
 // Both kernels of the backward pass let their two groups of warps take turns: tile pairs are numbered, a group has the even
 // ones and the other the odd ones, each with a buffer of 128 columns of tensor memory of its own, a thread a row.  A
 // pair's buffer holds S, then what its products leave of P, then dP, then dS.  While one group works the tensor cores
@@ -542,7 +556,10 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   const int walk = j0 < l.m ? max(0, CHUNKED ? min(rest, CHUNK) : rest) : 0, total = walk * group;     // tiles of queries
   if (total == 0) {
     wait_for_earlier();
-    let_next_begin();
+    if (threadIdx.x == 0) {
+      publish_rows(a);
+      let_next_begin();
+    }
     if (!CHUNKED) {
       clear_results<T>(a.d_v, b, kh, j0, ROWS, a.k_len, a.dim);
       clear_results<T>(a.d_k, b, kh, j0, ROWS, a.k_len, a.dim);
@@ -580,7 +597,10 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
   if (warp < COPY_WARP) {
     take_registers<BackwardRegisters::taken>();
     wait_for_earlier();          // the rows
-    let_next_begin();            // behind the wait: k_queries needs the rows too, and nothing of this kernel
+    if (threadIdx.x == 0) {
+      publish_rows(a);
+      let_next_begin();          // k_queries needs the rows too, and nothing of this kernel
+    }
     const int mine = warp / 4, j = j0 + threadIdx.x % ROWS;
     const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
     // this key's first query; the first query that all of the tile's keys have
@@ -888,6 +908,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const u32 lanes = (u32)(warp % 4 * 32) << 16, at = tmem + lanes + mine * ROWS;
     const int masked = q0 + ROWS > l.n ? 0 : (end_of(a, l, q0) - key0) / ROWS;
     const u64 row = ((u64)b * a.heads + h) * a.padded + i;
+    wait_for_rows(a);
     const float off = a.lse2[row], delta = a.delta[row], factor = Range<T>::small && total > 0 ? gradient_factor(a, b, kh) : 1.f;
     const u64 cs = pair(a.c, a.c), offs = pair(off, off), deltas = pair(delta, delta), factors = pair(factor, factor);
     if (total > 0) {            // Q and dO are left operands of every pair
@@ -1115,6 +1136,7 @@ Args args_of(const AttentionArgs& a) {
   r.lse2 = (float*)a.work;
   r.delta = r.lse2 + rows;
   r.norms = (u32*)(r.delta + rows);
+  r.rows_there = r.norms + 2 * (size_t)a.batch * a.kv_heads;
   r.parts = r.part_lse = nullptr;
   r.status = a.status;
   return r;
@@ -1164,10 +1186,10 @@ cudaError_t forward(u32 dtype, const AttentionArgs& a, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
-// the backward pass's work buffer: both vectors of the padded rows and the norms, then the chunks' shares
+// the backward pass's work buffer: both vectors of the padded rows, the norms and whether the rows are there, then the chunks' shares
 size_t rows_bytes(const AttentionArgs& a) {
   const size_t padded = ((size_t)a.q_len + ROWS - 1) / ROWS * ROWS;
-  return (sizeof(float) * 2 * a.batch * a.heads * padded + sizeof(u32) * 2 * a.batch * a.kv_heads + 255) / 256 * 256;
+  return (sizeof(float) * 2 * a.batch * a.heads * padded + sizeof(u32) * (2 * (size_t)a.batch * a.kv_heads + 1) + 255) / 256 * 256;
 }
 
 template <class T, int D>

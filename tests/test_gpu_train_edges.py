@@ -113,6 +113,29 @@ def test_half_precision_with_scores_of_millions(ctx, size, at):
     within(lse[0, 0], torch.full((200,), score, device="cuda").double(), torch.full((200,), (128 + 8) * F * score, device="cuda").double())
 
 
+@pytest.mark.parametrize("dtype, dim, q_len, k_len, causal", [("bf16", 64, 700, 700, True), ("f16", 64, 700, 700, True), ("bf16", 128, 500, 900, False),
+                                                             ("f16", 128, 900, 500, True), ("bf16", 64, 3, 4500, True), ("f16", 128, 4500, 3, False)])
+def test_attention_gradients_with_whatever_the_work_buffer_holds(ctx, ps, dtype, dim, q_len, k_len, causal):
+    """One buffer for calls in a row on operands that differ, and between them bytes of all sorts in it: the rows that a call reads are its own."""
+    cases = []
+    for seed in (22, 23):
+        q, k, v, d_out = tensors(seed, 2, q_len, k_len, 4, 2, dim, dtype)
+        out, lse = ctx.attention_forward(q, k, v, None, causal)
+        cases.append(((q, k, v, out, lse, d_out), ctx.attention_backward(q, k, v, out, lse, d_out, None, causal)))
+    work = torch.empty(ps.Context.attention_backward_bytes(2, q_len, k_len, 4, 2, dim), dtype=torch.uint8, device="cuda")
+    results = []
+    for turn in range(12):
+        if turn % 4 < 3:
+            work.fill_((0, 1, 255)[turn % 4])                       # (zeros, whole numbers that are not zero, NaN)
+        operands, want = cases[turn % 2]
+        grads = [torch.empty_like(t) for t in operands[:3]]
+        ctx.attention_backward_into(*operands, *grads, causal=causal, work=work)
+        results.append((grads, want))
+    ctx.check_status()
+    for grads, want in results:
+        assert all(torch.equal(g, w) for g, w in zip(grads, want))
+
+
 # ------------------------------------------------------------------ streams
 
 def all_operators(ctx, x):
