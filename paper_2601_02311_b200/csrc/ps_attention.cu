@@ -361,7 +361,7 @@ k_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       const int x = 2 * j + 1, slot = x % RING, next = (x + 1) % RING;
       const u32 v = ring + slot * TILE;
       w.wait(full + 8 * slot, x / RING & 1);
-      if (l.m < a.k_len && key0 + (j + 1) * ROWS > l.m && !w.dead) clear_rows<D>(v, l.m - key0 - j * ROWS);
+      if (l.m < a.k_len && key0 + (j + 1) * ROWS > l.m) clear_rows<D>(v, l.m - key0 - j * ROWS);
       if (j + 1 < most) w.wait(full + 8 * next, (x + 1) / RING & 1);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -738,7 +738,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
           w.wait(dp_full + 8 * two, x >> 1 & 1);           // (dP has read dO before, and cleared what is behind the end)
         } else {
           w.wait(do_full + 8 * two, x >> 1 & 1);
-          if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+          if (pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
         }
         w.wait(p_ready + 8 * two, x >> 1 & 1);
         fence_after();
@@ -777,7 +777,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
       auto scores = [&](int x) {                 // S^T = K Q^T, over dS^T of pair x - 2
         const u32 q = q_ring + x % 3 * TILE;
         w.wait(q_full + 8 * (x % 3), x / 3 & 1);
-        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
+        if (pad_from(x) < ROWS) clear_rows<D>(q, pad_from(x));
         if (x >= 2) w.wait(q_empty + 8 * ((x - 2) % 3), (x - 2) / 3 & 1);
         fence_after();
         if (elected() && !w.dead) {
@@ -791,7 +791,7 @@ k_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtens
         const u32 d = do_ring + two * TILE;
         if (APART) {
           w.wait(do_full + 8 * two, x >> 1 & 1);
-          if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
+          if (pad_from(x) < ROWS) clear_rows<D>(d, pad_from(x));
           if (x > 0) w.wait(ds_ready + 8 * (two ^ 1), (x - 1) >> 1 & 1);
         } else {
           w.wait(dv_done + 8 * two, x >> 1 & 1);
@@ -1024,7 +1024,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
       auto scores = [&](int x) {                 // S = Q K^T, over dS of pair x - GROUPS
         const u32 k = k_ring + x % 3 * TILE;
         w.wait(k_full + 8 * (x % 3), x / 3 & 1);
-        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
+        if (pad_from(x) < ROWS) clear_rows<D>(k, pad_from(x));
         if (x >= GROUPS) w.wait(k_empty + 8 * ((x - GROUPS) % 3), (x - GROUPS) / 3 & 1);
         fence_after();
         if (elected() && !w.dead) {
@@ -1037,7 +1037,7 @@ k_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         const int two = x & 1, at = x % GROUPS;
         const u32 v = v_ring + two * TILE;
         w.wait(v_full + 8 * two, x >> 1 & 1);
-        if (!w.dead && pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
+        if (pad_from(x) < ROWS) clear_rows<D>(v, pad_from(x));
         w.wait(s_read + 8 * at, x / GROUPS & 1);
         fence_after();
         if (elected() && !w.dead) {

@@ -75,7 +75,8 @@ __device__ __forceinline__ void load_bytes(u32 to, const void* from, u32 bytes, 
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
-// a warp: zeros in the rows of a tile from `first` on
+// a warp: zeros in the rows of a tile from `first` on.  (All of its lanes, whether or not they still wait for anything: a wait may have run
+// out for some of them alone, and the lanes meet at the end.)
 template <int D>
 __device__ __forceinline__ void clear_rows(u32 tile, int first) {
   for (int i = (int)(threadIdx.x % 32); i < (ROWS - first) * 8 * (D / 64); i += 32) {
