@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_train_operators import F, TYPES, normal, tensors, tiny_of, u_of, within
+from test_gpu_train_operators import F, TYPES, gradient_want, normal, tensors, tiny_of, u_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -134,6 +134,86 @@ def test_attention_gradients_with_whatever_the_work_buffer_holds(ctx, ps, dtype,
     ctx.check_status()
     for grads, want in results:
         assert all(torch.equal(g, w) for g, w in zip(grads, want))
+
+
+# ------------------------------------------------------------------ the table's gradient from more than 8192 tokens
+
+def some_ids(gen, tokens, rows, spread):
+    """Low rows are frequent (lists of thousands), most rows have none, some tokens name no row."""
+    return (torch.rand(tokens, device="cuda", generator=gen) ** spread * (rows + 2)).long() - 1
+
+
+# what is compiled: packs of 16 bytes or single elements, one or two of them a lane (above 2^25 elements of the table); columns in
+# one part or several; pieces of 32 in one wave or many; lists with and without pieces of 1024; a sort's block with one tile or more
+LARGE = [(9000, 300, 130, 2), (9000, 300, 1030, 2), (9000, 5, 1032, 1), (20000, 40000, 1024, 5), (9000, 40000, 901, 4), (8193, 33000, 1040, 1),
+         (20000, 9000, 4100, 3), (12000, 260, 4096, 2)]
+
+
+@pytest.mark.parametrize("dtype, grad", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("tokens, rows, dim, spread", LARGE)
+def test_table_gradient_of_many_tokens(ctx, dtype, grad, tokens, rows, dim, spread):
+    gen = torch.Generator("cuda").manual_seed(tokens + dim)
+    d_out = normal(gen, tokens, dim, dtype=TYPES[dtype])
+    ids = some_ids(gen, tokens, rows, spread)
+    want, bound = gradient_want(d_out, ids, rows, 0.7, 0, TYPES[grad])
+    got = ctx.embed_backward(d_out, ids, rows, 0.7, dtype=TYPES[grad])
+    ctx.check_status()
+    within(got, want, bound)
+    assert torch.equal(got, ctx.embed_backward(d_out, ids.int(), rows, 0.7, dtype=TYPES[grad]))
+
+
+@pytest.mark.parametrize("tokens, rows, dim, spread", [(303104, 1000, 8, 1), (303105, 1000, 8, 1), (310000, 300001, 5, 3), (700001, 30, 3, 2), (650000, 128000, 16, 4)])
+def test_table_gradient_with_several_tiles_a_block_of_the_sort(ctx, tokens, rows, dim, spread):
+    gen = torch.Generator("cuda").manual_seed(tokens)
+    d_out = normal(gen, tokens, dim, dtype=torch.bfloat16)
+    ids = some_ids(gen, tokens, rows, spread)
+    want, bound = gradient_want(d_out, ids, rows, 1.0, 0, torch.float32)
+    got = ctx.embed_backward(d_out, ids, rows, dtype=torch.float32)
+    ctx.check_status()
+    within(got, want, bound)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens, rows, dim", [(0, 50, 24), (9000, 300, 40), (9000, 300, 131), (9000, 40000, 1024), (20000, 40000, 901)])
+def test_table_gradient_of_many_tokens_added_to_what_is_there(ctx, dtype, tokens, rows, dim):
+    gen = torch.Generator("cuda").manual_seed(tokens + rows)
+    t = TYPES[dtype]
+    d_out, there = normal(gen, tokens, dim, dtype=t), normal(gen, rows, dim, dtype=t)
+    ids = (torch.rand(tokens, device="cuda", generator=gen) ** 3 * (rows // 2)).long() * 2              # every other row
+    want, bound = gradient_want(d_out, ids, rows, 1.3, 0, t)
+    want = want + there.double()
+    got = there.clone()
+    ctx.embed_backward_into(d_out, ids, got, 1.3, accumulate=True)
+    ctx.check_status()
+    within(got, want, bound + u_of(t) * want.abs() + 2 * F * (want.abs() + there.double().abs()))
+    assert torch.equal(got[1::2], there[1::2])
+
+
+@pytest.mark.parametrize("grad", TYPES)
+@pytest.mark.parametrize("rows, dim, first, stride", [(50, 70, 0, 88), (50, 72, 8, 88), (50, 70, 1, 89), (50, 264, 4, 280), (30000, 1120, 8, 1144), (30000, 1121, 3, 1127)])
+def test_table_gradient_of_many_tokens_into_rows_of_a_larger_tensor(ctx, grad, rows, dim, first, stride):
+    gen = torch.Generator("cuda").manual_seed(first + dim)
+    wide, table = normal(gen, 9000, stride, dtype=torch.bfloat16), normal(gen, rows, stride, dtype=TYPES[grad])
+    d_out, d_table = wide[:, first:first + dim], table[:, first:first + dim]
+    before = table.clone()
+    ids = some_ids(gen, 9000, rows, 2)
+    want, bound = gradient_want(d_out, ids, rows, 1.0, 0, TYPES[grad])
+    ctx.embed_backward_into(d_out, ids, d_table)
+    ctx.check_status()
+    within(d_table, want, bound)
+    assert torch.equal(table[:, :first], before[:, :first]) and torch.equal(table[:, first + dim:], before[:, first + dim:])
+
+
+@pytest.mark.parametrize("rows, dim, begins", [(1000, 64, (0, 1, 400)), (1000, 65, (0, 999)), (45000, 1024, (0, 7, 40000))])
+def test_table_gradient_of_many_tokens_on_shards_is_the_whole_tables(ctx, rows, dim, begins):
+    """A shard of the vocabulary has the very rows of the single device, also where the two take another number of packs a lane."""
+    gen = torch.Generator("cuda").manual_seed(6)
+    d_out = normal(gen, 12000, dim, dtype=torch.bfloat16)
+    ids = some_ids(gen, 12000, rows, 3)
+    whole = ctx.embed_backward(d_out, ids, rows)
+    for begin, end in zip(begins, begins[1:] + (rows,)):
+        assert torch.equal(ctx.embed_backward(d_out, ids, end - begin, first_row=begin), whole[begin:end])
+    ctx.check_status()
 
 
 # ------------------------------------------------------------------ streams
