@@ -459,7 +459,11 @@ int ps_verify_batch(ps_ctx* ctx, const ps_verify_shape* shape /* host */, const 
  * overlap inputs or one another except where said.  Elements are float (PS_F32),
  * bfloat16 (PS_BF16) or IEEE half (PS_F16); arithmetic is in 32 bits and a result is
  * rounded once, to nearest even, except for the two matrices that attention multiplies
- * in its operands' type (see there). */
+ * in its operands' type (see there).
+ *
+ * A call returns before its kernels have run.  Where a block of attention's waits for a copy or a product of
+ * its own for two seconds, it gives up: the call's results are not to be used, and ps_status, which
+ * waits for them, or the next call returns PS_E_DEVICE. */
 enum { PS_F32 = 0, PS_BF16 = 1, PS_F16 = 2 };
 
 /* Dropout, with an optional residual:

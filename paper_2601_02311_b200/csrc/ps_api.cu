@@ -706,7 +706,7 @@ static int attention_args(const ps_attention_shape& s, AttentionArgs& a) {
       s.heads % s.kv_heads || s.dim < 8 || s.dim > 128 || s.dim % 8 || (s.dtype != PS_BF16 && s.dtype != PS_F16) ||
       s.causal > 1 || !std::isfinite(s.scale))
     return PS_E_RANGE;
-  // what the grids can hold (a block for 128 queries or keys of a head, or for 16 rows)
+  // what the grids can hold (a block for 128 queries or keys of a head in one dimension; rows by 8 or more, heads and sequences in three)
   if ((u64)s.batch * s.heads * ((std::max(s.q_len, s.k_len) + 127) / 128) > (1u << 26)) return PS_E_RANGE;
   memset(&a, 0, sizeof(a));
   a.batch = (int)s.batch; a.q_len = (int)s.q_len; a.k_len = (int)s.k_len;

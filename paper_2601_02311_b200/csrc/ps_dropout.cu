@@ -9,7 +9,8 @@
 // key seed; threshold = round(p * 2^32) and scale = 1 / (1 - p).
 //
 // What bounds it: with a residual bytes, 65536 x 8192 in bfloat16, 3.2 GB: 528 us, 6.1 TB/s (0.94 of a copy's rate).  Without one the generator:
-// a group of four words is 20 wide products, of which an SM does 25 to 32 a cycle, and 20 exclusive-ors, 64 a cycle; 490 us where a copy takes 334.
+// a group of four words is 20 wide products (18 of numbers that depend on the element, 2 of the stream and the seed alone), of which an SM does
+// 25 to 32 a cycle, and 20 exclusive-ors, 64 a cycle; 490 us where a copy takes 334.
 // Accesses of 32 bytes are fewer instructions: with 16 the two took 567 and 542 us.  12301 x 5003 floats in rows that begin anywhere, 0.49 GB:
 // 99 us, 5.0 TB/s; where the tensors' rows do not even lie alike, by accesses of 4 bytes, 118.
 #include "ps_train.cuh"

@@ -482,7 +482,8 @@ u32 chunks_of(u64 dim, int columns) { return (u32)((dim + columns - 1) / columns
 u64 width_of(u64 dim) { return (dim + 7) / 8 * 8; }
 
 // How the radix sort goes: rows + 1 keys (the last one for tokens without a row), digits of up to 9 bits, a block for a
-// tile of 4096 tokens and no more blocks than the GPU has room for at once (each of them reads all blocks' counts).
+// tile of 2048 tokens, or for several where there would be more than 148 blocks: as many as the GPU has room for at once (each of them
+// reads all blocks' counts).
 constexpr u32 SORT_BLOCKS = 148;
 SortArgs sort_plan(const EmbedArgs& a) {
   SortArgs s;
@@ -637,8 +638,9 @@ cudaError_t gradient(const EmbedArgs& a, int sm_count, cudaStream_t stream) {
     const u32 chunks = chunks_of(a.dim, 32 * N);       // (up to 2^15, for up to 2^13 places)
     return launch_next(k_lists<T, G, N>, grid_for(g.n * chunks, sm_count, LIST_BLOCKS), 256, 0, stream, a, g, chunks, Divider(chunks), g.n * chunks);
   }
-  // (32000 rows of 768: 33.8 us with 256 columns a warp, 37.9 with 512; 256000 rows of 8192: 1225 and 1194; alike between 2^26 and
-  // 2^30 elements)
+  // One pack a lane in small tables, two in large ones (bfloat16, L2 flushed before).  32768 tokens into 8000 x 512: 59 us with one, 66 with two;
+  // 131072 into 256000 x 8192: 1188 and 1168.  Between 2^24 and 2^29 elements either is ahead, by 10 % at most (floats, 16000 x 1024: 104 and
+  // 95; bfloat16, 32000 x 1152: 81 and 89; 64000 x 4096: 192 and 196; 128000 x 4096: 285 and 286).
   if (a.rows * a.dim <= SMALL_TABLE) return write_rows<T, G, N, 8, 1, 4, 5>(a, g, sm_count, stream);
   return write_rows<T, G, N, 8, 2, 4, 3>(a, g, sm_count, stream);
 }
