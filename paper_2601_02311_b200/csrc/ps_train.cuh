@@ -124,7 +124,8 @@ struct Pack {
 
 // ---- A chain of kernels of one call.  A kernel that is started by launch_next may begin while the kernel before it in the
 // stream still runs: as soon as each block of that one has called let_next_begin (or ended).  What it reads of earlier kernels it reads
-// behind wait_for_earlier, which returns once they are done and their results visible.
+// behind wait_for_earlier, which returns once they are done and their results visible (k_queries of ps_attention.cu reads some of it
+// earlier, by an order of its own: publish_rows).
 __device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <class... Parameters, class... Arguments>
