@@ -557,6 +557,105 @@ int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps
                           const ps_heads* d_q, const ps_heads* d_k, const ps_heads* d_v, const int32_t* d_q_lens,
                           const int32_t* d_k_lens, void* d_work, uint64_t work_bytes);
 
+/* Layer norm over rows, and its gradients:
+ *   y = (x - mean) * rstd * weight + bias,  mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps)
+ *   g = d_y * weight;  xn = (x - mean) * rstd
+ *   d_x = rstd * (g - sum_c g / cols - xn * sum_c g xn / cols) + residual
+ *   d_weight = sum_r d_y xn;  d_bias = sum_r d_y
+ * Nothing of the size of x is kept between them but x itself: xn comes out of a row's two
+ * numbers.  weight (null: ones) and bias (null: zeros) are of x's type, [cols]; mean and rstd are floats, [rows]
+ * (the forward pass writes those that are not null).  `residual` (may be null) is the gradient that reaches x past the
+ * normalised branch.  d_weight and d_bias, of type grad_dtype, are computed where they are not null, in an order that
+ * depends on the sizes alone; with accumulate they are added to what is there (rounded once).  A row's results depend on
+ * that row alone.  y may be x; d_x may be d_y, x or residual (same pointer and stride).
+ * d_work: ps_layer_norm_backward_bytes, used like ps_embed_backward's (0 without d_weight and d_bias). */
+typedef struct {
+  void* data;                      /* a matrix [rows][cols] whose columns are contiguous  */
+  uint64_t stride;                 /* between rows, in elements; >= cols of several rows  */
+} ps_matrix;
+typedef struct {
+  uint64_t rows, cols;             /* rows 0 .. 2^31 - 1; cols 1 .. 2^20                  */
+  double eps;                      /* >= 0, finite as a float                             */
+  uint32_t dtype, grad_dtype;      /* of x, y, weight, bias and their like; of d_weight and d_bias */
+  uint32_t accumulate;             /* backward: 0 or 1                                    */
+  uint32_t pad;
+} ps_layer_norm_desc;
+int ps_layer_norm_forward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps_matrix* x, const void* d_weight,
+                          const void* d_bias, const ps_matrix* y, float* d_mean, float* d_rstd);
+uint64_t ps_layer_norm_backward_bytes(const ps_layer_norm_desc* desc);
+int ps_layer_norm_backward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps_matrix* y_grad, const ps_matrix* x,
+                           const float* d_mean, const float* d_rstd, const void* d_weight,
+                           const ps_matrix* residual /* may be null */, const ps_matrix* x_grad, void* d_weight_grad,
+                           void* d_bias_grad, void* d_work, uint64_t work_bytes);
+
+/* Rotary positions: of each head of q and k, pair i of the first rotary_dim elements is turned by its token's angle:
+ *   (a, b) -> magnitude * (a cos t - b sin t, b cos t + a sin t),  t = (position + first) * f_i
+ * The pair is elements (2 i, 2 i + 1) where interleaved, (i, i + rotary_dim / 2) where not; the elements behind
+ * rotary_dim are copied.  inverse turns by -t: the gradient is the same call with inverse changed, on the result's
+ * gradient.  f_i = base^(-2 i / rotary_dim), for contexts stretched by `factor`
+ *   f_i * (s + (1 - s) / factor),  s = clamp((original * f_i / 2 pi - low) / (high - low), 0, 1)
+ * (original = 0: s = 0, all positions are divided by factor).  Angles are whole numbers, in 2^-64 of a turn: the product
+ * with the position wraps around exactly, so far positions are as accurate as near ones, and f_i's own rounding to
+ * 2^-65 of a turn gives position p an error of p 2^-65 (and double's of f_i, p f_i 2^-52 at most).
+ * d_positions: null (token i of a sequence has position i), or integers, [batch] of `position_stride` apart
+ * (0: the same for all).  A shard of the sequence passes `first`.  q_out may be q, k_out k (same pointer and strides).
+ * k and k_out may be null (kv_heads 0). */
+typedef struct {
+  uint32_t batch;                  /* 0 .. 2^16 - 1; batch * len * (heads + kv_heads) <= 2^38 */
+  uint32_t len;                    /* 0 .. 2^24                                           */
+  uint32_t heads, kv_heads;        /* 1 .. 2^15, 0 .. 2^15                                */
+  uint32_t dim, rotary_dim;        /* 2 .. 256; 2 .. dim, even                            */
+  uint32_t dtype;                  /* PS_F32, PS_BF16 or PS_F16                           */
+  uint32_t interleaved, inverse;   /* 0 or 1                                              */
+  uint32_t position_bytes;         /* positions are int32_t (4) or int64_t (8)            */
+  uint64_t position_stride;
+  int64_t first;
+  double base;                     /* >= 1, finite                                        */
+  double factor;                   /* >= 1, finite                                        */
+  double original, low, high;      /* original >= 0; low < high where it counts; finite   */
+  double magnitude;                /* finite as a float                                   */
+} ps_rotary_desc;
+/* (ps_heads as for attention, but of any alignment that the type has, and strides of 0 for q and k) */
+int ps_rotary(ps_ctx* ctx, const ps_rotary_desc* desc, const ps_heads* q, const ps_heads* q_out, const ps_heads* k,
+              const ps_heads* k_out, const void* d_positions);
+
+/* A linear layer with what follows it in one pass, and its gradients:
+ *   pre = x weight^T + bias;  y = act(pre) + residual
+ *   d_pre = d_y * act'(pre)
+ *   d_x = (d_pre weight) * act_below'(below) + residual;  d_weight = d_pre^T x;  d_bias = sum_t d_pre
+ * x is [tokens][inputs], weight [outputs][inputs], y [tokens][outputs].  Forward: bias [outputs], residual and pre (written,
+ * rounded to the type) may be null.  Backward: `pre` is needed where there is an activation, and d_pre is rounded to the type
+ * before it is multiplied; `below`, [tokens][inputs], is what x came out of by below_activation: the result is then
+ * the gradient of that, and the layer below is given no activation of its own.  Null results are not computed.
+ * d_weight and d_bias, of the type or float (grad_dtype), are added to what is there with accumulate (rounded once).
+ *
+ * Products run on the tensor cores with sums of 32 bits.  A row of y or d_x depends on that row, weight and the widths
+ * alone, not on how many rows or columns the call has; so shards of tokens, and shards of outputs, compute the single device's bits.
+ * d_weight's sum over tokens has an order that depends on the sizes alone.
+ * Matrices begin at multiples of 16 bytes and have strides that are multiples of 16 bytes; bias any alignment of its type.
+ * Widths need not be multiples of anything.  What lies behind a row's last element is not used.
+ * residual may be y (forward) or d_x (backward) itself: same pointer and stride.
+ * d_work: ps_linear_backward_bytes, 256-byte aligned, used like ps_embed_backward's (may be 0). */
+enum { PS_ACT_NONE = 0, PS_ACT_RELU = 1, PS_ACT_GELU = 2 /* v Phi(v) */,
+       PS_ACT_GELU_TANH = 3 /* v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2 */, PS_ACT_SILU = 4 /* v / (1 + e^-v) */ };
+typedef struct {
+  uint64_t tokens;                 /* 0 .. 2^30                                           */
+  uint64_t inputs, outputs;        /* 1 .. 2^24                                           */
+  uint32_t dtype;                  /* PS_BF16 or PS_F16                                   */
+  uint32_t grad_dtype;             /* backward: of d_weight and d_bias: dtype or PS_F32   */
+  uint32_t activation;             /* PS_ACT_*                                            */
+  uint32_t below_activation;       /* backward, with `below`: PS_ACT_*                    */
+  uint32_t accumulate;             /* backward: 0 or 1                                    */
+  uint32_t pad;
+} ps_linear_desc;
+int ps_linear_forward(ps_ctx* ctx, const ps_linear_desc* desc, const ps_matrix* x, const ps_matrix* weight,
+                      const void* d_bias, const ps_matrix* residual, const ps_matrix* y, const ps_matrix* pre);
+uint64_t ps_linear_backward_bytes(const ps_linear_desc* desc);
+int ps_linear_backward(ps_ctx* ctx, const ps_linear_desc* desc, const ps_matrix* y_grad, const ps_matrix* x,
+                       const ps_matrix* weight, const ps_matrix* pre, const ps_matrix* below, const ps_matrix* residual,
+                       const ps_matrix* x_grad, const ps_matrix* weight_grad, void* d_bias_grad, void* d_work,
+                       uint64_t work_bytes);
+
 /* ------------------------------------------------------------------ measurement */
 /* Integer-pipe microbenchmark: `blocks` x 256 threads each run `iters` rounds
  * of 8 independent 32-bit add/logic chains of 16 operations.  Returns through

@@ -801,6 +801,238 @@ int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps
   return PS_OK;
 }
 
+// a matrix of the calls below: `step` is what its address and its rows' distance have to be multiples of, in elements
+static int take_matrix(const ps_matrix* m, u64 rows, u64 cols, u64 width, u64 step, ps_matrix& into) {
+  if (!m) return PS_E_NULLPTR;
+  into = *m;
+  if (rows == 0) return PS_OK;
+  if (!m->data) return PS_E_NULLPTR;
+  if (!aligned(m->data, step * width)) return PS_E_ALIGN;
+  if (rows == 1) {
+    into.stride = (cols + step - 1) / step * step;              // never multiplied by more than 0
+    return PS_OK;
+  }
+  if (m->stride % step) return PS_E_ALIGN;
+  if (m->stride < cols || m->stride > ((u64)1 << 40) / width / rows) return PS_E_RANGE;
+  return PS_OK;
+}
+static int take_optional(const ps_matrix* m, u64 rows, u64 cols, u64 width, u64 step, ps_matrix& into) {
+  into.data = nullptr, into.stride = 0;
+  return m ? take_matrix(m, rows, cols, width, step, into) : PS_OK;
+}
+// whether writing y is in the way of reading x, which may be the very same elements
+static bool spoils(const ps_matrix& y, const ps_matrix& x, u64 rows, u64 cols, u64 width) {
+  return x.data && overwrites(y.data, y.stride, x.data, x.stride, rows, cols, width);
+}
+
+static int norm_args(const ps_layer_norm_desc& d, NormArgs& a) {
+  if (d.rows > 0x7fffffffu || d.cols < 1 || d.cols > ((u64)1 << 20) || !(d.eps >= 0) || !std::isfinite((float)d.eps) || d.dtype > PS_F16 ||
+      d.grad_dtype > PS_F16 || d.accumulate > 1)
+    return PS_E_RANGE;
+  memset(&a, 0, sizeof(a));
+  a.rows = d.rows; a.cols = d.cols; a.eps = (float)d.eps;
+  a.grad_dtype = d.grad_dtype; a.accumulate = d.accumulate;
+  return PS_OK;
+}
+
+int ps_layer_norm_forward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps_matrix* x, const void* d_weight, const void* d_bias,
+                          const ps_matrix* y, float* d_mean, float* d_rstd) {
+  if (!ctx || !desc) return PS_E_NULLPTR;
+  NormArgs a;
+  int rc = norm_args(*desc, a);
+  if (rc != PS_OK) return rc;
+  const u64 width = desc->dtype == PS_F32 ? 4 : 2;
+  if ((rc = take_matrix(x, a.rows, a.cols, width, 1, a.x)) != PS_OK || (rc = take_matrix(y, a.rows, a.cols, width, 1, a.y)) != PS_OK) return rc;
+  if (!aligned(d_weight, width) || !aligned(d_bias, width) || !aligned(d_mean, 4) || !aligned(d_rstd, 4)) return PS_E_ALIGN;
+  if (a.rows == 0) return PS_OK;
+  if (spoils(a.y, a.x, a.rows, a.cols, width)) return PS_E_RANGE;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  a.weight = d_weight; a.bias = d_bias; a.mean = d_mean; a.rstd = d_rstd;
+  CUDA_OK(launch_norm_forward(desc->dtype, a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
+uint64_t ps_layer_norm_backward_bytes(const ps_layer_norm_desc* desc) {
+  NormArgs a;
+  return desc && norm_args(*desc, a) == PS_OK ? norm_backward_bytes(desc->dtype, a) : 0;
+}
+
+int ps_layer_norm_backward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps_matrix* y_grad, const ps_matrix* x, const float* d_mean,
+                           const float* d_rstd, const void* d_weight, const ps_matrix* residual, const ps_matrix* x_grad, void* d_weight_grad,
+                           void* d_bias_grad, void* d_work, uint64_t work_bytes) {
+  if (!ctx || !desc) return PS_E_NULLPTR;
+  NormArgs a;
+  int rc = norm_args(*desc, a);
+  if (rc != PS_OK) return rc;
+  const u64 width = desc->dtype == PS_F32 ? 4 : 2, grad_width = desc->grad_dtype == PS_F32 ? 4 : 2;
+  if ((rc = take_matrix(y_grad, a.rows, a.cols, width, 1, a.d_y)) != PS_OK || (rc = take_matrix(x, a.rows, a.cols, width, 1, a.x)) != PS_OK ||
+      (rc = take_optional(residual, a.rows, a.cols, width, 1, a.residual)) != PS_OK ||
+      (rc = take_matrix(x_grad, a.rows, a.cols, width, 1, a.d_x)) != PS_OK)
+    return rc;
+  const bool sums = d_weight_grad || d_bias_grad;
+  const u64 need = sums ? norm_backward_bytes(desc->dtype, a) : 0;
+  if ((a.rows && (!d_mean || !d_rstd)) || (need && !d_work)) return PS_E_NULLPTR;
+  if (!aligned(d_weight, width) || !aligned(d_mean, 4) || !aligned(d_rstd, 4) || !aligned(d_weight_grad, grad_width) ||
+      !aligned(d_bias_grad, grad_width) || !aligned(d_work, 256))
+    return PS_E_ALIGN;
+  if (work_bytes < need) return PS_E_RANGE;
+  if (a.rows && (spoils(a.d_x, a.d_y, a.rows, a.cols, width) || spoils(a.d_x, a.x, a.rows, a.cols, width) ||
+                 spoils(a.d_x, a.residual, a.rows, a.cols, width)))
+    return PS_E_RANGE;
+  if (a.rows == 0 && !sums) return PS_OK;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  a.weight = d_weight; a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
+  a.d_weight = d_weight_grad; a.d_bias = d_bias_grad;
+  a.parts = sums ? (float*)d_work : nullptr;
+  CUDA_OK(launch_norm_backward(desc->dtype, a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
+// heads of rotary positions: any alignment of the type, any strides; those that are written have none of 0
+static int take_any_heads(const ps_heads* h, u32 batch, u32 len, u32 heads, u64 width, bool written, ps_heads& into) {
+  if (!h || !h->data) return PS_E_NULLPTR;
+  if (!aligned(h->data, width)) return PS_E_ALIGN;
+  into = *h;
+  u64* strides[3] = {&into.batch_stride, &into.token_stride, &into.head_stride};
+  const u32 extents[3] = {batch, len, heads};
+  for (int i = 0; i < 3; ++i) {
+    if (extents[i] == 1) *strides[i] = 0;
+    else if ((written && *strides[i] == 0) || *strides[i] >= ((u64)1 << 38)) return PS_E_RANGE;
+  }
+  return PS_OK;
+}
+
+int ps_rotary(ps_ctx* ctx, const ps_rotary_desc* desc, const ps_heads* q, const ps_heads* q_out, const ps_heads* k, const ps_heads* k_out,
+              const void* d_positions) {
+  if (!ctx || !desc) return PS_E_NULLPTR;
+  const ps_rotary_desc& d = *desc;
+  if (d.batch > 65535 || d.len > (1u << 24) || d.heads < 1 || d.heads > 32768 || d.kv_heads > 32768 || d.dim < 2 || d.dim > 256 ||
+      d.rotary_dim < 2 || d.rotary_dim > d.dim || d.rotary_dim % 2 || d.dtype > PS_F16 || d.interleaved > 1 || d.inverse > 1 ||
+      (d.position_bytes != 4 && d.position_bytes != 8) || d.position_stride > ((u64)1 << 38) ||
+      (u64)d.batch * d.len * (d.heads + d.kv_heads) > ((u64)1 << 38))
+    return PS_E_RANGE;
+  if (!(d.base >= 1) || !std::isfinite(d.base) || !(d.factor >= 1) || !std::isfinite(d.factor) || !(d.original >= 0) || !std::isfinite(d.original) ||
+      !std::isfinite(d.low) || !std::isfinite(d.high) || (d.original > 0 && d.factor != 1 && !(d.low < d.high)) || !std::isfinite((float)d.magnitude))
+    return PS_E_RANGE;
+  if (d.batch == 0 || d.len == 0) return PS_OK;
+  RotaryArgs a;
+  memset(&a, 0, sizeof(a));
+  const u64 width = d.dtype == PS_F32 ? 4 : 2;
+  int rc;
+  if ((rc = take_any_heads(q, d.batch, d.len, d.heads, width, false, a.q)) != PS_OK ||
+      (rc = take_any_heads(q_out, d.batch, d.len, d.heads, width, true, a.q_out)) != PS_OK)
+    return rc;
+  if (d.kv_heads && ((rc = take_any_heads(k, d.batch, d.len, d.kv_heads, width, false, a.k)) != PS_OK ||
+                     (rc = take_any_heads(k_out, d.batch, d.len, d.kv_heads, width, true, a.k_out)) != PS_OK))
+    return rc;
+  if (!aligned(d_positions, d.position_bytes)) return PS_E_ALIGN;
+  const auto otherwise = [](const ps_heads& x, const ps_heads& y) {      // in the same place, but in another order
+    return x.data == y.data && (x.batch_stride != y.batch_stride || x.token_stride != y.token_stride || x.head_stride != y.head_stride);
+  };
+  if (otherwise(a.q, a.q_out) || (d.kv_heads && (otherwise(a.k, a.k_out) || a.k_out.data == a.q_out.data))) return PS_E_RANGE;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  a.positions = d_positions; a.position_stride = d.position_stride; a.position_bytes = d.position_bytes; a.first = d.first;
+  a.batch = d.batch; a.len = d.len; a.heads = d.heads; a.kv_heads = d.kv_heads; a.dim = d.dim; a.pairs = d.rotary_dim / 2;
+  a.interleaved = d.interleaved; a.inverse = d.inverse; a.magnitude = (float)d.magnitude;
+  // The frequencies, one from the other: 128 products in 64 bits of mantissa are off by less than 2^-56.
+  const long double turn = 6.283185307179586476925286766559L, step = powl((long double)d.base, -1.0L / a.pairs);
+  long double f = 1.0L;
+  for (u32 i = 0; i < a.pairs; ++i, f *= step) {
+    long double g = f;
+    if (d.factor != 1) {
+      long double s = 0;
+      if (d.original > 0) s = std::min(1.0L, std::max(0.0L, (d.original * f / turn - d.low) / ((long double)d.high - d.low)));
+      g = f * (s + (1 - s) / d.factor);
+    }
+    a.turns[i] = (u64)(g / turn * 18446744073709551616.0L + 0.5L);
+  }
+  CUDA_OK(launch_rotary(d.dtype, a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
+static int linear_args(const ps_linear_desc& d, LinearArgs& a) {
+  if (d.tokens > ((u64)1 << 30) || d.inputs < 1 || d.inputs > ((u64)1 << 24) || d.outputs < 1 || d.outputs > ((u64)1 << 24) ||
+      (d.dtype != PS_BF16 && d.dtype != PS_F16) || (d.grad_dtype != d.dtype && d.grad_dtype != PS_F32) || d.activation > PS_ACT_SILU ||
+      d.below_activation > PS_ACT_SILU || d.accumulate > 1)
+    return PS_E_RANGE;
+  if (d.tokens * std::max(d.inputs, d.outputs) > ((u64)1 << 39) || d.inputs * d.outputs > ((u64)1 << 38)) return PS_E_RANGE;
+  memset(&a, 0, sizeof(a));
+  a.tokens = d.tokens; a.inputs = d.inputs; a.outputs = d.outputs;
+  a.dtype = d.dtype; a.grad_dtype = d.grad_dtype; a.activation = d.activation; a.below_activation = d.below_activation;
+  a.accumulate = d.accumulate;
+  return PS_OK;
+}
+
+int ps_linear_forward(ps_ctx* ctx, const ps_linear_desc* desc, const ps_matrix* x, const ps_matrix* weight, const void* d_bias,
+                      const ps_matrix* residual, const ps_matrix* y, const ps_matrix* pre) {
+  if (!ctx || !desc) return PS_E_NULLPTR;
+  LinearArgs a;
+  int rc = linear_args(*desc, a);
+  if (rc != PS_OK) return rc;
+  if ((rc = take_matrix(x, a.tokens, a.inputs, 2, 8, a.x)) != PS_OK || (rc = take_matrix(weight, a.outputs, a.inputs, 2, 8, a.weight)) != PS_OK ||
+      (rc = take_optional(residual, a.tokens, a.outputs, 2, 8, a.residual)) != PS_OK ||
+      (rc = take_matrix(y, a.tokens, a.outputs, 2, 8, a.y)) != PS_OK || (rc = take_optional(pre, a.tokens, a.outputs, 2, 8, a.pre)) != PS_OK)
+    return rc;
+  if (!aligned(d_bias, 2)) return PS_E_ALIGN;
+  if (a.tokens == 0) return PS_OK;
+  if (spoils(a.y, a.residual, a.tokens, a.outputs, 2) || a.y.data == a.x.data || a.y.data == a.pre.data ||
+      (a.pre.data && (spoils(a.y, a.pre, a.tokens, a.outputs, 2) || a.pre.data == a.residual.data || spoils(a.pre, a.residual, a.tokens, a.outputs, 2))))
+    return PS_E_RANGE;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  a.bias = d_bias; a.status = ctx->h->status;
+  CUDA_OK(launch_linear_forward(a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
+uint64_t ps_linear_backward_bytes(const ps_linear_desc* desc) {
+  LinearArgs a;
+  return desc && linear_args(*desc, a) == PS_OK ? linear_backward_bytes(a) : 0;
+}
+
+int ps_linear_backward(ps_ctx* ctx, const ps_linear_desc* desc, const ps_matrix* y_grad, const ps_matrix* x, const ps_matrix* weight,
+                       const ps_matrix* pre, const ps_matrix* below, const ps_matrix* residual, const ps_matrix* x_grad,
+                       const ps_matrix* weight_grad, void* d_bias_grad, void* d_work, uint64_t work_bytes) {
+  if (!ctx || !desc) return PS_E_NULLPTR;
+  LinearArgs a;
+  int rc = linear_args(*desc, a);
+  if (rc != PS_OK) return rc;
+  const u64 grad_width = desc->grad_dtype == PS_F32 ? 4 : 2;
+  if ((rc = take_matrix(y_grad, a.tokens, a.outputs, 2, 8, a.d_y)) != PS_OK) return rc;
+  // (what a result needs is looked at only where that result is wanted)
+  if (a.activation && (rc = take_matrix(pre, a.tokens, a.outputs, 2, 8, a.pre)) != PS_OK) return rc;
+  if (x_grad && ((rc = take_matrix(weight, a.outputs, a.inputs, 2, 8, a.weight)) != PS_OK ||
+                 (a.below_activation && (rc = take_matrix(below, a.tokens, a.inputs, 2, 8, a.below)) != PS_OK) ||
+                 (rc = take_optional(residual, a.tokens, a.inputs, 2, 8, a.residual)) != PS_OK ||
+                 (rc = take_matrix(x_grad, a.tokens, a.inputs, 2, 8, a.d_x)) != PS_OK))
+    return rc;
+  if (weight_grad && ((rc = take_matrix(x, a.tokens, a.inputs, 2, 8, a.x)) != PS_OK ||
+                      (rc = take_matrix(weight_grad, a.outputs, a.inputs, grad_width, 16 / grad_width, a.d_weight)) != PS_OK))
+    return rc;
+  const u64 need = linear_backward_bytes(a);
+  if (need && !d_work) return PS_E_NULLPTR;
+  if (!aligned(d_bias_grad, grad_width) || !aligned(d_work, 256)) return PS_E_ALIGN;
+  if (work_bytes < need) return PS_E_RANGE;
+  if (x_grad && a.tokens && (spoils(a.d_x, a.residual, a.tokens, a.inputs, 2) || spoils(a.d_x, a.below, a.tokens, a.inputs, 2) ||
+                             a.d_x.data == a.d_y.data || a.d_x.data == a.x.data))
+    return PS_E_RANGE;
+  if (!x_grad && !weight_grad && !d_bias_grad) return PS_OK;
+  if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return PS_E_CUDA;
+  if (!x_grad || a.tokens == 0) a.d_x.data = nullptr;
+  a.d_bias = d_bias_grad; a.work = d_work; a.status = ctx->h->status;
+  CUDA_OK(launch_linear_backward(a, ctx->sm_count, ctx->stream));
+  return PS_OK;
+}
+
 // ------------------------------------------------------------------ measurement
 int ps_int_peak(ps_ctx* ctx, uint32_t blocks, uint32_t iters, uint32_t* d_sink, uint64_t* thread_ops) {
   if (!ctx || !d_sink || !thread_ops) return PS_E_NULLPTR;

@@ -162,3 +162,42 @@ cudaError_t launch_attention_forward(u32 dtype, const AttentionArgs& a, int sm_c
 size_t attention_forward_bytes(const AttentionArgs& a);
 size_t attention_backward_bytes(const AttentionArgs& a);
 cudaError_t launch_attention_backward(u32 dtype, const AttentionArgs& a, int sm_count, cudaStream_t stream);
+
+struct NormArgs {
+  ps_matrix x, y, d_y, residual, d_x;   // residual.data may be null
+  const void *weight, *bias;            // may be null
+  float *mean, *rstd;                   // forward: may be null
+  void *d_weight, *d_bias;              // may be null
+  u64 rows, cols;
+  float eps;
+  u32 grad_dtype, accumulate;
+  float* parts;                         // norm_backward_bytes; null without d_weight and d_bias
+};
+cudaError_t launch_norm_forward(u32 dtype, const NormArgs& a, int sm_count, cudaStream_t stream);
+size_t norm_backward_bytes(u32 dtype, const NormArgs& a);
+cudaError_t launch_norm_backward(u32 dtype, const NormArgs& a, int sm_count, cudaStream_t stream);
+
+constexpr int ROTARY_PAIRS = 128;
+struct RotaryArgs {
+  ps_heads q, q_out, k, k_out;
+  const void* positions;
+  u64 position_stride;
+  long long first;
+  u32 batch, len, heads, kv_heads, dim, pairs, position_bytes, interleaved, inverse;
+  float magnitude;
+  u64 turns[ROTARY_PAIRS];              // of a pair at a position: 2^-64 of a turn
+};
+cudaError_t launch_rotary(u32 dtype, const RotaryArgs& a, int sm_count, cudaStream_t stream);
+
+struct LinearArgs {
+  ps_matrix x, weight, y, pre, residual, below, d_y, d_x, d_weight;   // data null: not there
+  const void* bias;
+  void* d_bias;
+  u64 tokens, inputs, outputs;
+  u32 dtype, grad_dtype, activation, below_activation, accumulate;
+  void* work;                           // linear_backward_bytes
+  volatile u32* status;
+};
+cudaError_t launch_linear_forward(const LinearArgs& a, int sm_count, cudaStream_t stream);
+size_t linear_backward_bytes(const LinearArgs& a);
+cudaError_t launch_linear_backward(const LinearArgs& a, int sm_count, cudaStream_t stream);

@@ -1,0 +1,707 @@
+// The linear layer with what follows it, and its gradients: matrix products on the fifth-generation tensor cores.
+//
+//   y = act(x W^T + bias) + residual                       C[t][o], sum over the inputs:  both matrices lie along the sum
+//   dX = (dPre W) o act_below'(below) + residual           C[t][i], sum over the outputs: W lies across it
+//   dW = dPre^T x                                          C[o][i], sum over the tokens:  both lie across it
+//   dPre = dY o act'(pre),  dBias = sum_t dPre             elementwise and by columns, before the products
+//
+// One kernel does the three products.  A block (or a pair of blocks on two SMs, which share a tile of 256 x 256: each has
+// half of both operands, and reads half as much from the L2 as alone) walks over tiles of C; a warp copies operands
+// into a ring of shared memory, 64 columns of the sum at a time, a thread starts the products, whose sums stand in tensor memory twice
+// over, and eight warps bring a finished tile to memory while the next one is being summed: add the bias, activate, multiply, add, round.
+//
+// The sum over the inputs (outputs) is never cut, and goes in the same order in tiles of any size, so a row of y or dX does not
+// depend on what else the call computes.  The sum over the tokens is cut where dW has few tiles; a second kernel adds the parts in order.
+#include <algorithm>
+#include <atomic>
+#include "ps_columns.cuh"
+#include "ps_tensor.cuh"
+
+namespace {
+using namespace train;
+using namespace tensor;
+
+constexpr int STEP = 64;                  // of the sum, a stage of the ring
+constexpr int WRITERS = 8, COPY_WARP = 8, MMA_WARP = 9, THREADS = 320;
+constexpr u32 BUFFER = 32 * 128;          // a warp's 32 rows of 128 bytes on their way from or to memory
+constexpr u32 LEADER = 0xFEFFFFFFu;       // a shared-memory address, in the pair's first block
+
+// What is computed: which product, the type of its result, the tile's columns, and whether two blocks share it
+enum Kind { OUTPUT, INPUT_GRAD, WEIGHT_GRAD };
+template <class T_, class O_, Kind KIND_, int COLUMNS_, bool PAIR_>
+struct Form {
+  typedef T_ T;
+  typedef O_ O;
+  static constexpr Kind KIND = KIND_;
+  static constexpr int COLUMNS = COLUMNS_;
+  static constexpr bool PAIR = PAIR_;
+  static constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != OUTPUT;
+  static constexpr int B_ROWS = PAIR ? COLUMNS / 2 : COLUMNS;             // of this block
+  static constexpr u32 A_BYTES = ROWS * STEP * 2, B_BYTES = B_ROWS * STEP * 2, STAGE = A_BYTES + B_BYTES;
+  static constexpr u32 BUFFERS = WRITERS * 2 * BUFFER, AROUND = BUFFERS + WRITERS * 128 + 1024 + 256;   // (alignment, barriers)
+  static constexpr int STAGES = (int)((227 * 1024 - AROUND) / STAGE) < 8 ? (int)((227 * 1024 - AROUND) / STAGE) : 8;
+  static constexpr u32 SMEM = AROUND + STAGES * STAGE;
+  static constexpr u32 TMEM = 2 * COLUMNS;
+  static constexpr int CHUNK = 128 / sizeof(O);                           // columns of a buffer
+  static_assert(STAGES >= 3 && COLUMNS % CHUNK == 0 && TMEM <= 512 && SMEM > 116 * 1024, "");   // (one block an SM: it takes tensor memory alone)
+};
+
+struct Product {
+  u32 m, n, steps;                        // C's sizes, and stages of the sum
+  u32 m_tiles, n_tiles, splits, steps_each;
+  const void* bias;
+  u32 activation, below_activation;
+  u32 has_residual, has_below, has_pre;
+  volatile u32* status;
+};
+
+// ---- activations and their derivatives, in 32 bits.  (Exponentials and quotients with the fast functions' errors of a few 2^-23: what
+// follows is a rounding to 16 bits.)
+__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+constexpr float SQRT_HALF = 0.70710678f, TANH_FACTOR = 0.79788456f, TANH_CUBE = 0.044715f;
+template <int ACT>
+__device__ __forceinline__ float activated(float v) {
+  if (ACT == PS_ACT_RELU) return v > 0.f ? v : v != v ? v : 0.f;
+  if (ACT == PS_ACT_GELU) return 0.5f * v * (1.f + erff(v * SQRT_HALF));
+  if (ACT == PS_ACT_GELU_TANH) return v * sigmoid(2.f * TANH_FACTOR * fmaf(TANH_CUBE * v * v, v, v));
+  if (ACT == PS_ACT_SILU) return v * sigmoid(v);
+  return v;
+}
+template <int ACT>
+__device__ __forceinline__ float slope(float v) {
+  if (ACT == PS_ACT_RELU) return v > 0.f ? 1.f : 0.f;
+  if (ACT == PS_ACT_GELU) return fmaf(v * (0.5f * TANH_FACTOR), __expf(-0.5f * v * v), 0.5f * (1.f + erff(v * SQRT_HALF)));
+  if (ACT == PS_ACT_GELU_TANH) {
+    const float s = sigmoid(2.f * TANH_FACTOR * fmaf(TANH_CUBE * v * v, v, v));
+    return fmaf(v * s * (1.f - s), 2.f * TANH_FACTOR * fmaf(3.f * TANH_CUBE * v, v, 1.f), s);
+  }
+  if (ACT == PS_ACT_SILU) {
+    const float s = sigmoid(v);
+    return s * fmaf(v, 1.f - s, 1.f);
+  }
+  return 1.f;
+}
+template <int N>
+__device__ __forceinline__ void activate(u32 activation, float (&v)[N]) {
+#define PS_EACH(ACT)   \
+  if (activation == ACT) { _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] = activated<ACT>(v[e]); }
+  PS_EACH(PS_ACT_RELU) PS_EACH(PS_ACT_GELU) PS_EACH(PS_ACT_GELU_TANH) PS_EACH(PS_ACT_SILU)
+#undef PS_EACH
+}
+template <int N>
+__device__ __forceinline__ void times_slope(u32 activation, float (&v)[N], const float (&at)[N]) {
+#define PS_EACH(ACT)   \
+  if (activation == ACT) { _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] *= slope<ACT>(at[e]); }
+  PS_EACH(PS_ACT_RELU) PS_EACH(PS_ACT_GELU) PS_EACH(PS_ACT_GELU_TANH) PS_EACH(PS_ACT_SILU)
+#undef PS_EACH
+}
+
+// ---- a pair's instructions
+__device__ __forceinline__ u32 rank_in_pair() {
+  u32 r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ bool passed_in_pair(u32 bar, u32 parity) {
+  u32 ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ void arrive_at_leader(u32 bar) {
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void wait_for(Waiter& w, u32 bar, u32 parity) {
+  if (!PAIR) return w.wait(bar, parity);
+  if (w.dead || passed_in_pair(bar, parity)) return;
+  const u64 begin = now_ns();
+  while (!passed_in_pair(bar, parity))
+    if (now_ns() - begin > PATIENCE_NS) {
+      w.dead = true;
+      report(w.status, ST_TIMEOUT);
+      return;
+    }
+}
+
+// ---- copies of a box of two or three dimensions
+template <bool PAIR>
+__device__ __forceinline__ void load_box(u32 to, const CUtensorMap* map, int column, int row, u32 bar) {
+  if (PAIR)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(to), "l"(map), "r"(column), "r"(row), "r"(bar & LEADER) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(to), "l"(map), "r"(column), "r"(row), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void load_rows(u32 to, const CUtensorMap* map, int column, int row, u32 bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(to), "l"(map), "r"(column), "r"(row), "r"(0), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void store_rows(const CUtensorMap* map, int column, int row, int part, u32 from) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+               ::"l"(map), "r"(column), "r"(row), "r"(part), "r"(from) : "memory");
+}
+__device__ __forceinline__ void commit_stores() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void wait_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void wait_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// ---- products
+constexpr u32 ACROSS_PANEL = STEP * 128;          // bytes of 64 columns by 64 steps of a sum across them
+template <bool ACROSS>
+__device__ __forceinline__ u32 descriptor(u32 tile) {
+  return ((tile & 0x3FFFFu) >> 4) | (ACROSS ? (ACROSS_PANEL >> 4) << 16 : 1u << 16);
+}
+template <bool ACROSS>
+__device__ __forceinline__ constexpr u32 step_of(int s) { return ACROSS ? s * 128 : s * 2; }
+template <class F>
+__device__ __forceinline__ constexpr u32 instruction_of() {
+  return (1u << 4) | (Format<typename F::T>::code << 7) | (Format<typename F::T>::code << 10) | ((F::A_ACROSS ? 1u : 0u) << 15) |
+         ((F::B_ACROSS ? 1u : 0u) << 16) | ((u32)(F::COLUMNS >> 3) << 17) | ((u32)((F::PAIR ? 256 : 128) >> 4) << 24);
+}
+template <bool PAIR>
+__device__ __forceinline__ void multiply(u32 d, u32 a, u32 b, u32 ins, bool add) {
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(ins), "r"(DESC_HIGH), "r"(add ? 1u : 0u) : "memory");
+  else
+    mma_smem(d, a, b, ins, add);
+}
+// the barrier (of both blocks of a pair) is arrived at once the products started so far are done
+template <bool PAIR>
+__device__ __forceinline__ void commit_to(u32 bar) {
+  if (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
+  else
+    commit(bar);
+}
+template <bool PAIR>
+__device__ __forceinline__ void take_tmem(u32 to_smem, u32 columns) {
+  if (PAIR) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to_smem), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  } else {
+    tmem_alloc(to_smem, columns);
+  }
+}
+template <bool PAIR>
+__device__ __forceinline__ void leave_tmem(u32 at, u32 columns) {
+  if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+  else tmem_free(at, columns);
+}
+
+// Tiles in the order in which blocks take them: bands of BAND tiles of rows, in a band column by column, so that the tiles
+// that are summed at a time share their operands in the L2.
+constexpr u32 BAND = 8;
+struct Tile {
+  u32 m, n, part;
+};
+__device__ __forceinline__ Tile tile_at(const Product& p, u32 t) {
+  const u32 all = p.m_tiles * p.n_tiles, part = t / all;
+  t -= part * all;
+  const u32 band = t / (BAND * p.n_tiles), rest = t - band * BAND * p.n_tiles, height = min(BAND, p.m_tiles - band * BAND);
+  return {band * BAND + rest % height, rest / height, part};
+}
+
+__device__ __forceinline__ uint4 read16(u32 at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void write16(u32 at, u32 a, u32 b, u32 c, u32 d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// 32 columns of a lane's row in a buffer: in 16-byte pieces that are permuted by the row as the copies do it
+template <class E>
+__device__ __forceinline__ u32 piece_at(u32 row, int column, int i) {
+  const u32 piece = (u32)(column * (int)sizeof(E) / 16 + i);
+  return row * 128 + ((piece ^ (row & 7)) << 4);
+}
+template <class E>
+__device__ __forceinline__ void read32(u32 buffer, u32 row, int column, float (&v)[32]) {
+  constexpr int N = 16 / sizeof(E);
+#pragma unroll
+  for (int i = 0; i < 32 / N; ++i) {
+    const uint4 w = read16(buffer + piece_at<E>(row, column, i));
+    Pack<E, N> p;
+    p.w[0] = w.x, p.w[1] = w.y, p.w[2] = w.z, p.w[3] = w.w;
+    float f[N];
+    p.widen(f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[i * N + e] = f[e];
+  }
+}
+template <class E>
+__device__ __forceinline__ void write32(u32 buffer, u32 row, int column, const float (&v)[32]) {
+  constexpr int N = 16 / sizeof(E);
+#pragma unroll
+  for (int i = 0; i < 32 / N; ++i) {
+    float f[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = v[i * N + e];
+    Pack<E, N> p;
+    p.narrow(f);
+    write16(buffer + piece_at<E>(row, column, i), p.w[0], p.w[1], p.w[2], p.w[3]);
+  }
+}
+
+struct Maps {
+  CUtensorMap a, b, out, residual, more;        // more: pre, written, or below, read
+};
+
+template <class F>
+__global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Maps maps, const Product p) {
+  typedef typename F::T T;
+  typedef typename F::O O;
+  constexpr bool PAIR = F::PAIR;
+  constexpr int STAGES = F::STAGES, CHUNK = F::CHUNK;
+  extern __shared__ unsigned char raw[];
+  const u32 base = (smem_address(raw) + 1023u) & ~1023u;
+  const u32 ring = base, buffers = ring + STAGES * F::STAGE, biases = buffers + F::BUFFERS, bars = biases + WRITERS * 128;
+  // barriers: full and empty of each stage, full and empty of each sum, a writer's input
+  const auto full = [&](int s) { return bars + 8 * s; };
+  const auto empty = [&](int s) { return bars + 8 * (STAGES + s); };
+  const auto sum_full = [&](int s) { return bars + 8 * (2 * STAGES + s); };
+  const auto sum_empty = [&](int s) { return bars + 8 * (2 * STAGES + 2 + s); };
+  const auto input = [&](int w) { return bars + 8 * (2 * STAGES + 4 + w); };
+  __shared__ u32 tmem_at;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const u32 rank = PAIR ? rank_in_pair() : 0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) barrier_init(full(s), 1), barrier_init(empty(s), 1);
+    for (int s = 0; s < 2; ++s) barrier_init(sum_full(s), 1), barrier_init(sum_empty(s), WRITERS * (PAIR ? 2 : 1));
+    for (int w = 0; w < WRITERS; ++w) barrier_init(input(w), 1);
+    fence_barrier_init();
+  }
+  if (warp == MMA_WARP) take_tmem<PAIR>(smem_address(&tmem_at), F::TMEM);
+  fence_before();
+  __syncthreads();
+  if (PAIR) pair_sync();
+  fence_after();
+  const u32 tmem = tmem_at;
+
+  const u32 tiles = p.m_tiles * p.n_tiles * p.splits;
+  const u32 first = PAIR ? blockIdx.x / 2 : blockIdx.x, stride = PAIR ? gridDim.x / 2 : gridDim.x;
+  Waiter waiter(p.status);
+
+  if (warp == COPY_WARP) {
+    if (elected()) {
+      u32 turn = 0;                                 // stages filled so far
+      for (u32 t = first; t < tiles && !waiter.dead; t += stride) {
+        const Tile tile = tile_at(p, t);
+        const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS), column = (int)(tile.n * F::COLUMNS + rank * F::B_ROWS);
+        const u32 begin = tile.part * p.steps_each, end = min(begin + p.steps_each, p.steps);
+        for (u32 k = begin; k < end; ++k, ++turn) {
+          const int s = turn % STAGES;
+          wait_for<PAIR>(waiter, empty(s), (turn / STAGES + 1) & 1);
+          if (waiter.dead) break;
+          if (rank == 0) barrier_expect(full(s), (PAIR ? 2 : 1) * F::STAGE);
+          const u32 a = ring + s * F::STAGE, b = a + F::A_BYTES;
+          const int at = (int)(k * STEP);
+          if (F::A_ACROSS) {
+#pragma unroll
+            for (int i = 0; i < ROWS / 64; ++i) load_box<PAIR>(a + i * ACROSS_PANEL, &maps.a, row + 64 * i, at, full(s));
+          } else {
+            load_box<PAIR>(a, &maps.a, at, row, full(s));
+          }
+          if (F::B_ACROSS) {
+#pragma unroll
+            for (int i = 0; i < F::B_ROWS / 64; ++i) load_box<PAIR>(b + i * ACROSS_PANEL, &maps.b, column + 64 * i, at, full(s));
+          } else {
+            load_box<PAIR>(b, &maps.b, at, column, full(s));
+          }
+        }
+      }
+      if (rank == 0) {                              // leave no copy in flight, also where a wait has run out
+        Waiter last(p.status);
+        for (u32 i = turn > STAGES ? turn - STAGES : 0; i < turn; ++i) wait_for<PAIR>(last, full(i % STAGES), (i / STAGES) & 1);
+      }
+    }
+    __syncwarp();
+  } else if (warp == MMA_WARP) {
+    if (rank == 0 && elected()) {
+      constexpr u32 ins = instruction_of<F>();
+      u32 turn = 0, count = 0;
+      for (u32 t = first; t < tiles && !waiter.dead; t += stride, ++count) {
+        const u32 part = tile_at(p, t).part;
+        const u32 begin = part * p.steps_each, end = min(begin + p.steps_each, p.steps);
+        const u32 d = tmem + (count & 1) * F::COLUMNS;
+        wait_for<PAIR>(waiter, sum_empty(count & 1), (count / 2 + 1) & 1);
+        fence_after();
+        for (u32 k = begin; k < end && !waiter.dead; ++k, ++turn) {
+          const int s = turn % STAGES;
+          wait_for<PAIR>(waiter, full(s), (turn / STAGES) & 1);
+          if (waiter.dead) break;
+          fence_after();
+          const u32 a = descriptor<F::A_ACROSS>(ring + s * F::STAGE), b = descriptor<F::B_ACROSS>(ring + s * F::STAGE + F::A_BYTES);
+#pragma unroll
+          for (int i = 0; i < STEP / 16; ++i) multiply<PAIR>(d, a + step_of<F::A_ACROSS>(i), b + step_of<F::B_ACROSS>(i), ins, k > begin || i > 0);
+          commit_to<PAIR>(empty(s));
+        }
+        if (!waiter.dead) commit_to<PAIR>(sum_full(count & 1));
+      }
+    }
+    __syncwarp();
+  } else {
+    const u32 mine = buffers + warp * 2 * BUFFER, other = mine + BUFFER;       // result and residual; pre or below
+    const u32 bias_at = biases + warp * 128;
+    const int quarter = warp % 4, half = warp / 4;
+    u32 count = 0, inputs = 0;
+    for (u32 t = first; t < tiles; t += stride, ++count) {
+      const Tile tile = tile_at(p, t);
+      const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS + quarter * 32);
+      bool waited = false;
+#pragma unroll 1
+      for (int c = half; c < F::COLUMNS / CHUNK; c += 2) {
+        const int column = (int)(tile.n * F::COLUMNS + c * CHUNK);
+        if (row >= (int)p.m || column >= (int)p.n || waiter.dead) continue;
+        const bool reads = p.has_residual || (F::KIND == INPUT_GRAD && p.has_below);
+        if (lane == 0) {
+          wait_stores_read();                       // the buffers' last results have left
+          if (reads) {
+            barrier_expect(input(warp), ((p.has_residual ? 1 : 0) + (F::KIND == INPUT_GRAD && p.has_below ? 1 : 0)) * BUFFER);
+            if (p.has_residual) load_rows(mine, &maps.residual, column, row, input(warp));
+            if (F::KIND == INPUT_GRAD && p.has_below) load_rows(other, &maps.more, column, row, input(warp));
+          }
+        }
+        if (F::KIND == OUTPUT && p.bias) {
+#pragma unroll
+          for (int i = lane; i < CHUNK; i += 32) {
+            const unsigned short v = column + i < (int)p.n ? ((const unsigned short*)p.bias)[column + i] : (unsigned short)0;
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(bias_at + 2 * i), "h"(v) : "memory");
+          }
+        }
+        __syncwarp();
+        if (!waited) {
+          wait_for<PAIR>(waiter, sum_full(count & 1), (count / 2) & 1);
+          fence_after();
+          waited = true;
+        }
+        if (reads) wait_for<false>(waiter, input(warp), inputs++ & 1);
+        waiter.dead = __any_sync(0xffffffffu, waiter.dead);      // (the lanes go on together)
+        if (waiter.dead) continue;
+#pragma unroll
+        for (int h = 0; h < CHUNK; h += 32) {
+          u32 sum[32];
+          tmem_load32(sum, tmem + ((u32)(quarter * 32) << 16) + (count & 1) * F::COLUMNS + c * CHUNK + h);
+          wait_loads();
+          float v[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]);
+          if (F::KIND == OUTPUT) {
+            if (p.bias)
+#pragma unroll
+              for (int e = 0; e < 32; e += 8) {
+                const uint4 w = read16(bias_at + 2 * (h + e));
+                Pack<T, 8> b;
+                b.w[0] = w.x, b.w[1] = w.y, b.w[2] = w.z, b.w[3] = w.w;
+                float f[8];
+                b.widen(f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[e + i] += f[i];
+              }
+            if (p.has_pre) write32<T>(other, lane, h, v);
+            activate(p.activation, v);
+          }
+          float f[32];
+          if (F::KIND == INPUT_GRAD && p.has_below) {
+            read32<T>(other, lane, h, f);
+            times_slope(p.below_activation, v, f);
+          }
+          if (p.has_residual) {
+            read32<O>(mine, lane, h, f);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] += f[e];
+          }
+          write32<O>(mine, lane, h, v);
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) {
+          store_rows(&maps.out, column, row, (int)tile.part, mine);
+          if (F::KIND == OUTPUT && p.has_pre) store_rows(&maps.more, column, row, 0, other);
+          commit_stores();
+        }
+      }
+      if (!waited) {                                // (nothing of this tile is this warp's: it says so in turn all the same)
+        wait_for<PAIR>(waiter, sum_full(count & 1), (count / 2) & 1);
+        fence_after();
+      }
+      waiter.dead = __any_sync(0xffffffffu, waiter.dead);
+      fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (PAIR) arrive_at_leader(sum_empty(count & 1));
+        else barrier_arrive(sum_empty(count & 1));
+      }
+    }
+    if (lane == 0) wait_stores_done();
+    __syncwarp();
+  }
+  fence_before();
+  __syncthreads();
+  if (PAIR) pair_sync();                            // neither block leaves while the other's products read its memory
+  fence_after();
+  if (warp == MMA_WARP) leave_tmem<PAIR>(tmem, F::TMEM);
+}
+
+// ---- dW out of the parts of a sum that was cut: parts[splits][m][pitch], added in order
+template <class O>
+__global__ void __launch_bounds__(256) k_join_parts(const float* parts, u32 splits, u64 m, u32 n, u32 pitch, O* out, u64 stride, u32 accumulate) {
+  const u32 c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= n) return;
+  for (u64 r = blockIdx.y; r < m; r += gridDim.y) {
+    float sum = 0.f;
+#pragma unroll 4
+    for (u32 s = 0; s < splits; ++s) sum += parts[(s * m + r) * pitch + c];
+    O* const to = out + r * stride + c;
+    *to = narrow<O>(sum + (accumulate ? widen(*to) : 0.f));
+  }
+}
+
+// ---- dPre = dY o act'(pre), and its sums by columns: a warp has 256 columns, 8 a lane, a block eight rows at a time
+constexpr int SLOPE_COLUMNS = 256, SLOPE_WARPS = 8;
+template <class T>
+__global__ void __launch_bounds__(SLOPE_WARPS * 32) k_slope(const ps_matrix d_y, const ps_matrix pre, const ps_matrix d_pre, u64 rows, u32 cols,
+                                                           u64 rows_each, u32 activation, float* parts) {
+  __shared__ float sums[SLOPE_WARPS][SLOPE_COLUMNS];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const u32 column = blockIdx.x * SLOPE_COLUMNS + lane * 8;
+  const int here = column >= cols ? 0 : (int)min(8u, cols - column);
+  const u64 begin = blockIdx.y * rows_each, end = begin + rows_each < rows ? begin + rows_each : rows;
+  float sum[8] = {};
+  const auto load = [&](const T* from, Pack<T, 8>& p) {
+    p.clear();
+    if (here == 8) p.load(from);
+    else
+      for (int e = 0; e < here; ++e) p.w[e / 2] |= (u32)*reinterpret_cast<const unsigned short*>(from + e) << (16 * (e % 2));
+  };
+  if (here > 0)
+#pragma unroll 2
+    for (u64 r = begin + warp; r < end; r += SLOPE_WARPS) {
+      Pack<T, 8> g, at;
+      load((const T*)d_y.data + r * d_y.stride + column, g);
+      float v[8];
+      if (activation) {
+        load((const T*)pre.data + r * pre.stride + column, at);
+        float x[8];
+        g.widen(v);
+        at.widen(x);
+        times_slope(activation, v, x);
+        g.narrow(v);
+        T* const to = (T*)d_pre.data + r * d_pre.stride + column;
+        if (here == 8) g.store(to);
+        else
+          for (int e = 0; e < here; ++e) reinterpret_cast<unsigned short*>(to)[e] = (unsigned short)(g.w[e / 2] >> (16 * (e % 2)));
+      } else {
+        g.widen(v);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += v[e];
+    }
+  if (parts == nullptr) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[warp][lane * 8 + e] = sum[e];
+  __syncthreads();
+  const u32 c = blockIdx.x * SLOPE_COLUMNS + threadIdx.x;
+  if (c >= cols) return;
+  float all = 0.f;
+#pragma unroll
+  for (int w = 0; w < SLOPE_WARPS; ++w) all += sums[w][threadIdx.x];
+  parts[(u64)blockIdx.y * cols + c] = all;
+}
+
+// ------------------------------------------------------------------ host
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encoder() {
+  static const EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return (EncodeTiled)p;
+  }();
+  return f;
+}
+// a matrix as boxes of 128 bytes by `box_rows`; as one of `parts` matrices behind one another where it is written or read by warps
+template <class E>
+bool encode(CUtensorMap& map, u32 dtype, const ps_matrix& m, u64 rows, u64 cols, u32 box_rows, u32 parts) {
+  const cuuint64_t stride = rows > 1 ? m.stride * sizeof(E) : (cols * sizeof(E) + 15) / 16 * 16;
+  const cuuint64_t extents[3] = {cols, rows, parts ? parts : 1}, strides[2] = {stride, stride * rows};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / sizeof(E)), box_rows, 1}, steps[3] = {1, 1, 1};
+  const CUtensorMapDataType type = sizeof(E) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == PS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return encoder()(&map, type, parts ? 3 : 2, m.data, extents, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// C[m][n] = sum over k of A B, and what is done with it
+struct Call {
+  Kind kind;
+  ps_matrix a, b, out, residual, more;
+  u64 m, n, k;
+  u32 parts;                              // of the sum, stored one behind the other
+  const void* bias;
+  u32 activation, below_activation;
+};
+
+template <class F>
+cudaError_t product(u32 dtype, const Call& c, volatile u32* status, int sm_count, cudaStream_t stream) {
+  typedef typename F::T T;
+  typedef typename F::O O;
+  Maps maps = {};
+  Product p = {};
+  p.m = (u32)c.m, p.n = (u32)c.n, p.steps = (u32)((c.k + STEP - 1) / STEP);
+  p.m_tiles = (u32)((c.m + (F::PAIR ? 255 : 127)) / (F::PAIR ? 256 : 128));
+  p.n_tiles = (u32)((c.n + F::COLUMNS - 1) / F::COLUMNS);
+  p.steps_each = (p.steps + c.parts - 1) / c.parts;
+  p.splits = (p.steps + p.steps_each - 1) / p.steps_each;
+  p.bias = c.bias;
+  p.activation = c.activation, p.below_activation = c.below_activation;
+  p.has_residual = c.residual.data != nullptr;
+  p.has_below = F::KIND == INPUT_GRAD && c.more.data;
+  p.has_pre = F::KIND == OUTPUT && c.more.data;
+  p.status = status;
+  bool ok = F::A_ACROSS ? encode<T>(maps.a, dtype, c.a, c.k, c.m, STEP, 0) : encode<T>(maps.a, dtype, c.a, c.m, c.k, ROWS, 0);
+  ok = ok && (F::B_ACROSS ? encode<T>(maps.b, dtype, c.b, c.k, c.n, STEP, 0) : encode<T>(maps.b, dtype, c.b, c.n, c.k, F::B_ROWS, 0));
+  ok = ok && encode<O>(maps.out, dtype, c.out, c.m, c.n, 32, c.parts);
+  if (p.has_residual) ok = ok && encode<O>(maps.residual, dtype, c.residual, c.m, c.n, 32, 1);
+  if (c.more.data) ok = ok && encode<T>(maps.more, dtype, c.more, c.m, c.n, 32, 1);
+  if (!ok) return cudaErrorInvalidValue;
+  static std::atomic<u64> prepared{0};                      // devices on which the kernel's shared memory has been asked for
+  int device;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  if (device >= 64 || !(prepared.load() >> device & 1)) {
+    e = cudaFuncSetAttribute(k_product<F>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::SMEM);
+    if (e != cudaSuccess) return e;
+    if (device < 64) prepared |= (u64)1 << device;
+  }
+  const u64 tiles = (u64)p.m_tiles * p.n_tiles * p.splits;
+  if (tiles > 0x7fffffffu) return cudaErrorInvalidValue;
+  cudaLaunchAttribute pair;
+  pair.id = cudaLaunchAttributeClusterDimension;
+  pair.val.clusterDim.x = 2, pair.val.clusterDim.y = pair.val.clusterDim.z = 1;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3(F::PAIR ? 2 * (u32)std::min<u64>(tiles, sm_count / 2) : (u32)std::min<u64>(tiles, sm_count));
+  config.blockDim = dim3(THREADS);
+  config.dynamicSmemBytes = F::SMEM;
+  config.stream = stream;
+  config.attrs = &pair;
+  config.numAttrs = F::PAIR ? 1 : 0;
+  return cudaLaunchKernelEx(&config, k_product<F>, maps, p);
+}
+
+// Tiles of 256 x 256 by pairs where they fill the device, else of 128 x 128, or 128 x 64 where there are few.
+template <class T, class O, Kind KIND>
+cudaError_t product_of(u32 dtype, const Call& c, volatile u32* status, int sm_count, cudaStream_t stream) {
+  const auto tiles = [&](u64 m, u64 n) { return ((c.m + m - 1) / m) * ((c.n + n - 1) / n) * c.parts; };
+  if (tiles(256, 256) >= (u64)sm_count / 2) return product<Form<T, O, KIND, 256, true>>(dtype, c, status, sm_count, stream);
+  if (tiles(128, 128) >= (u64)sm_count / 2) return product<Form<T, O, KIND, 128, false>>(dtype, c, status, sm_count, stream);
+  return product<Form<T, O, KIND, 64, false>>(dtype, c, status, sm_count, stream);
+}
+
+constexpr ps_matrix NOTHING = {nullptr, 0};
+constexpr u64 SMS = 148;          // (what a sum's order depends on does not ask the device)
+
+// parts of the sum over the tokens for dW: as many as bring tiles for all SMs, each of 16 stages at least
+u32 weight_parts(const LinearArgs& a) {
+  const u64 tiles = ((a.outputs + 127) / 128) * ((a.inputs + 127) / 128), steps = (a.tokens + STEP - 1) / STEP;
+  const u64 parts = std::min(std::max<u64>(1, SMS / tiles), std::max<u64>(1, steps / 16));
+  if (parts == 1) return 1;
+  const u64 each = (steps + parts - 1) / parts;
+  return (u32)((steps + each - 1) / each);
+}
+u64 up(u64 n, u64 to) { return (n + to - 1) / to * to; }
+// chunks of rows for the sums by columns
+u64 slope_chunks(const LinearArgs& a) {
+  const u64 across = (a.outputs + SLOPE_COLUMNS - 1) / SLOPE_COLUMNS;
+  return std::max<u64>(1, std::min<u64>((a.tokens + 31) / 32, (6 * SMS + across - 1) / across));
+}
+struct Work {
+  size_t d_pre, sums, parts, all;
+};
+Work work_of(const LinearArgs& a) {
+  Work w;
+  w.d_pre = 0;
+  w.sums = a.activation ? up(a.tokens * up(a.outputs, 8) * 2, 256) : 0;
+  w.parts = w.sums + up(slope_chunks(a) * a.outputs * 4, 256);
+  const u32 parts = weight_parts(a);
+  w.all = w.parts + (parts > 1 ? parts * a.outputs * up(a.inputs, 4) * 4 : 0);
+  return w;
+}
+
+template <class T>
+cudaError_t forward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
+  Call c = {OUTPUT, a.x, a.weight, a.y, a.residual, a.pre, a.tokens, a.outputs, a.inputs, 1, a.bias, a.activation, 0};
+  return product_of<T, T, OUTPUT>(a.dtype, c, a.status, sm_count, stream);
+}
+
+template <class T>
+cudaError_t backward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
+  const Work w = work_of(a);
+  char* const work = (char*)a.work;
+  ps_matrix d_pre = a.d_y;
+  const bool products = a.d_x.data || a.d_weight.data;
+  if (a.activation || a.d_bias) {
+    float* const sums = a.d_bias ? (float*)(work + w.sums) : nullptr;
+    if (a.activation) d_pre = {work + w.d_pre, up(a.outputs, 8)};
+    const u64 chunks = slope_chunks(a), each = (a.tokens + chunks - 1) / chunks;
+    k_slope<T><<<dim3((u32)((a.outputs + SLOPE_COLUMNS - 1) / SLOPE_COLUMNS), (u32)chunks), SLOPE_WARPS * 32, 0, stream>>>(
+        a.d_y, a.pre, d_pre, a.tokens, (u32)a.outputs, each, a.activation, sums);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess && sums) e = join_columns(a.grad_dtype, sums, (u32)chunks, 1, a.outputs, a.d_bias, nullptr, a.accumulate, stream);
+    if (e != cudaSuccess || !products) return e;
+  }
+  if (a.d_x.data && a.tokens) {
+    const Call c = {INPUT_GRAD, d_pre, a.weight, a.d_x, a.residual, a.below, a.tokens, a.inputs, a.outputs, 1, nullptr, 0, a.below_activation};
+    const cudaError_t e = product_of<T, T, INPUT_GRAD>(a.dtype, c, a.status, sm_count, stream);
+    if (e != cudaSuccess) return e;
+  }
+  if (a.d_weight.data && a.tokens == 0) {
+    if (a.accumulate) return cudaSuccess;
+    const size_t width = a.grad_dtype == PS_F32 ? 4 : 2;
+    return cudaMemset2DAsync(a.d_weight.data, a.d_weight.stride * width, 0, a.inputs * width, a.outputs, stream);
+  }
+  if (a.d_weight.data) {
+    const u32 parts = weight_parts(a);
+    Call c = {WEIGHT_GRAD, d_pre, a.x, a.d_weight, a.accumulate ? a.d_weight : NOTHING, NOTHING, a.outputs, a.inputs, a.tokens, parts, nullptr, 0, 0};
+    if (parts == 1)
+      return a.grad_dtype == PS_F32 ? product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream)
+                                    : product_of<T, T, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
+    const u32 pitch = (u32)up(a.inputs, 4);
+    c.out = {work + w.parts, pitch};
+    c.residual = NOTHING;
+    cudaError_t e = product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((u32)((a.inputs + 255) / 256), (u32)std::min<u64>(a.outputs, 65535));
+    const float* const from = (const float*)(work + w.parts);
+    if (a.grad_dtype == PS_F32) k_join_parts<float><<<grid, 256, 0, stream>>>(from, parts, a.outputs, (u32)a.inputs, pitch, (float*)a.d_weight.data, a.d_weight.stride, a.accumulate);
+    else k_join_parts<T><<<grid, 256, 0, stream>>>(from, parts, a.outputs, (u32)a.inputs, pitch, (T*)a.d_weight.data, a.d_weight.stride, a.accumulate);
+    return cudaGetLastError();
+  }
+  return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t launch_linear_forward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
+  if (!encoder()) return cudaErrorNotSupported;
+  return a.dtype == PS_BF16 ? forward<__nv_bfloat16>(a, sm_count, stream) : forward<__half>(a, sm_count, stream);
+}
+
+size_t linear_backward_bytes(const LinearArgs& a) { return work_of(a).all; }
+
+cudaError_t launch_linear_backward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
+  if (!encoder()) return cudaErrorNotSupported;
+  return a.dtype == PS_BF16 ? backward<__nv_bfloat16>(a, sm_count, stream) : backward<__half>(a, sm_count, stream);
+}

@@ -53,7 +53,9 @@ EXPORTS = ("ps_create", "ps_destroy", "ps_status", "ps_strerror", "ps_space_crea
            "ps_space_points_per_model", "ps_space_decode", "ps_eval_batch", "ps_sweep_pareto",
            "ps_check_composition", "ps_int_peak", "ps_eval_compact_noalloc", "ps_select",
            "ps_verify_batch", "ps_select_compare", "ps_dropout", "ps_embed_forward", "ps_embed_backward_bytes",
-           "ps_embed_backward", "ps_attention_forward", "ps_attention_forward_bytes", "ps_attention_backward_bytes", "ps_attention_backward")
+           "ps_embed_backward", "ps_attention_forward", "ps_attention_forward_bytes", "ps_attention_backward_bytes", "ps_attention_backward",
+           "ps_layer_norm_forward", "ps_layer_norm_backward_bytes", "ps_layer_norm_backward", "ps_rotary", "ps_linear_forward",
+           "ps_linear_backward_bytes", "ps_linear_backward")
 
 
 class _SpaceDesc(C.Structure):
@@ -95,12 +97,17 @@ VERIFY_RESULT_DTYPE = np.dtype([("mem", "<u8"), ("comm", "<u8"), ("host", "<u8")
                                 ("pad", "<u4"), ("max_rel_err", "<f8")])
 
 
-# The training step's descriptors (ps_dropout_desc, ps_embed_desc, ps_heads, ps_attention_shape) as bytes: a ctypes
+# The training step's descriptors (ps_dropout_desc, ps_embed_desc, ps_heads, ps_attention_shape, ...) as bytes: a ctypes
 # Structure of as many fields takes a call several microseconds longer.
 _DROPOUT_DESC = struct.Struct("9QdII").pack
 _EMBED_DESC = struct.Struct("6Qd4I").pack
 _HEADS = struct.Struct("4Q").pack
 _ATTENTION_SHAPE = struct.Struct("8IfI").pack
+_MATRIX = struct.Struct("2Q").pack
+_LAYER_NORM_DESC = struct.Struct("2Qd4I").pack
+_ROTARY_DESC = struct.Struct("10IQq6d").pack
+_LINEAR_DESC = struct.Struct("3Q6I").pack
+ACTIVATIONS = {"none": 0, None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}   # PS_ACT_*
 _FLOAT_MOST = torch.finfo(torch.float32).max
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # PS_F32, PS_BF16, PS_F16
 
@@ -154,6 +161,15 @@ _lib.ps_attention_forward_bytes.restype = C.c_uint64
 _lib.ps_attention_backward_bytes.argtypes = [C.c_void_p]
 _lib.ps_attention_backward_bytes.restype = C.c_uint64
 _lib.ps_attention_backward.argtypes = [C.c_void_p] * 14 + [C.c_uint64]
+_lib.ps_layer_norm_forward.argtypes = [C.c_void_p] * 8
+_lib.ps_layer_norm_backward_bytes.argtypes = [C.c_void_p]
+_lib.ps_layer_norm_backward_bytes.restype = C.c_uint64
+_lib.ps_layer_norm_backward.argtypes = [C.c_void_p] * 12 + [C.c_uint64]
+_lib.ps_rotary.argtypes = [C.c_void_p] * 7
+_lib.ps_linear_forward.argtypes = [C.c_void_p] * 8
+_lib.ps_linear_backward_bytes.argtypes = [C.c_void_p]
+_lib.ps_linear_backward_bytes.restype = C.c_uint64
+_lib.ps_linear_backward.argtypes = [C.c_void_p] * 12 + [C.c_uint64]
 _lib.ps_int_peak.argtypes = [C.c_void_p, C.c_uint32, C.c_uint32, C.c_void_p,
                              C.POINTER(C.c_uint64)]
 
@@ -530,6 +546,210 @@ class Context:
     def attention_backward_bytes(batch: int, q_len: int, k_len: int, heads: int, kv_heads: int, dim: int) -> int:
         """Bytes of the work buffer that attention_backward_into takes."""
         return _lib.ps_attention_backward_bytes(_ATTENTION_SHAPE(batch, q_len, k_len, heads, kv_heads, dim, 1, 0, 1.0, 0))
+
+    def _matrix(self, t: torch.Tensor | None, where: str, name: str, shape, dtype) -> bytes | None:
+        if t is None:
+            return None
+        return _MATRIX(t.data_ptr(), self._row_stride(t, where, name, shape, dtype))
+
+    def _vector(self, t: torch.Tensor | None, where: str, name: str, n: int, dtype) -> int | None:
+        if t is None:
+            return None
+        if t.shape != (n,) or t.dtype != dtype or t.get_device() != self.device or (n > 1 and t.stride(0) != 1):
+            self._refuse(E_RANGE, where, f"{name} has to be {n} contiguous {dtype} on device {self.device}")
+        return t.data_ptr()
+
+    def _rows(self, x: torch.Tensor, where: str, name: str):
+        if x.dim() != 2 or x.dtype not in _DTYPE:
+            self._refuse(E_RANGE, where, f"{name} has to be [rows, cols] of float32, bfloat16 or float16")
+        return x.shape
+
+    def _finite(self, where: str, name: str, value: float):
+        if not -_FLOAT_MOST <= value <= _FLOAT_MOST:
+            self._refuse(E_RANGE, where, name)
+
+    def layer_norm_forward_into(self, x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor | None = None,
+                                bias: torch.Tensor | None = None, eps: float = 1e-5, mean: torch.Tensor | None = None,
+                                rstd: torch.Tensor | None = None):
+        """ps_layer_norm_forward on [rows, cols]; `mean` and `rstd`, float32 [rows], are written where they are given.  y may be x."""
+        where, dtype = "ps_layer_norm_forward", x.dtype
+        rows, cols = shape = self._rows(x, where, "x")
+        self._finite(where, "eps", eps)
+        self._enqueue(where, _lib.ps_layer_norm_forward, _LAYER_NORM_DESC(rows, cols, eps, _DTYPE[dtype], 0, 0, 0),
+                      self._matrix(x, where, "x", shape, dtype), self._vector(weight, where, "weight", cols, dtype),
+                      self._vector(bias, where, "bias", cols, dtype), self._matrix(y, where, "y", shape, dtype),
+                      self._vector(mean, where, "mean", rows, torch.float32), self._vector(rstd, where, "rstd", rows, torch.float32))
+
+    def layer_norm_forward(self, x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                           eps: float = 1e-5):
+        """(y [rows, cols], mean [rows], rstd [rows])."""
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        mean, rstd = x.new_empty((2, x.shape[0]), dtype=torch.float32).unbind()
+        self.layer_norm_forward_into(x, y, weight, bias, eps, mean, rstd)
+        return y, mean, rstd
+
+    def layer_norm_backward_into(self, d_y: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, d_x: torch.Tensor,
+                                 weight: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                                 d_weight: torch.Tensor | None = None, d_bias: torch.Tensor | None = None, accumulate: bool = False,
+                                 work: torch.Tensor | None = None):
+        """ps_layer_norm_backward: the gradient of x, plus `residual`, to d_x (which may be d_y, x or residual), and those of
+        weight and bias where they are given, written or (accumulate) added to.
+        `work`: a uint8 buffer of layer_norm_backward_bytes; without it one is allocated for a call that needs it."""
+        where, dtype = "ps_layer_norm_backward", x.dtype
+        rows, cols = shape = self._rows(x, where, "x")
+        sums = d_weight if d_weight is not None else d_bias
+        wide = dtype if sums is None else sums.dtype
+        if wide not in _DTYPE:
+            self._refuse(E_RANGE, where, "d_weight and d_bias have to be of float32, bfloat16 or float16")
+        desc = _LAYER_NORM_DESC(rows, cols, 0.0, _DTYPE[dtype], _DTYPE[wide], 1 if accumulate else 0, 0)
+        at, size = None, 0
+        if sums is not None:
+            work = self._work(work, _lib.ps_layer_norm_backward_bytes(desc), where)
+            at, size = work.data_ptr(), work.numel()
+        self._enqueue(where, _lib.ps_layer_norm_backward, desc, self._matrix(d_y, where, "d_y", shape, dtype),
+                      self._matrix(x, where, "x", shape, dtype), self._vector(mean, where, "mean", rows, torch.float32),
+                      self._vector(rstd, where, "rstd", rows, torch.float32), self._vector(weight, where, "weight", cols, dtype),
+                      self._matrix(residual, where, "residual", shape, dtype), self._matrix(d_x, where, "d_x", shape, dtype),
+                      self._vector(d_weight, where, "d_weight", cols, wide), self._vector(d_bias, where, "d_bias", cols, wide), at, size)
+
+    def layer_norm_backward(self, d_y: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                            weight: torch.Tensor | None = None, residual: torch.Tensor | None = None, dtype: torch.dtype | None = None):
+        """(d_x, d_weight, d_bias), the last two in x's type or `dtype`."""
+        d_x = torch.empty_like(x, memory_format=torch.contiguous_format)
+        d_weight, d_bias = (x.new_empty(x.shape[-1:], dtype=dtype) for _ in range(2))
+        self.layer_norm_backward_into(d_y, x, mean, rstd, d_x, weight, residual, d_weight, d_bias)
+        return d_x, d_weight, d_bias
+
+    @staticmethod
+    def layer_norm_backward_bytes(rows: int, cols: int, dtype: torch.dtype) -> int:
+        """Bytes of the work buffer that layer_norm_backward_into takes for gradients of weight and bias."""
+        return _lib.ps_layer_norm_backward_bytes(_LAYER_NORM_DESC(rows, cols, 0.0, _DTYPE[dtype], 0, 0, 0))
+
+    def rotary_into(self, q: torch.Tensor, q_out: torch.Tensor, k: torch.Tensor | None = None, k_out: torch.Tensor | None = None,
+                    positions: torch.Tensor | None = None, first: int = 0, base: float = 10000.0, dims: int | None = None,
+                    interleaved: bool = False, factor: float = 1.0, original: float = 0.0, low: float = 1.0, high: float = 32.0,
+                    magnitude: float = 1.0, inverse: bool = False):
+        """ps_rotary on [batch, len, heads, dim] of any strides; q_out may be q, k_out k.  `positions`: int32 or int64,
+        [len] or [batch, len]; without them a token's position is its place in the sequence.  `first` is added to all;
+        `dims` of a head's elements are turned (default: all)."""
+        where, dtype = "ps_rotary", q.dtype
+        if q.dim() != 4 or dtype not in _DTYPE or (k is None) != (k_out is None) or (k is not None and k.dim() != 4):
+            self._refuse(E_RANGE, where, "q, and k with k_out, are [batch, len, heads, dim] of float32, bfloat16 or float16")
+        batch, length, heads, dim = q.shape
+        kv_heads = 0 if k is None else k.shape[2]
+        width, apart, at = 4, 0, None
+        if positions is not None:
+            if positions.dtype not in (torch.int32, torch.int64) or positions.shape not in ((length,), (batch, length)) \
+                    or positions.get_device() != self.device:
+                self._refuse(E_RANGE, where, f"positions have to be [len] or [batch, len] of int32 or int64 on device {self.device}")
+            if length > 1 and positions.stride(-1) != 1:
+                self._refuse(E_ALIGN, where, "positions are not contiguous")
+            width, apart, at = positions.element_size(), positions.stride(0) if positions.dim() == 2 and batch > 1 else 0, positions.data_ptr()
+        if not -(1 << 63) <= first < 1 << 63:
+            self._refuse(E_RANGE, where, "first")
+        self._finite(where, "magnitude", magnitude)
+        dims = dim if dims is None else dims
+        if not 0 <= dims <= dim:
+            self._refuse(E_RANGE, where, "dims")
+        shapes = q.shape, (batch, length, kv_heads, dim)
+        desc = _ROTARY_DESC(batch, length, heads, kv_heads, dim, dims, _DTYPE[dtype], 1 if interleaved else 0, 1 if inverse else 0, width,
+                            apart, first, base, factor, original, low, high, magnitude)
+        self._enqueue(where, _lib.ps_rotary, desc, self._heads(q, where, "q", shapes[0], dtype),
+                      self._heads(q_out, where, "q_out", shapes[0], dtype),
+                      None if k is None else self._heads(k, where, "k", shapes[1], dtype),
+                      None if k is None else self._heads(k_out, where, "k_out", shapes[1], dtype), at)
+
+    def rotary(self, q: torch.Tensor, k: torch.Tensor | None = None, **how):
+        """q, or (q, k), turned by their positions; `how` as for rotary_into.  The gradient is the same call on the result's
+        gradients with inverse=True."""
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if k is None:
+            self.rotary_into(q, q_out, **how)
+            return q_out
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        self.rotary_into(q, q_out, k, k_out, **how)
+        return q_out, k_out
+
+    def _activation(self, where: str, name) -> int:
+        if name not in ACTIVATIONS:
+            self._refuse(E_RANGE, where, f"activation {name!r} is none of {', '.join(n for n in ACTIVATIONS if n)}")
+        return ACTIVATIONS[name]
+
+    def linear_forward_into(self, x: torch.Tensor, weight: torch.Tensor, y: torch.Tensor, bias: torch.Tensor | None = None,
+                            activation: str | None = None, residual: torch.Tensor | None = None, pre: torch.Tensor | None = None):
+        """ps_linear_forward: y [tokens, outputs] = act(x weight^T + bias) + residual, and what goes into the activation to
+        `pre` where it is given.  Rows of the matrices begin at multiples of 16 bytes; residual may be y."""
+        where, dtype = "ps_linear_forward", x.dtype
+        tokens, inputs = self._rows(x, where, "x")
+        outputs = self._rows(weight, where, "weight")[0]
+        code, shape = self._activation(where, activation), (tokens, outputs)
+        self._enqueue(where, _lib.ps_linear_forward, _LINEAR_DESC(tokens, inputs, outputs, _DTYPE[dtype], _DTYPE[dtype], code, 0, 0, 0),
+                      self._matrix(x, where, "x", (tokens, inputs), dtype), self._matrix(weight, where, "weight", (outputs, inputs), dtype),
+                      self._vector(bias, where, "bias", outputs, dtype), self._matrix(residual, where, "residual", shape, dtype),
+                      self._matrix(y, where, "y", shape, dtype), self._matrix(pre, where, "pre", shape, dtype))
+
+    @staticmethod
+    def _new_rows(like: torch.Tensor, rows: int, cols: int, dtype: torch.dtype | None = None) -> torch.Tensor:
+        """[rows, cols] whose rows begin at multiples of 16 bytes."""
+        pack = 4 if (dtype or like.dtype) == torch.float32 else 8
+        if cols % pack == 0:
+            return like.new_empty((rows, cols), dtype=dtype)
+        return like.new_empty((rows, (cols + pack - 1) // pack * pack), dtype=dtype)[:, :cols]
+
+    def linear_forward(self, x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, activation: str | None = None,
+                       residual: torch.Tensor | None = None, keep: bool = False):
+        """y, or with `keep` (y, pre): pre is what linear_backward takes.  (Columns of a larger tensor where outputs are no
+        multiple of 8.)"""
+        y = self._new_rows(x, x.shape[0], weight.shape[0])
+        pre = self._new_rows(x, x.shape[0], weight.shape[0]) if keep else None
+        self.linear_forward_into(x, weight, y, bias, activation, residual, pre)
+        return (y, pre) if keep else y
+
+    def linear_backward_into(self, d_y: torch.Tensor, x: torch.Tensor | None, weight: torch.Tensor | None,
+                             d_x: torch.Tensor | None = None, d_weight: torch.Tensor | None = None, d_bias: torch.Tensor | None = None,
+                             pre: torch.Tensor | None = None, activation: str | None = None, below: torch.Tensor | None = None,
+                             below_activation: str | None = None, residual: torch.Tensor | None = None, accumulate: bool = False,
+                             work: torch.Tensor | None = None):
+        """ps_linear_backward: those of the gradients of x, weight and bias that are given.  `pre` with an activation; `below` is
+        what x came out of by below_activation: d_x is then the gradient of that.  `residual` is added to d_x and may be
+        it.  accumulate adds to d_weight and d_bias.  x may be None without d_weight, weight without d_x.
+        `work`: a uint8 buffer of linear_backward_bytes; without it one is allocated for the call."""
+        where, dtype = "ps_linear_backward", d_y.dtype
+        tokens, outputs = self._rows(d_y, where, "d_y")
+        inputs = 1
+        for t, of in ((x, d_weight), (weight, d_x)):
+            if t is not None:
+                inputs = self._rows(t, where, "x and weight")[1]
+            elif of is not None:
+                self._refuse(E_NULLPTR, where, "the gradient of weight needs x, that of x needs weight")
+        sums = d_weight if d_weight is not None else d_bias
+        wide = dtype if sums is None else sums.dtype
+        if wide not in (dtype, torch.float32):
+            self._refuse(E_RANGE, where, f"d_weight and d_bias have to be {dtype} or float32")
+        code, below_code = self._activation(where, activation), self._activation(where, below_activation)
+        shape, in_shape, w_shape = (tokens, outputs), (tokens, inputs), (outputs, inputs)
+        desc = _LINEAR_DESC(tokens, inputs, outputs, _DTYPE[dtype], _DTYPE[wide], code, below_code, 1 if accumulate else 0, 0)
+        work = self._work(work, _lib.ps_linear_backward_bytes(desc), where)
+        self._enqueue(where, _lib.ps_linear_backward, desc, self._matrix(d_y, where, "d_y", shape, dtype),
+                      self._matrix(x, where, "x", in_shape, dtype), self._matrix(weight, where, "weight", w_shape, dtype),
+                      self._matrix(pre, where, "pre", shape, dtype), self._matrix(below, where, "below", in_shape, dtype),
+                      self._matrix(residual, where, "residual", in_shape, dtype), self._matrix(d_x, where, "d_x", in_shape, dtype),
+                      self._matrix(d_weight, where, "d_weight", w_shape, wide), self._vector(d_bias, where, "d_bias", outputs, wide),
+                      work.data_ptr(), work.numel())
+
+    def linear_backward(self, d_y: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre: torch.Tensor | None = None,
+                        activation: str | None = None, below: torch.Tensor | None = None, below_activation: str | None = None,
+                        residual: torch.Tensor | None = None, dtype: torch.dtype | None = None):
+        """(d_x, d_weight, d_bias), the last two in x's type or `dtype`."""
+        d_x, d_weight = self._new_rows(x, *x.shape), self._new_rows(weight, *weight.shape, dtype)
+        d_bias = weight.new_empty(weight.shape[:1], dtype=dtype)
+        self.linear_backward_into(d_y, x, weight, d_x, d_weight, d_bias, pre, activation, below, below_activation, residual)
+        return d_x, d_weight, d_bias
+
+    @staticmethod
+    def linear_backward_bytes(tokens: int, inputs: int, outputs: int, activation: str | None = None) -> int:
+        """Bytes of the work buffer that linear_backward_into takes."""
+        return _lib.ps_linear_backward_bytes(_LINEAR_DESC(tokens, inputs, outputs, 1, 1, ACTIVATIONS[activation], 0, 0, 0))
 
     def int_peak(self, blocks: int, iters: int, sink: torch.Tensor) -> int:
         ops = C.c_uint64()
