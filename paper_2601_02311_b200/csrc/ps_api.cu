@@ -849,7 +849,7 @@ int ps_layer_norm_forward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps_
   if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return PS_E_CUDA;
-  a.weight = d_weight; a.bias = d_bias; a.mean = d_mean; a.rstd = d_rstd;
+  a.weight = d_weight; a.bias = d_bias; a.mean = d_mean; a.rstd = d_rstd; a.status = ctx->h->status;
   CUDA_OK(launch_norm_forward(desc->dtype, a, ctx->sm_count, ctx->stream));
   return PS_OK;
 }
@@ -888,6 +888,7 @@ int ps_layer_norm_backward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps
   a.weight = d_weight; a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
   a.d_weight = d_weight_grad; a.d_bias = d_bias_grad;
   a.parts = sums ? (float*)d_work : nullptr;
+  a.status = ctx->h->status;
   CUDA_OK(launch_norm_backward(desc->dtype, a, ctx->sm_count, ctx->stream));
   return PS_OK;
 }

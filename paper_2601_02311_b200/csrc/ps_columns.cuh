@@ -1,11 +1,11 @@
 // Sums over the rows of a matrix, column by column, that stand in the same order on every run: blocks leave partial sums in
-// 32 bits, parts[n][arrays][cols], and this kernel adds them, first every eighth part, then the eight in a tree.
+// 32 bits, parts[n][arrays][cols], and this kernel adds them, first every 32nd part, then the 32 in a tree.
 #pragma once
 #include "ps_train.cuh"
 
 namespace train {
 
-constexpr int JOIN_COLUMNS = 32, JOIN_SLICES = 8;
+constexpr int JOIN_COLUMNS = 32, JOIN_SLICES = 32;
 template <class O>
 __global__ void __launch_bounds__(JOIN_COLUMNS* JOIN_SLICES) k_join_columns(const float* parts, u32 n, u64 cols, O* first, O* second, u32 accumulate) {
   __shared__ float sums[JOIN_SLICES][JOIN_COLUMNS];

@@ -172,6 +172,7 @@ struct NormArgs {
   float eps;
   u32 grad_dtype, accumulate;
   float* parts;                         // norm_backward_bytes; null without d_weight and d_bias
+  volatile u32* status;
 };
 cudaError_t launch_norm_forward(u32 dtype, const NormArgs& a, int sm_count, cudaStream_t stream);
 size_t norm_backward_bytes(u32 dtype, const NormArgs& a);

@@ -11,7 +11,9 @@
 // element where a row does not begin at 16 bytes), elements next to one another where it is not.  So a row's bits do not
 // depend on where it lies, nor on the other rows.
 #include <algorithm>
+#include <atomic>
 #include "ps_columns.cuh"
+#include "ps_tensor.cuh"
 
 namespace {
 using namespace train;
@@ -22,7 +24,7 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sums over the R threads of a row, the same bits in all of them: within a warp, then over the warps' sums in order.  One barrier a
+// Sums over the R threads of a row, the same bits in all of them: within a warp, then over the warps' sums in a tree.  One barrier a
 // call: the next one uses the other half of the slots.
 template <int R, int COUNT>
 struct RowSum {
@@ -32,15 +34,79 @@ struct RowSum {
   __device__ __forceinline__ void over(float (&v)[COUNT]) {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) v[i] = warp_sum(v[i]);
-    if (R == 32) return;
-    float* const mine = slots + turn * COUNT * (R / 32);
+    if (R == 32) return __syncwarp();
+    constexpr int WARPS = R / 32;
+    float* const mine = slots + turn * COUNT * WARPS;
     turn ^= 1;
     if (threadIdx.x % 32 == 0)
 #pragma unroll
-      for (int i = 0; i < COUNT; ++i) mine[i * (R / 32) + threadIdx.x / 32] = v[i];
-    __syncthreads();
+      for (int i = 0; i < COUNT; ++i) mine[i * WARPS + threadIdx.x / 32] = v[i];
+    asm volatile("bar.sync 1, %0;" ::"n"(R) : "memory");
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) v[i] = warp_sum((int)(threadIdx.x % 32) < R / 32 ? mine[i * (R / 32) + threadIdx.x % 32] : 0.f);
+    for (int i = 0; i < COUNT; ++i) {
+      v[i] = mine[i * WARPS + threadIdx.x % WARPS];
+#pragma unroll
+      for (int m = WARPS / 2; m > 0; m /= 2) v[i] += __shfl_xor_sync(0xffffffffu, v[i], m);
+    }
+  }
+};
+
+// Rows on their way: a ring of stages in shared memory, each with a row of every array that is read, brought by bulk copies that a warp of its
+// own starts.  (Started by a thread of the row's they took twice as long in all: the others wait for it at their next barrier.)
+// A copy begins and ends at multiples of 16 bytes: where a row does not, the rest of its first and last 16 bytes comes with it and is not used.
+constexpr u32 RING_MOST = 8;              // stages at most
+__host__ __device__ constexpr u32 slot_of(u64 cols, u32 width) { return (u32)((cols * width + 16 + 127) / 128 * 128); }
+struct Ring {
+  u32 base, bars, slot, stages, arrays;     // shared addresses; bytes of a row's place
+  __device__ __forceinline__ u32 at(u32 stage, u32 array) const { return base + (stage * arrays + array) * slot; }
+  __device__ __forceinline__ u32 full(u32 stage) const { return bars + 8 * stage; }
+  __device__ __forceinline__ u32 empty(u32 stage) const { return bars + 8 * (RING_MOST + stage); }
+  template <class T>
+  __device__ __forceinline__ static u32 lead(const ps_matrix& m, u64 r) { return (u32)reinterpret_cast<uintptr_t>((const T*)m.data + r * m.stride) & 15u; }
+  // all threads of the block; `warps` read the rows
+  __device__ __forceinline__ void begin(unsigned char* rows, u64* bar_at, int warps) {
+    base = (tensor::smem_address(rows) + 127u) & ~127u, bars = tensor::smem_address(bar_at);
+    if (threadIdx.x == 0) {
+      for (u32 s = 0; s < stages; ++s) tensor::barrier_init(full(s), 1), tensor::barrier_init(empty(s), warps);
+      tensor::fence_barrier_init();
+    }
+    __syncthreads();
+  }
+  // one thread: rows first, first + step, ... of up to three matrices
+  template <class T>
+  __device__ __forceinline__ void bring(tensor::Waiter& waiter, const ps_matrix& m0, const ps_matrix& m1, const ps_matrix& m2, u64 first, u64 step, u64 rows, u32 cols) const {
+    u32 stage = 0, parity = 1, filled = 0;
+    const char* p0 = (const char*)((const T*)m0.data + first * m0.stride);
+    const char* p1 = (const char*)((const T*)m1.data + first * m1.stride);
+    const char* p2 = (const char*)((const T*)m2.data + first * m2.stride);
+    const u64 by0 = step * m0.stride * sizeof(T), by1 = step * m1.stride * sizeof(T), by2 = step * m2.stride * sizeof(T);
+    const u32 bytes = cols * (u32)sizeof(T) + 15u;
+    const auto head = [](const char* p) { return (u32)reinterpret_cast<uintptr_t>(p) & 15u; };
+    const auto whole = [&](const char* p) { return (head(p) + bytes) & ~15u; };
+    for (u64 r = first; r < rows; r += step) {
+      waiter.wait(empty(stage), parity);
+      if (waiter.dead) break;
+      tensor::barrier_expect(full(stage), whole(p0) + (arrays > 1 ? whole(p1) : 0) + (arrays > 2 ? whole(p2) : 0));
+      tensor::load_bytes(at(stage, 0), p0 - head(p0), whole(p0), full(stage));
+      if (arrays > 1) tensor::load_bytes(at(stage, 1), p1 - head(p1), whole(p1), full(stage));
+      if (arrays > 2) tensor::load_bytes(at(stage, 2), p2 - head(p2), whole(p2), full(stage));
+      p0 += by0, p1 += by1, p2 += by2;
+      filled = min(filled + 1, stages);
+      if (++stage == stages) stage = 0, parity ^= 1;
+    }
+    // leave no copy in flight, also where a wait has run out
+    tensor::Waiter last(waiter.status);
+    for (; filled > 0; --filled) {
+      if (stage == 0) stage = stages, parity ^= 1;
+      --stage;
+      last.wait(full(stage), parity ^ 1);
+    }
+  }
+  // a warp: it has read the stage
+  __device__ __forceinline__ void leave(u32& stage, u32& parity) const {
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) tensor::barrier_arrive(empty(stage));
+    if (++stage == stages) stage = 0, parity ^= 1;
   }
 };
 
@@ -53,91 +119,201 @@ struct Piece {
   __device__ static __forceinline__ u32 bits(const float* p) { return __float_as_uint(*p); }
   __device__ static __forceinline__ u32 bits(const __nv_bfloat16* p) { return __bfloat16_as_ushort(*p); }
   __device__ static __forceinline__ u32 bits(const __half* p) { return __half_as_ushort(*p); }
-  __device__ __forceinline__ void put(int e, u32 b) {
-    if (sizeof(T) == 4) p.w[e] = b;
-    else p.w[e / 2] |= b << (16 * (e % 2));
+  __device__ __forceinline__ u64 both(int e) const { return Pack<T, E>::both(p.w, e, (const T*)nullptr); }        // (e even)
+  // The words stay, the floats that they were widened to do not: without it the compiler keeps those from one walk to the next, in registers
+  // that are not there.
+  __device__ __forceinline__ void forget() {
+    if (sizeof(T) == 2)
+#pragma unroll
+      for (int i = 0; i < Pack<T, E>::WORDS; ++i) asm volatile("" : "+r"(p.w[i]));
   }
-  // `wide`: the row begins at a multiple of 16 bytes.  Columns behind `cols` are zeros.
-  __device__ __forceinline__ void load(const T* row, u32 cols, bool wide) {
-    p.clear();
-    if (PACKED && wide) {
+  __device__ __forceinline__ void put_both(int e, u64 v) {
+    const float lo = split(v).x, hi = split(v).y;
+    if (sizeof(T) == 4) p.w[e] = __float_as_uint(lo), p.w[e + 1] = __float_as_uint(hi);
+    else p.w[e / 2] = Pack<T, E>::two(lo, hi, (const T*)nullptr);
+  }
+  // `wide`: rows begin at multiples of 16 bytes.  Columns behind `cols` are zeros.
+  // elements e .. e + G - 1 out of a row in shared memory, G = N or 2
+  __device__ static __forceinline__ void read(u32 (&w)[(PACKED ? 16 : 2 * (int)sizeof(T)) / 4], u32 row, int e, u32 cols, bool wide) {
+    constexpr int G = PACKED ? N : 2;
 #pragma unroll
-      for (int e = 0; e < E; e += N)
-        if (column(e) < cols) {
-          const uint4 v = *reinterpret_cast<const uint4*>(row + column(e));
-          constexpr int W = sizeof(T);      // (words of N elements: 4)
-          u32* const to = p.w + e * W / 4;
-          to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
+    for (int i = 0; i < (PACKED ? 16 : 2 * (int)sizeof(T)) / 4; ++i) w[i] = 0;
+    if constexpr (PACKED)
+      if (wide) {
+        if (column(e) < cols)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(row + column(e) * (u32)sizeof(T)));
+        return;
+      }
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+      if (column(e + i) < cols) {
+        const u32 at = row + column(e + i) * (u32)sizeof(T);
+        if constexpr (sizeof(T) == 4) {
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(at));
+        } else {
+          unsigned short v;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+          w[i / 2] |= (u32)v << (16 * (i % 2));
         }
-    } else {
+      }
+  }
+  __device__ __forceinline__ void take(u32 row, u32 cols, bool wide) {
+    constexpr int G = PACKED ? N : 2, W = G * (int)sizeof(T) / 4;
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (column(e) < cols) put(e, bits(row + column(e)));
+    for (int e = 0; e < E; e += G) {
+      u32 w[W];
+      read(w, row, e, cols, wide);
+#pragma unroll
+      for (int i = 0; i < W; ++i) p.w[e * (int)sizeof(T) / 4 + i] = w[i];
     }
   }
-  __device__ __forceinline__ void store(T* row, u32 cols, bool wide) const {
+  // as the row's elements from `first` on
+  __device__ __forceinline__ void store_at(T* row, int first, u32 cols, bool wide) const {
     if (PACKED && wide) {
 #pragma unroll
       for (int e = 0; e < E; e += N)
-        if (column(e) < cols) {
+        if (column(first + e) < cols) {
           const u32* const w = p.w + e * (int)sizeof(T) / 4;
-          *reinterpret_cast<uint4*>(row + column(e)) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(row + column(first + e)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (column(e) < cols) {
-          if (sizeof(T) == 4) reinterpret_cast<u32*>(row)[column(e)] = p.w[e];
-          else reinterpret_cast<unsigned short*>(row)[column(e)] = (unsigned short)(p.w[e / 2] >> (16 * (e % 2)));
+        if (column(first + e) < cols) {
+          if (sizeof(T) == 4) reinterpret_cast<u32*>(row)[column(first + e)] = p.w[e];
+          else reinterpret_cast<unsigned short*>(row)[column(first + e)] = (unsigned short)(p.w[e / 2] >> (16 * (e % 2)));
         }
     }
+  }
+  __device__ __forceinline__ void store(T* row, u32 cols, bool wide) const { store_at(row, 0, cols, wide); }
+};
+
+// the G elements of weight or bias that belong to elements e .. e + G - 1 of a Piece
+template <class T, int G>
+struct Vector {
+  u32 w[G * sizeof(T) < 4 ? 1 : G * (int)sizeof(T) / 4];
+  template <int R, bool PACKED>
+  __device__ __forceinline__ void load(const T* from, int e, u32 cols, bool wide, float without) {
+    typedef Piece<T, R, 32, PACKED> P;
+    if (from == nullptr) {
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof(w) / 4); ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(without) : Pack<T, G>::two(without, without, (const T*)nullptr);
+    } else if (PACKED && wide) {
+      const u32 c = P::column(e);
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (c < cols) v = *reinterpret_cast<const uint4*>(from + c);
+      w[0] = v.x, w[1] = v.y, w[G * (int)sizeof(T) / 4 > 2 ? 2 : 0] = v.z, w[G * (int)sizeof(T) / 4 > 3 ? 3 : 0] = v.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const u32 c = P::column(e + i), b = c < cols ? P::bits(from + c) : 0;
+        if (sizeof(T) == 4) w[i] = b;
+        else w[i / 2] = i % 2 ? w[i / 2] | b << 16 : b;
+      }
+    }
+  }
+  __device__ __forceinline__ u64 both(int i) const { return Pack<T, G>::both(w, i, (const T*)nullptr); }
+  __device__ __forceinline__ void forget() {          // (as Piece's)
+    if (sizeof(T) == 2)
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof(w) / 4); ++i) asm volatile("" : "+r"(w[i]));
   }
 };
+__device__ __forceinline__ u64 twice(float v) { return pair(v, v); }
+__device__ __forceinline__ float together(u64 v) { return split(v).x + split(v).y; }
 
 struct Wide {           // which rows begin at multiples of 16 bytes
   bool x, y, d_y, residual, d_x, weight, bias;
 };
 
-__host__ __device__ constexpr int threads_of(int r) { return r < 128 ? 128 : r; }
+// sqrt's reciprocal, the fast function's (off by up to 2 units) improved by a Newton step
+__device__ __forceinline__ float reciprocal_root(float v) {
+  const float y = rsqrtf(v), half = 0.5f * v;
+  return v > 0.f && v < INFINITY ? y * fmaf(-half * y, y, 1.5f) : y;
+}
 
+// Blocks of an SM at most, by the threads of a row: about 1024 threads, or 512 where they hold sums as well.
+__host__ __device__ constexpr int forward_blocks(int r) { return r == 32 ? 16 : r == 64 ? 8 : r == 128 ? 6 : r == 256 ? 3 : 2; }
+__host__ __device__ constexpr int backward_blocks(int r) { return r == 32 ? 8 : r == 64 ? 5 : r == 128 ? 3 : r == 256 ? 2 : 1; }
+
+// Elements of a thread whose weights stay in its registers as well.  Of more they are read again for each row.
+template <class T, int E> constexpr bool HELD = E * sizeof(T) <= 32;
+
+// A block has a row at a time, a thread E elements of it; a warp beside them brings the rows to come.
+// (At 16 bits a walk over the elements is issue slots as much as it is bytes: floats are taken two at a time.)
 template <class T, int R, int E, bool PACKED>
-__global__ void __launch_bounds__(threads_of(R)) k_norm(const NormArgs a, const Wide wide) {
+__global__ void __launch_bounds__(R + 32, forward_blocks(R)) k_norm(const NormArgs a, const Wide wide, Ring ring, float share) {
+  extern __shared__ unsigned char rows[];
   __shared__ float slots[2 * R / 32];
-  RowSum<R, 1> sum(slots);
-  constexpr int ROWS = threads_of(R) / R;
+  __shared__ u64 bars[2 * RING_MOST];
   const u32 cols = (u32)a.cols;
+  const u64 step = gridDim.x;
+  ring.begin(rows, bars, R / 32);
+  tensor::Waiter waiter(a.status);
+  if (threadIdx.x >= R) {
+    if (threadIdx.x == R) ring.bring<T>(waiter, a.x, a.x, a.x, blockIdx.x, step, a.rows, cols);
+    return;
+  }
+  RowSum<R, 1> sum(slots);
   typedef Piece<T, R, E, PACKED> P;
-  for (u64 r = (u64)blockIdx.x * ROWS + threadIdx.x / R; r < a.rows; r += (u64)gridDim.x * ROWS) {
-    P x, w, b;
-    x.load((const T*)a.x.data + r * a.x.stride, cols, wide.x);
-    if (a.weight) w.load((const T*)a.weight, cols, wide.weight);
-    if (a.bias) b.load((const T*)a.bias, cols, wide.bias);
-    float v[E], s[1] = {0.f};
-    x.p.widen(v);
+  constexpr int G = PACKED ? P::N : 2;          // elements that lie, or are read, together
+  constexpr bool HOLD = HELD<T, E>;
+  Vector<T, G> weights[HOLD ? E / G : 1], biases[HOLD ? E / G : 1];
+  if (HOLD)
 #pragma unroll
-    for (int e = 0; e < E; ++e) s[0] += v[e];
-    sum.over(s);
-    const float mean = s[0] / (float)cols;
-    s[0] = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      v[e] = P::column(e) < cols ? v[e] - mean : 0.f;
-      s[0] = fmaf(v[e], v[e], s[0]);
+    for (int e = 0; e < E; e += G) {
+      weights[e / G].template load<R, PACKED>((const T*)a.weight, e, cols, wide.weight, 1.f);
+      biases[e / G].template load<R, PACKED>((const T*)a.bias, e, cols, wide.bias, 0.f);
     }
+  u32 stage = 0, parity = 0;
+  T* to = (T*)a.y.data + blockIdx.x * a.y.stride;
+  for (u64 r = blockIdx.x; r < a.rows; r += step, to += step * a.y.stride) {
+    P x;
+    waiter.wait(ring.full(stage), parity);
+    x.take(ring.at(stage, 0) + Ring::lead<T>(a.x, r), cols, wide.x);
+    float s[1];
+    u64 part[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < E; e += 2) part[e / 2 % 2] = add2(part[e / 2 % 2], x.both(e));
+    ring.leave(stage, parity);
+    s[0] = together(add2(part[0], part[1]));
     sum.over(s);
-    const float rstd = 1.f / sqrtf(s[0] / (float)cols + a.eps);
-    float f[E];
-    if (a.weight) w.p.widen(f);
+    const float mean = s[0] * share;
+    const u64 less = twice(-mean);
+    part[0] = part[1] = 0;
+    x.forget();
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] *= a.weight ? rstd * f[e] : rstd;
-    if (a.bias) {
-      b.p.widen(f);
+    for (int e = 0; e < E; e += G) {
+      u64 more = 0;
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] += f[e];
+      for (int i = 0; i < G; i += 2) {
+        u64 d = add2(x.both(e + i), less);
+        if (!PACKED) d = pair(P::column(e) < cols ? split(d).x : 0.f, P::column(e + 1) < cols ? split(d).y : 0.f);
+        more = fma2(d, d, more);
+      }
+      if (!PACKED || P::column(e) < cols) part[e / G % 2] = add2(part[e / G % 2], more);
     }
-    x.p.narrow(v);
-    x.store((T*)a.y.data + r * a.y.stride, cols, wide.y);
-    if (threadIdx.x % R == 0) {
+    s[0] = together(add2(part[0], part[1]));
+    sum.over(s);
+    const float rstd = reciprocal_root(fmaf(s[0], share, a.eps));
+    const u64 by = twice(rstd);
+    x.forget();
+#pragma unroll
+    for (int e = 0; e < E; e += G) {
+      Vector<T, G> w, b;
+      if (HOLD) {
+        w = weights[HOLD ? e / G : 0], b = biases[HOLD ? e / G : 0];
+        w.forget(), b.forget();
+      } else {
+        asm volatile("" ::: "memory");          // (not all weights at once: there are no registers for it)
+        w.template load<R, PACKED>((const T*)a.weight, e, cols, wide.weight, 1.f);
+        b.template load<R, PACKED>((const T*)a.bias, e, cols, wide.bias, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < G; i += 2) x.put_both(e + i, fma2(add2(x.both(e + i), less), mul2(by, w.both(i)), b.both(i)));
+    }
+    x.store(to, cols, wide.y);
+    if (threadIdx.x == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
     }
@@ -175,73 +351,100 @@ __global__ void __launch_bounds__(LONG) k_norm_long(const NormArgs a) {
   }
 }
 
-// GRADS: the sums over this block's rows for dW and dB go to parts[block][2][cols]
+// GRADS: the sums over this block's rows for dW and dB go to parts[block][2][cols]: they are what the registers are for, so with 32 elements a thread
+// the second walk over a row reads it again from shared memory.
 template <class T, int R, int E, bool PACKED, bool GRADS>
-__global__ void __launch_bounds__(threads_of(R)) k_norm_grad(const NormArgs a, const Wide wide) {
-  constexpr int ROWS = threads_of(R) / R;
+__global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const NormArgs a, const Wide wide, Ring ring, float share) {
+  extern __shared__ unsigned char rows[];
   __shared__ float slots[2 * 2 * R / 32];
-  __shared__ float joined[ROWS > 1 && GRADS ? 2 * R * E : 1];
-  RowSum<R, 2> sum(slots);
+  __shared__ u64 bars[2 * RING_MOST];
   const u32 cols = (u32)a.cols;
+  const u64 step = gridDim.x;
+  ring.begin(rows, bars, R / 32);
+  tensor::Waiter waiter(a.status);
+  if (threadIdx.x >= R) {
+    if (threadIdx.x == R) ring.bring<T>(waiter, a.x, a.d_y, a.residual, blockIdx.x, step, a.rows, cols);
+    return;
+  }
+  RowSum<R, 2> sum(slots);
   typedef Piece<T, R, E, PACKED> P;
-  float of_w[E], of_b[E];
+  constexpr int G = PACKED ? P::N : 2, W = G * (int)sizeof(T) / 4;        // elements that are read together, and their words
+  typedef Pack<T, G> Group;
+  constexpr bool KEEP = E <= 16;                // what the second walk needs of the first, in registers
+  const u32 w_row = ring.at(ring.stages, 0);    // the weights stand behind the stages
+  for (u32 c = threadIdx.x; c < cols; c += R) {
+    if constexpr (sizeof(T) == 4)
+      asm volatile("st.shared.u32 [%0], %1;" ::"r"(w_row + 4 * c), "r"(a.weight ? P::bits((const T*)a.weight + c) : 0x3f800000u) : "memory");
+    else
+      asm volatile("st.shared.u16 [%0], %1;" ::"r"(w_row + 2 * c), "h"((unsigned short)(a.weight ? P::bits((const T*)a.weight + c) : Pack<T, 2>::two(1.f, 1.f, (const T*)nullptr))) : "memory");
+  }
+  asm volatile("bar.sync 1, %0;" ::"n"(R) : "memory");
+  u64 of_w[E / 2], of_b[E / 2];                 // two columns each
 #pragma unroll
-  for (int e = 0; e < E; ++e) of_w[e] = of_b[e] = 0.f;
-  for (u64 r = (u64)blockIdx.x * ROWS + threadIdx.x / R; r < a.rows; r += (u64)gridDim.x * ROWS) {
-    P x, d, w, more;
-    x.load((const T*)a.x.data + r * a.x.stride, cols, wide.x);
-    d.load((const T*)a.d_y.data + r * a.d_y.stride, cols, wide.d_y);
-    if (a.residual.data) more.load((const T*)a.residual.data + r * a.residual.stride, cols, wide.residual);
-    if (a.weight) w.load((const T*)a.weight, cols, wide.weight);
-    const float mean = a.mean[r], rstd = a.rstd[r];
-    float xn[E], g[E], f[E], s[2] = {0.f, 0.f};
-    x.p.widen(xn);
-    d.p.widen(g);
-    if (a.weight) w.p.widen(f);
+  for (int e = 0; e < E / 2; ++e) of_w[e] = of_b[e] = 0;
+  u32 stage = 0, parity = 0;
+  T* to = (T*)a.d_x.data + blockIdx.x * a.d_x.stride;
+  float next_mean = 0.f, next_rstd = 0.f;
+  if (blockIdx.x < a.rows) next_mean = a.mean[blockIdx.x], next_rstd = a.rstd[blockIdx.x];
+  for (u64 r = blockIdx.x; r < a.rows; r += step, to += step * a.d_x.stride) {
+    const u64 less = twice(-next_mean), by = twice(next_rstd);
+    if (r + step < a.rows) next_mean = a.mean[r + step], next_rstd = a.rstd[r + step];
+    const u32 x_row = ring.at(stage, 0) + Ring::lead<T>(a.x, r), d_row = ring.at(stage, 1) + Ring::lead<T>(a.d_y, r);
+    const u32 more_row = ring.at(stage, 2) + Ring::lead<T>(a.residual, r);          // (of a residual)
+    waiter.wait(ring.full(stage), parity);
+    float s[2];
+    u64 of_g = 0, of_gx = 0, kept_xn[KEEP ? E / 2 : 1], kept_g[KEEP ? E / 2 : 1];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      xn[e] = (xn[e] - mean) * rstd;
-      if (GRADS) {
-        of_w[e] = fmaf(g[e], xn[e], of_w[e]);
-        of_b[e] += g[e];
+    for (int e = 0; e < E; e += G) {
+      u32 x[W], d[W];
+      P::read(x, x_row, e, cols, wide.x);
+      P::read(d, d_row, e, cols, wide.d_y);
+      u32 w[W];
+      P::read(w, w_row, e, cols, true);
+#pragma unroll
+      for (int i = 0; i < G; i += 2) {
+        const u64 xn = mul2(add2(Group::both(x, i, (const T*)nullptr), less), by), dy = Group::both(d, i, (const T*)nullptr), g = mul2(dy, Group::both(w, i, (const T*)nullptr));
+        if (GRADS) {
+          of_w[(e + i) / 2] = fma2(dy, xn, of_w[(e + i) / 2]);
+          of_b[(e + i) / 2] = add2(of_b[(e + i) / 2], dy);
+        }
+        of_g = add2(of_g, g);
+        of_gx = fma2(g, xn, of_gx);             // (g is 0 behind the last column)
+        if (KEEP) kept_xn[(e + i) / 2] = xn, kept_g[(e + i) / 2] = g;
       }
-      if (a.weight) g[e] *= f[e];
-      s[0] += g[e];
-      s[1] = fmaf(g[e], xn[e], s[1]);         // (g is 0 behind the last column)
     }
+    s[0] = together(of_g);
+    s[1] = together(of_gx);
     sum.over(s);
-    const float along = s[0] / (float)cols, across = s[1] / (float)cols;
-    if (a.residual.data) more.p.widen(f);
+    const u64 along = twice(-s[0] * share), across = twice(-s[1] * share);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float v = rstd * (g[e] - fmaf(xn[e], across, along));
-      g[e] = a.residual.data ? v + f[e] : v;
+    for (int e = 0; e < E; e += G) {
+      u32 x[W], d[W], w[W], more[W] = {};
+      if (!KEEP) {
+        P::read(x, x_row, e, cols, wide.x);
+        P::read(d, d_row, e, cols, wide.d_y);
+        P::read(w, w_row, e, cols, true);
+      }
+      if (a.residual.data) P::read(more, more_row, e, cols, wide.residual);
+      Piece<T, R, G, PACKED> out;
+#pragma unroll
+      for (int i = 0; i < G; i += 2) {
+        const u64 xn = KEEP ? kept_xn[KEEP ? (e + i) / 2 : 0] : mul2(add2(Group::both(x, i, (const T*)nullptr), less), by);
+        const u64 g = KEEP ? kept_g[KEEP ? (e + i) / 2 : 0] : mul2(Group::both(d, i, (const T*)nullptr), Group::both(w, i, (const T*)nullptr));
+        const u64 v = add2(g, fma2(xn, across, along));
+        out.put_both(i, a.residual.data ? fma2(by, v, Group::both(more, i, (const T*)nullptr)) : mul2(by, v));
+      }
+      out.store_at(to, e, cols, wide.d_x);
     }
-    d.p.narrow(g);
-    d.store((T*)a.d_x.data + r * a.d_x.stride, cols, wide.d_x);
+    ring.leave(stage, parity);
   }
   if (GRADS) {
-    float* const to = a.parts + (u64)blockIdx.x * 2 * cols;
-    if (ROWS > 1) {               // the warps' sums, one warp after the other
-      for (int turn = 0; turn < ROWS; ++turn) {
-        if ((int)(threadIdx.x / R) == turn)
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const u32 at = e * R + threadIdx.x % R;
-            of_w[e] += turn ? joined[at] : 0.f;
-            of_b[e] += turn ? joined[R * E + at] : 0.f;
-            joined[at] = of_w[e];
-            joined[R * E + at] = of_b[e];
-          }
-        __syncthreads();
-      }
-      if (threadIdx.x / R != ROWS - 1) return;
-    }
+    float* const into = a.parts + (u64)blockIdx.x * 2 * cols;
 #pragma unroll
     for (int e = 0; e < E; ++e)
       if (P::column(e) < cols) {
-        to[P::column(e)] = of_w[e];
-        to[cols + P::column(e)] = of_b[e];
+        into[P::column(e)] = e % 2 ? split(of_w[e / 2]).y : split(of_w[e / 2]).x;
+        into[cols + P::column(e)] = e % 2 ? split(of_b[e / 2]).y : split(of_b[e / 2]).x;
       }
   }
 }
@@ -291,28 +494,64 @@ __global__ void __launch_bounds__(256) k_norm_columns(const NormArgs a, u64 rows
 }
 
 // blocks that the rows are spread over, at most
-u32 blocks_for(u64 rows, int rows_a_block, int resident, int sm_count) {
-  const u64 need = (rows + rows_a_block - 1) / rows_a_block, most = (u64)sm_count * resident;
-  return (u32)(need < most ? need : most);
-}
+u32 blocks_for(u64 rows, int resident, int sm_count) { return (u32)std::min<u64>(rows, (u64)sm_count * resident); }
 
-// Elements of a thread and threads of a row, by the width: as few threads as hold the row in E registers each.  The
-// backward pass has two sums a column beside the row's two matrices, hence fewer columns a thread.
-constexpr int E_FORWARD = 32;
-template <class T, int R, bool PACKED>
+// Blocks of an SM, and the ring that each has: as many blocks as `most` and have `wanted` stages in the SM's shared memory, and all the stages that they
+// have room for beside `more` rows.
+constexpr u32 ROOM = 224 * 1024;
+struct Layout {
+  int resident;
+  Ring ring;
+  u32 smem;
+};
+Layout layout_of(int most, u32 wanted, u64 cols, u32 width, u32 arrays, u32 more) {
+  Layout l = {};
+  l.ring.slot = slot_of(cols, width);
+  l.ring.arrays = arrays;
+  const u32 stage = l.ring.slot * arrays;
+  l.resident = most;
+  const auto stages = [&] { return (ROOM / l.resident - 2048 - more * l.ring.slot) / stage; };       // (a row is at most 64 KB)
+  while (l.resident > 1 && (ROOM / l.resident < 2048 + more * l.ring.slot || stages() < wanted)) --l.resident;
+  l.ring.stages = std::max(1u, std::min(RING_MOST, stages()));
+  l.smem = l.ring.stages * stage + more * l.ring.slot + 128;
+  return l;
+}
+Layout forward_layout(int threads, u64 cols, u32 width) { return layout_of(forward_blocks(threads), 4, cols, width, 1, 0); }
+Layout backward_layout(int threads, u64 cols, u32 width, u32 arrays) { return layout_of(backward_blocks(threads), 4, cols, width, arrays, 1); }
+// (asked for once a kernel and device)
+template <auto KERNEL>
+struct Prepared {
+  static cudaError_t smem(u32 bytes) {
+    static std::atomic<u64> devices{0};
+    if (bytes <= 47 * 1024) return cudaSuccess;
+    int device;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess || (device < 64 && devices.load() >> device & 1)) return e;
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
+    if (e == cudaSuccess && device < 64) devices |= (u64)1 << device;
+    return e;
+  }
+};
+
+// Threads of a row, by the width: as few as hold it in 16 elements each, of wide rows 32.
+template <class T, int R, int E, bool PACKED>
 cudaError_t forward(const NormArgs& a, const Wide& wide, int sm_count, cudaStream_t stream) {
-  const int threads = threads_of(R), resident = 2048 / threads;
-  k_norm<T, R, E_FORWARD, PACKED><<<blocks_for(a.rows, threads / R, resident, sm_count), threads, 0, stream>>>(a, wide);
+  constexpr auto kernel = k_norm<T, R, E, PACKED>;
+  const Layout l = forward_layout(R, a.cols, sizeof(T));
+  const cudaError_t e = Prepared<kernel>::smem(l.smem);
+  if (e != cudaSuccess) return e;
+  kernel<<<blocks_for(a.rows, l.resident, sm_count), R + 32, l.smem, stream>>>(a, wide, l.ring, 1.f / (float)a.cols);
   return cudaGetLastError();
 }
 template <class T, bool PACKED>
 cudaError_t forward(const NormArgs& a, const Wide& wide, int sm_count, cudaStream_t stream) {
-  if (a.cols <= 32 * E_FORWARD) return forward<T, 32, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 128 * E_FORWARD) return forward<T, 128, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 256 * E_FORWARD) return forward<T, 256, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 512 * E_FORWARD) return forward<T, 512, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 1024 * E_FORWARD) return forward<T, 1024, PACKED>(a, wide, sm_count, stream);
-  k_norm_long<T><<<blocks_for(a.rows, 1, 2, sm_count), LONG, 0, stream>>>(a);
+  if (a.cols <= 32 * 16) return forward<T, 32, 16, PACKED>(a, wide, sm_count, stream);
+  if (a.cols <= 64 * 16) return forward<T, 64, 16, PACKED>(a, wide, sm_count, stream);
+  if (a.cols <= 128 * 16) return forward<T, 128, 16, PACKED>(a, wide, sm_count, stream);
+  if (a.cols <= 256 * 16) return forward<T, 256, 16, PACKED>(a, wide, sm_count, stream);
+  if (a.cols <= 512 * 16) return forward<T, 512, 16, PACKED>(a, wide, sm_count, stream);
+  if (a.cols <= 512 * 32) return forward<T, 512, 32, PACKED>(a, wide, sm_count, stream);
+  k_norm_long<T><<<blocks_for(a.rows, 2, sm_count), LONG, 0, stream>>>(a);
   return cudaGetLastError();
 }
 Wide wide_of(const NormArgs& a, size_t width) {
@@ -325,43 +564,47 @@ cudaError_t forward(const NormArgs& a, int sm_count, cudaStream_t stream) {
   return a.cols % (16 / sizeof(T)) == 0 ? forward<T, true>(a, wide, sm_count, stream) : forward<T, false>(a, wide, sm_count, stream);
 }
 
-// the backward pass's shape: threads of a row (0: the long kernels) and blocks, which are the parts of the sums
+// The backward pass's shape: threads of a row, 16 or 32 elements each (0: the long kernels), and blocks, which are the parts of the sums; a block has four
+// rows at least.  (A number of blocks for 148 SMs, whatever the device has: the sums' order depends on the
+// sizes, and on whether there is a residual, alone.)
+constexpr int SMS = 148;
 struct Shape {
   int threads, elements;
   u32 blocks;
 };
-// (a number of blocks for 148 SMs, whatever the device has: the sums' order depends on the sizes alone)
-constexpr int SMS = 148;
-Shape backward_shape(u32 width, u64 rows, u64 cols) {
+Shape backward_shape(u32 width, u64 rows, u64 cols, u32 arrays) {
   Shape s = {0, 16, 0};
-  if (width == 2 && cols <= 1024) s.threads = 32, s.elements = 32;
-  else if (width == 4 && cols <= 512) s.threads = 32;
-  else if (cols <= 2048) s.threads = 128;
-  else if (cols <= 4096) s.threads = 256;
-  else if (cols <= 8192) s.threads = 512;
-  else if (width == 2 && cols <= 16384) s.threads = 512, s.elements = 32;
-  if (s.threads == 0) s.blocks = (u32)std::max<u64>(1, std::min<u64>((rows + 63) / 64, 64));          // (chunks of rows)
-  else {
-    const int block = threads_of(s.threads);
-    s.blocks = std::max(1u, blocks_for(rows, block / s.threads, s.elements == 32 && s.threads == 512 ? 1 : 512 / block, SMS));
+  if (cols <= 16384 && (2 * arrays + 1) * slot_of(cols, width) <= ROOM - 2048) {        // (two stages, and the weights)
+    s.threads = 32;
+    while (s.threads < 512 && cols > (u64)s.threads * 16) s.threads *= 2;
+    if (cols > 512 * 16) s.elements = 32;
   }
+  if (s.threads == 0) s.blocks = (u32)std::max<u64>(1, std::min<u64>((rows + 63) / 64, 64));          // (chunks of rows)
+  else s.blocks = (u32)std::max<u64>(1, std::min<u64>((rows + 3) / 4, SMS * backward_layout(s.threads, cols, width, arrays).resident));
   return s;
+}
+template <class T, int R, int E, bool PACKED, bool GRADS>
+cudaError_t backward(const NormArgs& a, const Wide& wide, const Shape& s, cudaStream_t stream) {
+  constexpr auto kernel = k_norm_grad<T, R, E, PACKED, GRADS>;
+  const Layout l = backward_layout(R, a.cols, sizeof(T), a.residual.data ? 3 : 2);
+  const cudaError_t e = Prepared<kernel>::smem(l.smem);
+  if (e != cudaSuccess) return e;
+  kernel<<<s.blocks, R + 32, l.smem, stream>>>(a, wide, l.ring, 1.f / (float)a.cols);
+  return cudaGetLastError();
 }
 template <class T, int R, int E, bool PACKED>
 cudaError_t backward(const NormArgs& a, const Wide& wide, const Shape& s, cudaStream_t stream) {
-  if (a.parts) k_norm_grad<T, R, E, PACKED, true><<<s.blocks, threads_of(R), 0, stream>>>(a, wide);
-  else k_norm_grad<T, R, E, PACKED, false><<<s.blocks, threads_of(R), 0, stream>>>(a, wide);
-  return cudaGetLastError();
+  return a.parts ? backward<T, R, E, PACKED, true>(a, wide, s, stream) : backward<T, R, E, PACKED, false>(a, wide, s, stream);
 }
 template <class T, bool PACKED>
 cudaError_t backward(const NormArgs& a, const Shape& s, int sm_count, cudaStream_t stream) {
   const Wide wide = wide_of(a, sizeof(T));
-  constexpr bool HALF = sizeof(T) == 2;
-  if (s.threads == 32) return backward<T, 32, HALF ? 32 : 16, PACKED>(a, wide, s, stream);
+  if (s.threads == 32) return backward<T, 32, 16, PACKED>(a, wide, s, stream);
+  if (s.threads == 64) return backward<T, 64, 16, PACKED>(a, wide, s, stream);
   if (s.threads == 128) return backward<T, 128, 16, PACKED>(a, wide, s, stream);
   if (s.threads == 256) return backward<T, 256, 16, PACKED>(a, wide, s, stream);
   if (s.threads == 512 && s.elements == 16) return backward<T, 512, 16, PACKED>(a, wide, s, stream);
-  if constexpr (HALF)
+  if constexpr (sizeof(T) == 2)
     if (s.threads == 512) return backward<T, 512, 32, PACKED>(a, wide, s, stream);
   if (a.parts) {                 // before d_x, which may stand in the place of d_y or x
     k_norm_columns<T><<<dim3((u32)((a.cols + 255) / 256), s.blocks), 256, 0, stream>>>(a, (a.rows + s.blocks - 1) / s.blocks);
@@ -369,12 +612,12 @@ cudaError_t backward(const NormArgs& a, const Shape& s, int sm_count, cudaStream
     if (e != cudaSuccess) return e;
   }
   if (a.rows == 0) return cudaSuccess;
-  k_norm_grad_long<T><<<blocks_for(a.rows, 1, 2, sm_count), LONG, 0, stream>>>(a);
+  k_norm_grad_long<T><<<blocks_for(a.rows, 2, sm_count), LONG, 0, stream>>>(a);
   return cudaGetLastError();
 }
 template <class T>
 cudaError_t backward(const NormArgs& a, int sm_count, cudaStream_t stream) {
-  const Shape s = backward_shape(sizeof(T), a.rows, a.cols);
+  const Shape s = backward_shape(sizeof(T), a.rows, a.cols, a.residual.data ? 3 : 2);
   if (a.rows == 0 && !a.parts) return cudaSuccess;
   const cudaError_t e = a.cols % (16 / sizeof(T)) == 0 ? backward<T, true>(a, s, sm_count, stream) : backward<T, false>(a, s, sm_count, stream);
   if (e != cudaSuccess || !a.parts) return e;
@@ -389,7 +632,8 @@ cudaError_t launch_norm_forward(u32 dtype, const NormArgs& a, int sm_count, cuda
 }
 
 size_t norm_backward_bytes(u32 dtype, const NormArgs& a) {
-  return (size_t)backward_shape(dtype == PS_F32 ? 4 : 2, a.rows, a.cols).blocks * 2 * a.cols * sizeof(float);
+  const u32 width = dtype == PS_F32 ? 4 : 2, blocks = std::max(backward_shape(width, a.rows, a.cols, 2).blocks, backward_shape(width, a.rows, a.cols, 3).blocks);
+  return (size_t)blocks * 2 * a.cols * sizeof(float);
 }
 
 cudaError_t launch_norm_backward(u32 dtype, const NormArgs& a, int sm_count, cudaStream_t stream) {

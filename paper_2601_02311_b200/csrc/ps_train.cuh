@@ -17,6 +17,33 @@ template <> __device__ __forceinline__ float narrow<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half narrow<__half>(float v) { return __float2half_rn(v); }
 
+// ---- arithmetic, two floats an instruction where there is one
+__device__ __forceinline__ u64 pair(float x, float y) {
+  u64 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 split(u64 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) {
+  u64 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ u64 add2(u64 a, u64 b) {
+  u64 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) {
+  u64 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // N consecutive elements in the 32-bit words that they were loaded as, by accesses of up to 16 bytes (load, store) or of
 // 32 (load32, store32: the address is a multiple of it)
 template <class T, int N>
@@ -101,7 +128,15 @@ struct Pack {
     }
   }
 
- private:
+  // element e of some words, elements e and e + 1 (e even), and two elements as a word
+  __device__ static __forceinline__ u64 both(const u32* w, int e, const float*) { return pair(__uint_as_float(w[e]), __uint_as_float(w[e + 1])); }
+  __device__ static __forceinline__ u64 both(const u32* w, int e, const __nv_bfloat16*) {
+    return pair(__uint_as_float(w[e / 2] << 16), __uint_as_float(w[e / 2] & 0xffff0000u));
+  }
+  __device__ static __forceinline__ u64 both(const u32* w, int e, const __half*) {
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[e / 2]));
+    return pair(v.x, v.y);
+  }
   __device__ static __forceinline__ float one(const u32* w, int e, const float*) { return __uint_as_float(w[e]); }
   __device__ static __forceinline__ float one(const u32* w, int e, const __nv_bfloat16*) {
     return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
