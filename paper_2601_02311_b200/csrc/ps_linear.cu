@@ -22,12 +22,15 @@ using namespace train;
 using namespace tensor;
 
 constexpr int STEP = 64;                  // of the sum, a stage of the ring
-constexpr int WRITERS = 8, COPY_WARP = 8, MMA_WARP = 9, THREADS = 320;
+constexpr int WRITERS = 8, COPY_WARP = 8, MMA_WARP = 9, TILE_WARP = 10, THREADS = 352;
+constexpr int TILES_AHEAD = 2;            // tiles that a block has taken on and not yet begun to write, at most
+constexpr int LOW_SHIFT = 12;             // see multiply_scaled
 constexpr u32 BUFFER = 32 * 128;          // a warp's 32 rows of 128 bytes on their way from or to memory
 constexpr u32 LEADER = 0xFEFFFFFFu;       // a shared-memory address, in the pair's first block
 
-// What is computed: which product, the type of its result, the tile's columns, and whether two blocks share it
-enum Kind { OUTPUT, INPUT_GRAD, WEIGHT_GRAD };
+// What is computed: which product (WEIGHT_GRAD_TWO: of dPre in two parts), the type of its result, the tile's columns, and whether two
+// blocks share it
+enum Kind { OUTPUT, INPUT_GRAD, WEIGHT_GRAD, WEIGHT_GRAD_TWO };
 template <class T_, class O_, Kind KIND_, int COLUMNS_, bool PAIR_>
 struct Form {
   typedef T_ T;
@@ -35,23 +38,26 @@ struct Form {
   static constexpr Kind KIND = KIND_;
   static constexpr int COLUMNS = COLUMNS_;
   static constexpr bool PAIR = PAIR_;
-  static constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != OUTPUT;
+  static constexpr bool TWO = KIND == WEIGHT_GRAD_TWO;
+  static constexpr bool A_ACROSS = KIND == WEIGHT_GRAD || TWO, B_ACROSS = KIND != OUTPUT;
   static constexpr int B_ROWS = PAIR ? COLUMNS / 2 : COLUMNS;             // of this block
-  static constexpr u32 A_BYTES = ROWS * STEP * 2, B_BYTES = B_ROWS * STEP * 2, STAGE = A_BYTES + B_BYTES;
-  static constexpr u32 BUFFERS = WRITERS * 2 * BUFFER, AROUND = BUFFERS + WRITERS * 128 + 1024 + 256;   // (alignment, barriers)
+  static constexpr int B_LOADED = B_ACROSS ? (B_ROWS + 63) / 64 * 64 : B_ROWS;      // (panels of 64 come whole)
+  static constexpr u32 A_BYTES = ROWS * STEP * 2, B_BYTES = B_LOADED * STEP * 2, STAGE = A_BYTES + B_BYTES;
+  static constexpr u32 BUFFERS = WRITERS * 2 * BUFFER, AROUND = BUFFERS + WRITERS * 128 + 1024 + 320;   // (alignment, barriers, tiles)
   static constexpr int STAGES = (int)((227 * 1024 - AROUND) / STAGE) < 8 ? (int)((227 * 1024 - AROUND) / STAGE) : 8;
   static constexpr u32 SMEM = AROUND + STAGES * STAGE;
-  static constexpr u32 TMEM = 2 * COLUMNS;
+  static constexpr u32 SUM = COLUMNS <= 64 ? 64 : COLUMNS <= 128 ? 128 : 256, TMEM = 2 * SUM;      // columns of tensor memory
   static constexpr int CHUNK = 128 / sizeof(O);                           // columns of a buffer
   static_assert(STAGES >= 3 && COLUMNS % CHUNK == 0 && TMEM <= 512 && SMEM > 116 * 1024, "");   // (one block an SM: it takes tensor memory alone)
 };
 
 struct Product {
   u32 m, n, steps;                        // C's sizes, and stages of the sum
-  u32 m_tiles, n_tiles, splits, steps_each;
+  u32 m_tiles, n_tiles, splits, steps_each, stage_bytes;
   const void* bias;
   u32 activation, below_activation;
   u32 has_residual, has_below, has_pre;
+  ps_matrix out, pre;                     // the results, for what stores of boxes cannot write (see store_edge); out.data null: they can
   volatile u32* status;
 };
 
@@ -73,6 +79,7 @@ __device__ __forceinline__ float slope(float v) {
   if (ACT == PS_ACT_GELU) return fmaf(v * (0.5f * TANH_FACTOR), __expf(-0.5f * v * v), 0.5f * (1.f + erff(v * SQRT_HALF)));
   if (ACT == PS_ACT_GELU_TANH) {
     const float s = sigmoid(2.f * TANH_FACTOR * fmaf(TANH_CUBE * v * v, v, v));
+    if (s * (1.f - s) == 0.f) return s;                     // (far out, where the other factor may be infinite)
     return fmaf(v * s * (1.f - s), 2.f * TANH_FACTOR * fmaf(3.f * TANH_CUBE * v, v, 1.f), s);
   }
   if (ACT == PS_ACT_SILU) {
@@ -113,6 +120,21 @@ __device__ __forceinline__ bool passed_in_pair(u32 bar, u32 parity) {
 }
 __device__ __forceinline__ void arrive_at_leader(u32 bar) {
   asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
+}
+// A product whose sum goes on from what is there times 2^-LOW_SHIFT: so a matrix in two parts, the low one held 2^LOW_SHIFT times as large (16-bit floats
+// of IEEE have no small numbers), needs one sum.
+template <bool PAIR>
+__device__ __forceinline__ void multiply_scaled(u32 d, u32 a, u32 b, u32 ins) {
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.eq.u32 p, 0, 0;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p, %5;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(ins), "r"(DESC_HIGH), "n"(LOW_SHIFT) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.eq.u32 p, 0, 0;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p, %5;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(ins), "r"(DESC_HIGH), "n"(LOW_SHIFT) : "memory");
 }
 template <bool PAIR>
 __device__ __forceinline__ void wait_for(Waiter& w, u32 bar, u32 parity) {
@@ -195,6 +217,32 @@ __device__ __forceinline__ void leave_tmem(u32 at, u32 columns) {
   else tmem_free(at, columns);
 }
 
+// ---- tiles.  The grid has a block (or pair) for each; those that run take over the tiles of those that have not begun, one after the other.  (SMs' clocks
+// differ when power is short, by a third between the slowest and the fastest seen: with tiles dealt out beforehand
+// 16384 tokens, 8192 to 32768 columns, took 7.6 ms instead of 5.7.)
+template <bool PAIR>
+__device__ __forceinline__ void ask_for_tile(u32 to, u32 bar) {
+  if (PAIR)
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.multicast::cluster::all.b128 [%0], [%1];" ::"r"(to), "r"(bar) : "memory");
+  else
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(to), "r"(bar) : "memory");
+}
+// the answer's first block, or none
+__device__ __forceinline__ bool answered(u32 at, u32& block) {
+  u32 taken;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t.reg .b32 y, z, w;\n\tld.shared.b128 r, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\tselp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, r;\n\t}"
+      : "=r"(taken), "=r"(block) : "r"(at) : "memory");
+  fence_async();                                    // (read before the next answer is written)
+  return taken != 0;
+}
+__device__ __forceinline__ void expect_at(u32 bar, u32 bytes, u32 rank) {
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %2;\n\tmbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [a], %1;\n\t}"
+               ::"r"(bar), "r"(bytes), "r"(rank) : "memory");
+}
+
 // Tiles in the order in which blocks take them: bands of BAND tiles of rows, in a band column by column, so that the tiles
 // that are summed at a time share their operands in the L2.
 constexpr u32 BAND = 8;
@@ -250,8 +298,33 @@ __device__ __forceinline__ void write32(u32 buffer, u32 row, int column, const f
   }
 }
 
+// A store of a box ends at the matrix's last column, but writes 16 bytes at least: where the last column is within them, a lane stores its row from the
+// buffer itself.
+template <class E>
+__device__ __forceinline__ void store_edge(const ps_matrix& m, u32 row, u32 column, u32 rows, u32 columns, u32 buffer) {
+  constexpr u32 N = 16 / sizeof(E);
+  const u32 lane = threadIdx.x % 32;
+  if (row + lane >= rows) return;
+  E* const to = (E*)m.data + (u64)(row + lane) * m.stride + column;
+#pragma unroll
+  for (u32 i = 0; i < 8; ++i) {
+    const uint4 w = read16(buffer + piece_at<E>(lane, 0, i));
+    if (column + (i + 1) * N <= columns) {
+      *reinterpret_cast<uint4*>(to + i * N) = w;
+    } else {
+      const u32 words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (u32 e = 0; e < N; ++e)
+        if (column + i * N + e < columns) {
+          if constexpr (sizeof(E) == 4) reinterpret_cast<u32*>(to)[i * N + e] = words[e];
+          else reinterpret_cast<unsigned short*>(to)[i * N + e] = (unsigned short)(words[e / 2] >> (16 * (e % 2)));
+        }
+    }
+  }
+}
+
 struct Maps {
-  CUtensorMap a, b, out, residual, more;        // more: pre, written, or below, read
+  CUtensorMap a, b, out, residual, more, low;   // more: pre, written, or below, read; low: a's second part
 };
 
 template <class F>
@@ -269,6 +342,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   const auto sum_full = [&](int s) { return bars + 8 * (2 * STAGES + s); };
   const auto sum_empty = [&](int s) { return bars + 8 * (2 * STAGES + 2 + s); };
   const auto input = [&](int w) { return bars + 8 * (2 * STAGES + 4 + w); };
+  const auto tile_full = [&](u32 n) { return bars + 8 * (2 * STAGES + 4 + WRITERS + n % TILES_AHEAD); };
+  const auto tile_empty = [&](u32 n) { return bars + 8 * (2 * STAGES + 4 + WRITERS + TILES_AHEAD + n % TILES_AHEAD); };
+  const auto answer = [&](u32 n) { return bars + 256 + 16 * (n % TILES_AHEAD); };
   __shared__ u32 tmem_at;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const u32 rank = PAIR ? rank_in_pair() : 0;
@@ -277,6 +353,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     for (int s = 0; s < STAGES; ++s) barrier_init(full(s), 1), barrier_init(empty(s), 1);
     for (int s = 0; s < 2; ++s) barrier_init(sum_full(s), 1), barrier_init(sum_empty(s), WRITERS * (PAIR ? 2 : 1));
     for (int w = 0; w < WRITERS; ++w) barrier_init(input(w), 1);
+    for (u32 n = 0; n < TILES_AHEAD; ++n) barrier_init(tile_full(n), 1), barrier_init(tile_empty(n), PAIR ? 2 * WRITERS + 4 : WRITERS + 3);
     fence_barrier_init();
   }
   if (warp == MMA_WARP) take_tmem<PAIR>(smem_address(&tmem_at), F::TMEM);
@@ -286,38 +363,53 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   fence_after();
   const u32 tmem = tmem_at;
 
-  const u32 tiles = p.m_tiles * p.n_tiles * p.splits;
-  const u32 first = PAIR ? blockIdx.x / 2 : blockIdx.x, stride = PAIR ? gridDim.x / 2 : gridDim.x;
+  const u32 first = PAIR ? blockIdx.x / 2 : blockIdx.x;
   Waiter waiter(p.status);
+  // a role's n-th answer: the tile to go on with, or none.  `speaks`: the thread that says that it has been read
+  const auto next_tile = [&](u32 n, u32& t, bool speaks) {
+    wait_for<PAIR>(waiter, tile_full(n), (n / TILES_AHEAD) & 1);
+    u32 block = 0;
+    const bool more = !waiter.dead && answered(answer(n), block);
+    t = PAIR ? block / 2 : block;
+    if (speaks) {
+      if (PAIR) arrive_at_leader(tile_empty(n));
+      else barrier_arrive(tile_empty(n));
+    }
+    return more;
+  };
 
   if (warp == COPY_WARP) {
     if (elected()) {
       u32 turn = 0;                                 // stages filled so far
-      for (u32 t = first; t < tiles && !waiter.dead; t += stride) {
+      u32 count = 0, t = first;
+      do {
         const Tile tile = tile_at(p, t);
         const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS), column = (int)(tile.n * F::COLUMNS + rank * F::B_ROWS);
         const u32 begin = tile.part * p.steps_each, end = min(begin + p.steps_each, p.steps);
-        for (u32 k = begin; k < end; ++k, ++turn) {
-          const int s = turn % STAGES;
-          wait_for<PAIR>(waiter, empty(s), (turn / STAGES + 1) & 1);
-          if (waiter.dead) break;
-          if (rank == 0) barrier_expect(full(s), (PAIR ? 2 : 1) * F::STAGE);
-          const u32 a = ring + s * F::STAGE, b = a + F::A_BYTES;
-          const int at = (int)(k * STEP);
-          if (F::A_ACROSS) {
+#pragma unroll 1
+        for (int low = F::TWO ? 1 : 0; low >= 0; --low)
+          for (u32 k = begin; k < end; ++k, ++turn) {
+            const int s = turn % STAGES;
+            wait_for<PAIR>(waiter, empty(s), (turn / STAGES + 1) & 1);
+            if (waiter.dead) break;
+            if (rank == 0) barrier_expect(full(s), (PAIR ? 2 : 1) * p.stage_bytes);
+            const u32 a = ring + s * F::STAGE, b = a + F::A_BYTES;
+            const CUtensorMap* const a_map = low ? &maps.low : &maps.a;
+            const int at = (int)(k * STEP);
+            if (F::A_ACROSS) {
 #pragma unroll
-            for (int i = 0; i < ROWS / 64; ++i) load_box<PAIR>(a + i * ACROSS_PANEL, &maps.a, row + 64 * i, at, full(s));
-          } else {
-            load_box<PAIR>(a, &maps.a, at, row, full(s));
-          }
-          if (F::B_ACROSS) {
+              for (int i = 0; i < ROWS / 64; ++i) load_box<PAIR>(a + i * ACROSS_PANEL, a_map, row + 64 * i, at, full(s));
+            } else {
+              load_box<PAIR>(a, a_map, at, row, full(s));
+            }
+            if (F::B_ACROSS) {
 #pragma unroll
-            for (int i = 0; i < F::B_ROWS / 64; ++i) load_box<PAIR>(b + i * ACROSS_PANEL, &maps.b, column + 64 * i, at, full(s));
-          } else {
-            load_box<PAIR>(b, &maps.b, at, column, full(s));
+              for (int i = 0; i < F::B_LOADED / 64; ++i) load_box<PAIR>(b + i * ACROSS_PANEL, &maps.b, column + 64 * i, at, full(s));
+            } else {
+              load_box<PAIR>(b, &maps.b, at, column, full(s));
+            }
           }
-        }
-      }
+      } while (!waiter.dead && next_tile(count++, t, true));
       if (rank == 0) {                              // leave no copy in flight, also where a wait has run out
         Waiter last(p.status);
         for (u32 i = turn > STAGES ? turn - STAGES : 0; i < turn; ++i) wait_for<PAIR>(last, full(i % STAGES), (i / STAGES) & 1);
@@ -327,33 +419,53 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   } else if (warp == MMA_WARP) {
     if (rank == 0 && elected()) {
       constexpr u32 ins = instruction_of<F>();
-      u32 turn = 0, count = 0;
-      for (u32 t = first; t < tiles && !waiter.dead; t += stride, ++count) {
+      u32 turn = 0, count = 0, t = first;
+      do {
         const u32 part = tile_at(p, t).part;
         const u32 begin = part * p.steps_each, end = min(begin + p.steps_each, p.steps);
-        const u32 d = tmem + (count & 1) * F::COLUMNS;
+        const u32 d = tmem + (count & 1) * F::SUM;
         wait_for<PAIR>(waiter, sum_empty(count & 1), (count / 2 + 1) & 1);
         fence_after();
-        for (u32 k = begin; k < end && !waiter.dead; ++k, ++turn) {
-          const int s = turn % STAGES;
-          wait_for<PAIR>(waiter, full(s), (turn / STAGES) & 1);
-          if (waiter.dead) break;
-          fence_after();
-          const u32 a = descriptor<F::A_ACROSS>(ring + s * F::STAGE), b = descriptor<F::B_ACROSS>(ring + s * F::STAGE + F::A_BYTES);
+#pragma unroll 1
+        for (int low = F::TWO ? 1 : 0; low >= 0; --low)
+          for (u32 k = begin; k < end && !waiter.dead; ++k, ++turn) {
+            const int s = turn % STAGES;
+            wait_for<PAIR>(waiter, full(s), (turn / STAGES) & 1);
+            if (waiter.dead) break;
+            fence_after();
+            const u32 a = descriptor<F::A_ACROSS>(ring + s * F::STAGE), b = descriptor<F::B_ACROSS>(ring + s * F::STAGE + F::A_BYTES);
 #pragma unroll
-          for (int i = 0; i < STEP / 16; ++i) multiply<PAIR>(d, a + step_of<F::A_ACROSS>(i), b + step_of<F::B_ACROSS>(i), ins, k > begin || i > 0);
-          commit_to<PAIR>(empty(s));
-        }
+            for (int i = 0; i < STEP / 16; ++i) {
+              if (F::TWO && i == 0 && low == 0 && k == begin) multiply_scaled<PAIR>(d, a, b, ins);
+              else multiply<PAIR>(d, a + step_of<F::A_ACROSS>(i), b + step_of<F::B_ACROSS>(i), ins, k > begin || i > 0);
+            }
+            commit_to<PAIR>(empty(s));
+          }
         if (!waiter.dead) commit_to<PAIR>(sum_full(count & 1));
+      } while (!waiter.dead && next_tile(count++, t, true));
+    }
+    __syncwarp();
+  } else if (warp == TILE_WARP) {
+    if (rank == 0 && elected()) {
+      u32 t;
+      for (u32 n = 0; !waiter.dead; ++n) {
+        wait_for<PAIR>(waiter, tile_empty(n), (n / TILES_AHEAD + 1) & 1);
+        if (waiter.dead) break;
+        if (PAIR) expect_at(tile_full(n), 16, 0), expect_at(tile_full(n), 16, 1);
+        else barrier_expect(tile_full(n), 16);
+        ask_for_tile<PAIR>(answer(n), tile_full(n));
+        if (!next_tile(n, t, true)) break;
       }
     }
+    __syncwarp();
     __syncwarp();
   } else {
     const u32 mine = buffers + warp * 2 * BUFFER, other = mine + BUFFER;       // result and residual; pre or below
     const u32 bias_at = biases + warp * 128;
     const int quarter = warp % 4, half = warp / 4;
-    u32 count = 0, inputs = 0;
-    for (u32 t = first; t < tiles; t += stride, ++count) {
+    u32 count = 0, inputs = 0, t = first;
+    bool more = true;
+    do {
       const Tile tile = tile_at(p, t);
       const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS + quarter * 32);
       bool waited = false;
@@ -389,7 +501,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
 #pragma unroll
         for (int h = 0; h < CHUNK; h += 32) {
           u32 sum[32];
-          tmem_load32(sum, tmem + ((u32)(quarter * 32) << 16) + (count & 1) * F::COLUMNS + c * CHUNK + h);
+          tmem_load32(sum, tmem + ((u32)(quarter * 32) << 16) + (count & 1) * F::SUM + c * CHUNK + h);
           wait_loads();
           float v[32];
 #pragma unroll
@@ -421,6 +533,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           }
           write32<O>(mine, lane, h, v);
         }
+        if (p.out.data && column + CHUNK > (int)p.n) {
+          store_edge<O>(p.out, row, column, p.m, p.n, mine);
+          if (F::KIND == OUTPUT && p.has_pre) store_edge<T>(p.pre, row, column, p.m, p.n, other);
+          __syncwarp();
+          continue;
+        }
         fence_async();
         __syncwarp();
         if (lane == 0) {
@@ -440,7 +558,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         if (PAIR) arrive_at_leader(sum_empty(count & 1));
         else barrier_arrive(sum_empty(count & 1));
       }
-    }
+      more = !waiter.dead && next_tile(count, t, false);
+      more = __all_sync(0xffffffffu, more);
+      if (lane == 0) {                              // (all lanes have read it)
+        if (PAIR) arrive_at_leader(tile_empty(count));
+        else barrier_arrive(tile_empty(count));
+      }
+      ++count;
+    } while (more);
     if (lane == 0) wait_stores_done();
     __syncwarp();
   }
@@ -465,10 +590,10 @@ __global__ void __launch_bounds__(256) k_join_parts(const float* parts, u32 spli
   }
 }
 
-// ---- dPre = dY o act'(pre), and its sums by columns: a warp has 256 columns, 8 a lane, a block eight rows at a time
+// ---- dPre = dY o act'(pre), rounded, and where `low` is given what the rounding took, 2^LOW_SHIFT times as large; and its sums by columns: a warp has 256 columns, 8 a lane, a block eight rows at a time
 constexpr int SLOPE_COLUMNS = 256, SLOPE_WARPS = 8;
 template <class T>
-__global__ void __launch_bounds__(SLOPE_WARPS * 32) k_slope(const ps_matrix d_y, const ps_matrix pre, const ps_matrix d_pre, u64 rows, u32 cols,
+__global__ void __launch_bounds__(SLOPE_WARPS * 32) k_slope(const ps_matrix d_y, const ps_matrix pre, const ps_matrix d_pre, const ps_matrix low, u64 rows, u32 cols,
                                                            u64 rows_each, u32 activation, float* parts) {
   __shared__ float sums[SLOPE_WARPS][SLOPE_COLUMNS];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -481,6 +606,11 @@ __global__ void __launch_bounds__(SLOPE_WARPS * 32) k_slope(const ps_matrix d_y,
     if (here == 8) p.load(from);
     else
       for (int e = 0; e < here; ++e) p.w[e / 2] |= (u32)*reinterpret_cast<const unsigned short*>(from + e) << (16 * (e % 2));
+  };
+  const auto store = [&](T* to, const Pack<T, 8>& p) {
+    if (here == 8) p.store(to);
+    else
+      for (int e = 0; e < here; ++e) reinterpret_cast<unsigned short*>(to)[e] = (unsigned short)(p.w[e / 2] >> (16 * (e % 2)));
   };
   if (here > 0)
 #pragma unroll 2
@@ -495,10 +625,15 @@ __global__ void __launch_bounds__(SLOPE_WARPS * 32) k_slope(const ps_matrix d_y,
         at.widen(x);
         times_slope(activation, v, x);
         g.narrow(v);
-        T* const to = (T*)d_pre.data + r * d_pre.stride + column;
-        if (here == 8) g.store(to);
-        else
-          for (int e = 0; e < here; ++e) reinterpret_cast<unsigned short*>(to)[e] = (unsigned short)(g.w[e / 2] >> (16 * (e % 2)));
+        store((T*)d_pre.data + r * d_pre.stride + column, g);
+        if (low.data) {
+          float f[8];
+          g.widen(f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = (v[e] - f[e]) * (float)(1 << LOW_SHIFT);
+          g.narrow(f);
+          store((T*)low.data + r * low.stride + column, g);
+        }
       } else {
         g.widen(v);
       }
@@ -544,6 +679,8 @@ bool encode(CUtensorMap& map, u32 dtype, const ps_matrix& m, u64 rows, u64 cols,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+constexpr ps_matrix NOTHING = {nullptr, 0};
+
 // C[m][n] = sum over k of A B, and what is done with it
 struct Call {
   Kind kind;
@@ -552,6 +689,7 @@ struct Call {
   u32 parts;                              // of the sum, stored one behind the other
   const void* bias;
   u32 activation, below_activation;
+  ps_matrix low;                          // a's second part (WEIGHT_GRAD_TWO)
 };
 
 template <class F>
@@ -571,9 +709,19 @@ cudaError_t product(u32 dtype, const Call& c, volatile u32* status, int sm_count
   p.has_below = F::KIND == INPUT_GRAD && c.more.data;
   p.has_pre = F::KIND == OUTPUT && c.more.data;
   p.status = status;
-  bool ok = F::A_ACROSS ? encode<T>(maps.a, dtype, c.a, c.k, c.m, STEP, 0) : encode<T>(maps.a, dtype, c.a, c.m, c.k, ROWS, 0);
-  ok = ok && (F::B_ACROSS ? encode<T>(maps.b, dtype, c.b, c.k, c.n, STEP, 0) : encode<T>(maps.b, dtype, c.b, c.n, c.k, F::B_ROWS, 0));
+  if (c.n % (16 / sizeof(O)) && c.parts == 1) {            // (the parts' rows are whole 16 bytes)
+    p.out = c.out;
+    if (p.has_pre) p.pre = c.more;
+  }
+  // Boxes have no more rows than the matrix (in eights): a copy takes its time for rows that are not there as well.  (What then stands in the
+  // rest of a tile in shared memory becomes results that are not stored.  A token, 8192 to 8192 columns: 33 us, with boxes of 128 rows 56.)
+  const auto box_rows = [](u64 rows, u32 most) { return (u32)std::min<u64>((rows + 7) / 8 * 8, most); };
+  const u32 a_rows = F::A_ACROSS ? STEP : box_rows(c.m, ROWS), b_rows = F::B_ACROSS ? STEP : box_rows(c.n, F::B_ROWS);
+  p.stage_bytes = (F::A_ACROSS ? F::A_BYTES : a_rows * 128) + (F::B_ACROSS ? F::B_BYTES : b_rows * 128);
+  bool ok = F::A_ACROSS ? encode<T>(maps.a, dtype, c.a, c.k, c.m, a_rows, 0) : encode<T>(maps.a, dtype, c.a, c.m, c.k, a_rows, 0);
+  ok = ok && (F::B_ACROSS ? encode<T>(maps.b, dtype, c.b, c.k, c.n, b_rows, 0) : encode<T>(maps.b, dtype, c.b, c.n, c.k, b_rows, 0));
   ok = ok && encode<O>(maps.out, dtype, c.out, c.m, c.n, 32, c.parts);
+  if (F::TWO) ok = ok && encode<T>(maps.low, dtype, c.low, c.k, c.m, STEP, 0);
   if (p.has_residual) ok = ok && encode<O>(maps.residual, dtype, c.residual, c.m, c.n, 32, 1);
   if (c.more.data) ok = ok && encode<T>(maps.more, dtype, c.more, c.m, c.n, 32, 1);
   if (!ok) return cudaErrorInvalidValue;
@@ -587,12 +735,12 @@ cudaError_t product(u32 dtype, const Call& c, volatile u32* status, int sm_count
     if (device < 64) prepared |= (u64)1 << device;
   }
   const u64 tiles = (u64)p.m_tiles * p.n_tiles * p.splits;
-  if (tiles > 0x7fffffffu) return cudaErrorInvalidValue;
+  if (tiles > 0x3fffffffu) return cudaErrorInvalidValue;
   cudaLaunchAttribute pair;
   pair.id = cudaLaunchAttributeClusterDimension;
   pair.val.clusterDim.x = 2, pair.val.clusterDim.y = pair.val.clusterDim.z = 1;
   cudaLaunchConfig_t config = {};
-  config.gridDim = dim3(F::PAIR ? 2 * (u32)std::min<u64>(tiles, sm_count / 2) : (u32)std::min<u64>(tiles, sm_count));
+  config.gridDim = dim3(F::PAIR ? 2 * (u32)tiles : (u32)tiles);
   config.blockDim = dim3(THREADS);
   config.dynamicSmemBytes = F::SMEM;
   config.stream = stream;
@@ -601,16 +749,36 @@ cudaError_t product(u32 dtype, const Call& c, volatile u32* status, int sm_count
   return cudaLaunchKernelEx(&config, k_product<F>, maps, p);
 }
 
-// Tiles of 256 x 256 by pairs where they fill the device, else of 128 x 128, or 128 x 64 where there are few.
+// The tile's shape: the one with which the blocks are done first by what was measured of it, in cycles: for 64 steps of the sum, for writing a tile (of
+// which the longer counts, tile after tile), and for a launch's beginning and end.
+struct TileCost {
+  u32 rows, columns;
+  bool pair;
+  u32 step, write, around;
+};
+constexpr TileCost TILE_COSTS[] = {{256, 256, true, 600, 3800, 13000}, {256, 192, true, 510, 3400, 12000}, {256, 128, true, 395, 1900, 11000},
+                                   {128, 128, false, 450, 1500, 10500}, {128, 64, false, 320, 1400, 9500}};
 template <class T, class O, Kind KIND>
 cudaError_t product_of(u32 dtype, const Call& c, volatile u32* status, int sm_count, cudaStream_t stream) {
-  const auto tiles = [&](u64 m, u64 n) { return ((c.m + m - 1) / m) * ((c.n + n - 1) / n) * c.parts; };
-  if (tiles(256, 256) >= (u64)sm_count / 2) return product<Form<T, O, KIND, 256, true>>(dtype, c, status, sm_count, stream);
-  if (tiles(128, 128) >= (u64)sm_count / 2) return product<Form<T, O, KIND, 128, false>>(dtype, c, status, sm_count, stream);
+  const u64 steps = ((c.k + STEP - 1) / STEP + c.parts - 1) / c.parts * (KIND == WEIGHT_GRAD_TWO ? 2 : 1);
+  u64 costs[5];
+  for (int i = 0; i < 5; ++i) {
+    const TileCost& t = TILE_COSTS[i];
+    const u64 tiles = ((c.m + t.rows - 1) / t.rows) * ((c.n + t.columns - 1) / t.columns) * c.parts, at_once = t.pair ? sm_count / 2 : sm_count;
+    // (half of a tile of 192 columns that lie across the sum is loaded as 128)
+    const u64 step = i == 1 && KIND != OUTPUT ? 640 : t.step;
+    costs[i] = (tiles + at_once - 1) / at_once * std::max<u64>(steps * step, t.write) + t.around;
+  }
+  int best = 0;
+  for (int i = 1; i < 5; ++i)
+    if (costs[i] < costs[best]) best = i;
+  if (best == 0) return product<Form<T, O, KIND, 256, true>>(dtype, c, status, sm_count, stream);
+  if (best == 1) return product<Form<T, O, KIND, 192, true>>(dtype, c, status, sm_count, stream);
+  if (best == 2) return product<Form<T, O, KIND, 128, true>>(dtype, c, status, sm_count, stream);
+  if (best == 3) return product<Form<T, O, KIND, 128, false>>(dtype, c, status, sm_count, stream);
   return product<Form<T, O, KIND, 64, false>>(dtype, c, status, sm_count, stream);
 }
 
-constexpr ps_matrix NOTHING = {nullptr, 0};
 constexpr u64 SMS = 148;          // (what a sum's order depends on does not ask the device)
 
 // parts of the sum over the tokens for dW: as many as bring tiles for all SMs, each of 16 stages at least
@@ -628,12 +796,12 @@ u64 slope_chunks(const LinearArgs& a) {
   return std::max<u64>(1, std::min<u64>((a.tokens + 31) / 32, (6 * SMS + across - 1) / across));
 }
 struct Work {
-  size_t d_pre, sums, parts, all;
+  size_t low, sums, parts, all;           // (d_pre stands first)
 };
 Work work_of(const LinearArgs& a) {
   Work w;
-  w.d_pre = 0;
-  w.sums = a.activation ? up(a.tokens * up(a.outputs, 8) * 2, 256) : 0;
+  w.low = a.activation ? up(a.tokens * up(a.outputs, 8) * 2, 256) : 0;
+  w.sums = a.activation && a.grad_dtype == PS_F32 ? 2 * w.low : w.low;
   w.parts = w.sums + up(slope_chunks(a) * a.outputs * 4, 256);
   const u32 parts = weight_parts(a);
   w.all = w.parts + (parts > 1 ? parts * a.outputs * up(a.inputs, 4) * 4 : 0);
@@ -642,7 +810,7 @@ Work work_of(const LinearArgs& a) {
 
 template <class T>
 cudaError_t forward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
-  Call c = {OUTPUT, a.x, a.weight, a.y, a.residual, a.pre, a.tokens, a.outputs, a.inputs, 1, a.bias, a.activation, 0};
+  Call c = {OUTPUT, a.x, a.weight, a.y, a.residual, a.pre, a.tokens, a.outputs, a.inputs, 1, a.bias, a.activation, 0, NOTHING};
   return product_of<T, T, OUTPUT>(a.dtype, c, a.status, sm_count, stream);
 }
 
@@ -650,20 +818,21 @@ template <class T>
 cudaError_t backward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
   const Work w = work_of(a);
   char* const work = (char*)a.work;
-  ps_matrix d_pre = a.d_y;
+  ps_matrix d_pre = a.d_y, low = NOTHING;
   const bool products = a.d_x.data || a.d_weight.data;
   if (a.activation || a.d_bias) {
     float* const sums = a.d_bias ? (float*)(work + w.sums) : nullptr;
-    if (a.activation) d_pre = {work + w.d_pre, up(a.outputs, 8)};
+    if (a.activation) d_pre = {work, up(a.outputs, 8)};
+    if (a.activation && a.grad_dtype == PS_F32 && a.d_weight.data) low = {work + w.low, up(a.outputs, 8)};
     const u64 chunks = slope_chunks(a), each = (a.tokens + chunks - 1) / chunks;
     k_slope<T><<<dim3((u32)((a.outputs + SLOPE_COLUMNS - 1) / SLOPE_COLUMNS), (u32)chunks), SLOPE_WARPS * 32, 0, stream>>>(
-        a.d_y, a.pre, d_pre, a.tokens, (u32)a.outputs, each, a.activation, sums);
+        a.d_y, a.pre, d_pre, low, a.tokens, (u32)a.outputs, each, a.activation, sums);
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess && sums) e = join_columns(a.grad_dtype, sums, (u32)chunks, 1, a.outputs, a.d_bias, nullptr, a.accumulate, stream);
     if (e != cudaSuccess || !products) return e;
   }
   if (a.d_x.data && a.tokens) {
-    const Call c = {INPUT_GRAD, d_pre, a.weight, a.d_x, a.residual, a.below, a.tokens, a.inputs, a.outputs, 1, nullptr, 0, a.below_activation};
+    const Call c = {INPUT_GRAD, d_pre, a.weight, a.d_x, a.residual, a.below, a.tokens, a.inputs, a.outputs, 1, nullptr, 0, a.below_activation, NOTHING};
     const cudaError_t e = product_of<T, T, INPUT_GRAD>(a.dtype, c, a.status, sm_count, stream);
     if (e != cudaSuccess) return e;
   }
@@ -674,14 +843,16 @@ cudaError_t backward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
   }
   if (a.d_weight.data) {
     const u32 parts = weight_parts(a);
-    Call c = {WEIGHT_GRAD, d_pre, a.x, a.d_weight, a.accumulate ? a.d_weight : NOTHING, NOTHING, a.outputs, a.inputs, a.tokens, parts, nullptr, 0, 0};
+    Call c = {WEIGHT_GRAD, d_pre, a.x, a.d_weight, a.accumulate ? a.d_weight : NOTHING, NOTHING, a.outputs, a.inputs, a.tokens, parts, nullptr, 0, 0, low};
+    if (parts == 1 && low.data) return product_of<T, float, WEIGHT_GRAD_TWO>(a.dtype, c, a.status, sm_count, stream);
     if (parts == 1)
       return a.grad_dtype == PS_F32 ? product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream)
                                     : product_of<T, T, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
     const u32 pitch = (u32)up(a.inputs, 4);
     c.out = {work + w.parts, pitch};
     c.residual = NOTHING;
-    cudaError_t e = product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
+    cudaError_t e = low.data ? product_of<T, float, WEIGHT_GRAD_TWO>(a.dtype, c, a.status, sm_count, stream)
+                             : product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
     if (e != cudaSuccess) return e;
     const dim3 grid((u32)((a.inputs + 255) / 256), (u32)std::min<u64>(a.outputs, 65535));
     const float* const from = (const float*)(work + w.parts);

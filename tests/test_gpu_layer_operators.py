@@ -389,3 +389,310 @@ def test_linear_of_whole_numbers(ctx, dtype, tokens, inputs, outputs):
     assert torch.equal(d_x, ((d_pre @ w.double()) * (below > 0) + in_res.double()).to(t))
     assert torch.equal(d_w, (d_pre.t() @ x.double()).to(t)) and torch.equal(d_b, d_pre.sum(0).to(t))
     ctx.check_status()
+
+
+def activation_want(v, name, with_slope):
+    """An activation or its derivative in 64 bits."""
+    v = v.detach().clone().requires_grad_()
+    y = {"none": lambda: v * 1.0, "relu": lambda: v.clamp(min=0.0), "gelu": lambda: v * 0.5 * torch.erfc(-v * math.sqrt(0.5)),
+         "gelu_tanh": lambda: 0.5 * v * (1 + torch.tanh(math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3))), "silu": lambda: v * torch.sigmoid(v)}[name]()
+    if not with_slope:
+        return y.detach()
+    return torch.where(v > 0, 1.0, 0.0).double() if name == "relu" else torch.autograd.grad(y.sum(), v)[0]
+
+
+ACTIVATIONS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+def products_err(a, b, dims):
+    """Sums on the tensor cores: sixteen products at a time, then one sum after the other, bits cut off rather than rounded (2 F)."""
+    return 2 * F * (dims / 16 + 16) * (a.double().abs() @ b.double().abs())
+
+
+def function_err(v, name):
+    """What the fast exponential (2 + 1.2 |argument| units of 2 F, arguments up to 1.6 |v| + 0.08 |v|^3 and up to 88), erf (2 units) and the
+    few operations around them do to an activation, relative to 1 + |v|."""
+    v = v.abs()
+    argument = {"none": 0 * v, "relu": 0 * v, "gelu": v * v / 2, "gelu_tanh": 1.6 * v + 0.072 * v ** 3, "silu": v}[name].clamp(max=88)
+    return 2 * F * (8 + 1.2 * argument) * (1 + v) * torch.where(argument >= 88, 0.0, 1.0) + 8 * F * (1 + v)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("activation", ACTIVATIONS)
+@pytest.mark.parametrize("tokens, inputs, outputs", [(3, 40, 70), (260, 200, 333), (1300, 264, 1301), (2500, 72, 2100)])
+def test_linear(ctx, dtype, activation, tokens, inputs, outputs):
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(tokens)
+    x, w = matrix(gen, tokens, inputs, t), matrix(gen, outputs, inputs, t, 2 * inputs ** -0.5)
+    bias, res = normal(gen, outputs, dtype=t), matrix(gen, tokens, outputs, t)
+    want = x.double() @ w.double().t() + bias.double()
+    err = products_err(x, w.t(), inputs) + F * want.abs()
+    y, pre = ctx.linear_forward(x, w, bias, activation, res, keep=True)
+    within(pre, want, err + rounded(want, t), "pre")
+    after = activation_want(want, activation, False)
+    # every slope is below 1.13
+    act_err = 1.13 * err + function_err(want, activation)
+    within(y, after + res.double(), act_err + F * (after + res.double()).abs() + rounded(after + res.double(), t), "y")
+    within(ctx.linear_forward(x, w, bias, activation), after, act_err + rounded(after, t), "y alone")
+    ctx.check_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("activation, below", [("none", "none"), ("none", "gelu"), ("gelu", "none"), ("gelu_tanh", "silu"), ("silu", "gelu_tanh"), ("relu", "relu")])
+@pytest.mark.parametrize("tokens, inputs, outputs", [(3, 40, 70), (333, 200, 260), (1300, 264, 1301), (5000, 130, 120), (2500, 2100, 72)])
+def test_linear_gradients(ctx, dtype, activation, below, tokens, inputs, outputs):
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(tokens + outputs)
+    x, w, d_y = matrix(gen, tokens, inputs, t), matrix(gen, outputs, inputs, t, inputs ** -0.5), matrix(gen, tokens, outputs, t)
+    pre, under, res = matrix(gen, tokens, outputs, t, 2.0), matrix(gen, tokens, inputs, t, 2.0), matrix(gen, tokens, inputs, t)
+    d_pre = d_y.double() * activation_want(pre.double(), activation, True)
+    exact_err = d_y.double().abs() * function_err(pre.double(), activation) + F * d_pre.abs()        # before it is rounded
+    pre_err = exact_err + (rounded(d_pre, t) if activation != "none" else 0.0)
+    slopes = activation_want(under.double(), below, True)
+    for wide in (None, torch.float32):
+        d_x, d_w, d_b = ctx.linear_backward(d_y, x, w, None if activation == "none" else pre, activation, None if below == "none" else under, below,
+                                            res, wide)
+        ctx.check_status()
+        sums = d_pre @ w.double()
+        want = sums * slopes + res.double()
+        err = (products_err(d_pre, w, outputs) + pre_err @ w.double().abs()) * slopes.abs() + sums.abs() * function_err(under.double(), below)
+        within(d_x, want, 1.01 * err + 2 * F * want.abs() + F * sums.abs() + rounded(want, t), "d_x")
+        want = d_pre.t() @ x.double()
+        # in 32 bits dPre comes in two parts: what is left out is a rounding of a rounding, of a number 2^12 times as large
+        left = exact_err + (u_of(t) * rounded(d_pre, t) + tiny_of(t) / 4096 if activation != "none" else 0.0) if wide else pre_err
+        err = 2 * products_err(d_pre.t(), x, tokens) + left.t() @ x.double().abs()
+        within(d_w, want, err + 2 * F * want.abs() + rounded(want, wide or t), "d_weight")
+        want = d_pre.sum(0)
+        within(d_b, want, exact_err.sum(0) + (tokens + 64) * F * d_pre.abs().sum(0) + rounded(want, wide or t), "d_bias")
+        again = ctx.linear_backward(d_y, x, w, None if activation == "none" else pre, activation, None if below == "none" else under, below, res, wide)
+        assert all(torch.equal(a, b) for a, b in zip((d_x, d_w, d_b), again))
+
+
+def test_linear_gradients_against_differences(ctx):
+    """Of sum(y * d_y) through a gelu, against central differences in 64 bits."""
+    gen = torch.Generator("cuda").manual_seed(8)
+    x, w, d_y = matrix(gen, 20, 24, torch.float16), matrix(gen, 16, 24, torch.float16, 0.3), matrix(gen, 20, 16, torch.float16)
+    bias = normal(gen, 16, dtype=torch.float16)
+    _, pre = ctx.linear_forward(x, w, bias, "gelu", keep=True)
+    grads = ctx.linear_backward(d_y, x, w, pre, "gelu", dtype=torch.float32)
+    args = [a.double().contiguous() for a in (x, w, bias)]
+
+    def value(x, w, b):
+        return (activation_want(x @ w.t() + b, "gelu", False) * d_y.double()).sum().item()
+    for which, grad in enumerate(grads):
+        grad = grad.double().contiguous()
+        for at in range(0, grad.numel(), 13):
+            ends = []
+            for sign in (1, -1):
+                moved = [a.clone() for a in args]
+                moved[which].view(-1)[at] += sign * 1e-4
+                ends.append(value(*moved))
+            # pre is rounded to 2^-11 of up to 5, a slope changes by at most 0.8 of that; d_x is rounded; sums of at most 20 such terms of up to 12
+            assert abs((ends[0] - ends[1]) / 2e-4 - grad.view(-1)[at].item()) < 20 * 12 * 0.8 * 5 * 2.0 ** -11
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_linear_rows_and_columns_do_not_see_each_other(ctx, dtype):
+    """The bits of a row, and of a column, are those of a call that has it alone: in tiles of every shape, beside rows of NaN."""
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(2)
+    x, w = matrix(gen, 2600, 520, t), matrix(gen, 2304, 520, t)
+    bias, res = normal(gen, 2304, dtype=t), matrix(gen, 2600, 2304, t)
+    y = ctx.linear_forward(x, w, bias, "gelu", res)
+    for rows, cols in ((slice(0, 1), slice(0, 2304)), (slice(700, 829), slice(0, 200)), (slice(3, 1003), slice(1000, 2200)), (slice(0, 2600), slice(2300, 2304)),
+                       (slice(100, 2148), slice(0, 1600))):
+        at = matrix(gen, rows.stop - rows.start, cols.stop - cols.start, t).copy_(res[rows, cols])
+        part = ctx.linear_forward(x[rows], w[cols], bias[cols], "gelu", at)
+        assert torch.equal(part, y[rows, cols])
+    d_y = matrix(gen, 2600, 2304, t)
+    below = matrix(gen, 2600, 520, t)
+    d_x = ctx.linear_backward(d_y, x, w, below=below, below_activation="silu")[0]
+    for rows in (slice(5, 6), slice(64, 200), slice(1000, 2600)):
+        part = torch.empty_like(x[rows])
+        ctx.linear_backward_into(d_y[rows], None, w, d_x=part, below=below[rows], below_activation="silu")
+        assert torch.equal(part, d_x[rows])
+    bad = x.clone()
+    bad[77] = math.nan
+    got = ctx.linear_forward(bad, w, bias, "gelu", res)
+    ctx.check_status()
+    keep = torch.arange(2600, device="cuda") != 77
+    assert torch.equal(got[keep], y[keep]) and got[77].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_linear_into_larger_tensors(ctx, dtype):
+    """What lies around a result is left alone; a residual may be the result; parts of the gradients; added to what is there."""
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(3)
+    whole = {n: normal(gen, r, c, dtype=t) for n, r, c in (("x", 150, 200), ("w", 140, 200), ("y", 150, 304), ("pre", 150, 304), ("dx", 150, 200))}
+    x, w, y, pre = whole["x"][5:138, 16:165], whole["w"][2:133, 8:157], whole["y"][1:134, 8:139], whole["pre"][7:140, 160:291]
+    before = {n: v.clone() for n, v in whole.items()}
+    start = y.clone()
+    bias = normal(gen, 140, dtype=t)[3:134]
+    want = ctx.linear_forward(x, w, bias, "silu", matrix(gen, 133, 131, t).copy_(start), keep=True)
+    ctx.linear_forward_into(x, w, y, bias, "silu", residual=y, pre=pre)
+    assert torch.equal(y, want[0]) and torch.equal(pre, want[1])
+    d_x, d_w, d_b = ctx.linear_backward(y, x, w, pre, "silu", residual=x)
+    into = whole["dx"][5:138, 16:165]
+    into.copy_(x)
+    wide_w, wide_b = normal(gen, 131, 152)[:, :149], normal(gen, 131)
+    w0, b0 = wide_w.clone(), wide_b.clone()
+    ctx.linear_backward_into(y, None, w, d_x=into, pre=pre, activation="silu", residual=into)
+    exact_w, exact_b = ctx.linear_backward(y, x, w, pre, "silu", dtype=torch.float32)[1:]
+    ctx.linear_backward_into(y, x, None, d_weight=wide_w, d_bias=wide_b, pre=pre, activation="silu", accumulate=True)
+    assert torch.equal(into, d_x) and torch.equal(wide_w, exact_w + w0) and torch.equal(wide_b, exact_b + b0)
+    only = torch.empty_like(d_b)
+    ctx.linear_backward_into(y, None, None, d_bias=only, pre=pre, activation="silu")
+    assert torch.equal(only, d_b)
+    narrow_w = matrix(gen, 131, 149, t)
+    n0 = narrow_w.clone()
+    ctx.linear_backward_into(y, x, None, d_weight=narrow_w, accumulate=True)
+    plain_w = ctx.linear_backward(y, x, w, dtype=torch.float32)[1]
+    ctx.check_status()
+    assert torch.equal(narrow_w, (plain_w + n0.float()).to(t))
+    for n, (r, c) in dict(y=(slice(1, 134), slice(8, 139)), pre=(slice(7, 140), slice(160, 291)), dx=(slice(5, 138), slice(16, 165))).items():
+        whole[n][r, c] = before[n][r, c]
+        assert torch.equal(whole[n], before[n])
+
+
+def test_linear_of_no_tokens(ctx):
+    x, w = torch.empty(0, 64, device="cuda", dtype=torch.bfloat16), torch.ones(32, 64, device="cuda", dtype=torch.bfloat16)
+    y = ctx.linear_forward(x, w)
+    d_x, d_w, d_b = ctx.linear_backward(y, x, w, y, "gelu", dtype=torch.float32)
+    kept = torch.ones(32, 64, device="cuda")
+    ctx.linear_backward_into(y, x, w, d_weight=kept, accumulate=True)
+    ctx.check_status()
+    assert y.shape == (0, 32) and d_x.shape == (0, 64) and d_w.eq(0).all() and d_b.eq(0).all() and kept.eq(1).all()
+
+
+@pytest.mark.parametrize("activation", ACTIVATIONS[1:])
+def test_activations_far_out(ctx, activation):
+    """Large arguments and infinities: an activation and its slope go to their limits."""
+    v = torch.tensor([0.0, -0.0, 1e-3, -1e-3, 9.0, -9.0, 30.0, -30.0, 88.0, -88.0, 1e3, -1e3, 1e4, -1e4], device="cuda", dtype=torch.bfloat16)
+    x = torch.zeros(16, 16, device="cuda", dtype=torch.bfloat16)
+    x[:14, 0] = v
+    one = torch.zeros(8, 16, device="cuda", dtype=torch.bfloat16)
+    one[:, 0] = 1
+    y, pre = ctx.linear_forward(x, one, activation=activation, keep=True)
+    assert torch.equal(pre[:14, 0], v)
+    want = activation_want(v.double(), activation, False)
+    # 1 + erf is off by what erf near -1 is, 2 units of 2^-24, however small it is itself: the bound is on the difference, not relative to it
+    within(y[:14, 0], want, rounded(want, torch.bfloat16) + function_err(v.double(), activation))
+    d_b = torch.empty(16, device="cuda")
+    wide = torch.zeros(8, 16, device="cuda", dtype=torch.bfloat16)
+    wide[0, :14] = v
+    unit = torch.zeros_like(wide)
+    unit[0] = 1
+    ctx.linear_backward_into(unit, None, None, d_bias=d_b, pre=wide, activation=activation)
+    ctx.check_status()
+    slope = activation_want(v.double(), activation, True)
+    slope = torch.where(slope.isnan(), (v > 0).double(), slope)              # (a product of 0 and infinity in the definition)
+    within(d_b[:14], slope, function_err(v.double(), activation) * (1 + v.double().abs()).clamp(max=10.0) + 1e-30)
+
+
+# ------------------------------------------------------------------ together
+
+def test_operators_on_streams_and_in_graphs(ps):
+    """Two contexts on two streams at once, and calls captured into a graph and replayed on other inputs."""
+    gen = torch.Generator("cuda").manual_seed(9)
+    base = ps.Context(0)
+    x, w, d_y = matrix(gen, 1000, 512, torch.bfloat16), matrix(gen, 768, 512, torch.bfloat16), matrix(gen, 1000, 768, torch.bfloat16)
+    scale = normal(gen, 512, dtype=torch.bfloat16)
+
+    def step(ctx, x, d_y):
+        n, mean, rstd = ctx.layer_norm_forward(x, scale)
+        q = ctx.rotary(n.view(1, 1000, 4, 128))
+        y, pre = ctx.linear_forward(q.view(1000, 512), w, activation="gelu", keep=True)
+        d_q, d_w, d_b = ctx.linear_backward(d_y, q.view(1000, 512), w, pre, "gelu", dtype=torch.float32)
+        d_n = ctx.rotary(d_q.view(1, 1000, 4, 128), inverse=True).view(1000, 512)
+        return (y, d_w, d_b) + ctx.layer_norm_backward(d_n, x, mean, rstd, scale, residual=x)
+    inputs = [(x, d_y), (x * 2 - 0.5, d_y * 0.5)]
+    want = [step(base, *i) for i in inputs]
+    streams = [torch.cuda.Stream() for _ in inputs]
+    contexts = [ps.Context(0, s) for s in streams]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(3):
+        for i, (s, c) in enumerate(zip(streams, contexts)):
+            with torch.cuda.stream(s):
+                got[i].append(step(c, *inputs[i]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in range(2) for run in got[i] for a, b in zip(run, want[i]))
+    hold = [t.clone() for t in inputs[0]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(streams[0]):
+        step(contexts[0], *hold)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        out = step(contexts[0], *hold)
+    for i in (1, 0, 1):
+        for to, t in zip(hold, inputs[i]):
+            to.copy_(t)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
+    for c in contexts + [base]:
+        c.check_status()
+
+
+def test_a_layer_of_a_transformer(ctx):
+    """Norm, projections, rotary positions, attention and a feed-forward layer, and all of their gradients, against
+    autograd in 64 bits.  Every tensor between two operators is rounded to bfloat16."""
+    gen = torch.Generator("cuda").manual_seed(12)
+    t, batch, length, heads, kv_heads, dim = torch.bfloat16, 2, 200, 4, 2, 64
+    hidden, rows = heads * dim, batch * length
+    x = normal(gen, rows, hidden, dtype=t)
+    p = dict(n1=1 + normal(gen, hidden, size=0.1), b1=normal(gen, hidden, size=0.1), qkv=normal(gen, (heads + 2 * kv_heads) * dim, hidden, size=hidden ** -0.5),
+             out=normal(gen, hidden, hidden, size=hidden ** -0.5), bo=normal(gen, hidden, size=0.1), n2=1 + normal(gen, hidden, size=0.1),
+             b2=normal(gen, hidden, size=0.1), up=normal(gen, 4 * hidden, hidden, size=hidden ** -0.5), bu=normal(gen, 4 * hidden, size=0.1),
+             down=normal(gen, hidden, 4 * hidden, size=(4 * hidden) ** -0.5), bd=normal(gen, hidden, size=0.1))
+    p = {k: v.to(t) for k, v in p.items()}
+    d_out = normal(gen, rows, hidden, dtype=t)
+
+    n1, mean1, rstd1 = ctx.layer_norm_forward(x, p["n1"], p["b1"])
+    qkv = ctx.linear_forward(n1, p["qkv"]).view(batch, length, heads + 2 * kv_heads, dim)
+    q, k, v = qkv[:, :, :heads], qkv[:, :, heads:heads + kv_heads], qkv[:, :, heads + kv_heads:]
+    ctx.rotary_into(q, q, k, k)
+    o, lse = ctx.attention_forward(q, k, v)
+    h = ctx.linear_forward(o.view(rows, hidden), p["out"], p["bo"], residual=x)
+    n2, mean2, rstd2 = ctx.layer_norm_forward(h, p["n2"], p["b2"])
+    a, pre = ctx.linear_forward(n2, p["up"], p["bu"], "gelu", keep=True)
+    y = ctx.linear_forward(a, p["down"], p["bd"], residual=h)
+
+    g = {}
+    d_pre, g["down"], g["bd"] = ctx.linear_backward(d_out, a, p["down"], below=pre, below_activation="gelu")
+    d_n2, g["up"], g["bu"] = ctx.linear_backward(d_pre, n2, p["up"])
+    d_h, g["n2"], g["b2"] = ctx.layer_norm_backward(d_n2, h, mean2, rstd2, p["n2"], residual=d_out)
+    d_o, g["out"], g["bo"] = ctx.linear_backward(d_h, o.view(rows, hidden), p["out"])
+    d_qkv = torch.empty_like(qkv)
+    d_q, d_k, d_v = d_qkv[:, :, :heads], d_qkv[:, :, heads:heads + kv_heads], d_qkv[:, :, heads + kv_heads:]
+    ctx.attention_backward_into(q, k, v, o, lse, d_o.view_as(o), d_q, d_k, d_v)
+    ctx.rotary_into(d_q, d_q, d_k, d_k, inverse=True)
+    d_n1, g["qkv"], _ = ctx.linear_backward(d_qkv.view(rows, -1), n1, p["qkv"])
+    g["x"], g["n1"], g["b1"] = ctx.layer_norm_backward(d_n1, x, mean1, rstd1, p["n1"], residual=d_h)
+    ctx.check_status()
+
+    e = {k: v.double().requires_grad_() for k, v in p.items()}
+    e["x"] = x.double().requires_grad_()
+
+    def layer_norm(x, w, b):
+        x = x - x.mean(1, keepdim=True)
+        return x * (x.square().mean(1, keepdim=True) + 1e-5).rsqrt() * w + b
+    at = torch.arange(length, device="cuda", dtype=torch.float64)[:, None, None] * 10000.0 ** (-torch.arange(dim // 2, device="cuda", dtype=torch.float64) / (dim // 2))
+
+    def turn(x):
+        a, b = x[..., :dim // 2], x[..., dim // 2:]
+        return torch.cat((a * at.cos() - b * at.sin(), b * at.cos() + a * at.sin()), -1)
+    z = (layer_norm(e["x"], e["n1"], e["b1"]) @ e["qkv"].t()).view(batch, length, -1, dim)
+    eq, ek, ev = (u.transpose(1, 2) for u in (turn(z[:, :, :heads]), turn(z[:, :, heads:heads + kv_heads]), z[:, :, heads + kv_heads:]))
+    ek, ev = (u.repeat_interleave(heads // kv_heads, 1) for u in (ek, ev))
+    s = (eq @ ek.transpose(-1, -2) * dim ** -0.5).masked_fill(torch.ones(length, length, device="cuda").triu(1).bool(), -math.inf)
+    eo = (torch.softmax(s, -1) @ ev).transpose(1, 2).reshape(rows, hidden)
+    eh = eo @ e["out"].t() + e["bo"] + e["x"]
+    ea = activation_slow_gelu(layer_norm(eh, e["n2"], e["b2"]) @ e["up"].t() + e["bu"])
+    ey = ea @ e["down"].t() + e["bd"] + eh
+    ey.backward(d_out.double())
+    # a tensor on the way is off by 2^-9 at most, relative and mostly evenly spread, and no path has more than 16 of them; they add up as squares
+    assert (y.double() - ey.detach()).norm() <= 4 * 2.0 ** -9 * ey.detach().norm()
+    for name, grad in g.items():
+        assert (grad.double() - e[name].grad).norm() <= 2 * 4 * 2.0 ** -9 * e[name].grad.norm(), name
+
+
+def activation_slow_gelu(v):
+    return v * 0.5 * torch.erfc(-v * math.sqrt(0.5))
