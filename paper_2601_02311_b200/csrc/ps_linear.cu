@@ -25,6 +25,9 @@ constexpr int STEP = 64;                  // of the sum, a stage of the ring
 constexpr int WRITERS = 8, COPY_WARP = 8, MMA_WARP = 9, TILE_WARP = 10, THREADS = 352;
 constexpr int TILES_AHEAD = 2;            // tiles that a block has taken on and not yet begun to write, at most
 constexpr int LOW_SHIFT = 12;             // see multiply_scaled
+// Steps that a sum which leaves in 32 bits takes in tensor memory at a time; it is then added to what is there.  (The tensor cores cut off what they add to a
+// sum, which draws it towards zero by about 2^-25 with every 16 products: 5003 tokens, 6e-6 of the gradient; rounded to 16 bits nobody sees it.)
+constexpr u32 STEPS_AT_ONCE = 64;
 constexpr u32 BUFFER = 32 * 128;          // a warp's 32 rows of 128 bytes on their way from or to memory
 constexpr u32 LEADER = 0xFEFFFFFFu;       // a shared-memory address, in the pair's first block
 
@@ -53,7 +56,7 @@ struct Form {
 
 struct Product {
   u32 m, n, steps;                        // C's sizes, and stages of the sum
-  u32 m_tiles, n_tiles, splits, steps_each, stage_bytes;
+  u32 m_tiles, n_tiles, splits, steps_each, steps_at_once, stage_bytes;
   const void* bias;
   u32 activation, below_activation;
   u32 has_residual, has_below, has_pre;
@@ -159,9 +162,9 @@ __device__ __forceinline__ void load_box(u32 to, const CUtensorMap* map, int col
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(to), "l"(map), "r"(column), "r"(row), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void load_rows(u32 to, const CUtensorMap* map, int column, int row, u32 bar) {
+__device__ __forceinline__ void load_rows(u32 to, const CUtensorMap* map, int column, int row, int part, u32 bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-               ::"r"(to), "l"(map), "r"(column), "r"(row), "r"(0), "r"(bar) : "memory");
+               ::"r"(to), "l"(map), "r"(column), "r"(row), "r"(part), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void store_rows(const CUtensorMap* map, int column, int row, int part, u32 from) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
@@ -385,30 +388,32 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       do {
         const Tile tile = tile_at(p, t);
         const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS), column = (int)(tile.n * F::COLUMNS + rank * F::B_ROWS);
-        const u32 begin = tile.part * p.steps_each, end = min(begin + p.steps_each, p.steps);
+        const u32 last = min((tile.part + 1) * p.steps_each, p.steps);
+        for (u32 begin = tile.part * p.steps_each; begin < last && !waiter.dead; begin += p.steps_at_once) {
 #pragma unroll 1
-        for (int low = F::TWO ? 1 : 0; low >= 0; --low)
-          for (u32 k = begin; k < end; ++k, ++turn) {
-            const int s = turn % STAGES;
-            wait_for<PAIR>(waiter, empty(s), (turn / STAGES + 1) & 1);
-            if (waiter.dead) break;
-            if (rank == 0) barrier_expect(full(s), (PAIR ? 2 : 1) * p.stage_bytes);
-            const u32 a = ring + s * F::STAGE, b = a + F::A_BYTES;
-            const CUtensorMap* const a_map = low ? &maps.low : &maps.a;
-            const int at = (int)(k * STEP);
-            if (F::A_ACROSS) {
+          for (int low = F::TWO ? 1 : 0; low >= 0; --low)
+            for (u32 k = begin, end = min(begin + p.steps_at_once, last); k < end; ++k, ++turn) {
+              const int s = turn % STAGES;
+              wait_for<PAIR>(waiter, empty(s), (turn / STAGES + 1) & 1);
+              if (waiter.dead) break;
+              if (rank == 0) barrier_expect(full(s), (PAIR ? 2 : 1) * p.stage_bytes);
+              const u32 a = ring + s * F::STAGE, b = a + F::A_BYTES;
+              const CUtensorMap* const a_map = low ? &maps.low : &maps.a;
+              const int at = (int)(k * STEP);
+              if (F::A_ACROSS) {
 #pragma unroll
-              for (int i = 0; i < ROWS / 64; ++i) load_box<PAIR>(a + i * ACROSS_PANEL, a_map, row + 64 * i, at, full(s));
-            } else {
-              load_box<PAIR>(a, a_map, at, row, full(s));
-            }
-            if (F::B_ACROSS) {
+                for (int i = 0; i < ROWS / 64; ++i) load_box<PAIR>(a + i * ACROSS_PANEL, a_map, row + 64 * i, at, full(s));
+              } else {
+                load_box<PAIR>(a, a_map, at, row, full(s));
+              }
+              if (F::B_ACROSS) {
 #pragma unroll
-              for (int i = 0; i < F::B_LOADED / 64; ++i) load_box<PAIR>(b + i * ACROSS_PANEL, &maps.b, column + 64 * i, at, full(s));
-            } else {
-              load_box<PAIR>(b, &maps.b, at, column, full(s));
+                for (int i = 0; i < F::B_LOADED / 64; ++i) load_box<PAIR>(b + i * ACROSS_PANEL, &maps.b, column + 64 * i, at, full(s));
+              } else {
+                load_box<PAIR>(b, &maps.b, at, column, full(s));
+              }
             }
-          }
+        }
       } while (!waiter.dead && next_tile(count++, t, true));
       if (rank == 0) {                              // leave no copy in flight, also where a wait has run out
         Waiter last(p.status);
@@ -419,29 +424,30 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   } else if (warp == MMA_WARP) {
     if (rank == 0 && elected()) {
       constexpr u32 ins = instruction_of<F>();
-      u32 turn = 0, count = 0, t = first;
+      u32 turn = 0, count = 0, sums = 0, t = first;
       do {
-        const u32 part = tile_at(p, t).part;
-        const u32 begin = part * p.steps_each, end = min(begin + p.steps_each, p.steps);
-        const u32 d = tmem + (count & 1) * F::SUM;
-        wait_for<PAIR>(waiter, sum_empty(count & 1), (count / 2 + 1) & 1);
-        fence_after();
+        const u32 part = tile_at(p, t).part, last = min((part + 1) * p.steps_each, p.steps);
+        for (u32 begin = part * p.steps_each; begin < last && !waiter.dead; begin += p.steps_at_once, ++sums) {
+          const u32 end = min(begin + p.steps_at_once, last), d = tmem + (sums & 1) * F::SUM;
+          wait_for<PAIR>(waiter, sum_empty(sums & 1), (sums / 2 + 1) & 1);
+          fence_after();
 #pragma unroll 1
-        for (int low = F::TWO ? 1 : 0; low >= 0; --low)
-          for (u32 k = begin; k < end && !waiter.dead; ++k, ++turn) {
-            const int s = turn % STAGES;
-            wait_for<PAIR>(waiter, full(s), (turn / STAGES) & 1);
-            if (waiter.dead) break;
-            fence_after();
-            const u32 a = descriptor<F::A_ACROSS>(ring + s * F::STAGE), b = descriptor<F::B_ACROSS>(ring + s * F::STAGE + F::A_BYTES);
+          for (int low = F::TWO ? 1 : 0; low >= 0; --low)
+            for (u32 k = begin; k < end && !waiter.dead; ++k, ++turn) {
+              const int s = turn % STAGES;
+              wait_for<PAIR>(waiter, full(s), (turn / STAGES) & 1);
+              if (waiter.dead) break;
+              fence_after();
+              const u32 a = descriptor<F::A_ACROSS>(ring + s * F::STAGE), b = descriptor<F::B_ACROSS>(ring + s * F::STAGE + F::A_BYTES);
 #pragma unroll
-            for (int i = 0; i < STEP / 16; ++i) {
-              if (F::TWO && i == 0 && low == 0 && k == begin) multiply_scaled<PAIR>(d, a, b, ins);
-              else multiply<PAIR>(d, a + step_of<F::A_ACROSS>(i), b + step_of<F::B_ACROSS>(i), ins, k > begin || i > 0);
+              for (int i = 0; i < STEP / 16; ++i) {
+                if (F::TWO && i == 0 && low == 0 && k == begin) multiply_scaled<PAIR>(d, a, b, ins);
+                else multiply<PAIR>(d, a + step_of<F::A_ACROSS>(i), b + step_of<F::B_ACROSS>(i), ins, k > begin || i > 0);
+              }
+              commit_to<PAIR>(empty(s));
             }
-            commit_to<PAIR>(empty(s));
-          }
-        if (!waiter.dead) commit_to<PAIR>(sum_full(count & 1));
+          if (!waiter.dead) commit_to<PAIR>(sum_full(sums & 1));
+        }
       } while (!waiter.dead && next_tile(count++, t, true));
     }
     __syncwarp();
@@ -458,105 +464,115 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       }
     }
     __syncwarp();
-    __syncwarp();
   } else {
     const u32 mine = buffers + warp * 2 * BUFFER, other = mine + BUFFER;       // result and residual; pre or below
     const u32 bias_at = biases + warp * 128;
     const int quarter = warp % 4, half = warp / 4;
-    u32 count = 0, inputs = 0, t = first;
+    u32 count = 0, sums = 0, inputs = 0, t = first;
     bool more = true;
     do {
       const Tile tile = tile_at(p, t);
+      const u32 last = min((tile.part + 1) * p.steps_each, p.steps);
       const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS + quarter * 32);
-      bool waited = false;
+      for (u32 begin = tile.part * p.steps_each; begin < last; begin += p.steps_at_once, ++sums) {
+        // what is added to: the residual, or what this very warp has written of the sum so far
+        const bool further = sizeof(O) == 4 && begin > tile.part * p.steps_each;
+        const bool adds = p.has_residual || further;
+        bool waited = false;
 #pragma unroll 1
-      for (int c = half; c < F::COLUMNS / CHUNK; c += 2) {
-        const int column = (int)(tile.n * F::COLUMNS + c * CHUNK);
-        if (row >= (int)p.m || column >= (int)p.n || waiter.dead) continue;
-        const bool reads = p.has_residual || (F::KIND == INPUT_GRAD && p.has_below);
-        if (lane == 0) {
-          wait_stores_read();                       // the buffers' last results have left
-          if (reads) {
-            barrier_expect(input(warp), ((p.has_residual ? 1 : 0) + (F::KIND == INPUT_GRAD && p.has_below ? 1 : 0)) * BUFFER);
-            if (p.has_residual) load_rows(mine, &maps.residual, column, row, input(warp));
-            if (F::KIND == INPUT_GRAD && p.has_below) load_rows(other, &maps.more, column, row, input(warp));
+        for (int c = half; c < F::COLUMNS / CHUNK; c += 2) {
+          const int column = (int)(tile.n * F::COLUMNS + c * CHUNK);
+          if (row >= (int)p.m || column >= (int)p.n || waiter.dead) continue;
+          const bool reads = adds || (F::KIND == INPUT_GRAD && p.has_below);
+          if (lane == 0) {
+            if (further) {
+              wait_stores_done();
+              asm volatile("fence.proxy.async;" ::: "memory");
+            }
+            wait_stores_read();                       // the buffers' last results have left
+            if (reads) {
+              barrier_expect(input(warp), ((adds ? 1 : 0) + (F::KIND == INPUT_GRAD && p.has_below ? 1 : 0)) * BUFFER);
+              if (adds) load_rows(mine, further ? &maps.out : &maps.residual, column, row, further ? (int)tile.part : 0, input(warp));
+              if (F::KIND == INPUT_GRAD && p.has_below) load_rows(other, &maps.more, column, row, 0, input(warp));
+            }
           }
-        }
-        if (F::KIND == OUTPUT && p.bias) {
+          if (F::KIND == OUTPUT && p.bias) {
 #pragma unroll
-          for (int i = lane; i < CHUNK; i += 32) {
-            const unsigned short v = column + i < (int)p.n ? ((const unsigned short*)p.bias)[column + i] : (unsigned short)0;
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(bias_at + 2 * i), "h"(v) : "memory");
+            for (int i = lane; i < CHUNK; i += 32) {
+              const unsigned short v = column + i < (int)p.n ? ((const unsigned short*)p.bias)[column + i] : (unsigned short)0;
+              asm volatile("st.shared.u16 [%0], %1;" ::"r"(bias_at + 2 * i), "h"(v) : "memory");
+            }
           }
-        }
-        __syncwarp();
-        if (!waited) {
-          wait_for<PAIR>(waiter, sum_full(count & 1), (count / 2) & 1);
-          fence_after();
-          waited = true;
-        }
-        if (reads) wait_for<false>(waiter, input(warp), inputs++ & 1);
-        waiter.dead = __any_sync(0xffffffffu, waiter.dead);      // (the lanes go on together)
-        if (waiter.dead) continue;
-#pragma unroll
-        for (int h = 0; h < CHUNK; h += 32) {
-          u32 sum[32];
-          tmem_load32(sum, tmem + ((u32)(quarter * 32) << 16) + (count & 1) * F::SUM + c * CHUNK + h);
-          wait_loads();
-          float v[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]);
-          if (F::KIND == OUTPUT) {
-            if (p.bias)
-#pragma unroll
-              for (int e = 0; e < 32; e += 8) {
-                const uint4 w = read16(bias_at + 2 * (h + e));
-                Pack<T, 8> b;
-                b.w[0] = w.x, b.w[1] = w.y, b.w[2] = w.z, b.w[3] = w.w;
-                float f[8];
-                b.widen(f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[e + i] += f[i];
-              }
-            if (p.has_pre) write32<T>(other, lane, h, v);
-            activate(p.activation, v);
-          }
-          float f[32];
-          if (F::KIND == INPUT_GRAD && p.has_below) {
-            read32<T>(other, lane, h, f);
-            times_slope(p.below_activation, v, f);
-          }
-          if (p.has_residual) {
-            read32<O>(mine, lane, h, f);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] += f[e];
-          }
-          write32<O>(mine, lane, h, v);
-        }
-        if (p.out.data && column + CHUNK > (int)p.n) {
-          store_edge<O>(p.out, row, column, p.m, p.n, mine);
-          if (F::KIND == OUTPUT && p.has_pre) store_edge<T>(p.pre, row, column, p.m, p.n, other);
           __syncwarp();
-          continue;
+          if (!waited) {
+            wait_for<PAIR>(waiter, sum_full(sums & 1), (sums / 2) & 1);
+            fence_after();
+            waited = true;
+          }
+          if (reads) wait_for<false>(waiter, input(warp), inputs++ & 1);
+          waiter.dead = __any_sync(0xffffffffu, waiter.dead);      // (the lanes go on together)
+          if (waiter.dead) continue;
+#pragma unroll
+          for (int h = 0; h < CHUNK; h += 32) {
+            u32 sum[32];
+            tmem_load32(sum, tmem + ((u32)(quarter * 32) << 16) + (sums & 1) * F::SUM + c * CHUNK + h);
+            wait_loads();
+            float v[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]);
+            if (F::KIND == OUTPUT) {
+              if (p.bias)
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                  const uint4 w = read16(bias_at + 2 * (h + e));
+                  Pack<T, 8> b;
+                  b.w[0] = w.x, b.w[1] = w.y, b.w[2] = w.z, b.w[3] = w.w;
+                  float f[8];
+                  b.widen(f);
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) v[e + i] += f[i];
+                }
+              if (p.has_pre) write32<T>(other, lane, h, v);
+              activate(p.activation, v);
+            }
+            float f[32];
+            if (F::KIND == INPUT_GRAD && p.has_below) {
+              read32<T>(other, lane, h, f);
+              times_slope(p.below_activation, v, f);
+            }
+            if (adds) {
+              read32<O>(mine, lane, h, f);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[e] += f[e];
+            }
+            write32<O>(mine, lane, h, v);
+          }
+          if (p.out.data && column + CHUNK > (int)p.n) {
+            store_edge<O>(p.out, row, column, p.m, p.n, mine);
+            if (F::KIND == OUTPUT && p.has_pre) store_edge<T>(p.pre, row, column, p.m, p.n, other);
+            if (sizeof(O) == 4) asm volatile("fence.proxy.async;" ::: "memory");        // (a copy may read it again)
+            __syncwarp();
+            continue;
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            store_rows(&maps.out, column, row, (int)tile.part, mine);
+            if (F::KIND == OUTPUT && p.has_pre) store_rows(&maps.more, column, row, 0, other);
+            commit_stores();
+          }
         }
-        fence_async();
+        if (!waited) {                                // (nothing of this tile is this warp's: it says so in turn all the same)
+          wait_for<PAIR>(waiter, sum_full(sums & 1), (sums / 2) & 1);
+          fence_after();
+        }
+        waiter.dead = __any_sync(0xffffffffu, waiter.dead);
+        fence_before();
         __syncwarp();
         if (lane == 0) {
-          store_rows(&maps.out, column, row, (int)tile.part, mine);
-          if (F::KIND == OUTPUT && p.has_pre) store_rows(&maps.more, column, row, 0, other);
-          commit_stores();
+          if (PAIR) arrive_at_leader(sum_empty(sums & 1));
+          else barrier_arrive(sum_empty(sums & 1));
         }
-      }
-      if (!waited) {                                // (nothing of this tile is this warp's: it says so in turn all the same)
-        wait_for<PAIR>(waiter, sum_full(count & 1), (count / 2) & 1);
-        fence_after();
-      }
-      waiter.dead = __any_sync(0xffffffffu, waiter.dead);
-      fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (PAIR) arrive_at_leader(sum_empty(count & 1));
-        else barrier_arrive(sum_empty(count & 1));
       }
       more = !waiter.dead && next_tile(count, t, false);
       more = __all_sync(0xffffffffu, more);
@@ -579,6 +595,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
 // ---- dW out of the parts of a sum that was cut: parts[splits][m][pitch], added in order
 template <class O>
 __global__ void __launch_bounds__(256) k_join_parts(const float* parts, u32 splits, u64 m, u32 n, u32 pitch, O* out, u64 stride, u32 accumulate) {
+  let_next_begin();
+  wait_for_earlier();
   const u32 c = blockIdx.x * 256 + threadIdx.x;
   if (c >= n) return;
   for (u64 r = blockIdx.y; r < m; r += gridDim.y) {
@@ -590,11 +608,12 @@ __global__ void __launch_bounds__(256) k_join_parts(const float* parts, u32 spli
   }
 }
 
-// ---- dPre = dY o act'(pre), rounded, and where `low` is given what the rounding took, 2^LOW_SHIFT times as large; and its sums by columns: a warp has 256 columns, 8 a lane, a block eight rows at a time
-constexpr int SLOPE_COLUMNS = 256, SLOPE_WARPS = 8;
+// ---- dPre = dY o act'(pre), rounded, and where `low` is given what the rounding took, 2^LOW_SHIFT times as large; and its sums by columns: a warp has 256 columns, 8 a lane, a block 16 rows at a time.
+// A chunk of the rows leaves its sums in parts, the only one in `out`.
+constexpr int SLOPE_COLUMNS = 256, SLOPE_WARPS = 16;
 template <class T>
-__global__ void __launch_bounds__(SLOPE_WARPS * 32) k_slope(const ps_matrix d_y, const ps_matrix pre, const ps_matrix d_pre, const ps_matrix low, u64 rows, u32 cols,
-                                                           u64 rows_each, u32 activation, float* parts) {
+__global__ void __launch_bounds__(SLOPE_WARPS * 32, 2) k_slope(const ps_matrix d_y, const ps_matrix pre, const ps_matrix d_pre, const ps_matrix low, u64 rows, u32 cols,
+                                                           u64 rows_each, u32 activation, float* parts, void* out, u32 out_wide, u32 accumulate) {
   __shared__ float sums[SLOPE_WARPS][SLOPE_COLUMNS];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const u32 column = blockIdx.x * SLOPE_COLUMNS + lane * 8;
@@ -605,15 +624,19 @@ __global__ void __launch_bounds__(SLOPE_WARPS * 32) k_slope(const ps_matrix d_y,
     p.clear();
     if (here == 8) p.load(from);
     else
-      for (int e = 0; e < here; ++e) p.w[e / 2] |= (u32)*reinterpret_cast<const unsigned short*>(from + e) << (16 * (e % 2));
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < here) p.w[e / 2] |= (u32)*reinterpret_cast<const unsigned short*>(from + e) << (16 * (e % 2));
   };
   const auto store = [&](T* to, const Pack<T, 8>& p) {
     if (here == 8) p.store(to);
     else
-      for (int e = 0; e < here; ++e) reinterpret_cast<unsigned short*>(to)[e] = (unsigned short)(p.w[e / 2] >> (16 * (e % 2)));
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < here) reinterpret_cast<unsigned short*>(to)[e] = (unsigned short)(p.w[e / 2] >> (16 * (e % 2)));
   };
   if (here > 0)
-#pragma unroll 2
+#pragma unroll 4
     for (u64 r = begin + warp; r < end; r += SLOPE_WARPS) {
       Pack<T, 8> g, at;
       load((const T*)d_y.data + r * d_y.stride + column, g);
@@ -640,16 +663,25 @@ __global__ void __launch_bounds__(SLOPE_WARPS * 32) k_slope(const ps_matrix d_y,
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += v[e];
     }
-  if (parts == nullptr) return;
+  if (parts == nullptr && out == nullptr) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) sums[warp][lane * 8 + e] = sum[e];
   __syncthreads();
   const u32 c = blockIdx.x * SLOPE_COLUMNS + threadIdx.x;
-  if (c >= cols) return;
-  float all = 0.f;
+  if (threadIdx.x >= SLOPE_COLUMNS || c >= cols) return;
+  float all[4] = {};
 #pragma unroll
-  for (int w = 0; w < SLOPE_WARPS; ++w) all += sums[w][threadIdx.x];
-  parts[(u64)blockIdx.y * cols + c] = all;
+  for (int w = 0; w < SLOPE_WARPS; ++w) all[w % 4] += sums[w][threadIdx.x];
+  const float total = (all[0] + all[1]) + (all[2] + all[3]);
+  if (parts) {
+    parts[(u64)blockIdx.y * cols + c] = total;
+  } else if (out_wide) {
+    float* const to = (float*)out + c;
+    *to = accumulate ? *to + total : total;
+  } else {
+    T* const to = (T*)out + c;
+    *to = narrow<T>(accumulate ? widen(*to) + total : total);
+  }
 }
 
 // ------------------------------------------------------------------ host
@@ -703,6 +735,7 @@ cudaError_t product(u32 dtype, const Call& c, volatile u32* status, int sm_count
   p.n_tiles = (u32)((c.n + F::COLUMNS - 1) / F::COLUMNS);
   p.steps_each = (p.steps + c.parts - 1) / c.parts;
   p.splits = (p.steps + p.steps_each - 1) / p.steps_each;
+  p.steps_at_once = sizeof(O) == 4 ? STEPS_AT_ONCE : p.steps_each;
   p.bias = c.bias;
   p.activation = c.activation, p.below_activation = c.below_activation;
   p.has_residual = c.residual.data != nullptr;
@@ -790,10 +823,10 @@ u32 weight_parts(const LinearArgs& a) {
   return (u32)((steps + each - 1) / each);
 }
 u64 up(u64 n, u64 to) { return (n + to - 1) / to * to; }
-// chunks of rows for the sums by columns
+// chunks of rows for the sums by columns: one where there are few (a launch less), else four blocks an SM, a row of a warp at a time or more
 u64 slope_chunks(const LinearArgs& a) {
   const u64 across = (a.outputs + SLOPE_COLUMNS - 1) / SLOPE_COLUMNS;
-  return std::max<u64>(1, std::min<u64>((a.tokens + 31) / 32, (6 * SMS + across - 1) / across));
+  return a.tokens <= 512 ? 1 : std::max<u64>(1, std::min<u64>((a.tokens + 63) / 64, (4 * SMS + across - 1) / across));
 }
 struct Work {
   size_t low, sums, parts, all;           // (d_pre stands first)
@@ -814,53 +847,52 @@ cudaError_t forward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
   return product_of<T, T, OUTPUT>(a.dtype, c, a.status, sm_count, stream);
 }
 
+// (The two products one after the other: started early by a programmatic launch, the second took the SMs from the first before its tiles were done, and
+// 5003 tokens, 1416 to 2503 columns, took 279 us instead of 166.)
 template <class T>
 cudaError_t backward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
   const Work w = work_of(a);
   char* const work = (char*)a.work;
+  const u64 chunks = slope_chunks(a);
+  float* const sums = a.d_bias && chunks > 1 ? (float*)(work + w.sums) : nullptr;
   ps_matrix d_pre = a.d_y, low = NOTHING;
-  const bool products = a.d_x.data || a.d_weight.data;
-  if (a.activation || a.d_bias) {
-    float* const sums = a.d_bias ? (float*)(work + w.sums) : nullptr;
-    if (a.activation) d_pre = {work, up(a.outputs, 8)};
-    if (a.activation && a.grad_dtype == PS_F32 && a.d_weight.data) low = {work + w.low, up(a.outputs, 8)};
-    const u64 chunks = slope_chunks(a), each = (a.tokens + chunks - 1) / chunks;
-    k_slope<T><<<dim3((u32)((a.outputs + SLOPE_COLUMNS - 1) / SLOPE_COLUMNS), (u32)chunks), SLOPE_WARPS * 32, 0, stream>>>(
-        a.d_y, a.pre, d_pre, low, a.tokens, (u32)a.outputs, each, a.activation, sums);
-    cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess && sums) e = join_columns(a.grad_dtype, sums, (u32)chunks, 1, a.outputs, a.d_bias, nullptr, a.accumulate, stream);
-    if (e != cudaSuccess || !products) return e;
-  }
-  if (a.d_x.data && a.tokens) {
+  if (a.activation) d_pre = {work, up(a.outputs, 8)};
+  if (a.activation && a.grad_dtype == PS_F32 && a.d_weight.data) low = {work + w.low, up(a.outputs, 8)};
+  cudaError_t e = cudaSuccess;
+  const auto slopes = [&] {
+    const dim3 grid((u32)((a.outputs + SLOPE_COLUMNS - 1) / SLOPE_COLUMNS), (u32)chunks);
+    const u64 each = (a.tokens + chunks - 1) / chunks;
+    const u32 wide = a.grad_dtype == PS_F32;
+    void* const out = chunks > 1 ? nullptr : a.d_bias;
+    k_slope<T><<<grid, SLOPE_WARPS * 32, 0, stream>>>(a.d_y, a.pre, d_pre, low, a.tokens, (u32)a.outputs, each, a.activation, sums, out, wide, a.accumulate);
+    return cudaGetLastError();
+  };
+  if (a.activation) e = slopes();
+  if (e == cudaSuccess && a.d_x.data && a.tokens) {
     const Call c = {INPUT_GRAD, d_pre, a.weight, a.d_x, a.residual, a.below, a.tokens, a.inputs, a.outputs, 1, nullptr, 0, a.below_activation, NOTHING};
-    const cudaError_t e = product_of<T, T, INPUT_GRAD>(a.dtype, c, a.status, sm_count, stream);
-    if (e != cudaSuccess) return e;
+    e = product_of<T, T, INPUT_GRAD>(a.dtype, c, a.status, sm_count, stream);
   }
-  if (a.d_weight.data && a.tokens == 0) {
-    if (a.accumulate) return cudaSuccess;
-    const size_t width = a.grad_dtype == PS_F32 ? 4 : 2;
-    return cudaMemset2DAsync(a.d_weight.data, a.d_weight.stride * width, 0, a.inputs * width, a.outputs, stream);
-  }
-  if (a.d_weight.data) {
-    const u32 parts = weight_parts(a);
+  const u32 parts = weight_parts(a), pitch = (u32)up(a.inputs, 4);
+  const bool wide = a.grad_dtype == PS_F32 || parts > 1;
+  if (e == cudaSuccess && a.d_weight.data && a.tokens) {
     Call c = {WEIGHT_GRAD, d_pre, a.x, a.d_weight, a.accumulate ? a.d_weight : NOTHING, NOTHING, a.outputs, a.inputs, a.tokens, parts, nullptr, 0, 0, low};
-    if (parts == 1 && low.data) return product_of<T, float, WEIGHT_GRAD_TWO>(a.dtype, c, a.status, sm_count, stream);
-    if (parts == 1)
-      return a.grad_dtype == PS_F32 ? product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream)
-                                    : product_of<T, T, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
-    const u32 pitch = (u32)up(a.inputs, 4);
-    c.out = {work + w.parts, pitch};
-    c.residual = NOTHING;
-    cudaError_t e = low.data ? product_of<T, float, WEIGHT_GRAD_TWO>(a.dtype, c, a.status, sm_count, stream)
-                             : product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
-    if (e != cudaSuccess) return e;
+    if (parts > 1) c.out = {work + w.parts, pitch}, c.residual = NOTHING;
+    e = !wide ? product_of<T, T, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream)
+        : low.data ? product_of<T, float, WEIGHT_GRAD_TWO>(a.dtype, c, a.status, sm_count, stream)
+                   : product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
+  } else if (e == cudaSuccess && a.d_weight.data && !a.accumulate) {
+    const size_t width = a.grad_dtype == PS_F32 ? 4 : 2;
+    e = cudaMemset2DAsync(a.d_weight.data, a.d_weight.stride * width, 0, a.inputs * width, a.outputs, stream);
+  }
+  if (e == cudaSuccess && a.d_weight.data && a.tokens && parts > 1) {
     const dim3 grid((u32)((a.inputs + 255) / 256), (u32)std::min<u64>(a.outputs, 65535));
     const float* const from = (const float*)(work + w.parts);
-    if (a.grad_dtype == PS_F32) k_join_parts<float><<<grid, 256, 0, stream>>>(from, parts, a.outputs, (u32)a.inputs, pitch, (float*)a.d_weight.data, a.d_weight.stride, a.accumulate);
-    else k_join_parts<T><<<grid, 256, 0, stream>>>(from, parts, a.outputs, (u32)a.inputs, pitch, (T*)a.d_weight.data, a.d_weight.stride, a.accumulate);
-    return cudaGetLastError();
+    if (a.grad_dtype == PS_F32) e = launch_next(k_join_parts<float>, grid, 256, 0, stream, from, parts, a.outputs, (u32)a.inputs, pitch, (float*)a.d_weight.data, a.d_weight.stride, a.accumulate);
+    else e = launch_next(k_join_parts<T>, grid, 256, 0, stream, from, parts, a.outputs, (u32)a.inputs, pitch, (T*)a.d_weight.data, a.d_weight.stride, a.accumulate);
   }
-  return cudaSuccess;
+  if (e == cudaSuccess && !a.activation && a.d_bias) e = slopes();
+  if (e == cudaSuccess && sums) e = join_columns(a.grad_dtype, sums, (u32)chunks, 1, a.outputs, a.d_bias, nullptr, a.accumulate, stream);
+  return e;
 }
 
 }  // namespace

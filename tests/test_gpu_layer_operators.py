@@ -696,3 +696,17 @@ def test_a_layer_of_a_transformer(ctx):
 
 def activation_slow_gelu(v):
     return v * 0.5 * torch.erfc(-v * math.sqrt(0.5))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_long_sums_keep_32_bits(ctx, dtype):
+    """A gradient in 32 bits over many tokens: what the tensor cores cut off does not add up.  All terms are positive, so that a
+    sum's every step is a large one."""
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(4)
+    x, d_y = matrix(gen, 40000, 72, t).abs_(), matrix(gen, 40000, 136, t).abs_()
+    want = d_y.double().t() @ x.double()
+    for outputs in (136, 8):
+        _, d_w, _ = ctx.linear_backward(d_y[:, :outputs], x, torch.zeros(outputs, 72, device="cuda", dtype=t), dtype=torch.float32)
+        ctx.check_status()
+        # 256 additions of 16 products a time, cut off (2 F each, relative to a sum that grows evenly: half of that), and ten of such sums
+        within(d_w, want[:outputs], (256 + 16 + 2 * 20) * F * want[:outputs])
