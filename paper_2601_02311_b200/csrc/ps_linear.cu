@@ -14,6 +14,7 @@
 // depend on what else the call computes.  The sum over the tokens is cut where dW has few tiles; a second kernel adds the parts in order.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 #include "ps_columns.cuh"
 #include "ps_tensor.cuh"
 
@@ -56,7 +57,7 @@ struct Form {
 
 struct Product {
   u32 m, n, steps;                        // C's sizes, and stages of the sum
-  u32 m_tiles, n_tiles, splits, steps_each, steps_at_once, stage_bytes;
+  u32 m_tiles, n_tiles, tiles, splits, steps_each, steps_at_once, stage_bytes;
   const void* bias;
   u32 activation, below_activation;
   u32 has_residual, has_below, has_pre;
@@ -330,12 +331,23 @@ struct Maps {
   CUtensorMap a, b, out, residual, more, low;   // more: pre, written, or below, read; low: a's second part
 };
 
-template <class F>
-__global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Maps maps, const Product p) {
+// One product, or two that do not need one another: the tiles of the second follow those of the first, whose are the longer ones, so that no SM
+// waits for the end of a product while there is another.  (5003 tokens, 1416 to 2503 columns: ONE_BY_ONE us for the two kernels, TOGETHER for one.)
+struct None {};
+template <class F, class G>
+__global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__ Maps maps_f, const __grid_constant__ Maps maps_g, const Product of_f,
+                                                        const Product of_g) {
   typedef typename F::T T;
-  typedef typename F::O O;
-  constexpr bool PAIR = F::PAIR;
-  constexpr int STAGES = F::STAGES, CHUNK = F::CHUNK;
+  constexpr bool PAIR = F::PAIR, BOTH = !std::is_same<G, None>::value;
+  constexpr int STAGES = F::STAGES;
+  // `f` for the product that a tile belongs to
+  const auto at_tile = [&](u32 t, const auto& f) {
+    if constexpr (BOTH) {
+      static_assert(F::STAGE == G::STAGE && F::COLUMNS == G::COLUMNS && F::PAIR == G::PAIR, "one ring, one shape");
+      if (t >= of_f.tiles) return f(G{}, maps_g, of_g, t - of_f.tiles);
+    }
+    return f(F{}, maps_f, of_f, t);
+  };
   extern __shared__ unsigned char raw[];
   const u32 base = (smem_address(raw) + 1023u) & ~1023u;
   const u32 ring = base, buffers = ring + STAGES * F::STAGE, biases = buffers + F::BUFFERS, bars = biases + WRITERS * 128;
@@ -367,7 +379,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   const u32 tmem = tmem_at;
 
   const u32 first = PAIR ? blockIdx.x / 2 : blockIdx.x;
-  Waiter waiter(p.status);
+  Waiter waiter(of_f.status);
   // a role's n-th answer: the tile to go on with, or none.  `speaks`: the thread that says that it has been read
   const auto next_tile = [&](u32 n, u32& t, bool speaks) {
     wait_for<PAIR>(waiter, tile_full(n), (n / TILES_AHEAD) & 1);
@@ -385,13 +397,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     if (elected()) {
       u32 turn = 0;                                 // stages filled so far
       u32 count = 0, t = first;
-      do {
+      const auto copy = [&](auto form, const Maps& maps, const Product& p, u32 t) {
+        typedef decltype(form) X;
         const Tile tile = tile_at(p, t);
         const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS), column = (int)(tile.n * F::COLUMNS + rank * F::B_ROWS);
         const u32 last = min((tile.part + 1) * p.steps_each, p.steps);
         for (u32 begin = tile.part * p.steps_each; begin < last && !waiter.dead; begin += p.steps_at_once) {
 #pragma unroll 1
-          for (int low = F::TWO ? 1 : 0; low >= 0; --low)
+          for (int low = X::TWO ? 1 : 0; low >= 0; --low)
             for (u32 k = begin, end = min(begin + p.steps_at_once, last); k < end; ++k, ++turn) {
               const int s = turn % STAGES;
               wait_for<PAIR>(waiter, empty(s), (turn / STAGES + 1) & 1);
@@ -400,55 +413,60 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
               const u32 a = ring + s * F::STAGE, b = a + F::A_BYTES;
               const CUtensorMap* const a_map = low ? &maps.low : &maps.a;
               const int at = (int)(k * STEP);
-              if (F::A_ACROSS) {
+              if (X::A_ACROSS) {
 #pragma unroll
                 for (int i = 0; i < ROWS / 64; ++i) load_box<PAIR>(a + i * ACROSS_PANEL, a_map, row + 64 * i, at, full(s));
               } else {
                 load_box<PAIR>(a, a_map, at, row, full(s));
               }
-              if (F::B_ACROSS) {
+              if (X::B_ACROSS) {
 #pragma unroll
-                for (int i = 0; i < F::B_LOADED / 64; ++i) load_box<PAIR>(b + i * ACROSS_PANEL, &maps.b, column + 64 * i, at, full(s));
+                for (int i = 0; i < X::B_LOADED / 64; ++i) load_box<PAIR>(b + i * ACROSS_PANEL, &maps.b, column + 64 * i, at, full(s));
               } else {
                 load_box<PAIR>(b, &maps.b, at, column, full(s));
               }
             }
         }
-      } while (!waiter.dead && next_tile(count++, t, true));
+      };
+      do at_tile(t, copy);
+      while (!waiter.dead && next_tile(count++, t, true));
       if (rank == 0) {                              // leave no copy in flight, also where a wait has run out
-        Waiter last(p.status);
+        Waiter last(of_f.status);
         for (u32 i = turn > STAGES ? turn - STAGES : 0; i < turn; ++i) wait_for<PAIR>(last, full(i % STAGES), (i / STAGES) & 1);
       }
     }
     __syncwarp();
   } else if (warp == MMA_WARP) {
     if (rank == 0 && elected()) {
-      constexpr u32 ins = instruction_of<F>();
       u32 turn = 0, count = 0, sums = 0, t = first;
-      do {
+      const auto sum_up = [&](auto form, const Maps&, const Product& p, u32 t) {
+        typedef decltype(form) X;
+        constexpr u32 ins = instruction_of<X>();
         const u32 part = tile_at(p, t).part, last = min((part + 1) * p.steps_each, p.steps);
         for (u32 begin = part * p.steps_each; begin < last && !waiter.dead; begin += p.steps_at_once, ++sums) {
           const u32 end = min(begin + p.steps_at_once, last), d = tmem + (sums & 1) * F::SUM;
           wait_for<PAIR>(waiter, sum_empty(sums & 1), (sums / 2 + 1) & 1);
           fence_after();
 #pragma unroll 1
-          for (int low = F::TWO ? 1 : 0; low >= 0; --low)
+          for (int low = X::TWO ? 1 : 0; low >= 0; --low)
             for (u32 k = begin; k < end && !waiter.dead; ++k, ++turn) {
               const int s = turn % STAGES;
               wait_for<PAIR>(waiter, full(s), (turn / STAGES) & 1);
               if (waiter.dead) break;
               fence_after();
-              const u32 a = descriptor<F::A_ACROSS>(ring + s * F::STAGE), b = descriptor<F::B_ACROSS>(ring + s * F::STAGE + F::A_BYTES);
+              const u32 a = descriptor<X::A_ACROSS>(ring + s * F::STAGE), b = descriptor<X::B_ACROSS>(ring + s * F::STAGE + F::A_BYTES);
 #pragma unroll
               for (int i = 0; i < STEP / 16; ++i) {
-                if (F::TWO && i == 0 && low == 0 && k == begin) multiply_scaled<PAIR>(d, a, b, ins);
-                else multiply<PAIR>(d, a + step_of<F::A_ACROSS>(i), b + step_of<F::B_ACROSS>(i), ins, k > begin || i > 0);
+                if (X::TWO && i == 0 && low == 0 && k == begin) multiply_scaled<PAIR>(d, a, b, ins);
+                else multiply<PAIR>(d, a + step_of<X::A_ACROSS>(i), b + step_of<X::B_ACROSS>(i), ins, k > begin || i > 0);
               }
               commit_to<PAIR>(empty(s));
             }
           if (!waiter.dead) commit_to<PAIR>(sum_full(sums & 1));
         }
-      } while (!waiter.dead && next_tile(count++, t, true));
+      };
+      do at_tile(t, sum_up);
+      while (!waiter.dead && next_tile(count++, t, true));
     }
     __syncwarp();
   } else if (warp == TILE_WARP) {
@@ -470,7 +488,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     const int quarter = warp % 4, half = warp / 4;
     u32 count = 0, sums = 0, inputs = 0, t = first;
     bool more = true;
-    do {
+    const auto write = [&](auto form, const Maps& maps, const Product& p, u32 t) {
+      typedef decltype(form) X;
+      typedef typename X::O O;
+      constexpr int CHUNK = X::CHUNK;
       const Tile tile = tile_at(p, t);
       const u32 last = min((tile.part + 1) * p.steps_each, p.steps);
       const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS + quarter * 32);
@@ -483,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         for (int c = half; c < F::COLUMNS / CHUNK; c += 2) {
           const int column = (int)(tile.n * F::COLUMNS + c * CHUNK);
           if (row >= (int)p.m || column >= (int)p.n || waiter.dead) continue;
-          const bool reads = adds || (F::KIND == INPUT_GRAD && p.has_below);
+          const bool reads = adds || (X::KIND == INPUT_GRAD && p.has_below);
           if (lane == 0) {
             if (further) {
               wait_stores_done();
@@ -491,12 +512,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             }
             wait_stores_read();                       // the buffers' last results have left
             if (reads) {
-              barrier_expect(input(warp), ((adds ? 1 : 0) + (F::KIND == INPUT_GRAD && p.has_below ? 1 : 0)) * BUFFER);
+              barrier_expect(input(warp), ((adds ? 1 : 0) + (X::KIND == INPUT_GRAD && p.has_below ? 1 : 0)) * BUFFER);
               if (adds) load_rows(mine, further ? &maps.out : &maps.residual, column, row, further ? (int)tile.part : 0, input(warp));
-              if (F::KIND == INPUT_GRAD && p.has_below) load_rows(other, &maps.more, column, row, 0, input(warp));
+              if (X::KIND == INPUT_GRAD && p.has_below) load_rows(other, &maps.more, column, row, 0, input(warp));
             }
           }
-          if (F::KIND == OUTPUT && p.bias) {
+          if (X::KIND == OUTPUT && p.bias) {
 #pragma unroll
             for (int i = lane; i < CHUNK; i += 32) {
               const unsigned short v = column + i < (int)p.n ? ((const unsigned short*)p.bias)[column + i] : (unsigned short)0;
@@ -520,7 +541,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             float v[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(sum[e]);
-            if (F::KIND == OUTPUT) {
+            if (X::KIND == OUTPUT) {
               if (p.bias)
 #pragma unroll
                 for (int e = 0; e < 32; e += 8) {
@@ -536,7 +557,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
               activate(p.activation, v);
             }
             float f[32];
-            if (F::KIND == INPUT_GRAD && p.has_below) {
+            if (X::KIND == INPUT_GRAD && p.has_below) {
               read32<T>(other, lane, h, f);
               times_slope(p.below_activation, v, f);
             }
@@ -549,7 +570,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           }
           if (p.out.data && column + CHUNK > (int)p.n) {
             store_edge<O>(p.out, row, column, p.m, p.n, mine);
-            if (F::KIND == OUTPUT && p.has_pre) store_edge<T>(p.pre, row, column, p.m, p.n, other);
+            if (X::KIND == OUTPUT && p.has_pre) store_edge<T>(p.pre, row, column, p.m, p.n, other);
             if (sizeof(O) == 4) asm volatile("fence.proxy.async;" ::: "memory");        // (a copy may read it again)
             __syncwarp();
             continue;
@@ -558,7 +579,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           __syncwarp();
           if (lane == 0) {
             store_rows(&maps.out, column, row, (int)tile.part, mine);
-            if (F::KIND == OUTPUT && p.has_pre) store_rows(&maps.more, column, row, 0, other);
+            if (X::KIND == OUTPUT && p.has_pre) store_rows(&maps.more, column, row, 0, other);
             commit_stores();
           }
         }
@@ -574,6 +595,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           else barrier_arrive(sum_empty(sums & 1));
         }
       }
+    };
+    do {
+      at_tile(t, write);
       more = !waiter.dead && next_tile(count, t, false);
       more = __all_sync(0xffffffffu, more);
       if (lane == 0) {                              // (all lanes have read it)
@@ -608,67 +632,76 @@ __global__ void __launch_bounds__(256) k_join_parts(const float* parts, u32 spli
   }
 }
 
-// ---- dPre = dY o act'(pre), rounded, and where `low` is given what the rounding took, 2^LOW_SHIFT times as large; and its sums by columns: a warp has 256 columns, 8 a lane, a block 16 rows at a time.
-// A chunk of the rows leaves its sums in parts, the only one in `out`.
-constexpr int SLOPE_COLUMNS = 256, SLOPE_WARPS = 16;
-template <class T>
+// ---- dPre = dY o act'(pre), rounded, and where `low` is given what the rounding took, 2^LOW_SHIFT times as large; and its sums by columns.  A lane has N
+// columns, 8 or, where there are few rows and so few blocks, 2; a block 16 rows at a time.  A chunk of the rows leaves its sums in parts, the only one
+// in `out`.  (Bytes bound it.  ACT is PS_ACT_NONE for the sums alone.)
+constexpr int SLOPE_WARPS = 16;
+template <class T, int N, int ACT>
 __global__ void __launch_bounds__(SLOPE_WARPS * 32, 2) k_slope(const ps_matrix d_y, const ps_matrix pre, const ps_matrix d_pre, const ps_matrix low, u64 rows, u32 cols,
-                                                           u64 rows_each, u32 activation, float* parts, void* out, u32 out_wide, u32 accumulate) {
-  __shared__ float sums[SLOPE_WARPS][SLOPE_COLUMNS];
+                                                           u64 rows_each, float* parts, void* out, u32 out_wide, u32 accumulate) {
+  constexpr int COLUMNS = 32 * N, AT_ONCE = N == 8 ? 4 : 8;
+  __shared__ float sums[SLOPE_WARPS][COLUMNS];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const u32 column = blockIdx.x * SLOPE_COLUMNS + lane * 8;
-  const int here = column >= cols ? 0 : (int)min(8u, cols - column);
+  const u32 column = blockIdx.x * COLUMNS + lane * N;
+  const int here = column >= cols ? 0 : (int)min((u32)N, cols - column);
   const u64 begin = blockIdx.y * rows_each, end = begin + rows_each < rows ? begin + rows_each : rows;
-  float sum[8] = {};
-  const auto load = [&](const T* from, Pack<T, 8>& p) {
+  float sum[N] = {};
+  const auto load = [&](const T* from, Pack<T, N>& p) {
     p.clear();
-    if (here == 8) p.load(from);
+    if (here == N) p.load(from);
     else
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < N; ++e)
         if (e < here) p.w[e / 2] |= (u32)*reinterpret_cast<const unsigned short*>(from + e) << (16 * (e % 2));
   };
-  const auto store = [&](T* to, const Pack<T, 8>& p) {
-    if (here == 8) p.store(to);
+  const auto store = [&](T* to, const Pack<T, N>& p) {
+    if (here == N) p.store(to);
     else
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < N; ++e)
         if (e < here) reinterpret_cast<unsigned short*>(to)[e] = (unsigned short)(p.w[e / 2] >> (16 * (e % 2)));
   };
   if (here > 0)
-#pragma unroll 4
-    for (u64 r = begin + warp; r < end; r += SLOPE_WARPS) {
-      Pack<T, 8> g, at;
-      load((const T*)d_y.data + r * d_y.stride + column, g);
-      float v[8];
-      if (activation) {
-        load((const T*)pre.data + r * pre.stride + column, at);
-        float x[8];
-        g.widen(v);
-        at.widen(x);
-        times_slope(activation, v, x);
-        g.narrow(v);
-        store((T*)d_pre.data + r * d_pre.stride + column, g);
-        if (low.data) {
-          float f[8];
-          g.widen(f);
+    for (u64 first = begin + warp; first < end; first += AT_ONCE * SLOPE_WARPS) {
+      Pack<T, N> g[AT_ONCE], at[AT_ONCE];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = (v[e] - f[e]) * (float)(1 << LOW_SHIFT);
-          g.narrow(f);
-          store((T*)low.data + r * low.stride + column, g);
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const u64 r = first + u * SLOPE_WARPS;
+        g[u].clear();
+        if (r < end) {
+          load((const T*)d_y.data + r * d_y.stride + column, g[u]);
+          if (ACT) load((const T*)pre.data + r * pre.stride + column, at[u]);
         }
-      } else {
-        g.widen(v);
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[e];
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const u64 r = first + u * SLOPE_WARPS;
+        float v[N], x[N];
+        g[u].widen(v);
+        if (ACT && r < end) {
+          at[u].widen(x);
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[e] *= slope<ACT>(x[e]);
+          g[u].narrow(v);
+          store((T*)d_pre.data + r * d_pre.stride + column, g[u]);
+          if (low.data) {
+            g[u].widen(x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e] = (v[e] - x[e]) * (float)(1 << LOW_SHIFT);
+            g[u].narrow(x);
+            store((T*)low.data + r * low.stride + column, g[u]);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += v[e];
+      }
     }
   if (parts == nullptr && out == nullptr) return;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sums[warp][lane * 8 + e] = sum[e];
+  for (int e = 0; e < N; ++e) sums[warp][lane * N + e] = sum[e];
   __syncthreads();
-  const u32 c = blockIdx.x * SLOPE_COLUMNS + threadIdx.x;
-  if (threadIdx.x >= SLOPE_COLUMNS || c >= cols) return;
+  const u32 c = blockIdx.x * COLUMNS + threadIdx.x;
+  if (threadIdx.x >= COLUMNS || c >= cols) return;
   float all[4] = {};
 #pragma unroll
   for (int w = 0; w < SLOPE_WARPS; ++w) all[w % 4] += sums[w][threadIdx.x];
@@ -724,12 +757,13 @@ struct Call {
   ps_matrix low;                          // a's second part (WEIGHT_GRAD_TWO)
 };
 
+// what a kernel is told of a product; one without a result has no tiles
 template <class F>
-cudaError_t product(u32 dtype, const Call& c, volatile u32* status, int sm_count, cudaStream_t stream) {
+bool describe(u32 dtype, const Call& c, volatile u32* status, Maps& maps, Product& p) {
   typedef typename F::T T;
   typedef typename F::O O;
-  Maps maps = {};
-  Product p = {};
+  p.status = status;
+  if (!c.out.data) return true;
   p.m = (u32)c.m, p.n = (u32)c.n, p.steps = (u32)((c.k + STEP - 1) / STEP);
   p.m_tiles = (u32)((c.m + (F::PAIR ? 255 : 127)) / (F::PAIR ? 256 : 128));
   p.n_tiles = (u32)((c.n + F::COLUMNS - 1) / F::COLUMNS);
@@ -741,7 +775,6 @@ cudaError_t product(u32 dtype, const Call& c, volatile u32* status, int sm_count
   p.has_residual = c.residual.data != nullptr;
   p.has_below = F::KIND == INPUT_GRAD && c.more.data;
   p.has_pre = F::KIND == OUTPUT && c.more.data;
-  p.status = status;
   if (c.n % (16 / sizeof(O)) && c.parts == 1) {            // (the parts' rows are whole 16 bytes)
     p.out = c.out;
     if (p.has_pre) p.pre = c.more;
@@ -757,29 +790,39 @@ cudaError_t product(u32 dtype, const Call& c, volatile u32* status, int sm_count
   if (F::TWO) ok = ok && encode<T>(maps.low, dtype, c.low, c.k, c.m, STEP, 0);
   if (p.has_residual) ok = ok && encode<O>(maps.residual, dtype, c.residual, c.m, c.n, 32, 1);
   if (c.more.data) ok = ok && encode<T>(maps.more, dtype, c.more, c.m, c.n, 32, 1);
-  if (!ok) return cudaErrorInvalidValue;
+  const u64 tiles = (u64)p.m_tiles * p.n_tiles * p.splits;
+  p.tiles = (u32)tiles;
+  return ok && tiles < (1u << 29);
+}
+
+template <class F, class G>
+cudaError_t launch_products(u32 dtype, const Call& f, const Call* g, volatile u32* status, cudaStream_t stream) {
+  Maps maps[2] = {};
+  Product p[2] = {};
+  if (!describe<F>(dtype, f, status, maps[0], p[0])) return cudaErrorInvalidValue;
+  if constexpr (!std::is_same<G, None>::value)
+    if (!describe<G>(dtype, *g, status, maps[1], p[1])) return cudaErrorInvalidValue;
   static std::atomic<u64> prepared{0};                      // devices on which the kernel's shared memory has been asked for
   int device;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
   if (device >= 64 || !(prepared.load() >> device & 1)) {
-    e = cudaFuncSetAttribute(k_product<F>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::SMEM);
+    e = cudaFuncSetAttribute(k_products<F, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::SMEM);
     if (e != cudaSuccess) return e;
     if (device < 64) prepared |= (u64)1 << device;
   }
-  const u64 tiles = (u64)p.m_tiles * p.n_tiles * p.splits;
-  if (tiles > 0x3fffffffu) return cudaErrorInvalidValue;
+  const u32 tiles = p[0].tiles + p[1].tiles;
   cudaLaunchAttribute pair;
   pair.id = cudaLaunchAttributeClusterDimension;
   pair.val.clusterDim.x = 2, pair.val.clusterDim.y = pair.val.clusterDim.z = 1;
   cudaLaunchConfig_t config = {};
-  config.gridDim = dim3(F::PAIR ? 2 * (u32)tiles : (u32)tiles);
+  config.gridDim = dim3(F::PAIR ? 2 * tiles : tiles);
   config.blockDim = dim3(THREADS);
   config.dynamicSmemBytes = F::SMEM;
   config.stream = stream;
   config.attrs = &pair;
   config.numAttrs = F::PAIR ? 1 : 0;
-  return cudaLaunchKernelEx(&config, k_product<F>, maps, p);
+  return cudaLaunchKernelEx(&config, k_products<F, G>, maps[0], maps[1], p[0], p[1]);
 }
 
 // The tile's shape: the one with which the blocks are done first by what was measured of it, in cycles: for 64 steps of the sum, for writing a tile (of
@@ -791,25 +834,48 @@ struct TileCost {
 };
 constexpr TileCost TILE_COSTS[] = {{256, 256, true, 600, 3800, 13000}, {256, 192, true, 510, 3400, 12000}, {256, 128, true, 395, 1900, 11000},
                                    {128, 128, false, 450, 1500, 10500}, {128, 64, false, 320, 1400, 9500}};
-template <class T, class O, Kind KIND>
-cudaError_t product_of(u32 dtype, const Call& c, volatile u32* status, int sm_count, cudaStream_t stream) {
-  const u64 steps = ((c.k + STEP - 1) / STEP + c.parts - 1) / c.parts * (KIND == WEIGHT_GRAD_TWO ? 2 : 1);
-  u64 costs[5];
+// (Tiles are dealt out one by one: with two products, or none that a block gets more of than another, the blocks are done when their share is.)
+int shape_for(const Call* const (&calls)[2], int sm_count) {
+  int best = 0;
+  u64 least = ~(u64)0;
   for (int i = 0; i < 5; ++i) {
     const TileCost& t = TILE_COSTS[i];
-    const u64 tiles = ((c.m + t.rows - 1) / t.rows) * ((c.n + t.columns - 1) / t.columns) * c.parts, at_once = t.pair ? sm_count / 2 : sm_count;
-    // (half of a tile of 192 columns that lie across the sum is loaded as 128)
-    const u64 step = i == 1 && KIND != OUTPUT ? 640 : t.step;
-    costs[i] = (tiles + at_once - 1) / at_once * std::max<u64>(steps * step, t.write) + t.around;
+    const u64 at_once = t.pair ? sm_count / 2 : sm_count;
+    u64 all = 0, longest = 0, shortest = ~(u64)0, count = 0;
+    for (const Call* c : calls)
+      if (c && c->out.data) {
+        const u64 tiles = ((c->m + t.rows - 1) / t.rows) * ((c->n + t.columns - 1) / t.columns) * c->parts;
+        const u64 steps = ((c->k + STEP - 1) / STEP + c->parts - 1) / c->parts * (c->kind == WEIGHT_GRAD_TWO ? 2 : 1);
+        // (half of a tile of 192 columns that lie across the sum is loaded as 128)
+        const u64 tile = std::max<u64>(steps * (i == 1 && c->kind != OUTPUT ? 640 : t.step), t.write);
+        all += tiles * tile, count += tiles;
+        longest = std::max(longest, tile), shortest = std::min(shortest, tile);
+      }
+    // one kind of tile: whole rounds; two: the share, and half of a short one more
+    const u64 cost = (longest == shortest ? (count + at_once - 1) / at_once * longest : std::max(longest, (all + at_once - 1) / at_once + shortest / 2)) + t.around;
+    if (cost < least) least = cost, best = i;
   }
-  int best = 0;
-  for (int i = 1; i < 5; ++i)
-    if (costs[i] < costs[best]) best = i;
-  if (best == 0) return product<Form<T, O, KIND, 256, true>>(dtype, c, status, sm_count, stream);
-  if (best == 1) return product<Form<T, O, KIND, 192, true>>(dtype, c, status, sm_count, stream);
-  if (best == 2) return product<Form<T, O, KIND, 128, true>>(dtype, c, status, sm_count, stream);
-  if (best == 3) return product<Form<T, O, KIND, 128, false>>(dtype, c, status, sm_count, stream);
-  return product<Form<T, O, KIND, 64, false>>(dtype, c, status, sm_count, stream);
+  return best;
+}
+template <class T>
+cudaError_t output(u32 dtype, const Call& c, volatile u32* status, int sm_count, cudaStream_t stream) {
+  switch (shape_for({&c, nullptr}, sm_count)) {
+    case 0: return launch_products<Form<T, T, OUTPUT, 256, true>, None>(dtype, c, nullptr, status, stream);
+    case 1: return launch_products<Form<T, T, OUTPUT, 192, true>, None>(dtype, c, nullptr, status, stream);
+    case 2: return launch_products<Form<T, T, OUTPUT, 128, true>, None>(dtype, c, nullptr, status, stream);
+    case 3: return launch_products<Form<T, T, OUTPUT, 128, false>, None>(dtype, c, nullptr, status, stream);
+    default: return launch_products<Form<T, T, OUTPUT, 64, false>, None>(dtype, c, nullptr, status, stream);
+  }
+}
+template <class T, class O, Kind KIND>
+cudaError_t gradients(u32 dtype, const Call& w, const Call& x, volatile u32* status, int sm_count, cudaStream_t stream) {
+  switch (shape_for({&w, &x}, sm_count)) {
+    case 0: return launch_products<Form<T, O, KIND, 256, true>, Form<T, T, INPUT_GRAD, 256, true>>(dtype, w, &x, status, stream);
+    case 1: return launch_products<Form<T, O, KIND, 192, true>, Form<T, T, INPUT_GRAD, 192, true>>(dtype, w, &x, status, stream);
+    case 2: return launch_products<Form<T, O, KIND, 128, true>, Form<T, T, INPUT_GRAD, 128, true>>(dtype, w, &x, status, stream);
+    case 3: return launch_products<Form<T, O, KIND, 128, false>, Form<T, T, INPUT_GRAD, 128, false>>(dtype, w, &x, status, stream);
+    default: return launch_products<Form<T, O, KIND, 64, false>, Form<T, T, INPUT_GRAD, 64, false>>(dtype, w, &x, status, stream);
+  }
 }
 
 constexpr u64 SMS = 148;          // (what a sum's order depends on does not ask the device)
@@ -823,17 +889,20 @@ u32 weight_parts(const LinearArgs& a) {
   return (u32)((steps + each - 1) / each);
 }
 u64 up(u64 n, u64 to) { return (n + to - 1) / to * to; }
-// chunks of rows for the sums by columns: one where there are few (a launch less), else four blocks an SM, a row of a warp at a time or more
+// chunks of rows for the sums by columns: one where there are few (a launch less), else four blocks an SM, four rows of a warp or more
+constexpr u64 FEW_TOKENS = 512;
 u64 slope_chunks(const LinearArgs& a) {
-  const u64 across = (a.outputs + SLOPE_COLUMNS - 1) / SLOPE_COLUMNS;
-  return a.tokens <= 512 ? 1 : std::max<u64>(1, std::min<u64>((a.tokens + 63) / 64, (4 * SMS + across - 1) / across));
+  const u64 across = (a.outputs + 255) / 256;
+  return a.tokens <= FEW_TOKENS ? 1 : std::max<u64>(1, std::min<u64>((a.tokens + 63) / 64, (4 * SMS + across - 1) / across));
 }
+// dPre's rows begin at multiples of 128 bytes: the products read it so in half the time
+u64 d_pre_stride(const LinearArgs& a) { return up(a.outputs, 64); }
 struct Work {
   size_t low, sums, parts, all;           // (d_pre stands first)
 };
 Work work_of(const LinearArgs& a) {
   Work w;
-  w.low = a.activation ? up(a.tokens * up(a.outputs, 8) * 2, 256) : 0;
+  w.low = a.activation ? up(a.tokens * d_pre_stride(a) * 2, 256) : 0;
   w.sums = a.activation && a.grad_dtype == PS_F32 ? 2 * w.low : w.low;
   w.parts = w.sums + up(slope_chunks(a) * a.outputs * 4, 256);
   const u32 parts = weight_parts(a);
@@ -844,49 +913,50 @@ Work work_of(const LinearArgs& a) {
 template <class T>
 cudaError_t forward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
   Call c = {OUTPUT, a.x, a.weight, a.y, a.residual, a.pre, a.tokens, a.outputs, a.inputs, 1, a.bias, a.activation, 0, NOTHING};
-  return product_of<T, T, OUTPUT>(a.dtype, c, a.status, sm_count, stream);
+  return output<T>(a.dtype, c, a.status, sm_count, stream);
 }
 
-// (The two products one after the other: started early by a programmatic launch, the second took the SMs from the first before its tiles were done, and
-// 5003 tokens, 1416 to 2503 columns, took 279 us instead of 166.)
 template <class T>
 cudaError_t backward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
-  const Work w = work_of(a);
+  const Work where = work_of(a);
   char* const work = (char*)a.work;
   const u64 chunks = slope_chunks(a);
-  float* const sums = a.d_bias && chunks > 1 ? (float*)(work + w.sums) : nullptr;
+  float* const sums = a.d_bias && chunks > 1 ? (float*)(work + where.sums) : nullptr;
   ps_matrix d_pre = a.d_y, low = NOTHING;
-  if (a.activation) d_pre = {work, up(a.outputs, 8)};
-  if (a.activation && a.grad_dtype == PS_F32 && a.d_weight.data) low = {work + w.low, up(a.outputs, 8)};
+  if (a.activation) d_pre = {work, d_pre_stride(a)};
+  if (a.activation && a.grad_dtype == PS_F32 && a.d_weight.data) low = {work + where.low, d_pre_stride(a)};
   cudaError_t e = cudaSuccess;
   const auto slopes = [&] {
-    const dim3 grid((u32)((a.outputs + SLOPE_COLUMNS - 1) / SLOPE_COLUMNS), (u32)chunks);
     const u64 each = (a.tokens + chunks - 1) / chunks;
+    const bool few = a.tokens <= FEW_TOKENS;
+    const dim3 grid((u32)((a.outputs + (few ? 63 : 255)) / (few ? 64 : 256)), (u32)chunks);
     const u32 wide = a.grad_dtype == PS_F32;
     void* const out = chunks > 1 ? nullptr : a.d_bias;
-    k_slope<T><<<grid, SLOPE_WARPS * 32, 0, stream>>>(a.d_y, a.pre, d_pre, low, a.tokens, (u32)a.outputs, each, a.activation, sums, out, wide, a.accumulate);
+    const auto go = [&](auto kernel) { kernel<<<grid, SLOPE_WARPS * 32, 0, stream>>>(a.d_y, a.pre, d_pre, low, a.tokens, (u32)a.outputs, each, sums, out, wide, a.accumulate); };
+#define PS_EACH(ACT) \
+  if (a.activation == ACT) go(few ? k_slope<T, 2, ACT> : k_slope<T, 8, ACT>);
+    PS_EACH(PS_ACT_NONE) PS_EACH(PS_ACT_RELU) PS_EACH(PS_ACT_GELU) PS_EACH(PS_ACT_GELU_TANH) PS_EACH(PS_ACT_SILU)
+#undef PS_EACH
     return cudaGetLastError();
   };
   if (a.activation) e = slopes();
-  if (e == cudaSuccess && a.d_x.data && a.tokens) {
-    const Call c = {INPUT_GRAD, d_pre, a.weight, a.d_x, a.residual, a.below, a.tokens, a.inputs, a.outputs, 1, nullptr, 0, a.below_activation, NOTHING};
-    e = product_of<T, T, INPUT_GRAD>(a.dtype, c, a.status, sm_count, stream);
-  }
   const u32 parts = weight_parts(a), pitch = (u32)up(a.inputs, 4);
   const bool wide = a.grad_dtype == PS_F32 || parts > 1;
-  if (e == cudaSuccess && a.d_weight.data && a.tokens) {
-    Call c = {WEIGHT_GRAD, d_pre, a.x, a.d_weight, a.accumulate ? a.d_weight : NOTHING, NOTHING, a.outputs, a.inputs, a.tokens, parts, nullptr, 0, 0, low};
-    if (parts > 1) c.out = {work + w.parts, pitch}, c.residual = NOTHING;
-    e = !wide ? product_of<T, T, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream)
-        : low.data ? product_of<T, float, WEIGHT_GRAD_TWO>(a.dtype, c, a.status, sm_count, stream)
-                   : product_of<T, float, WEIGHT_GRAD>(a.dtype, c, a.status, sm_count, stream);
+  if (e == cudaSuccess && a.tokens && (a.d_x.data || a.d_weight.data)) {
+    const Call x = {INPUT_GRAD, d_pre, a.weight, a.d_x, a.residual, a.below, a.tokens, a.inputs, a.outputs, 1, nullptr, 0, a.below_activation, NOTHING};
+    Call w = {low.data ? WEIGHT_GRAD_TWO : WEIGHT_GRAD, d_pre, a.x, a.d_weight, a.accumulate ? a.d_weight : NOTHING, NOTHING, a.outputs, a.inputs, a.tokens, parts,
+              nullptr, 0, 0, low};
+    if (a.d_weight.data && parts > 1) w.out = {work + where.parts, pitch}, w.residual = NOTHING;
+    e = !wide ? gradients<T, T, WEIGHT_GRAD>(a.dtype, w, x, a.status, sm_count, stream)
+        : low.data ? gradients<T, float, WEIGHT_GRAD_TWO>(a.dtype, w, x, a.status, sm_count, stream)
+                   : gradients<T, float, WEIGHT_GRAD>(a.dtype, w, x, a.status, sm_count, stream);
   } else if (e == cudaSuccess && a.d_weight.data && !a.accumulate) {
     const size_t width = a.grad_dtype == PS_F32 ? 4 : 2;
     e = cudaMemset2DAsync(a.d_weight.data, a.d_weight.stride * width, 0, a.inputs * width, a.outputs, stream);
   }
   if (e == cudaSuccess && a.d_weight.data && a.tokens && parts > 1) {
     const dim3 grid((u32)((a.inputs + 255) / 256), (u32)std::min<u64>(a.outputs, 65535));
-    const float* const from = (const float*)(work + w.parts);
+    const float* const from = (const float*)(work + where.parts);
     if (a.grad_dtype == PS_F32) e = launch_next(k_join_parts<float>, grid, 256, 0, stream, from, parts, a.outputs, (u32)a.inputs, pitch, (float*)a.d_weight.data, a.d_weight.stride, a.accumulate);
     else e = launch_next(k_join_parts<T>, grid, 256, 0, stream, from, parts, a.outputs, (u32)a.inputs, pitch, (T*)a.d_weight.data, a.d_weight.stride, a.accumulate);
   }
