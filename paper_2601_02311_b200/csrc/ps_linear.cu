@@ -24,7 +24,10 @@ using namespace tensor;
 
 constexpr int STEP = 64;                  // of the sum, a stage of the ring
 constexpr int WRITERS = 8, COPY_WARP = 8, MMA_WARP = 9, TILE_WARP = 10, THREADS = 352;
-constexpr int TILES_AHEAD = 2;            // tiles that a block has taken on and not yet begun to write, at most
+constexpr u32 TILES_AHEAD = 2;            // answers that some roles have read and others not
+// The next tile is asked for this many steps before the copies of one end: early enough for the ring to stay full, and no earlier, since a tile that is
+// taken is lost to the blocks that have nothing to do
+constexpr u32 ASK_BEFORE = 2;
 constexpr int LOW_SHIFT = 12;             // see multiply_scaled
 // Steps that a sum which leaves in 32 bits takes in tensor memory at a time; it is then added to what is there.  (The tensor cores cut off what they add to a
 // sum, which draws it towards zero by about 2^-25 with every 16 products: 5003 tokens, 6e-6 of the gradient; rounded to 16 bits nobody sees it.)
@@ -360,6 +363,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
   const auto tile_full = [&](u32 n) { return bars + 8 * (2 * STAGES + 4 + WRITERS + n % TILES_AHEAD); };
   const auto tile_empty = [&](u32 n) { return bars + 8 * (2 * STAGES + 4 + WRITERS + TILES_AHEAD + n % TILES_AHEAD); };
   const auto answer = [&](u32 n) { return bars + 256 + 16 * (n % TILES_AHEAD); };
+  const u32 wanted = bars + 256 + 16 * TILES_AHEAD;         // a tile's copies are nearly done: the next one may be asked for
   __shared__ u32 tmem_at;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const u32 rank = PAIR ? rank_in_pair() : 0;
@@ -369,6 +373,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
     for (int s = 0; s < 2; ++s) barrier_init(sum_full(s), 1), barrier_init(sum_empty(s), WRITERS * (PAIR ? 2 : 1));
     for (int w = 0; w < WRITERS; ++w) barrier_init(input(w), 1);
     for (u32 n = 0; n < TILES_AHEAD; ++n) barrier_init(tile_full(n), 1), barrier_init(tile_empty(n), PAIR ? 2 * WRITERS + 4 : WRITERS + 3);
+    barrier_init(wanted, 1);
     fence_barrier_init();
   }
   if (warp == MMA_WARP) take_tmem<PAIR>(smem_address(&tmem_at), F::TMEM);
@@ -402,10 +407,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
         const Tile tile = tile_at(p, t);
         const int row = (int)(tile.m * (PAIR ? 256 : 128) + rank * ROWS), column = (int)(tile.n * F::COLUMNS + rank * F::B_ROWS);
         const u32 last = min((tile.part + 1) * p.steps_each, p.steps);
+        u32 left = (last - tile.part * p.steps_each) * (X::TWO ? 2 : 1);
+        const u32 ask = min(left, ASK_BEFORE);
         for (u32 begin = tile.part * p.steps_each; begin < last && !waiter.dead; begin += p.steps_at_once) {
 #pragma unroll 1
           for (int low = X::TWO ? 1 : 0; low >= 0; --low)
             for (u32 k = begin, end = min(begin + p.steps_at_once, last); k < end; ++k, ++turn) {
+              if (left-- == ask && rank == 0) barrier_arrive(wanted);
               const int s = turn % STAGES;
               wait_for<PAIR>(waiter, empty(s), (turn / STAGES + 1) & 1);
               if (waiter.dead) break;
@@ -474,6 +482,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
       u32 t;
       for (u32 n = 0; !waiter.dead; ++n) {
         wait_for<PAIR>(waiter, tile_empty(n), (n / TILES_AHEAD + 1) & 1);
+        waiter.wait(wanted, n & 1);
         if (waiter.dead) break;
         if (PAIR) expect_at(tile_full(n), 16, 0), expect_at(tile_full(n), 16, 1);
         else barrier_expect(tile_full(n), 16);
@@ -889,14 +898,16 @@ u32 weight_parts(const LinearArgs& a) {
   return (u32)((steps + each - 1) / each);
 }
 u64 up(u64 n, u64 to) { return (n + to - 1) / to * to; }
-// chunks of rows for the sums by columns: one where there are few (a launch less), else four blocks an SM, four rows of a warp or more
+// Rows of a chunk for the sums by columns: all where there are few (a launch less), else as many as give each SM two blocks, in whole batches of a block.
 constexpr u64 FEW_TOKENS = 512;
-u64 slope_chunks(const LinearArgs& a) {
-  const u64 across = (a.outputs + 255) / 256;
-  return a.tokens <= FEW_TOKENS ? 1 : std::max<u64>(1, std::min<u64>((a.tokens + 63) / 64, (4 * SMS + across - 1) / across));
+u64 slope_rows(const LinearArgs& a) {
+  if (a.tokens <= FEW_TOKENS) return std::max<u64>(a.tokens, 1);
+  const u64 across = (a.outputs + 255) / 256, chunks = std::max<u64>(1, 2 * SMS / across);
+  return up((a.tokens + chunks - 1) / chunks, 4 * SLOPE_WARPS);
 }
-// dPre's rows begin at multiples of 128 bytes: the products read it so in half the time
-u64 d_pre_stride(const LinearArgs& a) { return up(a.outputs, 64); }
+u64 slope_chunks(const LinearArgs& a) { return std::max<u64>(1, (a.tokens + slope_rows(a) - 1) / slope_rows(a)); }
+// dPre's rows begin at multiples of 32 bytes: of rows that begin at 16 alone a box takes a fifth longer
+u64 d_pre_stride(const LinearArgs& a) { return up(a.outputs, 16); }
 struct Work {
   size_t low, sums, parts, all;           // (d_pre stands first)
 };
@@ -927,7 +938,7 @@ cudaError_t backward(const LinearArgs& a, int sm_count, cudaStream_t stream) {
   if (a.activation && a.grad_dtype == PS_F32 && a.d_weight.data) low = {work + where.low, d_pre_stride(a)};
   cudaError_t e = cudaSuccess;
   const auto slopes = [&] {
-    const u64 each = (a.tokens + chunks - 1) / chunks;
+    const u64 each = slope_rows(a);
     const bool few = a.tokens <= FEW_TOKENS;
     const dim3 grid((u32)((a.outputs + (few ? 63 : 255)) / (few ? 64 : 256)), (u32)chunks);
     const u32 wide = a.grad_dtype == PS_F32;

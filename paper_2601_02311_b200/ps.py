@@ -572,20 +572,27 @@ class Context:
                                 bias: torch.Tensor | None = None, eps: float = 1e-5, mean: torch.Tensor | None = None,
                                 rstd: torch.Tensor | None = None):
         """ps_layer_norm_forward on [rows, cols]; `mean` and `rstd`, float32 [rows], are written where they are given.  y may be x."""
+        where = "ps_layer_norm_forward"
+        rows, _ = shape = self._rows(x, where, "x")
+        self._norm_forward(x, weight, bias, eps, self._matrix(y, where, "y", shape, x.dtype), self._vector(mean, where, "mean", rows, torch.float32),
+                           self._vector(rstd, where, "rstd", rows, torch.float32))
+
+    def _norm_forward(self, x, weight, bias, eps, y: bytes, mean: int | None, rstd: int | None):
         where, dtype = "ps_layer_norm_forward", x.dtype
         rows, cols = shape = self._rows(x, where, "x")
         self._finite(where, "eps", eps)
         self._enqueue(where, _lib.ps_layer_norm_forward, _LAYER_NORM_DESC(rows, cols, eps, _DTYPE[dtype], 0, 0, 0),
                       self._matrix(x, where, "x", shape, dtype), self._vector(weight, where, "weight", cols, dtype),
-                      self._vector(bias, where, "bias", cols, dtype), self._matrix(y, where, "y", shape, dtype),
-                      self._vector(mean, where, "mean", rows, torch.float32), self._vector(rstd, where, "rstd", rows, torch.float32))
+                      self._vector(bias, where, "bias", cols, dtype), y, mean, rstd)
 
     def layer_norm_forward(self, x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                            eps: float = 1e-5):
         """(y [rows, cols], mean [rows], rstd [rows])."""
+        rows, cols = self._rows(x, "ps_layer_norm_forward", "x")
         y = torch.empty_like(x, memory_format=torch.contiguous_format)
-        mean, rstd = x.new_empty((2, x.shape[0]), dtype=torch.float32).unbind()
-        self.layer_norm_forward_into(x, y, weight, bias, eps, mean, rstd)
+        mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind()
+        at = mean.data_ptr()
+        self._norm_forward(x, weight, bias, eps, _MATRIX(y.data_ptr(), cols), at, at + 4 * rows)
         return y, mean, rstd
 
     def layer_norm_backward_into(self, d_y: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, d_x: torch.Tensor,
@@ -633,8 +640,16 @@ class Context:
         [len] or [batch, len]; without them a token's position is its place in the sequence.  `first` is added to all;
         `dims` of a head's elements are turned (default: all)."""
         where, dtype = "ps_rotary", q.dtype
-        if q.dim() != 4 or dtype not in _DTYPE or (k is None) != (k_out is None) or (k is not None and k.dim() != 4):
-            self._refuse(E_RANGE, where, "q, and k with k_out, are [batch, len, heads, dim] of float32, bfloat16 or float16")
+        if (k is None) != (k_out is None) or q.dim() != 4 or (k is not None and k.dim() != 4):
+            self._refuse(E_RANGE, where, "q, and k with k_out, are [batch, len, heads, dim]")
+        self._rotary(q, self._heads(q_out, where, "q_out", q.shape, dtype), k, None if k is None else self._heads(k_out, where, "k_out", (*q.shape[:2], k.shape[2], q.shape[3]), dtype),
+                     positions, first, base, dims, interleaved, factor, original, low, high, magnitude, inverse)
+
+    def _rotary(self, q, q_out: bytes, k, k_out: bytes | None, positions=None, first=0, base=10000.0, dims=None, interleaved=False, factor=1.0,
+                original=0.0, low=1.0, high=32.0, magnitude=1.0, inverse=False):
+        where, dtype = "ps_rotary", q.dtype
+        if dtype not in _DTYPE:
+            self._refuse(E_RANGE, where, "q has to be of float32, bfloat16 or float16")
         batch, length, heads, dim = q.shape
         kv_heads = 0 if k is None else k.shape[2]
         width, apart, at = 4, 0, None
@@ -651,24 +666,30 @@ class Context:
         dims = dim if dims is None else dims
         if not 0 <= dims <= dim:
             self._refuse(E_RANGE, where, "dims")
-        shapes = q.shape, (batch, length, kv_heads, dim)
         desc = _ROTARY_DESC(batch, length, heads, kv_heads, dim, dims, _DTYPE[dtype], 1 if interleaved else 0, 1 if inverse else 0, width,
                             apart, first, base, factor, original, low, high, magnitude)
-        self._enqueue(where, _lib.ps_rotary, desc, self._heads(q, where, "q", shapes[0], dtype),
-                      self._heads(q_out, where, "q_out", shapes[0], dtype),
-                      None if k is None else self._heads(k, where, "k", shapes[1], dtype),
-                      None if k is None else self._heads(k_out, where, "k_out", shapes[1], dtype), at)
+        self._enqueue(where, _lib.ps_rotary, desc, self._heads(q, where, "q", q.shape, dtype), q_out,
+                      None if k is None else self._heads(k, where, "k", (batch, length, kv_heads, dim), dtype), k_out, at)
 
     def rotary(self, q: torch.Tensor, k: torch.Tensor | None = None, **how):
         """q, or (q, k), turned by their positions; `how` as for rotary_into.  The gradient is the same call on the result's
         gradients with inverse=True."""
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if q.dim() != 4 or (k is not None and k.dim() != 4):
+            self._refuse(E_RANGE, "ps_rotary", "q and k are [batch, len, heads, dim]")
+        q_out, q_heads = self._new_heads(q)
         if k is None:
-            self.rotary_into(q, q_out, **how)
+            self._rotary(q, q_heads, None, None, **how)
             return q_out
-        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-        self.rotary_into(q, q_out, k, k_out, **how)
+        k_out, k_heads = self._new_heads(k)
+        self._rotary(q, q_heads, k, k_heads, **how)
         return q_out, k_out
+
+    @staticmethod
+    def _new_heads(like: torch.Tensor):
+        """A contiguous tensor of that shape, and the library's description of it."""
+        _, length, heads, dim = shape = like.shape
+        t = torch.empty_like(like, memory_format=torch.contiguous_format)
+        return t, _HEADS(t.data_ptr(), length * heads * dim, heads * dim, dim)
 
     def _activation(self, where: str, name) -> int:
         if name not in ACTIVATIONS:
@@ -680,30 +701,42 @@ class Context:
         """ps_linear_forward: y [tokens, outputs] = act(x weight^T + bias) + residual, and what goes into the activation to
         `pre` where it is given.  Rows of the matrices begin at multiples of 16 bytes; residual may be y."""
         where, dtype = "ps_linear_forward", x.dtype
-        tokens, inputs = self._rows(x, where, "x")
-        outputs = self._rows(weight, where, "weight")[0]
-        code, shape = self._activation(where, activation), (tokens, outputs)
-        self._enqueue(where, _lib.ps_linear_forward, _LINEAR_DESC(tokens, inputs, outputs, _DTYPE[dtype], _DTYPE[dtype], code, 0, 0, 0),
+        shape = self._rows(x, where, "x")[0], self._rows(weight, where, "weight")[0]
+        self._linear_forward(x, weight, bias, activation, residual, self._matrix(y, where, "y", shape, dtype), self._matrix(pre, where, "pre", shape, dtype))
+
+    def _linear_forward(self, x, weight, bias, activation, residual, y: bytes, pre: bytes | None):
+        where, dtype = "ps_linear_forward", x.dtype
+        tokens, inputs = x.shape
+        outputs = weight.shape[0]
+        code, of = self._activation(where, activation), _DTYPE[dtype]
+        self._enqueue(where, _lib.ps_linear_forward, _LINEAR_DESC(tokens, inputs, outputs, of, of, code, 0, 0, 0),
                       self._matrix(x, where, "x", (tokens, inputs), dtype), self._matrix(weight, where, "weight", (outputs, inputs), dtype),
-                      self._vector(bias, where, "bias", outputs, dtype), self._matrix(residual, where, "residual", shape, dtype),
-                      self._matrix(y, where, "y", shape, dtype), self._matrix(pre, where, "pre", shape, dtype))
+                      self._vector(bias, where, "bias", outputs, dtype), self._matrix(residual, where, "residual", (tokens, outputs), dtype), y, pre)
 
     @staticmethod
-    def _new_rows(like: torch.Tensor, rows: int, cols: int, dtype: torch.dtype | None = None) -> torch.Tensor:
-        """[rows, cols] whose rows begin at multiples of 16 bytes."""
+    def _new_rows(like: torch.Tensor, rows: int, cols: int, dtype: torch.dtype | None = None):
+        """[rows, cols] whose rows begin at multiples of 16 bytes, and the library's description of it."""
         pack = 4 if (dtype or like.dtype) == torch.float32 else 8
         if cols % pack == 0:
-            return like.new_empty((rows, cols), dtype=dtype)
-        return like.new_empty((rows, (cols + pack - 1) // pack * pack), dtype=dtype)[:, :cols]
+            t = like.new_empty((rows, cols), dtype=dtype)
+            return t, _MATRIX(t.data_ptr(), cols)
+        stride = (cols + pack - 1) // pack * pack
+        t = like.new_empty((rows, stride), dtype=dtype)[:, :cols]
+        return t, _MATRIX(t.data_ptr(), stride)
 
     def linear_forward(self, x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, activation: str | None = None,
                        residual: torch.Tensor | None = None, keep: bool = False):
         """y, or with `keep` (y, pre): pre is what linear_backward takes.  (Columns of a larger tensor where outputs are no
         multiple of 8.)"""
-        y = self._new_rows(x, x.shape[0], weight.shape[0])
-        pre = self._new_rows(x, x.shape[0], weight.shape[0]) if keep else None
-        self.linear_forward_into(x, weight, y, bias, activation, residual, pre)
-        return (y, pre) if keep else y
+        where = "ps_linear_forward"
+        tokens, outputs = self._rows(x, where, "x")[0], self._rows(weight, where, "weight")[0]
+        y, y_rows = self._new_rows(x, tokens, outputs)
+        if not keep:
+            self._linear_forward(x, weight, bias, activation, residual, y_rows, None)
+            return y
+        pre, pre_rows = self._new_rows(x, tokens, outputs)
+        self._linear_forward(x, weight, bias, activation, residual, y_rows, pre_rows)
+        return y, pre
 
     def linear_backward_into(self, d_y: torch.Tensor, x: torch.Tensor | None, weight: torch.Tensor | None,
                              d_x: torch.Tensor | None = None, d_weight: torch.Tensor | None = None, d_bias: torch.Tensor | None = None,
@@ -724,26 +757,37 @@ class Context:
                 self._refuse(E_NULLPTR, where, "the gradient of weight needs x, that of x needs weight")
         sums = d_weight if d_weight is not None else d_bias
         wide = dtype if sums is None else sums.dtype
-        if wide not in (dtype, torch.float32):
+        self._linear_backward(d_y, x, weight, inputs, wide, self._matrix(d_x, where, "d_x", (tokens, inputs), dtype),
+                              self._matrix(d_weight, where, "d_weight", (outputs, inputs), wide), self._vector(d_bias, where, "d_bias", outputs, wide),
+                              pre, activation, below, below_activation, residual, accumulate, work)
+
+    def _linear_backward(self, d_y, x, weight, inputs: int, wide, d_x: bytes | None, d_weight: bytes | None, d_bias: int | None, pre, activation, below,
+                         below_activation, residual, accumulate, work):
+        where, dtype = "ps_linear_backward", d_y.dtype
+        tokens, outputs = d_y.shape
+        if wide is not dtype and wide != torch.float32:
             self._refuse(E_RANGE, where, f"d_weight and d_bias have to be {dtype} or float32")
         code, below_code = self._activation(where, activation), self._activation(where, below_activation)
-        shape, in_shape, w_shape = (tokens, outputs), (tokens, inputs), (outputs, inputs)
+        shape, in_shape = (tokens, outputs), (tokens, inputs)
         desc = _LINEAR_DESC(tokens, inputs, outputs, _DTYPE[dtype], _DTYPE[wide], code, below_code, 1 if accumulate else 0, 0)
         work = self._work(work, _lib.ps_linear_backward_bytes(desc), where)
         self._enqueue(where, _lib.ps_linear_backward, desc, self._matrix(d_y, where, "d_y", shape, dtype),
-                      self._matrix(x, where, "x", in_shape, dtype), self._matrix(weight, where, "weight", w_shape, dtype),
+                      self._matrix(x, where, "x", in_shape, dtype), self._matrix(weight, where, "weight", (outputs, inputs), dtype),
                       self._matrix(pre, where, "pre", shape, dtype), self._matrix(below, where, "below", in_shape, dtype),
-                      self._matrix(residual, where, "residual", in_shape, dtype), self._matrix(d_x, where, "d_x", in_shape, dtype),
-                      self._matrix(d_weight, where, "d_weight", w_shape, wide), self._vector(d_bias, where, "d_bias", outputs, wide),
-                      work.data_ptr(), work.numel())
+                      self._matrix(residual, where, "residual", in_shape, dtype), d_x, d_weight, d_bias, work.data_ptr(), work.numel())
 
     def linear_backward(self, d_y: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre: torch.Tensor | None = None,
                         activation: str | None = None, below: torch.Tensor | None = None, below_activation: str | None = None,
                         residual: torch.Tensor | None = None, dtype: torch.dtype | None = None):
         """(d_x, d_weight, d_bias), the last two in x's type or `dtype`."""
-        d_x, d_weight = self._new_rows(x, *x.shape), self._new_rows(weight, *weight.shape, dtype)
-        d_bias = weight.new_empty(weight.shape[:1], dtype=dtype)
-        self.linear_backward_into(d_y, x, weight, d_x, d_weight, d_bias, pre, activation, below, below_activation, residual)
+        where = "ps_linear_backward"
+        self._rows(d_y, where, "d_y")
+        tokens, inputs = self._rows(x, where, "x")
+        outputs = self._rows(weight, where, "weight")[0]
+        (d_x, x_rows), (d_weight, w_rows) = self._new_rows(x, tokens, inputs), self._new_rows(weight, outputs, inputs, dtype)
+        d_bias = weight.new_empty((outputs,), dtype=dtype)
+        self._linear_backward(d_y, x, weight, inputs, d_weight.dtype, x_rows, w_rows, d_bias.data_ptr(), pre, activation, below, below_activation, residual,
+                              False, None)
         return d_x, d_weight, d_bias
 
     @staticmethod
