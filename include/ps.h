@@ -566,7 +566,7 @@ int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps
  * numbers.  weight (null: ones) and bias (null: zeros) are of x's type, [cols]; mean and rstd are floats, [rows]
  * (the forward pass writes those that are not null).  `residual` (may be null) is the gradient that reaches x past the
  * normalised branch.  d_weight and d_bias, of type grad_dtype, are computed where they are not null, in an order that
- * depends on the sizes alone; with accumulate they are added to what is there (rounded once).  A row's results depend on
+ * depends on the sizes, and on whether there is a residual, alone; with accumulate they are added to what is there (rounded once).  A row's results depend on
  * that row alone.  y may be x; d_x may be d_y, x or residual (same pointer and stride).
  * d_work: ps_layer_norm_backward_bytes, used like ps_embed_backward's (0 without d_weight and d_bias). */
 typedef struct {

@@ -51,6 +51,73 @@ struct RowSum {
   }
 };
 
+// ---- Rows that are shared by the blocks of a cluster, each with a range of the columns: their sums go through one another's shared memory.
+__device__ __forceinline__ u32 cluster_rank() {
+  u32 r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ u32 cluster_size() {
+  u32 r;
+  asm volatile("mov.u32 %0, %cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ bool passed_in_cluster(u32 bar, u32 parity) {
+  u32 ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+constexpr u32 CLUSTER_MOST = 8;
+// As RowSum, over the R threads of each of the cluster's blocks: every warp sends its sums to all blocks, and arrives at their barriers.
+template <int R, int COUNT>
+struct ClusterSum {
+  static constexpr u32 WARPS = R / 32, SLOTS = 2 * COUNT * CLUSTER_MOST * WARPS;
+  u32 slots, bars, rank, size, uses;
+  tensor::Waiter& waiter;
+  __device__ __forceinline__ ClusterSum(const float* s, const u64* b, tensor::Waiter& w)
+      : slots(tensor::smem_address(s)), bars(tensor::smem_address(b)), rank(cluster_rank()), size(cluster_size()), uses(0), waiter(w) {}
+  __device__ __forceinline__ void over(float (&v)[COUNT]) {
+    const u32 turn = uses & 1, parity = uses / 2 & 1, lane = threadIdx.x % 32, bar = bars + 8 * turn;
+    ++uses;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = warp_sum(v[i]);
+    const auto slot = [&](u32 i, u32 n) { return slots + 4 * ((turn * COUNT + i) * CLUSTER_MOST * WARPS + n); };
+    if (lane < size) {
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i)
+        asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f32 [a], %2;\n\t}"
+                     ::"r"(slot(i, rank * WARPS + threadIdx.x / 32)), "r"(lane), "f"(v[i]) : "memory");
+      asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}"
+                   ::"r"(bar), "r"(lane) : "memory");
+    }
+    __syncwarp();
+    if (!waiter.dead && !passed_in_cluster(bar, parity)) {
+      const u64 begin = tensor::now_ns();
+      while (!passed_in_cluster(bar, parity))
+        if (tensor::now_ns() - begin > tensor::PATIENCE_NS) {
+          waiter.dead = true;
+          report(waiter.status, ST_TIMEOUT);
+          break;
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      v[i] = 0.f;
+      for (u32 n = lane; n < size * WARPS; n += 32) {
+        float f;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(slot(i, n)) : "memory");
+        v[i] += f;
+      }
+      v[i] = warp_sum(v[i]);
+    }
+  }
+};
+
 // Rows on their way: a ring of stages in shared memory, each with a row of every array that is read, brought by bulk copies that a warp of its
 // own starts.  (Started by a thread of the row's they took twice as long in all: the others wait for it at their next barrier.)
 // A copy begins and ends at multiples of 16 bytes: where a row does not, the rest of its first and last 16 bytes comes with it and is not used.
@@ -194,7 +261,7 @@ struct Vector {
   u32 w[G * sizeof(T) < 4 ? 1 : G * (int)sizeof(T) / 4];
   template <int R, bool PACKED>
   __device__ __forceinline__ void load(const T* from, int e, u32 cols, bool wide, float without) {
-    typedef Piece<T, R, 32, PACKED> P;
+    typedef Piece<T, R, 64, PACKED> P;
     if (from == nullptr) {
 #pragma unroll
       for (int i = 0; i < (int)(sizeof(w) / 4); ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(without) : Pack<T, G>::two(without, without, (const T*)nullptr);
@@ -232,8 +299,27 @@ __device__ __forceinline__ float reciprocal_root(float v) {
   return v > 0.f && v < INFINITY ? y * fmaf(-half * y, y, 1.5f) : y;
 }
 
-// Blocks of an SM at most, by the threads of a row: about 1024 threads, or 512 where they hold sums as well.
-__host__ __device__ constexpr int forward_blocks(int r) { return r == 32 ? 16 : r == 64 ? 8 : r == 128 ? 6 : r == 256 ? 3 : 2; }
+template <int R, int COUNT, bool SHARED>
+__device__ __forceinline__ auto sum_of(float* slots, u64* bars, tensor::Waiter& waiter) {
+  if constexpr (SHARED) return ClusterSum<R, COUNT>(slots, bars, waiter);
+  else return RowSum<R, COUNT>(slots);
+}
+// all threads of the cluster: its barriers are there before, and its memory until after, all sums
+__device__ __forceinline__ void begin_sums(u64* bars, u32 arrivals) {
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) tensor::barrier_init(tensor::smem_address(bars + i), arrivals);
+    tensor::fence_barrier_init();
+  }
+  __syncthreads();
+  cluster_sync();
+}
+__device__ __forceinline__ void end_sums() {
+  __syncwarp();
+  cluster_sync();
+}
+
+// Blocks of an SM at most, by the threads of a row and a thread's bytes of it: about 1024 threads, or 512 where they hold sums as well.
+__host__ __device__ constexpr int forward_blocks(int r, int bytes) { return r == 32 ? 16 : r == 64 ? 12 : r == 128 ? 6 : r == 256 ? 3 : bytes <= 64 ? 2 : 1; }
 __host__ __device__ constexpr int backward_blocks(int r) { return r == 32 ? 8 : r == 64 ? 5 : r == 128 ? 3 : r == 256 ? 2 : 1; }
 
 // Elements of a thread whose weights stay in its registers as well.  Of more they are read again for each row.
@@ -241,20 +327,31 @@ template <class T, int E> constexpr bool HELD = E * sizeof(T) <= 32;
 
 // A block has a row at a time, a thread E elements of it; a warp beside them brings the rows to come.
 // (At 16 bits a walk over the elements is issue slots as much as it is bytes: floats are taken two at a time.)
-template <class T, int R, int E, bool PACKED>
-__global__ void __launch_bounds__(R + 32, forward_blocks(R)) k_norm(const NormArgs a, const Wide wide, Ring ring, float share) {
+template <class T, int R, int E, bool PACKED, bool SHARED>
+__global__ void __launch_bounds__(R + 32, forward_blocks(R, E * sizeof(T))) k_norm(const NormArgs args, const Wide wide, Ring ring, float share, u32 each) {
   extern __shared__ unsigned char rows[];
-  __shared__ float slots[2 * R / 32];
-  __shared__ u64 bars[2 * RING_MOST];
+  __shared__ float slots[SHARED ? ClusterSum<R, 1>::SLOTS : 2 * R / 32];
+  __shared__ u64 bars[2 * RING_MOST + 2];
+  NormArgs a = args;
+  u32 blocks = 1, begin = 0;                    // that share a row, and the columns' range
+  if (SHARED) {
+    blocks = cluster_size(), begin = cluster_rank() * each;
+    a.cols = min((u64)each, args.cols - begin);
+    for (ps_matrix* m : {&a.x, &a.y, &a.d_y, &a.residual, &a.d_x}) m->data = (T*)m->data + begin;
+    if (a.weight) a.weight = (const T*)a.weight + begin;
+    if (a.bias) a.bias = (const T*)a.bias + begin;
+  }
   const u32 cols = (u32)a.cols;
-  const u64 step = gridDim.x;
+  const u64 row = blockIdx.x / blocks, step = gridDim.x / blocks;
   ring.begin(rows, bars, R / 32);
+  if (SHARED) begin_sums(bars + 2 * RING_MOST, blocks * (R / 32));
   tensor::Waiter waiter(a.status);
   if (threadIdx.x >= R) {
-    if (threadIdx.x == R) ring.bring<T>(waiter, a.x, a.x, a.x, blockIdx.x, step, a.rows, cols);
+    if (threadIdx.x == R) ring.bring<T>(waiter, a.x, a.x, a.x, row, step, a.rows, cols);
+    if (SHARED) end_sums();
     return;
   }
-  RowSum<R, 1> sum(slots);
+  auto sum = sum_of<R, 1, SHARED>(slots, bars + 2 * RING_MOST, waiter);
   typedef Piece<T, R, E, PACKED> P;
   constexpr int G = PACKED ? P::N : 2;          // elements that lie, or are read, together
   constexpr bool HOLD = HELD<T, E>;
@@ -266,8 +363,8 @@ __global__ void __launch_bounds__(R + 32, forward_blocks(R)) k_norm(const NormAr
       biases[e / G].template load<R, PACKED>((const T*)a.bias, e, cols, wide.bias, 0.f);
     }
   u32 stage = 0, parity = 0;
-  T* to = (T*)a.y.data + blockIdx.x * a.y.stride;
-  for (u64 r = blockIdx.x; r < a.rows; r += step, to += step * a.y.stride) {
+  T* to = (T*)a.y.data + row * a.y.stride;
+  for (u64 r = row; r < a.rows; r += step, to += step * a.y.stride) {
     P x;
     waiter.wait(ring.full(stage), parity);
     x.take(ring.at(stage, 0) + Ring::lead<T>(a.x, r), cols, wide.x);
@@ -313,11 +410,12 @@ __global__ void __launch_bounds__(R + 32, forward_blocks(R)) k_norm(const NormAr
       for (int i = 0; i < G; i += 2) x.put_both(e + i, fma2(add2(x.both(e + i), less), mul2(by, w.both(i)), b.both(i)));
     }
     x.store(to, cols, wide.y);
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && begin == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
     }
   }
+  if (SHARED) end_sums();
 }
 
 // any width: a block walks the row three times (the second and third time out of the L2)
@@ -351,26 +449,37 @@ __global__ void __launch_bounds__(LONG) k_norm_long(const NormArgs a) {
   }
 }
 
-// GRADS: the sums over this block's rows for dW and dB go to parts[block][2][cols]: they are what the registers are for, so with 32 elements a thread
-// the second walk over a row reads it again from shared memory.
-template <class T, int R, int E, bool PACKED, bool GRADS>
-__global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const NormArgs a, const Wide wide, Ring ring, float share) {
+// GRADS: the sums over this block's rows for dW and dB go to parts[block][2][cols]: they and what the second walk needs of
+// the first are what the registers are for; the weights are in shared memory.
+template <class T, int R, bool PACKED, bool GRADS, bool SHARED>
+__global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const NormArgs args, const Wide wide, Ring ring, float share, u32 each) {
+  constexpr int E = 16;
   extern __shared__ unsigned char rows[];
-  __shared__ float slots[2 * 2 * R / 32];
-  __shared__ u64 bars[2 * RING_MOST];
+  __shared__ float slots[SHARED ? ClusterSum<R, 2>::SLOTS : 2 * 2 * R / 32];
+  __shared__ u64 bars[2 * RING_MOST + 2];
+  NormArgs a = args;
+  u32 blocks = 1, begin = 0;                    // that share a row, and the columns' range
+  if (SHARED) {
+    blocks = cluster_size(), begin = cluster_rank() * each;
+    a.cols = min((u64)each, args.cols - begin);
+    for (ps_matrix* m : {&a.x, &a.y, &a.d_y, &a.residual, &a.d_x}) m->data = (T*)m->data + begin;
+    if (a.weight) a.weight = (const T*)a.weight + begin;
+    if (a.bias) a.bias = (const T*)a.bias + begin;
+  }
   const u32 cols = (u32)a.cols;
-  const u64 step = gridDim.x;
+  const u64 row = blockIdx.x / blocks, step = gridDim.x / blocks;
   ring.begin(rows, bars, R / 32);
+  if (SHARED) begin_sums(bars + 2 * RING_MOST, blocks * (R / 32));
   tensor::Waiter waiter(a.status);
   if (threadIdx.x >= R) {
-    if (threadIdx.x == R) ring.bring<T>(waiter, a.x, a.d_y, a.residual, blockIdx.x, step, a.rows, cols);
+    if (threadIdx.x == R) ring.bring<T>(waiter, a.x, a.d_y, a.residual, row, step, a.rows, cols);
+    if (SHARED) end_sums();
     return;
   }
-  RowSum<R, 2> sum(slots);
+  auto sum = sum_of<R, 2, SHARED>(slots, bars + 2 * RING_MOST, waiter);
   typedef Piece<T, R, E, PACKED> P;
   constexpr int G = PACKED ? P::N : 2, W = G * (int)sizeof(T) / 4;        // elements that are read together, and their words
   typedef Pack<T, G> Group;
-  constexpr bool KEEP = E <= 16;                // what the second walk needs of the first, in registers
   const u32 w_row = ring.at(ring.stages, 0);    // the weights stand behind the stages
   for (u32 c = threadIdx.x; c < cols; c += R) {
     if constexpr (sizeof(T) == 4)
@@ -383,17 +492,17 @@ __global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const 
 #pragma unroll
   for (int e = 0; e < E / 2; ++e) of_w[e] = of_b[e] = 0;
   u32 stage = 0, parity = 0;
-  T* to = (T*)a.d_x.data + blockIdx.x * a.d_x.stride;
+  T* to = (T*)a.d_x.data + row * a.d_x.stride;
   float next_mean = 0.f, next_rstd = 0.f;
-  if (blockIdx.x < a.rows) next_mean = a.mean[blockIdx.x], next_rstd = a.rstd[blockIdx.x];
-  for (u64 r = blockIdx.x; r < a.rows; r += step, to += step * a.d_x.stride) {
+  if (row < a.rows) next_mean = a.mean[row], next_rstd = a.rstd[row];
+  for (u64 r = row; r < a.rows; r += step, to += step * a.d_x.stride) {
     const u64 less = twice(-next_mean), by = twice(next_rstd);
     if (r + step < a.rows) next_mean = a.mean[r + step], next_rstd = a.rstd[r + step];
     const u32 x_row = ring.at(stage, 0) + Ring::lead<T>(a.x, r), d_row = ring.at(stage, 1) + Ring::lead<T>(a.d_y, r);
     const u32 more_row = ring.at(stage, 2) + Ring::lead<T>(a.residual, r);          // (of a residual)
     waiter.wait(ring.full(stage), parity);
     float s[2];
-    u64 of_g = 0, of_gx = 0, kept_xn[KEEP ? E / 2 : 1], kept_g[KEEP ? E / 2 : 1];
+    u64 of_g = 0, of_gx = 0, kept_xn[E / 2], kept_g[E / 2];
 #pragma unroll
     for (int e = 0; e < E; e += G) {
       u32 x[W], d[W];
@@ -410,7 +519,7 @@ __global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const 
         }
         of_g = add2(of_g, g);
         of_gx = fma2(g, xn, of_gx);             // (g is 0 behind the last column)
-        if (KEEP) kept_xn[(e + i) / 2] = xn, kept_g[(e + i) / 2] = g;
+        kept_xn[(e + i) / 2] = xn, kept_g[(e + i) / 2] = g;
       }
     }
     s[0] = together(of_g);
@@ -419,19 +528,12 @@ __global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const 
     const u64 along = twice(-s[0] * share), across = twice(-s[1] * share);
 #pragma unroll
     for (int e = 0; e < E; e += G) {
-      u32 x[W], d[W], w[W], more[W] = {};
-      if (!KEEP) {
-        P::read(x, x_row, e, cols, wide.x);
-        P::read(d, d_row, e, cols, wide.d_y);
-        P::read(w, w_row, e, cols, true);
-      }
+      u32 more[W] = {};
       if (a.residual.data) P::read(more, more_row, e, cols, wide.residual);
       Piece<T, R, G, PACKED> out;
 #pragma unroll
       for (int i = 0; i < G; i += 2) {
-        const u64 xn = KEEP ? kept_xn[KEEP ? (e + i) / 2 : 0] : mul2(add2(Group::both(x, i, (const T*)nullptr), less), by);
-        const u64 g = KEEP ? kept_g[KEEP ? (e + i) / 2 : 0] : mul2(Group::both(d, i, (const T*)nullptr), Group::both(w, i, (const T*)nullptr));
-        const u64 v = add2(g, fma2(xn, across, along));
+        const u64 v = add2(kept_g[(e + i) / 2], fma2(kept_xn[(e + i) / 2], across, along));
         out.put_both(i, a.residual.data ? fma2(by, v, Group::both(more, i, (const T*)nullptr)) : mul2(by, v));
       }
       out.store_at(to, e, cols, wide.d_x);
@@ -439,14 +541,15 @@ __global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const 
     ring.leave(stage, parity);
   }
   if (GRADS) {
-    float* const into = a.parts + (u64)blockIdx.x * 2 * cols;
+    float* const into = a.parts + row * 2 * args.cols + begin;
 #pragma unroll
     for (int e = 0; e < E; ++e)
       if (P::column(e) < cols) {
         into[P::column(e)] = e % 2 ? split(of_w[e / 2]).y : split(of_w[e / 2]).x;
-        into[cols + P::column(e)] = e % 2 ? split(of_b[e / 2]).y : split(of_b[e / 2]).x;
+        into[args.cols + P::column(e)] = e % 2 ? split(of_b[e / 2]).y : split(of_b[e / 2]).x;
       }
   }
+  if (SHARED) end_sums();
 }
 
 // any width: dX by a block a row, in two walks
@@ -516,7 +619,7 @@ Layout layout_of(int most, u32 wanted, u64 cols, u32 width, u32 arrays, u32 more
   l.smem = l.ring.stages * stage + more * l.ring.slot + 128;
   return l;
 }
-Layout forward_layout(int threads, u64 cols, u32 width) { return layout_of(forward_blocks(threads), 4, cols, width, 1, 0); }
+Layout forward_layout(int threads, int bytes, u64 cols, u32 width) { return layout_of(forward_blocks(threads, bytes), 2, cols, width, 1, 0); }
 Layout backward_layout(int threads, u64 cols, u32 width, u32 arrays) { return layout_of(backward_blocks(threads), 4, cols, width, arrays, 1); }
 // (asked for once a kernel and device)
 template <auto KERNEL>
@@ -533,26 +636,62 @@ struct Prepared {
   }
 };
 
-// Threads of a row, by the width: as few as hold it in 16 elements each, of wide rows 32.
-template <class T, int R, int E, bool PACKED>
-cudaError_t forward(const NormArgs& a, const Wide& wide, int sm_count, cudaStream_t stream) {
-  constexpr auto kernel = k_norm<T, R, E, PACKED>;
-  const Layout l = forward_layout(R, a.cols, sizeof(T));
+// How a row is shared: by one block, or where it has more than 8192 columns (32 KB of floats) by a cluster of 2, 4 or 8, with `each` columns (whole
+// packs) in a block.  Clusters of 4 or 8 do not fill all SMs of a GPC: `clusters` of them run at a time.
+struct Sharing {
+  u32 blocks, each, clusters;
+};
+constexpr u32 A_BLOCKS_COLUMNS = 8192;
+constexpr int SMS = 148;
+Sharing sharing_of(u64 cols, u32 a_block) {
+  if (cols <= a_block) return {1, (u32)cols, SMS};
+  for (u32 blocks : {2, 4, 8})
+    if (cols <= (u64)blocks * a_block) return {blocks, (u32)(((cols + blocks - 1) / blocks + 7) / 8 * 8), blocks == 2 ? 74u : blocks == 4 ? 32u : 16u};
+  return {0, 0, 0};
+}
+template <class... Parameters, class... Arguments>
+cudaError_t launch_cluster(void (*kernel)(Parameters...), u32 grid, u32 cluster, u32 threads, u32 smem, cudaStream_t stream, const Arguments&... arguments) {
+  cudaLaunchAttribute together;
+  together.id = cudaLaunchAttributeClusterDimension;
+  together.val.clusterDim.x = cluster, together.val.clusterDim.y = together.val.clusterDim.z = 1;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3(grid);
+  config.blockDim = dim3(threads);
+  config.dynamicSmemBytes = smem;
+  config.stream = stream;
+  config.attrs = &together;
+  config.numAttrs = cluster > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&config, kernel, Parameters(arguments)...);
+}
+
+// Threads of a row, by the width: as few as hold it in 16 elements each, of rows of up to 64 KB in more of 512 threads.  (16384 columns of bfloat16:
+// 8000 rows, 143 us by one block, 223 by two.)
+template <class T, int R, bool PACKED, bool SHARED = false, int E = 16>
+cudaError_t forward(const NormArgs& a, const Wide& wide, const Sharing& sharing, int sm_count, cudaStream_t stream) {
+  constexpr auto kernel = k_norm<T, R, E, PACKED, SHARED>;
+  const Layout l = forward_layout(R, E * sizeof(T), sharing.each, sizeof(T));
   const cudaError_t e = Prepared<kernel>::smem(l.smem);
   if (e != cudaSuccess) return e;
-  kernel<<<blocks_for(a.rows, l.resident, sm_count), R + 32, l.smem, stream>>>(a, wide, l.ring, 1.f / (float)a.cols);
-  return cudaGetLastError();
+  const u64 groups = std::min<u64>(a.rows, (u64)(SHARED ? (int)sharing.clusters : sm_count) * l.resident);
+  return launch_cluster(kernel, (u32)groups * sharing.blocks, sharing.blocks, R + 32, l.smem, stream, a, wide, l.ring, 1.f / (float)a.cols, sharing.each);
 }
 template <class T, bool PACKED>
 cudaError_t forward(const NormArgs& a, const Wide& wide, int sm_count, cudaStream_t stream) {
-  if (a.cols <= 32 * 16) return forward<T, 32, 16, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 64 * 16) return forward<T, 64, 16, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 128 * 16) return forward<T, 128, 16, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 256 * 16) return forward<T, 256, 16, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 512 * 16) return forward<T, 512, 16, PACKED>(a, wide, sm_count, stream);
-  if (a.cols <= 512 * 32) return forward<T, 512, 32, PACKED>(a, wide, sm_count, stream);
-  k_norm_long<T><<<blocks_for(a.rows, 2, sm_count), LONG, 0, stream>>>(a);
-  return cudaGetLastError();
+  constexpr u32 MOST = 65536 / sizeof(T);
+  const Sharing s = a.cols <= MOST ? Sharing{1, (u32)a.cols, SMS} : sharing_of(a.cols, A_BLOCKS_COLUMNS);
+  if (s.blocks == 0) {
+    k_norm_long<T><<<blocks_for(a.rows, 2, sm_count), LONG, 0, stream>>>(a);
+    return cudaGetLastError();
+  }
+  if (s.blocks > 1) return forward<T, 512, PACKED, true>(a, wide, s, sm_count, stream);
+  if (a.cols <= 32 * 16) return forward<T, 32, PACKED>(a, wide, s, sm_count, stream);
+  if (a.cols <= 64 * 16) return forward<T, 64, PACKED>(a, wide, s, sm_count, stream);
+  if (a.cols <= 128 * 16) return forward<T, 128, PACKED>(a, wide, s, sm_count, stream);
+  if (a.cols <= 256 * 16) return forward<T, 256, PACKED>(a, wide, s, sm_count, stream);
+  if (a.cols <= 512 * 16) return forward<T, 512, PACKED>(a, wide, s, sm_count, stream);
+  if (a.cols <= 512 * 32) return forward<T, 512, PACKED, false, 32>(a, wide, s, sm_count, stream);
+  if constexpr (sizeof(T) == 2) return forward<T, 512, PACKED, false, 64>(a, wide, s, sm_count, stream);
+  return cudaErrorInvalidValue;          // (not reached: a row of floats is shared from there on)
 }
 Wide wide_of(const NormArgs& a, size_t width) {
   const auto at = [&](const ps_matrix& m) { return aligned_rows(m.data, m.stride, width, 16); };
@@ -564,50 +703,50 @@ cudaError_t forward(const NormArgs& a, int sm_count, cudaStream_t stream) {
   return a.cols % (16 / sizeof(T)) == 0 ? forward<T, true>(a, wide, sm_count, stream) : forward<T, false>(a, wide, sm_count, stream);
 }
 
-// The backward pass's shape: threads of a row, 16 or 32 elements each (0: the long kernels), and blocks, which are the parts of the sums; a block has four
-// rows at least.  (A number of blocks for 148 SMs, whatever the device has: the sums' order depends on the
-// sizes, and on whether there is a residual, alone.)
-constexpr int SMS = 148;
+// The backward pass's shape: threads of a row or a cluster's block, 16 elements each (0: the long kernels), and rows at a time, which are the parts of the
+// sums; a block has four rows at least.  (A number for 148 SMs, whatever the device has: the sums' order depends on the sizes, and on whether there is a
+// residual, alone.)
 struct Shape {
-  int threads, elements;
-  u32 blocks;
+  int threads;
+  u32 groups;
+  Sharing sharing;
 };
 Shape backward_shape(u32 width, u64 rows, u64 cols, u32 arrays) {
-  Shape s = {0, 16, 0};
-  if (cols <= 16384 && (2 * arrays + 1) * slot_of(cols, width) <= ROOM - 2048) {        // (two stages, and the weights)
-    s.threads = 32;
-    while (s.threads < 512 && cols > (u64)s.threads * 16) s.threads *= 2;
-    if (cols > 512 * 16) s.elements = 32;
+  // two stages and the weights have to fit: of floats with more than 4096 columns not always
+  const bool fits = cols <= A_BLOCKS_COLUMNS && (2 * arrays + 1) * slot_of(cols, width) <= ROOM - 2048;
+  Shape s = {0, 0, sharing_of(cols, width == 2 || fits ? A_BLOCKS_COLUMNS : A_BLOCKS_COLUMNS / 2)};
+  if (s.sharing.blocks == 0) {
+    s.groups = (u32)std::max<u64>(1, std::min<u64>((rows + 63) / 64, 64));          // (chunks of rows)
+    return s;
   }
-  if (s.threads == 0) s.blocks = (u32)std::max<u64>(1, std::min<u64>((rows + 63) / 64, 64));          // (chunks of rows)
-  else s.blocks = (u32)std::max<u64>(1, std::min<u64>((rows + 3) / 4, SMS * backward_layout(s.threads, cols, width, arrays).resident));
+  s.threads = s.sharing.blocks > 1 ? (width == 2 ? 512 : 256) : 32;
+  while (s.threads < 512 && s.sharing.each > (u64)s.threads * 16) s.threads *= 2;
+  s.groups = (u32)std::max<u64>(1, std::min<u64>((rows + 3) / 4, s.sharing.clusters * backward_layout(s.threads, s.sharing.each, width, arrays).resident));
   return s;
 }
-template <class T, int R, int E, bool PACKED, bool GRADS>
+template <class T, int R, bool PACKED, bool GRADS, bool SHARED>
 cudaError_t backward(const NormArgs& a, const Wide& wide, const Shape& s, cudaStream_t stream) {
-  constexpr auto kernel = k_norm_grad<T, R, E, PACKED, GRADS>;
-  const Layout l = backward_layout(R, a.cols, sizeof(T), a.residual.data ? 3 : 2);
+  constexpr auto kernel = k_norm_grad<T, R, PACKED, GRADS, SHARED>;
+  const Layout l = backward_layout(R, s.sharing.each, sizeof(T), a.residual.data ? 3 : 2);
   const cudaError_t e = Prepared<kernel>::smem(l.smem);
   if (e != cudaSuccess) return e;
-  kernel<<<s.blocks, R + 32, l.smem, stream>>>(a, wide, l.ring, 1.f / (float)a.cols);
-  return cudaGetLastError();
+  return launch_cluster(kernel, s.groups * s.sharing.blocks, s.sharing.blocks, R + 32, l.smem, stream, a, wide, l.ring, 1.f / (float)a.cols, s.sharing.each);
 }
-template <class T, int R, int E, bool PACKED>
+template <class T, int R, bool PACKED, bool SHARED = false>
 cudaError_t backward(const NormArgs& a, const Wide& wide, const Shape& s, cudaStream_t stream) {
-  return a.parts ? backward<T, R, E, PACKED, true>(a, wide, s, stream) : backward<T, R, E, PACKED, false>(a, wide, s, stream);
+  return a.parts ? backward<T, R, PACKED, true, SHARED>(a, wide, s, stream) : backward<T, R, PACKED, false, SHARED>(a, wide, s, stream);
 }
 template <class T, bool PACKED>
 cudaError_t backward(const NormArgs& a, const Shape& s, int sm_count, cudaStream_t stream) {
   const Wide wide = wide_of(a, sizeof(T));
-  if (s.threads == 32) return backward<T, 32, 16, PACKED>(a, wide, s, stream);
-  if (s.threads == 64) return backward<T, 64, 16, PACKED>(a, wide, s, stream);
-  if (s.threads == 128) return backward<T, 128, 16, PACKED>(a, wide, s, stream);
-  if (s.threads == 256) return backward<T, 256, 16, PACKED>(a, wide, s, stream);
-  if (s.threads == 512 && s.elements == 16) return backward<T, 512, 16, PACKED>(a, wide, s, stream);
-  if constexpr (sizeof(T) == 2)
-    if (s.threads == 512) return backward<T, 512, 32, PACKED>(a, wide, s, stream);
+  if (s.sharing.blocks > 1) return backward<T, sizeof(T) == 2 ? 512 : 256, PACKED, true>(a, wide, s, stream);
+  if (s.threads == 32) return backward<T, 32, PACKED>(a, wide, s, stream);
+  if (s.threads == 64) return backward<T, 64, PACKED>(a, wide, s, stream);
+  if (s.threads == 128) return backward<T, 128, PACKED>(a, wide, s, stream);
+  if (s.threads == 256) return backward<T, 256, PACKED>(a, wide, s, stream);
+  if (s.threads == 512) return backward<T, 512, PACKED>(a, wide, s, stream);
   if (a.parts) {                 // before d_x, which may stand in the place of d_y or x
-    k_norm_columns<T><<<dim3((u32)((a.cols + 255) / 256), s.blocks), 256, 0, stream>>>(a, (a.rows + s.blocks - 1) / s.blocks);
+    k_norm_columns<T><<<dim3((u32)((a.cols + 255) / 256), s.groups), 256, 0, stream>>>(a, (a.rows + s.groups - 1) / s.groups);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
@@ -621,7 +760,7 @@ cudaError_t backward(const NormArgs& a, int sm_count, cudaStream_t stream) {
   if (a.rows == 0 && !a.parts) return cudaSuccess;
   const cudaError_t e = a.cols % (16 / sizeof(T)) == 0 ? backward<T, true>(a, s, sm_count, stream) : backward<T, false>(a, s, sm_count, stream);
   if (e != cudaSuccess || !a.parts) return e;
-  return join_columns(a.grad_dtype, a.parts, s.blocks, 2, a.cols, a.d_weight, a.d_bias, a.accumulate, stream);
+  return join_columns(a.grad_dtype, a.parts, s.groups, 2, a.cols, a.d_weight, a.d_bias, a.accumulate, stream);
 }
 
 }  // namespace
@@ -632,8 +771,8 @@ cudaError_t launch_norm_forward(u32 dtype, const NormArgs& a, int sm_count, cuda
 }
 
 size_t norm_backward_bytes(u32 dtype, const NormArgs& a) {
-  const u32 width = dtype == PS_F32 ? 4 : 2, blocks = std::max(backward_shape(width, a.rows, a.cols, 2).blocks, backward_shape(width, a.rows, a.cols, 3).blocks);
-  return (size_t)blocks * 2 * a.cols * sizeof(float);
+  const u32 width = dtype == PS_F32 ? 4 : 2, groups = std::max(backward_shape(width, a.rows, a.cols, 2).groups, backward_shape(width, a.rows, a.cols, 3).groups);
+  return (size_t)groups * 2 * a.cols * sizeof(float);
 }
 
 cudaError_t launch_norm_backward(u32 dtype, const NormArgs& a, int sm_count, cudaStream_t stream) {

@@ -54,7 +54,7 @@ def norm_want(x, weight, bias, eps):
 
 
 NORM_SHAPES = [(1, 1), (3, 2), (5, 7), (4, 8), (2, 31), (9, 128), (130, 768), (7, 1000), (3, 1024), (5, 1032), (3, 1155), (11, 2048), (2, 2056),
-               (6, 4099), (3, 4104), (4, 5003), (2, 8192), (3, 8200), (2, 9001), (3, 16384), (2, 16392), (2, 20000), (2, 32768), (2, 32776), (1, 40001)]
+               (6, 4099), (3, 4104), (4, 5003), (2, 8192), (3, 8200), (2, 9001), (3, 16384), (2, 16392), (2, 20000), (2, 32768), (2, 32776), (1, 40001), (2, 65536), (3, 70000), (2, 70001)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -91,7 +91,7 @@ def grad_want(d_y, x, mean, rstd, weight, residual):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows, cols", NORM_SHAPES + [(3000, 257), (1500, 768), (700, 4096), (701, 5003), (3001, 8), (200, 33000)])
+@pytest.mark.parametrize("rows, cols", NORM_SHAPES + [(3000, 257), (1500, 768), (700, 4096), (701, 5003), (3001, 8), (200, 33000), (500, 12000), (300, 70000)])
 def test_layer_norm_gradients(ctx, dtype, rows, cols):
     t = TYPES[dtype]
     gen = torch.Generator("cuda").manual_seed(rows * 7 + cols)
