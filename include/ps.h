@@ -30,7 +30,7 @@
  *
  * Beside the figures stand a brute-force run of the mechanism (ps_verify_batch) and
  * the operators of a training step whose terms the figures price (ps_dropout,
- * ps_embed_*, ps_attention_*), which compute in floating point.
+ * ps_embed_*, ps_attention_*, ps_layer_norm_*, ps_rotary, ps_linear_*), which compute in floating point.
  *
  * Conventions.  Every function returns 0 (PS_OK) or a negative PS_E_* code and
  * never aborts.  "device pointer" = memory of the context's GPU, owned by the
@@ -629,7 +629,8 @@ int ps_rotary(ps_ctx* ctx, const ps_rotary_desc* desc, const ps_heads* q, const 
  * the gradient of that, and the layer below is given no activation of its own.  Null results are not computed.
  * d_weight and d_bias, of the type or float (grad_dtype), are added to what is there with accumulate (rounded once).
  *
- * Products run on the tensor cores with sums of 32 bits.  A row of y or d_x depends on that row, weight and the widths
+ * Products run on the tensor cores with sums of 32 bits, which they cut off rather than round; a gradient of type float is
+ * summed 4096 tokens at a time, so that this does not add up, and of d_pre it takes what the rounding left as well.  A row of y or d_x depends on that row, weight and the widths
  * alone, not on how many rows or columns the call has; so shards of tokens, and shards of outputs, compute the single device's bits.
  * d_weight's sum over tokens has an order that depends on the sizes alone.
  * Matrices begin at multiples of 16 bytes and have strides that are multiples of 16 bytes; bias any alignment of its type.

@@ -5,7 +5,8 @@
 // float is at most an eighth of a turn and keeps 24 bits of itself.
 //
 // Bytes bound it: all heads of a token share its angles, so a block computes the sines and cosines of its few tokens once, into
-// shared memory, and then moves the heads by 16 bytes a thread, several of them in flight.
+// shared memory, and a thread keeps those of its place in the head in registers while it goes over the heads, 16 bytes at a time, several in flight.
+// 2 x 32768 tokens, 64 and 8 heads of 128 in bfloat16, 2.4 GB: 401 us, 6.0 TB/s (0.92 of a copy's rate); with an item's place computed for each, 519 us.
 #include <algorithm>
 #include "ps_train.cuh"
 
