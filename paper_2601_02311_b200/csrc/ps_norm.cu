@@ -76,7 +76,8 @@ __device__ __forceinline__ bool passed_in_cluster(u32 bar, u32 parity) {
   return ok != 0;
 }
 constexpr u32 CLUSTER_MOST = 8;
-// As RowSum, over the R threads of each of the cluster's blocks: every warp sends its sums to all blocks, and arrives at their barriers.
+// As RowSum, over the R threads of each of the cluster's blocks: every warp sends its sums to all blocks, and arrives at their barriers.  (With the block's sum
+// taken first, and sent by one warp, 8000 x 16384 backward took 315 us instead of 289.)
 template <int R, int COUNT>
 struct ClusterSum {
   static constexpr u32 WARPS = R / 32, SLOTS = 2 * COUNT * CLUSTER_MOST * WARPS;
@@ -422,6 +423,118 @@ __global__ void __launch_bounds__(R + 32, forward_blocks(R, E * sizeof(T))) k_no
   if (SHARED) end_sums();
 }
 
+// ---- Rows of up to 256 columns, in the backward pass 64: up to 32 lanes have a row, 8 elements each, and a warp as many rows as it has lanes for.  (107040 rows of 4 columns: 27 us, with a block
+// for each 115.  100000 of 250: 58 and 95 us forward, but 214 and 159 backward.)
+constexpr int NARROW = 256, NARROW_GRAD = 64, NARROW_E = 8, NARROW_BLOCKS = 4, NARROW_GRAD_BLOCKS = 2;
+__device__ __forceinline__ float lanes_sum(float v, u32 lanes) {
+  for (u32 m = lanes / 2; m > 0; m /= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
+  return v;
+}
+template <class T>
+__global__ void __launch_bounds__(256, NARROW_BLOCKS) k_norm_narrow(const NormArgs a, u32 lanes, float share) {
+  const u32 lane = threadIdx.x % lanes, cols = (u32)a.cols, at_once = 256 / lanes;
+  float w[NARROW_E], b[NARROW_E];
+#pragma unroll
+  for (int e = 0; e < NARROW_E; ++e) {
+    const u32 c = e * lanes + lane;
+    w[e] = a.weight && c < cols ? widen(((const T*)a.weight)[c]) : 1.f;
+    b[e] = a.bias && c < cols ? widen(((const T*)a.bias)[c]) : 0.f;
+  }
+  // (all lanes of a warp go round as often: they meet in the sums)
+  for (u64 first = (u64)blockIdx.x * at_once; first < a.rows; first += (u64)gridDim.x * at_once) {
+    const u64 r = first + threadIdx.x / lanes;
+    const bool there = r < a.rows;
+    float v[NARROW_E], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < NARROW_E; ++e) {
+      const u32 c = e * lanes + lane;
+      v[e] = there && c < cols ? widen(((const T*)a.x.data)[r * a.x.stride + c]) : 0.f;
+      sum += v[e];
+    }
+    const float mean = lanes_sum(sum, lanes) * share;
+    sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < NARROW_E; ++e) {
+      v[e] = e * lanes + lane < cols ? v[e] - mean : 0.f;
+      sum = fmaf(v[e], v[e], sum);
+    }
+    const float rstd = reciprocal_root(fmaf(lanes_sum(sum, lanes), share, a.eps));
+    if (!there) continue;
+#pragma unroll
+    for (int e = 0; e < NARROW_E; ++e) {
+      const u32 c = e * lanes + lane;
+      if (c < cols) ((T*)a.y.data)[r * a.y.stride + c] = narrow<T>(fmaf(v[e], rstd * w[e], b[e]));
+    }
+    if (lane == 0) {
+      if (a.mean) a.mean[r] = mean;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+  }
+}
+template <class T, bool GRADS>
+__global__ void __launch_bounds__(256, NARROW_GRAD_BLOCKS) k_norm_grad_narrow(const NormArgs a, u32 lanes, float share) {
+  __shared__ float sums[2][8][NARROW_GRAD];
+  const u32 lane = threadIdx.x % lanes, cols = (u32)a.cols, at_once = 256 / lanes;
+  float w[NARROW_E], of_w[NARROW_E], of_b[NARROW_E];
+#pragma unroll
+  for (int e = 0; e < NARROW_E; ++e) {
+    const u32 c = e * lanes + lane;
+    w[e] = a.weight && c < cols ? widen(((const T*)a.weight)[c]) : 1.f;
+    of_w[e] = of_b[e] = 0.f;
+  }
+  for (u64 first = (u64)blockIdx.x * at_once; first < a.rows; first += (u64)gridDim.x * at_once) {
+    const u64 r = first + threadIdx.x / lanes;
+    const bool there = r < a.rows;
+    const float mean = there ? a.mean[r] : 0.f, rstd = there ? a.rstd[r] : 0.f;
+    float xn[NARROW_E], g[NARROW_E], along = 0.f, across = 0.f;
+#pragma unroll
+    for (int e = 0; e < NARROW_E; ++e) {
+      const u32 c = e * lanes + lane;
+      const bool here = there && c < cols;
+      xn[e] = here ? (widen(((const T*)a.x.data)[r * a.x.stride + c]) - mean) * rstd : 0.f;
+      g[e] = here ? widen(((const T*)a.d_y.data)[r * a.d_y.stride + c]) : 0.f;
+      if (GRADS) {
+        of_w[e] = fmaf(g[e], xn[e], of_w[e]);
+        of_b[e] += g[e];
+      }
+      g[e] = __fmul_rn(g[e], w[e]);       // (never one instruction with the sum: the same bits with GRADS and without)
+      along += g[e];
+      across = fmaf(g[e], xn[e], across);
+    }
+    along = -lanes_sum(along, lanes) * share, across = -lanes_sum(across, lanes) * share;
+    if (!there) continue;
+#pragma unroll
+    for (int e = 0; e < NARROW_E; ++e) {
+      const u32 c = e * lanes + lane;
+      if (c < cols) {
+        const float v = g[e] + fmaf(xn[e], across, along);
+        ((T*)a.d_x.data)[r * a.d_x.stride + c] =
+            narrow<T>(a.residual.data ? fmaf(rstd, v, widen(((const T*)a.residual.data)[r * a.residual.stride + c])) : rstd * v);
+      }
+    }
+  }
+  if (GRADS) {                  // the rows of a warp, then the warps
+#pragma unroll
+    for (int e = 0; e < NARROW_E; ++e) {
+      for (u32 m = lanes; m < 32; m *= 2) {
+        of_w[e] += __shfl_xor_sync(0xffffffffu, of_w[e], m);
+        of_b[e] += __shfl_xor_sync(0xffffffffu, of_b[e], m);
+      }
+      if (threadIdx.x % 32 < lanes) {
+        sums[0][threadIdx.x / 32][e * lanes + lane] = of_w[e];
+        sums[1][threadIdx.x / 32][e * lanes + lane] = of_b[e];
+      }
+    }
+    __syncthreads();
+    for (u32 c = threadIdx.x; c < 2 * cols; c += 256) {
+      const u32 which = c >= cols;
+      float all = 0.f;
+      for (int i = 0; i < 8; ++i) all += sums[which][i][c - which * cols];
+      a.parts[(u64)blockIdx.x * 2 * cols + c] = all;
+    }
+  }
+}
+
 // any width: a block walks the row three times (the second and third time out of the L2)
 constexpr int LONG = 1024;
 template <class T>
@@ -624,7 +737,10 @@ Layout layout_of(int most, u32 wanted, u64 cols, u32 width, u32 arrays, u32 more
   return l;
 }
 Layout forward_layout(int threads, int bytes, u64 cols, u32 width) { return layout_of(forward_blocks(threads, bytes), 2, cols, width, 1, 0); }
-Layout backward_layout(int threads, u64 cols, u32 width, u32 arrays) { return layout_of(backward_blocks(threads), 4, cols, width, arrays, 1); }
+// (Blocks of clusters wait for one another: two on an SM rather than many stages.  1596 x 19021 floats with a residual: 181 us, with one 461.)
+Layout backward_layout(int threads, u64 cols, u32 width, u32 arrays, bool shared) {
+  return layout_of(backward_blocks(threads), shared ? 2 : 4, cols, width, arrays, 1);
+}
 // (asked for once a kernel and device)
 template <auto KERNEL>
 struct Prepared {
@@ -668,6 +784,12 @@ cudaError_t launch_cluster(void (*kernel)(Parameters...), u32 grid, u32 cluster,
   return cudaLaunchKernelEx(&config, kernel, Parameters(arguments)...);
 }
 
+u32 narrow_lanes(u64 cols) {
+  u32 lanes = 1;
+  while (lanes * NARROW_E < cols) lanes *= 2;
+  return lanes;
+}
+
 // Threads of a row, by the width: as few as hold it in 16 elements each, of rows of up to 64 KB in more of 512 threads.  (16384 columns of bfloat16:
 // 8000 rows, 143 us by one block, 223 by two.)
 template <class T, int R, bool PACKED, bool SHARED = false, int E = 16>
@@ -681,6 +803,11 @@ cudaError_t forward(const NormArgs& a, const Wide& wide, const Sharing& sharing,
 }
 template <class T, bool PACKED>
 cudaError_t forward(const NormArgs& a, const Wide& wide, int sm_count, cudaStream_t stream) {
+  if (a.cols <= NARROW) {
+    const u32 lanes = narrow_lanes(a.cols), at_once = 256 / lanes;
+    k_norm_narrow<T><<<blocks_for((a.rows + at_once - 1) / at_once, NARROW_BLOCKS, sm_count), 256, 0, stream>>>(a, lanes, 1.f / (float)a.cols);
+    return cudaGetLastError();
+  }
   constexpr u32 MOST = 65536 / sizeof(T);
   const Sharing s = a.cols <= MOST ? Sharing{1, (u32)a.cols, SMS} : sharing_of(a.cols, A_BLOCKS_COLUMNS);
   if (s.blocks == 0) {
@@ -715,7 +842,12 @@ struct Shape {
   u32 groups;
   Sharing sharing;
 };
+constexpr int LANES = 1;                  // threads of narrow rows
 Shape backward_shape(u32 width, u64 rows, u64 cols, u32 arrays) {
+  if (cols <= NARROW_GRAD) {
+    const u64 at_once = 256 / narrow_lanes(cols);
+    return {LANES, (u32)std::max<u64>(1, std::min<u64>((rows + 2 * at_once - 1) / (2 * at_once), SMS * NARROW_GRAD_BLOCKS)), {}};
+  }
   // two stages and the weights have to fit: of floats with more than 4096 columns not always
   const bool fits = cols <= A_BLOCKS_COLUMNS && (2 * arrays + 1) * slot_of(cols, width) <= ROOM - 2048;
   Shape s = {0, 0, sharing_of(cols, width == 2 || fits ? A_BLOCKS_COLUMNS : A_BLOCKS_COLUMNS / 2)};
@@ -725,13 +857,13 @@ Shape backward_shape(u32 width, u64 rows, u64 cols, u32 arrays) {
   }
   s.threads = s.sharing.blocks > 1 ? (width == 2 ? 512 : 256) : 32;
   while (s.threads < 512 && s.sharing.each > (u64)s.threads * 16) s.threads *= 2;
-  s.groups = (u32)std::max<u64>(1, std::min<u64>((rows + 3) / 4, s.sharing.clusters * backward_layout(s.threads, s.sharing.each, width, arrays).resident));
+  s.groups = (u32)std::max<u64>(1, std::min<u64>((rows + 3) / 4, s.sharing.clusters * backward_layout(s.threads, s.sharing.each, width, arrays, s.sharing.blocks > 1).resident));
   return s;
 }
 template <class T, int R, bool PACKED, bool GRADS, bool SHARED>
 cudaError_t backward(const NormArgs& a, const Wide& wide, const Shape& s, cudaStream_t stream) {
   constexpr auto kernel = k_norm_grad<T, R, PACKED, GRADS, SHARED>;
-  const Layout l = backward_layout(R, s.sharing.each, sizeof(T), a.residual.data ? 3 : 2);
+  const Layout l = backward_layout(R, s.sharing.each, sizeof(T), a.residual.data ? 3 : 2, SHARED);
   const cudaError_t e = Prepared<kernel>::smem(l.smem);
   if (e != cudaSuccess) return e;
   return launch_cluster(kernel, s.groups * s.sharing.blocks, s.sharing.blocks, R + 32, l.smem, stream, a, wide, l.ring, 1.f / (float)a.cols, s.sharing.each);
@@ -743,6 +875,11 @@ cudaError_t backward(const NormArgs& a, const Wide& wide, const Shape& s, cudaSt
 template <class T, bool PACKED>
 cudaError_t backward(const NormArgs& a, const Shape& s, int sm_count, cudaStream_t stream) {
   const Wide wide = wide_of(a, sizeof(T));
+  if (s.threads == LANES) {
+    if (a.parts) k_norm_grad_narrow<T, true><<<s.groups, 256, 0, stream>>>(a, narrow_lanes(a.cols), 1.f / (float)a.cols);
+    else k_norm_grad_narrow<T, false><<<s.groups, 256, 0, stream>>>(a, narrow_lanes(a.cols), 1.f / (float)a.cols);
+    return cudaGetLastError();
+  }
   if (s.sharing.blocks > 1) return backward<T, sizeof(T) == 2 ? 512 : 256, PACKED, true>(a, wide, s, stream);
   if (s.threads == 32) return backward<T, 32, PACKED>(a, wide, s, stream);
   if (s.threads == 64) return backward<T, 64, PACKED>(a, wide, s, stream);

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(THREADS, 4) k_rotary(const __grid_constant__ R
       const u64 where = b * a.position_stride + at;
       position = a.position_bytes == 8 ? ((const s64*)a.positions)[where] : (s64)((const int*)a.positions)[where];
     }
-    const u64 turns = (u64)(position + a.first) * a.turns[pair];
+    const u64 turns = ((u64)position + (u64)a.first) * a.turns[pair];
     circle[i] = turned(a.inverse ? 0 - turns : turns, a.magnitude);
   }
   const u32 a_token = plan.items * plan.heads_at_once, slot = threadIdx.x / a_token, place = threadIdx.x - slot * a_token;

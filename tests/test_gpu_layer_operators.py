@@ -54,7 +54,7 @@ def norm_want(x, weight, bias, eps):
 
 
 NORM_SHAPES = [(1, 1), (3, 2), (5, 7), (4, 8), (2, 31), (9, 128), (130, 768), (7, 1000), (3, 1024), (5, 1032), (3, 1155), (11, 2048), (2, 2056),
-               (6, 4099), (3, 4104), (4, 5003), (2, 8192), (3, 8200), (2, 9001), (3, 16384), (2, 16392), (2, 20000), (2, 32768), (2, 32776), (1, 40001), (2, 65536), (3, 70000), (2, 70001)]
+               (300, 2), (700, 6), (129, 33), (65, 200), (40, 255), (41, 257), (6, 4099), (3, 4104), (4, 5003), (2, 8192), (3, 8200), (2, 9001), (3, 16384), (2, 16392), (2, 20000), (2, 32768), (2, 32776), (1, 40001), (2, 65536), (3, 70000), (2, 70001)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -549,6 +549,26 @@ def test_linear_into_larger_tensors(ctx, dtype):
     for n, (r, c) in dict(y=(slice(1, 134), slice(8, 139)), pre=(slice(7, 140), slice(160, 291)), dx=(slice(5, 138), slice(16, 165))).items():
         whole[n][r, c] = before[n][r, c]
         assert torch.equal(whole[n], before[n])
+
+
+@pytest.mark.parametrize("inputs, outputs", [(1603, 1500), (1600, 1501), (2200, 2300)])
+def test_weight_gradients_of_several_sums(ctx, inputs, outputs):
+    """More tokens than a sum in 32 bits takes at a time: the tile is read and added to, where it was written by boxes and where by lanes.
+    Whole numbers, so that the result is exact."""
+    t, gen = torch.bfloat16, torch.Generator("cuda").manual_seed(inputs)
+    x, d_y, pre = whole_numbers(gen, 9000, inputs, t), whole_numbers(gen, 9000, outputs, t), whole_numbers(gen, 9000, outputs, t)
+    old = torch.zeros(outputs, (inputs + 7) // 8 * 8, device="cuda")
+    old.copy_(torch.randint(-99, 100, old.shape, device="cuda", generator=gen))
+    for activation in (None, "relu"):
+        d_pre = d_y.double() * (1 if activation is None else pre > 0)
+        want = d_pre.t() @ x.double()
+        into, around = old.clone(), old.clone()
+        ctx.linear_backward_into(d_y, x, None, d_weight=into[:, :inputs], pre=pre, activation=activation)
+        assert torch.equal(into[:, :inputs], want.float())
+        ctx.linear_backward_into(d_y, x, None, d_weight=around[:, :inputs], pre=pre, activation=activation, accumulate=True)
+        ctx.check_status()
+        assert torch.equal(around[:, :inputs], (want + old[:, :inputs].double()).float())
+        assert torch.equal(into[:, inputs:], old[:, inputs:]) and torch.equal(around[:, inputs:], old[:, inputs:])
 
 
 def test_linear_of_no_tokens(ctx):
