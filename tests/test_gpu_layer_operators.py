@@ -410,7 +410,7 @@ def products_err(a, b, dims):
 
 
 def function_err(v, name):
-    """What the fast exponential (2 + 1.2 |argument| units of 2 F, arguments up to 1.6 |v| + 0.08 |v|^3 and up to 88), erf (2 units) and the
+    """What the fast exponential (2 + 1.2 |argument| units of 2 F, arguments up to 1.6 |v| + 0.08 |v|^3 and up to 88), erf (1.5e-7, 2.6 F) and the
     few operations around them do to an activation, relative to 1 + |v|."""
     v = v.abs()
     argument = {"none": 0 * v, "relu": 0 * v, "gelu": v * v / 2, "gelu_tanh": 1.6 * v + 0.072 * v ** 3, "silu": v}[name].clamp(max=88)
