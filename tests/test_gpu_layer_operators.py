@@ -730,3 +730,35 @@ def test_long_sums_keep_32_bits(ctx, dtype):
         ctx.check_status()
         # 256 additions of 16 products a time, cut off (2 F each, relative to a sum that grows evenly: half of that), and ten of such sums
         within(d_w, want[:outputs], (256 + 16 + 2 * 20) * F * want[:outputs])
+
+
+def test_products_beside_attention(ps):
+    """Kernels that each take all of an SM's tensor memory, from two streams at once."""
+    gen = torch.Generator("cuda").manual_seed(31)
+    x, w = matrix(gen, 3000, 520, torch.bfloat16), matrix(gen, 2000, 520, torch.bfloat16)
+    d_y = matrix(gen, 3000, 2000, torch.bfloat16)
+    q = normal(gen, 2, 700, 6, 128, dtype=torch.bfloat16)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    contexts = [ps.Context(0, s) for s in streams]
+
+    def layer(c):
+        return (c.linear_forward(x, w, activation="silu"),) + c.linear_backward(d_y, x, w, dtype=torch.float32)
+
+    def attend(c):
+        out, lse = c.attention_forward(q, q, q)
+        return (out, lse) + c.attention_backward(q, q, q, out, lse, q)
+    torch.cuda.synchronize()
+    want = []
+    for f, c, s in zip((layer, attend), contexts, streams):
+        with torch.cuda.stream(s):
+            want.append(f(c))
+        torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(6):
+        for i, (f, c, s) in enumerate(zip((layer, attend), contexts, streams)):
+            with torch.cuda.stream(s):
+                got[i].append(f(c))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in range(2) for run in got[i] for a, b in zip(run, want[i]))
+    for c in contexts:
+        c.check_status()
