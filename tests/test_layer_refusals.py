@@ -54,7 +54,7 @@ def norm(**change):
 
 def norm_grad(**change):
     args = dict(rows=4, cols=8, eps=0.0, dtype=0, grad_dtype=0, accumulate=0)
-    m = matrices(dict(d_y=[AT, 8], x=[AT + 1024, 8], residual=[AT + 2048, 8], d_x=[AT + 3072, 8]), change)
+    m = matrices(dict(d_y=[AT, 8], x=[AT + 1024, 8], residual=[AT + 2048, 8], d_x=[AT + 3328, 8]), change)
     ptr = dict(ctx=CTX, weight=AT + 4096, mean=AT + 4352, rstd=AT + 4608, d_weight=AT + 5120, d_bias=AT + 5376, work=AT + 16384, work_bytes=1 << 14)
     for k, v in change.items():
         (ptr if k in ptr else args)[k] = v
@@ -94,7 +94,7 @@ def rotary(**change):
     args = dict(batch=2, len=4, heads=4, kv_heads=2, dim=8, rotary_dim=8, dtype=1, interleaved=0, inverse=0, position_bytes=4, position_stride=0, first=0,
                 base=1e4, factor=1.0, original=0.0, low=1.0, high=32.0, magnitude=1.0)
     ptr = dict(ctx=CTX, positions=None)
-    heads = dict(q=[AT, 128, 32, 8], q_out=[AT + 1024, 128, 32, 8], k=[AT + 2048, 64, 16, 8], k_out=[AT + 3072, 64, 16, 8])
+    heads = dict(q=[AT, 128, 32, 8], q_out=[AT + 1024, 128, 32, 8], k=[AT + 2048, 64, 16, 8], k_out=[AT + 3328, 64, 16, 8])
     for k, v in change.items():
         if k in heads:
             heads[k] = None if v is None else [h if x is None else x for x, h in zip(v, heads[k])]
@@ -128,7 +128,7 @@ def test_rotary_of_nothing_is_done(change):
 
 def linear(**change):
     args = dict(tokens=4, inputs=8, outputs=16, dtype=1, grad_dtype=1, activation=0)
-    m = matrices(dict(x=[AT, 8], weight=[AT + 1024, 8], residual=[AT + 2048, 16], y=[AT + 3072, 16], pre=[AT + 4096, 16]), change)
+    m = matrices(dict(x=[AT, 8], weight=[AT + 1024, 8], residual=[AT + 2048, 16], y=[AT + 3328, 16], pre=[AT + 4096, 16]), change)
     ptr = dict(ctx=CTX, bias=AT + 5120)
     for k, v in change.items():
         (ptr if k in ptr else args)[k] = v
@@ -137,7 +137,7 @@ def linear(**change):
 
 def linear_grad(**change):
     args = dict(tokens=4, inputs=8, outputs=16, dtype=1, grad_dtype=0, activation=2, below_activation=2, accumulate=0)
-    m = matrices(dict(d_y=[AT, 16], x=[AT + 1024, 8], weight=[AT + 2048, 8], pre=[AT + 3072, 16], below=[AT + 4096, 8], residual=[AT + 5120, 8],
+    m = matrices(dict(d_y=[AT, 16], x=[AT + 1024, 8], weight=[AT + 2048, 8], pre=[AT + 3328, 16], below=[AT + 4096, 8], residual=[AT + 5120, 8],
                       d_x=[AT + 6144, 8], d_weight=[AT + 7168, 8]), change)
     ptr = dict(ctx=CTX, d_bias=AT + 8192, work=AT + 16384, work_bytes=1 << 14)
     for k, v in change.items():
@@ -149,11 +149,11 @@ def linear_grad(**change):
 @pytest.mark.parametrize("change, code", [
     (dict(ctx=None), ps.E_NULLPTR), (dict(x=None), ps.E_NULLPTR), (dict(weight=None), ps.E_NULLPTR), (dict(y=None), ps.E_NULLPTR),
     (dict(residual=(0, None)), ps.E_NULLPTR), (dict(x=(AT + 2, None)), ps.E_ALIGN), (dict(x=(None, 12)), ps.E_ALIGN), (dict(weight=(None, 9)), ps.E_ALIGN),
-    (dict(y=(AT + 3072 + 8, None)), ps.E_ALIGN), (dict(pre=(None, 20)), ps.E_ALIGN), (dict(bias=AT + 1), ps.E_ALIGN), (dict(y=(None, 8)), ps.E_RANGE),
+    (dict(y=(AT + 3328 + 8, None)), ps.E_ALIGN), (dict(pre=(None, 20)), ps.E_ALIGN), (dict(bias=AT + 1), ps.E_ALIGN), (dict(y=(None, 8)), ps.E_RANGE),
     (dict(tokens=(1 << 30) + 1), ps.E_RANGE), (dict(inputs=0), ps.E_RANGE), (dict(outputs=(1 << 24) + 1), ps.E_RANGE), (dict(dtype=0), ps.E_RANGE),
     (dict(dtype=3), ps.E_RANGE), (dict(grad_dtype=2), ps.E_RANGE), (dict(activation=5), ps.E_RANGE), (dict(below_activation=5), ps.E_RANGE),
     (dict(accumulate=2), ps.E_RANGE), (dict(x=(None, 1 << 50)), ps.E_RANGE), (dict(y=(AT + 2048 + 16, None)), ps.E_RANGE), (dict(y=(AT, None)), ps.E_RANGE),
-    (dict(pre=(AT + 3072, None)), ps.E_RANGE), (dict(pre=(AT + 2048, None)), ps.E_RANGE), (dict(tokens=1 << 30, inputs=1 << 20), ps.E_RANGE)])
+    (dict(pre=(AT + 3328, None)), ps.E_RANGE), (dict(pre=(AT + 2048, None)), ps.E_RANGE), (dict(tokens=1 << 30, inputs=1 << 20), ps.E_RANGE)])
 def test_linear_refuses(change, code):
     assert linear(**change) == code
 
