@@ -630,8 +630,9 @@ int ps_rotary(ps_ctx* ctx, const ps_rotary_desc* desc, const ps_heads* q, const 
  * d_weight and d_bias, of the type or float (grad_dtype), are added to what is there with accumulate (rounded once).
  *
  * Products run on the tensor cores with sums of 32 bits, which they cut off rather than round; a gradient of type float is
- * summed 4096 tokens at a time, so that this does not add up, and of d_pre it takes what the rounding left as well.  A row of y or d_x depends on that row, weight and the widths
- * alone, not on how many rows or columns the call has; so shards of tokens, and shards of outputs, compute the single device's bits.
+ * summed 1536 tokens at a time, so that this does not add up, and of d_pre it takes what the rounding left as well.
+ * A row of y or d_x depends on that row, weight and the widths alone, not on how many rows or columns the call has; so
+ * shards of tokens, and shards of outputs, compute the single device's bits.
  * d_weight's sum over tokens has an order that depends on the sizes alone.
  * Matrices begin at multiples of 16 bytes and have strides that are multiples of 16 bytes; bias any alignment of its type.
  * Widths need not be multiples of anything.  What lies behind a row's last element is not used.

@@ -728,7 +728,7 @@ def test_long_sums_keep_32_bits(ctx, dtype):
     for outputs in (136, 8):
         _, d_w, _ = ctx.linear_backward(d_y[:, :outputs], x, torch.zeros(outputs, 72, device="cuda", dtype=t), dtype=torch.float32)
         ctx.check_status()
-        # 256 additions of 16 products a time, cut off (2 F each, relative to a sum that grows evenly: half of that), and ten of such sums
+        # at most 256 additions of 16 products a time, cut off (2 F each, relative to a sum that grows evenly: half of that), and at most 40 such sums
         within(d_w, want[:outputs], (256 + 16 + 2 * 20) * F * want[:outputs])
 
 
