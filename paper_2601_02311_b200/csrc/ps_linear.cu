@@ -610,7 +610,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
           if (p.out.data && column + CHUNK > (int)p.n) {
             store_edge<O>(p.out, row, column, p.m, p.n, mine);
             if (X::KIND == OUTPUT && p.has_pre) store_edge<T>(p.pre, row, column, p.m, p.n, other);
-            if (sizeof(O) == 4) asm volatile("fence.proxy.async;" ::: "memory");        // (a copy may read it again)
+            // The next copy into the buffers comes behind what the lanes have read and written there; a sum in 32 bits is read from memory again, too.
+            if (sizeof(O) == 4) asm volatile("fence.proxy.async;" ::: "memory");
+            else fence_async();
             __syncwarp();
             continue;
           }
