@@ -294,6 +294,10 @@ struct Vector {
 __device__ __forceinline__ u64 twice(float v) { return pair(v, v); }
 __device__ __forceinline__ float together(u64 v) { return split(v).x + split(v).y; }
 
+// what stands n elements behind `p`; what is not there stays null (a block of a cluster asks whether there is a residual)
+template <class T> __device__ __forceinline__ void* moved(void* p, u32 n) { return p ? (T*)p + n : nullptr; }
+template <class T> __device__ __forceinline__ const void* moved(const void* p, u32 n) { return p ? (const T*)p + n : nullptr; }
+
 struct Wide {           // which rows begin at multiples of 16 bytes
   bool x, y, d_y, residual, d_x, weight, bias;
 };
@@ -342,9 +346,8 @@ __global__ void __launch_bounds__(R + 32, forward_blocks(R, E * sizeof(T))) k_no
   if (SHARED) {
     blocks = cluster_size(), begin = cluster_rank() * each;
     a.cols = min((u64)each, args.cols - begin);
-    for (ps_matrix* m : {&a.x, &a.y, &a.d_y, &a.residual, &a.d_x}) m->data = (T*)m->data + begin;
-    if (a.weight) a.weight = (const T*)a.weight + begin;
-    if (a.bias) a.bias = (const T*)a.bias + begin;
+    for (ps_matrix* m : {&a.x, &a.y}) m->data = moved<T>(m->data, begin);
+    a.weight = moved<T>(a.weight, begin), a.bias = moved<T>(a.bias, begin);
   }
   const u32 cols = (u32)a.cols;
   const u64 row = blockIdx.x / blocks, step = gridDim.x / blocks;
@@ -579,9 +582,8 @@ __global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const 
   if (SHARED) {
     blocks = cluster_size(), begin = cluster_rank() * each;
     a.cols = min((u64)each, args.cols - begin);
-    for (ps_matrix* m : {&a.x, &a.y, &a.d_y, &a.residual, &a.d_x}) m->data = (T*)m->data + begin;
-    if (a.weight) a.weight = (const T*)a.weight + begin;
-    if (a.bias) a.bias = (const T*)a.bias + begin;
+    for (ps_matrix* m : {&a.x, &a.d_y, &a.residual, &a.d_x}) m->data = moved<T>(m->data, begin);
+    a.weight = moved<T>(a.weight, begin);
   }
   const u32 cols = (u32)a.cols;
   const u64 row = blockIdx.x / blocks, step = gridDim.x / blocks;

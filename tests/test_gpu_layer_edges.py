@@ -43,3 +43,18 @@ def test_last_columns_between_copies(ctx, dtype, width):
         ctx.linear_backward_into(x, None, weight, d_x=d_x, below=below, below_activation="relu", residual=res)
         ctx.check_status()
         assert torch.equal(d_x, d_want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [4100, 8200, 12000, 16392, 33000, 65536])
+def test_shared_rows_without_a_residual(ctx, dtype, cols):
+    """A residual that is not there adds what one of zeros does, in every block that shares a row; with the columns' sums and without."""
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(cols)
+    x, d_y, weight = normal(gen, 40, cols, dtype=t), normal(gen, 40, cols, dtype=t), normal(gen, cols, dtype=t)
+    _, mean, rstd = ctx.layer_norm_forward(x, weight)
+    want = ctx.layer_norm_backward(d_y, x, mean, rstd, weight, torch.zeros_like(x))[0]
+    alone = torch.empty_like(x)
+    ctx.layer_norm_backward_into(d_y, x, mean, rstd, alone, weight)
+    with_sums = ctx.layer_norm_backward(d_y, x, mean, rstd, weight)[0]
+    ctx.check_status()
+    assert torch.equal(alone, want) and torch.equal(with_sums, want)
