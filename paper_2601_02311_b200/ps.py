@@ -791,9 +791,10 @@ class Context:
         return d_x, d_weight, d_bias
 
     @staticmethod
-    def linear_backward_bytes(tokens: int, inputs: int, outputs: int, activation: str | None = None) -> int:
-        """Bytes of the work buffer that linear_backward_into takes."""
-        return _lib.ps_linear_backward_bytes(_LINEAR_DESC(tokens, inputs, outputs, 1, 1, ACTIVATIONS[activation], 0, 0, 0))
+    def linear_backward_bytes(tokens: int, inputs: int, outputs: int, activation: str | None = None, dtype: torch.dtype | None = None) -> int:
+        """Bytes of the work buffer that linear_backward_into takes; `dtype`: of the gradients of weight and bias (default: enough for any)."""
+        wide = _DTYPE[torch.float32 if dtype is None else dtype]
+        return _lib.ps_linear_backward_bytes(_LINEAR_DESC(tokens, inputs, outputs, wide or _DTYPE[torch.bfloat16], wide, ACTIVATIONS[activation], 0, 0, 0))
 
     def int_peak(self, blocks: int, iters: int, sink: torch.Tensor) -> int:
         ops = C.c_uint64()

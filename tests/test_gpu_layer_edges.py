@@ -58,3 +58,34 @@ def test_shared_rows_without_a_residual(ctx, dtype, cols):
     with_sums = ctx.layer_norm_backward(d_y, x, mean, rstd, weight)[0]
     ctx.check_status()
     assert torch.equal(alone, want) and torch.equal(with_sums, want)
+
+
+@pytest.mark.parametrize("activation", [None, "gelu"])
+@pytest.mark.parametrize("wide", [None, torch.float32])
+@pytest.mark.parametrize("named", [True, False])
+def test_work_of_the_named_size(ctx, activation, wide, named):
+    """Buffers of exactly the size that the binding names are taken, and are enough: the results are those of a call that allocates its own."""
+    t, gen = torch.bfloat16, torch.Generator("cuda").manual_seed(5)
+    x, w, d_y, pre = normal(gen, 700, 72, dtype=t), normal(gen, 120, 72, dtype=t), normal(gen, 700, 120, dtype=t), normal(gen, 700, 120, dtype=t)
+    pre = None if activation is None else pre
+    want = ctx.linear_backward(d_y, x, w, pre, activation, dtype=wide)
+    got = [torch.empty_like(g) for g in want]
+    size = ctx.linear_backward_bytes(700, 72, 120, activation, *([wide or t] if named else []))
+    whole = torch.full((size + 512,), 77, dtype=torch.uint8, device="cuda")
+    ctx.linear_backward_into(d_y, x, w, *got, pre=pre, activation=activation, work=whole[256:256 + size])
+    ctx.check_status()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and whole[:256].eq(77).all() and whole[256 + size:].eq(77).all()
+
+
+@pytest.mark.parametrize("rows, cols", [(300, 64), (900, 1155), (100, 12000)])
+def test_norm_work_of_the_named_size(ctx, rows, cols):
+    gen = torch.Generator("cuda").manual_seed(cols)
+    x, d_y = normal(gen, rows, cols), normal(gen, rows, cols)
+    _, mean, rstd = ctx.layer_norm_forward(x)
+    want = ctx.layer_norm_backward(d_y, x, mean, rstd, residual=d_y)
+    got = [torch.empty_like(g) for g in want]
+    size = ctx.layer_norm_backward_bytes(rows, cols, x.dtype)
+    whole = torch.full((size + 512,), 77, dtype=torch.uint8, device="cuda")
+    ctx.layer_norm_backward_into(d_y, x, mean, rstd, got[0], None, d_y, *got[1:], work=whole[256:256 + size])
+    ctx.check_status()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and whole[:256].eq(77).all() and whole[256 + size:].eq(77).all()
