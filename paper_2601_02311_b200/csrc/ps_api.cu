@@ -9,6 +9,7 @@
 #include <atomic>
 #include <chrono>
 #include <cmath>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -118,6 +119,76 @@ bool overwrites(const void* y, u64 y_stride, const void* x, u64 x_stride, u64 ro
   const u64 pitch = y_stride * width, off = (ya > xa ? ya - xa : xa - ya) % pitch;
   return off < cols * width || pitch - off < cols * width;
 }
+
+// What an operand takes of memory: `bytes` at all sums of up to three strides' multiples.  (bytes 0: nothing.)
+typedef __int128 s128;
+struct Region {
+  static constexpr int DIMS = 3;
+  s128 begin = 0, end = 0;
+  u64 bytes = 0;
+  u64 stride[DIMS] = {}, extent[DIMS] = {1, 1, 1};
+  Region() {}
+  Region(const void* p, u64 n, u64 width) : begin((uintptr_t)p), bytes(p ? n * width : 0) { close(); }
+  Region(const ps_matrix& m, u64 rows, u64 cols, u64 width) : Region(rows ? m.data : nullptr, cols, width) { along(0, m.stride * width, rows); }
+  Region(const ps_heads& h, u32 batch, u32 len, u32 heads, u64 dim, u64 width) : Region(h.data, dim, width) {
+    along(0, h.batch_stride * width, batch), along(1, h.token_stride * width, len), along(2, h.head_stride * width, heads);
+  }
+  void along(int i, u64 by, u64 n) {
+    if (n > 1 && by) stride[i] = by, extent[i] = n;
+    close();
+  }
+  void close() {
+    end = begin + bytes;
+    for (int i = 0; i < DIMS; ++i) end += (s128)(extent[i] - 1) * stride[i];
+  }
+};
+// Whether some whole numbers lo <= n <= hi, one for each stride, bring `apart` strictly between -below and above.  The longest strides come first, so that
+// of each few numbers are left to try; where they are many after all, the answer is yes.
+struct Reach {
+  struct Term {
+    s128 stride, lo, hi;
+  };
+  Term terms[2 * Region::DIMS];
+  int count = 0, tries = 4096;
+  void add(u64 stride, s128 lo, s128 hi) {
+    int i = 0;
+    while (i < count && terms[i].stride > stride) ++i;
+    if (i < count && terms[i].stride == stride) {
+      terms[i].lo += lo, terms[i].hi += hi;
+      return;
+    }
+    for (int j = count++; j > i; --j) terms[j] = terms[j - 1];
+    terms[i] = {stride, lo, hi};
+  }
+  bool within(s128 apart, s128 below, s128 above, int at = 0) {
+    if (at == count) return -below < apart && apart < above;
+    if (--tries < 0) return true;
+    s128 low = 0, high = 0;                     // what the shorter strides can add
+    for (int i = at + 1; i < count; ++i) low += terms[i].stride * terms[i].lo, high += terms[i].stride * terms[i].hi;
+    const Term& t = terms[at];
+    const auto floor = [&](s128 n) { return n >= 0 ? n / t.stride : -((-n + t.stride - 1) / t.stride); };
+    const s128 first = std::max(t.lo, floor(-below - apart - high) + 1), last = std::min(t.hi, -floor(-(above - apart - low)) - 1);
+    for (s128 n = first; n <= last; ++n)
+      if (within(apart + n * t.stride, below, above, at + 1)) return true;
+    return false;
+  }
+};
+bool meet(const Region& a, const Region& b) {
+  if (!a.bytes || !b.bytes || a.end <= b.begin || b.end <= a.begin) return false;
+  Reach r;
+  for (int i = 0; i < Region::DIMS; ++i) {
+    if (a.extent[i] > 1) r.add(a.stride[i], 1 - (s128)a.extent[i], 0);
+    if (b.extent[i] > 1) r.add(b.stride[i], 0, (s128)b.extent[i] - 1);
+  }
+  return r.within(b.begin - a.begin, b.bytes, a.bytes);
+}
+// whether a result meets one of these
+bool meets(const Region& result, std::initializer_list<Region> others) {
+  for (const Region& other : others)
+    if (meet(result, other)) return true;
+  return false;
+}
+bool same_rows(const ps_matrix& x, const ps_matrix& y, u64 rows) { return x.data == y.data && (rows == 1 || x.stride == y.stride); }
 
 // flag bits a filter may require
 constexpr u32 KNOWN_FLAGS = (PS_F_PAPER_PRICED << 1) - 1u;
@@ -982,8 +1053,10 @@ int ps_linear_forward(ps_ctx* ctx, const ps_linear_desc* desc, const ps_matrix* 
     return rc;
   if (!aligned(d_bias, 2)) return PS_E_ALIGN;
   if (a.tokens == 0) return PS_OK;
-  if (spoils(a.y, a.residual, a.tokens, a.outputs, 2) || a.y.data == a.x.data || a.y.data == a.pre.data ||
-      (a.pre.data && (spoils(a.y, a.pre, a.tokens, a.outputs, 2) || a.pre.data == a.residual.data || spoils(a.pre, a.residual, a.tokens, a.outputs, 2))))
+  const Region x_at(a.x, a.tokens, a.inputs, 2), w_at(a.weight, a.outputs, a.inputs, 2), b_at(d_bias, a.outputs, 2),
+      r_at(a.residual, a.tokens, a.outputs, 2), y_at(a.y, a.tokens, a.outputs, 2), pre_at(a.pre, a.tokens, a.outputs, 2);
+  if (meets(y_at, {x_at, w_at, b_at, pre_at}) || meets(pre_at, {x_at, w_at, b_at, r_at}) ||
+      (!same_rows(a.y, a.residual, a.tokens) && meet(y_at, r_at)))
     return PS_E_RANGE;
   if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
   DeviceGuard guard(ctx->device);
@@ -1021,8 +1094,13 @@ int ps_linear_backward(ps_ctx* ctx, const ps_linear_desc* desc, const ps_matrix*
   if (need && !d_work) return PS_E_NULLPTR;
   if (!aligned(d_bias_grad, grad_width) || !aligned(d_work, 256)) return PS_E_ALIGN;
   if (work_bytes < need) return PS_E_RANGE;
-  if (x_grad && a.tokens && (spoils(a.d_x, a.residual, a.tokens, a.inputs, 2) || spoils(a.d_x, a.below, a.tokens, a.inputs, 2) ||
-                             a.d_x.data == a.d_y.data || a.d_x.data == a.x.data))
+  // (pre has been read before a product's result is written)
+  const Region y_at(a.d_y, a.tokens, a.outputs, 2), x_at(a.x, a.tokens, a.inputs, 2), w_at(a.weight, a.outputs, a.inputs, 2),
+      pre_at(a.pre, a.tokens, a.outputs, 2), below_at(a.below, a.tokens, a.inputs, 2), r_at(a.residual, a.tokens, a.inputs, 2),
+      dx_at(a.d_x, a.tokens, a.inputs, 2), dw_at(a.d_weight, a.outputs, a.inputs, grad_width), db_at(d_bias_grad, a.outputs, grad_width);
+  if (meets(dx_at, {y_at, x_at, w_at, dw_at, db_at}) || meets(dw_at, {y_at, x_at, w_at, below_at, r_at, db_at}) ||
+      meets(db_at, {y_at, x_at, w_at, pre_at, below_at, r_at}) || (!same_rows(a.d_x, a.residual, a.tokens) && meet(dx_at, r_at)) ||
+      (!same_rows(a.d_x, a.below, a.tokens) && meet(dx_at, below_at)))
     return PS_E_RANGE;
   if (!x_grad && !weight_grad && !d_bias_grad) return PS_OK;
   if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
