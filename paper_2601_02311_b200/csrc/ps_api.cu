@@ -188,6 +188,24 @@ bool meets(const Region& result, std::initializer_list<Region> others) {
     if (meet(result, other)) return true;
   return false;
 }
+// whether two of a result's own rows meet
+bool meets_itself(const Region& a) {
+  int order[Region::DIMS] = {0, 1, 2};
+  std::sort(order, order + Region::DIMS, [&](int i, int j) { return a.stride[i] < a.stride[j]; });
+  s128 reach = a.bytes;
+  bool apart = true;                            // (as in most tensors: each stride is past all that the shorter ones reach)
+  for (int i : order)
+    if (a.extent[i] > 1) apart = apart && reach <= a.stride[i], reach += (s128)(a.extent[i] - 1) * a.stride[i];
+  if (apart || a.bytes == 0) return false;
+  for (int one = 0; one < Region::DIMS; ++one) {
+    if (a.extent[one] == 1) continue;
+    Reach r;
+    for (int i = 0; i < Region::DIMS; ++i)
+      if (a.extent[i] > 1) r.add(a.stride[i], i == one ? 1 : 1 - (s128)a.extent[i], (s128)a.extent[i] - 1);
+    if (r.within(0, a.bytes, a.bytes)) return true;
+  }
+  return false;
+}
 bool same_rows(const ps_matrix& x, const ps_matrix& y, u64 rows) { return x.data == y.data && (rows == 1 || x.stride == y.stride); }
 
 // flag bits a filter may require
@@ -1002,10 +1020,16 @@ int ps_rotary(ps_ctx* ctx, const ps_rotary_desc* desc, const ps_heads* q, const 
                      (rc = take_any_heads(k_out, d.batch, d.len, d.kv_heads, width, true, a.k_out)) != PS_OK))
     return rc;
   if (!aligned(d_positions, d.position_bytes)) return PS_E_ALIGN;
-  const auto otherwise = [](const ps_heads& x, const ps_heads& y) {      // in the same place, but in another order
-    return x.data == y.data && (x.batch_stride != y.batch_stride || x.token_stride != y.token_stride || x.head_stride != y.head_stride);
+  const auto same = [](const ps_heads& x, const ps_heads& y) {
+    return x.data == y.data && x.batch_stride == y.batch_stride && x.token_stride == y.token_stride && x.head_stride == y.head_stride;
   };
-  if (otherwise(a.q, a.q_out) || (d.kv_heads && (otherwise(a.k, a.k_out) || a.k_out.data == a.q_out.data))) return PS_E_RANGE;
+  const auto heads_at = [&](const ps_heads& h, u32 heads) { return Region(h, d.batch, d.len, heads, d.dim, width); };
+  const Region q_at = heads_at(a.q, d.heads), q_out_at = heads_at(a.q_out, d.heads), k_at = heads_at(a.k, d.kv_heads), k_out_at = heads_at(a.k_out, d.kv_heads);
+  Region at_at(d_positions, d.len, d.position_bytes);
+  at_at.along(0, d.position_stride * d.position_bytes, d.batch);
+  if (meets(q_out_at, {k_at, k_out_at, at_at}) || meets(k_out_at, {q_at, at_at}) || (!same(a.q, a.q_out) && meet(q_out_at, q_at)) ||
+      (!same(a.k, a.k_out) && meet(k_out_at, k_at)) || meets_itself(q_out_at) || meets_itself(k_out_at))
+    return PS_E_RANGE;
   if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return PS_E_CUDA;

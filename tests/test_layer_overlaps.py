@@ -97,3 +97,66 @@ def test_linear_overlaps_against_the_elements_themselves(seed):
         assert got == (ps.E_RANGE if bad else TAKEN), (tokens, inputs, outputs, at, bias)
         seen.add(got)
     assert seen == {ps.E_RANGE, TAKEN}
+
+
+# q AT (2 x 4 x 4 heads of 8, 512 bytes), q_out AT + 1024, k AT + 2048 (256 bytes), k_out AT + 3328
+@pytest.mark.parametrize("change", [
+    dict(q_out=(AT + 2, None, None, None)), dict(q_out=(AT + 64, None, None, None)), dict(q_out=(AT - 510, None, None, None)),
+    dict(q_out=(AT + 16, None, None, None)), dict(q_out=(AT, None, 8, 32)), dict(q_out=(AT + 2048, None, None, None)), dict(q_out=(AT + 2048 - 500, None, None, None)),
+    dict(q_out=(AT + 3328 + 254, None, None, None)), dict(k_out=(AT, None, None, None)), dict(k_out=(AT + 510, None, None, None)),
+    dict(k_out=(AT + 2048 + 16, None, None, None)), dict(k_out=(AT + 1024 + 32, None, None, None)),
+    dict(positions=AT + 1024), dict(positions=AT + 3328 + 252), dict(positions=AT + 3328 - 16, position_stride=4),
+    # a result whose own heads, tokens or sequences meet
+    dict(q_out=(None, 128, 32, 4)), dict(q_out=(None, 128, 8, 8)), dict(q_out=(None, 96, 32, 8)), dict(q_out=(None, 8, 16, 24)), dict(k_out=(None, 64, 16, 7))])
+def test_rotary_refuses_results_over_operands(change):
+    assert answer(t.rotary, **change) == ps.E_RANGE
+
+
+@pytest.mark.parametrize("change", [
+    dict(), dict(q_out=(AT, None, None, None)), dict(q_out=(AT, None, None, None), k_out=(AT + 2048, None, None, None)), dict(q_out=(AT + 512, None, None, None)),
+    # heads of one buffer: q, k and a third kind, in place and turned into the third's place
+    dict(q=(AT, 256, 64, 8), k=(AT + 64, 256, 64, 8), q_out=(AT, 256, 64, 8), k_out=(AT + 64, 256, 64, 8)),
+    dict(q=(AT, 256, 64, 8), k=(AT + 64, 256, 64, 8), k_out=(AT + 96, 256, 64, 8)), dict(q=(AT, 256, 8, 64), q_out=(AT + 64, 256, 8, 64)),
+    # every second element of rows, heads before tokens, sequences inside heads
+    dict(q_out=(AT + 1024, 32, 64, 8)), dict(q_out=(AT + 1024, 32, 8, 64)), dict(q_out=(AT + 1024, 8, 16, 64)),
+    dict(q=(AT, 0, 0, 0)), dict(q=(AT, 0, 32, 8), q_out=(AT + 256, None, None, None)), dict(positions=AT + 512), dict(positions=AT + 1024 - 16)])
+def test_rotary_takes_results_beside_operands(change):
+    assert answer(t.rotary, **change) == TAKEN
+
+
+def of_heads(h, batch, length, heads, dim):
+    return [h[0] + 2 * (b * h[1] + i * h[2] + n * h[3] + e) for b in range(batch) for i in range(length) for n in range(heads) for e in range(dim)]
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_rotary_overlaps_against_the_elements_themselves(seed):
+    rng = random.Random(seed)
+    seen = set()
+    for _ in range(300):
+        batch, length, heads, kv_heads, dim = rng.randint(1, 3), rng.randint(1, 4), rng.randint(1, 4), rng.randint(0, 2), rng.choice([2, 5, 8])
+        count = dict(q=heads, q_out=heads, k=kv_heads, k_out=kv_heads)
+
+        def strides(n):
+            order, at, out = rng.sample(range(3), 3), dim + rng.choice([0, 0, 3]), [0, 0, 0]
+            for i in order:
+                out[i] = at
+                at = max(1, at * (batch, length, n)[i] + rng.choice([0, 0, 0, 8, -1]))
+            return out
+        common = strides(heads + 2 * kv_heads)
+        given = {n: (AT + 2 * rng.randint(0, 700), *(common if rng.random() < 0.7 else strides(count[n]))) for n in count}
+        for n in ("q", "k"):
+            if rng.random() < 0.3:
+                given[n + "_out"] = given[n]
+        e = {n: of_heads(h, batch, length, count[n], dim) for n, h in given.items()}
+        sets = {n: set(v) for n, v in e.items()}
+
+        def same(a, b):
+            return given[a][0] == given[b][0] and all(extent == 1 or x == y for extent, x, y in
+                                                      zip((batch, length, count[a]), given[a][1:], given[b][1:]))
+        bad = any(len(e[n]) != len(sets[n]) for n in ("q_out", "k_out")) or \
+            any(sets[a] & sets[b] for a, b in (("q_out", "k"), ("q_out", "k_out"), ("k_out", "q"))) or \
+            any(sets[n] & sets[n + "_out"] and not same(n, n + "_out") for n in ("q", "k"))
+        got = answer(t.rotary, batch=batch, len=length, heads=heads, kv_heads=kv_heads, dim=dim, rotary_dim=2, **given)
+        assert got == (ps.E_RANGE if bad else TAKEN), (batch, length, heads, kv_heads, dim, given)
+        seen.add(got)
+    assert seen == {ps.E_RANGE, TAKEN}
