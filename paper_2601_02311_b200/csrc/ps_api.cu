@@ -909,11 +909,6 @@ static int take_optional(const ps_matrix* m, u64 rows, u64 cols, u64 width, u64 
   into.data = nullptr, into.stride = 0;
   return m ? take_matrix(m, rows, cols, width, step, into) : PS_OK;
 }
-// whether writing y is in the way of reading x, which may be the very same elements
-static bool spoils(const ps_matrix& y, const ps_matrix& x, u64 rows, u64 cols, u64 width) {
-  return x.data && overwrites(y.data, y.stride, x.data, x.stride, rows, cols, width);
-}
-
 static int norm_args(const ps_layer_norm_desc& d, NormArgs& a) {
   if (d.rows > 0x7fffffffu || d.cols < 1 || d.cols > ((u64)1 << 20) || !(d.eps >= 0) || !std::isfinite((float)d.eps) || d.dtype > PS_F16 ||
       d.grad_dtype > PS_F16 || d.accumulate > 1)
@@ -934,7 +929,11 @@ int ps_layer_norm_forward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps_
   if ((rc = take_matrix(x, a.rows, a.cols, width, 1, a.x)) != PS_OK || (rc = take_matrix(y, a.rows, a.cols, width, 1, a.y)) != PS_OK) return rc;
   if (!aligned(d_weight, width) || !aligned(d_bias, width) || !aligned(d_mean, 4) || !aligned(d_rstd, 4)) return PS_E_ALIGN;
   if (a.rows == 0) return PS_OK;
-  if (spoils(a.y, a.x, a.rows, a.cols, width)) return PS_E_RANGE;
+  const Region x_at(a.x, a.rows, a.cols, width), y_at(a.y, a.rows, a.cols, width), w_at(d_weight, a.cols, width), b_at(d_bias, a.cols, width),
+      mean_at(d_mean, a.rows, 4), rstd_at(d_rstd, a.rows, 4);
+  if ((!same_rows(a.y, a.x, a.rows) && meet(y_at, x_at)) || meets(y_at, {w_at, b_at, mean_at, rstd_at}) || meets(mean_at, {x_at, w_at, b_at, rstd_at}) ||
+      meets(rstd_at, {x_at, w_at, b_at}))
+    return PS_E_RANGE;
   if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return PS_E_CUDA;
@@ -967,9 +966,12 @@ int ps_layer_norm_backward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps
       !aligned(d_bias_grad, grad_width) || !aligned(d_work, 256))
     return PS_E_ALIGN;
   if (work_bytes < need) return PS_E_RANGE;
-  if (a.rows && (spoils(a.d_x, a.d_y, a.rows, a.cols, width) || spoils(a.d_x, a.x, a.rows, a.cols, width) ||
-                 spoils(a.d_x, a.residual, a.rows, a.cols, width)))
-    return PS_E_RANGE;
+  // (the gradients of weight and bias are written when everything else has been read)
+  const auto rows_at = [&](const ps_matrix& m) { return Region(m, a.rows, a.cols, width); };
+  const Region dx_at = rows_at(a.d_x), dw_at(d_weight_grad, a.cols, grad_width), db_at(d_bias_grad, a.cols, grad_width);
+  for (const ps_matrix* m : {&a.d_y, &a.x, &a.residual})
+    if (!same_rows(a.d_x, *m, a.rows) && meet(dx_at, rows_at(*m))) return PS_E_RANGE;
+  if (meets(dx_at, {Region(d_weight, a.cols, width), Region(d_mean, a.rows, 4), Region(d_rstd, a.rows, 4), dw_at, db_at}) || meet(dw_at, db_at)) return PS_E_RANGE;
   if (a.rows == 0 && !sums) return PS_OK;
   if ((rc = pending_device_error(ctx)) != PS_OK) return rc;
   DeviceGuard guard(ctx->device);

@@ -160,3 +160,34 @@ def test_rotary_overlaps_against_the_elements_themselves(seed):
         assert got == (ps.E_RANGE if bad else TAKEN), (batch, length, heads, kv_heads, dim, given)
         seen.add(got)
     assert seen == {ps.E_RANGE, TAKEN}
+
+
+# x AT (128 bytes), y AT + 1024, weight AT + 2048 (32), bias AT + 2304, mean AT + 2560 (16), rstd AT + 2816
+@pytest.mark.parametrize("change", [
+    dict(y=(AT + 4, None)), dict(y=(AT - 124, None)), dict(y=(AT, 16)), dict(y=(AT + 2048 + 28, None)), dict(y=(AT + 2304, None)), dict(y=(AT + 2560 - 124, None)),
+    dict(y=(AT + 2816, None)), dict(mean=AT + 124), dict(mean=AT + 2048), dict(mean=AT + 2304 + 28), dict(mean=AT + 2816 - 12), dict(rstd=AT),
+    dict(rstd=AT + 2048 + 28), dict(rstd=AT + 2304 - 12)])
+def test_norm_refuses_results_over_operands(change):
+    assert answer(t.norm, **change) == ps.E_RANGE
+
+
+@pytest.mark.parametrize("change", [
+    dict(), dict(y=(AT, None)), dict(y=(AT + 128, None)), dict(x=(AT, 32), y=(AT + 32, 32)), dict(x=(AT + 32, 32), y=(AT, 32)), dict(mean=AT + 128),
+    dict(mean=AT + 2816 - 16), dict(weight=AT + 2304), dict(x=(AT, 16), mean=None, rstd=None)])
+def test_norm_takes_results_beside_operands(change):
+    assert answer(t.norm, **change) == TAKEN
+
+
+# d_y AT (128 bytes), x AT + 1024, residual AT + 2048, d_x AT + 3328, weight AT + 4096 (32), mean AT + 4352 (16), rstd AT + 4608, d_weight AT + 5120, d_bias AT + 5376
+@pytest.mark.parametrize("change", [
+    dict(d_x=(AT + 4, None)), dict(d_x=(AT + 1024 + 124, None)), dict(d_x=(AT + 2048 - 4, None)), dict(d_x=(AT + 4096 + 28, None)), dict(d_x=(AT + 4352, None)),
+    dict(d_x=(AT + 4608 - 124, None)), dict(d_x=(AT + 5120, None)), dict(d_x=(AT + 5376 + 28, None)), dict(d_weight=AT + 5376 - 28), dict(d_bias=AT + 5120)])
+def test_norm_gradients_refuse_results_over_operands(change):
+    assert answer(t.norm_grad, **change) == ps.E_RANGE
+
+
+@pytest.mark.parametrize("change", [
+    dict(), dict(d_x=(AT, None)), dict(d_x=(AT + 1024, None)), dict(d_x=(AT + 2048, None)), dict(d_x=(AT + 2048, None), residual=None),
+    dict(d_y=(AT, 32), d_x=(AT + 32, 32)), dict(d_weight=AT + 5376 - 32), dict(d_weight=AT + 4096)])
+def test_norm_gradients_take_results_beside_operands(change):
+    assert answer(t.norm_grad, **change) == TAKEN
