@@ -89,3 +89,34 @@ def test_norm_work_of_the_named_size(ctx, rows, cols):
     ctx.layer_norm_backward_into(d_y, x, mean, rstd, got[0], None, d_y, *got[1:], work=whole[256:256 + size])
     ctx.check_status()
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and whole[:256].eq(77).all() and whole[256 + size:].eq(77).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_gelu_keeps_its_digits_far_out(ctx, dtype):
+    """gelu and its slope against bounds relative to the results themselves, which are small on the negative side."""
+    t = TYPES[dtype]
+    v = torch.cat((torch.linspace(-13, 13, 1000), torch.tensor([-4.01, -6.0, -8.0, -3.0, -9.0, -0.75, 1e-3, -1e-3]))).cuda().to(t)
+    n = v.numel()
+    x = torch.zeros(n, 8, device="cuda", dtype=t)
+    x[:, 0] = v
+    one = torch.zeros(8, 8, device="cuda", dtype=t)
+    one[:, 0] = 1
+    y = ctx.linear_forward(x, one, activation="gelu")[:, 0]
+    e = v.double()
+    square = e.square() / 2
+    tail, density = torch.erfc(e.abs() * math.sqrt(0.5)) / 2, (-square).exp() / math.sqrt(2 * math.pi)
+    # the exponential: 2 units of 2 F, and three roundings of its argument, of F each; the polynomial 1.2e-6 = 20 F of the value and 2 F of its quotient; two
+    # products.  Results below 2^-126 are 0
+    exp_err = F * (4 + 3.4 * square)
+    tail_err = tail * (exp_err + 24 * F) + 2.0 ** -126
+    share = torch.where(e < 0, tail, 1 - tail)
+    within(y, e * share, e.abs() * tail_err + 2 * F * (e * share).abs() + u_of(t) * (e * share).abs() + tiny_of(t), "gelu")
+    pre = torch.zeros(4, n, device="cuda", dtype=t)
+    pre[0] = v
+    unit = torch.zeros_like(pre)
+    unit[0] = 1
+    slope = torch.empty(n, device="cuda")
+    ctx.linear_backward_into(unit, None, None, d_bias=slope, pre=pre, activation="gelu")
+    ctx.check_status()
+    want = share + e * density
+    within(slope, want, tail_err + (e * density).abs() * (exp_err + 4 * F) + 2 * F * (want.abs() + share), "slope")
