@@ -84,8 +84,8 @@ constexpr float LOG2_E = 1.44269504f, TANH_FACTOR = 0.79788456f, TANH_CUBE = 0.0
 // Phi(v), and e^(-v^2 / 2) on the way.  Phi(-|v|) = e^(-v^2 / 2) P(t), t = 1 / (1 + 0.34 |v|): P is a polynomial fitted to the quotient itself (least squares over
 // 0 <= |v| <= 14, reweighted until the largest error stood still, with up to 11 times the relative error where the value is small).  In floats it is off by
 // 1.8e-7 beside 1, and by 1.2e-6 of the value on the far side: a formula whose error is small beside 1 alone loses its digits there (one of 1.5e-7 had
-// gelu(-6) wrong by 0.4 %).  Every instruction counts: 2048 tokens, 1024 to 4096 columns, take 24.9 us, and 26.8 with __expf, which brings its argument into
-// range first, in place of the instruction.
+// gelu(-6) wrong by 0.4 %).  Every instruction counts: 2048 tokens, 1024 to 4096 columns, take 24.9 us, and 26.8 with __expf in place
+// of the instruction.
 __device__ __forceinline__ float normal_share(float v, float& e) {
   const float t = reciprocal(fmaf(fabsf(v), 0.34f, 1.f));
   e = exp2_fast(v * v * (-0.5f * LOG2_E));

@@ -4,7 +4,8 @@
 //   g = dY w;  xn = (x - mean) rstd;  dX = rstd (g - <g> - xn <g xn>) + residual;  dW = sum_r dY xn;  dB = sum_r dY
 //
 // with < > the mean over a row.  A row is read once and stays in registers: its mean first, then the sum of squared
-// distances from it, so that a large mean costs no digits.  Bytes bound both passes; dW and dB are summed in the
+// distances from it, so that a large mean costs no digits.  (Nor do the mean's own roundings where it is far larger than the distances: see
+// SUMS_ROUND.)  Bytes bound both passes; dW and dB are summed in the
 // registers of the threads that own the columns while the rows pass, so that the backward pass reads each matrix once.
 //
 // Which thread has which columns depends on the width alone: packs of 16 bytes where the width is a multiple of one (read element by
@@ -16,6 +17,7 @@
 // the backward pass took 1050 us.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 #include "ps_columns.cuh"
 #include "ps_tensor.cuh"
 
@@ -302,6 +304,23 @@ struct Wide {           // which rows begin at multiples of 16 bytes
   bool x, y, d_y, residual, d_x, weight, bias;
 };
 
+// s / n to the last place: the product with 1 / n, and what that leaves of s
+__device__ __forceinline__ float quotient(float s, float n, float share) {
+  const float q = s * share;
+  return fmaf(fmaf(-q, n, s), share, q);
+}
+// Where the distances are far smaller than the mean itself, a mean that is off by a few units of its last place shows in them; equal numbers would have distances at
+// all.  The quotient does not do that, but rounded sums do.  Sums of 16-bit numbers of one size are exact while their digits and the columns' together are 24, in
+// other kernels another walk over such a row (out of the L2) finds the mean of the distances, which is what the mean is off by.  (With it 65536 x 8192 of
+// bfloat16 took 439 us instead of 380 although no row needed it, for want of registers.)  All threads of a row have the same two numbers.
+template <class T> constexpr u32 LARGEST_SUM = sizeof(T) == 4 ? 1 : std::is_same<T, __half>::value ? 1 << 13 : 1 << 16;
+template <class T, u32 COLUMNS> constexpr bool SUMS_ROUND = COLUMNS > LARGEST_SUM<T>;
+__device__ __forceinline__ bool far_from_zero(float mean, float variance) { return mean * mean > 16.f * variance; }
+// the mean square distance, out of that from a mean that is `off`
+__device__ __forceinline__ float less_square(float variance, float off) {
+  const float v = fmaf(-off, off, variance);
+  return v < 0.f ? 0.f : v;                     // (NaN stays)
+}
 // sqrt's reciprocal, the fast function's (off by up to 2 units) improved by a Newton step
 __device__ __forceinline__ float reciprocal_root(float v) {
   const float y = rsqrtf(v), half = 0.5f * v;
@@ -337,7 +356,7 @@ template <class T, int E> constexpr bool HELD = E * sizeof(T) <= 32;
 // A block has a row at a time, a thread E elements of it; a warp beside them brings the rows to come.
 // (At 16 bits a walk over the elements is issue slots as much as it is bytes: floats are taken two at a time, which took 65536 x 8192 from 545 us to 441.)
 template <class T, int R, int E, bool PACKED, bool SHARED>
-__global__ void __launch_bounds__(R + 32, forward_blocks(R, E * sizeof(T))) k_norm(const NormArgs args, const Wide wide, Ring ring, float share, u32 each) {
+__global__ void __launch_bounds__(R + 32, forward_blocks(R, E * sizeof(T))) k_norm(const NormArgs args, const Wide wide, Ring ring, float count, float share, u32 each) {
   extern __shared__ unsigned char rows[];
   __shared__ float slots[SHARED ? ClusterSum<R, 1>::SLOTS : 2 * R / 32];
   __shared__ u64 bars[2 * RING_MOST + 2];
@@ -383,8 +402,8 @@ __global__ void __launch_bounds__(R + 32, forward_blocks(R, E * sizeof(T))) k_no
     ring.leave(stage, parity);
     s[0] = together(add2(part[0], part[1]));
     sum.over(s);
-    const float mean = s[0] * share;
-    const u64 less = twice(-mean);
+    float mean = quotient(s[0], count, share);
+    u64 less = twice(-mean);
     part[0] = part[1] = 0;
     x.forget();
 #pragma unroll
@@ -400,7 +419,17 @@ __global__ void __launch_bounds__(R + 32, forward_blocks(R, E * sizeof(T))) k_no
     }
     s[0] = together(add2(part[0], part[1]));
     sum.over(s);
-    const float rstd = reciprocal_root(fmaf(s[0], share, a.eps));
+    float square = s[0] * share;
+    if (SUMS_ROUND<T, (SHARED ? CLUSTER_MOST : 1) * R * E> && far_from_zero(mean, square)) {
+      const T* const again = (const T*)a.x.data + r * a.x.stride;      // (not written before all threads have the sum)
+      s[0] = 0.f;
+#pragma unroll 1
+      for (u32 c = threadIdx.x; c < cols; c += R) s[0] += widen(again[c]) - mean;
+      sum.over(s);
+      const float off = s[0] * share;
+      mean += off, less = twice(-mean), square = less_square(square, off);
+    }
+    const float rstd = reciprocal_root(square + a.eps);
     const u64 by = twice(rstd);
     x.forget();
 #pragma unroll
@@ -434,7 +463,7 @@ __device__ __forceinline__ float lanes_sum(float v, u32 lanes) {
   return v;
 }
 template <class T>
-__global__ void __launch_bounds__(256, NARROW_BLOCKS) k_norm_narrow(const NormArgs a, u32 lanes, float share) {
+__global__ void __launch_bounds__(256, NARROW_BLOCKS) k_norm_narrow(const NormArgs a, u32 lanes, float count, float share) {
   const u32 lane = threadIdx.x % lanes, cols = (u32)a.cols, at_once = 256 / lanes;
   float w[NARROW_E], b[NARROW_E];
 #pragma unroll
@@ -454,14 +483,25 @@ __global__ void __launch_bounds__(256, NARROW_BLOCKS) k_norm_narrow(const NormAr
       v[e] = there && c < cols ? widen(((const T*)a.x.data)[r * a.x.stride + c]) : 0.f;
       sum += v[e];
     }
-    const float mean = lanes_sum(sum, lanes) * share;
+    float mean = quotient(lanes_sum(sum, lanes), count, share);
     sum = 0.f;
 #pragma unroll
     for (int e = 0; e < NARROW_E; ++e) {
       v[e] = e * lanes + lane < cols ? v[e] - mean : 0.f;
       sum = fmaf(v[e], v[e], sum);
     }
-    const float rstd = reciprocal_root(fmaf(lanes_sum(sum, lanes), share, a.eps));
+    float square = lanes_sum(sum, lanes) * share;
+    const bool far = SUMS_ROUND<T, NARROW> && far_from_zero(mean, square);
+    if (__any_sync(0xffffffffu, far)) {           // (the lanes meet in the sum, which is for the rows that need it)
+      sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < NARROW_E; ++e) sum += v[e];
+      const float off = lanes_sum(sum, lanes) * share, moved = far ? mean + off - mean : 0.f;
+      square = far ? less_square(square, off) : square, mean += moved;
+#pragma unroll
+      for (int e = 0; e < NARROW_E; ++e) v[e] -= moved;
+    }
+    const float rstd = reciprocal_root(square + a.eps);
     if (!there) continue;
 #pragma unroll
     for (int e = 0; e < NARROW_E; ++e) {
@@ -550,14 +590,22 @@ __global__ void __launch_bounds__(LONG) k_norm_long(const NormArgs a) {
     float s[1] = {0.f};
     for (u32 c = threadIdx.x; c < a.cols; c += LONG) s[0] += widen(x[c]);
     sum.over(s);
-    const float mean = s[0] / (float)a.cols;
+    float mean = s[0] / (float)a.cols;
     s[0] = 0.f;
     for (u32 c = threadIdx.x; c < a.cols; c += LONG) {
       const float d = widen(x[c]) - mean;
       s[0] = fmaf(d, d, s[0]);
     }
     sum.over(s);
-    const float rstd = 1.f / sqrtf(s[0] / (float)a.cols + a.eps);
+    float square = s[0] / (float)a.cols;
+    if (far_from_zero(mean, square)) {
+      s[0] = 0.f;
+      for (u32 c = threadIdx.x; c < a.cols; c += LONG) s[0] += widen(x[c]) - mean;
+      sum.over(s);
+      const float off = s[0] / (float)a.cols;
+      mean += off, square = less_square(square, off);
+    }
+    const float rstd = 1.f / sqrtf(square + a.eps);
     for (u32 c = threadIdx.x; c < a.cols; c += LONG) {
       const float w = a.weight ? widen(((const T*)a.weight)[c]) : 1.f, b = a.bias ? widen(((const T*)a.bias)[c]) : 0.f;
       y[c] = narrow<T>((widen(x[c]) - mean) * (rstd * w) + b);
@@ -801,13 +849,13 @@ cudaError_t forward(const NormArgs& a, const Wide& wide, const Sharing& sharing,
   const cudaError_t e = Prepared<kernel>::smem(l.smem);
   if (e != cudaSuccess) return e;
   const u64 groups = std::min<u64>(a.rows, (u64)(SHARED ? (int)sharing.clusters : sm_count) * l.resident);
-  return launch_cluster(kernel, (u32)groups * sharing.blocks, sharing.blocks, R + 32, l.smem, stream, a, wide, l.ring, 1.f / (float)a.cols, sharing.each);
+  return launch_cluster(kernel, (u32)groups * sharing.blocks, sharing.blocks, R + 32, l.smem, stream, a, wide, l.ring, (float)a.cols, 1.f / (float)a.cols, sharing.each);
 }
 template <class T, bool PACKED>
 cudaError_t forward(const NormArgs& a, const Wide& wide, int sm_count, cudaStream_t stream) {
   if (a.cols <= NARROW) {
     const u32 lanes = narrow_lanes(a.cols), at_once = 256 / lanes;
-    k_norm_narrow<T><<<blocks_for((a.rows + at_once - 1) / at_once, NARROW_BLOCKS, sm_count), 256, 0, stream>>>(a, lanes, 1.f / (float)a.cols);
+    k_norm_narrow<T><<<blocks_for((a.rows + at_once - 1) / at_once, NARROW_BLOCKS, sm_count), 256, 0, stream>>>(a, lanes, (float)a.cols, 1.f / (float)a.cols);
     return cudaGetLastError();
   }
   constexpr u32 MOST = 65536 / sizeof(T);

@@ -120,3 +120,43 @@ def test_gelu_keeps_its_digits_far_out(ctx, dtype):
     ctx.check_status()
     want = share + e * density
     within(slope, want, tail_err + (e * density).abs() * (exp_err + 4 * F) + 2 * F * (want.abs() + share), "slope")
+
+
+SPREADS = [3, 7, 60, 250, 300, 1000, 1155, 2056, 5003, 9001, 12000, 16392, 20000, 33000, 70001]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", SPREADS)
+def test_rows_of_one_number(ctx, dtype, cols):
+    """Equal numbers are their own mean, whatever the sums' and the quotient's roundings: what comes out is the bias, bit by bit."""
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(cols)
+    values = torch.tensor([0.0, 7.1, -100.0, 100.1, 12345.0, 1e4, -3e4, 0.3, 1e-3, 77777.0 if dtype != "f16" else 65504.0], device="cuda").to(t)
+    x = values[:, None].expand(-1, cols).contiguous()
+    weight, bias = normal(gen, cols, dtype=t), normal(gen, cols, dtype=t)
+    y, mean, rstd = ctx.layer_norm_forward(x, weight, bias)
+    ctx.check_status()
+    assert torch.equal(y, bias.expand_as(y)) and torch.equal(mean, values.float())
+    # the first mean is off by at most depth + 2 roundings; of that square the sums and products leave 6 F
+    depth = max(32, -(-cols // 1024)) + 12
+    within(rstd, torch.full_like(mean, 1e-5).double().rsqrt(), 10 ** 2.5 * (5 * F + 3 * F * (depth * F * values.double()) ** 2 / 1e-5))
+
+
+@pytest.mark.parametrize("cols", SPREADS)
+def test_rows_far_from_zero(ctx, cols):
+    """Of a mean far above the spread only its last rounding is lost."""
+    gen = torch.Generator("cuda").manual_seed(cols)
+    x = torch.randint(-8, 9, (5, cols), device="cuda", generator=gen).float() + 12345.0
+    y, m, rstd = ctx.layer_norm_forward(x)
+    ctx.check_status()
+    e = x.double()
+    mean = e.mean(1, keepdim=True)
+    apart, var = e - mean, e.var(1, keepdim=True, unbiased=False)
+    root = (var + 1e-5).rsqrt()
+    d = max(32, -(-cols // 1024)) + 12
+    # the first mean is off by d F of it; distances from it are whole multiples of its unit and exact; their sum, the share and the second mean
+    first = d * F * mean
+    mean_err = F * mean + (d + 2) * F * (apart.abs().mean(1, keepdim=True) + first)
+    root_err = root * (((d + 6) * F * (var + first ** 2) + mean_err ** 2) / (var + 1e-5) / 2 + 4 * F)
+    within(m[:, None], mean, mean_err)
+    within(rstd[:, None], root, root_err + F * root)
+    within(y, apart * root, apart.abs() * (root_err + 4 * F * root) + mean_err * (root + root_err) + 2 * F * (apart * root).abs())
