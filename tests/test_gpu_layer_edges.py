@@ -160,3 +160,42 @@ def test_rows_far_from_zero(ctx, cols):
     within(m[:, None], mean, mean_err)
     within(rstd[:, None], root, root_err + F * root)
     within(y, apart * root, apart.abs() * (root_err + 4 * F * root) + mean_err * (root + root_err) + 2 * F * (apart * root).abs())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("activation", [None, "gelu"])
+def test_long_sums_are_taken_in_short_ones(ctx, dtype, activation):
+    """A gradient in 32 bits whose tiles each have a sum over all tokens, of positive terms: its mean error is that of 1536 tokens at a time."""
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(6)
+    tokens, inputs, outputs = 40000, 1600, 1536                      # (156 tiles of 128 x 128: the sum is not cut into parts)
+    x, d_y = normal(gen, tokens, inputs, dtype=t).abs_(), normal(gen, tokens, outputs, dtype=t).abs_()
+    pre = None if activation is None else normal(gen, tokens, outputs, dtype=t).abs_()
+    d_w = torch.empty(outputs, inputs, device="cuda")
+    ctx.linear_backward_into(d_y, x, None, d_weight=d_w, pre=pre, activation=activation)
+    ctx.check_status()
+    d_pre, err = d_y.double(), torch.zeros((), device="cuda", dtype=torch.float64)
+    if activation:
+        v = pre.double()
+        square = v.square() / 2
+        tail, density, exp_err = torch.erfc(v * math.sqrt(0.5)) / 2, (-square).exp() / math.sqrt(2 * math.pi), F * (4 + 3.4 * square)
+        # the slope as in test_gelu_keeps_its_digits_far_out, and the product with it
+        err = d_pre * (tail * (exp_err + 24 * F) + v * density * (exp_err + 4 * F) + 2 * F * (2 - 2 * tail + v * density))
+        d_pre = d_pre * (1 - tail + v * density)
+        err = (err + F * d_pre).t() @ x.double()
+        del v, square, tail, density, exp_err
+    want = d_pre.t() @ x.double()
+    off = (d_w.double() - want) / want
+    # A step of 16 products adds them to the sum with each cut off at a quarter of a unit of the sum's last place, and the whole at a unit (products of 2^-13 and 2^-14
+    # beside 2^11 are seen in whole sums of 15 or 16, those of 2^-15 not).  So it loses up to 16 / 4 + 1 = 5 units, half of that on average.  A unit is 2 F of
+    # the sum at most.  Of a sum that grows evenly to T it is, on average over the way, (r - 2/3) / r^2 times 2 F T with r = T / 2^floor(log2 T), which is
+    # 3/8 at most, at r = 4/3.  24 steps of the kernel are 96 of these: 96 * 2.5 * 0.75 F = 180 F on average, 96 * 5 F = 480 F for one that always loses
+    # most (its units add up to half of 96 * 2 F).  A twentieth more, since the sums do not grow quite evenly.  The 27 sums of 1536 tokens are rounded to nearest: 14 F.
+    # (With 64 steps at a time half precision lost 380 F on average, bfloat16, whose products are shorter, 150.)
+    mean, most = 1.05 * 180 * F, 1.05 * 480 * F + 14 * F
+    assert off.mean().abs() <= mean + (err / want).mean()
+    # of dPre in two parts, a rounding of a rounding
+    parts = 0.0 if activation is None else u_of(t) ** 2 + tiny_of(t) / 4096
+    within(d_w, want, (most + parts) * want + err)
+    # All entries lose alike, but for their sums' own sizes, a tenth of it; the parts' roundings vanish in so many terms, and 27 of the sums are 2 F.  One part alone
+    # would spread by 2^-8 / sqrt(3 * 40000) in bfloat16, 190 F, in half precision by 24 F.
+    assert off.std() <= 0.1 * 180 * F + 2 * F
