@@ -141,20 +141,6 @@ __device__ __forceinline__ void times_slope(u32 activation, float (&v)[N], const
 }
 
 // ---- a pair's instructions
-__device__ __forceinline__ u32 rank_in_pair() {
-  u32 r;
-  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void pair_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ bool passed_in_pair(u32 bar, u32 parity) {
-  u32 ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
 __device__ __forceinline__ void arrive_at_leader(u32 bar) {
   asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
 }
@@ -172,18 +158,6 @@ __device__ __forceinline__ void multiply_scaled(u32 d, u32 a, u32 b, u32 ins) {
         "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.eq.u32 p, 0, 0;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p, %5;\n\t}"
         ::"r"(d), "r"(a), "r"(b), "r"(ins), "r"(DESC_HIGH), "n"(LOW_SHIFT) : "memory");
-}
-template <bool PAIR>
-__device__ __forceinline__ void wait_for(Waiter& w, u32 bar, u32 parity) {
-  if (!PAIR) return w.wait(bar, parity);
-  if (w.dead || passed_in_pair(bar, parity)) return;
-  const u64 begin = now_ns();
-  while (!passed_in_pair(bar, parity))
-    if (now_ns() - begin > PATIENCE_NS) {
-      w.dead = true;
-      report(w.status, ST_TIMEOUT);
-      return;
-    }
 }
 
 // ---- copies of a box of two or three dimensions
@@ -400,7 +374,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
   const u32 wanted = bars + 256 + 16 * TILES_AHEAD;         // a tile's copies are nearly done: the next one may be asked for
   __shared__ u32 tmem_at;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const u32 rank = PAIR ? rank_in_pair() : 0;
+  const u32 rank = PAIR ? cluster_rank() : 0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) barrier_init(full(s), 1), barrier_init(empty(s), 1);
@@ -413,7 +387,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
   if (warp == MMA_WARP) take_tmem<PAIR>(smem_address(&tmem_at), F::TMEM);
   fence_before();
   __syncthreads();
-  if (PAIR) pair_sync();
+  if (PAIR) cluster_sync();
   fence_after();
   const u32 tmem = tmem_at;
 
@@ -421,7 +395,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
   Waiter waiter(of_f.status);
   // a role's n-th answer: the tile to go on with, or none.  `speaks`: the thread that says that it has been read
   const auto next_tile = [&](u32 n, u32& t, bool speaks) {
-    wait_for<PAIR>(waiter, tile_full(n), (n / TILES_AHEAD) & 1);
+    waiter.template wait<PAIR>(tile_full(n), (n / TILES_AHEAD) & 1);
     u32 block = 0;
     const bool more = !waiter.dead && answered(answer(n), block);
     t = PAIR ? block / 2 : block;
@@ -449,7 +423,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
             for (u32 k = begin, end = min(begin + p.steps_at_once, last); k < end; ++k, ++turn) {
               if (left-- == ask && rank == 0) barrier_arrive(wanted);
               const int s = turn % STAGES;
-              wait_for<PAIR>(waiter, empty(s), (turn / STAGES + 1) & 1);
+              waiter.template wait<PAIR>(empty(s), (turn / STAGES + 1) & 1);
               if (waiter.dead) break;
               if (rank == 0) barrier_expect(full(s), (PAIR ? 2 : 1) * p.stage_bytes);
               const u32 a = ring + s * F::STAGE, b = a + F::A_BYTES;
@@ -474,7 +448,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
       while (!waiter.dead && next_tile(count++, t, true));
       if (rank == 0) {                              // leave no copy in flight, also where a wait has run out
         Waiter last(of_f.status);
-        for (u32 i = turn > STAGES ? turn - STAGES : 0; i < turn; ++i) wait_for<PAIR>(last, full(i % STAGES), (i / STAGES) & 1);
+        for (u32 i = turn > STAGES ? turn - STAGES : 0; i < turn; ++i) last.template wait<PAIR>(full(i % STAGES), (i / STAGES) & 1);
       }
     }
     __syncwarp();
@@ -487,13 +461,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
         const u32 part = tile_at(p, t).part, last = min((part + 1) * p.steps_each, p.steps);
         for (u32 begin = part * p.steps_each; begin < last && !waiter.dead; begin += p.steps_at_once, ++sums) {
           const u32 end = min(begin + p.steps_at_once, last), d = tmem + (sums & 1) * F::SUM;
-          wait_for<PAIR>(waiter, sum_empty(sums & 1), (sums / 2 + 1) & 1);
+          waiter.template wait<PAIR>(sum_empty(sums & 1), (sums / 2 + 1) & 1);
           fence_after();
 #pragma unroll 1
           for (int low = X::TWO ? 1 : 0; low >= 0; --low)
             for (u32 k = begin; k < end && !waiter.dead; ++k, ++turn) {
               const int s = turn % STAGES;
-              wait_for<PAIR>(waiter, full(s), (turn / STAGES) & 1);
+              waiter.template wait<PAIR>(full(s), (turn / STAGES) & 1);
               if (waiter.dead) break;
               fence_after();
               const u32 a = descriptor<X::A_ACROSS>(ring + s * F::STAGE), b = descriptor<X::B_ACROSS>(ring + s * F::STAGE + F::A_BYTES);
@@ -515,7 +489,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
     if (rank == 0 && elected()) {
       u32 t;
       for (u32 n = 0; !waiter.dead; ++n) {
-        wait_for<PAIR>(waiter, tile_empty(n), (n / TILES_AHEAD + 1) & 1);
+        waiter.template wait<PAIR>(tile_empty(n), (n / TILES_AHEAD + 1) & 1);
         waiter.wait(wanted, n & 1);
         if (waiter.dead) break;
         if (PAIR) expect_at(tile_full(n), 16, 0), expect_at(tile_full(n), 16, 1);
@@ -569,11 +543,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
           }
           __syncwarp();
           if (!waited) {
-            wait_for<PAIR>(waiter, sum_full(sums & 1), (sums / 2) & 1);
+            waiter.template wait<PAIR>(sum_full(sums & 1), (sums / 2) & 1);
             fence_after();
             waited = true;
           }
-          if (reads) wait_for<false>(waiter, input(warp), inputs++ & 1);
+          if (reads) waiter.wait(input(warp), inputs++ & 1);
           waiter.dead = __any_sync(0xffffffffu, waiter.dead);      // (the lanes go on together)
           if (waiter.dead) continue;
 #pragma unroll
@@ -629,7 +603,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
           }
         }
         if (!waited) {                                // (nothing of this tile is this warp's: it says so in turn all the same)
-          wait_for<PAIR>(waiter, sum_full(sums & 1), (sums / 2) & 1);
+          waiter.template wait<PAIR>(sum_full(sums & 1), (sums / 2) & 1);
           fence_after();
         }
         waiter.dead = __any_sync(0xffffffffu, waiter.dead);
@@ -656,7 +630,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
   }
   fence_before();
   __syncthreads();
-  if (PAIR) pair_sync();                            // neither block leaves while the other's products read its memory
+  if (PAIR) cluster_sync();                         // neither block leaves while the other's products read its memory
   fence_after();
   if (warp == MMA_WARP) leave_tmem<PAIR>(tmem, F::TMEM);
 }

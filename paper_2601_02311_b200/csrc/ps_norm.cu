@@ -58,25 +58,6 @@ struct RowSum {
 };
 
 // ---- Rows that are shared by the blocks of a cluster, each with a range of the columns: their sums go through one another's shared memory.
-__device__ __forceinline__ u32 cluster_rank() {
-  u32 r;
-  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ u32 cluster_size() {
-  u32 r;
-  asm volatile("mov.u32 %0, %cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ bool passed_in_cluster(u32 bar, u32 parity) {
-  u32 ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
 constexpr u32 CLUSTER_MOST = 8;
 // As RowSum, over the R threads of each of the cluster's blocks: every warp sends its sums to all blocks, and arrives at their barriers.  (With the block's sum
 // taken first, and sent by one warp, 8000 x 16384 backward took 315 us instead of 289.)
@@ -86,7 +67,7 @@ struct ClusterSum {
   u32 slots, bars, rank, size, uses;
   tensor::Waiter& waiter;
   __device__ __forceinline__ ClusterSum(const float* s, const u64* b, tensor::Waiter& w)
-      : slots(tensor::smem_address(s)), bars(tensor::smem_address(b)), rank(cluster_rank()), size(cluster_size()), uses(0), waiter(w) {}
+      : slots(tensor::smem_address(s)), bars(tensor::smem_address(b)), rank(tensor::cluster_rank()), size(tensor::cluster_size()), uses(0), waiter(w) {}
   __device__ __forceinline__ void over(float (&v)[COUNT]) {
     const u32 turn = uses & 1, parity = uses / 2 & 1, lane = threadIdx.x % 32, bar = bars + 8 * turn;
     ++uses;
@@ -102,15 +83,7 @@ struct ClusterSum {
                    ::"r"(bar), "r"(lane) : "memory");
     }
     __syncwarp();
-    if (!waiter.dead && !passed_in_cluster(bar, parity)) {
-      const u64 begin = tensor::now_ns();
-      while (!passed_in_cluster(bar, parity))
-        if (tensor::now_ns() - begin > tensor::PATIENCE_NS) {
-          waiter.dead = true;
-          report(waiter.status, ST_TIMEOUT);
-          break;
-        }
-    }
+    waiter.template wait<true>(bar, parity);
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
@@ -339,11 +312,11 @@ __device__ __forceinline__ void begin_sums(u64* bars, u32 arrivals) {
     tensor::fence_barrier_init();
   }
   __syncthreads();
-  cluster_sync();
+  tensor::cluster_sync();
 }
 __device__ __forceinline__ void end_sums() {
   __syncwarp();
-  cluster_sync();
+  tensor::cluster_sync();
 }
 
 // Blocks of an SM at most, by the threads of a row and a thread's bytes of it: about 1024 threads, or 512 where they hold sums as well.
@@ -363,7 +336,7 @@ __global__ void __launch_bounds__(R + 32, forward_blocks(R, E * sizeof(T))) k_no
   NormArgs a = args;
   u32 blocks = 1, begin = 0;                    // that share a row, and the columns' range
   if (SHARED) {
-    blocks = cluster_size(), begin = cluster_rank() * each;
+    blocks = tensor::cluster_size(), begin = tensor::cluster_rank() * each;
     a.cols = min((u64)each, args.cols - begin);
     for (ps_matrix* m : {&a.x, &a.y}) m->data = moved<T>(m->data, begin);
     a.weight = moved<T>(a.weight, begin), a.bias = moved<T>(a.bias, begin);
@@ -628,7 +601,7 @@ __global__ void __launch_bounds__(R + 32, backward_blocks(R)) k_norm_grad(const 
   NormArgs a = args;
   u32 blocks = 1, begin = 0;                    // that share a row, and the columns' range
   if (SHARED) {
-    blocks = cluster_size(), begin = cluster_rank() * each;
+    blocks = tensor::cluster_size(), begin = tensor::cluster_rank() * each;
     a.cols = min((u64)each, args.cols - begin);
     for (ps_matrix* m : {&a.x, &a.d_y, &a.residual, &a.d_x}) m->data = moved<T>(m->data, begin);
     a.weight = moved<T>(a.weight, begin);

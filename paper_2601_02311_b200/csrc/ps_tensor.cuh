@@ -41,14 +41,24 @@ __device__ __forceinline__ bool barrier_passed(u32 bar, u32 parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
+// ... and by threads of any block of a cluster
+__device__ __forceinline__ bool barrier_passed_in_cluster(u32 bar, u32 parity) {
+  u32 ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 struct Waiter {
   volatile u32* status;
   bool dead;
   __device__ __forceinline__ explicit Waiter(volatile u32* s) : status(s), dead(false) {}
+  // CLUSTER: what other blocks of the cluster did before they arrived is to be seen as well
+  template <bool CLUSTER = false>
   __device__ __forceinline__ void wait(u32 bar, u32 parity) {
-    if (dead || barrier_passed(bar, parity)) return;
+    const auto passed = [&] { return CLUSTER ? barrier_passed_in_cluster(bar, parity) : barrier_passed(bar, parity); };
+    if (dead || passed()) return;
     const u64 begin = now_ns();
-    while (!barrier_passed(bar, parity))
+    while (!passed())
       if (now_ns() - begin > PATIENCE_NS) {
         dead = true;
         report(status, ST_TIMEOUT);
@@ -56,6 +66,21 @@ struct Waiter {
       }
   }
 };
+
+// ---- clusters
+__device__ __forceinline__ u32 cluster_rank() {
+  u32 r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ u32 cluster_size() {
+  u32 r;
+  asm volatile("mov.u32 %0, %cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 // ---- copies
 __device__ __forceinline__ void fence_barrier_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
