@@ -461,9 +461,9 @@ int ps_verify_batch(ps_ctx* ctx, const ps_verify_shape* shape /* host */, const 
  * rounded once, to nearest even, except for the two matrices that attention multiplies
  * in its operands' type (see there).
  *
- * A call returns before its kernels have run.  Where a block of attention's waits for a copy or a product of
- * its own for two seconds, it gives up: the call's results are not to be used, and ps_status, which
- * waits for them, or the next call returns PS_E_DEVICE. */
+ * A call returns before its kernels have run.  Where a block of attention's, layer norm's or a linear layer's waits for a
+ * copy, a product or the blocks that share its row or tile for two seconds, it gives up: the call's results are not to
+ * be used, and ps_status, which waits for them, or the next call returns PS_E_DEVICE. */
 enum { PS_F32 = 0, PS_BF16 = 1, PS_F16 = 2 };
 
 /* Dropout, with an optional residual:
@@ -567,11 +567,12 @@ int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps
  * (the forward pass writes those that are not null).  `residual` (may be null) is the gradient that reaches x past the
  * normalised branch.  d_weight and d_bias, of type grad_dtype, are computed where they are not null, in an order that
  * depends on the sizes, and on whether there is a residual, alone; with accumulate they are added to what is there (rounded once).  A row's results depend on
- * that row alone.  y may be x; d_x may be d_y, x or residual (same pointer and stride).
+ * that row alone.  y may be x; d_x may be d_y, x or residual (same pointer and stride); any other overlap with what is still read
+ * is refused.  The mean is right to its last place or two, also where it is far larger than the distances from it.
  * d_work: ps_layer_norm_backward_bytes, used like ps_embed_backward's (0 without d_weight and d_bias). */
 typedef struct {
   void* data;                      /* a matrix [rows][cols] whose columns are contiguous  */
-  uint64_t stride;                 /* between rows, in elements; >= cols of several rows  */
+  uint64_t stride;                 /* between rows, in elements; >= cols, and rows * stride up to 2^40 bytes, of several rows */
 } ps_matrix;
 typedef struct {
   uint64_t rows, cols;             /* rows 0 .. 2^31 - 1; cols 1 .. 2^20                  */
@@ -599,7 +600,8 @@ int ps_layer_norm_backward(ps_ctx* ctx, const ps_layer_norm_desc* desc, const ps
  * 2^-65 of a turn gives position p an error of p 2^-65 (and double's of f_i, p f_i 2^-52 at most).
  * d_positions: null (token i of a sequence has position i), or integers, [batch] of `position_stride` apart
  * (0: the same for all).  A shard of the sequence passes `first`.  q_out may be q, k_out k (same pointer and strides).
- * k and k_out may be null (kv_heads 0). */
+ * k and k_out may be null (kv_heads 0).  Other overlaps with what is read, of q_out and k_out, and of a result's own heads and
+ * tokens, are refused. */
 typedef struct {
   uint32_t batch;                  /* 0 .. 2^16 - 1; batch * len * (heads + kv_heads) <= 2^38 */
   uint32_t len;                    /* 0 .. 2^24                                           */
@@ -629,20 +631,23 @@ int ps_rotary(ps_ctx* ctx, const ps_rotary_desc* desc, const ps_heads* q, const 
  * the gradient of that, and the layer below is given no activation of its own.  Null results are not computed.
  * d_weight and d_bias, of the type or float (grad_dtype), are added to what is there with accumulate (rounded once).
  *
- * Products run on the tensor cores with sums of 32 bits, which they cut off rather than round; a gradient of type float is
- * summed 1536 tokens at a time, so that this does not add up, and of d_pre it takes what the rounding left as well.
+ * Products run on the tensor cores with sums of 32 bits, which they cut off rather than round (each product at a quarter of a
+ * unit of the sum's last place); a gradient of type float is summed 1536 tokens at a time, so that this does not add up, and of
+ * d_pre it takes what the rounding left as well, rounded to the type again: bfloat16 holds 16 bits of it, half 22.  Of the gradient's norm it is off by
+ * 1.5e-6 (bfloat16, without an activation) to 3e-6 (with one of its own), half by 1.8e-6; of terms of one sign alone by 3.1e-6 and 8.2e-6.
  * A row of y or d_x depends on that row, weight and the widths alone, not on how many rows or columns the call has; so
  * shards of tokens, and shards of outputs, compute the single device's bits.
  * d_weight's sum over tokens has an order that depends on the sizes alone.
  * Matrices begin at multiples of 16 bytes and have strides that are multiples of 16 bytes; bias any alignment of its type.
  * Widths need not be multiples of anything.  What lies behind a row's last element is not used.
- * residual may be y (forward) or d_x (backward) itself: same pointer and stride.
+ * residual may be y (forward) or d_x (backward) itself, and d_x may be below: same pointer and stride.  Other overlaps of results with what is still
+ * read, or with one another, are refused.
  * d_work: ps_linear_backward_bytes, 256-byte aligned, used like ps_embed_backward's (may be 0). */
 enum { PS_ACT_NONE = 0, PS_ACT_RELU = 1, PS_ACT_GELU = 2 /* v Phi(v) */,
        PS_ACT_GELU_TANH = 3 /* v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2 */, PS_ACT_SILU = 4 /* v / (1 + e^-v) */ };
 typedef struct {
   uint64_t tokens;                 /* 0 .. 2^30                                           */
-  uint64_t inputs, outputs;        /* 1 .. 2^24                                           */
+  uint64_t inputs, outputs;        /* 1 .. 2^24; tokens times either up to 2^39, inputs * outputs up to 2^38 */
   uint32_t dtype;                  /* PS_BF16 or PS_F16                                   */
   uint32_t grad_dtype;             /* backward: of d_weight and d_bias: dtype or PS_F32   */
   uint32_t activation;             /* PS_ACT_*                                            */

@@ -136,6 +136,9 @@ def test_rows_of_one_number(ctx, dtype, cols):
     y, mean, rstd = ctx.layer_norm_forward(x, weight, bias)
     ctx.check_status()
     assert torch.equal(y, bias.expand_as(y)) and torch.equal(mean, values.float())
+    in_place = x.clone()
+    ctx.layer_norm_forward_into(in_place, in_place, weight, bias)
+    assert torch.equal(in_place, y)
     # the first mean is off by at most depth + 2 roundings; of that square the sums and products leave 6 F
     depth = max(32, -(-cols // 1024)) + 12
     within(rstd, torch.full_like(mean, 1e-5).double().rsqrt(), 10 ** 2.5 * (5 * F + 3 * F * (depth * F * values.double()) ** 2 / 1e-5))
@@ -148,6 +151,11 @@ def test_rows_far_from_zero(ctx, cols):
     x = torch.randint(-8, 9, (5, cols), device="cuda", generator=gen).float() + 12345.0
     y, m, rstd = ctx.layer_norm_forward(x)
     ctx.check_status()
+    in_place = x.clone()
+    ctx.layer_norm_forward_into(in_place, in_place)
+    part = ctx.layer_norm_forward(torch.cat((x[3:], torch.zeros_like(x))))[0]          # beside rows that are not far
+    ctx.check_status()
+    assert torch.equal(in_place, y) and torch.equal(part[:2], y[3:])
     e = x.double()
     mean = e.mean(1, keepdim=True)
     apart, var = e - mean, e.var(1, keepdim=True, unbiased=False)
@@ -199,3 +207,18 @@ def test_long_sums_are_taken_in_short_ones(ctx, dtype, activation):
     # All entries lose alike, but for their sums' own sizes, a tenth of it; the parts' roundings vanish in so many terms, and 27 of the sums are 2 F.  One part alone
     # would spread by 2^-8 / sqrt(3 * 40000) in bfloat16, 190 F, in half precision by 24 F.
     assert off.std() <= 0.1 * 180 * F + 2 * F
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("width", [64, 333, 1000])
+def test_input_gradient_in_place_of_the_values_below(ctx, dtype, width):
+    """d_x may be `below` itself, alone and with a residual."""
+    t, gen = TYPES[dtype], torch.Generator("cuda").manual_seed(width)
+    d_y, w = whole_numbers(gen, 3000, 72, t), whole_numbers(gen, 72, width, t)
+    below, res = whole_numbers(gen, 3000, width, t), whole_numbers(gen, 3000, width, t, 9)
+    for r in (None, res):
+        want = ((d_y.double() @ w.double()) * (below > 0) + (0 if r is None else r.double())).to(t)
+        into = whole_numbers(gen, 3000, width, t).copy_(below)
+        ctx.linear_backward_into(d_y, None, w, d_x=into, below=into, below_activation="relu", residual=r)
+        ctx.check_status()
+        assert torch.equal(into, want)
