@@ -568,7 +568,7 @@ int ps_attention_backward(ps_ctx* ctx, const ps_attention_shape* shape, const ps
  * normalised branch.  d_weight and d_bias, of type grad_dtype, are computed where they are not null, in an order that
  * depends on the sizes, and on whether there is a residual, alone; with accumulate they are added to what is there (rounded once).  A row's results depend on
  * that row alone.  y may be x; d_x may be d_y, x or residual (same pointer and stride); any other overlap with what is still read
- * is refused.  The mean is right to its last place or two, also where it is far larger than the distances from it.
+ * is refused.  The mean is off by the roundings of a sum in 32 bits, and by its last place or two alone where it is far larger than the distances from it.
  * d_work: ps_layer_norm_backward_bytes, used like ps_embed_backward's (0 without d_weight and d_bias). */
 typedef struct {
   void* data;                      /* a matrix [rows][cols] whose columns are contiguous  */

@@ -222,3 +222,61 @@ def test_input_gradient_in_place_of_the_values_below(ctx, dtype, width):
         ctx.linear_backward_into(d_y, None, w, d_x=into, below=into, below_activation="relu", residual=r)
         ctx.check_status()
         assert torch.equal(into, want)
+
+
+def test_rows_far_apart(ctx):
+    """Offsets past 32 bits: rows, heads and sequences whose distance is above 2^31 elements give the bits of contiguous ones."""
+    t, gen = torch.bfloat16, torch.Generator("cuda").manual_seed(9)
+    rows, apart = 4, (1 << 31) + 16
+    whole = torch.empty((rows - 1) * apart + (1 << 16), dtype=t, device="cuda")
+    taken = [0]
+
+    def far(like):
+        """The matrix with its rows far apart, beside those that have been placed so."""
+        begin = taken[0]
+        taken[0] += (like.shape[1] + 7) // 8 * 8
+        return whole.as_strided(like.shape, (apart, 1), begin).copy_(like)
+    for cols in (100, 1000, 12000):
+        taken[0] = 0
+        x, d_y, res = (normal(gen, rows, cols, dtype=t) for _ in range(3))
+        weight = normal(gen, cols, dtype=t)
+        y, mean, rstd = ctx.layer_norm_forward(x, weight)
+        grads = ctx.layer_norm_backward(d_y, x, mean, rstd, weight, res)
+        x, d_y, res, into = far(x), far(d_y), far(res), far(torch.zeros_like(x))
+        ctx.layer_norm_forward_into(x, into, weight)
+        assert torch.equal(into, y)
+        got = [torch.empty_like(g) for g in grads[1:]]
+        ctx.layer_norm_backward_into(d_y, x, mean, rstd, into, weight, res, *got)
+        assert torch.equal(into, grads[0]) and all(torch.equal(a, b) for a, b in zip(got, grads[1:]))
+    for inputs, outputs in ((72, 136), (75, 133)):
+        taken[0] = 0
+        x, w, d_y, pre, res = (whole_numbers(gen, *s, t) for s in ((rows, inputs), (rows, inputs), (rows, rows), (rows, outputs), (rows, outputs)))
+        wide = whole_numbers(gen, outputs, inputs, t)
+        d_out = whole_numbers(gen, rows, outputs, t)
+        want, kept = ctx.linear_forward(x, wide, residual=res, activation="relu", keep=True)
+        d_x, d_w, _ = ctx.linear_backward(d_out, x, wide, pre, "relu", residual=x)
+        few = ctx.linear_forward(x, w)
+        few_grads = ctx.linear_backward(d_y, x, w, dtype=torch.float32)
+        y, p, r = far(want), far(kept), far(res)
+        y.zero_(), p.zero_()
+        x_far, w_far = far(x), far(w)
+        ctx.linear_forward_into(x_far, wide, y, residual=r, activation="relu", pre=p)
+        assert torch.equal(y, want) and torch.equal(p, kept)
+        into = far(torch.zeros_like(x))
+        got_w = torch.empty(outputs, (inputs + 7) // 8 * 8, device="cuda", dtype=t)[:, :inputs]
+        ctx.linear_backward_into(far(d_out), x_far, wide, into, got_w, pre=far(pre), activation="relu", residual=x_far)
+        assert torch.equal(into, d_x) and torch.equal(got_w, d_w)
+        assert torch.equal(ctx.linear_forward(x_far, w_far), few)
+        floats = whole.view(torch.float32).as_strided((rows, inputs), (apart // 2, 1), 1 << 14)
+        ctx.linear_backward_into(d_y, x_far, w_far, d_weight=floats)
+        assert torch.equal(floats, few_grads[1])
+    q = normal(gen, rows, 5, 3, 64, dtype=t)
+    want = ctx.rotary(q)
+    for order in ((0, 1, 2, 3), (1, 0, 2, 3), (2, 1, 0, 3)):           # which of sequences, tokens and heads are far apart
+        shape = [q.shape[i] for i in order]
+        place = whole.as_strided([min(shape[0], rows)] + shape[1:], (apart, shape[2] * 64, 64, 1), 0).permute(*order)
+        part = tuple(slice(0, n) for n in place.shape)
+        place.copy_(q[part])
+        ctx.rotary_into(place, place)
+        assert torch.equal(place, want[part])
+    ctx.check_status()
